@@ -337,6 +337,148 @@ UMEM_API umem_status umem_key_norm(int32_t heads, int32_t n, int32_t dk, const f
                           const float* gamma, const float* beta, float eps, float* out,
                           hipStream_t stream);
 
+/* The norms before and after a block of the model around the layer, with the block's gate and the
+ * scale of the residual sum (Pre-LN placement; Trick 2's LayerNorm, or RMS):
+ *   entry   n  = Norm_in(h)                         what the block (umem_query) reads
+ *   exit    h' = res_scale h + out_scale act(gate) * Norm_out(y)       y: what the block returned
+ *   Norm(x) = x^ gamma + beta per row of d elements, x^ = (x - mean) / sqrt(var + eps) (LAYER,
+ *   population variance) or x / sqrt(mean x^2 + eps) (RMS), or x itself (NONE; exit only). */
+enum { UMEM_NORM_LAYER = 0, UMEM_NORM_RMS = 1, UMEM_NORM_NONE = 2 };
+enum { UMEM_GATE_NONE = 0, UMEM_GATE_CHANNEL = 1, UMEM_GATE_TOKEN = 2, UMEM_GATE_FULL = 3 };
+enum { UMEM_ACT_LINEAR = 0, UMEM_ACT_SIGMOID = 1 };
+typedef struct umem_block_desc {
+  int32_t d;         /* width of the residual stream */
+  int32_t norm_in;   /* the entry's norm: UMEM_NORM_LAYER or _RMS */
+  int32_t norm_out;  /* the exit's norm: UMEM_NORM_LAYER, _RMS or _NONE */
+  int32_t gate;      /* UMEM_GATE_NONE; _CHANNEL fp32 [d]; _TOKEN fp32 [T]; _FULL ytype [T, d] */
+  int32_t gate_act;  /* UMEM_ACT_LINEAR (the gate as given) or UMEM_ACT_SIGMOID */
+  int32_t htype;     /* UMEM_F32 or UMEM_BF16: the residual stream and its gradients */
+  int32_t ytype;     /* the block's side: n, y, a full gate, and their gradients */
+  float eps;         /* finite, >= 0 (at 0 a row without spread gives NaN, as 0 / 0) */
+  float res_scale;   /* finite; the residual stream's factor */
+  float out_scale;   /* finite; the gated output's factor */
+} umem_block_desc;
+/* Requirements (UMEM_ERR_INVALID_ARG otherwise): d >= 1, the enumerations as listed.
+ * Limits (UMEM_ERR_UNSUPPORTED beyond them): d <= 16384; T <= 2^20.
+ * Arrays [T, d] are dense; every array is aligned to its elements (rows of a multiple of 4
+ * elements in arrays aligned to 4 elements are moved in pieces of four).  Arithmetic and statistics
+ * are fp32; a bf16 result is rounded once, to nearest even.  Every row is computed from its own
+ * elements alone, so NaN and infinities of one token stay in its row (the sums over tokens of the
+ * backward take them in). */
+
+/* n [T, d] of ytype = Norm_in(h), h [T, d] of htype, gamma fp32 [d], beta fp32 [d] or NULL (zeros).
+ * n may equal h where the types are the same. */
+UMEM_API umem_status umem_block_in(const umem_block_desc* bd, int32_t T, const void* h, const float* gamma,
+                          const float* beta, void* n, hipStream_t stream);
+
+/* h_out [T, d] of htype = res_scale h + out_scale act(gate) * Norm_out(y); with n_next also the next
+ * block's entry in the same pass, n_next [T, d] of ytype = Norm_in(h_out) of the stream as stored.
+ *   h, y         [T, d] of htype and ytype
+ *   gate         as the descriptor says; NULL iff UMEM_GATE_NONE
+ *   gamma, beta  fp32 [d] of Norm_out: gamma NULL iff UMEM_NORM_NONE; beta optional, NULL with it
+ *   gamma_next, beta_next, n_next  all of the next entry (beta_next optional), or all NULL
+ *   h_out may equal h, n_next may equal y; else outputs overlap neither inputs nor each other. */
+UMEM_API umem_status umem_block_out(const umem_block_desc* bd, int32_t T, const void* h, const void* y,
+                           const void* gate, const float* gamma, const float* beta, void* h_out,
+                           const float* gamma_next, const float* beta_next, void* n_next,
+                           hipStream_t stream);
+
+/* Scratch bytes that the two backward calls need for T tokens. */
+UMEM_API umem_status umem_block_backward_workspace_size(const umem_block_desc* bd, int32_t T, size_t* bytes);
+
+/* Backward of umem_block_in, with the gradient that the stream has from past the block added:
+ *   dh = dres + J^T dn,  dgamma[j] = sum_t dn[t, j] x^[t, j],  dbeta[j] = sum_t dn[t, j]
+ *   h, gamma  as for the forward (the statistics are recomputed from h)
+ *   dn        [T, d] of ytype: the gradient of n
+ *   dres      [T, d] of htype, or NULL for zeros
+ *   dh        [T, d] of htype (written; may equal h or dres)
+ *   dgamma    fp32 [d]; dbeta fp32 [d], or NULL (no shift)
+ *   accumulate  0: dgamma and dbeta are written; 1: added to
+ *   ws        16-byte aligned scratch of umem_block_backward_workspace_size bytes
+ * The sums over tokens run in a fixed order.  With T == 0 and accumulate == 0 nothing is written. */
+UMEM_API umem_status umem_block_in_backward(const umem_block_desc* bd, int32_t T, const void* h,
+                                   const float* gamma, const void* dn, const void* dres, void* dh,
+                                   float* dgamma, float* dbeta, int32_t accumulate, void* ws,
+                                   size_t ws_bytes, hipStream_t stream);
+
+/* Backward of umem_block_out from dh_out, the whole gradient of h_out (where n_next was taken, that is
+ * the dh of umem_block_in_backward of the next entry):
+ *   dh = res_scale dh_out;  with dm = out_scale dh_out: dgate = dm Norm_out(y) act'(gate), summed over
+ *   tokens for a channel gate and over channels for a token gate;  dy = J^T (act(gate) dm), dgamma and
+ *   dbeta as above
+ *   y, gate, gamma, beta  as for the forward
+ *   dh_out  [T, d] of htype;  dh [T, d] of htype, or NULL (not wanted; may equal dh_out)
+ *   dy      [T, d] of ytype (may equal y)
+ *   dgate   like gate (NULL iff no gate; a full gate's may equal gate)
+ *   dgamma  fp32 [d], NULL iff UMEM_NORM_NONE;  dbeta fp32 [d], given iff beta is
+ *   accumulate  0: dgamma, dbeta and a channel gate's dgate are written; 1: added to (the gradients of
+ *           a token or full gate are written in any case) */
+UMEM_API umem_status umem_block_out_backward(const umem_block_desc* bd, int32_t T, const void* y, const void* gate,
+                                    const float* gamma, const float* beta, const void* dh_out, void* dh,
+                                    void* dy, void* dgate, float* dgamma, float* dbeta,
+                                    int32_t accumulate, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* One gradient of a training step. */
+typedef struct umem_grad {
+  const void* grad;      /* [rows, row_len] of dtype, device memory, aligned to its elements */
+  void* out;             /* where umem_grad_clip writes it: equal to grad, or memory apart */
+  const int32_t* n_rows; /* device memory: only the first *n_rows rows count (the n_rows of
+                          * umem_gather_backward_rows; at most `rows` are read), or NULL: all rows */
+  int64_t rows, row_len;
+  int64_t dtype;         /* UMEM_F32 or UMEM_BF16 */
+} umem_grad;
+
+/* Scratch bytes umem_grad_norm needs for n gradients.  `grads` is HOST memory, here and below: it is
+ * read before the call returns.  n <= 2048 (UMEM_ERR_UNSUPPORTED beyond), rows * row_len <= 2^40. */
+UMEM_API umem_status umem_grad_workspace_size(int32_t n, const umem_grad* grads, size_t* bytes);
+
+/* The global norm of n gradients: *sumsq = sum over all of them of g^2, *norm = sqrt(*sumsq).
+ *   norm   fp32 [1], device memory
+ *   sumsq  fp64 [1], device memory, or NULL: the sum of squares, to be added over the ranks of a
+ *          sharded model before the square root
+ *   ws     16-byte aligned scratch of umem_grad_workspace_size bytes
+ * Squares and sums are fp64 (a square neither overflows nor vanishes), added in an order that the sizes
+ * alone fix.  NaN and infinities go through to the norm.  n == 0 gives a norm of 0. */
+UMEM_API umem_status umem_grad_norm(int32_t n, const umem_grad* grads, float* norm, double* sumsq, void* ws,
+                           size_t ws_bytes, hipStream_t stream);
+
+/* Clipping to a global norm: out = g c, c = 1 where *norm <= max_norm, else max_norm / *norm (a NaN norm
+ * makes every element NaN; an infinite one makes finite elements 0).  A bf16 product is rounded
+ * once.  norm fp32 [1] on the device, as umem_grad_norm writes it; max_norm >= 0, +inf for none.
+ * Rows from *n_rows on are left as they are.  An out that overlaps another gradient or out, or its own
+ * gradient without being equal to it, is UMEM_ERR_INVALID_ARG. */
+UMEM_API umem_status umem_grad_clip(int32_t n, const umem_grad* grads, float max_norm, const float* norm,
+                           hipStream_t stream);
+
+/* Low-rank adapters of many requests beside a shared projection (umem_project, umem_query's linear):
+ *   out[t] = base[t] + scale[i] B_i (A_i x[t]),  i = ids[t];  out[t] = base[t] where i is not in [0, n) */
+typedef struct umem_adapter_desc {
+  int32_t n;      /* adapters */
+  int32_t rank;   /* their rank (smaller ones padded with zeros) */
+  int32_t d_in, d_out;
+  int32_t xtype;  /* UMEM_F32 or UMEM_BF16: x */
+  int32_t otype;  /* base and out */
+} umem_adapter_desc;
+/* Requirements (UMEM_ERR_INVALID_ARG otherwise): every count >= 1.
+ * Limits (UMEM_ERR_UNSUPPORTED beyond them): rank, d_in and d_out multiples of 8; rank <= 128; d_in
+ * and d_out <= 2^16; T <= 2^20. */
+
+/* Scratch bytes umem_adapter_add needs for T tokens. */
+UMEM_API umem_status umem_adapter_workspace_size(const umem_adapter_desc* ad, int32_t T, size_t* bytes);
+
+/*   x      [T, d_in] of xtype;  ids int32 [T]: each token's adapter, -1 for none
+ *   a      bf16 bits [n, rank, d_in];  b bf16 bits [n, d_out, rank] (output-major, as a linear
+ *          layer's weight);  scale fp32 [n], or NULL for ones
+ *   base   [T, d_out] of otype, or NULL for zeros;  out [T, d_out] of otype (may equal base)
+ *   ws     256-byte aligned scratch of umem_adapter_workspace_size bytes (NULL if 0)
+ * x, a, b, base and out are 16-byte aligned (UMEM_ERR_INVALID_ARG otherwise).  fp32 x and A_i x are not
+ * rounded: they enter the matrix cores as sums of bf16 parts; accumulation is fp32 and a bf16 out is
+ * rounded once.  The result does not depend on timing. */
+UMEM_API umem_status umem_adapter_add(const umem_adapter_desc* ad, int32_t T, const void* x, const int32_t* ids,
+                             const uint16_t* a, const uint16_t* b, const float* scale,
+                             const void* base, void* out, void* ws, size_t ws_bytes,
+                             hipStream_t stream);
+
 /* A static, human-readable name of a status code. */
 UMEM_API const char* umem_status_string(umem_status status);
 

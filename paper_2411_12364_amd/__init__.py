@@ -31,13 +31,20 @@ UMEM_STATIC_SCRATCH_BYTES = 64 << 20
 UMEM_F32, UMEM_BF16 = 0, 1
 UMEM_GRID_ADD, UMEM_GRID_TUCKER = 0, 1
 UMEM_W_RAW, UMEM_W_SOFTMAX = 0, 1
+UMEM_NORM_LAYER, UMEM_NORM_RMS, UMEM_NORM_NONE = 0, 1, 2
+UMEM_GATE_NONE, UMEM_GATE_CHANNEL, UMEM_GATE_TOKEN, UMEM_GATE_FULL = 0, 1, 2, 3
+UMEM_ACT_LINEAR, UMEM_ACT_SIGMOID = 0, 1
 
 EXPORTED = ("umem_workspace_size", "umem_axis_scores", "umem_select", "umem_score_topk",
             "umem_gather_sum", "umem_project_workspace_size", "umem_project", "umem_forward",
             "umem_forward_noalloc",
             "umem_query_workspace_size", "umem_query", "umem_key_norm",
             "umem_gather_backward_workspace_size", "umem_gather_backward", "umem_gather_backward_rows",
-            "umem_score_backward_workspace_size", "umem_score_backward", "umem_status_string")
+            "umem_score_backward_workspace_size", "umem_score_backward",
+            "umem_block_in", "umem_block_out", "umem_block_backward_workspace_size",
+            "umem_block_in_backward", "umem_block_out_backward",
+            "umem_grad_workspace_size", "umem_grad_norm", "umem_grad_clip",
+            "umem_adapter_workspace_size", "umem_adapter_add", "umem_status_string")
 
 
 class umem_desc(ctypes.Structure):
@@ -57,6 +64,29 @@ class umem_query_desc(ctypes.Structure):
     ]
 
 
+class umem_block_desc(ctypes.Structure):
+    _fields_ = [
+        ("d", ctypes.c_int32), ("norm_in", ctypes.c_int32), ("norm_out", ctypes.c_int32),
+        ("gate", ctypes.c_int32), ("gate_act", ctypes.c_int32), ("htype", ctypes.c_int32),
+        ("ytype", ctypes.c_int32), ("eps", ctypes.c_float), ("res_scale", ctypes.c_float),
+        ("out_scale", ctypes.c_float),
+    ]
+
+
+class umem_grad(ctypes.Structure):
+    _fields_ = [
+        ("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n_rows", ctypes.c_void_p),
+        ("rows", ctypes.c_int64), ("row_len", ctypes.c_int64), ("dtype", ctypes.c_int64),
+    ]
+
+
+class umem_adapter_desc(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int32), ("rank", ctypes.c_int32), ("d_in", ctypes.c_int32),
+        ("d_out", ctypes.c_int32), ("xtype", ctypes.c_int32), ("otype", ctypes.c_int32),
+    ]
+
+
 class UmemError(RuntimeError):
     def __init__(self, status: int, what: str = ""):
         self.status = status
@@ -68,6 +98,8 @@ def _load() -> ctypes.CDLL:
         raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build() first")
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    F32 = ctypes.c_float
+    BD, AD = ctypes.POINTER(umem_block_desc), ctypes.POINTER(umem_adapter_desc)
     D = ctypes.POINTER(umem_desc)
     sig = {
         "umem_workspace_size": [D, I32, ctypes.POINTER(SZ)],
@@ -88,6 +120,16 @@ def _load() -> ctypes.CDLL:
                                       SZ, P],
         "umem_score_backward_workspace_size": [D, I32, ctypes.POINTER(SZ)],
         "umem_score_backward": [D, I32, P, P, P, P, P, P, P, P, P, P, P, P, P, P, SZ, P],
+        "umem_block_in": [BD, I32, P, P, P, P, P],
+        "umem_block_out": [BD, I32, P, P, P, P, P, P, P, P, P, P],
+        "umem_block_backward_workspace_size": [BD, I32, ctypes.POINTER(SZ)],
+        "umem_block_in_backward": [BD, I32, P, P, P, P, P, P, P, I32, P, SZ, P],
+        "umem_block_out_backward": [BD, I32, P, P, P, P, P, P, P, P, P, P, I32, P, SZ, P],
+        "umem_grad_workspace_size": [I32, P, ctypes.POINTER(SZ)],
+        "umem_grad_norm": [I32, P, P, P, P, SZ, P],
+        "umem_grad_clip": [I32, P, F32, P, P],
+        "umem_adapter_workspace_size": [AD, I32, ctypes.POINTER(SZ)],
+        "umem_adapter_add": [AD, I32, P, P, P, P, P, P, P, P, SZ, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -245,3 +287,75 @@ def umem_score_backward(desc, T, q_row, q_col, k_row, k_col, core, idx, w, dw, d
     return _lib.umem_score_backward(_d(desc), T, _p(q_row), _p(q_col), _p(k_row), _p(k_col),
                                     _p(core), _p(idx), _p(w), _p(dw), _p(dq_row), _p(dq_col),
                                     _p(dk_row), _p(dk_col), _p(dcore), _p(ws), ws_bytes, _s(stream))
+
+
+def umem_block_in(bd, T, h, gamma, beta, n, stream=None) -> int:
+    return _lib.umem_block_in(_d(bd), T, _p(h), _p(gamma), _p(beta), _p(n), _s(stream))
+
+
+def umem_block_out(bd, T, h, y, gate, gamma, beta, h_out, gamma_next=None, beta_next=None,
+                   n_next=None, stream=None) -> int:
+    return _lib.umem_block_out(_d(bd), T, _p(h), _p(y), _p(gate), _p(gamma), _p(beta), _p(h_out),
+                               _p(gamma_next), _p(beta_next), _p(n_next), _s(stream))
+
+
+def umem_block_backward_workspace_size(bd, T):
+    """Returns (status, bytes)."""
+    out = ctypes.c_size_t(0)
+    st = _lib.umem_block_backward_workspace_size(_d(bd), T, ctypes.byref(out))
+    return st, out.value
+
+
+def umem_block_in_backward(bd, T, h, gamma, dn, dres, dh, dgamma, dbeta, accumulate, ws, ws_bytes,
+                           stream=None) -> int:
+    return _lib.umem_block_in_backward(_d(bd), T, _p(h), _p(gamma), _p(dn), _p(dres), _p(dh),
+                                       _p(dgamma), _p(dbeta), accumulate, _p(ws), ws_bytes, _s(stream))
+
+
+def umem_block_out_backward(bd, T, y, gate, gamma, beta, dh_out, dh, dy, dgate, dgamma, dbeta,
+                            accumulate, ws, ws_bytes, stream=None) -> int:
+    return _lib.umem_block_out_backward(_d(bd), T, _p(y), _p(gate), _p(gamma), _p(beta), _p(dh_out),
+                                        _p(dh), _p(dy), _p(dgate), _p(dgamma), _p(dbeta), accumulate,
+                                        _p(ws), ws_bytes, _s(stream))
+
+
+def _table(n, grads):
+    """The host address of n gradients: an array ``(umem_grad * n)``, or a C-ordered int64 numpy array
+    [n, 6] with a row of the struct's six fields for each."""
+    if isinstance(grads, ctypes.Array):
+        if grads._type_ is not umem_grad or len(grads) < n:
+            raise ValueError("grads: an array of at least n umem_grad")
+        return ctypes.addressof(grads)
+    if grads is None:
+        return None
+    if grads.dtype != "int64" or grads.ndim != 2 or grads.shape[1] != 6 or grads.shape[0] < n or \
+            not grads.flags.c_contiguous:
+        raise ValueError("grads: int64 [n, 6], C-ordered")
+    return grads.ctypes.data
+
+
+def umem_grad_workspace_size(n, grads):
+    """Returns (status, bytes)."""
+    out = ctypes.c_size_t(0)
+    st = _lib.umem_grad_workspace_size(n, _table(n, grads), ctypes.byref(out))
+    return st, out.value
+
+
+def umem_grad_norm(n, grads, norm, sumsq, ws, ws_bytes, stream=None) -> int:
+    return _lib.umem_grad_norm(n, _table(n, grads), _p(norm), _p(sumsq), _p(ws), ws_bytes, _s(stream))
+
+
+def umem_grad_clip(n, grads, max_norm, norm, stream=None) -> int:
+    return _lib.umem_grad_clip(n, _table(n, grads), max_norm, _p(norm), _s(stream))
+
+
+def umem_adapter_workspace_size(ad, T):
+    """Returns (status, bytes)."""
+    out = ctypes.c_size_t(0)
+    st = _lib.umem_adapter_workspace_size(_d(ad), T, ctypes.byref(out))
+    return st, out.value
+
+
+def umem_adapter_add(ad, T, x, ids, a, b, scale, base, out, ws=None, ws_bytes=0, stream=None) -> int:
+    return _lib.umem_adapter_add(_d(ad), T, _p(x), _p(ids), _p(a), _p(b), _p(scale), _p(base), _p(out),
+                                 _p(ws), ws_bytes, _s(stream))

@@ -464,6 +464,308 @@ UMEM_API umem_status umem_score_backward(const umem_desc* desc, int32_t T, const
 
 namespace {
 
+bool finite(float x) { return x - x == 0.0f; }
+
+size_t esize(int32_t dtype) { return dtype == UMEM_BF16 ? 2 : 4; }
+
+bool known_type(int64_t dtype) { return dtype == UMEM_F32 || dtype == UMEM_BF16; }
+
+// An array of a call, for the checks that outputs lie apart from what the kernels read meanwhile.
+struct Span {
+  const void* p;
+  size_t bytes;
+};
+
+bool apart(const Span& a, const Span& b) {
+  if (a.p == nullptr || b.p == nullptr || a.bytes == 0 || b.bytes == 0) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x + a.bytes <= y || y + b.bytes <= x;
+}
+
+// Whether `out` is apart from the n arrays in[], or is in[same] itself.
+bool out_fits(const Span& out, const Span* in, int n, int same = -1) {
+  for (int i = 0; i < n; ++i)
+    if (!apart(out, in[i]) && !(i == same && out.p == in[i].p && out.bytes == in[i].bytes)) return false;
+  return true;
+}
+
+umem_status check_block_desc(const umem_block_desc* bd) {
+  if (bd == nullptr || bd->d < 1) return UMEM_ERR_INVALID_ARG;
+  if (bd->norm_in != UMEM_NORM_LAYER && bd->norm_in != UMEM_NORM_RMS) return UMEM_ERR_INVALID_ARG;
+  if (bd->norm_out < UMEM_NORM_LAYER || bd->norm_out > UMEM_NORM_NONE) return UMEM_ERR_INVALID_ARG;
+  if (bd->gate < UMEM_GATE_NONE || bd->gate > UMEM_GATE_FULL) return UMEM_ERR_INVALID_ARG;
+  if (bd->gate_act != UMEM_ACT_LINEAR && bd->gate_act != UMEM_ACT_SIGMOID) return UMEM_ERR_INVALID_ARG;
+  if (!known_type(bd->htype) || !known_type(bd->ytype)) return UMEM_ERR_INVALID_ARG;
+  if (!finite(bd->eps) || bd->eps < 0.0f || !finite(bd->res_scale) || !finite(bd->out_scale))
+    return UMEM_ERR_INVALID_ARG;
+  if (bd->d > kMaxBlockWidth) return UMEM_ERR_UNSUPPORTED;
+  return UMEM_OK;
+}
+
+// The arrays of a block call: [T, d] of the stream's or the block's type, fp32 [d], the gate.
+struct BlockSpans {
+  size_t h, y, row, gate;
+  int32_t gate_type;
+  BlockSpans(const umem_block_desc& bd, int32_t T) {
+    const size_t n = static_cast<size_t>(T) * bd.d;
+    h = n * esize(bd.htype);
+    y = n * esize(bd.ytype);
+    row = static_cast<size_t>(bd.d) * 4;
+    gate_type = bd.gate == UMEM_GATE_FULL ? bd.ytype : UMEM_F32;
+    gate = bd.gate == UMEM_GATE_FULL ? y : bd.gate == UMEM_GATE_TOKEN ? static_cast<size_t>(T) * 4 : row;
+  }
+};
+
+umem_status check_block_ws(const umem_block_desc& bd, int32_t T, const void* ws, size_t ws_bytes) {
+  if (ws == nullptr || !aligned(ws, 16) || ws_bytes < block_backward_workspace_bytes(bd, T)) return UMEM_ERR_WORKSPACE;
+  return UMEM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+UMEM_API umem_status umem_block_in(const umem_block_desc* bd, int32_t T, const void* h, const float* gamma,
+                                   const float* beta, void* n, hipStream_t stream) {
+  umem_status st = check_block_desc(bd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK || T == 0) return st;
+  if (!h || !gamma || !n) return UMEM_ERR_INVALID_ARG;
+  const BlockSpans z(*bd, T);
+  if (!aligned(h, esize(bd->htype)) || !aligned(n, esize(bd->ytype)) || !aligned(gamma, 4) || !aligned(beta, 4))
+    return UMEM_ERR_INVALID_ARG;
+  const Span in[] = {{h, z.h}, {gamma, z.row}, {beta, z.row}};
+  if (!out_fits({n, z.y}, in, 3, 0)) return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_block_in(*bd, T, h, gamma, beta, n, stream));
+}
+
+UMEM_API umem_status umem_block_out(const umem_block_desc* bd, int32_t T, const void* h, const void* y,
+                                    const void* gate, const float* gamma, const float* beta, void* h_out,
+                                    const float* gamma_next, const float* beta_next, void* n_next,
+                                    hipStream_t stream) {
+  umem_status st = check_block_desc(bd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK || T == 0) return st;
+  if (!h || !y || !h_out) return UMEM_ERR_INVALID_ARG;
+  if ((gate != nullptr) != (bd->gate != UMEM_GATE_NONE)) return UMEM_ERR_INVALID_ARG;
+  if ((gamma != nullptr) != (bd->norm_out != UMEM_NORM_NONE) || (beta && !gamma)) return UMEM_ERR_INVALID_ARG;
+  if ((gamma_next != nullptr) != (n_next != nullptr) || (beta_next && !n_next)) return UMEM_ERR_INVALID_ARG;
+  const BlockSpans z(*bd, T);
+  if (!aligned(h, esize(bd->htype)) || !aligned(h_out, esize(bd->htype)) || !aligned(y, esize(bd->ytype)) ||
+      !aligned(n_next, esize(bd->ytype)) || !aligned(gate, esize(z.gate_type)) || !aligned(gamma, 4) ||
+      !aligned(beta, 4) || !aligned(gamma_next, 4) || !aligned(beta_next, 4))
+    return UMEM_ERR_INVALID_ARG;
+  const Span in[] = {{h, z.h},       {y, z.y},           {gate, z.gate},      {gamma, z.row},
+                     {beta, z.row}, {gamma_next, z.row}, {beta_next, z.row}};
+  if (!out_fits({h_out, z.h}, in, 7, 0) || !out_fits({n_next, z.y}, in, 7, 1) || !apart({h_out, z.h}, {n_next, z.y}))
+    return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_block_out(*bd, T, h, y, gate, gamma, beta, h_out, gamma_next, beta_next, n_next, stream));
+}
+
+UMEM_API umem_status umem_block_backward_workspace_size(const umem_block_desc* bd, int32_t T, size_t* bytes) {
+  if (bytes == nullptr) return UMEM_ERR_INVALID_ARG;
+  *bytes = 0;
+  umem_status st = check_block_desc(bd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK) return st;
+  *bytes = block_backward_workspace_bytes(*bd, T);
+  return UMEM_OK;
+}
+
+UMEM_API umem_status umem_block_in_backward(const umem_block_desc* bd, int32_t T, const void* h, const float* gamma,
+                                            const void* dn, const void* dres, void* dh, float* dgamma,
+                                            float* dbeta, int32_t accumulate, void* ws, size_t ws_bytes,
+                                            hipStream_t stream) {
+  umem_status st = check_block_desc(bd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK) return st;
+  if (accumulate != 0 && accumulate != 1) return UMEM_ERR_INVALID_ARG;
+  if (T == 0) return UMEM_OK;
+  if (!h || !gamma || !dn || !dh || !dgamma) return UMEM_ERR_INVALID_ARG;
+  const size_t hs = esize(bd->htype);
+  if (!aligned(h, hs) || !aligned(dres, hs) || !aligned(dh, hs) || !aligned(dn, esize(bd->ytype)) ||
+      !aligned(gamma, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4))
+    return UMEM_ERR_INVALID_ARG;
+  st = check_block_ws(*bd, T, ws, ws_bytes);
+  if (st != UMEM_OK) return st;
+  const BlockSpans z(*bd, T);
+  const Span in[] = {{h, z.h}, {dres, z.h}, {dn, z.y}, {gamma, z.row},
+                     {ws, block_backward_workspace_bytes(*bd, T)}};
+  const Span dx{dh, z.h}, dg{dgamma, z.row}, db{dbeta, z.row};
+  if ((!out_fits(dx, in, 5, 0) && !out_fits(dx, in, 5, 1)) || !out_fits(dg, in, 5) || !out_fits(db, in, 5) ||
+      !apart(dx, dg) || !apart(dx, db) || !apart(dg, db))
+    return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_block_in_backward(*bd, T, h, gamma, dn, dres, dh, dgamma, dbeta, accumulate != 0, ws,
+                                             stream));
+}
+
+UMEM_API umem_status umem_block_out_backward(const umem_block_desc* bd, int32_t T, const void* y, const void* gate,
+                                             const float* gamma, const float* beta, const void* dh_out, void* dh,
+                                             void* dy, void* dgate, float* dgamma, float* dbeta,
+                                             int32_t accumulate, void* ws, size_t ws_bytes, hipStream_t stream) {
+  umem_status st = check_block_desc(bd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK) return st;
+  if (accumulate != 0 && accumulate != 1) return UMEM_ERR_INVALID_ARG;
+  if (T == 0) return UMEM_OK;
+  if (!y || !dh_out || !dy) return UMEM_ERR_INVALID_ARG;
+  const bool gated = bd->gate != UMEM_GATE_NONE, normed = bd->norm_out != UMEM_NORM_NONE;
+  if ((gate != nullptr) != gated || (dgate != nullptr) != gated) return UMEM_ERR_INVALID_ARG;
+  if ((gamma != nullptr) != normed || (dgamma != nullptr) != normed) return UMEM_ERR_INVALID_ARG;
+  if ((beta && !gamma) || (beta != nullptr) != (dbeta != nullptr)) return UMEM_ERR_INVALID_ARG;
+  const BlockSpans z(*bd, T);
+  const size_t hs = esize(bd->htype), ys = esize(bd->ytype), gs = esize(z.gate_type);
+  if (!aligned(y, ys) || !aligned(dy, ys) || !aligned(dh_out, hs) || !aligned(dh, hs) || !aligned(gate, gs) ||
+      !aligned(dgate, gs) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4))
+    return UMEM_ERR_INVALID_ARG;
+  st = check_block_ws(*bd, T, ws, ws_bytes);
+  if (st != UMEM_OK) return st;
+  const Span in[] = {{y, z.y},       {dh_out, z.h}, {gate, z.gate},
+                     {gamma, z.row}, {beta, z.row}, {ws, block_backward_workspace_bytes(*bd, T)}};
+  const Span out[] = {{dy, z.y}, {dh, z.h}, {dgate, z.gate}, {dgamma, z.row}, {dbeta, z.row}};
+  const int same[] = {0, 1, bd->gate == UMEM_GATE_FULL ? 2 : -1, -1, -1};
+  for (int i = 0; i < 5; ++i)
+    if (!out_fits(out[i], in, 6, same[i]) || !out_fits(out[i], out, i)) return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_block_out_backward(*bd, T, y, gate, gamma, beta, dh_out, dh, dy, dgate, dgamma, dbeta,
+                                              accumulate != 0, ws, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+// for_clip: the outs are written, so they are checked as well.
+umem_status check_grads(int32_t n, const umem_grad* grads, bool for_clip) {
+  if (n < 0 || (n > 0 && grads == nullptr)) return UMEM_ERR_INVALID_ARG;
+  if (n > kMaxGrads) return UMEM_ERR_UNSUPPORTED;
+  int64_t total = 0;
+  for (int i = 0; i < n; ++i) {
+    const umem_grad& g = grads[i];
+    if (g.rows < 0 || g.row_len < 0 || !known_type(g.dtype)) return UMEM_ERR_INVALID_ARG;
+    if (g.rows == 0 || g.row_len == 0) continue;
+    constexpr int64_t kMost = INT64_C(1) << 40;
+    if (g.rows > kMost / g.row_len) return UMEM_ERR_UNSUPPORTED;
+    total += g.rows * g.row_len;
+    if (total > kMost) return UMEM_ERR_UNSUPPORTED;
+    const size_t es = esize(static_cast<int32_t>(g.dtype));
+    if (g.grad == nullptr || !aligned(g.grad, es) || !aligned(g.n_rows, 4)) return UMEM_ERR_INVALID_ARG;
+    if (for_clip && (g.out == nullptr || !aligned(g.out, es))) return UMEM_ERR_INVALID_ARG;
+  }
+  return UMEM_OK;
+}
+
+// Whether an out overlaps another gradient or out, or its own gradient other than being it: one pass
+// over all of them in the order of their addresses, with the furthest ends so far.
+bool grads_clash(int32_t n, const umem_grad* grads) {
+  struct Range {
+    uintptr_t from, to;
+    bool written;
+  };
+  static_assert(2 * kMaxGrads * sizeof(Range) <= 128 << 10, "the ranges live on the caller's stack");
+  Range r[2 * kMaxGrads];
+  int m = 0;
+  for (int i = 0; i < n; ++i) {
+    const umem_grad& g = grads[i];
+    const uintptr_t bytes = static_cast<uintptr_t>(g.rows) * g.row_len * esize(static_cast<int32_t>(g.dtype));
+    if (bytes == 0) continue;
+    const uintptr_t in = reinterpret_cast<uintptr_t>(g.grad), out = reinterpret_cast<uintptr_t>(g.out);
+    r[m++] = {out, out + bytes, true};
+    if (in != out) r[m++] = {in, in + bytes, false};
+  }
+  std::sort(r, r + m, [](const Range& a, const Range& b) { return a.from < b.from; });
+  uintptr_t any = 0, written = 0;
+  for (int i = 0; i < m; ++i) {
+    if (r[i].from < (r[i].written ? any : written)) return true;
+    any = std::max(any, r[i].to);
+    if (r[i].written) written = std::max(written, r[i].to);
+  }
+  return false;
+}
+
+}  // namespace
+
+extern "C" {
+
+UMEM_API umem_status umem_grad_workspace_size(int32_t n, const umem_grad* grads, size_t* bytes) {
+  if (bytes == nullptr) return UMEM_ERR_INVALID_ARG;
+  *bytes = 0;
+  const umem_status st = check_grads(n, grads, false);
+  if (st != UMEM_OK) return st;
+  *bytes = grad_workspace_bytes(n, grads);
+  return UMEM_OK;
+}
+
+UMEM_API umem_status umem_grad_norm(int32_t n, const umem_grad* grads, float* norm, double* sumsq, void* ws,
+                                    size_t ws_bytes, hipStream_t stream) {
+  const umem_status st = check_grads(n, grads, false);
+  if (st != UMEM_OK) return st;
+  if (norm == nullptr || !aligned(norm, 4) || !aligned(sumsq, 8)) return UMEM_ERR_INVALID_ARG;
+  const size_t need = grad_workspace_bytes(n, grads);
+  if (need > 0 && (ws == nullptr || !aligned(ws, 16) || ws_bytes < need)) return UMEM_ERR_WORKSPACE;
+  return hip_status(launch_grad_norm(n, grads, norm, sumsq, ws, stream));
+}
+
+UMEM_API umem_status umem_grad_clip(int32_t n, const umem_grad* grads, float max_norm, const float* norm,
+                                    hipStream_t stream) {
+  const umem_status st = check_grads(n, grads, true);
+  if (st != UMEM_OK) return st;
+  if (!(max_norm >= 0.0f) || norm == nullptr || !aligned(norm, 4) || grads_clash(n, grads)) return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_grad_clip(n, grads, max_norm, norm, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+umem_status check_adapter_desc(const umem_adapter_desc* ad) {
+  if (ad == nullptr || ad->n < 1 || ad->rank < 1 || ad->d_in < 1 || ad->d_out < 1) return UMEM_ERR_INVALID_ARG;
+  if (!known_type(ad->xtype) || !known_type(ad->otype)) return UMEM_ERR_INVALID_ARG;
+  if (ad->rank % 8 != 0 || ad->d_in % 8 != 0 || ad->d_out % 8 != 0 || ad->rank > kMaxAdapterRank ||
+      ad->d_in > kMaxAdapterWidth || ad->d_out > kMaxAdapterWidth)
+    return UMEM_ERR_UNSUPPORTED;
+  return UMEM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+UMEM_API umem_status umem_adapter_workspace_size(const umem_adapter_desc* ad, int32_t T, size_t* bytes) {
+  if (bytes == nullptr) return UMEM_ERR_INVALID_ARG;
+  *bytes = 0;
+  umem_status st = check_adapter_desc(ad);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK) return st;
+  *bytes = adapter_workspace_bytes(*ad, T);
+  return UMEM_OK;
+}
+
+UMEM_API umem_status umem_adapter_add(const umem_adapter_desc* ad, int32_t T, const void* x, const int32_t* ids,
+                                      const uint16_t* a, const uint16_t* b, const float* scale, const void* base,
+                                      void* out, void* ws, size_t ws_bytes, hipStream_t stream) {
+  umem_status st = check_adapter_desc(ad);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK || T == 0) return st;
+  if (!x || !ids || !a || !b || !out) return UMEM_ERR_INVALID_ARG;
+  if (!aligned(x, 16) || !aligned(a, 16) || !aligned(b, 16) || !aligned(base, 16) || !aligned(out, 16) ||
+      !aligned(ids, 4) || !aligned(scale, 4))
+    return UMEM_ERR_INVALID_ARG;
+  const size_t need = adapter_workspace_bytes(*ad, T);
+  if (need > 0 && (ws == nullptr || !aligned(ws, kAlign) || ws_bytes < need)) return UMEM_ERR_WORKSPACE;
+  const size_t t = T, n = ad->n, r = ad->rank;
+  const Span y{out, t * ad->d_out * esize(ad->otype)};
+  const Span in[] = {{base, y.bytes},          {x, t * ad->d_in * esize(ad->xtype)},
+                     {ids, t * 4},             {a, n * r * ad->d_in * 2},
+                     {b, n * ad->d_out * r * 2}, {scale, n * 4},
+                     {ws, need}};
+  if (!out_fits(y, in, 7, 0)) return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_adapter_add(*ad, T, x, ids, a, b, scale, base, out, ws, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
 umem_status forward_into(const umem_desc* desc, int32_t T, const float* q_row, const float* q_col,
                          const float* k_row, const float* k_col, const float* core,
                          const void* values, const int32_t* perm, const uint16_t* w_proj,

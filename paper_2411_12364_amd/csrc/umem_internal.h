@@ -141,6 +141,36 @@ hipError_t launch_query(const umem_query_desc& qd, int B, int L, const float* x,
 hipError_t launch_key_norm(int heads, int n, int dk, const float* keys, const float* gamma,
                            const float* beta, float eps, float* out, hipStream_t s);
 
+// The norms before and after a block (block.hip).  ws: block_backward_workspace_bytes bytes.
+constexpr int kMaxBlockWidth = 16384;
+hipError_t launch_block_in(const umem_block_desc& bd, int T, const void* h, const float* gamma, const float* beta,
+                           void* n, hipStream_t s);
+hipError_t launch_block_out(const umem_block_desc& bd, int T, const void* h, const void* y, const void* gate,
+                            const float* gamma, const float* beta, void* h_out, const float* gamma_next,
+                            const float* beta_next, void* n_next, hipStream_t s);
+size_t block_backward_workspace_bytes(const umem_block_desc& bd, int T);
+hipError_t launch_block_in_backward(const umem_block_desc& bd, int T, const void* h, const float* gamma,
+                                    const void* dn, const void* dres, void* dh, float* dgamma, float* dbeta,
+                                    bool accumulate, void* ws, hipStream_t s);
+hipError_t launch_block_out_backward(const umem_block_desc& bd, int T, const void* y, const void* gate,
+                                     const float* gamma, const float* beta, const void* dh_out, void* dh, void* dy,
+                                     void* dgate, float* dgamma, float* dbeta, bool accumulate, void* ws,
+                                     hipStream_t s);
+
+// The global gradient norm and clipping (grad.hip).  ws: grad_workspace_bytes bytes.
+constexpr int kMaxGrads = 2048;
+size_t grad_workspace_bytes(int n, const umem_grad* grads);
+hipError_t launch_grad_norm(int n, const umem_grad* grads, float* norm, double* sumsq, void* ws, hipStream_t s);
+hipError_t launch_grad_clip(int n, const umem_grad* grads, float max_norm, const float* norm, hipStream_t s);
+
+// Low-rank adapters (adapter.hip).  ws: adapter_workspace_bytes bytes.
+constexpr int kMaxAdapterRank = 128;
+constexpr int kMaxAdapterWidth = 1 << 16;
+size_t adapter_workspace_bytes(const umem_adapter_desc& ad, int T);
+hipError_t launch_adapter_add(const umem_adapter_desc& ad, int T, const void* x, const int32_t* ids,
+                              const uint16_t* a, const uint16_t* b, const float* scale, const void* base,
+                              void* out, void* ws, hipStream_t s);
+
 // a8.  ws: project_workspace_bytes(...) bytes, 256-byte aligned (the intermediate and the
 // split-K partials); w_proj == nullptr is the output linear alone ([T, dv] by [dv, d_out]).
 size_t project_workspace_bytes(int T, int expand, int dv, int dv_virt, int d_out);

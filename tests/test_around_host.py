@@ -1,0 +1,210 @@
+"""Refusals of the block, gradient and adapter entry points, on the host: every call below fails
+validation, sizes a workspace or has nothing to do, so no kernel is launched."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import paper_2411_12364_amd as U
+
+OK, ARG, UNS, WS = U.UMEM_OK, U.UMEM_ERR_INVALID_ARG, U.UMEM_ERR_UNSUPPORTED, U.UMEM_ERR_WORKSPACE
+MB = 1 << 20
+
+
+def at(i):
+    """Addresses 64 MiB apart, never dereferenced."""
+    return (i + 1) * 64 * MB
+
+
+def bd(**kw):
+    base = dict(d=256, norm_in=0, norm_out=0, gate=0, gate_act=0, htype=0, ytype=0, eps=1e-5, res_scale=1.0,
+                out_scale=1.0)
+    return U.umem_block_desc(*{**base, **kw}.values())
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(), OK), (dict(d=0), ARG), (dict(d=16384), OK), (dict(d=16385), UNS), (dict(d=1), OK),
+    (dict(norm_in=2), ARG), (dict(norm_in=-1), ARG), (dict(norm_out=3), ARG), (dict(norm_out=2), OK),
+    (dict(gate=4), ARG), (dict(gate=-1), ARG), (dict(gate_act=2), ARG), (dict(htype=2), ARG), (dict(ytype=-1), ARG),
+    (dict(eps=-1e-9), ARG), (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG), (dict(eps=0.0), OK),
+    (dict(res_scale=float("inf")), ARG), (dict(out_scale=float("nan")), ARG),
+])
+def test_block_descriptor(kw, want):
+    st, n = U.umem_block_backward_workspace_size(bd(**kw), 8)
+    assert st == want and (n > 0) == (want == OK)
+    assert U.umem_block_in(bd(**kw), 0, None, None, None, None, 0) == want
+    assert U.umem_block_backward_workspace_size(bd(), -1)[0] == ARG
+    assert U.umem_block_backward_workspace_size(bd(), (1 << 20) + 1)[0] == UNS
+    assert U.umem_block_backward_workspace_size(bd(), 0) == (OK, 0)
+
+
+def test_block_in_refusals():
+    h, g, b, n = at(0), at(1), at(2), at(3)
+    call = lambda h=h, g=g, b=b, n=n, d=bd(), T=8: U.umem_block_in(d, T, h, g, b, n, 0)   # noqa: E731
+    assert call(h=None) == ARG and call(g=None) == ARG and call(n=None) == ARG
+    assert call(h=h + 2) == ARG and call(n=n + 1) == ARG and call(g=g + 2) == ARG and call(b=b + 3) == ARG
+    assert call(h=h + 1, d=bd(htype=1)) == ARG
+    assert call(n=h + 4) == ARG                                        # overlaps h without being it
+    assert call(n=h, d=bd(htype=1)) == ARG                             # ... in another type
+    assert call(n=g) == ARG
+    assert call(T=-1) == ARG and call(T=(1 << 20) + 1) == UNS
+
+
+def test_block_out_refusals():
+    names = ["h", "y", "gate", "gamma", "beta", "h_out", "gamma_next", "beta_next", "n_next"]
+    base = {k: at(i) for i, k in enumerate(names)}
+
+    def call(desc=bd(gate=1), T=8, **kw):
+        return U.umem_block_out(desc, T, *{**base, **kw}.values(), 0)
+
+    for k in ("h", "y", "h_out", "gate", "gamma"):
+        assert call(**{k: None}) == ARG, k
+    assert call(desc=bd(gate=0)) == ARG                                 # a gate that the descriptor lacks
+    assert call(desc=bd(gate=1, norm_out=2)) == ARG                     # gamma without a norm
+    assert call(desc=bd(gate=1, norm_out=2), gamma=None) == ARG         # beta without a norm
+    assert call(gamma_next=None) == ARG and call(n_next=None) == ARG    # half of the next entry
+    assert call(gamma_next=None, n_next=None) == ARG                    # its shift alone
+    for k in names:
+        assert call(**{k: base[k] + 1}) == ARG, k
+    assert call(h_out=base["y"]) == ARG and call(h_out=base["h"] + 256) == ARG
+    assert call(n_next=base["h"]) == ARG and call(n_next=base["h_out"]) == ARG
+    assert call(desc=bd(gate=3), h_out=base["gate"]) == ARG
+
+
+def test_block_backward_refusals():
+    st, need = U.umem_block_backward_workspace_size(bd(gate=1), 8)
+    assert st == OK
+    names = ["h", "gamma", "dn", "dres", "dh", "dgamma", "dbeta"]
+    base = {k: at(i) for i, k in enumerate(names)}
+    ws = at(20)
+
+    def call(T=8, acc=0, ws=ws, n=need, desc=bd(), **kw):
+        return U.umem_block_in_backward(desc, T, *{**base, **kw}.values(), acc, ws, n, 0)
+
+    for k in ("h", "gamma", "dn", "dh", "dgamma"):
+        assert call(**{k: None}) == ARG, k
+    for k in names:
+        assert call(**{k: base[k] + 2}) == ARG, k
+    assert call(acc=2) == ARG and call(acc=-1) == ARG and call(T=0, acc=2) == ARG and call(T=0) == OK
+    assert call(ws=None) == WS and call(ws=ws + 8) == WS and call(n=need - 1) == WS
+    assert call(dh=base["dn"]) == ARG and call(dgamma=base["dbeta"]) == ARG and call(dgamma=ws) == ARG
+    assert call(dh=base["h"] + 512) == ARG and call(dh=ws) == ARG
+
+    names = ["y", "gate", "gamma", "beta", "dh_out", "dh", "dy", "dgate", "dgamma", "dbeta"]
+    base = {k: at(i) for i, k in enumerate(names)}
+
+    def call(T=8, acc=0, ws=ws, n=need, desc=bd(gate=1), **kw):      # noqa: F811
+        return U.umem_block_out_backward(desc, T, *{**base, **kw}.values(), acc, ws, n, 0)
+
+    for k in ("y", "gate", "gamma", "dh_out", "dy", "dgate", "dgamma"):
+        assert call(**{k: None}) == ARG, k
+    assert call(beta=None) == ARG and call(dbeta=None) == ARG
+    assert call(desc=bd(gate=0)) == ARG and call(desc=bd(gate=1, norm_out=2)) == ARG
+    for k in names:
+        assert call(**{k: base[k] + 1}) == ARG, k
+    assert call(acc=3) == ARG and call(T=0) == OK
+    assert call(ws=None) == WS and call(ws=ws + 4) == WS and call(n=0) == WS
+    assert call(dy=base["dh_out"]) == ARG and call(dh=base["y"]) == ARG and call(dgate=base["gate"]) == ARG
+    assert call(dy=base["dh"]) == ARG and call(dgamma=base["gamma"]) == ARG and call(dbeta=ws + 16) == ARG
+
+
+def grads(*rows):
+    return (U.umem_grad * len(rows))(*[U.umem_grad(*r) for r in rows])
+
+
+def test_grad_refusals():
+    norm, ws = at(30), at(31)
+    good = grads((at(0), at(1), None, 4, 100, 0), (at(2), at(2), at(3), 7, 33, 1))
+    st, need = U.umem_grad_workspace_size(2, good)
+    assert st == OK and need > 0
+    assert U.umem_grad_workspace_size(0, None) == (OK, 0) and U.umem_grad_workspace_size(1, None)[0] == ARG
+    assert U.umem_grad_workspace_size(-1, good)[0] == ARG
+    assert U.umem_grad_workspace_size(2049, (U.umem_grad * 2049)())[0] == UNS
+    assert U.umem_grad_norm(2, good, None, None, ws, need, 0) == ARG
+    assert U.umem_grad_norm(2, good, norm + 2, None, ws, need, 0) == ARG
+    assert U.umem_grad_norm(2, good, norm, norm + 4, ws, need, 0) == ARG
+    assert U.umem_grad_norm(2, good, norm, None, None, need, 0) == WS
+    assert U.umem_grad_norm(2, good, norm, None, ws, need - 1, 0) == WS
+    assert U.umem_grad_norm(2, good, norm, None, ws + 8, need, 0) == WS
+    assert U.umem_grad_clip(2, good, -1.0, norm, 0) == ARG and U.umem_grad_clip(2, good, float("nan"), norm, 0) == ARG
+    assert U.umem_grad_clip(2, good, 1.0, None, 0) == ARG
+    bad = {
+        "rows": (at(0), at(1), None, -1, 4, 0), "row_len": (at(0), at(1), None, 4, -1, 0),
+        "type": (at(0), at(1), None, 4, 4, 2), "null": (None, at(1), None, 4, 4, 0),
+        "odd": (at(0) + 2, at(1), None, 4, 4, 0), "odd rows": (at(0), at(1), at(2) + 1, 4, 4, 0),
+    }
+    for name, row in bad.items():
+        assert U.umem_grad_workspace_size(1, grads(row))[0] == ARG, name
+        assert U.umem_grad_norm(1, grads(row), norm, None, ws, 1 << 20, 0) == ARG, name
+        assert U.umem_grad_clip(1, grads(row), 1.0, norm, 0) == ARG, name
+    for row in ((at(0), at(1), None, 1 << 30, 1 << 11, 0), (at(0), at(1), None, 1 << 62, 1 << 62, 0)):
+        assert U.umem_grad_workspace_size(1, grads(row))[0] == UNS
+    # without elements nothing of a gradient is looked at
+    assert U.umem_grad_workspace_size(1, grads((None, None, None, 0, 100, 0))) == (OK, 0)
+    assert U.umem_grad_clip(1, grads((None, None, None, 5, 0, 1)), 1.0, norm, 0) == OK
+    assert U.umem_grad_clip(0, None, 1.0, norm, 0) == OK
+    # no place to write, or one that another is read from or written to
+    k = 4096
+    for rows in ([(at(0), None, None, 1, k, 0)], [(at(0), at(1) + 2, None, 1, k, 0)],
+                 [(at(0), at(0) + 4, None, 1, k, 0)],
+                 [(at(0), at(1), None, 1, k, 0), (at(2), at(1) + 4 * k - 4, None, 1, k, 0)],
+                 [(at(0), at(0), None, 1, k, 0), (at(0), at(0), None, 1, k, 0)],
+                 [(at(0), at(1), None, 1, k, 0), (at(1) + 4, at(3), None, 1, 8, 0)],
+                 [(at(2), at(3), None, 1, k, 0), (at(1), at(1), None, 1, k, 0), (at(0), at(2) - 4, None, 1, 2, 0)]):
+        assert U.umem_grad_clip(len(rows), grads(*rows), 1.0, norm, 0) == ARG, rows
+
+
+def test_grad_tables_of_the_binding():
+    rows = [(at(0), at(1), 0, 4, 100, 0), (at(2), at(2), at(3), 7, 33, 1)]
+    table = np.array(rows, dtype=np.int64)
+    assert U.umem_grad_workspace_size(2, table) == U.umem_grad_workspace_size(2, grads(*rows))
+    assert ctypes.sizeof(U.umem_grad) == 48
+    for wrong in (table.astype(np.float64), table[:, :5], table.T, table[:1], table[0], table[:, ::-1]):
+        with pytest.raises(ValueError):
+            U.umem_grad_workspace_size(2, wrong)
+    with pytest.raises(ValueError):
+        U.umem_grad_workspace_size(2, grads(rows[0]))
+    with pytest.raises(ValueError):
+        U.umem_grad_workspace_size(2, (ctypes.c_int64 * 12)())
+
+
+def ad(**kw):
+    base = dict(n=4, rank=16, d_in=64, d_out=128, xtype=0, otype=0)
+    return U.umem_adapter_desc(*{**base, **kw}.values())
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(), OK), (dict(n=0), ARG), (dict(rank=0), ARG), (dict(d_in=0), ARG), (dict(d_out=-8), ARG),
+    (dict(xtype=2), ARG), (dict(otype=-1), ARG), (dict(rank=12), UNS), (dict(rank=136), UNS), (dict(rank=128), OK),
+    (dict(d_in=60), UNS), (dict(d_out=1 << 17), UNS), (dict(d_in=1 << 16), OK),
+])
+def test_adapter_descriptor(kw, want):
+    assert U.umem_adapter_workspace_size(ad(**kw), 8)[0] == want
+    assert U.umem_adapter_add(ad(**kw), 0, None, None, None, None, None, None, None, None, 0, 0) == want
+    assert U.umem_adapter_workspace_size(ad(), -1)[0] == ARG
+    assert U.umem_adapter_workspace_size(ad(), (1 << 20) + 1)[0] == UNS
+
+
+def test_adapter_refusals():
+    names = ["x", "ids", "a", "b", "scale", "base", "out"]
+    base = {k: at(i) for i, k in enumerate(names)}
+
+    def call(T=8, **kw):
+        return U.umem_adapter_add(ad(), T, *{**base, **kw}.values(), at(20), 32 * MB, 0)
+
+    for k in ("x", "ids", "a", "b", "out"):
+        assert call(**{k: None}) == ARG, k
+    for k in names:
+        assert call(**{k: base[k] + 2}) == ARG, k
+    for k in ("x", "a", "b", "base", "out"):
+        assert call(**{k: base[k] + 8}) == ARG, k
+    assert call(out=base["x"]) == ARG and call(out=base["base"] + 16) == ARG and call(out=base["b"] + 1024) == ARG
+    assert call(T=-1) == ARG
+    for T in (1, 8, 100, 5000):
+        st, need = U.umem_adapter_workspace_size(ad(), T)
+        assert st == OK
+        if need:
+            args = [ad(), T, *base.values()]
+            assert U.umem_adapter_add(*args, None, need, 0) == WS
+            assert U.umem_adapter_add(*args, at(20), need - 1, 0) == WS
+            assert U.umem_adapter_add(*args, at(20) + 16, need, 0) == WS

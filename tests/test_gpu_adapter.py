@@ -1,0 +1,194 @@
+"""Low-rank adapters of many requests on the GPU against the float64 oracle.
+
+u = 2^-24.  Products of bf16 weights with fp32 values are split without loss, so what is rounded are
+sums: of d_in terms (each of at most 2 roundings of its size: splitting and adding), then of rank terms,
+the scale and the base.  out is off by at most
+  u [ (d_in + 64) |s| |B| |A| |x|  +  (rank + 64) |s| |B| |v|  +  4 |base| + 4 |out| ],
+and half a step of bf16, 2^-8 of its value, where it is stored so.  (The sums of magnitudes are exact bounds;
+no cancellation is counted on.)
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle.block_oracle as B
+import paper_2411_12364_amd as U
+
+pytestmark = pytest.mark.gpu
+u = 2.0 ** -24
+
+
+def make(T, n, rank, d_in, d_out, seed, x="f32", o="f32", base=True, scale=True):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+    def rand(shape, s, dt):
+        return (torch.randn(shape, generator=g, device="cuda") * s).to(dt)
+
+    return dict(
+        desc=U.umem_adapter_desc(n, rank, d_in, d_out, int(x == "bf16"), int(o == "bf16")),
+        x=rand((T, d_in), 1.0, t[x]), a=rand((n, rank, d_in), d_in ** -0.5, torch.bfloat16),
+        b=rand((n, d_out, rank), rank ** -0.5, torch.bfloat16),
+        scale=torch.rand(n, generator=g, device="cuda") + 0.5 if scale else None,
+        base=rand((T, d_out), 1.0, t[o]) if base else None, out=torch.full((T, d_out), 9.0, dtype=t[o], device="cuda"),
+        g=g)
+
+
+def call(s, ids, out=None, base="base"):
+    T = len(ids)
+    st, need = U.umem_adapter_workspace_size(s["desc"], T)
+    U.check(st)
+    ws = torch.full((max(need, 256),), 0xFF, dtype=torch.uint8, device="cuda")        # NaN wherever it is read unwritten
+    out = s["out"] if out is None else out
+    U.check(U.umem_adapter_add(s["desc"], T, s["x"], ids, s["a"], s["b"], s["scale"], s[base], out, ws, ws.numel()))
+    return out
+
+
+def host(x):
+    return None if x is None else x.detach().double().cpu().numpy()
+
+
+def check(s, ids, out):
+    d = s["desc"]
+    x, a, b, scale, base = (host(s[k]) for k in ("x", "a", "b", "scale", "base"))
+    i = ids.cpu().numpy()
+    want = B.adapter_add(x, i, a, b, scale, base)
+    size = B.adapter_add(np.abs(x), i, np.abs(a), np.abs(b), scale, None)
+    low = np.zeros_like(size)
+    for t, j in enumerate(i):
+        if 0 <= j < d.n:
+            low[t] = (1.0 if scale is None else scale[j]) * (np.abs(b[j]) @ np.abs(a[j] @ x[t]))
+    tol = u * ((d.d_in + 64) * size + (d.rank + 64) * low + 4 * np.abs(want) + (0 if base is None else 4 * np.abs(base)))
+    tol += np.abs(want) * (2.0 ** -8 if d.otype else 0.0) + 1e-30
+    got = host(out)
+    over = np.abs(got - want) - tol
+    assert np.isfinite(got).all() and (over <= 0).all(), (float(over.max()), float(np.abs(got - want).max()))
+    # the bound is generous where terms cancel: the whole as a norm as well, two roundings a sum on average
+    rel = np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-30)
+    assert rel <= (2.0 ** -8 if d.otype else 2e-6), rel
+
+
+# tokens, adapters, rank, d_in, d_out
+SIZES = [(1, 1, 8, 8, 8), (1, 3, 16, 1024, 2048), (2, 2, 128, 264, 136), (5, 64, 16, 72, 4096), (16, 4, 24, 1000, 1000),
+         (17, 9, 8, 4096, 512), (33, 2, 64, 2048, 896), (64, 64, 16, 1024, 2048), (100, 7, 40, 520, 1032),
+         (255, 3, 32, 128, 264), (300, 300, 8, 64, 64), (513, 5, 56, 1024, 336), (1000, 12, 16, 2048, 896),
+         (2049, 16, 32, 256, 520), (4096, 3, 8, 64, 1024)]
+TYPES = [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16")]
+
+
+def ids_of(kind, T, n, g):
+    if kind == "random":
+        return torch.randint(-1, n, (T,), generator=g, device="cuda").to(torch.int32)
+    if kind == "one":
+        return torch.full((T,), n - 1, dtype=torch.int32, device="cuda")
+    runs = torch.sort(torch.randint(0, n, (T,), generator=g, device="cuda")).values
+    return ((runs * 7 + 3) % n).to(torch.int32)                          # requests in runs
+
+
+@pytest.mark.parametrize("i,size", enumerate(SIZES), ids=["x".join(map(str, s)) for s in SIZES])
+@pytest.mark.parametrize("kind", ["random", "runs", "one"])
+def test_adapters(i, size, kind):
+    x, o = TYPES[(i + len(kind)) % 4]
+    print(f"[case] adapters {size} {kind} {x} {o}", flush=True)
+    s = make(*size, 40 + i, x, o, base=i % 3 != 2, scale=i % 4 != 3)
+    ids = ids_of(kind, size[0], size[1], s["g"])
+    out = call(s, ids)
+    check(s, ids, out)
+    if s["base"] is not None:                                            # in place: the same bits
+        want, out = out.clone(), s["base"].clone()
+        U.check(U.umem_adapter_add(s["desc"], size[0], s["x"], ids, s["a"], s["b"], s["scale"], out, out,
+                                   ws := torch.empty(max(256, U.umem_adapter_workspace_size(s["desc"], size[0])[1]),
+                                                     dtype=torch.uint8, device="cuda"), ws.numel()))
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("T", [1, 37, 700])
+def test_tokens_without_an_adapter(T):
+    """ids outside [0, n): the base as it is (or zeros), whatever x holds there."""
+    s = make(T, 3, 16, 256, 512, 2)
+    ids = torch.tensor([-1, 3, 2 ** 31 - 1, -2 ** 31][:max(1, min(4, T))] * T, dtype=torch.int32, device="cuda")[:T].contiguous()
+    s["x"].fill_(float("nan"))
+    assert torch.equal(call(s, ids), s["base"])
+    s["base"] = None
+    assert (call(s, ids) == 0).all()
+    if T > 8:                                                            # among others that have one
+        s = make(T, 3, 16, 256, 512, 3)
+        ids = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+        ids[5], ids[T - 1] = 2, 0
+        s["x"][6], s["x"][4] = float("nan"), float("inf")
+        out = call(s, ids)
+        rest = [t for t in range(T) if t not in (5, T - 1)]
+        assert torch.equal(out[rest], s["base"][rest])
+        few = [5, T - 1]
+        part = {**s, "x": s["x"][few], "base": s["base"][few]}
+        check(part, ids[few], out[few])
+
+
+def test_nan_stays_with_its_token_and_adapter():
+    s = make(64, 4, 16, 256, 512, 4)
+    ids = (torch.arange(64, device="cuda") % 4).to(torch.int32)
+    clean = call(s, ids).clone()
+    s["x"][10, 3] = float("nan")
+    s["a"][3] = float("inf")
+    out = call(s, ids)
+    rest = [t for t in range(64) if t != 10 and t % 4 != 3]
+    assert torch.equal(out[rest], clean[rest])
+    assert torch.isnan(out[10]).all() and not torch.isfinite(out[3]).any()
+
+
+def test_every_digit_of_the_input_counts():
+    """x = 1 + 2^-23 against weights that cancel its leading part: a rounded x would give zero."""
+    s = make(3, 1, 8, 64, 64, 6, base=False, scale=False)
+    s["x"].fill_(1.0)
+    s["x"][:, 0] = 1.0 + 2.0 ** -23
+    s["a"].zero_()
+    s["a"][0, 0, 0], s["a"][0, 0, 1] = 1.0, -1.0
+    s["b"].zero_()
+    s["b"][0, :, 0] = 1.0
+    out = call(s, torch.zeros(3, dtype=torch.int32, device="cuda"))
+    assert torch.equal(out, torch.full_like(out, 2.0 ** -23))
+
+
+def test_offsets_past_32_bits():
+    """2^20 tokens of 2056: out has 2.16e9 elements."""
+    T, d_out = 1 << 20, 2056
+    s = make(64, 2, 8, 64, d_out, 8, x="bf16", o="bf16", base=False)
+    s["x"] = torch.randn((T, 64), generator=s["g"], device="cuda").to(torch.bfloat16)
+    s["out"] = torch.full((T, d_out), 9.0, dtype=torch.bfloat16, device="cuda")
+    ids = (torch.arange(T, device="cuda") % 3 - 1).to(torch.int32)
+    out = call(s, ids)
+    at = torch.tensor([0, 1, 2, T // 2, T - 3, T - 2, T - 1], device="cuda")
+    check({**s, "x": s["x"][at]}, ids[at], out[at])
+
+
+@pytest.mark.parametrize("T", [3, 64, 900])
+def test_captured_and_on_another_stream(T):
+    s = make(T, 6, 16, 512, 1024, 12)
+    ids = ids_of("random", T, 6, s["g"])
+    st, need = U.umem_adapter_workspace_size(s["desc"], T)
+    U.check(st)
+    ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+
+    def step(out):
+        U.check(U.umem_adapter_add(s["desc"], T, s["x"], ids, s["a"], s["b"], s["scale"], s["base"], out, ws, ws.numel()))
+
+    want, out = torch.empty_like(s["out"]), torch.empty_like(s["out"])
+    step(want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(out)
+    side.synchronize()
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out)
+    for k in range(3):
+        ids.copy_(torch.roll(ids, 1))
+        s["x"].mul_(1.5)
+        step(want)
+        torch.cuda.synchronize()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), k
