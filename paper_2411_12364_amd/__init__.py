@@ -143,6 +143,11 @@ def _load() -> ctypes.CDLL:
 _lib = _load()
 
 
+# The current device and its current stream's handle.  torch builds without a GPU lack these calls.
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda d: torch.cuda.current_stream(d).cuda_stream)
+
+
 def _p(x):
     """A device address: None -> NULL, int -> itself, torch tensor -> data_ptr()."""
     if x is None:
@@ -151,14 +156,19 @@ def _p(x):
         return x
     if not x.is_contiguous():
         raise ValueError("tensor arguments must be contiguous")
-    if x.device.type != "cuda":
+    if not x.is_cuda:
         raise ValueError("tensor arguments must live on the GPU")
     return x.data_ptr()
 
 
-def _s(stream):
+def _s(stream, like=None):
+    """A stream's handle; None is torch's current stream, of the current device, on which the tensor
+    ``like`` (where it is one) has to live then."""
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        device = _get_device()
+        if like is not None and not isinstance(like, int) and like.get_device() != device:
+            raise ValueError("tensor arguments must live on the current device, or a stream be given")
+        return _raw_stream(device)
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -290,13 +300,13 @@ def umem_score_backward(desc, T, q_row, q_col, k_row, k_col, core, idx, w, dw, d
 
 
 def umem_block_in(bd, T, h, gamma, beta, n, stream=None) -> int:
-    return _lib.umem_block_in(_d(bd), T, _p(h), _p(gamma), _p(beta), _p(n), _s(stream))
+    return _lib.umem_block_in(_d(bd), T, _p(h), _p(gamma), _p(beta), _p(n), _s(stream, h))
 
 
 def umem_block_out(bd, T, h, y, gate, gamma, beta, h_out, gamma_next=None, beta_next=None,
                    n_next=None, stream=None) -> int:
     return _lib.umem_block_out(_d(bd), T, _p(h), _p(y), _p(gate), _p(gamma), _p(beta), _p(h_out),
-                               _p(gamma_next), _p(beta_next), _p(n_next), _s(stream))
+                               _p(gamma_next), _p(beta_next), _p(n_next), _s(stream, h))
 
 
 def umem_block_backward_workspace_size(bd, T):
@@ -309,14 +319,14 @@ def umem_block_backward_workspace_size(bd, T):
 def umem_block_in_backward(bd, T, h, gamma, dn, dres, dh, dgamma, dbeta, accumulate, ws, ws_bytes,
                            stream=None) -> int:
     return _lib.umem_block_in_backward(_d(bd), T, _p(h), _p(gamma), _p(dn), _p(dres), _p(dh),
-                                       _p(dgamma), _p(dbeta), accumulate, _p(ws), ws_bytes, _s(stream))
+                                       _p(dgamma), _p(dbeta), accumulate, _p(ws), ws_bytes, _s(stream, h))
 
 
 def umem_block_out_backward(bd, T, y, gate, gamma, beta, dh_out, dh, dy, dgate, dgamma, dbeta,
                             accumulate, ws, ws_bytes, stream=None) -> int:
     return _lib.umem_block_out_backward(_d(bd), T, _p(y), _p(gate), _p(gamma), _p(beta), _p(dh_out),
                                         _p(dh), _p(dy), _p(dgate), _p(dgamma), _p(dbeta), accumulate,
-                                        _p(ws), ws_bytes, _s(stream))
+                                        _p(ws), ws_bytes, _s(stream, y))
 
 
 def _table(n, grads):
@@ -342,11 +352,11 @@ def umem_grad_workspace_size(n, grads):
 
 
 def umem_grad_norm(n, grads, norm, sumsq, ws, ws_bytes, stream=None) -> int:
-    return _lib.umem_grad_norm(n, _table(n, grads), _p(norm), _p(sumsq), _p(ws), ws_bytes, _s(stream))
+    return _lib.umem_grad_norm(n, _table(n, grads), _p(norm), _p(sumsq), _p(ws), ws_bytes, _s(stream, norm))
 
 
 def umem_grad_clip(n, grads, max_norm, norm, stream=None) -> int:
-    return _lib.umem_grad_clip(n, _table(n, grads), max_norm, _p(norm), _s(stream))
+    return _lib.umem_grad_clip(n, _table(n, grads), max_norm, _p(norm), _s(stream, norm))
 
 
 def umem_adapter_workspace_size(ad, T):
@@ -358,4 +368,4 @@ def umem_adapter_workspace_size(ad, T):
 
 def umem_adapter_add(ad, T, x, ids, a, b, scale, base, out, ws=None, ws_bytes=0, stream=None) -> int:
     return _lib.umem_adapter_add(_d(ad), T, _p(x), _p(ids), _p(a), _p(b), _p(scale), _p(base), _p(out),
-                                 _p(ws), ws_bytes, _s(stream))
+                                 _p(ws), ws_bytes, _s(stream, x))

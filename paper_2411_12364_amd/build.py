@@ -12,7 +12,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libumem.so")
 PROBE_LIB = os.path.join(PKG, "libumem_probe.so")
 SOURCES = ["umem_api.hip", "score.hip", "select.hip", "gather.hip", "project.hip", "query.hip", "sort.hip", "backward.hip",
-           "block.hip", "grad.hip", "adapter.hip"]
+           "block.hip", "block_backward.hip", "grad.hip", "adapter.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

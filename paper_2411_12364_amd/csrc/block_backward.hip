@@ -1,0 +1,308 @@
+// The backward of the norms before and after a block (block.hip).
+//
+// With v = gamma * (gradient of Norm's output) and r = 1 / spread, per row
+//   dx = r (v - mean(v) - x^ mean(v x^))          (mean(v) for LayerNorm only)
+// and over the rows  dgamma = sum dn x^,  dbeta = sum dn,  a channel gate's gradient.
+//
+// The statistics are recomputed from the row, which has to be read in any case: mean(v) is summed beside the
+// row's mean, and v's product with the centred row beside its variance, so a row takes two rounds of sums
+// over its group (RMS: one).  A group walks rows with its columns' parameters and column sums in registers,
+// the next row's loads in flight; the workgroups' column sums are added up in order by a second kernel.
+#include "block_rows.h"
+
+namespace umem {
+namespace {
+
+struct EntryBackArgs {
+  const void *h, *dn, *dres;
+  const float* gamma;
+  void* dh;
+  float* part;                 // [workgroups][dgamma, dbeta][d]
+  int T, d, stride;
+  bool centre, shift;
+  float eps;
+};
+
+struct ExitBackArgs {
+  const void *y, *gate, *dh_out;
+  const float *gamma, *beta;
+  void *dh, *dy, *dgate;
+  float* part;                 // [workgroups][dgamma, dbeta, dgate of a channel gate][d], those there are
+  int T, d, stride, norm_out, gate_kind;
+  bool sigmoid;
+  float eps, a, s;
+};
+
+// x -> x^, and r with the two means of the backward.
+struct BackSums {
+  float r, s0, s1;
+};
+template <int G, int PER>
+__device__ __forceinline__ BackSums back_sums(Row<PER>& x, const Row<PER>& v, int lane, int d, bool centre, float eps,
+                                              GroupSum<G>& gs) {
+  const float inv_d = 1.0f / static_cast<float>(d);
+  BackSums b{0.f, 0.f, 0.f};
+  if (centre) {
+    float sx = add_up(x), sv = add_up(v);
+    gs.sum2(sx, sv);
+    b.s0 = sv * inv_d;
+    centre_row<G>(x, sx * inv_d, lane, d);
+  }
+  float q = dot(x, x), vx = dot(v, x);
+  gs.sum2(q, vx);
+  b.r = 1.0f / sqrtf(q * inv_d + eps);
+  b.s1 = vx * b.r * inv_d;
+#pragma unroll
+  for (int p = 0; p < PER; ++p) x.v[p] *= b.r;
+  return b;
+}
+
+// A workgroup's column sums to its place of the partial sums: its groups' are added in order in LDS.
+template <int G, int PER>
+__device__ __forceinline__ void write_part(const Row<PER>& acc, float* part, int lane, int d, float* lds) {
+  Row<PER> s = acc;
+  if constexpr (Group<G>::kRows > 1) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      __syncthreads();
+      *reinterpret_cast<rf32x4*>(lds + threadIdx.x * 4) = acc.v[p];
+      __syncthreads();
+#pragma unroll
+      for (int w = 1; w < Group<G>::kRows; ++w) s.v[p] += *reinterpret_cast<const rf32x4*>(lds + (w * G + lane) * 4);
+    }
+    if (Group<G>::index() != 0) return;      // (its s starts from its own sums)
+  }
+  store_row<G>(part, s, lane, d);
+}
+
+template <typename HT, typename YT, int G, int PER>
+__global__ __launch_bounds__(Group<G>::kThreads) void entry_back_kernel(EntryBackArgs k) {
+  __shared__ float lds[2][Group<G>::kWaves][2];
+  __shared__ __align__(16) float sums[Group<G>::kRows > 1 ? 1024 : 4];
+  const int lane = Group<G>::lane(), d = k.d;
+  GroupSum<G> gs{lds, 0};
+  const HT *h = static_cast<const HT*>(k.h), *dres = static_cast<const HT*>(k.dres);
+  const YT* dn = static_cast<const YT*>(k.dn);
+  const bool more = dres != nullptr;
+  Row<PER> dg{}, db{};
+  int row = blockIdx.x * Group<G>::kRows + Group<G>::index();
+  RawRow<HT, PER> h_ahead{}, u_ahead{};
+  RawRow<YT, PER> n_ahead{};
+  if (row < k.T) {
+    const size_t at = static_cast<size_t>(row) * d;
+    h_ahead = load_raw<G, PER>(h + at, lane, d);
+    n_ahead = load_raw<G, PER>(dn + at, lane, d);
+    if (more) u_ahead = load_raw<G, PER>(dres + at, lane, d);
+  }
+  const Row<PER> gamma = load_params<G, PER>(k.gamma, 1.f, lane, d);
+  for (; row < k.T; row += k.stride) {
+    const Row<PER> n = widen(n_ahead), up = widen(u_ahead);
+    Row<PER> x = widen(h_ahead), v;
+    if (row + k.stride < k.T) {
+      const size_t next = static_cast<size_t>(row + k.stride) * d;
+      h_ahead = load_raw<G, PER>(h + next, lane, d);
+      n_ahead = load_raw<G, PER>(dn + next, lane, d);
+      if (more) u_ahead = load_raw<G, PER>(dres + next, lane, d);
+    }
+#pragma unroll
+    for (int p = 0; p < PER; ++p) v.v[p] = n.v[p] * gamma.v[p];
+    const BackSums b = back_sums<G>(x, v, lane, d, k.centre, k.eps, gs);
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float xh = x.v[p][i];
+        dg.v[p][i] = fmaf(n.v[p][i], xh, dg.v[p][i]);
+        db.v[p][i] += n.v[p][i];
+        v.v[p][i] = fmaf(v.v[p][i] - b.s0 - xh * b.s1, b.r, up.v[p][i]);
+      }
+    store_row<G>(static_cast<HT*>(k.dh) + static_cast<size_t>(row) * d, v, lane, d);
+  }
+  float* part = k.part + static_cast<size_t>(blockIdx.x) * (k.shift ? 2 : 1) * d;
+  write_part<G>(dg, part, lane, d, sums);
+  if (k.shift) write_part<G>(db, part + d, lane, d, sums);
+}
+
+template <typename HT, typename YT, int G, int PER>
+__global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackArgs k) {
+  __shared__ float lds[2][Group<G>::kWaves][2];
+  __shared__ __align__(16) float sums[Group<G>::kRows > 1 ? 1024 : 4];
+  const int lane = Group<G>::lane(), d = k.d;
+  const bool norm = k.norm_out != UMEM_NORM_NONE, full = k.gate_kind == UMEM_GATE_FULL,
+             channel = k.gate_kind == UMEM_GATE_CHANNEL, token = k.gate_kind == UMEM_GATE_TOKEN;
+  GroupSum<G> gs{lds, 0};
+  const HT* dh_out = static_cast<const HT*>(k.dh_out);
+  const YT *y = static_cast<const YT*>(k.y), *gate = static_cast<const YT*>(k.gate);
+  Row<PER> dg{}, db{}, dc{};
+  int row = blockIdx.x * Group<G>::kRows + Group<G>::index();
+  RawRow<YT, PER> y_ahead{}, g_ahead{};
+  RawRow<HT, PER> h_ahead{};
+  if (row < k.T) {
+    const size_t at = static_cast<size_t>(row) * d;
+    y_ahead = load_raw<G, PER>(y + at, lane, d);
+    h_ahead = load_raw<G, PER>(dh_out + at, lane, d);
+    if (full) g_ahead = load_raw<G, PER>(gate + at, lane, d);
+  }
+  const Row<PER> gamma = load_params<G, PER>(k.gamma, 1.f, lane, d), beta = load_params<G, PER>(k.beta, 0.f, lane, d);
+  // a channel gate's value; its slope comes from it
+  Row<PER> value = load_params<G, PER>(channel ? static_cast<const float*>(k.gate) : nullptr, 1.f, lane, d);
+  if (channel && k.sigmoid) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) value.v[p][i] = sigmoid(value.v[p][i]);
+  }
+  for (; row < k.T; row += k.stride) {
+    const size_t at = static_cast<size_t>(row) * d;
+    Row<PER> x = widen(y_ahead), up = widen(h_ahead), g = full ? widen(g_ahead) : value, v;
+    if (row + k.stride < k.T) {
+      const size_t next = static_cast<size_t>(row + k.stride) * d;
+      y_ahead = load_raw<G, PER>(y + next, lane, d);
+      h_ahead = load_raw<G, PER>(dh_out + next, lane, d);
+      if (full) g_ahead = load_raw<G, PER>(gate + next, lane, d);
+    }
+    if (k.dh != nullptr) {
+#pragma unroll
+      for (int p = 0; p < PER; ++p) v.v[p] = up.v[p] * k.a;
+      store_row<G>(static_cast<HT*>(k.dh) + at, v, lane, d);
+    }
+    if (full && k.sigmoid) {
+#pragma unroll
+      for (int p = 0; p < PER; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g.v[p][i] = sigmoid(g.v[p][i]);
+    }
+    float of_token = 1.f;
+    if (token) {
+      of_token = static_cast<const float*>(k.gate)[row];
+      if (k.sigmoid) of_token = sigmoid(of_token);
+    }
+    // up: out_scale dh_out, the gradient of the gated output; g: that of Norm_out's output
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      up.v[p] *= k.s;
+      v.v[p] = up.v[p] * (g.v[p] * of_token) * gamma.v[p];
+    }
+    BackSums b{1.f, 0.f, 0.f};
+    if (norm) b = back_sums<G>(x, v, lane, d, k.norm_out == UMEM_NORM_LAYER, k.eps, gs);
+    float st = 0.f;
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float xh = x.v[p][i], gv = g.v[p][i];
+        // the gradient of the gate's value, and of its argument
+        float dz = up.v[p][i] * fmaf(xh, gamma.v[p][i], beta.v[p][i]);
+        st += dz;
+        if (k.sigmoid) dz *= gv * (1.0f - gv);
+        const float dm = up.v[p][i] * (gv * of_token);
+        dg.v[p][i] = fmaf(dm, xh, dg.v[p][i]);
+        db.v[p][i] += dm;
+        dc.v[p][i] += dz;
+        up.v[p][i] = dz;
+        v.v[p][i] = norm ? (v.v[p][i] - b.s0 - xh * b.s1) * b.r : v.v[p][i];
+      }
+    if (full) store_row<G>(static_cast<YT*>(k.dgate) + at, up, lane, d);
+    store_row<G>(static_cast<YT*>(k.dy) + at, v, lane, d);
+    if (token) {
+      st = gs.sum(st);
+      if (lane == 0) static_cast<float*>(k.dgate)[row] = k.sigmoid ? st * (of_token * (1.0f - of_token)) : st;
+    }
+  }
+  const int q = (norm ? 1 : 0) + (k.beta != nullptr ? 1 : 0) + (channel ? 1 : 0);
+  float* part = k.part + static_cast<size_t>(blockIdx.x) * q * d;
+  if (norm) {
+    write_part<G>(dg, part, lane, d, sums);
+    part += d;
+  }
+  if (k.beta != nullptr) {
+    write_part<G>(db, part, lane, d, sums);
+    part += d;
+  }
+  if (channel) write_part<G>(dc, part, lane, d, sums);
+}
+
+// The column sums: 64 threads a column take every 64th partial sum each, in order, and theirs are added
+// in a fixed tree, so that the result does not depend on timing.
+struct ColumnArgs {
+  const float* part;
+  float* out[3];
+  int q, d, parts;
+  bool accumulate;
+};
+
+constexpr int kColWide = 16, kColDeep = 64;
+__global__ __launch_bounds__(kColWide * kColDeep) void column_sum_kernel(ColumnArgs k) {
+  __shared__ float lds[kColDeep][kColWide];
+  const int x = threadIdx.x % kColWide, deep = threadIdx.x / kColWide;
+  const int n = k.q * k.d, c = blockIdx.x * kColWide + x;
+  float s = 0.f;
+  if (c < n)
+#pragma unroll 8
+    for (int w = deep; w < k.parts; w += kColDeep) s += k.part[static_cast<size_t>(w) * n + c];
+  lds[deep][x] = s;
+#pragma unroll
+  for (int half = kColDeep / 2; half > 0; half >>= 1) {
+    __syncthreads();
+    if (deep < half) lds[deep][x] += lds[deep + half][x];
+  }
+  if (deep != 0 || c >= n) return;
+  s = lds[0][x];
+  const int which = c / k.d;
+  float* out = (which == 0 ? k.out[0] : which == 1 ? k.out[1] : k.out[2]) + (c - which * k.d);
+  *out = k.accumulate ? *out + s : s;
+}
+
+// Workgroups of a backward, and its rows of partial sums.
+constexpr int kMaxParts = 512;
+
+hipError_t launch_columns(const ColumnArgs& c, hipStream_t s) {
+  const int n = c.q * c.d;
+  hipLaunchKernelGGL(column_sum_kernel, dim3((n + kColWide - 1) / kColWide), dim3(kColWide * kColDeep), 0, s, c);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t block_backward_workspace_bytes(const umem_block_desc& bd, int T) {
+  if (T == 0) return 0;
+  const size_t bytes = static_cast<size_t>(row_workgroups(row_shape(bd.d), T, kMaxParts)) * 3 * bd.d * sizeof(float);
+  return (bytes + 255) / 256 * 256;
+}
+
+hipError_t launch_block_in_backward(const umem_block_desc& bd, int T, const void* h, const float* gamma,
+                                    const void* dn, const void* dres, void* dh, float* dgamma, float* dbeta,
+                                    bool accumulate, void* ws, hipStream_t s) {
+  clear_stale_error();
+  const RowShape shape = row_shape(bd.d);
+  const int wgs = row_workgroups(shape, T, kMaxParts);
+  const EntryBackArgs k{h, dn, dres, gamma, dh, static_cast<float*>(ws), T, bd.d, wgs * (shape.group == 64 ? 4 : 1),
+                        bd.norm_in == UMEM_NORM_LAYER, dbeta != nullptr, bd.eps};
+#define UMEM_ROW_GO(K, THR) hipLaunchKernelGGL(K, dim3(wgs), dim3(THR), 0, s, k)
+  UMEM_ROW_LAUNCH(entry_back_kernel)
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_columns({static_cast<const float*>(ws), {dgamma, dbeta, nullptr}, dbeta ? 2 : 1, bd.d, wgs, accumulate}, s);
+}
+
+hipError_t launch_block_out_backward(const umem_block_desc& bd, int T, const void* y, const void* gate,
+                                     const float* gamma, const float* beta, const void* dh_out, void* dh, void* dy,
+                                     void* dgate, float* dgamma, float* dbeta, bool accumulate, void* ws,
+                                     hipStream_t s) {
+  clear_stale_error();
+  const RowShape shape = row_shape(bd.d);
+  const int wgs = row_workgroups(shape, T, kMaxParts);
+  const ExitBackArgs k{y, gate, dh_out, gamma, beta, dh, dy, dgate, static_cast<float*>(ws), T, bd.d,
+                       wgs * (shape.group == 64 ? 4 : 1), bd.norm_out, bd.gate, bd.gate_act == UMEM_ACT_SIGMOID,
+                       bd.eps, bd.res_scale, bd.out_scale};
+  UMEM_ROW_LAUNCH(exit_back_kernel)
+#undef UMEM_ROW_GO
+  const hipError_t e = hipGetLastError();
+  ColumnArgs c{static_cast<const float*>(ws), {nullptr, nullptr, nullptr}, 0, bd.d, wgs, accumulate};
+  if (dgamma != nullptr) c.out[c.q++] = dgamma;
+  if (dbeta != nullptr) c.out[c.q++] = dbeta;
+  if (bd.gate == UMEM_GATE_CHANNEL) c.out[c.q++] = static_cast<float*>(dgate);
+  return e != hipSuccess || c.q == 0 ? e : launch_columns(c, s);
+}
+
+}  // namespace umem

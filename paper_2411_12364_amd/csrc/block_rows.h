@@ -1,139 +1,229 @@
-// Rows of a residual stream in the registers of a group of threads (block.hip): the loads, stores and
-// sums that the norms before and after a block share.  Not part of the public ABI.
+// Rows of a residual stream in the registers of a group of threads (block.hip, block_backward.hip): the
+// loads, stores and sums that the norms before and after a block share.  Not part of the public ABI.
 #pragma once
+
+#include <algorithm>
 
 #include "umem_internal.h"
 
 namespace umem {
 
-typedef float bf32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bb16x4 __attribute__((ext_vector_type(4)));
+typedef float rf32x4 __attribute__((ext_vector_type(4)));
 
-// A row's elements are dealt to the G threads of its group in runs of four: element
-// (p G + lane) 4 + i is v[p][i] of thread `lane`.  Elements past the row are zeros.
-template <int PER>
-struct RowRegs {
-  bf32x4 v[PER];
-};
-
-__device__ __forceinline__ bf32x4 widen(bf32x4 x) { return x; }
-__device__ __forceinline__ bf32x4 widen(bb16x4 x) {
-  return bf32x4{static_cast<float>(x.x), static_cast<float>(x.y), static_cast<float>(x.z), static_cast<float>(x.w)};
-}
+// Four consecutive elements as they lie in memory.  Rows of an odd width start at any element, so the
+// type promises no more than an element's alignment: global loads and stores of 8 and 16 bytes need none.
 template <typename T>
-struct Four;
-template <>
-struct Four<float> {
-  using type = bf32x4;
-};
-template <>
-struct Four<__bf16> {
-  using type = bb16x4;
+struct Quad {
+  typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T))));
 };
 
-// VEC: d % 4 == 0 and rows aligned to four elements; else the elements are taken one by one.
-template <bool VEC, typename T>
-__device__ __forceinline__ bf32x4 load4(const T* row, int e, int d) {
-  if constexpr (VEC) {
-    if (e >= d) return bf32x4{0.f, 0.f, 0.f, 0.f};
-    return widen(*reinterpret_cast<const typename Four<T>::type*>(row + e));
-  } else {
-    bf32x4 r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = e + i < d ? static_cast<float>(row[e + i]) : 0.f;
-    return r;
-  }
-}
+// A group is 64 threads (a wave; four rows to a workgroup) or a workgroup.  Element (p G + lane) 4 + i of
+// a row belongs to v[p][i] of thread `lane`; elements past the row are zeros.
+template <int G>
+struct Group {
+  static constexpr int kThreads = G > 256 ? G : 256;
+  static constexpr int kRows = kThreads / G;
+  static constexpr int kWaves = G / kWave;
+  static __device__ __forceinline__ int lane() { return threadIdx.x % G; }
+  static __device__ __forceinline__ int index() { return threadIdx.x / G; }
+};
 
-template <bool VEC, typename T>
-__device__ __forceinline__ void store4(T* row, int e, int d, bf32x4 x) {
-  const typename Four<T>::type r = {static_cast<T>(x.x), static_cast<T>(x.y), static_cast<T>(x.z), static_cast<T>(x.w)};
-  if constexpr (VEC) {
-    if (e < d) *reinterpret_cast<typename Four<T>::type*>(row + e) = r;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (e + i < d) row[e + i] = r[i];
-  }
-}
+// A row as it lies in memory: half the registers where it is bf16 and waits for its turn.
+template <typename T, int PER>
+struct RawRow {
+  typename Quad<T>::type v[PER];
+};
+template <int PER>
+struct Row {
+  rf32x4 v[PER];
+};
 
-template <int G, int PER, bool VEC, typename T>
-__device__ __forceinline__ RowRegs<PER> load_row(const T* row, int lane, int d) {
-  RowRegs<PER> r;
+template <int G, int PER, typename T>
+__device__ __forceinline__ RawRow<T, PER> load_raw(const T* row, int lane, int d) {
+  RawRow<T, PER> r;
 #pragma unroll
-  for (int p = 0; p < PER; ++p) r.v[p] = load4<VEC>(row, (p * G + lane) * 4, d);
+  for (int p = 0; p < PER; ++p) {
+    const int e = (p * G + lane) * 4;
+    r.v[p] = T(0);
+    if (e + 4 <= d) {
+      r.v[p] = *reinterpret_cast<const typename Quad<T>::type*>(row + e);
+    } else if (e < d) {                      // the last thread of a row of no multiple of four
+      r.v[p].x = row[e];
+      if (e + 1 < d) r.v[p].y = row[e + 1];
+      if (e + 2 < d) r.v[p].z = row[e + 2];
+    }
+  }
   return r;
 }
 
-// The sums of up to two values over a group: a wave by shuffles, a workgroup of G threads by its
-// waves' sums in LDS, added in wave order by every thread (the same bits in all of them).  `turn`
-// picks one of two LDS buffers, so that one barrier a sum is enough.
+template <typename T, int PER>
+__device__ __forceinline__ Row<PER> widen(const RawRow<T, PER>& r) {
+  Row<PER> x;
+#pragma unroll
+  for (int p = 0; p < PER; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.v[p][i] = static_cast<float>(r.v[p][i]);
+  return x;
+}
+
+// A vector of parameters [d], or `otherwise` in every element where there is none.
+template <int G, int PER>
+__device__ __forceinline__ Row<PER> load_params(const float* p, float otherwise, int lane, int d) {
+  if (p != nullptr) return widen<float, PER>(load_raw<G, PER>(p, lane, d));
+  Row<PER> r;
+#pragma unroll
+  for (int q = 0; q < PER; ++q) r.v[q] = otherwise;
+  return r;
+}
+
+template <int G, int PER, typename T>
+__device__ __forceinline__ void store_row(T* row, const Row<PER>& x, int lane, int d) {
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const int e = (p * G + lane) * 4;
+    const typename Quad<T>::type r = {static_cast<T>(x.v[p].x), static_cast<T>(x.v[p].y), static_cast<T>(x.v[p].z),
+                                      static_cast<T>(x.v[p].w)};
+    if (e + 4 <= d) {
+      *reinterpret_cast<typename Quad<T>::type*>(row + e) = r;
+    } else if (e < d) {
+      row[e] = r.x;
+      if (e + 1 < d) row[e + 1] = r.y;
+      if (e + 2 < d) row[e + 2] = r.z;
+    }
+  }
+}
+
+// The sum over a wave in every lane, by data-parallel moves inside the register file (a shuffle
+// through LDS costs several times as long, and a row waits for two to five of these sums).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum_dpp(float v) {
+  v = dpp_add<0xB1, 0xf>(v);       // lane ^ 1
+  v = dpp_add<0x4E, 0xf>(v);       // lane ^ 2
+  v = dpp_add<0x141, 0xf>(v);      // mirrored in 8 lanes
+  v = dpp_add<0x140, 0xf>(v);      // mirrored in 16
+  v = dpp_add<0x142, 0xa>(v);      // lane 15 of 16-lane rows 0 and 2 added to rows 1 and 3
+  v = dpp_add<0x143, 0xc>(v);      // lane 31 added to rows 2 and 3
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+
+// Two sums over a group: a wave's by wave_sum_dpp, a workgroup's by its waves' sums in LDS, added in wave
+// order by every thread (the same bits in all of them).  `turn` picks one of two LDS buffers, so that
+// one barrier a sum is enough.
 template <int G>
 struct GroupSum {
-  static constexpr int kWaves = G / kWave;
-  float (*lds)[2][kWaves];            // [2][2][kWaves]
+  static constexpr int kWaves = Group<G>::kWaves;
+  float (*lds)[kWaves][2];            // [2][kWaves][2]
   int turn;
 
   __device__ __forceinline__ void sum2(float& a, float& b) {
-    a = wave_sum(a);
-    b = wave_sum(b);
+    a = wave_sum_dpp(a);
+    b = wave_sum_dpp(b);
     if constexpr (kWaves > 1) {
-      const int wave = threadIdx.x / kWave;
       if ((threadIdx.x & (kWave - 1)) == 0) {
-        lds[turn][0][wave] = a;
-        lds[turn][1][wave] = b;
+        lds[turn][threadIdx.x / kWave][0] = a;
+        lds[turn][threadIdx.x / kWave][1] = b;
       }
       __syncthreads();
       a = b = 0.f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        a += lds[turn][0][w];
-        b += lds[turn][1][w];
+        a += lds[turn][w][0];
+        b += lds[turn][w][1];
       }
       turn ^= 1;
     }
   }
   __device__ __forceinline__ float sum(float a) {
-    a = wave_sum(a);
-    if constexpr (kWaves > 1) {
-      const int wave = threadIdx.x / kWave;
-      if ((threadIdx.x & (kWave - 1)) == 0) lds[turn][0][wave] = a;
-      __syncthreads();
-      a = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) a += lds[turn][0][w];
-      turn ^= 1;
-    }
+    float none = 0.f;
+    sum2(a, none);
     return a;
   }
 };
 
-// x -> x^ in place (elements past the row stay zero); returns 1 / spread.  The variance is taken of
-// the centred row, which keeps its digits where the mean is far from zero.
-template <int G, int PER>
-__device__ __forceinline__ float normalise(RowRegs<PER>& x, int lane, int d, bool centre, float eps, GroupSum<G>& gs) {
-  const float inv_d = 1.0f / static_cast<float>(d);
-  if (centre) {
-    float s = 0.f;
+template <int PER>
+__device__ __forceinline__ float add_up(const Row<PER>& x) {
+  float s = 0.f;
 #pragma unroll
-    for (int p = 0; p < PER; ++p) s += (x.v[p].x + x.v[p].y) + (x.v[p].z + x.v[p].w);
-    const float mean = gs.sum(s) * inv_d;
-#pragma unroll
-    for (int p = 0; p < PER; ++p)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x.v[p][i] = (p * G + lane) * 4 + i < d ? x.v[p][i] - mean : 0.f;
-  }
-  float q = 0.f;
-#pragma unroll
-  for (int p = 0; p < PER; ++p)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q = fmaf(x.v[p][i], x.v[p][i], q);
-  const float r = 1.0f / sqrtf(gs.sum(q) * inv_d + eps);
-#pragma unroll
-  for (int p = 0; p < PER; ++p)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[p][i] *= r;
-  return r;
+  for (int p = 0; p < PER; ++p) s += (x.v[p].x + x.v[p].y) + (x.v[p].z + x.v[p].w);
+  return s;
 }
+template <int PER>
+__device__ __forceinline__ float dot(const Row<PER>& x, const Row<PER>& y) {
+  float s = 0.f;
+#pragma unroll
+  for (int p = 0; p < PER; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = fmaf(x.v[p][i], y.v[p][i], s);
+  return s;
+}
+
+// x - mean in the row's elements, zeros past it.
+template <int G, int PER>
+__device__ __forceinline__ void centre_row(Row<PER>& x, float mean, int lane, int d) {
+#pragma unroll
+  for (int p = 0; p < PER; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.v[p][i] = (p * G + lane) * 4 + i < d ? x.v[p][i] - mean : 0.f;
+}
+
+// x -> x^ in place.  The variance is taken of the centred row, which keeps its digits where the mean is
+// far from zero.
+template <int G, int PER>
+__device__ __forceinline__ void normalise(Row<PER>& x, int lane, int d, bool centre, float eps, GroupSum<G>& gs) {
+  const float inv_d = 1.0f / static_cast<float>(d);
+  if (centre) centre_row<G>(x, gs.sum(add_up(x)) * inv_d, lane, d);
+  const float r = 1.0f / sqrtf(gs.sum(dot(x, x)) * inv_d + eps);
+#pragma unroll
+  for (int p = 0; p < PER; ++p) x.v[p] *= r;
+}
+
+// 1 / (1 + e^-z); the reciprocal is the hardware's, within one step of fp32.
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + expf(-z)); }
+
+// How rows of d elements are dealt to threads: eight elements a thread where the row has them (more in
+// flight and in registers lets fewer waves run), four in the shortest rows.
+struct RowShape {
+  int group, per;
+};
+inline RowShape row_shape(int d) {
+  if (d <= 256) return {64, 1};
+  if (d <= 512) return {64, 2};
+  if (d <= 1024) return {256, 1};
+  if (d <= 2048) return {256, 2};
+  if (d <= 4096) return {512, 2};
+  return {1024, d <= 8192 ? 2 : 4};
+}
+
+// Workgroups for T rows, at most `most`, each with as many rows as the others or one fewer.
+inline int row_workgroups(const RowShape& s, int T, int most) {
+  const int rows = s.group == 64 ? 4 : 1;
+  const int need = (T + rows - 1) / rows, turns = (need + most - 1) / most;
+  return (need + turns - 1) / turns;
+}
+
+// GO(kernel instance, threads) for the row shape and the types of h and y.
+#define UMEM_ROW_SHAPES(KERNEL, HT, YT)                                                             \
+  switch (shape.group * 8 + shape.per) {                                                            \
+    case 64 * 8 + 1: UMEM_ROW_GO((KERNEL<HT, YT, 64, 1>), 256); break;                              \
+    case 64 * 8 + 2: UMEM_ROW_GO((KERNEL<HT, YT, 64, 2>), 256); break;                              \
+    case 256 * 8 + 1: UMEM_ROW_GO((KERNEL<HT, YT, 256, 1>), 256); break;                            \
+    case 256 * 8 + 2: UMEM_ROW_GO((KERNEL<HT, YT, 256, 2>), 256); break;                            \
+    case 512 * 8 + 2: UMEM_ROW_GO((KERNEL<HT, YT, 512, 2>), 512); break;                            \
+    case 1024 * 8 + 2: UMEM_ROW_GO((KERNEL<HT, YT, 1024, 2>), 1024); break;                         \
+    default: UMEM_ROW_GO((KERNEL<HT, YT, 1024, 4>), 1024); break;                                   \
+  }
+#define UMEM_ROW_LAUNCH(KERNEL)                            \
+  if (bd.htype == UMEM_F32 && bd.ytype == UMEM_F32) {      \
+    UMEM_ROW_SHAPES(KERNEL, float, float)                  \
+  } else if (bd.htype == UMEM_F32) {                       \
+    UMEM_ROW_SHAPES(KERNEL, float, __bf16)                 \
+  } else if (bd.ytype == UMEM_F32) {                       \
+    UMEM_ROW_SHAPES(KERNEL, __bf16, float)                 \
+  } else {                                                 \
+    UMEM_ROW_SHAPES(KERNEL, __bf16, __bf16)                \
+  }
 
 }  // namespace umem
