@@ -1,13 +1,31 @@
 // Low-rank adapters of many requests beside a shared projection:
-//   out[t] = base[t] + scale[i] B_i (A_i x[t]),  i = ids[t]
+//   out[t] = base[t] + scale[i] B_i (A_i x[t]),  i = ids[t];  out[t] = base[t] where i is no adapter
+//
+// * token_kernel, few tokens (which then mostly have an adapter of their own): a workgroup takes a token
+//   and a range of its outputs, both products in one launch.  Bound by the latency of a chain of loads (id,
+//   A's rows, B's rows); the ranges recompute A x, whose rows come from L2 after the first, so that few
+//   tokens still use many CUs.
+// * low_kernel and out_kernel, many tokens: A x on the matrix cores by tiles of 64 tokens and a piece of
+//   d_in each, its sums over the pieces through the workspace, then B times those by tiles and a range of
+//   outputs.  Bound by HBM (x, base and out once); the adapters come from L2, once for the 16 tokens of a
+//   product that share one.  A launch for both, with all of d_in and A for 16 tokens in one workgroup, waited
+//   for twice as many bytes from L2 in every CU (4,096 tokens in 16 runs, rank 32, 2,048 by 896: 21 us).
+//
+// Nothing is rounded on the way: an fp32 value is the sum of three bf16 parts of 8 bits each, whose
+// products with bf16 weights are exact in the matrix cores' fp32 accumulators.
 #include <algorithm>
+#include <cmath>
 
 #include "umem_internal.h"
 
 namespace umem {
 namespace {
 
-constexpr int THREADS = 256;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 struct AdapterArgs {
   const void* x;
@@ -17,65 +35,603 @@ struct AdapterArgs {
   const void* base;
   void* out;
   int T, n, rank, d_in, d_out;
+  int splits;                  // workgroups that share a token's (a tile's) outputs
+  float* low;                  // many tokens: [pieces of d_in][T][rank, padded] partial sums of A x
+  int pieces;                  // pieces of d_in
 };
 
-typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ float lo_of(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float hi_of(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 
-// A workgroup a token: a wave a row of A_i, then a thread an output.
-template <typename XT, typename OT>
-__global__ __launch_bounds__(THREADS) void adapter_token_kernel(AdapterArgs k) {
-  __shared__ float low[kMaxAdapterRank];
-  const int t = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int id = k.ids[t];
-  const bool on = id >= 0 && id < k.n;
-  if (on) {
-    const XT* x = static_cast<const XT*>(k.x) + static_cast<size_t>(t) * k.d_in;
-    const float scale = k.scale != nullptr ? k.scale[id] : 1.0f;
-    for (int r = wave; r < k.rank; r += THREADS / kWave) {
-      const uint16_t* a = k.a + (static_cast<size_t>(id) * k.rank + r) * k.d_in;
-      float s = 0.f;
-      for (int c = lane * 8; c < k.d_in; c += kWave * 8) {
-        const u16x8 w = *reinterpret_cast<const u16x8*>(a + c);
+// Eight consecutive values of x in fp32.
+struct Eight {
+  float v[8];
+};
+__device__ __forceinline__ Eight load8(const float* p) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+  return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+__device__ __forceinline__ Eight load8(const __bf16* p) {
+  const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+  return {{lo_of(a.x), hi_of(a.x), lo_of(a.y), hi_of(a.y), lo_of(a.z), hi_of(a.z), lo_of(a.w), hi_of(a.w)}};
+}
+__device__ __forceinline__ float dot8(u32x4 w, const Eight& x, float s) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(bf16_to_f32(w[i]), static_cast<float>(x[c + i]), s);
+  for (int i = 0; i < 4; ++i) {
+    s = fmaf(lo_of(w[i]), x.v[2 * i], s);
+    s = fmaf(hi_of(w[i]), x.v[2 * i + 1], s);
+  }
+  return s;
+}
+
+__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
+__device__ __forceinline__ f32x4 load4(const __bf16* p) {
+  const u32x2 a = *reinterpret_cast<const u32x2*>(p);
+  return {lo_of(a.x), hi_of(a.x), lo_of(a.y), hi_of(a.y)};
+}
+__device__ __forceinline__ void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
+__device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
+  *reinterpret_cast<bf16x4*>(p) = bf16x4{static_cast<__bf16>(v.x), static_cast<__bf16>(v.y),
+                                         static_cast<__bf16>(v.z), static_cast<__bf16>(v.w)};
+}
+
+// ---------------------------------------------------------------- few tokens
+
+constexpr int kTokenThreads = 256, kTokenWaves = kTokenThreads / kWave;
+constexpr int kAhead = 8;      // 16-byte pieces of B that a thread loads before A x is known
+
+// ROWS: rows of A a wave takes, rank <= 4 ROWS.
+template <typename XT, typename OT, int ROWS>
+__global__ __launch_bounds__(kTokenThreads) void token_kernel(AdapterArgs k) {
+  __shared__ __align__(16) float low[kMaxAdapterRank];
+  const int t = blockIdx.x, part = blockIdx.y;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int id = k.ids[t];
+  const bool on = id >= 0 && id < k.n;               // (the same in the whole workgroup)
+  // this workgroup's outputs, and this thread's
+  const int per = (k.d_out + k.splits - 1) / k.splits, first = part * per, last = min(k.d_out, first + per);
+  const OT* base = k.base != nullptr ? static_cast<const OT*>(k.base) + static_cast<size_t>(t) * k.d_out : nullptr;
+  OT* out = static_cast<OT*>(k.out) + static_cast<size_t>(t) * k.d_out;
+  if (!on) {
+    for (int o = first + threadIdx.x; o < last; o += kTokenThreads) out[o] = base != nullptr ? base[o] : OT(0);
+    return;
+  }
+  const int pieces = k.rank / 8;
+  const uint16_t* b = k.b + static_cast<size_t>(id) * k.d_out * k.rank;
+  u32x4 ahead[kAhead];
+  const bool early = pieces * ((per + kTokenThreads - 1) / kTokenThreads) <= kAhead;
+  if (early) {
+    int o = first + threadIdx.x, q = 0;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (o < last) ahead[i] = *reinterpret_cast<const u32x4*>(b + static_cast<size_t>(o) * k.rank + q * 8);
+      if (++q == pieces) {
+        q = 0;
+        o += kTokenThreads;
       }
-      s = wave_sum(s);
-      if (lane == 0) low[r] = s * scale;
+    }
+  }
+  // A x: a wave's rows side by side, so that its loads of a step are all in flight together
+  const XT* x = static_cast<const XT*>(k.x) + static_cast<size_t>(t) * k.d_in;
+  const uint16_t* a = k.a + static_cast<size_t>(id) * k.rank * k.d_in;
+  float acc[ROWS] = {};
+#pragma unroll 2
+  for (int c = lane * 8; c < k.d_in; c += kWave * 8) {
+    const Eight xv = load8(x + c);
+    u32x4 w[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const int row = wave + r * kTokenWaves;
+      w[r] = row < k.rank ? *reinterpret_cast<const u32x4*>(a + static_cast<size_t>(row) * k.d_in + c) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) acc[r] = dot8(w[r], xv, acc[r]);
+  }
+  const float scale = k.scale != nullptr ? k.scale[id] : 1.0f;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const float s = wave_sum(acc[r]);
+    if (lane == 0) low[wave + r * kTokenWaves] = s * scale;
+  }
+  __syncthreads();
+  if (early) {
+    int o = first + threadIdx.x, q = 0;
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (o < last) v = dot8(ahead[i], load8(low + q * 8), v);
+      if (++q == pieces) {
+        if (o < last) out[o] = static_cast<OT>(base != nullptr ? static_cast<float>(base[o]) + v : v);
+        q = 0;
+        v = 0.f;
+        o += kTokenThreads;
+      }
+    }
+    return;
+  }
+  for (int o = first + threadIdx.x; o < last; o += kTokenThreads) {
+    float v = 0.f;
+    for (int i = 0; i < pieces; ++i)
+      v = dot8(*reinterpret_cast<const u32x4*>(b + static_cast<size_t>(o) * k.rank + i * 8), load8(low + i * 8), v);
+    out[o] = static_cast<OT>(base != nullptr ? static_cast<float>(base[o]) + v : v);
+  }
+}
+
+// ---------------------------------------------------------------- many tokens
+
+constexpr int kThreads = 512, kWaves = kThreads / kWave;
+constexpr int kTile = 64, kGroup = 16;       // tokens of a workgroup, and of a matrix product
+
+// x = p[0] + p[1] + p[2], each of 8 significant bits (cut off, not rounded, so that the largest values stay
+// finite); an infinity is its first part alone.  Four values as three times four bf16.
+struct Parts4 {
+  u32x2 p[3];
+};
+__device__ __forceinline__ Parts4 split4(f32x4 x) {
+  uint32_t bits[3][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float rest = x[i];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      const uint32_t cut = __float_as_uint(rest) & 0xFFFF0000u;
+      bits[q][i] = cut;
+      rest -= __uint_as_float(cut);
+      if (q == 0) rest = fabsf(x[i]) == INFINITY ? 0.f : rest;
+    }
+  }
+  Parts4 r;
+#pragma unroll
+  for (int q = 0; q < 3; ++q) r.p[q] = u32x2{(bits[q][0] >> 16) | bits[q][1], (bits[q][2] >> 16) | bits[q][3]};
+  return r;
+}
+
+// Buffer resource of a raw byte range: loads past it give zeros, stores past it are dropped, so the edges
+// (tokens past T, ranks past the rank, columns past a width) need no branches around loads and stores.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p, size_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), static_cast<short>(0), static_cast<int>(bytes), 0x00020000);
+}
+constexpr uint32_t kOutside = 0x80000000u;   // past any range here (they are below 2^26 bytes)
+__device__ __forceinline__ u32x4 fetch16(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+  return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+}
+
+// The tokens of a tile, one a lane, and the (span, adapter) pairs among them, a span being 16 CG tokens: the
+// first token of each adapter in its span stands for the pair.
+template <int CG>
+struct Tile {
+  static constexpr int kSpan = kGroup * CG;
+  int id;                    // this lane's token's adapter, or -1
+  uint64_t leads;
+  // The id is fetched before a kernel's other loads (they come back in order), and looked at after.
+  __device__ __forceinline__ void fetch(const int32_t* ids, int t0, int T) {
+    const int t = t0 + (threadIdx.x & (kWave - 1));
+    id = t < T ? ids[t] : -1;
+  }
+  __device__ __forceinline__ void find(int n) {
+    if (id < 0 || id >= n) id = -1;
+    if constexpr (CG == 1) {       // 16 lanes are a row of the data-parallel moves
+      bool first = id >= 0;
+      earlier<1>(first);
+      leads = __ballot(first);
+    } else {
+      leads = 0;
+      const uint64_t on = __ballot(id >= 0);
+#pragma unroll
+      for (int c = 0; c < kTile / kSpan; ++c) {
+        for (uint64_t left = on & (~0ull >> (kTile - kSpan)) << (c * kSpan); left != 0;) {
+          const int first = __builtin_ctzll(left);
+          leads |= 1ull << first;
+          left &= ~__ballot(id == __builtin_amdgcn_readlane(id, first));
+        }
+      }
+    }
+  }
+  template <int S>
+  __device__ __forceinline__ void earlier(bool& first) {
+    // the id S lanes back in the row of 16; past its start -1, which is no adapter
+    first = first && __builtin_amdgcn_update_dpp(-1, id, 0x110 + S, 0xf, 0xf, false) != id;
+    if constexpr (S < 15) earlier<S + 1>(first);
+  }
+  // The place of pair p's first token.
+  __device__ __forceinline__ int place(int p) const {
+    const int lane = threadIdx.x & (kWave - 1);
+    const bool it = ((leads >> lane) & 1) != 0 && __popcll(leads & lanemask_lt()) == p;
+    return __builtin_ctzll(__ballot(it));
+  }
+  // Whether the token of this lane's column in the 16 from `first` on has adapter `lead`.
+  __device__ __forceinline__ bool mine(int first, int lead) const {
+    return __shfl(id, first + (threadIdx.x & (kGroup - 1)), kWave) == lead;
+  }
+};
+
+// A 16 x 16 x 32 product takes its first operand's rows and its second's columns from lanes % 16, eight
+// consecutive k from lane / 16; lane % 16 of the result is its column, and the lane holds rows
+// 4 (lane / 16) + 0..3 of it.  The weights are the rows (ranks, then outputs), tokens the columns, so that a
+// lane ends up with four consecutive values of one token; columns of tokens with another adapter are
+// computed along and dropped (a token's values reach no other column).
+
+// low[piece][t][:] = A x over the piece's columns.  x of the tile is staged in LDS in bf16 parts; a wave
+// takes (pair, 16 ranks) items, whose weights go from global memory to its registers, the next item's
+// while this one is multiplied.  NB: 16-byte pieces of x that a thread stages.  RT: rank / 16, rounded up.
+// CG: products that share loaded weights; 1 up to rank 32, where a tile of one adapter would leave waves
+// without an item, 2 beyond (rank 64, 2,048 by 2,048: 13.8 us, not 16.5).
+template <typename XT>
+constexpr int piece_width(int nb) {
+  return nb * kThreads / kTile * static_cast<int>(16 / sizeof(XT));
+}
+
+template <typename XT, int NB, int CG>
+__global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs k, int RT) {
+  constexpr int kParts = sizeof(XT) == 4 ? 3 : 1, kPer = 16 / sizeof(XT), kPiece = piece_width<XT>(NB);
+  constexpr int kPitch = kPiece + 8, kPlane = kTile * kPitch, kSteps = kPiece / 32, kPerRow = kPiece / kPer;
+  extern __shared__ __align__(16) uint16_t staged[];    // [parts][64][pitch]
+  const int t0 = blockIdx.x * kTile, begin = blockIdx.y * kPiece, width = min(kPiece, k.d_in - begin);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int col = lane & 15, quad = lane >> 4;
+  const int tokens = min(kTile, k.T - t0);
+  const size_t row = static_cast<size_t>(k.d_in) * sizeof(XT);
+  const __amdgpu_buffer_rsrc_t rx = rsrc(static_cast<const XT*>(k.x) + static_cast<size_t>(t0) * k.d_in, tokens * row);
+  Tile<CG> tile;
+  tile.fetch(k.ids, t0, k.T);
+  u32x4 v[NB];
+#pragma unroll
+  for (int u = 0; u < NB; ++u) {
+    const int f = threadIdx.x + u * kThreads, r = f / kPerRow, c = f % kPerRow * kPer;
+    v[u] = fetch16(rx, c < width ? static_cast<uint32_t>(r * k.d_in + begin + c) * static_cast<uint32_t>(sizeof(XT)) : kOutside);
+  }
+  tile.find(k.n);
+  if (tile.leads == 0) return;                          // (the same in every wave)
+  // an item's weights in one or two halves, 32 registers at a time, so that two workgroups fit a CU
+  constexpr int kHalf = kSteps < 8 ? kSteps : 8, kHalves = kSteps / kHalf;
+  const int items = __popcll(tile.leads) * RT;
+  struct Half {
+    int first, lead, rt;
+    u32x4 w[kHalf];
+  } even, odd;
+  auto load = [&](Half& n, int half) {                  // (the wave's own count of halves)
+    const int item = wave + half / kHalves * kWaves, from_step = half % kHalves * kHalf;
+    if (item >= items) return;
+    const int pair = item / RT;
+    const int at = tile.place(pair);
+    n.rt = item - pair * RT;
+    n.first = at & ~(Tile<CG>::kSpan - 1);
+    n.lead = __builtin_amdgcn_readlane(tile.id, at);
+    const __amdgpu_buffer_rsrc_t ra = rsrc(k.a + static_cast<size_t>(n.lead) * k.rank * k.d_in,
+                                           static_cast<size_t>(k.rank) * k.d_in * 2);
+    const int at_k = from_step * 32 + quad * 8;
+    const uint32_t from = static_cast<uint32_t>((n.rt * 16 + col) * k.d_in + begin + at_k) * 2u;
+#pragma unroll
+    for (int s = 0; s < kHalf; ++s)
+      n.w[s] = fetch16(ra, s * 32 + at_k < width ? from + static_cast<uint32_t>(s) * 64u : kOutside);
+  };
+  f32x4 acc[CG];
+  auto finish = [&](const Half& n, int half) {
+    const int item = wave + half / kHalves * kWaves, from_step = half % kHalves * kHalf;
+    if (item >= items) return;
+    const uint16_t* xs = staged + (n.first + col) * kPitch + from_step * 32 + quad * 8;
+    if (from_step == 0) {
+#pragma unroll
+      for (int c = 0; c < CG; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int s = 0; s < kHalf; ++s)
+#pragma unroll
+      for (int q = 0; q < kParts; ++q)
+#pragma unroll
+        for (int c = 0; c < CG; ++c)
+          acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf16x8, n.w[s]),
+              *reinterpret_cast<const bf16x8*>(xs + q * kPlane + c * kGroup * kPitch + s * 32), acc[c], 0, 0, 0);
+    if (from_step + kHalf != kSteps) return;
+#pragma unroll
+    for (int c = 0; c < CG; ++c) {
+      const int first = n.first + c * kGroup;
+      if (tile.mine(first, n.lead))
+        *reinterpret_cast<f32x4*>(k.low + ((static_cast<size_t>(blockIdx.y) * k.T + t0 + first + col) * RT + n.rt) * 16 + quad * 4) = acc[c];
+    }
+  };
+  load(even, 0);
+#pragma unroll
+  for (int u = 0; u < NB; ++u) {
+    const int f = threadIdx.x + u * kThreads, r = f / kPerRow, c = f % kPerRow * kPer;
+    if constexpr (kParts == 1) {
+      *reinterpret_cast<u32x4*>(staged + r * kPitch + c) = v[u];
+    } else {
+      const Parts4 s = split4(__builtin_bit_cast(f32x4, v[u]));
+#pragma unroll
+      for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(staged + q * kPlane + r * kPitch + c) = s.p[q];
     }
   }
   __syncthreads();
-  const OT* base = k.base != nullptr ? static_cast<const OT*>(k.base) + static_cast<size_t>(t) * k.d_out : nullptr;
-  OT* out = static_cast<OT*>(k.out) + static_cast<size_t>(t) * k.d_out;
-  for (int o = threadIdx.x; o < k.d_out; o += THREADS) {
-    float s = 0.f;
-    if (on) {
-      const uint16_t* b = k.b + (static_cast<size_t>(id) * k.d_out + o) * k.rank;
-      for (int r = 0; r < k.rank; r += 8) {
-        const u16x8 w = *reinterpret_cast<const u16x8*>(b + r);
+  for (int half = 0; wave + half / kHalves * kWaves < items; half += 2) {
+    load(odd, half + 1);
+    finish(even, half);
+    load(even, half + 2);
+    finish(odd, half + 1);
+  }
+}
+
+// Four values of base and out.
+template <typename OT>
+struct Quad4;
+template <>
+struct Quad4<float> {
+  u32x4 raw;
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t at) { raw = fetch16(r, at); }
+  __device__ __forceinline__ void add_store(__amdgpu_buffer_rsrc_t r, uint32_t at, f32x4 d) const {
+    const f32x4 v = __builtin_bit_cast(f32x4, raw) + d;
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, at, 0, 0);
+  }
+};
+template <>
+struct Quad4<__bf16> {
+  u32x2 raw;
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    raw = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
+  }
+  __device__ __forceinline__ void add_store(__amdgpu_buffer_rsrc_t r, uint32_t at, f32x4 d) const {
+    const f32x4 v = f32x4{lo_of(raw.x), hi_of(raw.x), lo_of(raw.y), hi_of(raw.y)} + d;
+    const bf16x4 o = {static_cast<__bf16>(v.x), static_cast<__bf16>(v.y), static_cast<__bf16>(v.z), static_cast<__bf16>(v.w)};
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, o), r, at, 0, 0);
+  }
+};
+
+// out = base + B (scale low), a tile of tokens and a range of outputs a workgroup.  The pieces' sums are
+// added in order as they are staged.  KT: steps of 32 over the rank.
+//
+// Where at least four tokens share an adapter on average, a wave takes units of a pair and 16 U outputs on the
+// matrix cores, a unit's loads in flight while the one before is multiplied; else (a decode batch of many
+// adapters) the products would compute 16 columns for one or two, and a wave takes a token and 128 outputs,
+// two to a lane.
+constexpr int kManyPairs = kTile / 4;
+
+template <typename OT, int KT>
+__global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
+  constexpr int CG = KT == 1 ? 1 : 2, U = KT == 1 ? 4 : KT == 2 ? 2 : 1;
+  constexpr int kPitch = KT * 32 + 8, kPlane = kTile * kPitch;
+  __shared__ __align__(16) uint16_t staged[3 * kPlane];
+  float* plain = reinterpret_cast<float*>(staged);      // with many pairs: [64][32 KT] in fp32
+  static_assert(kTile * KT * 8 == KT * kThreads && kTile * KT * 32 * 4 <= 3 * kPlane * 2, "the plain values take the place of the parts");
+  const int t0 = blockIdx.x * kTile;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int col = lane & 15, quad = lane >> 4;
+  const int tokens = min(kTile, k.T - t0);
+  // this workgroup's output tiles of 16
+  const int n_out = (k.d_out + 15) / 16, per = (n_out + k.splits - 1) / k.splits;
+  const int o_begin = blockIdx.y * per, o_end = min(n_out, o_begin + per);
+  Tile<CG> tile;
+  tile.fetch(k.ids, t0, k.T);
+  // the rank values of a token are 4 RT pieces of four; ranks past the rank are zeros of zero weights.  (Tokens
+  // without an adapter have none: what the workspace holds there goes nowhere.)
+  f32x4 low[KT];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(bf16_to_f32(w[i]), low[r + i], s);
+  for (int u = 0; u < KT; ++u) {
+    const int f = threadIdx.x + u * kThreads, tok = f / (KT * 8), r4 = f % (KT * 8);
+    low[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (tok < tokens && r4 < RT * 4) {
+      const float* p = k.low + (static_cast<size_t>(t0 + tok) * RT * 4 + r4) * 4;
+      const size_t stride = static_cast<size_t>(k.T) * RT * 16;
+#pragma unroll 8
+      for (int i = 0; i < k.pieces; ++i) low[u] += *reinterpret_cast<const f32x4*>(p + i * stride);
+    }
+  }
+  tile.find(k.n);
+  const int pairs = __popcll(tile.leads);
+  const bool many = pairs > kManyPairs;
+  const size_t row = static_cast<size_t>(k.d_out) * sizeof(OT);
+  const __amdgpu_buffer_rsrc_t rout = rsrc(static_cast<OT*>(k.out) + static_cast<size_t>(t0) * k.d_out, tokens * row);
+  // no base: an empty range, which reads as zeros
+  const __amdgpu_buffer_rsrc_t rbase =
+      k.base != nullptr ? rsrc(static_cast<const OT*>(k.base) + static_cast<size_t>(t0) * k.d_out, tokens * row)
+                        : rsrc(k.out, 0);
+  // the units, pair by pair, in equal runs for the waves
+  const int blocks = (max(0, o_end - o_begin) + U - 1) / U, units = pairs * blocks;
+  const int u_begin = units * wave / kWaves, u_end = units * (wave + 1) / kWaves;
+  struct Unit {
+    u32x4 w[U][KT];
+    Quad4<OT> from[U][CG];
+    int first, lead, o;
+  } even, odd;
+  auto offset = [&](const Unit& n, int u, int c) {
+    const int at = (n.o + u) * 16 + quad * 4, first = n.first + c * kGroup;
+    return tile.mine(first, n.lead) && n.o + u < o_end && at < k.d_out
+               ? static_cast<uint32_t>((first + col) * k.d_out + at) * static_cast<uint32_t>(sizeof(OT)) : kOutside;
+  };
+  auto load = [&](Unit& n, int unit) {
+    if (unit >= u_end) return;
+    const int pair = unit / blocks, place = tile.place(pair);
+    n.lead = __builtin_amdgcn_readlane(tile.id, place);
+    n.first = place & ~(Tile<CG>::kSpan - 1);
+    n.o = o_begin + (unit - pair * blocks) * U;
+    const __amdgpu_buffer_rsrc_t rb = rsrc(k.b + static_cast<size_t>(n.lead) * k.d_out * k.rank,
+                                           static_cast<size_t>(k.d_out) * k.rank * 2);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int s = 0; s < KT; ++s) {
+        const int kk = s * 32 + quad * 8;
+        n.w[u][s] = fetch16(rb, kk < k.rank && n.o + u < o_end ? static_cast<uint32_t>(((n.o + u) * 16 + col) * k.rank + kk) * 2u : kOutside);
+      }
+#pragma unroll
+      for (int c = 0; c < CG; ++c) n.from[u][c].load(rbase, offset(n, u, c));
+    }
+  };
+  // the first unit's loads, before the rank values are there
+  if (!many) load(even, u_begin);
+#pragma unroll
+  for (int u = 0; u < KT; ++u) {
+    const int f = threadIdx.x + u * kThreads, tok = f / (KT * 8), r4 = f % (KT * 8);
+    const int id = __shfl(tile.id, tok, kWave);
+    if (k.scale != nullptr && id >= 0) low[u] *= k.scale[id];
+    if (many) {
+      *reinterpret_cast<f32x4*>(plain + tok * KT * 32 + r4 * 4) = low[u];
+    } else {
+      const Parts4 s = split4(low[u]);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(staged + q * kPlane + tok * kPitch + r4 * 4) = s.p[q];
+    }
+  }
+  // tokens without an adapter
+  const uint64_t none = __ballot(tile.id < 0 && lane < tokens);
+  if (none != 0) {
+    for (int tok = wave; tok < tokens; tok += kWaves) {
+      if (((none >> tok) & 1) == 0) continue;
+      for (int o = o_begin * 16 + lane * 4; o < min(o_end * 16, k.d_out); o += kWave * 4) {
+        const uint32_t off = static_cast<uint32_t>(tok * k.d_out + o) * static_cast<uint32_t>(sizeof(OT));
+        Quad4<OT> from;
+        from.load(rbase, off);
+        from.add_store(rout, off, f32x4{0.f, 0.f, 0.f, 0.f});
       }
     }
-    out[o] = static_cast<OT>(base != nullptr ? static_cast<float>(base[o]) + s : s);
   }
+  __syncthreads();
+  if (many) {
+    const int o_last = min(o_end * 16, k.d_out);
+    for (int tok = wave; tok < tokens; tok += kWaves) {
+      const int id = __builtin_amdgcn_readlane(tile.id, tok);
+      if (id < 0) continue;
+      const uint16_t* b = k.b + static_cast<size_t>(id) * k.d_out * k.rank;
+      const float* low = plain + tok * KT * 32;
+      const OT* base = k.base != nullptr ? static_cast<const OT*>(k.base) + static_cast<size_t>(t0 + tok) * k.d_out : nullptr;
+      OT* out = static_cast<OT*>(k.out) + static_cast<size_t>(t0 + tok) * k.d_out;
+      for (int o = o_begin * 16 + lane; o < o_last; o += 2 * kWave) {
+        const bool two = o + kWave < o_last;
+        const uint16_t *b0 = b + static_cast<size_t>(o) * k.rank, *b1 = two ? b0 + static_cast<size_t>(kWave) * k.rank : b0;
+        float s0 = base != nullptr ? static_cast<float>(base[o]) : 0.f;
+        float s1 = base != nullptr && two ? static_cast<float>(base[o + kWave]) : 0.f;
+        float v0 = 0.f, v1 = 0.f;
+#pragma unroll 2
+        for (int r = 0; r < k.rank; r += 8) {
+          const Eight l = load8(low + r);
+          const u32x4 w0 = *reinterpret_cast<const u32x4*>(b0 + r), w1 = *reinterpret_cast<const u32x4*>(b1 + r);
+          v0 = dot8(w0, l, v0);
+          v1 = dot8(w1, l, v1);
+        }
+        out[o] = static_cast<OT>(s0 + v0);
+        if (two) out[o + kWave] = static_cast<OT>(s1 + v1);
+      }
+    }
+    return;
+  }
+  auto finish = [&](const Unit& n, int unit) {
+    if (unit >= u_end) return;
+#pragma unroll
+    for (int c = 0; c < CG; ++c) {
+      const uint16_t* p = staged + (n.first + c * kGroup + col) * kPitch + quad * 8;
+      bf16x8 v[KT][3];
+#pragma unroll
+      for (int s = 0; s < KT; ++s)
+#pragma unroll
+        for (int q = 0; q < 3; ++q) v[s][q] = *reinterpret_cast<const bf16x8*>(p + q * kPlane + s * 32);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < KT; ++s)
+#pragma unroll
+          for (int q = 2; q >= 0; --q)
+            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, n.w[u][s]), v[s][q], d, 0, 0, 0);
+        n.from[u][c].add_store(rout, offset(n, u, c), d);
+      }
+    }
+  };
+  for (int unit = u_begin; unit < u_end; unit += 2) {
+    load(odd, unit + 1);
+    finish(even, unit);
+    load(even, unit + 2);
+    finish(odd, unit + 1);
+  }
+}
+
+// From this many tokens on, tiles of 64.  At 512 tokens of 64 adapters in random order, rank 16, 1,024 by 2,048, a
+// workgroup a token takes 13.8 us and tiles 18.7, of 8 adapters in runs 12.4 and 9.9; at 1,024 tokens random
+// 15.8 and 19.8, runs (rank 32, 2,048 by 896) 19.8 and 13.2; at 2,048 random 27.9 and 26.5, runs 29.8 and 14.7.
+constexpr int kTileFrom = 768;
+
+// Pieces of d_in: the widest that make 512 workgroups (two for each CU; 1,024 were no faster), as wider ones
+// leave fewer partial sums.  nb: 16-byte pieces of x to a thread.  8 of bf16 take 66 KiB of LDS, two workgroups
+// to a CU; of fp32 (three parts) 99 KiB, one: 4,096 tokens by 2,048 then take 16.5 us, with 4 13.6.
+struct Plan {
+  int nb, piece, pieces, splits, rank_tiles;
+};
+Plan plan_of(const umem_adapter_desc& ad, int T) {
+  Plan p;
+  const int tiles = (T + kTile - 1) / kTile;
+  for (p.nb = ad.xtype == UMEM_F32 ? 4 : 8;; p.nb /= 2) {
+    p.piece = ad.xtype == UMEM_F32 ? piece_width<float>(p.nb) : piece_width<__bf16>(p.nb);
+    p.pieces = (ad.d_in + p.piece - 1) / p.piece;
+    if (p.nb == 1 || static_cast<int64_t>(tiles) * p.pieces >= 512) break;
+  }
+  p.splits = std::max(1, std::min(512 / tiles, (ad.d_out + 127) / 128));
+  p.rank_tiles = (ad.rank + 15) / 16;
+  return p;
 }
 
 }  // namespace
 
-size_t adapter_workspace_bytes(const umem_adapter_desc& ad, int T) { return 0; }
+size_t adapter_workspace_bytes(const umem_adapter_desc& ad, int T) {
+  if (T < kTileFrom) return 0;
+  const Plan p = plan_of(ad, T);
+  return (static_cast<size_t>(p.pieces) * T * p.rank_tiles * 16 * sizeof(float) + 255) / 256 * 256;
+}
 
 hipError_t launch_adapter_add(const umem_adapter_desc& ad, int T, const void* x, const int32_t* ids,
                               const uint16_t* a, const uint16_t* b, const float* scale, const void* base,
                               void* out, void* ws, hipStream_t s) {
   clear_stale_error();
-  const AdapterArgs k{x, ids, a, b, scale, base, out, T, ad.n, ad.rank, ad.d_in, ad.d_out};
-#define UMEM_ADAPTER(XT, OT) \
-  hipLaunchKernelGGL((adapter_token_kernel<XT, OT>), dim3(T), dim3(THREADS), 0, s, k)
-  if (ad.xtype == UMEM_F32 && ad.otype == UMEM_F32) UMEM_ADAPTER(float, float);
-  else if (ad.xtype == UMEM_F32) UMEM_ADAPTER(float, __bf16);
-  else if (ad.otype == UMEM_F32) UMEM_ADAPTER(__bf16, float);
-  else UMEM_ADAPTER(__bf16, __bf16);
+  AdapterArgs k{x, ids, a, b, scale, base, out, T, ad.n, ad.rank, ad.d_in, ad.d_out, 1, nullptr, 0};
+  if (T < kTileFrom) {
+    k.splits = std::max(1, std::min(512 / T, (ad.d_out + 255) / 256));
+    const int rows = (ad.rank + 3) / 4;
+#define UMEM_TOKEN(XT, OT, ROWS) \
+  hipLaunchKernelGGL((token_kernel<XT, OT, ROWS>), dim3(T, k.splits), dim3(kTokenThreads), 0, s, k)
+#define UMEM_ADAPTER(XT, OT)                   \
+  if (rows <= 2) UMEM_TOKEN(XT, OT, 2);        \
+  else if (rows <= 4) UMEM_TOKEN(XT, OT, 4);   \
+  else if (rows <= 8) UMEM_TOKEN(XT, OT, 8);   \
+  else if (rows <= 16) UMEM_TOKEN(XT, OT, 16); \
+  else UMEM_TOKEN(XT, OT, 32);
+    if (ad.xtype == UMEM_F32 && ad.otype == UMEM_F32) { UMEM_ADAPTER(float, float) }
+    else if (ad.xtype == UMEM_F32) { UMEM_ADAPTER(float, __bf16) }
+    else if (ad.otype == UMEM_F32) { UMEM_ADAPTER(__bf16, float) }
+    else { UMEM_ADAPTER(__bf16, __bf16) }
 #undef UMEM_ADAPTER
+#undef UMEM_TOKEN
+    return hipGetLastError();
+  }
+  const Plan p = plan_of(ad, T);
+  const int tiles = (T + kTile - 1) / kTile;
+  k.splits = p.splits;
+  k.low = static_cast<float*>(ws);
+  k.pieces = p.pieces;
+  const dim3 grid(tiles, p.pieces), block(kThreads);
+  const size_t lds = static_cast<size_t>(kTile) * (p.piece + 8) * 2 * (ad.xtype == UMEM_F32 ? 3 : 1);
+#define UMEM_LOW(XT, NB, CG) hipLaunchKernelGGL((low_kernel<XT, NB, CG>), grid, block, lds, s, k, p.rank_tiles)
+#define UMEM_LOW_RANK(XT, NB)                \
+  if (ad.rank <= 32) UMEM_LOW(XT, NB, 1);    \
+  else UMEM_LOW(XT, NB, 2);
+#define UMEM_ADAPTER(XT)                         \
+  if (p.nb == 4) { UMEM_LOW_RANK(XT, 4) }        \
+  else if (p.nb == 2) { UMEM_LOW_RANK(XT, 2) }   \
+  else { UMEM_LOW_RANK(XT, 1) }
+  if (ad.xtype == UMEM_F32) { UMEM_ADAPTER(float) }
+  else if (p.nb == 8) { UMEM_LOW_RANK(__bf16, 8) }
+  else { UMEM_ADAPTER(__bf16) }
+#undef UMEM_ADAPTER
+#undef UMEM_LOW_RANK
+#undef UMEM_LOW
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+#define UMEM_OUT(OT, KT) hipLaunchKernelGGL((out_kernel<OT, KT>), dim3(tiles, p.splits), block, 0, s, k, p.rank_tiles)
+#define UMEM_ADAPTER(OT)                    \
+  if (ad.rank <= 32) UMEM_OUT(OT, 1);       \
+  else if (ad.rank <= 64) UMEM_OUT(OT, 2);  \
+  else UMEM_OUT(OT, 4);
+  if (ad.otype == UMEM_F32) { UMEM_ADAPTER(float) }
+  else { UMEM_ADAPTER(__bf16) }
+#undef UMEM_ADAPTER
+#undef UMEM_OUT
   return hipGetLastError();
 }
 

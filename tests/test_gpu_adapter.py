@@ -72,7 +72,9 @@ def check(s, ids, out):
 SIZES = [(1, 1, 8, 8, 8), (1, 3, 16, 1024, 2048), (2, 2, 128, 264, 136), (5, 64, 16, 72, 4096), (16, 4, 24, 1000, 1000),
          (17, 9, 8, 4096, 512), (33, 2, 64, 2048, 896), (64, 64, 16, 1024, 2048), (100, 7, 40, 520, 1032),
          (255, 3, 32, 128, 264), (300, 300, 8, 64, 64), (513, 5, 56, 1024, 336), (1000, 12, 16, 2048, 896),
-         (2049, 16, 32, 256, 520), (4096, 3, 8, 64, 1024)]
+         (2049, 16, 32, 256, 520), (4096, 3, 8, 64, 1024), (767, 9, 16, 512, 264), (768, 9, 16, 512, 264),
+         (800, 50, 72, 1024, 520), (1024, 1024, 8, 64, 200), (1030, 6, 128, 136, 264), (4097, 3, 48, 2048, 64),
+         (4100, 5, 16, 4096, 72)]
 TYPES = [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16")]
 
 
@@ -102,7 +104,7 @@ def test_adapters(i, size, kind):
         assert torch.equal(out, want)
 
 
-@pytest.mark.parametrize("T", [1, 37, 700])
+@pytest.mark.parametrize("T", [1, 37, 700, 2001])
 def test_tokens_without_an_adapter(T):
     """ids outside [0, n): the base as it is (or zeros), whatever x holds there."""
     s = make(T, 3, 16, 256, 512, 2)
@@ -124,29 +126,50 @@ def test_tokens_without_an_adapter(T):
         check(part, ids[few], out[few])
 
 
-def test_nan_stays_with_its_token_and_adapter():
-    s = make(64, 4, 16, 256, 512, 4)
-    ids = (torch.arange(64, device="cuda") % 4).to(torch.int32)
+@pytest.mark.parametrize("T", [64, 2048])
+def test_nan_stays_with_its_token_and_adapter(T):
+    s = make(T, 4, 16, 256, 512, 4)
+    ids = (torch.arange(T, device="cuda") % 4).to(torch.int32)
     clean = call(s, ids).clone()
     s["x"][10, 3] = float("nan")
     s["a"][3] = float("inf")
     out = call(s, ids)
-    rest = [t for t in range(64) if t != 10 and t % 4 != 3]
+    rest = [t for t in range(T) if t != 10 and t % 4 != 3]
     assert torch.equal(out[rest], clean[rest])
     assert torch.isnan(out[10]).all() and not torch.isfinite(out[3]).any()
 
 
-def test_every_digit_of_the_input_counts():
+@pytest.mark.parametrize("T", [3, 2000])
+def test_every_digit_of_the_input_counts(T):
     """x = 1 + 2^-23 against weights that cancel its leading part: a rounded x would give zero."""
-    s = make(3, 1, 8, 64, 64, 6, base=False, scale=False)
+    s = make(T, 1, 8, 64, 64, 6, base=False, scale=False)
     s["x"].fill_(1.0)
     s["x"][:, 0] = 1.0 + 2.0 ** -23
     s["a"].zero_()
     s["a"][0, 0, 0], s["a"][0, 0, 1] = 1.0, -1.0
     s["b"].zero_()
     s["b"][0, :, 0] = 1.0
-    out = call(s, torch.zeros(3, dtype=torch.int32, device="cuda"))
+    out = call(s, torch.zeros(T, dtype=torch.int32, device="cuda"))
     assert torch.equal(out, torch.full_like(out, 2.0 ** -23))
+
+
+@pytest.mark.parametrize("T", [2, 2000])
+def test_largest_values_and_infinities(T):
+    """The largest fp32 values stay finite on the way, an infinity is itself."""
+    s = make(T, 1, 8, 64, 64, 6, base=False, scale=False)
+    big = torch.finfo(torch.float32).max
+    s["x"].zero_()
+    s["x"][:, 0] = big
+    s["x"][1, 0] = float("inf")
+    s["a"].zero_()
+    s["a"][0, :, 0] = 0.5
+    s["b"].zero_()
+    s["b"][0, :, 0] = 1.0
+    s["b"][0, :, 1] = -0.5
+    out = call(s, torch.zeros(T, dtype=torch.int32, device="cuda"))
+    rest = torch.arange(T, device="cuda") != 1
+    want = torch.full_like(out[rest], big * 0.25)
+    assert ((out[rest] - want).abs() <= 4 * u * want).all() and not torch.isfinite(out[1]).any()
 
 
 def test_offsets_past_32_bits():
@@ -161,7 +184,7 @@ def test_offsets_past_32_bits():
     check({**s, "x": s["x"][at]}, ids[at], out[at])
 
 
-@pytest.mark.parametrize("T", [3, 64, 900])
+@pytest.mark.parametrize("T", [3, 64, 900, 3000])
 def test_captured_and_on_another_stream(T):
     s = make(T, 6, 16, 512, 1024, 12)
     ids = ids_of("random", T, 6, s["g"])
