@@ -2,9 +2,9 @@
 //
 //   sumsq = sum_i g_i^2,  norm = sqrt(sumsq);   out = g c,  c = 1 if norm <= max else max / norm
 //
-// Both passes stream: the norm reads every element once, the clip reads and writes it.  The tensors
-// travel in the kernel's arguments, up to 64 a launch, so a step's call copies nothing to the GPU and
-// can be captured.  A tensor is cut into pieces of one size, a workgroup each; a piece's sum of squares
+// Both passes stream: the norm reads every element once, the clip reads and writes it, from the last piece to
+// the first, so that it begins with what the norm left in the caches.  The tensors travel in the kernel's
+// arguments, up to 112 a launch, so a step's call copies nothing to the GPU and can be captured.  A tensor is cut into pieces of one size, a workgroup each; a piece's sum of squares
 // is fp64 (the square of a float is exact there, and the conversion and the addition cost less than the
 // load), written to its own place and added up in order by one workgroup.
 #include <algorithm>
@@ -15,7 +15,7 @@ namespace umem {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int kTable = 64;                     // tensors in one launch's arguments: 3.6 of 4 KiB
+constexpr int kTable = 112, kCounted = 8;      // tensors in one launch's arguments; with rows counted on the GPU
 constexpr int64_t kPiece = 8192;               // elements of the smallest piece
 constexpr int64_t kPieces = 8192;              // pieces of a call, about, from which they get larger
 
@@ -25,22 +25,29 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 struct Tensor {
   const void* grad;
   void* out;
-  const int32_t* n_rows;
-  int64_t rows, row_len;
-  int32_t bf16;
+  int64_t count;                               // elements; bit 62: of bf16
   int32_t first;                               // its first piece in the launch
+  int32_t counted;                             // its place among the counted ones, or -1
+};
+struct Counted {
+  const int32_t* n_rows;
+  int64_t row_len;
 };
 struct Table {
   Tensor t[kTable];
+  Counted c[kCounted];
 };
-static_assert(sizeof(Tensor) == 48, "the table has to fit the 4 KiB of a kernel's arguments");
+constexpr int64_t kBf16 = INT64_C(1) << 62;
+static_assert(sizeof(Table) <= 4096 - 256, "the table has to fit the 4 KiB of a kernel's arguments");
 
 // The tensor of piece `b`: the last one that starts at or before it (tensors without elements have no
 // pieces and are left out of the table; unused places start past every piece).
 __device__ __forceinline__ int tensor_of(const Table& tab, int b) {
   const int lane = threadIdx.x & (kWave - 1);
-  const uint64_t before = __ballot(tab.t[lane].first <= b);
-  return __builtin_amdgcn_readfirstlane(__popcll(before) - 1);
+  const int hi = kWave + lane;
+  int before = __popcll(__ballot(tab.t[lane].first <= b));
+  before += __popcll(__ballot(hi < kTable && tab.t[min(hi, kTable - 1)].first <= b));
+  return __builtin_amdgcn_readfirstlane(before - 1);
 }
 
 // A piece is [u0, u1) of its tensor's elements counted from the 16-byte boundary at or before the first
@@ -48,13 +55,16 @@ __device__ __forceinline__ int tensor_of(const Table& tab, int b) {
 struct Piece {
   int64_t u0, u1, shift, end;
 };
-__device__ __forceinline__ Piece piece_of(const Tensor& t, int b, int64_t size, int esize) {
+__device__ __forceinline__ Piece piece_of(const Table& tab, const Tensor& t, int b, int64_t size, int esize) {
   Piece p;
   p.shift = static_cast<int64_t>((reinterpret_cast<uintptr_t>(t.grad) & 15) / esize);
-  int64_t rows = t.rows;
-  if (t.n_rows != nullptr) rows = min(rows, static_cast<int64_t>(max(*t.n_rows, 0)));
-  p.end = rows * t.row_len + p.shift;
-  p.u0 = (b - t.first) * size;
+  int64_t count = t.count & ~kBf16;
+  if (t.counted >= 0) {
+    const Counted& c = tab.c[t.counted];
+    count = min(count, static_cast<int64_t>(max(*c.n_rows, 0)) * c.row_len);
+  }
+  p.end = count + p.shift;
+  p.u0 = static_cast<int64_t>(b - t.first) * size;
   p.u1 = min(p.u0 + size, p.end);
   return p;
 }
@@ -119,8 +129,9 @@ __device__ __forceinline__ double piece_squares(const Tensor& t, const Piece& p)
 __global__ __launch_bounds__(THREADS) void squares_kernel(Table tab, int64_t size, double* part) {
   __shared__ double lds[THREADS / kWave];
   const Tensor& t = tab.t[tensor_of(tab, blockIdx.x)];
-  const Piece p = piece_of(t, blockIdx.x, size, t.bf16 ? 2 : 4);
-  double s = t.bf16 ? piece_squares<__bf16>(t, p) : piece_squares<float>(t, p);
+  const bool bf16 = (t.count & kBf16) != 0;
+  const Piece p = piece_of(tab, t, blockIdx.x, size, bf16 ? 2 : 4);
+  double s = bf16 ? piece_squares<__bf16>(t, p) : piece_squares<float>(t, p);
   s = wave_sum_f64(s);
   if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = s;
   __syncthreads();
@@ -166,8 +177,11 @@ __device__ __forceinline__ void piece_scale(const Tensor& t, const Piece& p, flo
   const int64_t from = max(p.u0, p.shift);
   if (((reinterpret_cast<uintptr_t>(t.grad) ^ reinterpret_cast<uintptr_t>(t.out)) & 15) != 0) {
     // the two lie differently to the 16-byte boundaries: element by element
+    const T* __restrict__ from_in = in;        // (they are apart, or they would lie alike)
+    T* __restrict__ to = out;
+#pragma unroll 8
     for (int64_t e = from + threadIdx.x; e < p.u1; e += THREADS)
-      out[e] = static_cast<T>(static_cast<float>(in[e]) * c);
+      to[e] = static_cast<T>(static_cast<float>(from_in[e]) * c);
     return;
   }
   const int64_t step = static_cast<int64_t>(THREADS) * kPer;
@@ -193,10 +207,12 @@ __device__ __forceinline__ void piece_scale(const Tensor& t, const Piece& p, flo
 __global__ __launch_bounds__(THREADS) void clip_kernel(Table tab, int64_t size, float max_norm, const float* norm) {
   const float v = *norm;
   const float c = v <= max_norm ? 1.0f : max_norm / v;
-  const Tensor& t = tab.t[tensor_of(tab, blockIdx.x)];
+  const int b = gridDim.x - 1 - blockIdx.x;
+  const Tensor& t = tab.t[tensor_of(tab, b)];
   if (c == 1.0f && t.out == t.grad) return;      // times one in place
-  const Piece p = piece_of(t, blockIdx.x, size, t.bf16 ? 2 : 4);
-  if (t.bf16) piece_scale<__bf16>(t, p, c);
+  const bool bf16 = (t.count & kBf16) != 0;
+  const Piece p = piece_of(tab, t, b, size, bf16 ? 2 : 4);
+  if (bf16) piece_scale<__bf16>(t, p, c);
   else piece_scale<float>(t, p, c);
 }
 
@@ -214,28 +230,33 @@ int64_t pieces_of(const umem_grad& g, int64_t size) {
   return (count + shift + size - 1) / size;
 }
 
-// The launches of a call: up to kTable tensors each; go(table, pieces, pieces before them).
-template <typename Go>
-hipError_t each_table(int n, const umem_grad* grads, int64_t size, Go go) {
-  hipError_t e = hipSuccess;
-  int64_t before = 0;
-  for (int i = 0; i < n && e == hipSuccess;) {
-    Table tab;
-    int used = 0;
-    int64_t pieces = 0;
-    for (; i < n && used < kTable; ++i) {
-      const int64_t mine = pieces_of(grads[i], size);
-      if (mine == 0) continue;
-      tab.t[used++] = {grads[i].grad, grads[i].out, grads[i].n_rows, grads[i].rows, grads[i].row_len,
-                       grads[i].dtype == UMEM_BF16, static_cast<int32_t>(pieces)};
-      pieces += mine;
-    }
-    if (used == 0) break;
-    for (int j = used; j < kTable; ++j) tab.t[j] = {nullptr, nullptr, nullptr, 0, 0, 0, INT32_MAX};
-    e = go(tab, static_cast<int>(pieces), before);
-    before += pieces;
+// One launch's tensors: from grads[*i] on, or back from grads[*i - 1], as many as fit, in the list's order.
+// Returns their pieces.
+int fill_table(const umem_grad* grads, int n, int64_t size, bool back, int* i, Table* tab) {
+  int at[kTable], used = 0, counted = 0;
+  while (used < kTable && (back ? *i > 0 : *i < n)) {
+    const int k = back ? *i - 1 : *i;
+    const bool some = pieces_of(grads[k], size) > 0;
+    if (some && grads[k].n_rows != nullptr && counted == kCounted) break;
+    *i += back ? -1 : 1;
+    if (!some) continue;
+    counted += grads[k].n_rows != nullptr ? 1 : 0;
+    at[used++] = k;
   }
-  return e;
+  if (back) std::reverse(at, at + used);
+  int pieces = 0, c = 0;
+  for (int j = 0; j < used; ++j) {
+    const umem_grad& g = grads[at[j]];
+    tab->t[j] = {g.grad, g.out, g.rows * g.row_len | (g.dtype == UMEM_BF16 ? kBf16 : 0), pieces, -1};
+    if (g.n_rows != nullptr) {
+      tab->t[j].counted = c;
+      tab->c[c++] = {g.n_rows, g.row_len};
+    }
+    pieces += static_cast<int>(pieces_of(g, size));
+  }
+  for (int j = used; j < kTable; ++j) tab->t[j] = {nullptr, nullptr, 0, INT32_MAX, -1};
+  for (; c < kCounted; ++c) tab->c[c] = {nullptr, 0};
+  return pieces;
 }
 
 }  // namespace
@@ -252,12 +273,15 @@ hipError_t launch_grad_norm(int n, const umem_grad* grads, float* norm, double* 
   const int64_t size = piece_size(n, grads);
   double* part = static_cast<double*>(ws);
   int64_t total = 0;
-  hipError_t e = each_table(n, grads, size, [&](const Table& tab, int pieces, int64_t before) {
-    hipLaunchKernelGGL(squares_kernel, dim3(pieces), dim3(THREADS), 0, s, tab, size, part + before);
-    total = before + pieces;
-    return hipGetLastError();
-  });
-  if (e != hipSuccess) return e;
+  for (int i = 0; i < n;) {
+    Table tab;
+    const int pieces = fill_table(grads, n, size, false, &i, &tab);
+    if (pieces == 0) break;
+    hipLaunchKernelGGL(squares_kernel, dim3(pieces), dim3(THREADS), 0, s, tab, size, part + total);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    total += pieces;
+  }
   hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kSumThreads), 0, s, part, static_cast<int>(total), norm, sumsq);
   return hipGetLastError();
 }
@@ -265,10 +289,15 @@ hipError_t launch_grad_norm(int n, const umem_grad* grads, float* norm, double* 
 hipError_t launch_grad_clip(int n, const umem_grad* grads, float max_norm, const float* norm, hipStream_t s) {
   clear_stale_error();
   const int64_t size = piece_size(n, grads);
-  return each_table(n, grads, size, [&](const Table& tab, int pieces, int64_t) {
+  for (int i = n; i > 0;) {
+    Table tab;
+    const int pieces = fill_table(grads, n, size, true, &i, &tab);
+    if (pieces == 0) break;
     hipLaunchKernelGGL(clip_kernel, dim3(pieces), dim3(THREADS), 0, s, tab, size, max_norm, norm);
-    return hipGetLastError();
-  });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace umem

@@ -654,30 +654,31 @@ umem_status check_grads(int32_t n, const umem_grad* grads, bool for_clip) {
   return UMEM_OK;
 }
 
-// Whether an out overlaps another gradient or out, or its own gradient other than being it: one pass
-// over all of them in the order of their addresses, with the furthest ends so far.
+// Whether an out overlaps another gradient or out, or its own gradient other than being it.
 bool grads_clash(int32_t n, const umem_grad* grads) {
   struct Range {
     uintptr_t from, to;
-    bool written;
   };
-  static_assert(2 * kMaxGrads * sizeof(Range) <= 128 << 10, "the ranges live on the caller's stack");
-  Range r[2 * kMaxGrads];
-  int m = 0;
+  static_assert(2 * kMaxGrads * sizeof(Range) <= 64 << 10, "the ranges live on the caller's stack");
+  Range out[kMaxGrads], in[kMaxGrads];
+  int outs = 0, ins = 0;
   for (int i = 0; i < n; ++i) {
     const umem_grad& g = grads[i];
     const uintptr_t bytes = static_cast<uintptr_t>(g.rows) * g.row_len * esize(static_cast<int32_t>(g.dtype));
     if (bytes == 0) continue;
-    const uintptr_t in = reinterpret_cast<uintptr_t>(g.grad), out = reinterpret_cast<uintptr_t>(g.out);
-    r[m++] = {out, out + bytes, true};
-    if (in != out) r[m++] = {in, in + bytes, false};
+    const uintptr_t a = reinterpret_cast<uintptr_t>(g.grad), b = reinterpret_cast<uintptr_t>(g.out);
+    out[outs++] = {b, b + bytes};
+    if (a != b) in[ins++] = {a, a + bytes};
   }
-  std::sort(r, r + m, [](const Range& a, const Range& b) { return a.from < b.from; });
-  uintptr_t any = 0, written = 0;
-  for (int i = 0; i < m; ++i) {
-    if (r[i].from < (r[i].written ? any : written)) return true;
-    any = std::max(any, r[i].to);
-    if (r[i].written) written = std::max(written, r[i].to);
+  const auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
+  if (!std::is_sorted(out, out + outs, before)) std::sort(out, out + outs, before);
+  if (!std::is_sorted(in, in + ins, before)) std::sort(in, in + ins, before);
+  for (int i = 1; i < outs; ++i)
+    if (out[i].from < out[i - 1].to) return true;
+  // the outs are apart: a gradient meets the last that starts at or before it, or the next
+  for (int i = 0, j = 0; i < ins; ++i) {
+    while (j < outs && out[j].from <= in[i].from) ++j;
+    if ((j > 0 && out[j - 1].to > in[i].from) || (j < outs && out[j].from < in[i].to)) return true;
   }
   return false;
 }

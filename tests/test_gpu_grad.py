@@ -117,6 +117,18 @@ def test_more_tensors_than_one_launch_takes():
     assert abs(float(sumsq) - B.global_norm([g.double().cpu().numpy() for g in grads]) ** 2) <= 1e-11 * float(sumsq)
 
 
+def test_many_counted_on_the_gpu():
+    """More tensors with their rows on the GPU than one launch takes, others between them."""
+    shapes = [((i * 7) % 40 + 1, 33) if i % 3 == 0 else (100 + i,) for i in range(61)]
+    grads = make(shapes, 13, {4, 9, 30})
+    outs = [torch.full_like(g, 9.0) for g in grads]
+    n_rows = {i: torch.tensor([(i * 5) % 50], dtype=torch.int32, device="cuda") for i in range(0, 61, 3)}
+    tab = table(grads, outs, n_rows)
+    norm = norm_of(tab)
+    U.check(U.umem_grad_clip(len(tab), tab, 0.02, norm))
+    check(grads, outs, 0.02, norm, n_rows)
+
+
 def test_nothing_to_sum():
     norm = norm_of((U.umem_grad * 1)(), 0)
     assert float(norm) == 0.0
