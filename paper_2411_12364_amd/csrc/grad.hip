@@ -7,6 +7,12 @@
 // arguments, up to 112 a launch, so a step's call copies nothing to the GPU and can be captured.  A tensor is cut into pieces of one size, a workgroup each; a piece's sum of squares
 // is fp64 (the square of a float is exact there, and the conversion and the addition cost less than the
 // load), written to its own place and added up in order by one workgroup.
+//
+// Bound by HBM.  The clip's loads and stores are marked as not to be kept: kept in the 256 MB cache, written
+// lines were evicted while later kernels read, and 786 MB of gradients took 432 us in both passes together,
+// 386 so (norm 125 and clip 251, 6.3 TB/s each; 82 MB 52 and 45 us, 16 MB 20 either way, also with a reader
+// of the results behind).  The norm's loads are kept, for the clip: marked as well they made the norm 111 us
+// and the clip 272.
 #include <algorithm>
 
 #include "umem_internal.h"
@@ -189,9 +195,9 @@ __device__ __forceinline__ void piece_scale(const Tensor& t, const Piece& p, flo
   while (u + (kDeep - 1) * step + kPer <= p.u1 && u >= from) {
     u32x4 x[kDeep];
 #pragma unroll
-    for (int i = 0; i < kDeep; ++i) x[i] = *reinterpret_cast<const u32x4*>(in + u + i * step);
+    for (int i = 0; i < kDeep; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(in + u + i * step));
 #pragma unroll
-    for (int i = 0; i < kDeep; ++i) *reinterpret_cast<u32x4*>(out + u + i * step) = scaled<T>(x[i], c);
+    for (int i = 0; i < kDeep; ++i) __builtin_nontemporal_store(scaled<T>(x[i], c), reinterpret_cast<u32x4*>(out + u + i * step));
     u += kDeep * step;
   }
   for (; u < p.u1; u += step) {
