@@ -429,7 +429,8 @@ typedef struct umem_grad {
 } umem_grad;
 
 /* Scratch bytes umem_grad_norm needs for n gradients.  `grads` is HOST memory, here and below: it is
- * read before the call returns.  n <= 2048 (UMEM_ERR_UNSUPPORTED beyond), rows * row_len <= 2^40. */
+ * read before the call returns.  n <= 2048 and at most 2^40 elements in all (UMEM_ERR_UNSUPPORTED
+ * beyond).  The size depends on n and the gradients' sizes and types alone, not on where they lie. */
 UMEM_API umem_status umem_grad_workspace_size(int32_t n, const umem_grad* grads, size_t* bytes);
 
 /* The global norm of n gradients: *sumsq = sum over all of them of g^2, *norm = sqrt(*sumsq).

@@ -228,12 +228,11 @@ int64_t piece_size(int n, const umem_grad* grads) {
   return std::max<int64_t>(1, (total / kPieces + kPiece - 1) / kPiece) * kPiece;
 }
 
+// Pieces of a tensor that starts anywhere between two 16-byte boundaries, so that the workspace a program
+// sized once does for its gradients wherever they lie.
 int64_t pieces_of(const umem_grad& g, int64_t size) {
-  const int64_t count = g.rows * g.row_len;
-  if (count == 0) return 0;
-  const int64_t esize = g.dtype == UMEM_BF16 ? 2 : 4;
-  const int64_t shift = static_cast<int64_t>((reinterpret_cast<uintptr_t>(g.grad) & 15) / esize);
-  return (count + shift + size - 1) / size;
+  const int64_t count = g.rows * g.row_len, shift = g.dtype == UMEM_BF16 ? 7 : 3;
+  return count == 0 ? 0 : (count + shift + size - 1) / size;
 }
 
 // One launch's tensors: from grads[*i] on, or back from grads[*i - 1], as many as fit, in the list's order.

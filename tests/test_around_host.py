@@ -208,3 +208,25 @@ def test_adapter_refusals():
             assert U.umem_adapter_add(*args, None, need, 0) == WS
             assert U.umem_adapter_add(*args, at(20), need - 1, 0) == WS
             assert U.umem_adapter_add(*args, at(20) + 16, need, 0) == WS
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """Without a stream the current device's is taken: a tensor that lives elsewhere is an error, not a launch."""
+    class Elsewhere:
+        is_cuda = True
+        is_contiguous = staticmethod(lambda: True)
+        data_ptr = staticmethod(lambda: at(0))
+        get_device = staticmethod(lambda: 1)
+
+    monkeypatch.setattr(U, "_get_device", lambda: 0)
+    monkeypatch.setattr(U, "_raw_stream", lambda device: 0)
+    x = Elsewhere()
+    calls = [lambda s: U.umem_block_in(bd(), 0, x, x, x, x, s), lambda s: U.umem_block_out(bd(), 0, x, x, None, x, x, x, stream=s),
+             lambda s: U.umem_block_in_backward(bd(), 0, x, x, x, x, x, x, x, 0, x, 0, s),
+             lambda s: U.umem_block_out_backward(bd(), 0, x, None, x, x, x, x, x, None, x, x, 0, x, 0, s),
+             lambda s: U.umem_grad_norm(-1, None, x, None, x, 0, s), lambda s: U.umem_grad_clip(-1, None, 1.0, x, s),
+             lambda s: U.umem_adapter_add(ad(), 0, x, x, x, x, x, x, x, stream=s)]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call(None)
+        assert call(7) in (OK, ARG)                                     # a stream given: the caller's word

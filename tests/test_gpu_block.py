@@ -116,6 +116,9 @@ def test_entry(i, size, kind):
     U.check(U.umem_block_in(bd, T, x.h, x.gamma, x.beta, n))
     want = B.block_in(host(x.h), kind, host(x.gamma), host(x.beta), EPS)
     within(n, want, norm_tol(host(x.h), kind, host(x.gamma), want, y), "n")
+    if h == y:                                                           # in place: the same bits
+        U.check(U.umem_block_in(bd, T, x.h, x.gamma, x.beta, x.h))
+        assert torch.equal(x.h, n)
 
 
 @pytest.mark.parametrize("i,size", enumerate(SIZES), ids=["%dx%d" % s for s in SIZES])
