@@ -64,23 +64,21 @@ __device__ __forceinline__ float dot8(u32x4 w, const Eight& x, float s) {
   return s;
 }
 
-__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-__device__ __forceinline__ f32x4 load4(const __bf16* p) {
-  const u32x2 a = *reinterpret_cast<const u32x2*>(p);
-  return {lo_of(a.x), hi_of(a.x), lo_of(a.y), hi_of(a.y)};
-}
-__device__ __forceinline__ void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
-__device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
-  *reinterpret_cast<bf16x4*>(p) = bf16x4{static_cast<__bf16>(v.x), static_cast<__bf16>(v.y),
-                                         static_cast<__bf16>(v.z), static_cast<__bf16>(v.w)};
-}
-
 // ---------------------------------------------------------------- few tokens
 
-constexpr int kTokenThreads = 256, kTokenWaves = kTokenThreads / kWave;
-constexpr int kAhead = 8;      // 16-byte pieces of B that a thread loads before A x is known
+// 64 tokens of 64 adapters, rank 16, 1,024 by 2,048: 4.0 us, with 256 or 1,024 threads to a token 4.6.
+constexpr int kTokenThreads = 512, kTokenWaves = kTokenThreads / kWave;
+constexpr int kAhead = 8;      // 16-byte pieces of B that a thread has in flight
 
-// ROWS: rows of A a wave takes, rank <= 4 ROWS.
+// A thread's pieces of B, kAhead of them: outputs kTokenThreads apart, each of rank / 8 pieces, and base beside
+// the first piece of each.
+template <typename OT>
+struct Pieces {
+  u32x4 w[kAhead];
+  float base[kAhead];
+};
+
+// ROWS: rows of A a wave takes.
 template <typename XT, typename OT, int ROWS>
 __global__ __launch_bounds__(kTokenThreads) void token_kernel(AdapterArgs k) {
   __shared__ __align__(16) float low[kMaxAdapterRank];
@@ -98,19 +96,23 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(AdapterArgs k) {
   }
   const int pieces = k.rank / 8;
   const uint16_t* b = k.b + static_cast<size_t>(id) * k.d_out * k.rank;
-  u32x4 ahead[kAhead];
-  const bool early = pieces * ((per + kTokenThreads - 1) / kTokenThreads) <= kAhead;
-  if (early) {
-    int o = first + threadIdx.x, q = 0;
+  int o_ahead = first + threadIdx.x, q_ahead = 0;       // the next piece to load
+  auto load = [&](Pieces<OT>& n) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      if (o < last) ahead[i] = *reinterpret_cast<const u32x4*>(b + static_cast<size_t>(o) * k.rank + q * 8);
-      if (++q == pieces) {
-        q = 0;
-        o += kTokenThreads;
+      if (o_ahead < last) {
+        n.w[i] = *reinterpret_cast<const u32x4*>(b + static_cast<size_t>(o_ahead) * k.rank + q_ahead * 8);
+        if (q_ahead == 0) n.base[i] = base != nullptr ? static_cast<float>(base[o_ahead]) : 0.f;
+      }
+      if (++q_ahead == pieces) {
+        q_ahead = 0;
+        o_ahead += kTokenThreads;
       }
     }
-  }
+  };
+  // the first pieces are on their way before A x is known
+  Pieces<OT> even, odd;
+  load(even);
   // A x: a wave's rows side by side, so that its loads of a step are all in flight together
   const XT* x = static_cast<const XT*>(k.x) + static_cast<size_t>(t) * k.d_in;
   const uint16_t* a = k.a + static_cast<size_t>(id) * k.rank * k.d_in;
@@ -134,26 +136,28 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(AdapterArgs k) {
     if (lane == 0) low[wave + r * kTokenWaves] = s * scale;
   }
   __syncthreads();
-  if (early) {
-    int o = first + threadIdx.x, q = 0;
-    float v = 0.f;
+  int o = first + threadIdx.x, q = 0;
+  float v = 0.f, from = 0.f;
+  auto finish = [&](const Pieces<OT>& n) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      if (o < last) v = dot8(ahead[i], load8(low + q * 8), v);
+      if (q == 0) from = n.base[i];
+      if (o < last) v = dot8(n.w[i], load8(low + q * 8), v);
       if (++q == pieces) {
-        if (o < last) out[o] = static_cast<OT>(base != nullptr ? static_cast<float>(base[o]) + v : v);
+        if (o < last) out[o] = static_cast<OT>(from + v);
         q = 0;
         v = 0.f;
         o += kTokenThreads;
       }
     }
-    return;
-  }
-  for (int o = first + threadIdx.x; o < last; o += kTokenThreads) {
-    float v = 0.f;
-    for (int i = 0; i < pieces; ++i)
-      v = dot8(*reinterpret_cast<const u32x4*>(b + static_cast<size_t>(o) * k.rank + i * 8), load8(low + i * 8), v);
-    out[o] = static_cast<OT>(base != nullptr ? static_cast<float>(base[o]) + v : v);
+  };
+  // pieces left, the same for all threads of the workgroup
+  for (int left = (last - first + kTokenThreads - 1) / kTokenThreads * pieces; left > 0; left -= 2 * kAhead) {
+    if (left > kAhead) load(odd);
+    finish(even);
+    if (left <= kAhead) break;
+    if (left > 2 * kAhead) load(even);
+    finish(odd);
   }
 }
 
@@ -544,10 +548,14 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
   }
 }
 
-// From this many tokens on, tiles of 64.  At 512 tokens of 64 adapters in random order, rank 16, 1,024 by 2,048, a
-// workgroup a token takes 13.8 us and tiles 18.7, of 8 adapters in runs 12.4 and 9.9; at 1,024 tokens random
-// 15.8 and 19.8, runs (rank 32, 2,048 by 896) 19.8 and 13.2; at 2,048 random 27.9 and 26.5, runs 29.8 and 14.7.
-constexpr int kTileFrom = 768;
+// Tiles of 64 from this many ranks of tokens on (1,536 tokens of rank 16, 384 of rank 64).  A workgroup a token
+// does its own A x whoever shares the adapter, a tile shares it but has few workgroups.  In us, a workgroup a
+// token and tiles, for 8 or 16 adapters in runs and for 64 in random order: rank 16, 1,024 by 2,048: 512
+// tokens 7.3, 9.8 and 9.7, 18.7; 1,536 tokens 16.6, 14.6 and 21.7, 25.3; 4,096 tokens random 52, 42.  Rank 32,
+// 2,048 by 896: 768 tokens 15.1, 14.1; 2,048 tokens 29, 14.7.  Rank 64, 2,048 by 2,048: 256 tokens 25.5, 18.1
+// and 27.8, 70; 512 tokens 44, 15.7.
+constexpr int kTileFrom = 24576;
+bool by_tiles(const umem_adapter_desc& ad, int T) { return static_cast<int64_t>(T) * ad.rank >= kTileFrom; }
 
 // Pieces of d_in: the widest that make 512 workgroups (two for each CU; 1,024 were no faster), as wider ones
 // leave fewer partial sums.  nb: 16-byte pieces of x to a thread.  8 of bf16 take 66 KiB of LDS, two workgroups
@@ -571,7 +579,7 @@ Plan plan_of(const umem_adapter_desc& ad, int T) {
 }  // namespace
 
 size_t adapter_workspace_bytes(const umem_adapter_desc& ad, int T) {
-  if (T < kTileFrom) return 0;
+  if (T == 0 || !by_tiles(ad, T)) return 0;
   const Plan p = plan_of(ad, T);
   return (static_cast<size_t>(p.pieces) * T * p.rank_tiles * 16 * sizeof(float) + 255) / 256 * 256;
 }
@@ -581,17 +589,17 @@ hipError_t launch_adapter_add(const umem_adapter_desc& ad, int T, const void* x,
                               void* out, void* ws, hipStream_t s) {
   clear_stale_error();
   AdapterArgs k{x, ids, a, b, scale, base, out, T, ad.n, ad.rank, ad.d_in, ad.d_out, 1, nullptr, 0};
-  if (T < kTileFrom) {
-    k.splits = std::max(1, std::min(512 / T, (ad.d_out + 255) / 256));
-    const int rows = (ad.rank + 3) / 4;
+  if (!by_tiles(ad, T)) {
+    k.splits = std::max(1, std::min(256 / T, (ad.d_out + kTokenThreads - 1) / kTokenThreads));
+    const int rows = (ad.rank + kTokenWaves - 1) / kTokenWaves;
 #define UMEM_TOKEN(XT, OT, ROWS) \
   hipLaunchKernelGGL((token_kernel<XT, OT, ROWS>), dim3(T, k.splits), dim3(kTokenThreads), 0, s, k)
 #define UMEM_ADAPTER(XT, OT)                   \
-  if (rows <= 2) UMEM_TOKEN(XT, OT, 2);        \
+  if (rows <= 1) UMEM_TOKEN(XT, OT, 1);        \
+  else if (rows <= 2) UMEM_TOKEN(XT, OT, 2);   \
   else if (rows <= 4) UMEM_TOKEN(XT, OT, 4);   \
   else if (rows <= 8) UMEM_TOKEN(XT, OT, 8);   \
-  else if (rows <= 16) UMEM_TOKEN(XT, OT, 16); \
-  else UMEM_TOKEN(XT, OT, 32);
+  else UMEM_TOKEN(XT, OT, 16);
     if (ad.xtype == UMEM_F32 && ad.otype == UMEM_F32) { UMEM_ADAPTER(float, float) }
     else if (ad.xtype == UMEM_F32) { UMEM_ADAPTER(float, __bf16) }
     else if (ad.otype == UMEM_F32) { UMEM_ADAPTER(__bf16, float) }

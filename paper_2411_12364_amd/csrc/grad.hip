@@ -148,7 +148,13 @@ constexpr int kSumThreads = 1024;
 __global__ __launch_bounds__(kSumThreads) void norm_kernel(const double* part, int n, float* norm, double* sumsq) {
   __shared__ double lds[kSumThreads / kWave];
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += kSumThreads) s += part[i];
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * kSumThreads) {
+    double v[8];                               // eight in flight, added in order
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = i0 + u * kSumThreads < n ? part[i0 + u * kSumThreads] : 0.0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += v[u];
+  }
   s = wave_sum_f64(s);
   if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = s;
   __syncthreads();

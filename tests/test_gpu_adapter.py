@@ -74,7 +74,8 @@ SIZES = [(1, 1, 8, 8, 8), (1, 3, 16, 1024, 2048), (2, 2, 128, 264, 136), (5, 64,
          (255, 3, 32, 128, 264), (300, 300, 8, 64, 64), (513, 5, 56, 1024, 336), (1000, 12, 16, 2048, 896),
          (2049, 16, 32, 256, 520), (4096, 3, 8, 64, 1024), (767, 9, 16, 512, 264), (768, 9, 16, 512, 264),
          (800, 50, 72, 1024, 520), (1024, 1024, 8, 64, 200), (1030, 6, 128, 136, 264), (4097, 3, 48, 2048, 64),
-         (4100, 5, 16, 4096, 72)]
+         (4100, 5, 16, 4096, 72), (1535, 9, 16, 264, 520), (1536, 9, 16, 264, 520), (192, 3, 128, 520, 264),
+         (400, 90, 64, 264, 1000)]
 TYPES = [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16")]
 
 
