@@ -451,7 +451,8 @@ UMEM_API umem_status umem_grad_norm(int32_t n, const umem_grad* grads, float* no
 UMEM_API umem_status umem_grad_clip(int32_t n, const umem_grad* grads, float max_norm, const float* norm,
                            hipStream_t stream);
 
-/* Low-rank adapters of many requests beside a shared projection (umem_project, umem_query's linear):
+/* Low-rank adapters of many requests beside a shared projection (umem_project's output, or the query
+ * linear: umem_query_adapted below):
  *   out[t] = base[t] + scale[i] B_i (A_i x[t]),  i = ids[t];  out[t] = base[t] where i is not in [0, n) */
 typedef struct umem_adapter_desc {
   int32_t n;      /* adapters */
@@ -479,6 +480,22 @@ UMEM_API umem_status umem_adapter_add(const umem_adapter_desc* ad, int32_t T, co
                              const uint16_t* a, const uint16_t* b, const float* scale,
                              const void* base, void* out, void* ws, size_t ws_bytes,
                              hipStream_t stream);
+
+/* umem_query with low-rank adapters beside its query linear, for tokens t = b * L + l of requests that
+ * each bring an adapter: the linear's output of a token becomes
+ *   W_q y[t] + scale[i] B_i (A_i y[t]),  i = ids[t],  before the LayerNorm,
+ * y the convolved rows as the linear takes them (rounded to bf16, nearest even).
+ *   ad   n and rank; d_in = d_model, d_out = A * heads * dk (row queries, then column queries), xtype
+ *        UMEM_BF16, otype UMEM_F32 (UMEM_ERR_INVALID_ARG otherwise)
+ *   ids, a, b, scale  as for umem_adapter_add; everything else as for umem_query
+ *   ws   16-byte aligned scratch of umem_query_adapted_workspace_size(...) bytes */
+UMEM_API umem_status umem_query_adapted_workspace_size(const umem_query_desc* qd, const umem_adapter_desc* ad,
+                                              int32_t B, int32_t L, size_t* bytes);
+UMEM_API umem_status umem_query_adapted(const umem_query_desc* qd, const umem_adapter_desc* ad, int32_t B, int32_t L,
+                               const float* x, const float* x_hist, const float* conv_w, const uint16_t* w_q,
+                               const int32_t* ids, const uint16_t* a, const uint16_t* b, const float* scale,
+                               const float* gamma, const float* beta, float* q_row, float* q_col, void* ws,
+                               size_t ws_bytes, hipStream_t stream);
 
 /* A static, human-readable name of a status code. */
 UMEM_API const char* umem_status_string(umem_status status);

@@ -44,7 +44,8 @@ EXPORTED = ("umem_workspace_size", "umem_axis_scores", "umem_select", "umem_scor
             "umem_block_in", "umem_block_out", "umem_block_backward_workspace_size",
             "umem_block_in_backward", "umem_block_out_backward",
             "umem_grad_workspace_size", "umem_grad_norm", "umem_grad_clip",
-            "umem_adapter_workspace_size", "umem_adapter_add", "umem_status_string")
+            "umem_adapter_workspace_size", "umem_adapter_add",
+            "umem_query_adapted_workspace_size", "umem_query_adapted", "umem_status_string")
 
 
 class umem_desc(ctypes.Structure):
@@ -130,6 +131,9 @@ def _load() -> ctypes.CDLL:
         "umem_grad_clip": [I32, P, F32, P, P],
         "umem_adapter_workspace_size": [AD, I32, ctypes.POINTER(SZ)],
         "umem_adapter_add": [AD, I32, P, P, P, P, P, P, P, P, SZ, P],
+        "umem_query_adapted_workspace_size": [ctypes.POINTER(umem_query_desc), AD, I32, I32, ctypes.POINTER(SZ)],
+        "umem_query_adapted": [ctypes.POINTER(umem_query_desc), AD, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P, P,
+                               SZ, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -369,3 +373,17 @@ def umem_adapter_workspace_size(ad, T):
 def umem_adapter_add(ad, T, x, ids, a, b, scale, base, out, ws=None, ws_bytes=0, stream=None) -> int:
     return _lib.umem_adapter_add(_d(ad), T, _p(x), _p(ids), _p(a), _p(b), _p(scale), _p(base), _p(out),
                                  _p(ws), ws_bytes, _s(stream, x))
+
+
+def umem_query_adapted_workspace_size(qd, ad, B, L):
+    """Returns (status, bytes)."""
+    out = ctypes.c_size_t(0)
+    st = _lib.umem_query_adapted_workspace_size(_d(qd), _d(ad), B, L, ctypes.byref(out))
+    return st, out.value
+
+
+def umem_query_adapted(qd, ad, B, L, x, x_hist, conv_w, w_q, ids, a, b, scale, gamma, beta, q_row, q_col,
+                       ws, ws_bytes, stream=None) -> int:
+    return _lib.umem_query_adapted(_d(qd), _d(ad), B, L, _p(x), _p(x_hist), _p(conv_w), _p(w_q), _p(ids),
+                                   _p(a), _p(b), _p(scale), _p(gamma), _p(beta), _p(q_row), _p(q_col),
+                                   _p(ws), ws_bytes, _s(stream, x))

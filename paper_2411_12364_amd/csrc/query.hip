@@ -234,7 +234,7 @@ size_t query_workspace_bytes(const umem_query_desc& qd, int64_t T) {
 hipError_t launch_query(const umem_query_desc& qd, int B, int L, const float* x,
                         const float* x_hist, const float* conv_w, const uint16_t* w_q,
                         const float* gamma, const float* beta, float* q_row, float* q_col,
-                        void* ws, hipStream_t s) {
+                        void* ws, const QueryAdapters* adapters, hipStream_t s) {
   clear_stale_error();
   const int T = B * L;
   if (T == 0) return hipSuccess;
@@ -248,8 +248,13 @@ hipError_t launch_query(const umem_query_desc& qd, int B, int L, const float* x,
   hipError_t e = launch_conv(x, qd.conv_k > 1 ? x_hist : nullptr, conv_w, y, T, L, qd.d_model, qd.conv_k, s);
   int splits = 1;
   if (e == hipSuccess) e = gemm_bf16_parts(y, w_q, q_raw, T, nq, qd.d_model, part, s, &splits);
+  // the adapters' share is added to the product, or to the first of its partial sums
+  float* first = splits > 1 ? part : q_raw;
+  if (e == hipSuccess && adapters != nullptr)
+    e = launch_adapter_add(adapters->ad, T, y, adapters->ids, adapters->a, adapters->b, adapters->scale, first, first,
+                           adapters->ws, s);
   if (e == hipSuccess)
-    e = launch_ln<false>(splits > 1 ? part : q_raw, splits, static_cast<size_t>(T) * nq, q_row,
+    e = launch_ln<false>(first, splits, static_cast<size_t>(T) * nq, q_row,
                          qd.shared ? q_row : q_col, gamma, beta,
                          static_cast<size_t>(T) * A * qd.heads, qd.dk, A * qd.heads, qd.heads,
                          qd.eps, s);

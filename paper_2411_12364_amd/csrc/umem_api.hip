@@ -317,6 +317,18 @@ umem_status check_query_desc(const umem_query_desc* qd) {
   return UMEM_OK;
 }
 
+umem_status check_query_ptrs(const umem_query_desc* qd, const float* x, const float* x_hist, const float* conv_w,
+                             const uint16_t* w_q, const float* gamma, const float* beta, const float* q_row,
+                             const float* q_col) {
+  if (!x || !conv_w || !w_q || !gamma || !beta || !q_row) return UMEM_ERR_INVALID_ARG;
+  if ((q_col == nullptr) != (qd->shared == 1)) return UMEM_ERR_INVALID_ARG;
+  if (!aligned(x, 16) || !aligned(x_hist, 16) || !aligned(conv_w, 16) || !aligned(w_q, 16))
+    return UMEM_ERR_INVALID_ARG;
+  if (!aligned(gamma, 4) || !aligned(beta, 4) || !aligned(q_row, 4) || !aligned(q_col, 4))
+    return UMEM_ERR_INVALID_ARG;
+  return UMEM_OK;
+}
+
 umem_status check_query_tokens(int32_t B, int32_t L) {
   if (B < 0 || L < 0) return UMEM_ERR_INVALID_ARG;
   if (static_cast<int64_t>(B) * L > kMaxTokens) return UMEM_ERR_UNSUPPORTED;
@@ -346,16 +358,12 @@ UMEM_API umem_status umem_query(const umem_query_desc* qd, int32_t B, int32_t L,
   if (st == UMEM_OK) st = check_query_tokens(B, L);
   if (st != UMEM_OK) return st;
   if (static_cast<int64_t>(B) * L == 0) return UMEM_OK;
-  if (!x || !conv_w || !w_q || !gamma || !beta || !q_row) return UMEM_ERR_INVALID_ARG;
-  if ((q_col == nullptr) != (qd->shared == 1)) return UMEM_ERR_INVALID_ARG;
-  if (!aligned(x, 16) || !aligned(x_hist, 16) || !aligned(conv_w, 16) || !aligned(w_q, 16))
-    return UMEM_ERR_INVALID_ARG;
-  if (!aligned(gamma, 4) || !aligned(beta, 4) || !aligned(q_row, 4) || !aligned(q_col, 4))
-    return UMEM_ERR_INVALID_ARG;
+  st = check_query_ptrs(qd, x, x_hist, conv_w, w_q, gamma, beta, q_row, q_col);
+  if (st != UMEM_OK) return st;
   const size_t need = query_workspace_bytes(*qd, static_cast<int64_t>(B) * L);
   if (ws == nullptr || !aligned(ws, 16) || ws_bytes < need) return UMEM_ERR_WORKSPACE;
   return hip_status(launch_query(*qd, B, L, x, x_hist, conv_w, w_q, gamma, beta, q_row, q_col, ws,
-                                 stream));
+                                 nullptr, stream));
 }
 
 UMEM_API umem_status umem_key_norm(int32_t heads, int32_t n, int32_t dk, const float* keys,
@@ -761,6 +769,57 @@ UMEM_API umem_status umem_adapter_add(const umem_adapter_desc* ad, int32_t T, co
                      {ws, need}};
   if (!out_fits(y, in, 7, 0)) return UMEM_ERR_INVALID_ARG;
   return hip_status(launch_adapter_add(*ad, T, x, ids, a, b, scale, base, out, ws, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+umem_status check_query_adapters(const umem_query_desc* qd, const umem_adapter_desc* ad, int32_t B, int32_t L) {
+  umem_status st = check_query_desc(qd);
+  if (st == UMEM_OK) st = check_adapter_desc(ad);
+  if (st == UMEM_OK) st = check_query_tokens(B, L);
+  if (st != UMEM_OK) return st;
+  const int64_t nq = static_cast<int64_t>(qd->shared ? 1 : 2) * qd->heads * qd->dk;
+  if (ad->d_in != qd->d_model || ad->d_out != nq || ad->xtype != UMEM_BF16 || ad->otype != UMEM_F32)
+    return UMEM_ERR_INVALID_ARG;
+  return UMEM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+UMEM_API umem_status umem_query_adapted_workspace_size(const umem_query_desc* qd, const umem_adapter_desc* ad,
+                                                       int32_t B, int32_t L, size_t* bytes) {
+  if (bytes == nullptr) return UMEM_ERR_INVALID_ARG;
+  *bytes = 0;
+  const umem_status st = check_query_adapters(qd, ad, B, L);
+  if (st != UMEM_OK) return st;
+  const int64_t T = static_cast<int64_t>(B) * L;
+  *bytes = round_up(query_workspace_bytes(*qd, T)) + adapter_workspace_bytes(*ad, static_cast<int>(T));
+  return UMEM_OK;
+}
+
+UMEM_API umem_status umem_query_adapted(const umem_query_desc* qd, const umem_adapter_desc* ad, int32_t B, int32_t L,
+                                        const float* x, const float* x_hist, const float* conv_w,
+                                        const uint16_t* w_q, const int32_t* ids, const uint16_t* a,
+                                        const uint16_t* b, const float* scale, const float* gamma,
+                                        const float* beta, float* q_row, float* q_col, void* ws, size_t ws_bytes,
+                                        hipStream_t stream) {
+  umem_status st = check_query_adapters(qd, ad, B, L);
+  if (st != UMEM_OK) return st;
+  const int64_t T = static_cast<int64_t>(B) * L;
+  if (T == 0) return UMEM_OK;
+  st = check_query_ptrs(qd, x, x_hist, conv_w, w_q, gamma, beta, q_row, q_col);
+  if (st != UMEM_OK) return st;
+  if (!ids || !a || !b || !aligned(ids, 4) || !aligned(a, 16) || !aligned(b, 16) || !aligned(scale, 4))
+    return UMEM_ERR_INVALID_ARG;
+  const size_t own = round_up(query_workspace_bytes(*qd, T));
+  if (ws == nullptr || !aligned(ws, 16) || ws_bytes < own + adapter_workspace_bytes(*ad, static_cast<int>(T)))
+    return UMEM_ERR_WORKSPACE;
+  const QueryAdapters adapters{*ad, ids, a, b, scale, static_cast<char*>(ws) + own};
+  return hip_status(launch_query(*qd, B, L, x, x_hist, conv_w, w_q, gamma, beta, q_row, q_col, ws, &adapters, stream));
 }
 
 }  // extern "C"

@@ -134,10 +134,18 @@ hipError_t launch_score_backward(const umem_desc& d, int T, const float* q_row, 
 
 // The query front-end and the key LayerNorm (query.hip).  ws: query_workspace_bytes bytes.
 size_t query_workspace_bytes(const umem_query_desc& qd, int64_t T);
+// adapters: those beside the query linear, or NULL; their own scratch of adapter_workspace_bytes bytes.
+struct QueryAdapters {
+  umem_adapter_desc ad;
+  const int32_t* ids;
+  const uint16_t *a, *b;
+  const float* scale;
+  void* ws;
+};
 hipError_t launch_query(const umem_query_desc& qd, int B, int L, const float* x,
                         const float* x_hist, const float* conv_w, const uint16_t* w_q,
                         const float* gamma, const float* beta, float* q_row, float* q_col,
-                        void* ws, hipStream_t s);
+                        void* ws, const QueryAdapters* adapters, hipStream_t s);
 hipError_t launch_key_norm(int heads, int n, int dk, const float* keys, const float* gamma,
                            const float* beta, float eps, float* out, hipStream_t s);
 

@@ -230,3 +230,28 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         with pytest.raises(ValueError):
             call(None)
         assert call(7) in (OK, ARG)                                     # a stream given: the caller's word
+
+
+def test_adapted_query_refusals():
+    qd = U.umem_query_desc(64, 3, 2, 32, 0, 1e-5)                        # 2 axes of 2 heads of 32: 128 outputs
+    good = dict(xtype=1)
+    st, need = U.umem_query_adapted_workspace_size(qd, ad(**good), 4, 5)
+    assert st == OK and need >= U.umem_query_workspace_size(qd, 4, 5)[1]
+    assert U.umem_query_adapted_workspace_size(qd, ad(**good), 0, 5)[0] == OK
+    for kw, want in ((dict(d_in=72), ARG), (dict(d_out=64), ARG), (dict(xtype=0), ARG), (dict(otype=1), ARG), (dict(n=0), ARG),
+                     (dict(rank=12), UNS)):
+        assert U.umem_query_adapted_workspace_size(qd, ad(**{**good, **kw}), 4, 5)[0] == want, kw
+    assert U.umem_query_adapted_workspace_size(U.umem_query_desc(60, 3, 2, 32, 0, 1e-5), ad(**good), 4, 5)[0] == UNS
+    assert U.umem_query_adapted_workspace_size(qd, ad(**good), -1, 5)[0] == ARG
+    names = ["x", "hist", "conv", "wq", "ids", "a", "b", "scale", "gamma", "beta", "q_row", "q_col"]
+    base = {k: at(i) for i, k in enumerate(names)}
+
+    def call(ws=at(20), n=need, B=4, **kw):
+        return U.umem_query_adapted(qd, ad(**good), B, 5, *{**base, **kw}.values(), ws, n, 0)
+
+    for k in ("x", "conv", "wq", "ids", "a", "b", "gamma", "beta", "q_row", "q_col"):
+        assert call(**{k: None}) == ARG, k
+    for k in names:
+        assert call(**{k: base[k] + 2}) == ARG, k
+    assert call(ws=None) == WS and call(ws=at(20) + 8) == WS and call(n=need - 1) == WS
+    assert call(B=0, x=None) == OK and call(B=-1) == ARG

@@ -12,7 +12,10 @@ import pytest
 import torch
 
 import oracle.block_oracle as B
+import oracle.query_oracle as Q
 import paper_2411_12364_amd as U
+import synth as S
+from synth import configs as CF
 
 pytestmark = pytest.mark.gpu
 u = 2.0 ** -24
@@ -216,3 +219,76 @@ def test_captured_and_on_another_stream(T):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want), k
+
+
+# ---------------------------------------------------------------- beside the query linear
+
+FRONT_ENDS = [
+    # one new token of each sequence; a prompt each, cut off at ragged places; enough tokens for the tiles
+    CF.FrontEnd("adapted-decode", B=24, L=1, d_model=256, conv_k=4, heads=2, dk=64, shared=True, seed=51),
+    CF.FrontEnd("adapted-separate", B=3, L=37, d_model=1024, conv_k=3, heads=1, dk=40, shared=False, seed=52, history=False),
+    CF.FrontEnd("adapted-prompts", B=4, L=431, d_model=512, conv_k=4, heads=2, dk=128, shared=True, seed=53),
+]
+
+
+def qdesc(fe):
+    return U.umem_query_desc(fe.d_model, fe.conv_k, fe.heads, fe.dk, int(fe.shared), fe.eps)
+
+
+def row_err(got, want):
+    """Of the largest value of each query."""
+    got, want = got.reshape(-1, want.shape[-1]), want.reshape(-1, want.shape[-1])
+    return float((np.abs(got - want).max(axis=1) / np.abs(want).max(axis=1)).max())
+
+
+# fp32 accumulation, and a rare bf16 rounding of the convolved rows decided the other way
+ROUNDED_RTOL = 2e-3
+
+
+@pytest.mark.parametrize("fe", FRONT_ENDS, ids=[f.name for f in FRONT_ENDS])
+def test_adapted_query(fe):
+    """The front-end with an adapter for each sequence against the oracle's steps with the merged weights, from
+    its own convolved rows rounded to bf16 as the linear takes them; without an adapter for any token, and
+    with adapters of zeros, bit for bit umem_query."""
+    print(f"[case] adapted query {fe.name}", flush=True)
+    inp = CF.front_end_inputs(fe)
+    A, n, rank, nq = (1 if fe.shared else 2), 3, 16, fe.n_queries
+    s = make(fe.T, n, rank, fe.d_model, nq, fe.seed, "bf16", "f32")
+    s["b"] *= 0.5                                                        # adapters of the size of the linear's output
+    seq = torch.randint(-1, n, (fe.B,), generator=s["g"], device="cuda").to(torch.int32)
+    seq[0], seq[1] = 0, -1
+    ids = seq.repeat_interleave(fe.L).contiguous()
+    st, need = U.umem_query_adapted_workspace_size(qdesc(fe), s["desc"], fe.B, fe.L)
+    U.check(st)
+    dev = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()   # noqa: E731
+    args = [dev(inp["x"]), dev(inp["hist"]), dev(inp["conv_w"]), dev(CF.output_major(inp["w_q"]).view(np.int16))]
+    norms = [dev(inp["gamma"]), dev(inp["beta"])]
+    q_row = torch.empty((fe.T, fe.heads, fe.dk), device="cuda")
+    q_col = q_row if fe.shared else torch.empty_like(q_row)
+    st, plain = U.umem_query_workspace_size(qdesc(fe), fe.B, fe.L)
+    U.check(st)
+    ws = torch.empty(max(plain, 256), dtype=torch.uint8, device="cuda")
+    U.check(U.umem_query(qdesc(fe), fe.B, fe.L, *args, *norms, q_row, None if fe.shared else q_col, ws, ws.numel()))
+
+    def call(ids, b=s["b"]):
+        ws = torch.full((max(need, 256),), 0xFF, dtype=torch.uint8, device="cuda")
+        row = torch.empty_like(q_row)
+        col = None if fe.shared else torch.empty_like(q_row)
+        U.check(U.umem_query_adapted(qdesc(fe), s["desc"], fe.B, fe.L, *args, ids, s["a"], b, s["scale"], *norms, row, col,
+                                     ws, ws.numel()))
+        return row, (row if fe.shared else col)
+
+    for got in (call(torch.full_like(ids, -1)), call(ids, torch.zeros_like(s["b"]))):
+        assert torch.equal(got[0], q_row) and torch.equal(got[1], q_col)
+    got = call(ids)
+    y = Q.causal_conv(inp["x"], inp["conv_w"], inp["hist"]).reshape(fe.T, fe.d_model)
+    y = S.bf16_bits_to_f32(S.f32_to_bf16_bits(y.astype(np.float32))).reshape(y.shape).astype(np.float64)
+    wq = S.bf16_bits_to_f32(inp["w_q"]).reshape(inp["w_q"].shape).astype(np.float64)
+    lin = B.adapter_add(y, ids.cpu().numpy(), host(s["a"]), host(s["b"]), host(s["scale"]), Q.query_linear(y, wq))
+    want = Q.layer_norm(lin.reshape(fe.T, A, fe.heads, fe.dk), np.asarray(inp["gamma"], np.float64).reshape(A, fe.heads, fe.dk),
+                        np.asarray(inp["beta"], np.float64).reshape(A, fe.heads, fe.dk), fe.eps)
+    for x, a in ((got[0], 0), (got[1], A - 1)):
+        assert row_err(host(x), want[:, a]) <= ROUNDED_RTOL
+    off = ids.cpu().numpy() < 0                                          # sequences without one: as without any
+    assert torch.equal(got[0][torch.from_numpy(off).cuda()], q_row[torch.from_numpy(off).cuda()])
+    assert not torch.equal(got[0], q_row)
