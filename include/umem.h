@@ -10,6 +10,8 @@
  *   a6  IVE address map    Sec. 3.2 IVE eqs. (13), (14)
  *   a7  gather-sum         eq. (1) o = V^T s; eq. (15) per virtual block; heads add (Sec. 3.1)
  *   a8  projection         eq. (15) sum_p W_p^T (.); Sec. 3.2 Trick 6 output linear
+ * and, for the model around it, the norms before and after a block, the global gradient norm with
+ * clipping, and low-rank adapters beside the projections.
  *
  * Conventions shared by every entry point:
  *   - All array arguments are DEVICE pointers owned by the caller, dense and row-major, unless
@@ -30,7 +32,8 @@
  *     (Additive grid: it is searched at the pairs of places a, b in its axes' orders with
  *     (a+1)(b+1) <= topm, which hold its best scores unless +inf meets -inf.)
  *   - Indices are int32 (n*n < 2^31); byte offsets into the value table are 64-bit.
- *   - Alignment: q/k/core 16 bytes, values and fp32 outputs 16 bytes, other arrays 4 bytes.
+ *   - Alignment: q/k/core 16 bytes, values and fp32 outputs 16 bytes, other arrays 4 bytes, unless
+ *     stated otherwise.
  *   - T == 0 is a no-op once the descriptor is valid.
  *   - Functions are reentrant; calls on one stream run in order.
  */
