@@ -51,7 +51,7 @@ __device__ __forceinline__ void sigmoid_row(Row<PER>& g) {
     for (int i = 0; i < 4; ++i) g.v[p][i] = sigmoid(g.v[p][i]);
 }
 
-template <typename HT, typename YT, int G, int PER, bool FULL>
+template <typename HT, typename YT, int G, int PER, RowEnd END>
 __global__ __launch_bounds__(Group<G>::kThreads) void entry_kernel(EntryArgs k) {
   __shared__ float lds[2][Group<G>::kWaves][2];
   const int lane = Group<G>::lane(), d = k.d;
@@ -59,17 +59,17 @@ __global__ __launch_bounds__(Group<G>::kThreads) void entry_kernel(EntryArgs k) 
   if (row >= k.T) return;                    // whole groups: a group of several waves is a workgroup
   GroupSum<G> gs{lds, 0};
   const HT* h = static_cast<const HT*>(k.h);
-  RawRow<HT, PER> ahead = load_raw<G, PER, FULL>(h + static_cast<size_t>(row) * d, lane, d);
-  const Row<PER> gamma = load_params<G, PER, FULL>(k.gamma, 1.f, lane, d), beta = load_params<G, PER, FULL>(k.beta, 0.f, lane, d);
+  RawRow<HT, PER> ahead = load_raw<G, PER, END>(h + static_cast<size_t>(row) * d, lane, d);
+  const Row<PER> gamma = load_params<G, PER, END>(k.gamma, 1.f, lane, d), beta = load_params<G, PER, END>(k.beta, 0.f, lane, d);
   for (; row < k.T; row += k.stride) {
     Row<PER> x = widen(ahead);
-    if (row + k.stride < k.T) ahead = load_raw<G, PER, FULL>(h + static_cast<size_t>(row + k.stride) * d, lane, d);
-    normalise<G, FULL>(x, lane, d, k.centre, k.eps, gs);
-    store_row<G, FULL>(static_cast<YT*>(k.n) + static_cast<size_t>(row) * d, affine(x, gamma, beta), lane, d);
+    if (row + k.stride < k.T) ahead = load_raw<G, PER, END>(h + static_cast<size_t>(row + k.stride) * d, lane, d);
+    normalise<G, END>(x, lane, d, k.centre, k.eps, gs);
+    store_row<G, END>(static_cast<YT*>(k.n) + static_cast<size_t>(row) * d, affine(x, gamma, beta), lane, d);
   }
 }
 
-template <typename HT, typename YT, int G, int PER, bool FULL>
+template <typename HT, typename YT, int G, int PER, RowEnd END>
 __global__ __launch_bounds__(Group<G>::kThreads) void exit_kernel(ExitArgs k) {
   __shared__ float lds[2][Group<G>::kWaves][2];
   const int lane = Group<G>::lane(), d = k.d;
@@ -80,13 +80,13 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_kernel(ExitArgs k) {
   const YT *y = static_cast<const YT*>(k.y), *full = static_cast<const YT*>(k.gate);
   const bool norm = k.norm_out != UMEM_NORM_NONE, gated = k.gate_kind == UMEM_GATE_FULL;
   size_t at = static_cast<size_t>(row) * d;
-  RawRow<YT, PER> y_ahead = load_raw<G, PER, FULL>(y + at, lane, d), g_ahead{};
-  RawRow<HT, PER> h_ahead = load_raw<G, PER, FULL>(h + at, lane, d);
-  if (gated) g_ahead = load_raw<G, PER, FULL>(full + at, lane, d);
-  const Row<PER> gamma = load_params<G, PER, FULL>(k.gamma, 1.f, lane, d), beta = load_params<G, PER, FULL>(k.beta, 0.f, lane, d);
-  const Row<PER> gamma2 = load_params<G, PER, FULL>(k.gamma_next, 1.f, lane, d),
-                 beta2 = load_params<G, PER, FULL>(k.beta_next, 0.f, lane, d);
-  Row<PER> channel = load_params<G, PER, FULL>(k.gate_kind == UMEM_GATE_CHANNEL ? static_cast<const float*>(k.gate) : nullptr,
+  RawRow<YT, PER> y_ahead = load_raw<G, PER, END>(y + at, lane, d), g_ahead{};
+  RawRow<HT, PER> h_ahead = load_raw<G, PER, END>(h + at, lane, d);
+  if (gated) g_ahead = load_raw<G, PER, END>(full + at, lane, d);
+  const Row<PER> gamma = load_params<G, PER, END>(k.gamma, 1.f, lane, d), beta = load_params<G, PER, END>(k.beta, 0.f, lane, d);
+  const Row<PER> gamma2 = load_params<G, PER, END>(k.gamma_next, 1.f, lane, d),
+                 beta2 = load_params<G, PER, END>(k.beta_next, 0.f, lane, d);
+  Row<PER> channel = load_params<G, PER, END>(k.gate_kind == UMEM_GATE_CHANNEL ? static_cast<const float*>(k.gate) : nullptr,
                                          1.f, lane, d);
   if (k.gate_kind == UMEM_GATE_CHANNEL && k.sigmoid) sigmoid_row(channel);
   for (; row < k.T; row += k.stride) {
@@ -94,9 +94,9 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_kernel(ExitArgs k) {
     Row<PER> m = widen(y_ahead), r = widen(h_ahead), g = gated ? widen(g_ahead) : channel;
     if (row + k.stride < k.T) {
       const size_t next = static_cast<size_t>(row + k.stride) * d;
-      y_ahead = load_raw<G, PER, FULL>(y + next, lane, d);
-      h_ahead = load_raw<G, PER, FULL>(h + next, lane, d);
-      if (gated) g_ahead = load_raw<G, PER, FULL>(full + next, lane, d);
+      y_ahead = load_raw<G, PER, END>(y + next, lane, d);
+      h_ahead = load_raw<G, PER, END>(h + next, lane, d);
+      if (gated) g_ahead = load_raw<G, PER, END>(full + next, lane, d);
     }
     if (gated && k.sigmoid) sigmoid_row(g);
     float token = k.s;
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_kernel(ExitArgs k) {
       token *= k.sigmoid ? sigmoid(z) : z;
     }
     if (norm) {
-      normalise<G, FULL>(m, lane, d, k.norm_out == UMEM_NORM_LAYER, k.eps, gs);
+      normalise<G, END>(m, lane, d, k.norm_out == UMEM_NORM_LAYER, k.eps, gs);
       m = affine(m, gamma, beta);
     }
     // the next entry's norm is taken of the stream as it is stored
@@ -114,12 +114,12 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_kernel(ExitArgs k) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float v = fmaf(k.a, r.v[p][i], token * (g.v[p][i] * m.v[p][i]));
-        r.v[p][i] = FULL || (p * G + lane) * 4 + i < d ? static_cast<float>(static_cast<HT>(v)) : 0.f;
+        r.v[p][i] = in_row<G, END>(p, i, lane, d) ? static_cast<float>(static_cast<HT>(v)) : 0.f;
       }
-    store_row<G, FULL>(static_cast<HT*>(k.h_out) + at, r, lane, d);
+    store_row<G, END>(static_cast<HT*>(k.h_out) + at, r, lane, d);
     if (k.n_next == nullptr) continue;
-    normalise<G, FULL>(r, lane, d, k.centre_next, k.eps, gs);
-    store_row<G, FULL>(static_cast<YT*>(k.n_next) + at, affine(r, gamma2, beta2), lane, d);
+    normalise<G, END>(r, lane, d, k.centre_next, k.eps, gs);
+    store_row<G, END>(static_cast<YT*>(k.n_next) + at, affine(r, gamma2, beta2), lane, d);
   }
 }
 

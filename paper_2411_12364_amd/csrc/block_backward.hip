@@ -37,7 +37,7 @@ struct ExitBackArgs {
 struct BackSums {
   float r, s0, s1;
 };
-template <int G, bool FULL, int PER>
+template <int G, RowEnd END, int PER>
 __device__ __forceinline__ BackSums back_sums(Row<PER>& x, const Row<PER>& v, int lane, int d, bool centre, float eps,
                                               GroupSum<G>& gs) {
   const float inv_d = 1.0f / static_cast<float>(d);
@@ -46,7 +46,7 @@ __device__ __forceinline__ BackSums back_sums(Row<PER>& x, const Row<PER>& v, in
     float sx = add_up(x), sv = add_up(v);
     gs.sum2(sx, sv);
     b.s0 = sv * inv_d;
-    centre_row<G, FULL>(x, sx * inv_d, lane, d);
+    centre_row<G, END>(x, sx * inv_d, lane, d);
   }
   float q = dot(x, x), vx = dot(v, x);
   gs.sum2(q, vx);
@@ -58,7 +58,7 @@ __device__ __forceinline__ BackSums back_sums(Row<PER>& x, const Row<PER>& v, in
 }
 
 // A workgroup's column sums to its place of the partial sums: its groups' are added in order in LDS.
-template <int G, bool FULL, int PER>
+template <int G, RowEnd END, int PER>
 __device__ __forceinline__ void write_part(const Row<PER>& acc, float* part, int lane, int d, float* lds) {
   Row<PER> s = acc;
   if constexpr (Group<G>::kRows > 1) {
@@ -72,10 +72,10 @@ __device__ __forceinline__ void write_part(const Row<PER>& acc, float* part, int
     }
     if (Group<G>::index() != 0) return;      // (its s starts from its own sums)
   }
-  store_row<G, FULL>(part, s, lane, d);
+  store_row<G, END>(part, s, lane, d);
 }
 
-template <typename HT, typename YT, int G, int PER, bool FULL>
+template <typename HT, typename YT, int G, int PER, RowEnd END>
 __global__ __launch_bounds__(Group<G>::kThreads) void entry_back_kernel(EntryBackArgs k) {
   __shared__ float lds[2][Group<G>::kWaves][2];
   __shared__ __align__(16) float sums[Group<G>::kRows > 1 ? 1024 : 4];
@@ -90,23 +90,23 @@ __global__ __launch_bounds__(Group<G>::kThreads) void entry_back_kernel(EntryBac
   RawRow<YT, PER> n_ahead{};
   if (row < k.T) {
     const size_t at = static_cast<size_t>(row) * d;
-    h_ahead = load_raw<G, PER, FULL>(h + at, lane, d);
-    n_ahead = load_raw<G, PER, FULL>(dn + at, lane, d);
-    if (more) u_ahead = load_raw<G, PER, FULL>(dres + at, lane, d);
+    h_ahead = load_raw<G, PER, END>(h + at, lane, d);
+    n_ahead = load_raw<G, PER, END>(dn + at, lane, d);
+    if (more) u_ahead = load_raw<G, PER, END>(dres + at, lane, d);
   }
-  const Row<PER> gamma = load_params<G, PER, FULL>(k.gamma, 1.f, lane, d);
+  const Row<PER> gamma = load_params<G, PER, END>(k.gamma, 1.f, lane, d);
   for (; row < k.T; row += k.stride) {
     const Row<PER> n = widen(n_ahead), up = widen(u_ahead);
     Row<PER> x = widen(h_ahead), v;
     if (row + k.stride < k.T) {
       const size_t next = static_cast<size_t>(row + k.stride) * d;
-      h_ahead = load_raw<G, PER, FULL>(h + next, lane, d);
-      n_ahead = load_raw<G, PER, FULL>(dn + next, lane, d);
-      if (more) u_ahead = load_raw<G, PER, FULL>(dres + next, lane, d);
+      h_ahead = load_raw<G, PER, END>(h + next, lane, d);
+      n_ahead = load_raw<G, PER, END>(dn + next, lane, d);
+      if (more) u_ahead = load_raw<G, PER, END>(dres + next, lane, d);
     }
 #pragma unroll
     for (int p = 0; p < PER; ++p) v.v[p] = n.v[p] * gamma.v[p];
-    const BackSums b = back_sums<G, FULL>(x, v, lane, d, k.centre, k.eps, gs);
+    const BackSums b = back_sums<G, END>(x, v, lane, d, k.centre, k.eps, gs);
 #pragma unroll
     for (int p = 0; p < PER; ++p)
 #pragma unroll
@@ -116,14 +116,14 @@ __global__ __launch_bounds__(Group<G>::kThreads) void entry_back_kernel(EntryBac
         db.v[p][i] += n.v[p][i];
         v.v[p][i] = fmaf(v.v[p][i] - b.s0 - xh * b.s1, b.r, up.v[p][i]);
       }
-    store_row<G, FULL>(static_cast<HT*>(k.dh) + static_cast<size_t>(row) * d, v, lane, d);
+    store_row<G, END>(static_cast<HT*>(k.dh) + static_cast<size_t>(row) * d, v, lane, d);
   }
   float* part = k.part + static_cast<size_t>(blockIdx.x) * (k.shift ? 2 : 1) * d;
-  write_part<G, FULL>(dg, part, lane, d, sums);
-  if (k.shift) write_part<G, FULL>(db, part + d, lane, d, sums);
+  write_part<G, END>(dg, part, lane, d, sums);
+  if (k.shift) write_part<G, END>(db, part + d, lane, d, sums);
 }
 
-template <typename HT, typename YT, int G, int PER, bool FULL>
+template <typename HT, typename YT, int G, int PER, RowEnd END>
 __global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackArgs k) {
   __shared__ float lds[2][Group<G>::kWaves][2];
   __shared__ __align__(16) float sums[Group<G>::kRows > 1 ? 1024 : 4];
@@ -139,13 +139,13 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackA
   RawRow<HT, PER> h_ahead{};
   if (row < k.T) {
     const size_t at = static_cast<size_t>(row) * d;
-    y_ahead = load_raw<G, PER, FULL>(y + at, lane, d);
-    h_ahead = load_raw<G, PER, FULL>(dh_out + at, lane, d);
-    if (full) g_ahead = load_raw<G, PER, FULL>(gate + at, lane, d);
+    y_ahead = load_raw<G, PER, END>(y + at, lane, d);
+    h_ahead = load_raw<G, PER, END>(dh_out + at, lane, d);
+    if (full) g_ahead = load_raw<G, PER, END>(gate + at, lane, d);
   }
-  const Row<PER> gamma = load_params<G, PER, FULL>(k.gamma, 1.f, lane, d), beta = load_params<G, PER, FULL>(k.beta, 0.f, lane, d);
+  const Row<PER> gamma = load_params<G, PER, END>(k.gamma, 1.f, lane, d), beta = load_params<G, PER, END>(k.beta, 0.f, lane, d);
   // a channel gate's value; its slope comes from it
-  Row<PER> value = load_params<G, PER, FULL>(channel ? static_cast<const float*>(k.gate) : nullptr, 1.f, lane, d);
+  Row<PER> value = load_params<G, PER, END>(channel ? static_cast<const float*>(k.gate) : nullptr, 1.f, lane, d);
   if (channel && k.sigmoid) {
 #pragma unroll
     for (int p = 0; p < PER; ++p)
@@ -157,14 +157,14 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackA
     Row<PER> x = widen(y_ahead), up = widen(h_ahead), g = full ? widen(g_ahead) : value, v;
     if (row + k.stride < k.T) {
       const size_t next = static_cast<size_t>(row + k.stride) * d;
-      y_ahead = load_raw<G, PER, FULL>(y + next, lane, d);
-      h_ahead = load_raw<G, PER, FULL>(dh_out + next, lane, d);
-      if (full) g_ahead = load_raw<G, PER, FULL>(gate + next, lane, d);
+      y_ahead = load_raw<G, PER, END>(y + next, lane, d);
+      h_ahead = load_raw<G, PER, END>(dh_out + next, lane, d);
+      if (full) g_ahead = load_raw<G, PER, END>(gate + next, lane, d);
     }
     if (k.dh != nullptr) {
 #pragma unroll
       for (int p = 0; p < PER; ++p) v.v[p] = up.v[p] * k.a;
-      store_row<G, FULL>(static_cast<HT*>(k.dh) + at, v, lane, d);
+      store_row<G, END>(static_cast<HT*>(k.dh) + at, v, lane, d);
     }
     if (full && k.sigmoid) {
 #pragma unroll
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackA
       v.v[p] = up.v[p] * (g.v[p] * of_token) * gamma.v[p];
     }
     BackSums b{1.f, 0.f, 0.f};
-    if (norm) b = back_sums<G, FULL>(x, v, lane, d, k.norm_out == UMEM_NORM_LAYER, k.eps, gs);
+    if (norm) b = back_sums<G, END>(x, v, lane, d, k.norm_out == UMEM_NORM_LAYER, k.eps, gs);
     float st = 0.f;
 #pragma unroll
     for (int p = 0; p < PER; ++p)
@@ -202,8 +202,8 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackA
         up.v[p][i] = dz;
         v.v[p][i] = norm ? (v.v[p][i] - b.s0 - xh * b.s1) * b.r : v.v[p][i];
       }
-    if (full) store_row<G, FULL>(static_cast<YT*>(k.dgate) + at, up, lane, d);
-    store_row<G, FULL>(static_cast<YT*>(k.dy) + at, v, lane, d);
+    if (full) store_row<G, END>(static_cast<YT*>(k.dgate) + at, up, lane, d);
+    store_row<G, END>(static_cast<YT*>(k.dy) + at, v, lane, d);
     if (token) {
       st = gs.sum(st);
       if (lane == 0) static_cast<float*>(k.dgate)[row] = k.sigmoid ? st * (of_token * (1.0f - of_token)) : st;
@@ -212,14 +212,14 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackA
   const int q = (norm ? 1 : 0) + (k.beta != nullptr ? 1 : 0) + (channel ? 1 : 0);
   float* part = k.part + static_cast<size_t>(blockIdx.x) * q * d;
   if (norm) {
-    write_part<G, FULL>(dg, part, lane, d, sums);
+    write_part<G, END>(dg, part, lane, d, sums);
     part += d;
   }
   if (k.beta != nullptr) {
-    write_part<G, FULL>(db, part, lane, d, sums);
+    write_part<G, END>(db, part, lane, d, sums);
     part += d;
   }
-  if (channel) write_part<G, FULL>(dc, part, lane, d, sums);
+  if (channel) write_part<G, END>(dc, part, lane, d, sums);
 }
 
 // The column sums: 128 threads take every 128th partial row each, in order, of four columns, and theirs

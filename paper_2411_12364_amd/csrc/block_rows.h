@@ -38,19 +38,29 @@ struct Row {
   rf32x4 v[PER];
 };
 
-// FULL: the row fills its group's registers (d = 4 G PER), so nothing is masked: without the branches for
-// a row's end and the selects 4,096 bf16 rows of 2,048 leave the block (norms on both sides, a full
-// gate) in 19 us, not 24.
-template <int G, int PER, bool FULL, typename T>
+// How rows end: they fill their group's registers (d = 4 G PER), end between two fours, or within one.
+// Loads past a row's fours are sent to its first four and the result dropped, so that only a last, partial
+// four takes a branch.  A branch around every load, and an element by element end in it, cost 900 rows of 4,092
+// 22 us to leave the block, 14 so; full rows without the selects 4,096 bf16 rows of 2,048 19.0, 20.7 with them.
+enum RowEnd { kFull, kFours, kAny };
+
+template <int G, int PER, RowEnd END, typename T>
 __device__ __forceinline__ RawRow<T, PER> load_raw(const T* row, int lane, int d) {
   RawRow<T, PER> r;
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
     const int e = (p * G + lane) * 4;
-    r.v[p] = T(0);
-    if (FULL || e + 4 <= d) {
+    if (END == kFull) {
       r.v[p] = *reinterpret_cast<const typename Quad<T>::type*>(row + e);
-    } else if (e < d) {                      // the last thread of a row of no multiple of four
+      continue;
+    }
+    r.v[p] = T(0);
+    if (END == kFours || d >= 4) {
+      const bool in = e + 4 <= d;
+      const typename Quad<T>::type x = *reinterpret_cast<const typename Quad<T>::type*>(row + (in ? e : 0));
+      r.v[p] = in ? x : r.v[p];
+    }
+    if (END == kAny && e < d && e + 4 > d) {
       r.v[p].x = row[e];
       if (e + 1 < d) r.v[p].y = row[e + 1];
       if (e + 2 < d) r.v[p].z = row[e + 2];
@@ -70,25 +80,25 @@ __device__ __forceinline__ Row<PER> widen(const RawRow<T, PER>& r) {
 }
 
 // A vector of parameters [d], or `otherwise` in every element where there is none.
-template <int G, int PER, bool FULL>
+template <int G, int PER, RowEnd END>
 __device__ __forceinline__ Row<PER> load_params(const float* p, float otherwise, int lane, int d) {
-  if (p != nullptr) return widen<float, PER>(load_raw<G, PER, FULL>(p, lane, d));
+  if (p != nullptr) return widen<float, PER>(load_raw<G, PER, END>(p, lane, d));
   Row<PER> r;
 #pragma unroll
   for (int q = 0; q < PER; ++q) r.v[q] = otherwise;
   return r;
 }
 
-template <int G, bool FULL, int PER, typename T>
+template <int G, RowEnd END, int PER, typename T>
 __device__ __forceinline__ void store_row(T* row, const Row<PER>& x, int lane, int d) {
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
     const int e = (p * G + lane) * 4;
     const typename Quad<T>::type r = {static_cast<T>(x.v[p].x), static_cast<T>(x.v[p].y), static_cast<T>(x.v[p].z),
                                       static_cast<T>(x.v[p].w)};
-    if (FULL || e + 4 <= d) {
+    if (END == kFull || e + 4 <= d) {
       *reinterpret_cast<typename Quad<T>::type*>(row + e) = r;
-    } else if (e < d) {
+    } else if (END == kAny && e < d) {
       row[e] = r.x;
       if (e + 1 < d) row[e + 1] = r.y;
       if (e + 2 < d) row[e + 2] = r.z;
@@ -170,21 +180,26 @@ __device__ __forceinline__ float dot(const Row<PER>& x, const Row<PER>& y) {
   return s;
 }
 
+template <int G, RowEnd END>
+__device__ __forceinline__ bool in_row(int p, int i, int lane, int d) {
+  return END == kFull || (p * G + lane) * 4 + (END == kFours ? 0 : i) < d;
+}
+
 // x - mean in the row's elements, zeros past it.
-template <int G, bool FULL, int PER>
+template <int G, RowEnd END, int PER>
 __device__ __forceinline__ void centre_row(Row<PER>& x, float mean, int lane, int d) {
 #pragma unroll
   for (int p = 0; p < PER; ++p)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[p][i] = FULL || (p * G + lane) * 4 + i < d ? x.v[p][i] - mean : 0.f;
+    for (int i = 0; i < 4; ++i) x.v[p][i] = in_row<G, END>(p, i, lane, d) ? x.v[p][i] - mean : 0.f;
 }
 
 // x -> x^ in place.  The variance is taken of the centred row, which keeps its digits where the mean is
 // far from zero.
-template <int G, bool FULL, int PER>
+template <int G, RowEnd END, int PER>
 __device__ __forceinline__ void normalise(Row<PER>& x, int lane, int d, bool centre, float eps, GroupSum<G>& gs) {
   const float inv_d = 1.0f / static_cast<float>(d);
-  if (centre) centre_row<G, FULL>(x, gs.sum(add_up(x)) * inv_d, lane, d);
+  if (centre) centre_row<G, END>(x, gs.sum(add_up(x)) * inv_d, lane, d);
   const float r = rsqrtf(gs.sum(dot(x, x)) * inv_d + eps);
 #pragma unroll
   for (int p = 0; p < PER; ++p) x.v[p] *= r;
@@ -214,10 +229,11 @@ inline int row_workgroups(const RowShape& s, int T, int most) {
   return (need + turns - 1) / turns;
 }
 
-// GO(kernel instance, threads) for the row shape, whether rows fill it, and the types of h and y.
-#define UMEM_ROW_FULL(KERNEL, HT, YT, G, PER, THR)                  \
-  if (bd.d == 4 * G * PER) UMEM_ROW_GO((KERNEL<HT, YT, G, PER, true>), THR); \
-  else UMEM_ROW_GO((KERNEL<HT, YT, G, PER, false>), THR);
+// GO(kernel instance, threads) for the row shape, how rows end, and the types of h and y.
+#define UMEM_ROW_FULL(KERNEL, HT, YT, G, PER, THR)                                          \
+  if (bd.d == 4 * G * PER) UMEM_ROW_GO((KERNEL<HT, YT, G, PER, kFull>), THR);               \
+  else if (bd.d % 4 == 0) UMEM_ROW_GO((KERNEL<HT, YT, G, PER, kFours>), THR);               \
+  else UMEM_ROW_GO((KERNEL<HT, YT, G, PER, kAny>), THR);
 #define UMEM_ROW_SHAPES(KERNEL, HT, YT)                                     \
   switch (shape.group * 8 + shape.per) {                                    \
     case 64 * 8 + 1: UMEM_ROW_FULL(KERNEL, HT, YT, 64, 1, 256) break;       \
