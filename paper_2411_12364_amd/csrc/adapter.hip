@@ -9,7 +9,8 @@
 //   d_in each, its sums over the pieces through the workspace, then B times those by tiles and a range of
 //   outputs.  Bound by HBM (x, base and out once); the adapters come from L2, once for the 16 tokens of a
 //   product that share one.  A launch for both, with all of d_in and A for 16 tokens in one workgroup, waited
-//   for twice as many bytes from L2 in every CU (4,096 tokens in 16 runs, rank 32, 2,048 by 896: 21 us).
+//   for twice as many bytes from L2 in every CU (16 runs, rank 32, 2,048 by 896: 1,024 tokens 20.8 us, now 13.7;
+//   4,096 tokens 22, now 20).
 //
 // Nothing is rounded on the way: an fp32 value is the sum of three bf16 parts of 8 bits each, whose
 // products with bf16 weights are exact in the matrix cores' fp32 accumulators.
@@ -68,17 +69,55 @@ __device__ __forceinline__ float dot8(u32x4 w, const Eight& x, float s) {
 
 // 64 tokens of 64 adapters, rank 16, 1,024 by 2,048: 4.0 us, with 256 or 1,024 threads to a token 4.6.
 constexpr int kTokenThreads = 512, kTokenWaves = kTokenThreads / kWave;
-constexpr int kAhead = 8;      // 16-byte pieces of B that a thread has in flight
 
-// A thread's pieces of B, kAhead of them: outputs kTokenThreads apart, each of rank / 8 pieces, and base beside
-// the first piece of each.
-template <typename OT>
-struct Pieces {
-  u32x4 w[kAhead];
-  float base[kAhead];
+// 64 outputs of a token and a wave: L lanes to a row of B, 8 ranks each (lanes past the rank have zeros), so
+// that a load is 1,024 consecutive bytes where the rank is 8 L; row u 64 / L + lane / L in load u.  The sums
+// over the L lanes leave lane l with output l % L * (64 / L) + l / L.  (A row a lane, with no sums, asks for the same lines L
+// times: 256 tokens, rank 64, 2,048 by 2,048: 28.6 us, so 19.)
+template <int L, typename OT>
+struct Rows64 {
+  u32x4 w[L];
+  float from;
+  static __device__ __forceinline__ int lane() { return threadIdx.x & (kWave - 1); }
+  static __device__ __forceinline__ int mine() { return lane() % L * (kWave / L) + lane() / L; }
+  // Outputs from o on, those below `last`; b, base: of the token.
+  __device__ __forceinline__ void load(const uint16_t* b, const OT* base, int rank, int o, int last) {
+    const int q = lane() % L * 8;
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+      const int row = o + u * (kWave / L) + lane() / L;
+      w[u] = u32x4{0, 0, 0, 0};
+      if (row < last && q < rank) w[u] = *reinterpret_cast<const u32x4*>(b + static_cast<size_t>(row) * rank + q);
+    }
+    from = base != nullptr && o + mine() < last ? static_cast<float>(base[o + mine()]) : 0.f;
+  }
+  __device__ __forceinline__ void store(const Eight& low, OT* out, int o, int last) const {
+    float v[L];
+#pragma unroll
+    for (int u = 0; u < L; ++u) v[u] = dot8(w[u], low, 0.f);
+    if constexpr (L >= 16) fold<8, 0x140>(v);          // from the mirrored lane of 16
+    if constexpr (L >= 8) fold<4, 0x141>(v);           // of 8
+    if constexpr (L >= 4) fold<2, 0x4E>(v);            // from the lane two off
+    if constexpr (L >= 2) fold<1, 0xB1>(v);            // one off
+    if (o + mine() < last) out[o + mine()] = static_cast<OT>(from + v[0]);
+  }
+  // Half of the sums go to the partner lane, its half of the others comes back.
+  template <int H, int Move>
+  static __device__ __forceinline__ void fold(float* v) {
+    const bool upper = (lane() & H) != 0;
+#pragma unroll
+    for (int u = 0; u < H; ++u) {
+      const float keep = upper ? v[u + H] : v[u], send = upper ? v[u] : v[u + H];
+      v[u] = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(send), Move, 0xf, 0xf, true));
+    }
+  }
+  // The lane's eight of a token's rank values.
+  static __device__ __forceinline__ Eight lows(const float* low, int rank) {
+    return lane() % L * 8 < rank ? load8(low + lane() % L * 8) : Eight{};
+  }
 };
 
-// ROWS: rows of A a wave takes.
+// ROWS: rows of A a wave takes, and the lanes to a row of B: a rank of at most 8 ROWS.
 template <typename XT, typename OT, int ROWS>
 __global__ __launch_bounds__(kTokenThreads) void token_kernel(AdapterArgs k) {
   __shared__ __align__(16) float low[kMaxAdapterRank];
@@ -94,30 +133,22 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(AdapterArgs k) {
     for (int o = first + threadIdx.x; o < last; o += kTokenThreads) out[o] = base != nullptr ? base[o] : OT(0);
     return;
   }
-  const int pieces = k.rank / 8;
   const uint16_t* b = k.b + static_cast<size_t>(id) * k.d_out * k.rank;
-  int o_ahead = first + threadIdx.x, q_ahead = 0;       // the next piece to load
-  auto load = [&](Pieces<OT>& n) {
+  // kAhead blocks of outputs are loaded together, the first before A x is known
+  using Rows = Rows64<ROWS, OT>;
+  constexpr int kAhead = ROWS < 8 ? 8 / ROWS : 1;
+  Rows even[kAhead], odd[kAhead];
+  auto load = [&](Rows* n, int o) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (o_ahead < last) {
-        n.w[i] = *reinterpret_cast<const u32x4*>(b + static_cast<size_t>(o_ahead) * k.rank + q_ahead * 8);
-        if (q_ahead == 0) n.base[i] = base != nullptr ? static_cast<float>(base[o_ahead]) : 0.f;
-      }
-      if (++q_ahead == pieces) {
-        q_ahead = 0;
-        o_ahead += kTokenThreads;
-      }
-    }
+    for (int i = 0; i < kAhead; ++i) n[i].load(b, base, k.rank, o + i * kTokenThreads, last);
   };
-  // the first pieces are on their way before A x is known
-  Pieces<OT> even, odd;
-  load(even);
+  int o = first + wave * kWave;
+  load(even, o);
   // A x: a wave's rows side by side, so that its loads of a step are all in flight together
   const XT* x = static_cast<const XT*>(k.x) + static_cast<size_t>(t) * k.d_in;
   const uint16_t* a = k.a + static_cast<size_t>(id) * k.rank * k.d_in;
   float acc[ROWS] = {};
-#pragma unroll 2
+#pragma unroll(ROWS < 8 ? 2 : 1)
   for (int c = lane * 8; c < k.d_in; c += kWave * 8) {
     const Eight xv = load8(x + c);
     u32x4 w[ROWS];
@@ -136,28 +167,18 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(AdapterArgs k) {
     if (lane == 0) low[wave + r * kTokenWaves] = s * scale;
   }
   __syncthreads();
-  int o = first + threadIdx.x, q = 0;
-  float v = 0.f, from = 0.f;
-  auto finish = [&](const Pieces<OT>& n) {
+  const Eight lows = Rows::lows(low, k.rank);
+  auto finish = [&](const Rows* n, int o) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (q == 0) from = n.base[i];
-      if (o < last) v = dot8(n.w[i], load8(low + q * 8), v);
-      if (++q == pieces) {
-        if (o < last) out[o] = static_cast<OT>(from + v);
-        q = 0;
-        v = 0.f;
-        o += kTokenThreads;
-      }
-    }
+    for (int i = 0; i < kAhead; ++i) n[i].store(lows, out, o + i * kTokenThreads, last);
   };
-  // pieces left, the same for all threads of the workgroup
-  for (int left = (last - first + kTokenThreads - 1) / kTokenThreads * pieces; left > 0; left -= 2 * kAhead) {
-    if (left > kAhead) load(odd);
-    finish(even);
-    if (left <= kAhead) break;
-    if (left > 2 * kAhead) load(even);
-    finish(odd);
+  constexpr int kStep = kAhead * kTokenThreads;
+  for (; o < last; o += 2 * kStep) {
+    if (o + kStep < last) load(odd, o + kStep);
+    finish(even, o);
+    if (o + kStep >= last) break;
+    if (o + 2 * kStep < last) load(even, o + 2 * kStep);
+    finish(odd, o + kStep);
   }
 }
 
@@ -286,53 +307,62 @@ __global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs k, int RT) {
   }
   tile.find(k.n);
   if (tile.leads == 0) return;                          // (the same in every wave)
-  // an item's weights in one or two halves, 32 registers at a time, so that two workgroups fit a CU
-  constexpr int kHalf = kSteps < 8 ? kSteps : 8, kHalves = kSteps / kHalf;
+  // an item's weights in one or two halves of 8 steps, or those of two items of two steps: up to 32 registers at
+  // a time, so that two workgroups fit a CU
+  constexpr int kHalf = kSteps < 8 ? kSteps : 8, kHalves = kSteps / kHalf, kItems = kHalf < 4 ? 2 : 1;
   const int items = __popcll(tile.leads) * RT;
   struct Half {
-    int first, lead, rt;
-    u32x4 w[kHalf];
+    int first[kItems], lead[kItems], rt[kItems];
+    u32x4 w[kItems][kHalf];
   } even, odd;
+  auto item_of = [&](int half, int i) { return wave + (half / kHalves * kItems + i) * kWaves; };
   auto load = [&](Half& n, int half) {                  // (the wave's own count of halves)
-    const int item = wave + half / kHalves * kWaves, from_step = half % kHalves * kHalf;
-    if (item >= items) return;
-    const int pair = item / RT;
-    const int at = tile.place(pair);
-    n.rt = item - pair * RT;
-    n.first = at & ~(Tile<CG>::kSpan - 1);
-    n.lead = __builtin_amdgcn_readlane(tile.id, at);
-    const __amdgpu_buffer_rsrc_t ra = rsrc(k.a + static_cast<size_t>(n.lead) * k.rank * k.d_in,
-                                           static_cast<size_t>(k.rank) * k.d_in * 2);
-    const int at_k = from_step * 32 + quad * 8;
-    const uint32_t from = static_cast<uint32_t>((n.rt * 16 + col) * k.d_in + begin + at_k) * 2u;
+    const int from_step = half % kHalves * kHalf;
 #pragma unroll
-    for (int s = 0; s < kHalf; ++s)
-      n.w[s] = fetch16(ra, s * 32 + at_k < width ? from + static_cast<uint32_t>(s) * 64u : kOutside);
+    for (int i = 0; i < kItems; ++i) {
+      const int item = item_of(half, i);
+      if (item >= items) return;
+      const int pair = item / RT;
+      const int at = tile.place(pair);
+      n.rt[i] = item - pair * RT;
+      n.first[i] = at & ~(Tile<CG>::kSpan - 1);
+      n.lead[i] = __builtin_amdgcn_readlane(tile.id, at);
+      const __amdgpu_buffer_rsrc_t ra = rsrc(k.a + static_cast<size_t>(n.lead[i]) * k.rank * k.d_in,
+                                             static_cast<size_t>(k.rank) * k.d_in * 2);
+      const int at_k = from_step * 32 + quad * 8;
+      const uint32_t from = static_cast<uint32_t>((n.rt[i] * 16 + col) * k.d_in + begin + at_k) * 2u;
+#pragma unroll
+      for (int s = 0; s < kHalf; ++s)
+        n.w[i][s] = fetch16(ra, s * 32 + at_k < width ? from + static_cast<uint32_t>(s) * 64u : kOutside);
+    }
   };
   f32x4 acc[CG];
   auto finish = [&](const Half& n, int half) {
-    const int item = wave + half / kHalves * kWaves, from_step = half % kHalves * kHalf;
-    if (item >= items) return;
-    const uint16_t* xs = staged + (n.first + col) * kPitch + from_step * 32 + quad * 8;
-    if (from_step == 0) {
+    const int from_step = half % kHalves * kHalf;
 #pragma unroll
-      for (int c = 0; c < CG; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int i = 0; i < kItems; ++i) {
+      if (item_of(half, i) >= items) return;
+      const uint16_t* xs = staged + (n.first[i] + col) * kPitch + from_step * 32 + quad * 8;
+      if (from_step == 0) {
 #pragma unroll
-    for (int s = 0; s < kHalf; ++s)
+        for (int c = 0; c < CG; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
 #pragma unroll
-      for (int q = 0; q < kParts; ++q)
+      for (int s = 0; s < kHalf; ++s)
 #pragma unroll
-        for (int c = 0; c < CG; ++c)
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              __builtin_bit_cast(bf16x8, n.w[s]),
-              *reinterpret_cast<const bf16x8*>(xs + q * kPlane + c * kGroup * kPitch + s * 32), acc[c], 0, 0, 0);
-    if (from_step + kHalf != kSteps) return;
+        for (int q = 0; q < kParts; ++q)
 #pragma unroll
-    for (int c = 0; c < CG; ++c) {
-      const int first = n.first + c * kGroup;
-      if (tile.mine(first, n.lead))
-        *reinterpret_cast<f32x4*>(k.low + ((static_cast<size_t>(blockIdx.y) * k.T + t0 + first + col) * RT + n.rt) * 16 + quad * 4) = acc[c];
+          for (int c = 0; c < CG; ++c)
+            acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, n.w[i][s]),
+                *reinterpret_cast<const bf16x8*>(xs + q * kPlane + c * kGroup * kPitch + s * 32), acc[c], 0, 0, 0);
+      if (from_step + kHalf != kSteps) return;
+#pragma unroll
+      for (int c = 0; c < CG; ++c) {
+        const int first = n.first[i] + c * kGroup;
+        if (tile.mine(first, n.lead[i]))
+          *reinterpret_cast<f32x4*>(k.low + ((static_cast<size_t>(blockIdx.y) * k.T + t0 + first + col) * RT + n.rt[i]) * 16 + quad * 4) = acc[c];
+      }
     }
   };
   load(even, 0);
@@ -348,7 +378,7 @@ __global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs k, int RT) {
     }
   }
   __syncthreads();
-  for (int half = 0; wave + half / kHalves * kWaves < items; half += 2) {
+  for (int half = 0; item_of(half, 0) < items; half += 2) {
     load(odd, half + 1);
     finish(even, half);
     load(even, half + 2);
@@ -363,6 +393,9 @@ template <>
 struct Quad4<float> {
   u32x4 raw;
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t at) { raw = fetch16(r, at); }
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, uint32_t at) const {
+    __builtin_amdgcn_raw_buffer_store_b128(raw, r, at, 0, 0);
+  }
   __device__ __forceinline__ void add_store(__amdgpu_buffer_rsrc_t r, uint32_t at, f32x4 d) const {
     const f32x4 v = __builtin_bit_cast(f32x4, raw) + d;
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, at, 0, 0);
@@ -374,6 +407,9 @@ struct Quad4<__bf16> {
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
     raw = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
   }
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, uint32_t at) const {
+    __builtin_amdgcn_raw_buffer_store_b64(raw, r, at, 0, 0);
+  }
   __device__ __forceinline__ void add_store(__amdgpu_buffer_rsrc_t r, uint32_t at, f32x4 d) const {
     const f32x4 v = f32x4{lo_of(raw.x), hi_of(raw.x), lo_of(raw.y), hi_of(raw.y)} + d;
     const bf16x4 o = {static_cast<__bf16>(v.x), static_cast<__bf16>(v.y), static_cast<__bf16>(v.z), static_cast<__bf16>(v.w)};
@@ -384,11 +420,54 @@ struct Quad4<__bf16> {
 // out = base + B (scale low), a tile of tokens and a range of outputs a workgroup.  The pieces' sums are
 // added in order as they are staged.  KT: steps of 32 over the rank.
 //
-// Where at least four tokens share an adapter on average, a wave takes units of a pair and 16 U outputs on the
-// matrix cores, a unit's loads in flight while the one before is multiplied; else (a decode batch of many
-// adapters) the products would compute 16 columns for one or two, and a wave takes a token and 128 outputs,
-// two to a lane.
-constexpr int kManyPairs = kTile / 4;
+// Where at least two tokens share an adapter on average, a wave takes units of a pair and 16 U outputs on the
+// matrix cores, a unit's loads in flight while the one before is multiplied; else (a batch of many adapters in no
+// order) the products would compute 16 columns for one or two, and by_token does it.  Rank 32, 2,048 by 896,
+// 2,048 tokens: of 8 adapters in random order (28 pairs) 13.6 us, by token 19.6; of 64 (55 pairs) 24, by token
+// 21.  Rank 64, 2,048 by 2,048, 512 tokens of 64 in random order: by token 33, an output a lane 47.
+constexpr int kManyPairs = kTile / 2;
+
+// The wave's tokens of a tile (every eighth), a token and kBlocks times 64 outputs at a time.  ids: the tile's, a lane each.
+template <int L, typename OT>
+__device__ __forceinline__ void by_token(const AdapterArgs& k, const float* low, int pitch, int ids, int t0, int tokens,
+                                         int wave, int begin, int end) {
+  using Rows = Rows64<L, OT>;
+  constexpr int kBlocks = L < 4 ? 4 / L : 1, kStep = kBlocks * kWave;
+  const int blocks = (end - begin + kStep - 1) / kStep;
+  const int units = blocks > 0 ? (tokens - wave + kWaves - 1) / kWaves * blocks : 0;
+  struct Unit {
+    Rows rows[kBlocks];
+    int tok, o;
+    bool on;
+  } even, odd;
+  auto load = [&](Unit& n, int unit) {
+    n.on = unit < units;
+    if (!n.on) return;
+    n.tok = wave + unit / blocks * kWaves;
+    n.o = begin + unit % blocks * kStep;
+    const int id = __builtin_amdgcn_readlane(ids, n.tok);
+    n.on = id >= 0;
+    if (!n.on) return;
+    const uint16_t* b = k.b + static_cast<size_t>(id) * k.d_out * k.rank;
+    const OT* base = k.base != nullptr ? static_cast<const OT*>(k.base) + static_cast<size_t>(t0 + n.tok) * k.d_out : nullptr;
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) n.rows[i].load(b, base, k.rank, n.o + i * kWave, end);
+  };
+  auto finish = [&](const Unit& n) {
+    if (!n.on) return;
+    OT* out = static_cast<OT*>(k.out) + static_cast<size_t>(t0 + n.tok) * k.d_out;
+    const Eight lows = Rows::lows(low + n.tok * pitch, k.rank);
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) n.rows[i].store(lows, out, n.o + i * kWave, end);
+  };
+  load(even, 0);
+  for (int unit = 0; unit < units; unit += 2) {
+    load(odd, unit + 1);
+    finish(even);
+    load(even, unit + 2);
+    finish(odd);
+  }
+}
 
 template <typename OT, int KT>
 __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
@@ -406,14 +485,14 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
   const int o_begin = blockIdx.y * per, o_end = min(n_out, o_begin + per);
   Tile<CG> tile;
   tile.fetch(k.ids, t0, k.T);
-  // the rank values of a token are 4 RT pieces of four; ranks past the rank are zeros of zero weights.  (Tokens
-  // without an adapter have none: what the workspace holds there goes nowhere.)
+  // the rank values of a token are pieces of four; ranks past the rank are zeros.  (Tokens without an adapter
+  // have none: what the workspace holds there goes nowhere.)
   f32x4 low[KT];
 #pragma unroll
   for (int u = 0; u < KT; ++u) {
     const int f = threadIdx.x + u * kThreads, tok = f / (KT * 8), r4 = f % (KT * 8);
     low[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (tok < tokens && r4 < RT * 4) {
+    if (tok < tokens && r4 * 4 < k.rank) {
       const float* p = k.low + (static_cast<size_t>(t0 + tok) * RT * 4 + r4) * 4;
       const size_t stride = static_cast<size_t>(k.T) * RT * 16;
 #pragma unroll 8
@@ -485,36 +564,18 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
         const uint32_t off = static_cast<uint32_t>(tok * k.d_out + o) * static_cast<uint32_t>(sizeof(OT));
         Quad4<OT> from;
         from.load(rbase, off);
-        from.add_store(rout, off, f32x4{0.f, 0.f, 0.f, 0.f});
+        from.store(rout, off);
       }
     }
   }
   __syncthreads();
   if (many) {
-    const int o_last = min(o_end * 16, k.d_out);
-    for (int tok = wave; tok < tokens; tok += kWaves) {
-      const int id = __builtin_amdgcn_readlane(tile.id, tok);
-      if (id < 0) continue;
-      const uint16_t* b = k.b + static_cast<size_t>(id) * k.d_out * k.rank;
-      const float* low = plain + tok * KT * 32;
-      const OT* base = k.base != nullptr ? static_cast<const OT*>(k.base) + static_cast<size_t>(t0 + tok) * k.d_out : nullptr;
-      OT* out = static_cast<OT*>(k.out) + static_cast<size_t>(t0 + tok) * k.d_out;
-      for (int o = o_begin * 16 + lane; o < o_last; o += 2 * kWave) {
-        const bool two = o + kWave < o_last;
-        const uint16_t *b0 = b + static_cast<size_t>(o) * k.rank, *b1 = two ? b0 + static_cast<size_t>(kWave) * k.rank : b0;
-        float s0 = base != nullptr ? static_cast<float>(base[o]) : 0.f;
-        float s1 = base != nullptr && two ? static_cast<float>(base[o + kWave]) : 0.f;
-        float v0 = 0.f, v1 = 0.f;
-#pragma unroll 2
-        for (int r = 0; r < k.rank; r += 8) {
-          const Eight l = load8(low + r);
-          const u32x4 w0 = *reinterpret_cast<const u32x4*>(b0 + r), w1 = *reinterpret_cast<const u32x4*>(b1 + r);
-          v0 = dot8(w0, l, v0);
-          v1 = dot8(w1, l, v1);
-        }
-        out[o] = static_cast<OT>(s0 + v0);
-        if (two) out[o + kWave] = static_cast<OT>(s1 + v1);
-      }
+    if constexpr (KT == 1) {
+      if (k.rank <= 8) by_token<1, OT>(k, plain, KT * 32, tile.id, t0, tokens, wave, o_begin * 16, min(o_end * 16, k.d_out));
+      else if (k.rank <= 16) by_token<2, OT>(k, plain, KT * 32, tile.id, t0, tokens, wave, o_begin * 16, min(o_end * 16, k.d_out));
+      else by_token<4, OT>(k, plain, KT * 32, tile.id, t0, tokens, wave, o_begin * 16, min(o_end * 16, k.d_out));
+    } else {
+      by_token<KT * 4, OT>(k, plain, KT * 32, tile.id, t0, tokens, wave, o_begin * 16, min(o_end * 16, k.d_out));
     }
     return;
   }
@@ -548,13 +609,13 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
   }
 }
 
-// Tiles of 64 from this many ranks of tokens on (1,536 tokens of rank 16, 384 of rank 64).  A workgroup a token
-// does its own A x whoever shares the adapter, a tile shares it but has few workgroups.  In us, a workgroup a
-// token and tiles, for 8 or 16 adapters in runs and for 64 in random order: rank 16, 1,024 by 2,048: 512
-// tokens 7.3, 9.8 and 9.7, 18.7; 1,536 tokens 16.6, 14.6 and 21.7, 25.3; 4,096 tokens random 52, 42.  Rank 32,
-// 2,048 by 896: 768 tokens 15.1, 14.1; 2,048 tokens 29, 14.7.  Rank 64, 2,048 by 2,048: 256 tokens 25.5, 18.1
-// and 27.8, 70; 512 tokens 44, 15.7.
-constexpr int kTileFrom = 24576;
+// Tiles of 64 from this many ranks of tokens on (2,560 tokens of rank 16, 640 of rank 64).  A workgroup a token
+// does its own A x whoever shares the adapter, a tile shares it, but only among tokens that lie together, and
+// has few workgroups.  In us, a workgroup a token and tiles, for 8 adapters in runs, 64 in runs, 64 in random
+// order (which only the device knows): rank 16, 1,024 by 2,048: 2,048 tokens 20, 21, 25 and 16, 16, 30; 4,096
+// 36, 36, 44 and 20, 21, 48.  Rank 32, 2,048 by 896: 1,024 tokens 16, 20, 24 and 14, 15, 40; 2,048 28, 27, 43
+// and 15, 17, 53.  Rank 64, 2,048 by 2,048: 512 tokens 19, 36, 33 and 16, 25, 57; 1,024 34, 44, 63 and 19, 25, 79.
+constexpr int kTileFrom = 40960;
 bool by_tiles(const umem_adapter_desc& ad, int T) { return static_cast<int64_t>(T) * ad.rank >= kTileFrom; }
 
 // Pieces of d_in: the widest that make 512 workgroups (two for each CU; 1,024 were no faster), as wider ones

@@ -78,7 +78,10 @@ SIZES = [(1, 1, 8, 8, 8), (1, 3, 16, 1024, 2048), (2, 2, 128, 264, 136), (5, 64,
          (2049, 16, 32, 256, 520), (4096, 3, 8, 64, 1024), (767, 9, 16, 512, 264), (768, 9, 16, 512, 264),
          (800, 50, 72, 1024, 520), (1024, 1024, 8, 64, 200), (1030, 6, 128, 136, 264), (4097, 3, 48, 2048, 64),
          (4100, 5, 16, 4096, 72), (1535, 9, 16, 264, 520), (1536, 9, 16, 264, 520), (192, 3, 128, 520, 264),
-         (400, 90, 64, 264, 1000)]
+         (400, 90, 64, 264, 1000), (5119, 70, 8, 72, 264), (5121, 3, 8, 520, 136), (5200, 4000, 8, 64, 200),
+         (2559, 9, 16, 264, 520), (2560, 400, 16, 264, 520), (1300, 700, 32, 520, 392), (640, 64, 64, 264, 1000),
+         (639, 3, 64, 264, 1000), (320, 90, 128, 264, 520), (333, 2, 128, 1032, 264), (700, 80, 56, 4096, 72),
+         (1800, 60, 24, 1032, 200), (450, 60, 96, 72, 328)]
 TYPES = [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16")]
 
 
@@ -108,7 +111,7 @@ def test_adapters(i, size, kind):
         assert torch.equal(out, want)
 
 
-@pytest.mark.parametrize("T", [1, 37, 700, 2001])
+@pytest.mark.parametrize("T", [1, 37, 700, 2001, 2801])
 def test_tokens_without_an_adapter(T):
     """ids outside [0, n): the base as it is (or zeros), whatever x holds there."""
     s = make(T, 3, 16, 256, 512, 2)
@@ -130,7 +133,7 @@ def test_tokens_without_an_adapter(T):
         check(part, ids[few], out[few])
 
 
-@pytest.mark.parametrize("T", [64, 2048])
+@pytest.mark.parametrize("T", [64, 2048, 2800])
 def test_nan_stays_with_its_token_and_adapter(T):
     s = make(T, 4, 16, 256, 512, 4)
     ids = (torch.arange(T, device="cuda") % 4).to(torch.int32)
@@ -143,7 +146,7 @@ def test_nan_stays_with_its_token_and_adapter(T):
     assert torch.isnan(out[10]).all() and not torch.isfinite(out[3]).any()
 
 
-@pytest.mark.parametrize("T", [3, 2000])
+@pytest.mark.parametrize("T", [3, 2000, 6000])
 def test_every_digit_of_the_input_counts(T):
     """x = 1 + 2^-23 against weights that cancel its leading part: a rounded x would give zero."""
     s = make(T, 1, 8, 64, 64, 6, base=False, scale=False)
@@ -157,7 +160,7 @@ def test_every_digit_of_the_input_counts(T):
     assert torch.equal(out, torch.full_like(out, 2.0 ** -23))
 
 
-@pytest.mark.parametrize("T", [2, 2000])
+@pytest.mark.parametrize("T", [2, 2000, 6000])
 def test_largest_values_and_infinities(T):
     """The largest fp32 values stay finite on the way, an infinity is itself."""
     s = make(T, 1, 8, 64, 64, 6, base=False, scale=False)
@@ -174,6 +177,41 @@ def test_largest_values_and_infinities(T):
     rest = torch.arange(T, device="cuda") != 1
     want = torch.full_like(out[rest], big * 0.25)
     assert ((out[rest] - want).abs() <= 4 * u * want).all() and not torch.isfinite(out[1]).any()
+
+
+@pytest.mark.parametrize("T,n", [(7, 3), (6000, 3), (6000, 4000)])
+@pytest.mark.parametrize("rank", [8, 24, 40])
+def test_an_infinite_input_gives_infinities(T, n, rank):
+    """Its token's outputs are infinite with the signs of the weights' products, not NaN, whatever rank the
+    kernel pads to; the other tokens' stay what they are."""
+    s = make(T, n, rank, 64, 136, 11)
+    s["a"], s["b"] = s["a"].abs() + 0.25, s["b"].abs() + 0.25
+    s["b"][:, ::3] *= -1
+    ids = ids_of("random", T, n, s["g"])
+    ids[1], ids[4] = 0, n - 1
+    clean = call(s, ids).clone()
+    s["x"][1, 5], s["x"][4, 63] = float("inf"), -float("inf")
+    out = call(s, ids)
+    sign = torch.ones(136, device="cuda")
+    sign[::3] = -1
+    assert torch.equal(out[1], sign * float("inf")) and torch.equal(out[4], -sign * float("inf"))
+    rest = [t for t in range(T) if t not in (1, 4)]
+    assert torch.equal(out[rest], clean[rest])
+
+
+@pytest.mark.parametrize("o", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [5, 2800])
+def test_base_of_negative_zeros(T, o):
+    """A token without an adapter keeps its base bit for bit."""
+    s = make(T, 3, 16, 64, 136, 9, o=o)
+    s["base"].mul_(0.0).abs_().neg_()
+    ids = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    ids[3] = 1
+    out = call(s, ids)
+    rest = [t for t in range(T) if t != 3]
+    bits = torch.int32 if o == "f32" else torch.int16
+    assert torch.equal(out[rest].view(bits), s["base"][rest].view(bits))
+    assert torch.signbit(s["base"]).all()
 
 
 def test_offsets_past_32_bits():
@@ -228,6 +266,7 @@ FRONT_ENDS = [
     CF.FrontEnd("adapted-decode", B=24, L=1, d_model=256, conv_k=4, heads=2, dk=64, shared=True, seed=51),
     CF.FrontEnd("adapted-separate", B=3, L=37, d_model=1024, conv_k=3, heads=1, dk=40, shared=False, seed=52, history=False),
     CF.FrontEnd("adapted-prompts", B=4, L=431, d_model=512, conv_k=4, heads=2, dk=128, shared=True, seed=53),
+    CF.FrontEnd("adapted-long-prompts", B=4, L=801, d_model=256, conv_k=4, heads=2, dk=64, shared=True, seed=54),
 ]
 
 
