@@ -88,22 +88,20 @@ __global__ __launch_bounds__(Group<G>::kThreads) void entry_back_kernel(EntryBac
   int row = blockIdx.x * Group<G>::kRows + Group<G>::index();
   RawRow<HT, PER> h_ahead{}, u_ahead{};
   RawRow<YT, PER> n_ahead{};
-  if (row < k.T) {
-    const size_t at = static_cast<size_t>(row) * d;
+  auto load = [&](int r) {
+    const size_t at = static_cast<size_t>(r) * d;
     h_ahead = load_raw<G, PER, END>(h + at, lane, d);
     n_ahead = load_raw<G, PER, END>(dn + at, lane, d);
     if (more) u_ahead = load_raw<G, PER, END>(dres + at, lane, d);
-  }
-  const Row<PER> gamma = load_params<G, PER, END>(k.gamma, 1.f, lane, d);
+  };
+  constexpr bool kAhead = !kWide<G, PER>;
+  if (kAhead && row < k.T) load(row);
+  const Params<G, PER, END> of_gamma(k.gamma, 1.f, lane, d);
   for (; row < k.T; row += k.stride) {
-    const Row<PER> n = widen(n_ahead), up = widen(u_ahead);
-    Row<PER> x = widen(h_ahead), v;
-    if (row + k.stride < k.T) {
-      const size_t next = static_cast<size_t>(row + k.stride) * d;
-      h_ahead = load_raw<G, PER, END>(h + next, lane, d);
-      n_ahead = load_raw<G, PER, END>(dn + next, lane, d);
-      if (more) u_ahead = load_raw<G, PER, END>(dres + next, lane, d);
-    }
+    if (!kAhead) load(row);
+    const Row<PER> n = widen<G, END>(n_ahead, lane, d), up = widen<G, END>(u_ahead, lane, d), gamma = of_gamma.row(lane, d);
+    Row<PER> x = widen<G, END>(h_ahead, lane, d), v;
+    if (kAhead && row + k.stride < k.T) load(row + k.stride);
 #pragma unroll
     for (int p = 0; p < PER; ++p) v.v[p] = n.v[p] * gamma.v[p];
     const BackSums b = back_sums<G, END>(x, v, lane, d, k.centre, k.eps, gs);
@@ -137,41 +135,31 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackA
   int row = blockIdx.x * Group<G>::kRows + Group<G>::index();
   RawRow<YT, PER> y_ahead{}, g_ahead{};
   RawRow<HT, PER> h_ahead{};
-  if (row < k.T) {
-    const size_t at = static_cast<size_t>(row) * d;
+  auto load = [&](int r) {
+    const size_t at = static_cast<size_t>(r) * d;
     y_ahead = load_raw<G, PER, END>(y + at, lane, d);
     h_ahead = load_raw<G, PER, END>(dh_out + at, lane, d);
     if (full) g_ahead = load_raw<G, PER, END>(gate + at, lane, d);
-  }
-  const Row<PER> gamma = load_params<G, PER, END>(k.gamma, 1.f, lane, d), beta = load_params<G, PER, END>(k.beta, 0.f, lane, d);
+  };
+  constexpr bool kAhead = !kWide<G, PER>;
+  if (kAhead && row < k.T) load(row);
+  const Params<G, PER, END> of_gamma(k.gamma, 1.f, lane, d), of_beta(k.beta, 0.f, lane, d);
   // a channel gate's value; its slope comes from it
-  Row<PER> value = load_params<G, PER, END>(channel ? static_cast<const float*>(k.gate) : nullptr, 1.f, lane, d);
-  if (channel && k.sigmoid) {
-#pragma unroll
-    for (int p = 0; p < PER; ++p)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) value.v[p][i] = sigmoid(value.v[p][i]);
-  }
+  Params<G, PER, END> value(channel ? static_cast<const float*>(k.gate) : nullptr, 1.f, lane, d);
+  if (value.kKept && channel && k.sigmoid) sigmoid_row(value.kept);
   for (; row < k.T; row += k.stride) {
     const size_t at = static_cast<size_t>(row) * d;
-    Row<PER> x = widen(y_ahead), up = widen(h_ahead), g = full ? widen(g_ahead) : value, v;
-    if (row + k.stride < k.T) {
-      const size_t next = static_cast<size_t>(row + k.stride) * d;
-      y_ahead = load_raw<G, PER, END>(y + next, lane, d);
-      h_ahead = load_raw<G, PER, END>(dh_out + next, lane, d);
-      if (full) g_ahead = load_raw<G, PER, END>(gate + next, lane, d);
-    }
+    if (!kAhead) load(row);
+    Row<PER> x = widen<G, END>(y_ahead, lane, d), up = widen<G, END>(h_ahead, lane, d), v;
+    Row<PER> g = full ? widen<G, END>(g_ahead, lane, d) : value.row(lane, d);
+    if (kAhead && row + k.stride < k.T) load(row + k.stride);
     if (k.dh != nullptr) {
 #pragma unroll
       for (int p = 0; p < PER; ++p) v.v[p] = up.v[p] * k.a;
       store_row<G, END>(static_cast<HT*>(k.dh) + at, v, lane, d);
     }
-    if (full && k.sigmoid) {
-#pragma unroll
-      for (int p = 0; p < PER; ++p)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g.v[p][i] = sigmoid(g.v[p][i]);
-    }
+    if (k.sigmoid && (full || (!value.kKept && channel))) sigmoid_row(g);
+    const Row<PER> gamma = of_gamma.row(lane, d);
     float of_token = 1.f;
     if (token) {
       of_token = static_cast<const float*>(k.gate)[row];
@@ -185,6 +173,7 @@ __global__ __launch_bounds__(Group<G>::kThreads) void exit_back_kernel(ExitBackA
     }
     BackSums b{1.f, 0.f, 0.f};
     if (norm) b = back_sums<G, END>(x, v, lane, d, k.norm_out == UMEM_NORM_LAYER, k.eps, gs);
+    const Row<PER> beta = of_beta.row(lane, d);
     float st = 0.f;
 #pragma unroll
     for (int p = 0; p < PER; ++p)
@@ -264,6 +253,9 @@ __global__ __launch_bounds__(kColWide * kColDeep) void column_sum_kernel(ColumnA
 
 // Workgroups of a backward, and its rows of partial sums.
 constexpr int kMaxParts = 512;
+// Rows of 4,097 to 8,192 (row_shape), 512 threads a row: the exit's backward of 2,048 fp32 rows of 5,000 87 us, with 1,024
+// threads 117; bf16 50 and 67.
+constexpr int kFours8K = 4;
 
 hipError_t launch_columns(const ColumnArgs& c, hipStream_t s) {
   const int n = c.q * c.d;
@@ -275,7 +267,7 @@ hipError_t launch_columns(const ColumnArgs& c, hipStream_t s) {
 
 size_t block_backward_workspace_bytes(const umem_block_desc& bd, int T) {
   if (T == 0) return 0;
-  const size_t bytes = static_cast<size_t>(row_workgroups(row_shape(bd.d), T, kMaxParts)) * 3 * bd.d * sizeof(float);
+  const size_t bytes = static_cast<size_t>(row_workgroups(row_shape(bd.d, kFours8K), T, kMaxParts)) * 3 * bd.d * sizeof(float);
   return (bytes + 255) / 256 * 256;
 }
 
@@ -283,12 +275,12 @@ hipError_t launch_block_in_backward(const umem_block_desc& bd, int T, const void
                                     const void* dn, const void* dres, void* dh, float* dgamma, float* dbeta,
                                     bool accumulate, void* ws, hipStream_t s) {
   clear_stale_error();
-  const RowShape shape = row_shape(bd.d);
+  const RowShape shape = row_shape(bd.d, kFours8K);
   const int wgs = row_workgroups(shape, T, kMaxParts);
   const EntryBackArgs k{h, dn, dres, gamma, dh, static_cast<float*>(ws), T, bd.d, wgs * (shape.group == 64 ? 4 : 1),
                         bd.norm_in == UMEM_NORM_LAYER, dbeta != nullptr, bd.eps};
 #define UMEM_ROW_GO(K, THR) hipLaunchKernelGGL(K, dim3(wgs), dim3(THR), 0, s, k)
-  UMEM_ROW_LAUNCH(entry_back_kernel)
+  UMEM_ROW_LAUNCH(entry_back_kernel, kFours8K)
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   return launch_columns({static_cast<const float*>(ws), {dgamma, dbeta, nullptr}, dbeta ? 2 : 1, bd.d, wgs, accumulate}, s);
@@ -299,12 +291,12 @@ hipError_t launch_block_out_backward(const umem_block_desc& bd, int T, const voi
                                      void* dgate, float* dgamma, float* dbeta, bool accumulate, void* ws,
                                      hipStream_t s) {
   clear_stale_error();
-  const RowShape shape = row_shape(bd.d);
+  const RowShape shape = row_shape(bd.d, kFours8K);
   const int wgs = row_workgroups(shape, T, kMaxParts);
   const ExitBackArgs k{y, gate, dh_out, gamma, beta, dh, dy, dgate, static_cast<float*>(ws), T, bd.d,
                        wgs * (shape.group == 64 ? 4 : 1), bd.norm_out, bd.gate, bd.gate_act == UMEM_ACT_SIGMOID,
                        bd.eps, bd.res_scale, bd.out_scale};
-  UMEM_ROW_LAUNCH(exit_back_kernel)
+  UMEM_ROW_LAUNCH(exit_back_kernel, kFours8K)
 #undef UMEM_ROW_GO
   const hipError_t e = hipGetLastError();
   ColumnArgs c{static_cast<const float*>(ws), {nullptr, nullptr, nullptr}, 0, bd.d, wgs, accumulate};

@@ -40,9 +40,22 @@ struct Row {
 
 // How rows end: they fill their group's registers (d = 4 G PER), end between two fours, or within one.
 // Loads past a row's fours are sent to its first four and the result dropped, so that only a last, partial
-// four takes a branch.  A branch around every load, and an element by element end in it, cost 900 rows of 4,092
-// 22 us to leave the block, 14 so; full rows without the selects 4,096 bf16 rows of 2,048 19.0, 20.7 with them.
+// four takes a branch, of bf16 none.  A branch around every load, and an element by element end in it, cost 900
+// rows of 4,092 22 us to leave the block, 14 so; full rows without the selects 4,096 bf16 rows of 2,048 19.0, 20.7
+// with them.  bf16 elements taken singly share a register with what the row's other loads write: 8,192 bf16
+// rows of 2,047 left the block in 65 us, 50 with the end taken from the row's last four (their backward 100 and
+// 69; entry's 66 and 45); fp32 rows are 5 to 15 percent faster with the branch.
 enum RowEnd { kFull, kFours, kAny };
+
+// Rows past 8,192, 16 elements to each of 1,024 threads with 128 registers: a group's parameters are read again
+// for each row, and few or none of the next row's loads are in flight, or registers are spilled (1,024 rows of
+// 12,288 left the block in 194 us, 86 so, in bf16 135 and 51).
+template <int G, int PER>
+constexpr bool kWide = G == 1024 && PER == 4;
+
+// Rows of bf16 and the widest, where they end within a four, are masked where they are used, in widen.
+template <typename T, int G, int PER, RowEnd END>
+constexpr bool kLate = END == kAny && (sizeof(T) == 2 || kWide<G, PER>);
 
 template <int G, int PER, RowEnd END, typename T>
 __device__ __forceinline__ RawRow<T, PER> load_raw(const T* row, int lane, int d) {
@@ -52,6 +65,11 @@ __device__ __forceinline__ RawRow<T, PER> load_raw(const T* row, int lane, int d
     const int e = (p * G + lane) * 4;
     if (END == kFull) {
       r.v[p] = *reinterpret_cast<const typename Quad<T>::type*>(row + e);
+      continue;
+    }
+    if (kLate<T, G, PER, END> && d >= 4) {
+      // a last, partial four is the row's last four elements
+      r.v[p] = *reinterpret_cast<const typename Quad<T>::type*>(row + (e + 4 <= d ? e : e < d ? d - 4 : 0));
       continue;
     }
     r.v[p] = T(0);
@@ -69,25 +87,51 @@ __device__ __forceinline__ RawRow<T, PER> load_raw(const T* row, int lane, int d
   return r;
 }
 
-template <typename T, int PER>
-__device__ __forceinline__ Row<PER> widen(const RawRow<T, PER>& r) {
+template <int G, RowEnd END, typename T, int PER>
+__device__ __forceinline__ Row<PER> widen(const RawRow<T, PER>& r, int lane, int d) {
   Row<PER> x;
 #pragma unroll
-  for (int p = 0; p < PER; ++p)
+  for (int p = 0; p < PER; ++p) {
+    typename Quad<T>::type q = r.v[p];
+    if (kLate<T, G, PER, END> && d >= 4) {
+      const int e = (p * G + lane) * 4, rest = d & 3;      // 1 to 3 elements, at the end of the last four
+      const typename Quad<T>::type last = {rest == 1 ? q.w : rest == 2 ? q.z : q.y,
+                                           rest == 1 ? T(0) : rest == 2 ? q.w : q.z, rest == 3 ? q.w : T(0), T(0)};
+      q = e + 4 <= d ? q : last;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[p][i] = static_cast<float>(r.v[p][i]);
+      for (int i = 0; i < 4; ++i) q[i] = e < d ? q[i] : T(0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.v[p][i] = static_cast<float>(q[i]);
+  }
   return x;
 }
 
 // A vector of parameters [d], or `otherwise` in every element where there is none.
 template <int G, int PER, RowEnd END>
 __device__ __forceinline__ Row<PER> load_params(const float* p, float otherwise, int lane, int d) {
-  if (p != nullptr) return widen<float, PER>(load_raw<G, PER, END>(p, lane, d));
+  if (p != nullptr) return widen<G, END>(load_raw<G, PER, END>(p, lane, d), lane, d);
   Row<PER> r;
 #pragma unroll
   for (int q = 0; q < PER; ++q) r.v[q] = otherwise;
   return r;
 }
+
+// Parameters of a group's columns, in registers over its rows where there are enough.
+template <int G, int PER, RowEnd END>
+struct Params {
+  static constexpr bool kKept = !kWide<G, PER>;
+  const float* p;
+  float otherwise;
+  Row<PER> kept;
+  __device__ __forceinline__ Params(const float* from, float o, int lane, int d) : p(from), otherwise(o) {
+    if constexpr (kKept) kept = load_params<G, PER, END>(p, otherwise, lane, d);
+  }
+  __device__ __forceinline__ Row<PER> row(int lane, int d) const {
+    if constexpr (kKept) return kept;
+    else return load_params<G, PER, END>(p, otherwise, lane, d);
+  }
+};
 
 template <int G, RowEnd END, int PER, typename T>
 __device__ __forceinline__ void store_row(T* row, const Row<PER>& x, int lane, int d) {
@@ -208,18 +252,28 @@ __device__ __forceinline__ void normalise(Row<PER>& x, int lane, int d, bool cen
 // 1 / (1 + e^-z); the reciprocal is the hardware's, within one step of fp32.
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + expf(-z)); }
 
+template <int PER>
+__device__ __forceinline__ void sigmoid_row(Row<PER>& g) {
+#pragma unroll
+  for (int p = 0; p < PER; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g.v[p][i] = sigmoid(g.v[p][i]);
+}
+
 // How rows of d elements are dealt to threads: eight elements a thread where the row has them (more in
-// flight and in registers lets fewer waves run), four in the shortest rows.
+// flight and in registers lets fewer waves run), four in the shortest rows.  From 4,097 to 8,192 by `fours` fours a
+// thread, of 512 (4) or 1,024 (2) threads.
 struct RowShape {
   int group, per;
 };
-inline RowShape row_shape(int d) {
+inline RowShape row_shape(int d, int fours) {
   if (d <= 256) return {64, 1};
   if (d <= 512) return {64, 2};
   if (d <= 1024) return {256, 1};
   if (d <= 2048) return {256, 2};
   if (d <= 4096) return {512, 2};
-  return {1024, d <= 8192 ? 2 : 4};
+  if (d <= 8192) return {2048 / fours, fours};
+  return {1024, 4};
 }
 
 // Workgroups for T rows, at most `most`, each with as many rows as the others or one fewer.
@@ -234,25 +288,25 @@ inline int row_workgroups(const RowShape& s, int T, int most) {
   if (bd.d == 4 * G * PER) UMEM_ROW_GO((KERNEL<HT, YT, G, PER, kFull>), THR);               \
   else if (bd.d % 4 == 0) UMEM_ROW_GO((KERNEL<HT, YT, G, PER, kFours>), THR);               \
   else UMEM_ROW_GO((KERNEL<HT, YT, G, PER, kAny>), THR);
-#define UMEM_ROW_SHAPES(KERNEL, HT, YT)                                     \
+#define UMEM_ROW_SHAPES(KERNEL, HT, YT, FOURS)                              \
   switch (shape.group * 8 + shape.per) {                                    \
     case 64 * 8 + 1: UMEM_ROW_FULL(KERNEL, HT, YT, 64, 1, 256) break;       \
     case 64 * 8 + 2: UMEM_ROW_FULL(KERNEL, HT, YT, 64, 2, 256) break;       \
     case 256 * 8 + 1: UMEM_ROW_FULL(KERNEL, HT, YT, 256, 1, 256) break;     \
     case 256 * 8 + 2: UMEM_ROW_FULL(KERNEL, HT, YT, 256, 2, 256) break;     \
     case 512 * 8 + 2: UMEM_ROW_FULL(KERNEL, HT, YT, 512, 2, 512) break;     \
-    case 1024 * 8 + 2: UMEM_ROW_FULL(KERNEL, HT, YT, 1024, 2, 1024) break;  \
+    case 2048 / FOURS * 8 + FOURS: UMEM_ROW_FULL(KERNEL, HT, YT, 2048 / FOURS, FOURS, 2048 / FOURS) break; \
     default: UMEM_ROW_FULL(KERNEL, HT, YT, 1024, 4, 1024) break;            \
   }
-#define UMEM_ROW_LAUNCH(KERNEL)                            \
+#define UMEM_ROW_LAUNCH(KERNEL, FOURS)                     \
   if (bd.htype == UMEM_F32 && bd.ytype == UMEM_F32) {      \
-    UMEM_ROW_SHAPES(KERNEL, float, float)                  \
+    UMEM_ROW_SHAPES(KERNEL, float, float, FOURS)                  \
   } else if (bd.htype == UMEM_F32) {                       \
-    UMEM_ROW_SHAPES(KERNEL, float, __bf16)                 \
+    UMEM_ROW_SHAPES(KERNEL, float, __bf16, FOURS)                 \
   } else if (bd.ytype == UMEM_F32) {                       \
-    UMEM_ROW_SHAPES(KERNEL, __bf16, float)                 \
+    UMEM_ROW_SHAPES(KERNEL, __bf16, float, FOURS)                 \
   } else {                                                 \
-    UMEM_ROW_SHAPES(KERNEL, __bf16, __bf16)                \
+    UMEM_ROW_SHAPES(KERNEL, __bf16, __bf16, FOURS)                \
   }
 
 }  // namespace umem

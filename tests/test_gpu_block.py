@@ -101,7 +101,9 @@ def column_tol(terms, terms_err):
 
 # rows in a wave's registers, in a workgroup's of 256 and of 1024; odd widths; few rows and many
 SIZES = [(1, 1), (3, 3), (5, 64), (1, 255), (7, 512), (1025, 513), (2, 1000), (1023, 1024), (1100, 1023),
-         (1024, 2048), (4, 2048), (1, 2050), (33, 4096), (9, 4100), (3, 5001), (2, 16384)]
+         (1024, 2048), (4, 2048), (1, 2050), (33, 4096), (9, 4100), (3, 5001), (2, 16384),
+         (520, 8192), (600, 9000), (515, 12289), (3, 16383), (700, 6001), (5, 8193), (530, 8197), (514, 16384),
+         (4, 8190), (540, 4099)]
 TYPES = [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")]
 
 
