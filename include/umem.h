@@ -449,8 +449,8 @@ UMEM_API umem_status umem_grad_norm(int32_t n, const umem_grad* grads, float* no
 /* Clipping to a global norm: out = g c, c = 1 where *norm <= max_norm, else max_norm / *norm (a NaN norm
  * makes every element NaN; an infinite one makes finite elements 0).  A bf16 product is rounded
  * once.  norm fp32 [1] on the device, as umem_grad_norm writes it; max_norm >= 0, +inf for none.
- * Rows from *n_rows on are left as they are.  An out that overlaps another gradient or out, or its own
- * gradient without being equal to it, is UMEM_ERR_INVALID_ARG. */
+ * Rows from *n_rows on are left as they are.  An out that overlaps another gradient or out, norm or
+ * a row count, or its own gradient without being equal to it, is UMEM_ERR_INVALID_ARG. */
 UMEM_API umem_status umem_grad_clip(int32_t n, const umem_grad* grads, float max_norm, const float* norm,
                            hipStream_t stream);
 

@@ -4,9 +4,10 @@
 //
 // Both passes stream: the norm reads every element once, the clip reads and writes it, from the last piece to
 // the first, so that it begins with what the norm left in the caches.  The tensors travel in the kernel's
-// arguments, up to 112 a launch, so a step's call copies nothing to the GPU and can be captured.  A tensor is cut into pieces of one size, a workgroup each; a piece's sum of squares
-// is fp64 (the square of a float is exact there, and the conversion and the addition cost less than the
-// load), written to its own place and added up in order by one workgroup.
+// arguments, up to 112 a launch, so a step's call copies nothing to the GPU and can be captured.  A tensor is
+// cut into pieces of one size, a workgroup each; a piece's sum of squares is fp64 (the square of a float is
+// exact there, and the conversion and the addition cost less than the load), written to its own place and
+// added up in order by one workgroup.
 //
 // Bound by HBM.  The clip's loads and stores are marked as not to be kept: kept in the 256 MB cache, written
 // lines were evicted while later kernels read, and 786 MB of gradients took 432 us in both passes together,

@@ -662,13 +662,14 @@ umem_status check_grads(int32_t n, const umem_grad* grads, bool for_clip) {
   return UMEM_OK;
 }
 
-// Whether an out overlaps another gradient or out, or its own gradient other than being it.
-bool grads_clash(int32_t n, const umem_grad* grads) {
+// Whether an out overlaps another gradient or out, its own gradient other than being it, or what the kernels
+// read beside them: the norm and the row counts.
+bool grads_clash(int32_t n, const umem_grad* grads, const float* norm) {
   struct Range {
     uintptr_t from, to;
   };
-  static_assert(2 * kMaxGrads * sizeof(Range) <= 64 << 10, "the ranges live on the caller's stack");
-  Range out[kMaxGrads], in[kMaxGrads];
+  static_assert((3 * kMaxGrads + 1) * sizeof(Range) <= 128 << 10, "the ranges live on the caller's stack");
+  Range out[kMaxGrads], in[2 * kMaxGrads + 1];
   int outs = 0, ins = 0;
   for (int i = 0; i < n; ++i) {
     const umem_grad& g = grads[i];
@@ -677,7 +678,10 @@ bool grads_clash(int32_t n, const umem_grad* grads) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(g.grad), b = reinterpret_cast<uintptr_t>(g.out);
     out[outs++] = {b, b + bytes};
     if (a != b) in[ins++] = {a, a + bytes};
+    const uintptr_t rows = reinterpret_cast<uintptr_t>(g.n_rows);
+    if (rows != 0 && (ins == 0 || in[ins - 1].from != rows)) in[ins++] = {rows, rows + sizeof(int32_t)};
   }
+  in[ins++] = {reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm) + sizeof(float)};
   const auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
   if (!std::is_sorted(out, out + outs, before)) std::sort(out, out + outs, before);
   if (!std::is_sorted(in, in + ins, before)) std::sort(in, in + ins, before);
@@ -708,7 +712,8 @@ UMEM_API umem_status umem_grad_norm(int32_t n, const umem_grad* grads, float* no
                                     size_t ws_bytes, hipStream_t stream) {
   const umem_status st = check_grads(n, grads, false);
   if (st != UMEM_OK) return st;
-  if (norm == nullptr || !aligned(norm, 4) || !aligned(sumsq, 8)) return UMEM_ERR_INVALID_ARG;
+  if (norm == nullptr || !aligned(norm, 4) || !aligned(sumsq, 8) || !apart({norm, sizeof(float)}, {sumsq, sizeof(double)}))
+    return UMEM_ERR_INVALID_ARG;
   const size_t need = grad_workspace_bytes(n, grads);
   if (need > 0 && (ws == nullptr || !aligned(ws, 16) || ws_bytes < need)) return UMEM_ERR_WORKSPACE;
   return hip_status(launch_grad_norm(n, grads, norm, sumsq, ws, stream));
@@ -718,7 +723,7 @@ UMEM_API umem_status umem_grad_clip(int32_t n, const umem_grad* grads, float max
                                     hipStream_t stream) {
   const umem_status st = check_grads(n, grads, true);
   if (st != UMEM_OK) return st;
-  if (!(max_norm >= 0.0f) || norm == nullptr || !aligned(norm, 4) || grads_clash(n, grads)) return UMEM_ERR_INVALID_ARG;
+  if (!(max_norm >= 0.0f) || norm == nullptr || !aligned(norm, 4) || grads_clash(n, grads, norm)) return UMEM_ERR_INVALID_ARG;
   return hip_status(launch_grad_clip(n, grads, max_norm, norm, stream));
 }
 

@@ -154,6 +154,19 @@ def test_grad_refusals():
         assert U.umem_grad_clip(len(rows), grads(*rows), 1.0, norm, 0) == ARG, rows
 
 
+def test_a_clipped_gradient_is_apart_from_the_norm_and_the_row_counts():
+    """What the kernels read while they write the outs."""
+    row, k = (at(0), at(1), at(2), 4, 1024, 0), 4 * 4 * 1024
+    assert U.umem_grad_clip(1, grads(row), 1.0, at(1), 0) == ARG
+    assert U.umem_grad_clip(1, grads(row), 1.0, at(1) + k - 4, 0) == ARG
+    assert U.umem_grad_clip(1, grads((at(0), at(1), at(1) + 8, 4, 1024, 0)), 1.0, at(9), 0) == ARG
+    other = (at(3), at(4), None, 4, 1024, 1)
+    assert U.umem_grad_clip(2, grads((at(0), at(1), at(4), 4, 1024, 0), other), 1.0, at(9), 0) == ARG
+    assert U.umem_grad_norm(1, grads(row), at(9) + 4, at(9), at(10), 1 << 20, 0) == ARG
+    # apart, in a table without elements, which launches nothing
+    assert U.umem_grad_clip(1, grads((at(0), at(1), at(2), 0, 1024, 0)), 1.0, at(9), 0) == OK
+
+
 def test_grad_tables_of_the_binding():
     rows = [(at(0), at(1), 0, 4, 100, 0), (at(2), at(2), at(3), 7, 33, 1)]
     table = np.array(rows, dtype=np.int64)
