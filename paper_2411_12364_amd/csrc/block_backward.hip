@@ -251,8 +251,9 @@ __global__ __launch_bounds__(kColWide * kColDeep) void column_sum_kernel(ColumnA
   }
 }
 
-// Workgroups of a backward, and its rows of partial sums.
-constexpr int kMaxParts = 512;
+// Workgroups of a backward, and its rows of partial sums: two for each CU, or one of 512 threads or more, whose rows
+// are as many bytes (exit's backward of 2,048 bf16 rows of 4,096 31.5 us, with two 34, of 300 rows 13 and 16; 8,192 bf16 rows of 2,048 take 49 with two workgroups of 256 threads, 59 with one).
+int most_parts(const RowShape& s) { return s.group >= 512 ? 256 : 512; }
 // Rows of 4,097 to 8,192 (row_shape), 512 threads a row: the exit's backward of 2,048 fp32 rows of 5,000 87 us, with 1,024
 // threads 117; bf16 50 and 67.
 constexpr int kFours8K = 4;
@@ -267,7 +268,8 @@ hipError_t launch_columns(const ColumnArgs& c, hipStream_t s) {
 
 size_t block_backward_workspace_bytes(const umem_block_desc& bd, int T) {
   if (T == 0) return 0;
-  const size_t bytes = static_cast<size_t>(row_workgroups(row_shape(bd.d, kFours8K), T, kMaxParts)) * 3 * bd.d * sizeof(float);
+  const RowShape shape = row_shape(bd.d, kFours8K);
+  const size_t bytes = static_cast<size_t>(row_workgroups(shape, T, most_parts(shape))) * 3 * bd.d * sizeof(float);
   return (bytes + 255) / 256 * 256;
 }
 
@@ -276,7 +278,7 @@ hipError_t launch_block_in_backward(const umem_block_desc& bd, int T, const void
                                     bool accumulate, void* ws, hipStream_t s) {
   clear_stale_error();
   const RowShape shape = row_shape(bd.d, kFours8K);
-  const int wgs = row_workgroups(shape, T, kMaxParts);
+  const int wgs = row_workgroups(shape, T, most_parts(shape));
   const EntryBackArgs k{h, dn, dres, gamma, dh, static_cast<float*>(ws), T, bd.d, wgs * (shape.group == 64 ? 4 : 1),
                         bd.norm_in == UMEM_NORM_LAYER, dbeta != nullptr, bd.eps};
 #define UMEM_ROW_GO(K, THR) hipLaunchKernelGGL(K, dim3(wgs), dim3(THR), 0, s, k)
@@ -292,7 +294,7 @@ hipError_t launch_block_out_backward(const umem_block_desc& bd, int T, const voi
                                      hipStream_t s) {
   clear_stale_error();
   const RowShape shape = row_shape(bd.d, kFours8K);
-  const int wgs = row_workgroups(shape, T, kMaxParts);
+  const int wgs = row_workgroups(shape, T, most_parts(shape));
   const ExitBackArgs k{y, gate, dh_out, gamma, beta, dh, dy, dgate, static_cast<float*>(ws), T, bd.d,
                        wgs * (shape.group == 64 ? 4 : 1), bd.norm_out, bd.gate, bd.gate_act == UMEM_ACT_SIGMOID,
                        bd.eps, bd.res_scale, bd.out_scale};
