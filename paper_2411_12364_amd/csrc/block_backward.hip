@@ -133,7 +133,8 @@ __global__ __launch_bounds__(Group<G>::kThreads) void entry_back_kernel(EntryBac
   const Params<G, PER, END> of_gamma(k.gamma, 1.f, lane, d);
   for (; row < k.T; row += k.stride) {
     if (!kAhead) load(row);
-    const Row<PER> n = widen<G, END>(n_ahead, lane, d), up = widen<G, END>(u_ahead, lane, d), gamma = of_gamma.row(lane, d);
+    const Row<PER> n = widen<G, END>(n_ahead, lane, d), up = widen<G, END>(u_ahead, lane, d),
+                   gamma = of_gamma.row(lane, d);
     Row<PER> x = widen<G, END>(h_ahead, lane, d), v;
     if (kAhead && row + k.stride < k.T) load(row + k.stride);
 #pragma unroll
@@ -295,8 +296,9 @@ __global__ __launch_bounds__(kColWide * kColDeep) void column_sum_kernel(ColumnA
   }
 }
 
-// Workgroups of a backward, and its rows of partial sums: two for each CU, or one of 512 threads or more, whose rows
-// are as many bytes (exit's backward of 2,048 bf16 rows of 4,096 31.5 us, with two 34, of 300 rows 13 and 16; 8,192 bf16 rows of 2,048 take 49 with two workgroups of 256 threads, 59 with one).
+// Workgroups of a backward, and its rows of partial sums: two for each CU, or one of 512 threads or more, whose
+// rows are as many bytes (exit's backward of 2,048 bf16 rows of 4,096 31.5 us, with two 34, of 300 rows 13 and
+// 16; 8,192 bf16 rows of 2,048 take 49 with two workgroups of 256 threads, 59 with one).
 int most_parts(const RowShape& s) { return s.group >= 512 ? 256 : 512; }
 // Rows of 4,097 to 8,192 (row_shape), 512 threads a row: the exit's backward of 2,048 fp32 rows of 5,000 87 us, with 1,024
 // threads 117; bf16 50 and 67.
