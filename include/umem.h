@@ -386,7 +386,7 @@ UMEM_API umem_status umem_block_out(const umem_block_desc* bd, int32_t T, const 
                            const float* gamma_next, const float* beta_next, void* n_next,
                            hipStream_t stream);
 
-/* Scratch bytes that the two backward calls need for T tokens. */
+/* Scratch bytes that the two backward calls need for T tokens or fewer. */
 UMEM_API umem_status umem_block_backward_workspace_size(const umem_block_desc* bd, int32_t T, size_t* bytes);
 
 /* Backward of umem_block_in, with the gradient that the stream has from past the block added:

@@ -312,10 +312,13 @@ hipError_t launch_columns(const ColumnArgs& c, hipStream_t s) {
 
 }  // namespace
 
+// A workgroup's row of partial sums for each of the most workgroups that T rows or fewer take: row_workgroups
+// itself falls where another turn of rows begins (512 rows of 2,048: 512 workgroups; 513: 257), and a
+// workspace sized once for the longest batch has to do for the shorter ones.
 size_t block_backward_workspace_bytes(const umem_block_desc& bd, int T) {
   if (T == 0) return 0;
   const RowShape shape = row_shape(bd.d, kFours8K);
-  const size_t bytes = static_cast<size_t>(row_workgroups(shape, T, most_parts(shape))) * 3 * bd.d * sizeof(float);
+  const size_t bytes = static_cast<size_t>(std::min(row_groups(shape, T), most_parts(shape))) * 3 * bd.d * sizeof(float);
   return (bytes + 255) / 256 * 256;
 }
 

@@ -276,10 +276,14 @@ inline RowShape row_shape(int d, int fours) {
   return {1024, 4};
 }
 
+// Workgroups that hold T rows at once.
+inline int row_groups(const RowShape& s, int T) {
+  const int rows = s.group == 64 ? 4 : 1;
+  return (T + rows - 1) / rows;
+}
 // Workgroups for T rows, at most `most`, each with as many rows as the others or one fewer.
 inline int row_workgroups(const RowShape& s, int T, int most) {
-  const int rows = s.group == 64 ? 4 : 1;
-  const int need = (T + rows - 1) / rows, turns = (need + most - 1) / most;
+  const int need = row_groups(s, T), turns = (need + most - 1) / most;
   return (need + turns - 1) / turns;
 }
 

@@ -108,6 +108,16 @@ def test_block_backward_refusals():
     assert call(dy=base["dh"]) == ARG and call(dgamma=base["gamma"]) == ARG and call(dbeta=ws + 16) == ARG
 
 
+@pytest.mark.parametrize("d", [1, 256, 257, 512, 513, 1024, 2048, 2049, 4096, 5000, 8192, 8193, 16384])
+def test_block_workspace_never_falls_with_the_tokens(d):
+    """A program sizes its workspace once, for its longest batch."""
+    sizes = [U.umem_block_backward_workspace_size(bd(d=d), T) for T in range(4200)]
+    assert all(st == OK for st, _ in sizes)
+    sizes = [n for _, n in sizes] + [U.umem_block_backward_workspace_size(bd(d=d), T)[1] for T in (1 << 16, (1 << 16) + 1, 1 << 20)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+    assert sizes[-1] <= 512 * 3 * 4 * d + 256                            # whatever the batch
+
+
 def grads(*rows):
     return (U.umem_grad * len(rows))(*[U.umem_grad(*r) for r in rows])
 

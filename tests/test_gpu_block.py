@@ -242,6 +242,25 @@ def test_exit_backward(i, size, norm_out, gate):
         assert before is None or torch.equal(after, before + alone)
 
 
+@pytest.mark.parametrize("T,longest,d", [(512, 513, 2048), (256, 257, 5000), (2048, 2049, 512), (300, 16384, 300)])
+def test_the_workspace_of_a_longer_batch(T, longest, d):
+    """A batch in the workspace sized for a longer one: the same gradients."""
+    x = Inputs(T, d, 17, gate="channel")
+    bd = desc(d, "layer", "layer", "channel")
+    need = U.umem_block_backward_workspace_size(bd, longest)[1]
+
+    def grads(ws, n):
+        dh, dy, dg, db, dg2, db2, dgate = (torch.empty_like(t) for t in (x.h, x.y, x.gamma, x.beta, x.gamma, x.beta, x.gate))
+        U.check(U.umem_block_in_backward(bd, T, x.h, x.gamma, x.dn, x.dres, dh, dg, db, 0, ws, n))
+        U.check(U.umem_block_out_backward(bd, T, x.y, x.gate, x.gamma, x.beta, x.dh_out, None, dy, dgate, dg2, db2, 0, ws, n))
+        return dh, dy, dg, db, dg2, db2, dgate
+
+    ws = ws_for(bd, T)
+    want = grads(ws, ws.numel())
+    ws = torch.full((need,), 0xA5, dtype=torch.uint8, device="cuda")
+    assert all(torch.equal(a, b) for a, b in zip(grads(ws, need), want))
+
+
 def test_rows_keep_to_themselves():
     """A token of NaN or infinities, one of zeros, and a gate of zero: every other row as without them."""
     T, d = 1200, 1024
