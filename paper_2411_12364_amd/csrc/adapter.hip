@@ -621,6 +621,7 @@ bool by_tiles(const umem_adapter_desc& ad, int T) { return static_cast<int64_t>(
 // Pieces of d_in: the widest that make 512 workgroups (two for each CU; 1,024 were no faster), as wider ones
 // leave fewer partial sums.  nb: 16-byte pieces of x to a thread.  8 of bf16 take 66 KiB of LDS, two workgroups
 // to a CU; of fp32 (three parts) 99 KiB, one: 4,096 tokens by 2,048 then take 16.5 us, with 4 13.6.
+constexpr int kLowWorkgroups = 512;
 struct Plan {
   int nb, piece, pieces, splits, rank_tiles;
 };
@@ -630,7 +631,7 @@ Plan plan_of(const umem_adapter_desc& ad, int T) {
   for (p.nb = ad.xtype == UMEM_F32 ? 4 : 8;; p.nb /= 2) {
     p.piece = ad.xtype == UMEM_F32 ? piece_width<float>(p.nb) : piece_width<__bf16>(p.nb);
     p.pieces = (ad.d_in + p.piece - 1) / p.piece;
-    if (p.nb == 1 || static_cast<int64_t>(tiles) * p.pieces >= 512) break;
+    if (p.nb == 1 || static_cast<int64_t>(tiles) * p.pieces >= kLowWorkgroups) break;
   }
   p.splits = std::max(1, std::min(512 / tiles, (ad.d_out + 127) / 128));
   p.rank_tiles = (ad.rank + 15) / 16;
@@ -639,10 +640,18 @@ Plan plan_of(const umem_adapter_desc& ad, int T) {
 
 }  // namespace
 
+// The most that T tokens or fewer take: fewer tiles have narrower pieces, which leave more sums of a token (bf16 x of
+// 4,096, rank 32: 4,032 tokens 8.3 MB, 4,096 4.2).  So every width that T tokens or fewer take is looked at, at the
+// most tokens that take it.
 size_t adapter_workspace_bytes(const umem_adapter_desc& ad, int T) {
-  if (T == 0 || !by_tiles(ad, T)) return 0;
-  const Plan p = plan_of(ad, T);
-  return (static_cast<size_t>(p.pieces) * T * p.rank_tiles * 16 * sizeof(float) + 255) / 256 * 256;
+  size_t most = 0;
+  while (T > 0 && by_tiles(ad, T)) {
+    const Plan p = plan_of(ad, T);
+    most = std::max(most, (static_cast<size_t>(p.pieces) * T * p.rank_tiles * 16 * sizeof(float) + 255) / 256 * 256);
+    if (p.nb == 1) break;
+    T = ((kLowWorkgroups + p.pieces - 1) / p.pieces - 1) * kTile;
+  }
+  return most;
 }
 
 hipError_t launch_adapter_add(const umem_adapter_desc& ad, int T, const void* x, const int32_t* ids,

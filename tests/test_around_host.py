@@ -208,6 +208,19 @@ def test_adapter_descriptor(kw, want):
     assert U.umem_adapter_workspace_size(ad(), (1 << 20) + 1)[0] == UNS
 
 
+@pytest.mark.parametrize("kw", [
+    dict(d_in=1024, rank=16, xtype=1), dict(d_in=4096, rank=32, xtype=1), dict(d_in=2048, rank=64), dict(d_in=4096, rank=128),
+    dict(d_in=1 << 16, rank=128, xtype=1), dict(d_in=1 << 16, rank=8), dict(d_in=72, rank=24), dict(d_in=264, rank=128),
+    dict(d_in=8192, rank=8, xtype=1),
+])
+def test_adapter_workspace_never_falls_with_the_tokens(kw):
+    """A program sizes its workspace once, for its longest prompts."""
+    tokens = [*range(0, 9000), *range(9000, 70000, 61), 1 << 17, (1 << 20) - 1, 1 << 20]
+    sizes = [U.umem_adapter_workspace_size(ad(**kw), T) for T in tokens]
+    assert all(st == OK for st, _ in sizes)
+    assert all(a[1] <= b[1] for a, b in zip(sizes, sizes[1:]))
+
+
 def test_adapter_refusals():
     names = ["x", "ids", "a", "b", "scale", "base", "out"]
     base = {k: at(i) for i, k in enumerate(names)}

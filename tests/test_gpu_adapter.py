@@ -214,6 +214,22 @@ def test_base_of_negative_zeros(T, o):
     assert torch.signbit(s["base"]).all()
 
 
+@pytest.mark.parametrize("T,longest,rank,d_in,x", [(4032, 4096, 32, 4096, "bf16"), (1920, 4096, 32, 4096, "bf16"),
+                                                   (640, 1024, 64, 2048, "f32"), (1984, 1985, 32, 2048, "f32"),
+                                                   (100, 8192, 16, 1024, "f32")])
+def test_the_workspace_of_more_tokens(T, longest, rank, d_in, x):
+    """Fewer tokens in the workspace sized for more: the same sums."""
+    s = make(T, 9, rank, d_in, 264, 15, x)
+    ids = ids_of("runs", T, 9, s["g"])
+    want = call(s, ids).clone()
+    st, need = U.umem_adapter_workspace_size(s["desc"], longest)
+    U.check(st)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(want, 9.0)
+    U.check(U.umem_adapter_add(s["desc"], T, s["x"], ids, s["a"], s["b"], s["scale"], s["base"], out, ws, need))
+    assert torch.equal(out, want)
+
+
 def test_offsets_past_32_bits():
     """2^20 tokens of 2056: out has 2.16e9 elements."""
     T, d_out = 1 << 20, 2056
