@@ -35,6 +35,7 @@
  *   - Alignment: q/k/core 16 bytes, values and fp32 outputs 16 bytes, other arrays 4 bytes, unless
  *     stated otherwise.
  *   - T == 0 is a no-op once the descriptor is valid.
+ *   - A workspace's size never falls as the tokens grow: one sized for the longest batch does for all.
  *   - Functions are reentrant; calls on one stream run in order.
  */
 #ifndef UMEM_H
@@ -215,8 +216,9 @@ UMEM_API umem_status umem_forward(const umem_desc* desc, int32_t T, const float*
  * workspace taken from a static array of UMEM_STATIC_SCRATCH_BYTES in each GPU's memory instead
  * of the caller.  Neither this call nor the kernels it enqueues allocate or free memory.
  *   Arguments as for umem_forward, without ws and ws_bytes.
- *   UMEM_ERR_SCRATCH_LIMIT (nothing enqueued) when umem_workspace_size(desc, T) exceeds
- *   UMEM_STATIC_SCRATCH_BYTES (the 20.07M-slot decode layer fits up to 779 tokens).
+ *   UMEM_ERR_SCRATCH_LIMIT (nothing enqueued) when these T tokens need more than
+ *   UMEM_STATIC_SCRATCH_BYTES, which they do not where umem_workspace_size(desc, T) is within it (the
+ *   20.07M-slot decode layer fits up to 779 tokens).
  *   The array of a GPU is created with the library's code on that GPU and held until the process
  *   ends; the first call on a device looks up its address (UMEM_ERR_HIP if that fails).  `stream`
  *   must belong to the calling thread's current device.  Every call on one GPU uses the same

@@ -114,6 +114,17 @@ Layout layout(const umem_desc* d, int32_t T) {
   return L;
 }
 
+// The most bytes that T tokens or fewer take, so that a workspace sized once for the longest batch does for the
+// shorter ones.  A product over a long K is split in more ways where it has fewer tiles, and its partial sums
+// can then take more (a query of 2,048 by 896: 576 tokens 20.9 MB, 577 12.7).  The split changes at tiles of 64
+// rows alone, and between them every part grows.  A call itself asks for no more than it takes.
+template <typename F>
+size_t most_upto(int64_t T, F bytes) {
+  size_t most = bytes(static_cast<int32_t>(T));
+  for (int64_t t = 64; t < T; t += 64) most = std::max(most, bytes(static_cast<int32_t>(t)));
+  return most;
+}
+
 umem_status check_ws(const umem_desc* d, int32_t T, const void* ws, size_t ws_bytes) {
   const Layout L = layout(d, T);
   if (L.total > 0 && (ws == nullptr || !aligned(ws, kAlign) || ws_bytes < L.total))
@@ -188,7 +199,8 @@ UMEM_API umem_status umem_workspace_size(const umem_desc* desc, int32_t T, size_
   umem_status st = check_desc(desc);
   if (st == UMEM_OK) st = check_tokens(T);
   if (st != UMEM_OK) return st;
-  *bytes = layout(desc, T).total;
+  const bool project = desc->dv_virt > 0 || desc->d_out > 0;
+  *bytes = project ? most_upto(T, [=](int32_t t) { return layout(desc, t).total; }) : layout(desc, T).total;
   return UMEM_OK;
 }
 
@@ -287,7 +299,7 @@ UMEM_API umem_status umem_project_workspace_size(int32_t T, int32_t expand, int3
   umem_status st = check_project_shape(expand, dv, dv_virt, d_out, dv_virt > 0, d_out > 0);
   if (st == UMEM_OK) st = check_tokens(T);
   if (st != UMEM_OK) return st;
-  *bytes = project_workspace_bytes(T, expand, dv, dv_virt, d_out);
+  *bytes = most_upto(T, [=](int32_t t) { return project_workspace_bytes(t, expand, dv, dv_virt, d_out); });
   return UMEM_OK;
 }
 
@@ -329,6 +341,10 @@ umem_status check_query_ptrs(const umem_query_desc* qd, const float* x, const fl
   return UMEM_OK;
 }
 
+size_t query_workspace_most(const umem_query_desc& qd, int64_t T) {
+  return most_upto(T, [&](int32_t t) { return query_workspace_bytes(qd, t); });
+}
+
 umem_status check_query_tokens(int32_t B, int32_t L) {
   if (B < 0 || L < 0) return UMEM_ERR_INVALID_ARG;
   if (static_cast<int64_t>(B) * L > kMaxTokens) return UMEM_ERR_UNSUPPORTED;
@@ -346,7 +362,7 @@ UMEM_API umem_status umem_query_workspace_size(const umem_query_desc* qd, int32_
   umem_status st = check_query_desc(qd);
   if (st == UMEM_OK) st = check_query_tokens(B, L);
   if (st != UMEM_OK) return st;
-  *bytes = query_workspace_bytes(*qd, static_cast<int64_t>(B) * L);
+  *bytes = query_workspace_most(*qd, static_cast<int64_t>(B) * L);
   return UMEM_OK;
 }
 
@@ -802,7 +818,7 @@ UMEM_API umem_status umem_query_adapted_workspace_size(const umem_query_desc* qd
   const umem_status st = check_query_adapters(qd, ad, B, L);
   if (st != UMEM_OK) return st;
   const int64_t T = static_cast<int64_t>(B) * L;
-  *bytes = round_up(query_workspace_bytes(*qd, T)) + adapter_workspace_bytes(*ad, static_cast<int>(T));
+  *bytes = round_up(query_workspace_most(*qd, T)) + adapter_workspace_bytes(*ad, static_cast<int>(T));
   return UMEM_OK;
 }
 

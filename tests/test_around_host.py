@@ -268,6 +268,33 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         assert call(7) in (OK, ARG)                                     # a stream given: the caller's word
 
 
+def never_falls(size, tokens=(*range(0, 5000), *range(5000, 40000, 61), 1 << 16, 1 << 18, (1 << 18) + 1)):
+    sizes = [size(T) for T in tokens]
+    assert all(st == OK for st, _ in sizes)
+    assert all(a[1] <= b[1] for a, b in zip(sizes, sizes[1:]))
+
+
+@pytest.mark.parametrize("q", [(64, 3, 2, 32, 0), (2048, 5, 2, 224, 0), (1024, 3, 2, 64, 1), (768, 3, 4, 128, 0), (4096, 1, 1, 64, 1)])
+def test_query_workspaces_never_fall_with_the_tokens(q):
+    """Also where the query linear is split over d_model, in more ways for fewer tokens."""
+    qd = U.umem_query_desc(*q, 1e-5)
+    never_falls(lambda T: U.umem_query_workspace_size(qd, T, 1))
+    a = ad(d_in=q[0], d_out=(2 - q[4]) * q[2] * q[3], xtype=1, rank=32)
+    never_falls(lambda T: U.umem_query_adapted_workspace_size(qd, a, 1, T))
+
+
+@pytest.mark.parametrize("shape", [(1, 1024, 1024, 0), (4, 512, 1024, 2048), (1, 2048, 0, 2048), (1, 4096, 0, 1024), (1, 1 << 18, 0, 128),
+                                   (4, 896, 896, 2048), (6, 512, 336, 1024), (16, 2048, 256, 0)])
+def test_projection_workspaces_never_fall_with_the_tokens(shape):
+    never_falls(lambda T: U.umem_project_workspace_size(T, *shape))
+
+
+@pytest.mark.parametrize("n,dv,dv_virt,d_out", [(16, 128, 512, 2048), (16, 512, 0, 2048), (512, 1024, 0, 512), (64, 512, 1024, 512)])
+def test_layer_workspaces_never_fall_with_the_tokens(n, dv, dv_virt, d_out):
+    d = U.umem_desc(2, 256, n, 2, 16, 16, 1, 0, n * n, dv, 1, 1, dv_virt, d_out, 1)
+    never_falls(lambda T: U.umem_workspace_size(d, T))
+
+
 def test_adapted_query_refusals():
     qd = U.umem_query_desc(64, 3, 2, 32, 0, 1e-5)                        # 2 axes of 2 heads of 32: 128 outputs
     good = dict(xtype=1)
