@@ -171,7 +171,12 @@ __global__ __launch_bounds__(kThreads) void sort_scatter_kernel(
 // Tiles of 2048 pairs (half the steps in each wave's chain, twice the workgroups) where there are
 // several; up to 4096 pairs one tile needs no scan, and from 2^19 pairs on the chip is full either
 // way and tiles of 4096 halve the counts to scan.
-int sort_steps(int M) { return M > 4096 && M < (1 << 19) ? 4 : 8; }
+constexpr int kSortFull = 1 << 19;
+int sort_steps(int M) { return M > 4096 && M < kSortFull ? 4 : 8; }
+int sort_tiles(int M) {
+  const int tile = kSortThreads * sort_steps(M);
+  return (M + tile - 1) / tile;
+}
 
 // One tile's counts are its totals: they share their place, and no scan runs.
 size_t count_words(int tiles) {
@@ -184,7 +189,7 @@ SortPlan sort_plan(int M, int bits, void* ws) {
   SortPlan p;
   p.M = M;
   p.tile = kSortThreads * sort_steps(M);
-  p.tiles = (M + p.tile - 1) / p.tile;
+  p.tiles = sort_tiles(M);
   p.passes = bits <= 0 ? 1 : (bits + kSortMaxDigitBits - 1) / kSortMaxDigitBits;
   p.dbits = bits <= 0 ? 1 : (bits + p.passes - 1) / p.passes;     // <= kSortMaxDigitBits
   p.a = static_cast<uint2*>(ws);
@@ -197,9 +202,11 @@ SortPlan sort_plan(int M, int bits, void* ws) {
   return p;
 }
 
+// (From kSortFull pairs on the counts are fewer than just below: those below are held, so that a workspace for more
+// pairs does for fewer.)
 size_t sort_workspace_bytes(int M) {
-  const int tile = kSortThreads * sort_steps(M);
-  const size_t words = std::max(count_words((M + tile - 1) / tile), static_cast<size_t>(M));
+  size_t words = std::max(count_words(sort_tiles(M)), static_cast<size_t>(M));
+  if (M >= kSortFull) words = std::max(words, count_words(sort_tiles(kSortFull - 1)));
   return 2 * static_cast<size_t>(M) * sizeof(uint2) + (16 + words) * sizeof(uint32_t);
 }
 

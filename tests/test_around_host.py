@@ -295,6 +295,15 @@ def test_layer_workspaces_never_fall_with_the_tokens(n, dv, dv_virt, d_out):
     never_falls(lambda T: U.umem_workspace_size(d, T))
 
 
+@pytest.mark.parametrize("bag,dv", [(1, 8), (32, 512), (64, 512), (84, 448)])
+def test_backward_workspaces_never_fall_with_the_tokens(bag, dv):
+    """Also past 2^19 entries, from where the sort takes larger tiles."""
+    tokens = range(0, (1 << 20) // bag, max(1, 32 // bag))
+    never_falls(lambda T: U.umem_gather_backward_workspace_size(T, bag, dv), tokens)
+    d = U.umem_desc(2, 256, 64, 2, 16, 16, 1, 0, 64 * 64, 128, 1, 1, 0, 0, 1)
+    never_falls(lambda T: U.umem_score_backward_workspace_size(d, T), range(0, 30000, 5))
+
+
 def test_adapted_query_refusals():
     qd = U.umem_query_desc(64, 3, 2, 32, 0, 1e-5)                        # 2 axes of 2 heads of 32: 128 outputs
     good = dict(xtype=1)
