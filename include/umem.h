@@ -470,7 +470,8 @@ typedef struct umem_adapter_desc {
  * Limits (UMEM_ERR_UNSUPPORTED beyond them): rank, d_in and d_out multiples of 8; rank <= 128; d_in
  * and d_out <= 2^16; T <= 2^20. */
 
-/* Scratch bytes umem_adapter_add needs for T tokens or fewer. */
+/* Scratch bytes umem_adapter_add needs for T tokens or fewer: at most 4 r max(T, 2^17), r the rank rounded up to a
+ * multiple of 16. */
 UMEM_API umem_status umem_adapter_workspace_size(const umem_adapter_desc* ad, int32_t T, size_t* bytes);
 
 /*   x      [T, d_in] of xtype;  ids int32 [T]: each token's adapter, -1 for none

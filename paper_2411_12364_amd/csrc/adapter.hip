@@ -5,10 +5,10 @@
 //   and a range of its outputs, both products in one launch.  Bound by the latency of a chain of loads (id,
 //   A's rows, B's rows); the ranges recompute A x, whose rows come from L2 after the first, so that few
 //   tokens still use many CUs.
-// * low_kernel and out_kernel, many tokens: A x on the matrix cores by tiles of 64 tokens and a piece of
-//   d_in each, its sums over the pieces through the workspace, then B times those by tiles and a range of
-//   outputs.  Bound by HBM (x, base and out once); the adapters come from L2, once for the 16 tokens of a
-//   product that share one.  A launch for both, with all of d_in and A for 16 tokens in one workgroup, waited
+// * low_kernel and out_kernel, many tokens: A x on the matrix cores by tiles of 64 tokens and a run of pieces of
+//   d_in each, its sums over the runs through the workspace, then B times those by tiles and a range of
+//   outputs.  Bound by HBM (x, base and out once, and 8 bytes for each token, rank and run); the adapters come
+//   from L2, once for the 16 tokens of a product that share one.  A launch for both, with all of d_in and A for 16 tokens in one workgroup, waited
 //   for twice as many bytes from L2 in every CU (16 runs, rank 32, 2,048 by 896: 1,024 tokens 20.8 us, now 13.7;
 //   4,096 tokens 22, now 20).
 //
@@ -37,8 +37,8 @@ struct AdapterArgs {
   void* out;
   int T, n, rank, d_in, d_out;
   int splits;                  // workgroups that share a token's (a tile's) outputs
-  float* low;                  // many tokens: [pieces of d_in][T][rank, padded] partial sums of A x
-  int pieces;                  // pieces of d_in
+  float* low;                  // many tokens: [runs of pieces of d_in][T][rank, padded] partial sums of A x
+  int runs;                    // runs of pieces of d_in
 };
 
 __device__ __forceinline__ float lo_of(uint32_t pair) { return __uint_as_float(pair << 16); }
@@ -276,22 +276,28 @@ struct Tile {
 // lane ends up with four consecutive values of one token; columns of tokens with another adapter are
 // computed along and dropped (a token's values reach no other column).
 
-// low[piece][t][:] = A x over the piece's columns.  x of the tile is staged in LDS in bf16 parts; a wave
-// takes (pair, 16 ranks) items, whose weights go from global memory to its registers, the next item's
+// low[run][t][:] = A x over the columns of a run of `walk` pieces.  x of the tile and a piece is staged in LDS in bf16
+// parts; a wave takes (pair, 16 ranks) items, whose weights go from global memory to its registers, the next item's
 // while this one is multiplied.  NB: 16-byte pieces of x that a thread stages.  RT: rank / 16, rounded up.
 // CG: products that share loaded weights; 1 up to rank 32, where a tile of one adapter would leave waves
 // without an item, 2 beyond (rank 64, 2,048 by 2,048: 13.8 us, not 16.5).
+// WALK: more than one piece.  A wave's items are the same in each, so a lane adds to the sums that it wrote itself.
+// (The next piece's x fetched before this one is multiplied: 142 to 174 registers for bf16, one workgroup to a CU, and
+// slower in fp32 as well, 487 us where 481 are; so four waves a SIMD, and the other workgroup's work in between.)
 template <typename XT>
 constexpr int piece_width(int nb) {
   return nb * kThreads / kTile * static_cast<int>(16 / sizeof(XT));
 }
 
-template <typename XT, int NB, int CG>
-__global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs k, int RT) {
+template <typename XT, int NB, int CG, bool WALK>
+__global__ __launch_bounds__(kThreads, WALK ? 4 : 1) void low_kernel(AdapterArgs k, int RT, int walk) {
   constexpr int kParts = sizeof(XT) == 4 ? 3 : 1, kPer = 16 / sizeof(XT), kPiece = piece_width<XT>(NB);
   constexpr int kPitch = kPiece + 8, kPlane = kTile * kPitch, kSteps = kPiece / 32, kPerRow = kPiece / kPer;
   extern __shared__ __align__(16) uint16_t staged[];    // [parts][64][pitch]
-  const int t0 = blockIdx.x * kTile, begin = blockIdx.y * kPiece, width = min(kPiece, k.d_in - begin);
+  const int t0 = blockIdx.x * kTile;
+  int begin = blockIdx.y * (WALK ? walk * kPiece : kPiece), width = min(kPiece, k.d_in - begin);
+  const int end = WALK ? min(begin + walk * kPiece, k.d_in) : 0;
+  bool more = false;                                    // whether sums of the run's earlier pieces are there
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int col = lane & 15, quad = lane >> 4;
   const int tokens = min(kTile, k.T - t0);
@@ -299,22 +305,19 @@ __global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs k, int RT) {
   const __amdgpu_buffer_rsrc_t rx = rsrc(static_cast<const XT*>(k.x) + static_cast<size_t>(t0) * k.d_in, tokens * row);
   Tile<CG> tile;
   tile.fetch(k.ids, t0, k.T);
-  u32x4 v[NB];
-#pragma unroll
-  for (int u = 0; u < NB; ++u) {
-    const int f = threadIdx.x + u * kThreads, r = f / kPerRow, c = f % kPerRow * kPer;
-    v[u] = fetch16(rx, c < width ? static_cast<uint32_t>(r * k.d_in + begin + c) * static_cast<uint32_t>(sizeof(XT)) : kOutside);
-  }
-  tile.find(k.n);
-  if (tile.leads == 0) return;                          // (the same in every wave)
   // an item's weights in one or two halves of 8 steps, or those of two items of two steps: up to 32 registers at
   // a time, so that two workgroups fit a CU
   constexpr int kHalf = kSteps < 8 ? kSteps : 8, kHalves = kSteps / kHalf, kItems = kHalf < 4 ? 2 : 1;
-  const int items = __popcll(tile.leads) * RT;
+  int items = 0;
   struct Half {
     int first[kItems], lead[kItems], rt[kItems];
     u32x4 w[kItems][kHalf];
+    f32x4 sums[WALK ? kItems : 1][CG];
   } even, odd;
+  // this lane's four sums of an item's tokens from `first` on
+  auto sums_at = [&](int first, int rt) {
+    return reinterpret_cast<f32x4*>(k.low + ((static_cast<size_t>(blockIdx.y) * k.T + t0 + first + col) * RT + rt) * 16 + quad * 4);
+  };
   auto item_of = [&](int half, int i) { return wave + (half / kHalves * kItems + i) * kWaves; };
   auto load = [&](Half& n, int half) {                  // (the wave's own count of halves)
     const int from_step = half % kHalves * kHalf;
@@ -334,6 +337,15 @@ __global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs k, int RT) {
 #pragma unroll
       for (int s = 0; s < kHalf; ++s)
         n.w[i][s] = fetch16(ra, s * 32 + at_k < width ? from + static_cast<uint32_t>(s) * 64u : kOutside);
+      if constexpr (WALK) {
+        if (from_step != 0) continue;
+#pragma unroll
+        for (int c = 0; c < CG; ++c) {
+          const int first = n.first[i] + c * kGroup;
+          n.sums[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (more && tile.mine(first, n.lead[i])) n.sums[i][c] = *sums_at(first, n.rt[i]);
+        }
+      }
     }
   };
   f32x4 acc[CG];
@@ -345,7 +357,7 @@ __global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs k, int RT) {
       const uint16_t* xs = staged + (n.first[i] + col) * kPitch + from_step * 32 + quad * 8;
       if (from_step == 0) {
 #pragma unroll
-        for (int c = 0; c < CG; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < CG; ++c) acc[c] = WALK ? n.sums[i][c] : f32x4{0.f, 0.f, 0.f, 0.f};
       }
 #pragma unroll
       for (int s = 0; s < kHalf; ++s)
@@ -360,29 +372,47 @@ __global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs k, int RT) {
 #pragma unroll
       for (int c = 0; c < CG; ++c) {
         const int first = n.first[i] + c * kGroup;
-        if (tile.mine(first, n.lead[i]))
-          *reinterpret_cast<f32x4*>(k.low + ((static_cast<size_t>(blockIdx.y) * k.T + t0 + first + col) * RT + n.rt[i]) * 16 + quad * 4) = acc[c];
+        if (tile.mine(first, n.lead[i])) *sums_at(first, n.rt[i]) = acc[c];
       }
     }
   };
-  load(even, 0);
+  for (;;) {
+    u32x4 v[NB];
 #pragma unroll
-  for (int u = 0; u < NB; ++u) {
-    const int f = threadIdx.x + u * kThreads, r = f / kPerRow, c = f % kPerRow * kPer;
-    if constexpr (kParts == 1) {
-      *reinterpret_cast<u32x4*>(staged + r * kPitch + c) = v[u];
-    } else {
-      const Parts4 s = split4(__builtin_bit_cast(f32x4, v[u]));
-#pragma unroll
-      for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(staged + q * kPlane + r * kPitch + c) = s.p[q];
+    for (int u = 0; u < NB; ++u) {
+      const int f = threadIdx.x + u * kThreads, r = f / kPerRow, c = f % kPerRow * kPer;
+      v[u] = fetch16(rx, c < width ? static_cast<uint32_t>(r * k.d_in + begin + c) * static_cast<uint32_t>(sizeof(XT)) : kOutside);
     }
-  }
-  __syncthreads();
-  for (int half = 0; item_of(half, 0) < items; half += 2) {
-    load(odd, half + 1);
-    finish(even, half);
-    load(even, half + 2);
-    finish(odd, half + 1);
+    if (!more) {
+      tile.find(k.n);
+      if (tile.leads == 0) return;                      // (the same in every wave)
+      items = __popcll(tile.leads) * RT;
+    }
+    load(even, 0);
+    if (more) __syncthreads();                          // no wave reads the last piece any more
+#pragma unroll
+    for (int u = 0; u < NB; ++u) {
+      const int f = threadIdx.x + u * kThreads, r = f / kPerRow, c = f % kPerRow * kPer;
+      if constexpr (kParts == 1) {
+        *reinterpret_cast<u32x4*>(staged + r * kPitch + c) = v[u];
+      } else {
+        const Parts4 s = split4(__builtin_bit_cast(f32x4, v[u]));
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(staged + q * kPlane + r * kPitch + c) = s.p[q];
+      }
+    }
+    __syncthreads();
+    for (int half = 0; item_of(half, 0) < items; half += 2) {
+      load(odd, half + 1);
+      finish(even, half);
+      load(even, half + 2);
+      finish(odd, half + 1);
+    }
+    if constexpr (!WALK) return;
+    begin += kPiece;
+    if (begin >= end) return;
+    width = min(kPiece, k.d_in - begin);
+    more = true;
   }
 }
 
@@ -417,7 +447,7 @@ struct Quad4<__bf16> {
   }
 };
 
-// out = base + B (scale low), a tile of tokens and a range of outputs a workgroup.  The pieces' sums are
+// out = base + B (scale low), a tile of tokens and a range of outputs a workgroup.  The runs' sums are
 // added in order as they are staged.  KT: steps of 32 over the rank.
 //
 // Where at least two tokens share an adapter on average, a wave takes units of a pair and 16 U outputs on the
@@ -496,7 +526,7 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
       const float* p = k.low + (static_cast<size_t>(t0 + tok) * RT * 4 + r4) * 4;
       const size_t stride = static_cast<size_t>(k.T) * RT * 16;
 #pragma unroll 8
-      for (int i = 0; i < k.pieces; ++i) low[u] += *reinterpret_cast<const f32x4*>(p + i * stride);
+      for (int i = 0; i < k.runs; ++i) low[u] += *reinterpret_cast<const f32x4*>(p + i * stride);
     }
   }
   tile.find(k.n);
@@ -621,18 +651,28 @@ bool by_tiles(const umem_adapter_desc& ad, int T) { return static_cast<int64_t>(
 // Pieces of d_in: the widest that make 512 workgroups (two for each CU; 1,024 were no faster), as wider ones
 // leave fewer partial sums.  nb: 16-byte pieces of x to a thread.  8 of bf16 take 66 KiB of LDS, two workgroups
 // to a CU; of fp32 (three parts) 99 KiB, one: 4,096 tokens by 2,048 then take 16.5 us, with 4 13.6.
-constexpr int kLowWorkgroups = 512;
+// Workgroups walk several of the widest pieces, adding up their sums, where that leaves this many: the sums are then
+// of no more tiles than that, or one for each token, whatever d_in is.  A sum for every piece was as many bytes as
+// fp32 x itself at rank 128, and 2 GB of scratch for 8,192 tokens by 65,536 (1,687 us; 67 MB and 1,467 so).  65,536 fp32
+// tokens by 2,048, rank 64: 494 us and 268 MB, 481 and 34 so; with 512 workgroups 500, with 1,024 500, with 4,096
+// 489.  (bf16 x has a quarter of the sums: 32,768 tokens by 8,192, rank 128, 488 us, 479 so; 131,072 by 2,048,
+// rank 64, 419 us, 424 so.)
+constexpr int kLowWorkgroups = 512, kWalkWorkgroups = 2048;
 struct Plan {
-  int nb, piece, pieces, splits, rank_tiles;
+  int nb, piece, pieces, walk, runs, splits, rank_tiles;       // walk: pieces of a run
 };
 Plan plan_of(const umem_adapter_desc& ad, int T) {
   Plan p;
   const int tiles = (T + kTile - 1) / kTile;
-  for (p.nb = ad.xtype == UMEM_F32 ? 4 : 8;; p.nb /= 2) {
+  const int widest = ad.xtype == UMEM_F32 ? 4 : 8;
+  for (p.nb = widest;; p.nb /= 2) {
     p.piece = ad.xtype == UMEM_F32 ? piece_width<float>(p.nb) : piece_width<__bf16>(p.nb);
     p.pieces = (ad.d_in + p.piece - 1) / p.piece;
     if (p.nb == 1 || static_cast<int64_t>(tiles) * p.pieces >= kLowWorkgroups) break;
   }
+  p.runs = p.nb == widest ? std::min(p.pieces, std::max(1, kWalkWorkgroups / tiles)) : p.pieces;
+  p.walk = (p.pieces + p.runs - 1) / p.runs;
+  p.runs = (p.pieces + p.walk - 1) / p.walk;
   p.splits = std::max(1, std::min(512 / tiles, (ad.d_out + 127) / 128));
   p.rank_tiles = (ad.rank + 15) / 16;
   return p;
@@ -642,12 +682,13 @@ Plan plan_of(const umem_adapter_desc& ad, int T) {
 
 // The most that T tokens or fewer take: fewer tiles have narrower pieces, which leave more sums of a token (bf16 x of
 // 4,096, rank 32: 4,032 tokens 8.3 MB, 4,096 4.2).  So every width that T tokens or fewer take is looked at, at the
-// most tokens that take it.
+// most tokens that take it; runs of pieces have at most kWalkWorkgroups tiles of sums, or one for each token.
 size_t adapter_workspace_bytes(const umem_adapter_desc& ad, int T) {
   size_t most = 0;
   while (T > 0 && by_tiles(ad, T)) {
     const Plan p = plan_of(ad, T);
-    most = std::max(most, (static_cast<size_t>(p.pieces) * T * p.rank_tiles * 16 * sizeof(float) + 255) / 256 * 256);
+    const size_t sums = std::min(static_cast<size_t>(p.pieces) * T, std::max<size_t>(kWalkWorkgroups * kTile, T));
+    most = std::max(most, (sums * p.rank_tiles * 16 * sizeof(float) + 255) / 256 * 256);
     if (p.nb == 1) break;
     T = ((kLowWorkgroups + p.pieces - 1) / p.pieces - 1) * kTile;
   }
@@ -682,19 +723,22 @@ hipError_t launch_adapter_add(const umem_adapter_desc& ad, int T, const void* x,
   const int tiles = (T + kTile - 1) / kTile;
   k.splits = p.splits;
   k.low = static_cast<float*>(ws);
-  k.pieces = p.pieces;
-  const dim3 grid(tiles, p.pieces), block(kThreads);
+  k.runs = p.runs;
+  const dim3 grid(tiles, p.runs), block(kThreads);
   const size_t lds = static_cast<size_t>(kTile) * (p.piece + 8) * 2 * (ad.xtype == UMEM_F32 ? 3 : 1);
-#define UMEM_LOW(XT, NB, CG) hipLaunchKernelGGL((low_kernel<XT, NB, CG>), grid, block, lds, s, k, p.rank_tiles)
-#define UMEM_LOW_RANK(XT, NB)                \
-  if (ad.rank <= 32) UMEM_LOW(XT, NB, 1);    \
-  else UMEM_LOW(XT, NB, 2);
-#define UMEM_ADAPTER(XT)                         \
-  if (p.nb == 4) { UMEM_LOW_RANK(XT, 4) }        \
-  else if (p.nb == 2) { UMEM_LOW_RANK(XT, 2) }   \
-  else { UMEM_LOW_RANK(XT, 1) }
-  if (ad.xtype == UMEM_F32) { UMEM_ADAPTER(float) }
-  else if (p.nb == 8) { UMEM_LOW_RANK(__bf16, 8) }
+#define UMEM_LOW(XT, NB, CG, WALK) \
+  hipLaunchKernelGGL((low_kernel<XT, NB, CG, WALK>), grid, block, lds, s, k, p.rank_tiles, p.walk)
+#define UMEM_LOW_RANK(XT, NB, WALK)                \
+  if (ad.rank <= 32) UMEM_LOW(XT, NB, 1, WALK);    \
+  else UMEM_LOW(XT, NB, 2, WALK);
+#define UMEM_ADAPTER(XT)                                \
+  if (p.nb == 4) { UMEM_LOW_RANK(XT, 4, false) }        \
+  else if (p.nb == 2) { UMEM_LOW_RANK(XT, 2, false) }   \
+  else { UMEM_LOW_RANK(XT, 1, false) }
+  if (ad.xtype == UMEM_F32 && p.walk > 1) { UMEM_LOW_RANK(float, 4, true) }
+  else if (ad.xtype == UMEM_F32) { UMEM_ADAPTER(float) }
+  else if (p.walk > 1) { UMEM_LOW_RANK(__bf16, 8, true) }
+  else if (p.nb == 8) { UMEM_LOW_RANK(__bf16, 8, false) }
   else { UMEM_ADAPTER(__bf16) }
 #undef UMEM_ADAPTER
 #undef UMEM_LOW_RANK

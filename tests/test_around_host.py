@@ -221,6 +221,15 @@ def test_adapter_workspace_never_falls_with_the_tokens(kw):
     assert all(a[1] <= b[1] for a, b in zip(sizes, sizes[1:]))
 
 
+def test_adapter_workspace_does_not_grow_with_the_input_width():
+    for kw in (dict(rank=128), dict(rank=8), dict(rank=72, xtype=1), dict(rank=16, xtype=1)):
+        r = (kw["rank"] + 15) // 16 * 16
+        for d_in in (64, 2048, 4096 + 72, 1 << 16):
+            for T in (*range(300, 20000, 119), 1 << 16, (1 << 17) + 1, 1 << 20):
+                st, n = U.umem_adapter_workspace_size(ad(d_in=d_in, **kw), T)
+                assert st == OK and n <= 4 * r * max(T, 1 << 17) + 256, (kw, d_in, T)
+
+
 def test_adapter_refusals():
     names = ["x", "ids", "a", "b", "scale", "base", "out"]
     base = {k: at(i) for i, k in enumerate(names)}

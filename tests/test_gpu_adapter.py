@@ -230,6 +230,45 @@ def test_the_workspace_of_more_tokens(T, longest, rank, d_in, x):
     assert torch.equal(out, want)
 
 
+# tokens, adapters, rank, d_in, d_out: wide enough that a workgroup sums over several pieces of d_in, the last run
+# and the last piece shorter
+WIDE = [((4100, 5, 128, 8264, 72), "f32", "runs"), ((4100, 300, 24, 8264, 72), "f32", "random"),
+        ((1300, 3, 32, 12616, 264), "f32", "one"), ((1300, 9, 40, 50248, 64), "bf16", "random"),
+        ((4100, 6, 16, 16392, 136), "bf16", "runs"), ((4100, 7, 72, 16392, 64), "bf16", "one")]
+
+
+@pytest.mark.parametrize("size,x,kind", WIDE, ids=["x".join(map(str, s)) for s, _, _ in WIDE])
+def test_wide_inputs(size, x, kind):
+    print(f"[case] wide adapters {size} {x} {kind}", flush=True)
+    s = make(*size, 80, x, "f32")
+    ids = ids_of(kind, size[0], size[1], s["g"])
+    out = call(s, ids)
+    check(s, ids, out)
+    assert torch.equal(call(s, ids, torch.empty_like(out)), out)
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_wide_inputs_of_few_adapted_tokens(x):
+    """Whole tiles without an adapter, and NaN and infinities among the others."""
+    T, d_in = 4100, 8264 if x == "f32" else 16392
+    s = make(T, 3, 24, d_in, 72, 81, x)
+    ids = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    at = [5, 70, 71, 2000, T - 1]
+    ids[at] = torch.tensor([2, 0, 1, 1, 0], dtype=torch.int32, device="cuda")
+    few = torch.tensor(at, device="cuda")
+    s["x"][6], s["x"][72], s["x"][T - 2] = float("nan"), float("inf"), float("nan")
+    out = call(s, ids)
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[few] = False
+    assert torch.equal(out[rest], s["base"][rest])
+    check({**s, "x": s["x"][few], "base": s["base"][few]}, ids[few], out[few])
+    s["a"], s["b"] = s["a"].abs() + 0.25, s["b"].abs() + 0.25
+    s["x"][70, d_in - 1], s["x"][2000, 0] = float("inf"), float("nan")
+    out = call(s, ids)
+    assert (out[70] == float("inf")).all() and torch.isnan(out[2000]).all()
+    assert torch.isfinite(out[[5, 71, T - 1]]).all()
+
+
 def test_offsets_past_32_bits():
     """2^20 tokens of 2056: out has 2.16e9 elements."""
     T, d_out = 1 << 20, 2056
