@@ -616,6 +616,7 @@ UMEM_API umem_status umem_block_in_backward(const umem_block_desc* bd, int32_t T
   const Span in[] = {{h, z.h}, {dres, z.h}, {dn, z.y}, {gamma, z.row},
                      {ws, block_backward_workspace_bytes(*bd, T)}};
   const Span dx{dh, z.h}, dg{dgamma, z.row}, db{dbeta, z.row};
+  if (!out_fits(in[4], in, 4)) return UMEM_ERR_INVALID_ARG;          // the scratch is written while they are read
   if ((!out_fits(dx, in, 5, 0) && !out_fits(dx, in, 5, 1)) || !out_fits(dg, in, 5) || !out_fits(db, in, 5) ||
       !apart(dx, dg) || !apart(dx, db) || !apart(dg, db))
     return UMEM_ERR_INVALID_ARG;
@@ -648,6 +649,7 @@ UMEM_API umem_status umem_block_out_backward(const umem_block_desc* bd, int32_t 
                      {gamma, z.row}, {beta, z.row}, {ws, block_backward_workspace_bytes(*bd, T)}};
   const Span out[] = {{dy, z.y}, {dh, z.h}, {dgate, z.gate}, {dgamma, z.row}, {dbeta, z.row}};
   const int same[] = {0, 1, bd->gate == UMEM_GATE_FULL ? 2 : -1, -1, -1};
+  if (!out_fits(in[5], in, 5)) return UMEM_ERR_INVALID_ARG;
   for (int i = 0; i < 5; ++i)
     if (!out_fits(out[i], in, 6, same[i]) || !out_fits(out[i], out, i)) return UMEM_ERR_INVALID_ARG;
   return hip_status(launch_block_out_backward(*bd, T, y, gate, gamma, beta, dh_out, dh, dy, dgate, dgamma, dbeta,

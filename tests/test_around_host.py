@@ -118,6 +118,22 @@ def test_block_workspace_never_falls_with_the_tokens(d):
     assert sizes[-1] <= 512 * 3 * 4 * d + 256                            # whatever the batch
 
 
+def test_block_backward_scratch_is_apart_from_the_inputs():
+    """The scratch is written while other workgroups read."""
+    desc = bd(gate=1)
+    need = U.umem_block_backward_workspace_size(desc, 8)[1]
+    names = ["h", "gamma", "dn", "dres", "dh", "dgamma", "dbeta"]
+    base = {k: at(i) for i, k in enumerate(names)}
+    for k in ("h", "gamma", "dn", "dres"):
+        for ws in (base[k], base[k] + 16, base[k] - need + 16):
+            assert U.umem_block_in_backward(bd(), 8, *base.values(), 0, ws, need, 0) == ARG, k
+    names = ["y", "gate", "gamma", "beta", "dh_out", "dh", "dy", "dgate", "dgamma", "dbeta"]
+    base = {k: at(i) for i, k in enumerate(names)}
+    for k in ("y", "gate", "gamma", "beta", "dh_out"):
+        for ws in (base[k], base[k] + 16, base[k] - need + 16):
+            assert U.umem_block_out_backward(desc, 8, *base.values(), 0, ws, need, 0) == ARG, k
+
+
 def grads(*rows):
     return (U.umem_grad * len(rows))(*[U.umem_grad(*r) for r in rows])
 
