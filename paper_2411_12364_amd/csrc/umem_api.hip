@@ -790,7 +790,7 @@ UMEM_API umem_status umem_adapter_add(const umem_adapter_desc* ad, int32_t T, co
                      {ids, t * 4},             {a, n * r * ad->d_in * 2},
                      {b, n * ad->d_out * r * 2}, {scale, n * 4},
                      {ws, need}};
-  if (!out_fits(y, in, 7, 0)) return UMEM_ERR_INVALID_ARG;
+  if (!out_fits(y, in, 7, 0) || !out_fits(in[6], in, 6)) return UMEM_ERR_INVALID_ARG;
   return hip_status(launch_adapter_add(*ad, T, x, ids, a, b, scale, base, out, ws, stream));
 }
 

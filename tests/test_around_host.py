@@ -271,6 +271,18 @@ def test_adapter_refusals():
             assert U.umem_adapter_add(*args, at(20) + 16, need, 0) == WS
 
 
+def test_adapter_scratch_is_apart_from_the_inputs():
+    """Tiles write it while others read; calls that need none take whatever they are given."""
+    desc = ad(rank=16, d_in=64)
+    need = U.umem_adapter_workspace_size(desc, 5000)[1]
+    assert need > 0 and U.umem_adapter_workspace_size(desc, 8)[1] == 0
+    names = ["x", "ids", "a", "b", "scale", "base", "out"]
+    base = {k: at(i) for i, k in enumerate(names)}
+    for k in names:
+        for ws in (base[k], base[k] + 256 if k in ("x", "ids", "base", "out") else base[k], base[k] - need // 256 * 256 + 256):
+            assert U.umem_adapter_add(desc, 5000, *base.values(), ws, need, 0) == ARG, k
+
+
 def test_tensors_of_another_device_are_refused(monkeypatch):
     """Without a stream the current device's is taken: a tensor that lives elsewhere is an error, not a launch."""
     class Elsewhere:
