@@ -444,7 +444,8 @@ UMEM_API umem_status umem_grad_workspace_size(int32_t n, const umem_grad* grads,
  *          sharded model before the square root
  *   ws     16-byte aligned scratch of umem_grad_workspace_size bytes
  * Squares and sums are fp64 (a square neither overflows nor vanishes), added in an order that the sizes
- * alone fix.  NaN and infinities go through to the norm.  n == 0 gives a norm of 0. */
+ * alone fix.  NaN and infinities go through to the norm.  n == 0 gives a norm of 0.  norm, sumsq and ws overlap
+ * neither a gradient, a row count nor each other (UMEM_ERR_INVALID_ARG). */
 UMEM_API umem_status umem_grad_norm(int32_t n, const umem_grad* grads, float* norm, double* sumsq, void* ws,
                            size_t ws_bytes, hipStream_t stream);
 

@@ -680,6 +680,21 @@ umem_status check_grads(int32_t n, const umem_grad* grads, bool for_clip) {
   return UMEM_OK;
 }
 
+// Whether what the norm writes (itself, the sum of squares, the scratch) overlaps a gradient, a row count or each other.
+bool norm_clashes(int32_t n, const umem_grad* grads, const Span& norm, const Span& sumsq, const Span& ws) {
+  const Span out[] = {norm, sumsq, ws};
+  if (!apart(norm, sumsq) || !apart(norm, ws) || !apart(sumsq, ws)) return true;
+  for (int i = 0; i < n; ++i) {
+    const umem_grad& g = grads[i];
+    const Span in{g.grad, static_cast<size_t>(g.rows) * g.row_len * esize(static_cast<int32_t>(g.dtype))};
+    if (in.bytes == 0) continue;
+    const Span rows{g.n_rows, sizeof(int32_t)};
+    for (const Span& o : out)
+      if (!apart(o, in) || !apart(o, rows)) return true;
+  }
+  return false;
+}
+
 // Whether an out overlaps another gradient or out, its own gradient other than being it, or what the kernels
 // read beside them: the norm and the row counts.
 bool grads_clash(int32_t n, const umem_grad* grads, const float* norm) {
@@ -730,9 +745,9 @@ UMEM_API umem_status umem_grad_norm(int32_t n, const umem_grad* grads, float* no
                                     size_t ws_bytes, hipStream_t stream) {
   const umem_status st = check_grads(n, grads, false);
   if (st != UMEM_OK) return st;
-  if (norm == nullptr || !aligned(norm, 4) || !aligned(sumsq, 8) || !apart({norm, sizeof(float)}, {sumsq, sizeof(double)}))
-    return UMEM_ERR_INVALID_ARG;
+  if (norm == nullptr || !aligned(norm, 4) || !aligned(sumsq, 8)) return UMEM_ERR_INVALID_ARG;
   const size_t need = grad_workspace_bytes(n, grads);
+  if (norm_clashes(n, grads, {norm, sizeof(float)}, {sumsq, sizeof(double)}, {ws, need})) return UMEM_ERR_INVALID_ARG;
   if (need > 0 && (ws == nullptr || !aligned(ws, 16) || ws_bytes < need)) return UMEM_ERR_WORKSPACE;
   return hip_status(launch_grad_norm(n, grads, norm, sumsq, ws, stream));
 }

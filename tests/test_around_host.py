@@ -193,6 +193,20 @@ def test_a_clipped_gradient_is_apart_from_the_norm_and_the_row_counts():
     assert U.umem_grad_clip(1, grads((at(0), at(1), at(2), 0, 1024, 0)), 1.0, at(9), 0) == OK
 
 
+def test_the_norm_is_apart_from_the_gradients_and_its_scratch():
+    """What umem_grad_norm writes, against what it reads and against each other."""
+    tab = grads((at(0), at(1), at(2), 4, 1024, 0), (at(3), at(4), None, 40, 1024, 1))
+    st, need = U.umem_grad_workspace_size(2, tab)
+    assert st == OK and need > 0
+    call = lambda norm=at(9), sumsq=at(10), ws=at(11): U.umem_grad_norm(2, tab, norm, sumsq, ws, need, 0)   # noqa: E731
+    last = at(3) + 2 * 40 * 1024
+    for a in (at(0), at(0) + 4 * 4 * 1024 - 8, at(3) + 8, last - 8, at(2)):
+        assert call(norm=a) == ARG and call(sumsq=a // 8 * 8) == ARG
+    for a in (at(0), at(0) - need + 16, at(2) - 16, last - 16, at(9) - 16, at(10), at(9) // 16 * 16):
+        assert call(ws=a) == ARG, a
+    assert call(norm=at(10) + 4) == ARG and call(norm=at(11) + 8) == ARG and call(sumsq=at(11) + need - 8) == ARG
+
+
 def test_grad_tables_of_the_binding():
     rows = [(at(0), at(1), 0, 4, 100, 0), (at(2), at(2), at(3), 7, 33, 1)]
     table = np.array(rows, dtype=np.int64)
