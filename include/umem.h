@@ -495,7 +495,8 @@ UMEM_API umem_status umem_adapter_add(const umem_adapter_desc* ad, int32_t T, co
  * y the convolved rows as the linear takes them (rounded to bf16, nearest even).
  *   ad   n and rank; d_in = d_model, d_out = A * heads * dk (row queries, then column queries), xtype
  *        UMEM_BF16, otype UMEM_F32 (UMEM_ERR_INVALID_ARG otherwise)
- *   ids, a, b, scale  as for umem_adapter_add; everything else as for umem_query
+ *   ids, a, b, scale  as for umem_adapter_add; everything else as for umem_query.  q_row, q_col and ws
+ *        overlap neither an input nor each other (UMEM_ERR_INVALID_ARG)
  *   ws   16-byte aligned scratch of umem_query_adapted_workspace_size(...) bytes */
 UMEM_API umem_status umem_query_adapted_workspace_size(const umem_query_desc* qd, const umem_adapter_desc* ad,
                                               int32_t B, int32_t L, size_t* bytes);

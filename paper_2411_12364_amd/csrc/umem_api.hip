@@ -854,8 +854,16 @@ UMEM_API umem_status umem_query_adapted(const umem_query_desc* qd, const umem_ad
   if (!ids || !a || !b || !aligned(ids, 4) || !aligned(a, 16) || !aligned(b, 16) || !aligned(scale, 4))
     return UMEM_ERR_INVALID_ARG;
   const size_t own = round_up(query_workspace_bytes(*qd, T));
-  if (ws == nullptr || !aligned(ws, 16) || ws_bytes < own + adapter_workspace_bytes(*ad, static_cast<int>(T)))
-    return UMEM_ERR_WORKSPACE;
+  const size_t need = own + adapter_workspace_bytes(*ad, static_cast<int>(T));
+  if (ws == nullptr || !aligned(ws, 16) || ws_bytes < need) return UMEM_ERR_WORKSPACE;
+  const size_t t = T, d = qd->d_model, nq = ad->d_out, half = t * qd->heads * qd->dk * 4, na = ad->n, r = ad->rank;
+  const Span in[] = {{x, t * d * 4},   {x_hist, static_cast<size_t>(B) * (qd->conv_k - 1) * d * 4},
+                     {conv_w, qd->conv_k * d * 4}, {w_q, nq * d * 2}, {ids, t * 4},
+                     {a, na * r * d * 2}, {b, na * nq * r * 2}, {scale, na * 4},
+                     {gamma, nq * 4},  {beta, nq * 4}};
+  const Span out[] = {{q_row, half}, {q_col, half}, {ws, need}};
+  for (int i = 0; i < 3; ++i)
+    if (!out_fits(out[i], in, 10) || !out_fits(out[i], out, i)) return UMEM_ERR_INVALID_ARG;
   const QueryAdapters adapters{*ad, ids, a, b, scale, static_cast<char*>(ws) + own};
   return hip_status(launch_query(*qd, B, L, x, x_hist, conv_w, w_q, gamma, beta, q_row, q_col, ws, &adapters, stream));
 }

@@ -378,3 +378,26 @@ def test_adapted_query_refusals():
         assert call(**{k: base[k] + 2}) == ARG, k
     assert call(ws=None) == WS and call(ws=at(20) + 8) == WS and call(n=need - 1) == WS
     assert call(B=0, x=None) == OK and call(B=-1) == ARG
+
+
+def test_adapted_query_outputs_are_apart():
+    """The queries and the scratch, from what is read and from each other."""
+    qd = U.umem_query_desc(64, 3, 2, 32, 0, 1e-5)
+    desc = ad(xtype=1)
+    need = U.umem_query_adapted_workspace_size(qd, desc, 4, 5)[1]
+    names = ["x", "hist", "conv", "wq", "ids", "a", "b", "scale", "gamma", "beta", "q_row", "q_col"]
+    base = {k: at(i) for i, k in enumerate(names)}
+    sizes = dict(x=4 * 5 * 64 * 4, hist=4 * 2 * 64 * 4, conv=3 * 64 * 4, wq=128 * 64 * 2, ids=20 * 4, a=4 * 16 * 64 * 2, b=4 * 128 * 16 * 2,
+                 scale=16, gamma=512, beta=512, q_row=20 * 64 * 4, q_col=20 * 64 * 4)
+
+    def call(ws=at(20), **kw):
+        return U.umem_query_adapted(qd, desc, 4, 5, *{**base, **kw}.values(), ws, need, 0)
+
+    for k in names:
+        for out in ("q_row", "q_col"):
+            if out == k:
+                continue
+            for a in (base[k], base[k] + sizes[k] - 4, base[k] - sizes[out] + 4):
+                assert call(**{out: a}) == ARG, (k, out)
+        for a in (base[k], base[k] + sizes[k] - 16, base[k] - need + 16):
+            assert call(ws=a) == ARG, k
