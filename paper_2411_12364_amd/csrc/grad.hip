@@ -38,7 +38,7 @@ struct Tensor {
 };
 struct Counted {
   const int32_t* n_rows;
-  int64_t row_len;
+  int64_t rows, row_len;
 };
 struct Table {
   Tensor t[kTable];
@@ -68,7 +68,8 @@ __device__ __forceinline__ Piece piece_of(const Table& tab, const Tensor& t, int
   int64_t count = t.count & ~kBf16;
   if (t.counted >= 0) {
     const Counted& c = tab.c[t.counted];
-    count = min(count, static_cast<int64_t>(max(*c.n_rows, 0)) * c.row_len);
+    // (limited before the product, which may not fit 64 bits for a count past the rows there are)
+    count = min(static_cast<int64_t>(max(*c.n_rows, 0)), c.rows) * c.row_len;
   }
   p.end = count + p.shift;
   p.u0 = static_cast<int64_t>(b - t.first) * size;
@@ -262,12 +263,12 @@ int fill_table(const umem_grad* grads, int n, int64_t size, bool back, int* i, T
     tab->t[j] = {g.grad, g.out, g.rows * g.row_len | (g.dtype == UMEM_BF16 ? kBf16 : 0), pieces, -1};
     if (g.n_rows != nullptr) {
       tab->t[j].counted = c;
-      tab->c[c++] = {g.n_rows, g.row_len};
+      tab->c[c++] = {g.n_rows, g.rows, g.row_len};
     }
     pieces += static_cast<int>(pieces_of(g, size));
   }
   for (int j = used; j < kTable; ++j) tab->t[j] = {nullptr, nullptr, 0, INT32_MAX, -1};
-  for (; c < kCounted; ++c) tab->c[c] = {nullptr, 0};
+  for (; c < kCounted; ++c) tab->c[c] = {nullptr, 0, 0};
   return pieces;
 }
 

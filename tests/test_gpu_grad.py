@@ -177,6 +177,19 @@ def test_a_tensor_past_32_bits():
     assert float(g[-1]) == 2048.0 and float(g[1 << 31]) == 1024.0 and bool((g[:1 << 31] == 0.25).all())
 
 
+def test_a_row_count_past_the_rows_of_long_rows():
+    """2^31 - 1 rows counted, of 2^32 + 8 elements each: their product is past 63 bits, and the one row there is counts."""
+    n = (1 << 32) + 8
+    g = torch.empty((1, n), dtype=torch.bfloat16, device="cuda").zero_()
+    g[0, 0], g[0, 1 << 32], g[0, n - 1] = 3.0, 12.0, 4.0
+    many = torch.tensor([2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    tab = table([g], [g], {0: many})
+    norm = norm_of(tab)
+    assert float(norm) == 13.0
+    U.check(U.umem_grad_clip(1, tab, 6.5, norm))
+    assert [float(g[0, i]) for i in (0, 1, 1 << 32, n - 1)] == [1.5, 0.0, 6.0, 2.0]
+
+
 def test_twice_the_same_and_captured():
     """The same bits from every run; a captured norm and clip replayed on new gradients and row counts."""
     grads = make([(500, 512), (4097,), (33,)], 5, {1})
