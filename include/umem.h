@@ -482,8 +482,8 @@ UMEM_API umem_status umem_adapter_workspace_size(const umem_adapter_desc* ad, in
  *   ws     256-byte aligned scratch of umem_adapter_workspace_size bytes (NULL if 0)
  * x, a, b, base and out are 16-byte aligned (UMEM_ERR_INVALID_ARG otherwise).  fp32 x and A_i x are not
  * rounded: they enter the matrix cores as sums of bf16 parts; accumulation is fp32 and a bf16 out is
- * rounded once.  NaN and infinities of x stay with their token; an infinite weight may give NaN where it is
- * multiplied by a finite value.  The result does not depend on timing. */
+ * rounded once.  NaN and infinities of x stay with their token; infinite sums and products are what
+ * the formula's are.  The result does not depend on timing. */
 UMEM_API umem_status umem_adapter_add(const umem_adapter_desc* ad, int32_t T, const void* x, const int32_t* ids,
                              const uint16_t* a, const uint16_t* b, const float* scale,
                              const void* base, void* out, void* ws, size_t ws_bytes,

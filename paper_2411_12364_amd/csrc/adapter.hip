@@ -211,6 +211,12 @@ __device__ __forceinline__ Parts4 split4(f32x4 x) {
   return r;
 }
 
+// An infinite weight meets the zeros among the parts of an ordinary value: a sum that comes out NaN is taken again
+// from the values themselves, so that it is what the formula gives, however many tokens there are.
+__device__ __forceinline__ bool any_nan(f32x4 x) {
+  return x.x != x.x || x.y != x.y || x.z != x.z || x.w != x.w;
+}
+
 // Buffer resource of a raw byte range: loads past it give zeros, stores past it are dropped, so the edges
 // (tokens past T, ranks past the rank, columns past a width) need no branches around loads and stores.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p, size_t bytes) {
@@ -372,7 +378,21 @@ __global__ __launch_bounds__(kThreads, WALK ? 4 : 1) void low_kernel(AdapterArgs
 #pragma unroll
       for (int c = 0; c < CG; ++c) {
         const int first = n.first[i] + c * kGroup;
-        if (tile.mine(first, n.lead[i])) *sums_at(first, n.rt[i]) = acc[c];
+        if (!tile.mine(first, n.lead[i])) continue;
+        if (kParts > 1 && any_nan(acc[c])) {
+          const int r0 = n.rt[i] * 16 + quad * 4;       // (of padded ranks nothing is read)
+          f32x4 s = WALK ? n.sums[i][c] : f32x4{0.f, 0.f, 0.f, 0.f};
+          if (r0 < k.rank) {
+            const XT* x = static_cast<const XT*>(k.x) + static_cast<size_t>(t0 + first + col) * k.d_in + begin;
+            const uint16_t* a = k.a + (static_cast<size_t>(n.lead[i]) * k.rank + r0) * k.d_in + begin;
+#pragma unroll 1
+            for (int j = 0; j < width; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) s[r] = fmaf(lo_of(a[static_cast<size_t>(r) * k.d_in + j]), static_cast<float>(x[j]), s[r]);
+          }
+          acc[c] = s;
+        }
+        *sums_at(first, n.rt[i]) = acc[c];
       }
     }
   };
@@ -627,7 +647,19 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
 #pragma unroll
           for (int q = 2; q >= 0; --q)
             d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, n.w[u][s]), v[s][q], d, 0, 0, 0);
-        n.from[u][c].add_store(rout, offset(n, u, c), d);
+        const uint32_t at = offset(n, u, c);
+        if (at != kOutside && any_nan(d)) {
+          const uint16_t* v = staged + (n.first + c * kGroup + col) * kPitch;
+          const uint16_t* b = k.b + (static_cast<size_t>(n.lead) * k.d_out + (n.o + u) * 16 + quad * 4) * k.rank;
+          d = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+          for (int j = 0; j < k.rank; ++j) {
+            const float x = lo_of(v[j]) + (lo_of(v[kPlane + j]) + lo_of(v[2 * kPlane + j]));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) d[r] = fmaf(lo_of(b[r * k.rank + j]), x, d[r]);
+          }
+        }
+        n.from[u][c].add_store(rout, at, d);
       }
     }
   };

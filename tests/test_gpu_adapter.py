@@ -199,6 +199,29 @@ def test_an_infinite_input_gives_infinities(T, n, rank):
     assert torch.equal(out[rest], clean[rest])
 
 
+@pytest.mark.parametrize("T,n", [(7, 3), (6000, 3), (6000, 4000)])
+@pytest.mark.parametrize("rank,x", [(8, "f32"), (24, "bf16"), (40, "f32"), (128, "f32"), (64, "bf16")])
+def test_infinite_weights_give_what_the_formula_gives(T, n, rank, x):
+    """Whatever the number of tokens: infinities of A, of B and of both, zeros of x among what they meet."""
+    s = make(T, n, rank, 136, 72, 21, x)
+    s["x"][::5, 17] = 0.0
+    s["a"][0, 3, 17], s["a"][1, rank - 1, 135] = float("inf"), -float("inf")
+    s["b"][1, 5, 2], s["b"][1, 71, rank - 1], s["b"][2, 9, 0], s["b"][2, 9, 1] = float("inf"), float("inf"), -float("inf"), float("inf")
+    ids = ids_of("random", T, n, s["g"])
+    ids[1], ids[4], ids[5], ids[6] = 0, 1, 0, 2
+    out = host(call(s, ids))
+    v = {k: host(s[k]) for k in ("x", "a", "b", "scale", "base")}
+    i = ids.cpu().numpy()
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = B.adapter_add(v["x"], i, v["a"], v["b"], v["scale"], v["base"])
+    assert np.isposinf(want).any() and np.isneginf(want).any() and np.isnan(want).any() and np.isfinite(want).any()
+    assert (np.isnan(out) == np.isnan(want)).all()
+    assert (np.isposinf(out) == np.isposinf(want)).all() and (np.isneginf(out) == np.isneginf(want)).all()
+    fine = (i != 0) & (i != 1) & (i != 2)
+    few = torch.from_numpy(fine).cuda()
+    check({**s, "x": s["x"][few], "base": s["base"][few]}, ids[few], torch.from_numpy(out).cuda()[few])
+
+
 @pytest.mark.parametrize("o", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [5, 2800])
 def test_base_of_negative_zeros(T, o):
