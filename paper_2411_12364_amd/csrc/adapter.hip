@@ -674,7 +674,7 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
 // Tiles of 64 from this many ranks of tokens on (2,560 tokens of rank 16, 640 of rank 64).  A workgroup a token
 // does its own A x whoever shares the adapter, a tile shares it, but only among tokens that lie together, and
 // has few workgroups.  In us, a workgroup a token and tiles, for 8 adapters in runs, 64 in runs, 64 in random
-// order (which only the device knows): rank 16, 1,024 by 2,048: 2,048 tokens 20, 21, 25 and 16, 16, 30; 4,096
+// order (only the device knows it; what n alone says of the sharing is not used): rank 16, 1,024 by 2,048: 2,048 tokens 20, 21, 25 and 16, 16, 30; 4,096
 // 36, 36, 44 and 20, 21, 48.  Rank 32, 2,048 by 896: 1,024 tokens 16, 20, 24 and 14, 15, 40; 2,048 28, 27, 43
 // and 15, 17, 53.  Rank 64, 2,048 by 2,048: 512 tokens 19, 36, 33 and 16, 25, 57; 1,024 34, 44, 63 and 19, 25, 79.
 constexpr int kTileFrom = 40960;

@@ -35,7 +35,7 @@ struct ExitBackArgs {
 
 // A group's column sums: in registers, or, of the widest rows, whose threads have none left, each thread's own
 // in LDS (no thread reads another's, so nothing waits): 1,024 fp32 rows of 12,288 leave the exit's backward in
-// 113 us, in registers that spill 172, the entry's in 47 and 67.
+// 112 us, with the sums in registers, of which more are spilled then, 172, the entry's in 46 and 67.
 template <int G, int PER>
 struct ColumnSums {
   static constexpr bool kLds = kWide<G, PER>;
@@ -300,8 +300,9 @@ __global__ __launch_bounds__(kColWide * kColDeep) void column_sum_kernel(ColumnA
 // rows are as many bytes (exit's backward of 2,048 bf16 rows of 4,096 31.5 us, with two 34, of 300 rows 13 and
 // 16; 8,192 bf16 rows of 2,048 take 49 with two workgroups of 256 threads, 59 with one).
 int most_parts(const RowShape& s) { return s.group >= 512 ? 256 : 512; }
-// Rows of 4,097 to 8,192 (row_shape), 512 threads a row: the exit's backward of 2,048 fp32 rows of 5,000 87 us, with 1,024
-// threads 117; bf16 50 and 67.
+// Rows of 4,097 to 8,192 (row_shape), 512 threads a row: the exit's backward of 2,048 fp32 rows of 5,000 79 us, with 1,024
+// threads 112; bf16 43 and 62.  Both spill: 2 to 98 registers
+// in nine of twelve instances, with 1,024 threads 23 to 112 in all.
 constexpr int kFours8K = 4;
 
 hipError_t launch_columns(const ColumnArgs& c, hipStream_t s) {

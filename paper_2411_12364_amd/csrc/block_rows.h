@@ -48,8 +48,10 @@ struct Row {
 enum RowEnd { kFull, kFours, kAny };
 
 // Rows past 8,192, 16 elements to each of 1,024 threads with 128 registers: a group's parameters are read again
-// for each row, and few or none of the next row's loads are in flight, or registers are spilled (1,024 rows of
-// 12,288 left the block in 194 us, 86 so, in bf16 135 and 51).
+// for each row, and few or none of the next row's loads are in flight, or more registers are spilled (1,024 rows of
+// 12,288 left the block in 194 us, 89 so, in bf16 135 and 51).  Not all spills are gone: the exit has 6 to 30 of them,
+// its backward 42 to 62, entry's backward 0 to 8, and at widths that end within a four 54 to 78, 185 to 220 and up to 99:
+// 1,024 fp32 rows of 12,289 leave the block in 154 us (bf16 121), their backward takes 221 (185), entry's 127 (109).
 template <int G, int PER>
 constexpr bool kWide = G == 1024 && PER == 4;
 
