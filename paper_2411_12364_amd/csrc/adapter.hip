@@ -212,9 +212,13 @@ __device__ __forceinline__ Parts4 split4(f32x4 x) {
 }
 
 // An infinite weight meets the zeros among the parts of an ordinary value: a sum that comes out NaN is taken again
-// from the values themselves, so that it is what the formula gives, however many tokens there are.
+// from the values themselves, so that it is what the formula gives, however many tokens there are.  (Until all four
+// sums of a lane are NaN, so a NaN among the values ends it.)
 __device__ __forceinline__ bool any_nan(f32x4 x) {
   return x.x != x.x || x.y != x.y || x.z != x.z || x.w != x.w;
+}
+__device__ __forceinline__ bool all_nan(f32x4 x) {
+  return x.x != x.x && x.y != x.y && x.z != x.z && x.w != x.w;
 }
 
 // Buffer resource of a raw byte range: loads past it give zeros, stores past it are dropped, so the edges
@@ -386,7 +390,7 @@ __global__ __launch_bounds__(kThreads, WALK ? 4 : 1) void low_kernel(AdapterArgs
             const XT* x = static_cast<const XT*>(k.x) + static_cast<size_t>(t0 + first + col) * k.d_in + begin;
             const uint16_t* a = k.a + (static_cast<size_t>(n.lead[i]) * k.rank + r0) * k.d_in + begin;
 #pragma unroll 1
-            for (int j = 0; j < width; ++j)
+            for (int j = 0; j < width && !all_nan(s); ++j)
 #pragma unroll
               for (int r = 0; r < 4; ++r) s[r] = fmaf(lo_of(a[static_cast<size_t>(r) * k.d_in + j]), static_cast<float>(x[j]), s[r]);
           }
@@ -653,7 +657,7 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
           const uint16_t* b = k.b + (static_cast<size_t>(n.lead) * k.d_out + (n.o + u) * 16 + quad * 4) * k.rank;
           d = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-          for (int j = 0; j < k.rank; ++j) {
+          for (int j = 0; j < k.rank && !all_nan(d); ++j) {
             const float x = lo_of(v[j]) + (lo_of(v[kPlane + j]) + lo_of(v[2 * kPlane + j]));
 #pragma unroll
             for (int r = 0; r < 4; ++r) d[r] = fmaf(lo_of(b[r * k.rank + j]), x, d[r]);
