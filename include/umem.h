@@ -367,7 +367,7 @@ typedef struct umem_block_desc {
  * Limits (UMEM_ERR_UNSUPPORTED beyond them): d <= 16384; T <= 2^20.
  * Arrays [T, d] are dense; every array is aligned to its elements (rows of a multiple of 4
  * elements in arrays aligned to 4 elements are moved in pieces of four).  Arithmetic and statistics
- * are fp32 (the mean of a row's squares has to be below 2^128, or its 1 / sqrt is 0); a bf16 result is rounded
+ * are fp32 (the sum of a row's squares has to be below 2^128, or its 1 / sqrt is 0); a bf16 result is rounded
  * once, to nearest even.  Every row is computed from its own
  * elements alone, so NaN and infinities of one token stay in its row (the sums over tokens of the
  * backward take them in). */
@@ -411,7 +411,7 @@ UMEM_API umem_status umem_block_in_backward(const umem_block_desc* bd, int32_t T
  * the dh of umem_block_in_backward of the next entry):
  *   dh = res_scale dh_out;  with dm = out_scale dh_out: dgate = dm Norm_out(y) act'(gate), summed over
  *   tokens for a channel gate and over channels for a token gate (a sigmoid's slope is g (1 - g) of its fp32
- *   value g: within 2^-22 of itself, not of its size, where g is near one);  dy = J^T (act(gate) dm), dgamma and
+ *   value g: within 2^-22, which is more than the slope itself where the gate is past 15);  dy = J^T (act(gate) dm), dgamma and
  *   dbeta as above
  *   y, gate, gamma, beta  as for the forward
  *   dh_out  [T, d] of htype;  dh [T, d] of htype, or NULL (not wanted; may equal dh_out)
