@@ -301,8 +301,8 @@ __global__ __launch_bounds__(kColWide * kColDeep) void column_sum_kernel(ColumnA
 // 16; 8,192 bf16 rows of 2,048 take 49 with two workgroups of 256 threads, 59 with one).
 int most_parts(const RowShape& s) { return s.group >= 512 ? 256 : 512; }
 // Rows of 4,097 to 8,192 (row_shape), 512 threads a row: the exit's backward of 2,048 fp32 rows of 5,000 79 us, with 1,024
-// threads 112; bf16 43 and 62.  Both spill: 2 to 98 registers
-// in nine of twelve instances, with 1,024 threads 23 to 112 in all.
+// threads 112; bf16 43 and 62.  Both spill: 2 to 98 registers in nine of twelve instances, with 1,024
+// threads 23 to 112 in all.
 constexpr int kFours8K = 4;
 
 hipError_t launch_columns(const ColumnArgs& c, hipStream_t s) {
