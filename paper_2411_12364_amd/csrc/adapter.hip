@@ -9,8 +9,8 @@
 //   d_in each, its sums over the runs through the workspace, then B times those by tiles and a range of
 //   outputs.  Bound by HBM (x, base and out once, and 8 bytes for each token, rank and run); the adapters come
 //   from L2, once for the 16 tokens of a product that share one.  A launch for both, with all of d_in and A for
-//   16 tokens in one workgroup, waited for twice as many bytes from L2 in every CU (16 runs, rank 32, 2,048 by 896: 1,024 tokens 20.8 us, now 13.7;
-//   4,096 tokens 22, now 20).
+//   16 tokens in one workgroup, waited for twice as many bytes from L2 in every CU (16 runs, rank 32, 2,048 by
+//   896: 1,024 tokens 20.8 us, now 13.7; 4,096 tokens 22, now 20).
 //
 // Nothing is rounded on the way: an fp32 value is the sum of three bf16 parts of 8 bits each, whose
 // products with bf16 weights are exact in the matrix cores' fp32 accumulators.
@@ -680,8 +680,8 @@ __global__ __launch_bounds__(kThreads) void out_kernel(AdapterArgs k, int RT) {
 // does its own A x whoever shares the adapter, a tile shares it, but only among tokens that lie together, and
 // has few workgroups.  In us, a workgroup a token and tiles, for 8 adapters in runs, 64 in runs, 64 in random
 // order (only the device knows it; what n alone says of the sharing is not used): rank 16, 1,024 by 2,048: 2,048
-// tokens 20, 21, 25 and 16, 16, 30; 4,096 36, 36, 44 and 20, 21, 48.  Rank 32, 2,048 by 896: 1,024 tokens 16, 20, 24 and 14, 15, 40; 2,048 28, 27, 43
-// and 15, 17, 53.  Rank 64, 2,048 by 2,048: 512 tokens 19, 36, 33 and 16, 25, 57; 1,024 34, 44, 63 and 19, 25, 79.
+// tokens 20, 21, 25 and 16, 16, 30; 4,096 36, 36, 44 and 20, 21, 48.  Rank 32, 2,048 by 896: 1,024 tokens
+// 16, 20, 24 and 14, 15, 40; 2,048 28, 27, 43 and 15, 17, 53.  Rank 64, 2,048 by 2,048: 512 tokens 19, 36, 33 and 16, 25, 57; 1,024 34, 44, 63 and 19, 25, 79.
 constexpr int kTileFrom = 40960;
 bool by_tiles(const umem_adapter_desc& ad, int T) { return static_cast<int64_t>(T) * ad.rank >= kTileFrom; }
 
