@@ -11,7 +11,8 @@
  *   a7  gather-sum         eq. (1) o = V^T s; eq. (15) per virtual block; heads add (Sec. 3.1)
  *   a8  projection         eq. (15) sum_p W_p^T (.); Sec. 3.2 Trick 6 output linear
  * and, for the model around it, the norms before and after a block, the global gradient norm with
- * clipping, and low-rank adapters beside the projections.
+ * clipping, low-rank adapters beside the projections, the lookup of token rows, the cross entropy of a
+ * large vocabulary, and the orthogonalised update of a matrix.
  *
  * Conventions shared by every entry point:
  *   - All array arguments are DEVICE pointers owned by the caller, dense and row-major, unless
@@ -507,6 +508,123 @@ UMEM_API umem_status umem_query_adapted(const umem_query_desc* qd, const umem_ad
                                const int32_t* ids, const uint16_t* a, const uint16_t* b, const float* scale,
                                const float* gamma, const float* beta, float* q_row, float* q_col, void* ws,
                                size_t ws_bytes, hipStream_t stream);
+
+/* A model's first operator: the rows of its tokens, and their gradient. */
+typedef struct umem_embed_desc {
+  int32_t vocab;   /* rows of the table */
+  int32_t d;       /* their width */
+  int32_t wtype;   /* UMEM_F32 or UMEM_BF16: the table */
+  int32_t otype;   /* the looked-up rows, and their gradient */
+  float scale;     /* finite; their factor */
+} umem_embed_desc;
+/* Requirements (UMEM_ERR_INVALID_ARG otherwise): vocab, d >= 1, the types as listed, a finite scale.
+ * Limits (UMEM_ERR_UNSUPPORTED beyond them): d <= 16384; T <= 2^20.
+ * Every array is aligned to its elements (rows of a multiple of 4 elements in arrays aligned to 4 elements are
+ * moved fastest). */
+
+/* out[t] = scale * table[ids[t]], rounded once; zeros where ids[t] is not in [0, vocab) (a padded place).
+ *   table  [vocab, d] of wtype;  ids int32 [T];  out [T, d] of otype, apart from both */
+UMEM_API umem_status umem_embed(const umem_embed_desc* ed, int32_t T, const void* table, const int32_t* ids, void* out,
+                       hipStream_t stream);
+
+/* Scratch bytes that the two gradient calls need for T tokens or fewer. */
+UMEM_API umem_status umem_embed_backward_workspace_size(const umem_embed_desc* ed, int32_t T, size_t* bytes);
+
+/* Gradient of umem_embed: dtable[v] += scale * sum over t with ids[t] = v of dout[t].  Rows without a token
+ * are not touched, padded places (ids[t] not in [0, vocab)) are not read.  Sums are fp32, over a row's tokens in an
+ * order that ids alone fix.
+ *   dout    [T, d] of otype;  dtable fp32 [vocab, d] (accumulated; where the head's weight is the table,
+ *           the array that umem_head_backward writes)
+ *   ws      16-byte aligned scratch of umem_embed_backward_workspace_size bytes
+ * dtable and ws overlap neither an input nor each other (UMEM_ERR_INVALID_ARG). */
+UMEM_API umem_status umem_embed_backward(const umem_embed_desc* ed, int32_t T, const int32_t* ids, const void* dout,
+                                float* dtable, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The same with the gradient returned compactly, one row per distinct token, as umem_gather_backward_rows returns
+ * it (and umem_grad takes it):
+ *   rows    int32 [T] (capacity): the distinct tokens, ascending; the first *n_rows are written
+ *   d_rows  fp32 [T, d] (capacity): d_rows[r] = scale * sum of dout over the tokens rows[r] (written; rows from
+ *           *n_rows on untouched)
+ *   n_rows  int32 [1], device memory (written; 0 where every place is padded)
+ * The outputs and ws overlap neither an input nor each other.  T == 0 writes nothing (n_rows included). */
+UMEM_API umem_status umem_embed_backward_rows(const umem_embed_desc* ed, int32_t T, const int32_t* ids, const void* dout,
+                                     int32_t* rows, float* d_rows, int32_t* n_rows, void* ws, size_t ws_bytes,
+                                     hipStream_t stream);
+
+/* A model's last operator: softmax cross entropy over its vocabulary, from the hidden states; the logits are
+ * never kept:
+ *   z[t, v] = scale * <x[t], w[v]>,  lse[t] = log sum_v exp z[t, v],  loss[t] = lse[t] - z[t, targets[t]],
+ * loss[t] = 0 where targets[t] is not in [0, vocab) (a token that does not count). */
+typedef struct umem_head_desc {
+  int32_t vocab;   /* rows of the weight */
+  int32_t d;       /* width of the hidden states */
+  int32_t xtype;   /* UMEM_F32 or UMEM_BF16: x, and its gradient */
+  int32_t gtype;   /* the weight's gradient */
+  float scale;     /* finite; the logits' factor (an inverse temperature) */
+} umem_head_desc;
+/* Requirements (UMEM_ERR_INVALID_ARG otherwise): vocab, d >= 1, the types as listed, a finite scale.
+ * Limits (UMEM_ERR_UNSUPPORTED beyond them): d a multiple of 8; d <= 16384; vocab <= 2^20; T <= 2^20.
+ * Sums, statistics and losses are fp32 or more.  fp32 x is not rounded: it enters the matrix cores as a
+ * sum of bf16 parts.  A logit of NaN makes its token's loss NaN; what one token holds stays with it in loss, lse and dx. */
+
+/* Scratch bytes that umem_head_loss needs for T tokens or fewer. */
+UMEM_API umem_status umem_head_loss_workspace_size(const umem_head_desc* hd, int32_t T, size_t* bytes);
+
+/*   x        [T, d] of xtype;  w bf16 bits [vocab, d] (output-major, as a linear layer's weight)
+ *   targets  int32 [T]
+ *   loss     fp32 [T];  lse fp32 [T] (written for every token, whether it counts or not)
+ *   ws       256-byte aligned scratch of umem_head_loss_workspace_size bytes
+ * x and w are 16-byte aligned.  loss, lse and ws overlap neither an input nor each other (UMEM_ERR_INVALID_ARG). */
+UMEM_API umem_status umem_head_loss(const umem_head_desc* hd, int32_t T, const void* x, const uint16_t* w,
+                           const int32_t* targets, float* loss, float* lse, void* ws, size_t ws_bytes,
+                           hipStream_t stream);
+
+/* Scratch bytes that umem_head_backward needs for T tokens or fewer: r below for a piece of the vocabulary at a
+ * time, x and the piece of w transposed, a sum of dx in fp32. */
+UMEM_API umem_status umem_head_backward_workspace_size(const umem_head_desc* hd, int32_t T, size_t* bytes);
+
+/* Backward of umem_head_loss; the logits are made again from x and w:
+ *   r[t, v] = scale * dloss[t] * (exp(z[t, v] - lse[t]) - [v = targets[t]]), 0 for a token that does not count
+ *   dx = r w (0 for such a token),  dw = r^T x (what such a token's x holds does not reach it)
+ *   x, w, targets, lse  as for the forward (lse its output)
+ *   dloss       fp32 [T]: the gradient of the losses (1 / their number, for their mean), or NULL for ones
+ *   dx          [T, d] of xtype;  dw [vocab, d] of gtype; both 16-byte aligned
+ *   accumulate  0: dw is written; 1: added to (fp32 only, UMEM_ERR_INVALID_ARG otherwise)
+ *   ws          256-byte aligned scratch of umem_head_backward_workspace_size bytes
+ * r enters the products as bf16 where the result is bf16 (which is then rounded once more), and whole, as a sum of
+ * bf16 parts, where it is fp32.  The sums over tokens run in a fixed order.  dx, dw and ws overlap neither an
+ * input nor each other (UMEM_ERR_INVALID_ARG).  T == 0 writes nothing. */
+UMEM_API umem_status umem_head_backward(const umem_head_desc* hd, int32_t T, const void* x, const uint16_t* w,
+                               const int32_t* targets, const float* lse, const float* dloss, void* dx, void* dw,
+                               int32_t accumulate, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The orthogonalised update of n matrices of one shape by Newton-Schulz products, each on its own:
+ *   X = G / (|G|_F + eps);  steps times  X = a X + (b A + c A^2) X,  A = X X^T (X^T X where rows > cols, from
+ *   the right);  out = decay * out + scale * X
+ * With a = 3.4445, b = -4.7750, c = 2.0315 five steps take singular values between 0.01 and 1 of X to near 1.  decay
+ * and scale let the call update a weight in place (1 - rate * weight decay, and - rate). */
+typedef struct umem_orth_desc {
+  int32_t n;           /* matrices, one after another */
+  int32_t rows, cols;
+  int32_t gtype;       /* UMEM_F32 or UMEM_BF16: g */
+  int32_t otype;       /* out */
+  int32_t steps;
+  float a, b, c;       /* finite */
+  float eps;           /* finite, >= 0 (at 0 a matrix of zeros gives NaN, as 0 / 0) */
+  float decay, scale;  /* finite; with a decay of 0 out is written and not read */
+} umem_orth_desc;
+/* Requirements (UMEM_ERR_INVALID_ARG otherwise): n, rows, cols, steps >= 1, the types as listed.
+ * Limits (UMEM_ERR_UNSUPPORTED beyond them): rows and cols <= 2^16; n < 2^16; n * rows * cols <= 2^33; steps <= 16.
+ * Between the steps a matrix has 22 bits of each value of 2^-14 or more and an absolute error of 2^-37 below; its
+ * values stay below 16 where the coefficients keep singular values of [0, 1] there (an entry of X, A or b A + c A^2
+ * that reaches 16 becomes infinite).  Sums are fp32, the norm fp64. */
+UMEM_API umem_status umem_orthogonalize_workspace_size(const umem_orth_desc* od, size_t* bytes);
+
+/*   g    [n, rows, cols] of gtype;  out [n, rows, cols] of otype (may equal g); both aligned to their elements
+ *   ws   256-byte aligned scratch of umem_orthogonalize_workspace_size bytes
+ * out and ws overlap neither each other nor g, but for an out that is g. */
+UMEM_API umem_status umem_orthogonalize(const umem_orth_desc* od, const void* g, void* out, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
 
 /* A static, human-readable name of a status code. */
 UMEM_API const char* umem_status_string(umem_status status);

@@ -45,7 +45,10 @@ EXPORTED = ("umem_workspace_size", "umem_axis_scores", "umem_select", "umem_scor
             "umem_block_in_backward", "umem_block_out_backward",
             "umem_grad_workspace_size", "umem_grad_norm", "umem_grad_clip",
             "umem_adapter_workspace_size", "umem_adapter_add",
-            "umem_query_adapted_workspace_size", "umem_query_adapted", "umem_status_string")
+            "umem_query_adapted_workspace_size", "umem_query_adapted",
+            "umem_embed", "umem_embed_backward_workspace_size", "umem_embed_backward", "umem_embed_backward_rows",
+            "umem_head_loss_workspace_size", "umem_head_loss", "umem_head_backward_workspace_size",
+            "umem_head_backward", "umem_orthogonalize_workspace_size", "umem_orthogonalize", "umem_status_string")
 
 
 class umem_desc(ctypes.Structure):
@@ -88,6 +91,28 @@ class umem_adapter_desc(ctypes.Structure):
     ]
 
 
+class umem_embed_desc(ctypes.Structure):
+    _fields_ = [
+        ("vocab", ctypes.c_int32), ("d", ctypes.c_int32), ("wtype", ctypes.c_int32), ("otype", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class umem_head_desc(ctypes.Structure):
+    _fields_ = [
+        ("vocab", ctypes.c_int32), ("d", ctypes.c_int32), ("xtype", ctypes.c_int32), ("gtype", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class umem_orth_desc(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int32), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("gtype", ctypes.c_int32),
+        ("otype", ctypes.c_int32), ("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float),
+        ("c", ctypes.c_float), ("eps", ctypes.c_float), ("decay", ctypes.c_float), ("scale", ctypes.c_float),
+    ]
+
+
 class UmemError(RuntimeError):
     def __init__(self, status: int, what: str = ""):
         self.status = status
@@ -101,6 +126,7 @@ def _load() -> ctypes.CDLL:
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     F32 = ctypes.c_float
     BD, AD = ctypes.POINTER(umem_block_desc), ctypes.POINTER(umem_adapter_desc)
+    ED, HD, OD = (ctypes.POINTER(t) for t in (umem_embed_desc, umem_head_desc, umem_orth_desc))
     D = ctypes.POINTER(umem_desc)
     sig = {
         "umem_workspace_size": [D, I32, ctypes.POINTER(SZ)],
@@ -134,6 +160,16 @@ def _load() -> ctypes.CDLL:
         "umem_query_adapted_workspace_size": [ctypes.POINTER(umem_query_desc), AD, I32, I32, ctypes.POINTER(SZ)],
         "umem_query_adapted": [ctypes.POINTER(umem_query_desc), AD, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P, P,
                                SZ, P],
+        "umem_embed": [ED, I32, P, P, P, P],
+        "umem_embed_backward_workspace_size": [ED, I32, ctypes.POINTER(SZ)],
+        "umem_embed_backward": [ED, I32, P, P, P, P, SZ, P],
+        "umem_embed_backward_rows": [ED, I32, P, P, P, P, P, P, SZ, P],
+        "umem_head_loss_workspace_size": [HD, I32, ctypes.POINTER(SZ)],
+        "umem_head_loss": [HD, I32, P, P, P, P, P, P, SZ, P],
+        "umem_head_backward_workspace_size": [HD, I32, ctypes.POINTER(SZ)],
+        "umem_head_backward": [HD, I32, P, P, P, P, P, P, P, I32, P, SZ, P],
+        "umem_orthogonalize_workspace_size": [OD, ctypes.POINTER(SZ)],
+        "umem_orthogonalize": [OD, P, P, P, SZ, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -387,3 +423,58 @@ def umem_query_adapted(qd, ad, B, L, x, x_hist, conv_w, w_q, ids, a, b, scale, g
     return _lib.umem_query_adapted(_d(qd), _d(ad), B, L, _p(x), _p(x_hist), _p(conv_w), _p(w_q), _p(ids),
                                    _p(a), _p(b), _p(scale), _p(gamma), _p(beta), _p(q_row), _p(q_col),
                                    _p(ws), ws_bytes, _s(stream, x))
+
+
+def umem_embed(ed, T, table, ids, out, stream=None) -> int:
+    return _lib.umem_embed(_d(ed), T, _p(table), _p(ids), _p(out), _s(stream, ids))
+
+
+def umem_embed_backward_workspace_size(ed, T):
+    """Returns (status, bytes)."""
+    out = ctypes.c_size_t(0)
+    st = _lib.umem_embed_backward_workspace_size(_d(ed), T, ctypes.byref(out))
+    return st, out.value
+
+
+def umem_embed_backward(ed, T, ids, dout, dtable, ws, ws_bytes, stream=None) -> int:
+    return _lib.umem_embed_backward(_d(ed), T, _p(ids), _p(dout), _p(dtable), _p(ws), ws_bytes, _s(stream, ids))
+
+
+def umem_embed_backward_rows(ed, T, ids, dout, rows, d_rows, n_rows, ws, ws_bytes, stream=None) -> int:
+    return _lib.umem_embed_backward_rows(_d(ed), T, _p(ids), _p(dout), _p(rows), _p(d_rows), _p(n_rows), _p(ws),
+                                         ws_bytes, _s(stream, ids))
+
+
+def umem_head_loss_workspace_size(hd, T):
+    """Returns (status, bytes)."""
+    out = ctypes.c_size_t(0)
+    st = _lib.umem_head_loss_workspace_size(_d(hd), T, ctypes.byref(out))
+    return st, out.value
+
+
+def umem_head_loss(hd, T, x, w, targets, loss, lse, ws, ws_bytes, stream=None) -> int:
+    return _lib.umem_head_loss(_d(hd), T, _p(x), _p(w), _p(targets), _p(loss), _p(lse), _p(ws), ws_bytes,
+                               _s(stream, x))
+
+
+def umem_head_backward_workspace_size(hd, T):
+    """Returns (status, bytes)."""
+    out = ctypes.c_size_t(0)
+    st = _lib.umem_head_backward_workspace_size(_d(hd), T, ctypes.byref(out))
+    return st, out.value
+
+
+def umem_head_backward(hd, T, x, w, targets, lse, dloss, dx, dw, accumulate, ws, ws_bytes, stream=None) -> int:
+    return _lib.umem_head_backward(_d(hd), T, _p(x), _p(w), _p(targets), _p(lse), _p(dloss), _p(dx), _p(dw),
+                                   accumulate, _p(ws), ws_bytes, _s(stream, x))
+
+
+def umem_orthogonalize_workspace_size(od):
+    """Returns (status, bytes)."""
+    out = ctypes.c_size_t(0)
+    st = _lib.umem_orthogonalize_workspace_size(_d(od), ctypes.byref(out))
+    return st, out.value
+
+
+def umem_orthogonalize(od, g, out, ws, ws_bytes, stream=None) -> int:
+    return _lib.umem_orthogonalize(_d(od), _p(g), _p(out), _p(ws), ws_bytes, _s(stream, g))

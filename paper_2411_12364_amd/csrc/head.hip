@@ -1,0 +1,569 @@
+// The head of a model: softmax cross entropy of a large vocabulary from the hidden states, and its gradients, without
+// the logits ever being kept.
+//
+//   z[t][v] = s <x[t], W[v]>,  lse[t] = log sum_v exp z[t][v],  loss[t] = lse[t] - z[t][y[t]]
+//   r[t][v] = s dloss[t] (exp(z[t][v] - lse[t]) - [v = y[t]]),  dx = r W,  dW (+)= r^T x
+//
+// Forward: tiles of logits (tiles.h; the vocabulary along m) are made on the matrix cores and reduced where
+// they are, in registers, to each token's maximum and sum of exponentials over the tile's rows; a second kernel joins the
+// tiles' pairs in their order.  Backward: the vocabulary goes by pieces; for each the logits are made again, r goes to
+// scratch in bf16 in both orders, and two more products take it, all three with k innermost (x and the piece's rows of
+// W are laid out transposed beforehand).  Bounded by the matrix cores: 2 T V d operations forward, 6 T V d backward, but
+// for few tokens, where W is read once at the rate of the memory.
+//
+// Rounding: logits and sums are fp32 of bf16 operands; fp32 x is three bf16 parts, which hold it whole.  r enters its
+// products as one bf16 part where the result is bf16 (both roundings are of the result's own size), and as
+// three, which hold it whole, where the result is fp32.  r is made for losses' gradients of at most 1, and the largest of
+// them and s are multiplied in last, in fp32: the gradient of a mean has one value for all tokens, and a target's
+// r of nearly that value times -s would be rounded the same way for all of them.
+#include <algorithm>
+
+#include "tiles.h"
+
+namespace umem {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ uint32_t bf16_bits(float x) {
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
+}
+__device__ __forceinline__ float bits_f32(uint32_t b) { return __uint_as_float(b << 16); }
+
+// Part `part` of x as a sum of bf16 parts.  What is past the first part of a value that is no number, or too large for
+// bf16, is zero.
+template <int N>
+__device__ __forceinline__ void bf16_parts(float x, uint32_t (&p)[N]) {
+  float rest = x;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    p[i] = bf16_bits(rest);
+    const float v = bits_f32(p[i]);
+    rest = fabsf(v) <= 3.4e38f ? rest - v : 0.f;
+  }
+}
+
+// ---------------------------------------------------------------- layouts
+
+// fp32 x to its parts, [3][T][d].
+__global__ __launch_bounds__(kThreads) void head_split_kernel(const float* __restrict__ x, uint16_t* __restrict__ parts,
+                                                              size_t n) {
+  const size_t i = (static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
+  if (i >= n) return;
+  const f32x4 v = *reinterpret_cast<const f32x4*>(x + i);
+  uint32_t p[4][3];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) bf16_parts(v[j], p[j]);
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    *reinterpret_cast<u32x2*>(parts + k * n + i) = u32x2{p[0][k] | p[1][k] << 16, p[2][k] | p[3][k] << 16};
+}
+
+// in [rows, cols] (cols a multiple of 8) to out [parts][cols][ld], zeros from `rows` on and in the place of rows whose
+// target is none (0 times what is no number would reach the others' sums).
+template <typename T, int PARTS>
+__global__ __launch_bounds__(kThreads) void head_transpose_kernel(const T* __restrict__ in, int rows, int cols,
+                                                                  uint16_t* __restrict__ out, int64_t ld,
+                                                                  const int32_t* __restrict__ targets, int vocab) {
+  __shared__ uint16_t tile[PARTS][64][66];
+  const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int r = r0 + i * 4 + threadIdx.x / 64, c = c0 + threadIdx.x % 64;
+    bool on = r < rows && c < cols;
+    if (on && targets) on = static_cast<uint32_t>(targets[r]) < static_cast<uint32_t>(vocab);
+    uint32_t p[PARTS] = {};
+    if (on) {
+      if constexpr (sizeof(T) == 4) bf16_parts(static_cast<float>(in[static_cast<int64_t>(r) * cols + c]), p);
+      else p[0] = in[static_cast<int64_t>(r) * cols + c];
+    }
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) tile[k][threadIdx.x % 64][i * 4 + threadIdx.x / 64] = static_cast<uint16_t>(p[k]);
+  }
+  __syncthreads();
+  const int64_t part = static_cast<int64_t>(cols) * ld;
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = i * 8 + threadIdx.x / 32, r = (threadIdx.x % 32) * 2;
+      if (c0 + c < cols && r0 + r < ld)
+        *reinterpret_cast<uint32_t*>(out + k * part + static_cast<int64_t>(c0 + c) * ld + r0 + r) =
+            tile[k][c][r] | static_cast<uint32_t>(tile[k][c][r + 1]) << 16;
+    }
+}
+
+// ---------------------------------------------------------------- forward
+
+// Each token's (reference, sum of exp(z - reference)) over the tile's rows of W, to stats[tile][T]; the reference is
+// the maximum, or 0 where that is not finite.  goal[t]: the target's logit, by the tile that holds it.
+template <int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void head_stats_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
+                                                                 const int32_t* __restrict__ targets,
+                                                                 float2* __restrict__ stats, float* __restrict__ goal) {
+  typedef Tile<false, BM, BN, WR, WC> Tl;
+  __shared__ __align__(16) uint16_t buf0[Tl::kElems];
+  __shared__ __align__(16) uint16_t buf1[Tl::kElems];
+  __shared__ float2 waves[WR][BN];
+  const int item = tile_item(tiles_m * tiles_n);
+  if (item >= tiles_m * tiles_n) return;                    // the whole workgroup: no barrier is skipped
+  const TilePlace at = tile_place(item, tiles_m, tiles_n);
+  Tl tile;
+  tile.init(p, at.m * BM, at.n * BN);
+  f32x4 acc[Tl::MT][Tl::NT];
+  tile.run(p, 0, p.n * ((p.k + kTileBK - 1) / kTileBK), buf0, buf1, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
+  const int V = p.a_rows, T = p.b_rows;
+  const int v0 = at.m * BM + wr * Tl::MT * 16 + 4 * (lane >> 4);
+#pragma unroll
+  for (int j = 0; j < Tl::NT; ++j) {
+    const int n = (wc * Tl::NT + j) * 16 + (lane & 15), t = at.n * BN + n;
+    const int y = t < T ? targets[t] : -1;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < Tl::MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int v = v0 + i * 16 + r;
+        acc[i][j][r] = v < V ? acc[i][j][r] * scale : -INFINITY;
+        if (v == y && v < V) goal[t] = acc[i][j][r];
+        top = fmaxf(top, acc[i][j][r]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    top = fabsf(top) < INFINITY ? top : 0.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < Tl::MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += __expf(acc[i][j][r] - top);
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (lane < 16) waves[wr][n] = float2{top, sum};
+  }
+  __syncthreads();
+  for (int n = threadIdx.x; n < BN; n += Tl::kThreads) {
+    const int t = at.n * BN + n;
+    if (t >= T) continue;
+    float top = waves[0][n].x;
+#pragma unroll
+    for (int w = 1; w < WR; ++w) top = fmaxf(top, waves[w][n].x);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WR; ++w) sum += waves[w][n].y * __expf(waves[w][n].x - top);
+    stats[static_cast<int64_t>(at.m) * T + t] = float2{top, sum};
+  }
+}
+
+// The tiles' pairs of each token, 16 lanes a token, added in fp64 in the order of the tiles.
+__global__ __launch_bounds__(kThreads) void head_join_kernel(const float2* __restrict__ stats,
+                                                             const float* __restrict__ goal,
+                                                             const int32_t* __restrict__ targets, int T, int vocab,
+                                                             int tiles, float* __restrict__ loss,
+                                                             float* __restrict__ lse) {
+  __shared__ float tops[16][17];
+  __shared__ double sums[16][17];
+  const int n = threadIdx.x % 16, q = threadIdx.x / 16, t = blockIdx.x * 16 + n;
+  float top = -INFINITY;
+  if (t < T)
+    for (int i = q; i < tiles; i += 16) top = fmaxf(top, stats[static_cast<int64_t>(i) * T + t].x);
+  tops[q][n] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, tops[i][n]);
+  double sum = 0.0;
+  if (t < T)
+    for (int i = q; i < tiles; i += 16) {
+      const float2 s = stats[static_cast<int64_t>(i) * T + t];
+      sum += s.y * exp(static_cast<double>(s.x) - top);
+    }
+  sums[q][n] = sum;
+  __syncthreads();
+  if (q != 0 || t >= T) return;
+  sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum += sums[i][n];
+  const double all = top + log(sum);
+  lse[t] = static_cast<float>(all);
+  loss[t] = static_cast<uint32_t>(targets[t]) < static_cast<uint32_t>(vocab) ? static_cast<float>(all - goal[t]) : 0.f;
+}
+
+// ---------------------------------------------------------------- backward
+
+// The largest |dloss| of the tokens that count, as kMostBlocks maxima over fixed ranges.
+constexpr int kMostBlocks = 64;
+
+__global__ __launch_bounds__(kThreads) void head_most_kernel(const float* __restrict__ dloss,
+                                                             const int32_t* __restrict__ targets, int T, int vocab,
+                                                             float* __restrict__ most) {
+  __shared__ float waves[kThreads / kWave];
+  float m = 0.f;
+  for (int t = blockIdx.x * kThreads + threadIdx.x; t < T; t += kMostBlocks * kThreads)
+    if (static_cast<uint32_t>(targets[t]) < static_cast<uint32_t>(vocab)) m = fmaxf(m, fabsf(dloss[t]));
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+  if ((threadIdx.x & (kWave - 1)) == 0) waves[threadIdx.x / kWave] = m;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (int w = 1; w < kThreads / kWave; ++w) m = fmaxf(m, waves[w]);
+  most[blockIdx.x] = m;
+}
+
+// The largest of them; 1 without any, or where it is no finite number above 0.
+__device__ __forceinline__ float most_of(const float* most) {
+  if (most == nullptr) return 1.f;
+  float m = most[threadIdx.x & (kWave - 1)];
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+  return m > 0.f && m < INFINITY ? m : 1.f;
+}
+static_assert(kMostBlocks == kWave, "a lane each");
+
+// r of a piece of the vocabulary, over s and the largest dloss, in bf16 parts: rows[part][T][piece] and cols[part][piece][t_pad], zeros past the piece's rows
+// of W, past T and for tokens without a target.  The tile goes through LDS, [token][v], its 16-byte
+// pieces permuted by the token's number so that both orders of reading meet all banks.
+template <int BM, int BN, int WR, int WC, int PR, int PC>
+__global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
+                                                                 const int32_t* __restrict__ targets,
+                                                                 const float* __restrict__ lse,
+                                                                 const float* __restrict__ dloss,
+                                                                 const float* __restrict__ most, int v_first, int vocab,
+                                                                 int piece, int t_pad, uint16_t* __restrict__ rows,
+                                                                 uint16_t* __restrict__ cols) {
+  typedef Tile<false, BM, BN, WR, WC> Tl;
+  static_assert(BM * BN <= 2 * Tl::kElems && BM % 64 == 0 && BN % 64 == 0, "a tile of bf16 fits the operands' LDS");
+  __shared__ __align__(16) uint16_t buf0[Tl::kElems];
+  __shared__ __align__(16) uint16_t buf1[Tl::kElems];
+  const int item = tile_item(tiles_m * tiles_n);
+  if (item >= tiles_m * tiles_n) return;
+  const TilePlace at = tile_place(item, tiles_m, tiles_n);
+  Tl tile;
+  tile.init(p, at.m * BM, at.n * BN);
+  f32x4 acc[Tl::MT][Tl::NT];
+  tile.run(p, 0, p.n * ((p.k + kTileBK - 1) / kTileBK), buf0, buf1, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
+  const int V = p.a_rows, T = p.b_rows;
+  const int m0 = wr * Tl::MT * 16 + 4 * (lane >> 4);
+  const float largest = most_of(most);
+#pragma unroll
+  for (int j = 0; j < Tl::NT; ++j) {
+    const int t = at.n * BN + (wc * Tl::NT + j) * 16 + (lane & 15);
+    const int y = t < T ? targets[t] : -1;
+    const bool on = static_cast<uint32_t>(y) < static_cast<uint32_t>(vocab);
+    const float l = on ? lse[t] : 0.f, g = on ? (dloss ? dloss[t] / largest : 1.f) : 0.f;
+#pragma unroll
+    for (int i = 0; i < Tl::MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int v = at.m * BM + m0 + i * 16 + r;
+        const float e = __expf(fmaf(acc[i][j][r], scale, -l)) - (v_first + v == y ? 1.f : 0.f);
+        acc[i][j][r] = on && v < V ? g * e : 0.f;
+      }
+  }
+  // token n's first element; a 16-byte piece of it is at place (piece ^ turn(n)) of the 8 in its group
+  const auto row_at = [&](int n) { return (n < BN / 2 ? buf0 : buf1) + (n % (BN / 2)) * BM; };
+  const auto turn = [](int n) { return (n ^ (n >> 3)) & 7; };
+  constexpr int kParts = PR > PC ? PR : PC;
+#pragma unroll
+  for (int part = 0; part < kParts; ++part) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < Tl::NT; ++j)
+#pragma unroll
+      for (int i = 0; i < Tl::MT; ++i) {
+        const int n = (wc * Tl::NT + j) * 16 + (lane & 15), m = m0 + i * 16;
+        uint32_t b[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          b[r] = bf16_bits(acc[i][j][r]);
+          const float v = bits_f32(b[r]);
+          acc[i][j][r] = fabsf(v) <= 3.4e38f ? acc[i][j][r] - v : 0.f;
+        }
+        *reinterpret_cast<u32x2*>(row_at(n) + (((m >> 3) ^ turn(n)) << 3) + (m & 7)) =
+            u32x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
+      }
+    __syncthreads();
+    if (part < PR) {
+      uint16_t* to = rows + static_cast<int64_t>(part) * T * piece;
+      for (int i = threadIdx.x; i < BN * (BM / 8); i += Tl::kThreads) {
+        const int n = i / (BM / 8), c = i % (BM / 8), t = at.n * BN + n, v = at.m * BM + c * 8;
+        if (t < T && v < piece)
+          *reinterpret_cast<u32x4*>(to + static_cast<int64_t>(t) * piece + v) =
+              *reinterpret_cast<const u32x4*>(row_at(n) + ((c ^ turn(n)) << 3));
+      }
+    }
+    if (part < PC) {
+      uint16_t* to = cols + static_cast<int64_t>(part) * piece * t_pad;
+      // eight lanes to a row of eight 16-byte pieces (64 tokens), eight rows of W to a wave
+      for (int i = threadIdx.x; i < BM * (BN / 8); i += Tl::kThreads) {
+        const int group = i / 64, m = (group % (BM / 8)) * 8 + (i & 7), n8 = (group / (BM / 8)) * 64 + ((i >> 3) & 7) * 8;
+        const int t = at.n * BN + n8, v = at.m * BM + m;
+        uint32_t b[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) b[k] = row_at(n8 + k)[(((m >> 3) ^ turn(n8 + k)) << 3) + (m & 7)];
+        if (t < t_pad && v < piece)
+          *reinterpret_cast<u32x4*>(to + static_cast<int64_t>(v) * t_pad + t) =
+              u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16};
+      }
+    }
+  }
+}
+
+// A product whose m lies along the rows of the output, [n][m] of ld: out = D scale (the largest dloss) + before (each
+// where it is given).  Rows n whose entry of targets is not in [0, vocab) become zeros.
+template <typename OT, int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void head_product_kernel(TilePairs p, int tiles_m, int tiles_n,
+                                                                   const float* before, OT* out, int64_t ld, float scale,
+                                                                   const float* __restrict__ most,
+                                                                   const int32_t* __restrict__ targets, int vocab) {
+  typedef Tile<false, BM, BN, WR, WC> Tl;
+  __shared__ __align__(16) uint16_t buf0[Tl::kElems];
+  __shared__ __align__(16) uint16_t buf1[Tl::kElems];
+  const int item = tile_item(tiles_m * tiles_n);
+  if (item >= tiles_m * tiles_n) return;
+  const TilePlace at = tile_place(item, tiles_m, tiles_n);
+  Tl tile;
+  tile.init(p, at.m * BM, at.n * BN);
+  f32x4 acc[Tl::MT][Tl::NT];
+  tile.run(p, 0, p.n * ((p.k + kTileBK - 1) / kTileBK), buf0, buf1, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
+  const float largest = most_of(most);
+#pragma unroll
+  for (int j = 0; j < Tl::NT; ++j) {
+    const int n = at.n * BN + (wc * Tl::NT + j) * 16 + (lane & 15);
+    if (n >= p.b_rows) continue;
+    const bool off = targets && static_cast<uint32_t>(targets[n]) >= static_cast<uint32_t>(vocab);
+#pragma unroll
+    for (int i = 0; i < Tl::MT; ++i) {
+      const int m = at.m * BM + (wr * Tl::MT + i) * 16 + 4 * (lane >> 4);
+      if (m >= p.a_rows) continue;
+      const int64_t o = n * ld + m;
+      f32x4 v = acc[i][j] * scale * largest;
+      if (before) v += *reinterpret_cast<const f32x4*>(before + o);
+      if (off) v = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (sizeof(OT) == 4)
+        *reinterpret_cast<f32x4*>(out + o) = v;
+      else
+        *reinterpret_cast<u32x2*>(out + o) =
+            u32x2{bf16_bits(v.x) | bf16_bits(v.y) << 16, bf16_bits(v.z) | bf16_bits(v.w) << 16};
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Tiles of 256 x 256 where there are enough rows of both operands, else of 64 x 64.
+constexpr int kSmallTokens = 128;
+bool large_tiles(int m, int n) { return m > 128 && n > kSmallTokens; }
+
+int x_parts(const umem_head_desc& hd) { return hd.xtype == UMEM_F32 ? 3 : 1; }
+int row_parts(const umem_head_desc& hd) { return hd.xtype == UMEM_F32 ? 3 : 1; }       // of r, for dx
+int col_parts(const umem_head_desc& hd) { return hd.gtype == UMEM_F32 ? 3 : 1; }       // of r, for dW
+
+// Rows of the vocabulary in a piece of the backward.  r's scratch holds 2^26 values of a part in each order at most (from
+// 2^18 tokens on 256 rows of every token), W's transposed piece 2^14 rows.
+constexpr int64_t kPieceRows = 1 << 14, kPieceValues = 1 << 26;
+int64_t most_piece(const umem_head_desc& hd) { return std::min(kPieceRows, up(hd.vocab, 256)); }
+int64_t piece_values(const umem_head_desc& hd, int T) {
+  const int64_t t = up(T, 64);
+  return std::min(t * most_piece(hd), std::max(kPieceValues, t * 256));
+}
+int piece_rows(const umem_head_desc& hd, int T) {
+  const int64_t t = up(T, 64), most = std::min(most_piece(hd), std::max<int64_t>(256, piece_values(hd, T) / t / 256 * 256));
+  const int64_t pieces = (hd.vocab + most - 1) / most;
+  return static_cast<int>(up((hd.vocab + pieces - 1) / pieces, 256));
+}
+
+// The forward goes by bands of tokens, so that its scratch and its grids are bounded; a workspace for T tokens holds what
+// the small tiles of fewer need.
+constexpr int kBandTokens = 1 << 15;
+struct ForwardLayout {
+  size_t parts, stats, goal, total;
+  ForwardLayout(const umem_head_desc& hd, int T) {
+    const size_t t = std::min(T, kBandTokens), d = hd.d, small = (hd.vocab + 63) / 64, large = (hd.vocab + 255) / 256;
+    parts = 0;
+    stats = up256(hd.xtype == UMEM_F32 ? 3 * t * d * 2 : 0);
+    goal = stats + up256(sizeof(float2) * (large_tiles(hd.vocab, T) ? std::max(small * kSmallTokens, large * t) : small * t));
+    total = goal + up256(t * sizeof(float));
+  }
+};
+struct BackwardLayout {
+  size_t parts, xt, wt, rows, cols, sum, most, total;
+  BackwardLayout(const umem_head_desc& hd, int T) {
+    const size_t t = T, tp = up(T, 64), d = hd.d, values = piece_values(hd, T);
+    parts = 0;
+    xt = up256(hd.xtype == UMEM_F32 ? 3 * t * d * 2 : 0);
+    wt = xt + up256(x_parts(hd) * d * tp * 2);
+    rows = wt + up256(d * most_piece(hd) * 2);
+    cols = rows + up256(row_parts(hd) * values * 2);
+    sum = cols + up256(col_parts(hd) * values * 2);
+    most = sum + up256(t * d * sizeof(float));
+    total = most + up256(kMostBlocks * sizeof(float));
+  }
+};
+
+// The logits' operands: rows of W along m, tokens along n.
+TilePairs logit_pairs(const umem_head_desc& hd, int T, const void* x, const uint16_t* parts, const uint16_t* w, int v) {
+  TilePairs p{};
+  p.n = x_parts(hd);
+  for (int i = 0; i < p.n; ++i) {
+    p.a[i] = w;
+    p.b[i] = hd.xtype == UMEM_F32 ? parts + static_cast<size_t>(p.n - 1 - i) * T * hd.d : static_cast<const uint16_t*>(x);
+  }
+  p.a_rows = v;
+  p.b_rows = T;
+  p.k = hd.d;
+  p.a_ld = p.b_ld = hd.d;
+  return p;
+}
+
+void split_x(const umem_head_desc& hd, int T, const void* x, uint16_t* parts, hipStream_t s) {
+  const size_t n = static_cast<size_t>(T) * hd.d;
+  hipLaunchKernelGGL(head_split_kernel, dim3(static_cast<unsigned>((n / 4 + kThreads - 1) / kThreads)), dim3(kThreads), 0, s,
+                     static_cast<const float*>(x), parts, n);
+}
+
+template <typename OT>
+void product(const TilePairs& p, const float* before, OT* out, int64_t ld, float scale, const float* most,
+             const int32_t* targets, int vocab, hipStream_t s) {
+#define UMEM_PRODUCT(BM, BN, WR, WC)                                                                              \
+  {                                                                                                               \
+    const int tm = (p.a_rows + BM - 1) / BM, tn = (p.b_rows + BN - 1) / BN;                                       \
+    hipLaunchKernelGGL((head_product_kernel<OT, BM, BN, WR, WC>), dim3(tile_grid(tm * tn)), dim3(64 * WR * WC), 0, \
+                       s, p, tm, tn, before, out, ld, scale, most, targets, vocab);                                            \
+  }
+  if (large_tiles(p.a_rows, p.b_rows)) UMEM_PRODUCT(256, 256, 4, 2)
+  else UMEM_PRODUCT(64, 64, 2, 2)
+#undef UMEM_PRODUCT
+}
+
+template <int PR, int PC>
+void slope(const TilePairs& p, float scale, const int32_t* targets, const float* lse, const float* dloss,
+           const float* most, int v_first, int vocab, int piece, int t_pad, uint16_t* rows, uint16_t* cols,
+           hipStream_t s) {
+#define UMEM_SLOPE(BM, BN, WR, WC)                                                                              \
+  {                                                                                                             \
+    const int tm = (piece + BM - 1) / BM, tn = (p.b_rows + BN - 1) / BN;                                        \
+    hipLaunchKernelGGL((head_slope_kernel<BM, BN, WR, WC, PR, PC>), dim3(tile_grid(tm * tn)),                   \
+                       dim3(64 * WR * WC), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first, vocab,    \
+                       piece, t_pad, rows, cols);                                                               \
+  }
+  if (large_tiles(piece, p.b_rows)) UMEM_SLOPE(256, 256, 4, 2)
+  else UMEM_SLOPE(64, 64, 2, 2)
+#undef UMEM_SLOPE
+}
+
+}  // namespace
+
+size_t head_loss_workspace_bytes(const umem_head_desc& hd, int T) { return T == 0 ? 0 : ForwardLayout(hd, T).total; }
+
+hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, const uint16_t* w, const int32_t* targets,
+                            float* loss, float* lse, void* ws, hipStream_t s) {
+  clear_stale_error();
+  const ForwardLayout L(hd, T);
+  char* base = static_cast<char*>(ws);
+  uint16_t* parts = reinterpret_cast<uint16_t*>(base + L.parts);
+  float2* stats = reinterpret_cast<float2*>(base + L.stats);
+  float* goal = reinterpret_cast<float*>(base + L.goal);
+  for (int t0 = 0; t0 < T; t0 += kBandTokens) {
+    const int t = std::min(kBandTokens, T - t0);
+    const char* xb = static_cast<const char*>(x) + static_cast<size_t>(t0) * hd.d * (hd.xtype == UMEM_F32 ? 4 : 2);
+    if (hd.xtype == UMEM_F32) split_x(hd, t, xb, parts, s);
+    const TilePairs p = logit_pairs(hd, t, xb, parts, w, hd.vocab);
+    int tiles = 0;
+#define UMEM_STATS(BM, BN, WR, WC)                                                                              \
+  {                                                                                                             \
+    const int tn = (t + BN - 1) / BN;                                                                           \
+    tiles = (hd.vocab + BM - 1) / BM;                                                                           \
+    hipLaunchKernelGGL((head_stats_kernel<BM, BN, WR, WC>), dim3(tile_grid(tiles * tn)), dim3(64 * WR * WC), 0, \
+                       s, p, tiles, tn, hd.scale, targets + t0, stats, goal);                                   \
+  }
+    if (large_tiles(hd.vocab, T)) UMEM_STATS(256, 256, 4, 2)
+    else UMEM_STATS(64, 64, 2, 2)
+#undef UMEM_STATS
+    hipLaunchKernelGGL(head_join_kernel, dim3((t + 15) / 16), dim3(kThreads), 0, s, stats, goal, targets + t0, t, hd.vocab,
+                       tiles, loss + t0, lse + t0);
+  }
+  return hipGetLastError();
+}
+
+size_t head_backward_workspace_bytes(const umem_head_desc& hd, int T) { return T == 0 ? 0 : BackwardLayout(hd, T).total; }
+
+hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, const uint16_t* w, const int32_t* targets,
+                                const float* lse, const float* dloss, void* dx, void* dw, bool accumulate, void* ws,
+                                hipStream_t s) {
+  clear_stale_error();
+  const BackwardLayout L(hd, T);
+  char* base = static_cast<char*>(ws);
+  const auto at = [&](size_t o) { return reinterpret_cast<uint16_t*>(base + o); };
+  uint16_t *parts = at(L.parts), *xt = at(L.xt), *wt = at(L.wt), *rows = at(L.rows), *cols = at(L.cols);
+  float* sum = reinterpret_cast<float*>(base + L.sum);
+  const int d = hd.d, V = hd.vocab, t_pad = static_cast<int>(up(T, 64)), piece = piece_rows(hd, T);
+  const int pr = row_parts(hd), pc = col_parts(hd);
+  const bool wide = hd.xtype == UMEM_F32;
+  float* most = dloss ? reinterpret_cast<float*>(base + L.most) : nullptr;
+  if (dloss)
+    hipLaunchKernelGGL(head_most_kernel, dim3(kMostBlocks), dim3(kThreads), 0, s, dloss, targets, T, V, most);
+  const dim3 x_grid(t_pad / 64, (d + 63) / 64);
+  if (wide) {
+    split_x(hd, T, x, parts, s);
+    hipLaunchKernelGGL((head_transpose_kernel<float, 3>), x_grid, dim3(kThreads), 0, s, static_cast<const float*>(x), T, d,
+                       xt, static_cast<int64_t>(t_pad), targets, V);
+  } else {
+    hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), x_grid, dim3(kThreads), 0, s,
+                       static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_pad), targets, V);
+  }
+  for (int v0 = 0; v0 < V; v0 += piece) {
+    const int v = std::min(piece, V - v0);
+    const uint16_t* wp = w + static_cast<int64_t>(v0) * d;
+    const TilePairs z = logit_pairs(hd, T, x, parts, wp, v);
+    const auto make = pr == 3 ? (pc == 3 ? slope<3, 3> : slope<3, 1>) : (pc == 3 ? slope<1, 3> : slope<1, 1>);
+    make(z, hd.scale, targets, lse, dloss, most, v0, V, piece, t_pad, rows, cols, s);
+    // dx: channels along m, tokens along n, the piece along k
+    hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), dim3(piece / 64, (d + 63) / 64), dim3(kThreads), 0, s, wp, v,
+                       d, wt, static_cast<int64_t>(piece), nullptr, 0);
+    TilePairs p{};
+    p.n = pr;
+    for (int i = 0; i < pr; ++i) {
+      p.a[i] = wt;
+      p.b[i] = rows + static_cast<int64_t>(pr - 1 - i) * T * piece;
+    }
+    p.a_rows = d;
+    p.b_rows = T;
+    p.k = piece;
+    p.a_ld = p.b_ld = piece;
+    const float* before = v0 > 0 ? sum : nullptr;
+    if (v0 + piece < V) product(p, before, sum, d, hd.scale, most, nullptr, 0, s);
+    else if (wide) product(p, before, static_cast<float*>(dx), d, hd.scale, most, targets, V, s);
+    else product(p, before, static_cast<__bf16*>(dx), d, hd.scale, most, targets, V, s);
+    // dW: channels along m, the piece's rows along n, tokens along k.  Of fp32 x and r the pairs of parts that add to
+    // 24 bits of the product; of fp32 x and one part of r what adds to more than r has.
+    static constexpr int kPairs[6][2] = {{0, 2}, {1, 1}, {2, 0}, {0, 1}, {1, 0}, {0, 0}};
+    p = TilePairs{};
+    const int64_t x_part = static_cast<int64_t>(d) * t_pad, c_part = static_cast<int64_t>(piece) * t_pad;
+    for (const auto& xr : kPairs) {
+      const bool in = wide ? (pc == 3 || (xr[1] == 0 && xr[0] < 2)) : (xr[0] == 0 && xr[1] < pc);
+      if (!in) continue;
+      p.a[p.n] = xt + xr[0] * x_part;
+      p.b[p.n++] = cols + xr[1] * c_part;
+    }
+    p.a_rows = d;
+    p.b_rows = v;
+    p.k = t_pad;
+    p.a_ld = p.b_ld = t_pad;
+    const int64_t w_at = static_cast<int64_t>(v0) * d;
+    if (hd.gtype == UMEM_F32) {
+      float* g = static_cast<float*>(dw) + w_at;
+      product(p, accumulate ? g : nullptr, g, d, hd.scale, most, nullptr, 0, s);
+    } else {
+      product(p, nullptr, static_cast<__bf16*>(dw) + w_at, d, hd.scale, most, nullptr, 0, s);
+    }
+  }
+  return hipGetLastError();
+}
+
+}  // namespace umem

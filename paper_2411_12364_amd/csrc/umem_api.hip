@@ -872,6 +872,186 @@ UMEM_API umem_status umem_query_adapted(const umem_query_desc* qd, const umem_ad
 
 namespace {
 
+umem_status check_embed_desc(const umem_embed_desc* ed) {
+  if (ed == nullptr || ed->vocab < 1 || ed->d < 1 || !known_type(ed->wtype) || !known_type(ed->otype) ||
+      !finite(ed->scale))
+    return UMEM_ERR_INVALID_ARG;
+  return ed->d > kMaxModelWidth ? UMEM_ERR_UNSUPPORTED : UMEM_OK;
+}
+
+// The gradient calls' checks: in[] ids, dout; out[] what the call writes beside ws.
+umem_status check_embed_backward(const umem_embed_desc* ed, int32_t T, const int32_t* ids, const void* dout,
+                                 const Span* out, int outs, const void* ws, size_t ws_bytes) {
+  if (!ids || !dout || !aligned(ids, 4) || !aligned(dout, esize(ed->otype))) return UMEM_ERR_INVALID_ARG;
+  const size_t need = embed_backward_workspace_bytes(*ed, T), t = T;
+  if (ws == nullptr || !aligned(ws, 16) || ws_bytes < need) return UMEM_ERR_WORKSPACE;
+  const Span in[] = {{ids, t * 4}, {dout, t * ed->d * esize(ed->otype)}, {ws, need}};
+  if (!out_fits(in[2], in, 2)) return UMEM_ERR_INVALID_ARG;
+  for (int i = 0; i < outs; ++i)
+    if (!out_fits(out[i], in, 3) || !out_fits(out[i], out, i)) return UMEM_ERR_INVALID_ARG;
+  return UMEM_OK;
+}
+
+umem_status check_head_desc(const umem_head_desc* hd) {
+  if (hd == nullptr || hd->vocab < 1 || hd->d < 1 || !known_type(hd->xtype) || !known_type(hd->gtype) ||
+      !finite(hd->scale))
+    return UMEM_ERR_INVALID_ARG;
+  if (hd->d % 8 != 0 || hd->d > kMaxModelWidth || hd->vocab > kMaxHeadVocab) return UMEM_ERR_UNSUPPORTED;
+  return UMEM_OK;
+}
+
+umem_status check_orth_desc(const umem_orth_desc* od) {
+  if (od == nullptr || od->n < 1 || od->rows < 1 || od->cols < 1 || od->steps < 1 || !known_type(od->gtype) ||
+      !known_type(od->otype))
+    return UMEM_ERR_INVALID_ARG;
+  if (!finite(od->a) || !finite(od->b) || !finite(od->c) || !finite(od->eps) || od->eps < 0.0f || !finite(od->decay) ||
+      !finite(od->scale))
+    return UMEM_ERR_INVALID_ARG;
+  if (od->rows > kMaxOrthSide || od->cols > kMaxOrthSide || od->n > kMaxOrthBatch || od->steps > kMaxOrthSteps ||
+      static_cast<int64_t>(od->rows) * od->cols > kMaxOrthElements / od->n)
+    return UMEM_ERR_UNSUPPORTED;
+  return UMEM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+UMEM_API umem_status umem_embed(const umem_embed_desc* ed, int32_t T, const void* table, const int32_t* ids, void* out,
+                                hipStream_t stream) {
+  umem_status st = check_embed_desc(ed);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK || T == 0) return st;
+  if (!table || !ids || !out) return UMEM_ERR_INVALID_ARG;
+  if (!aligned(table, esize(ed->wtype)) || !aligned(ids, 4) || !aligned(out, esize(ed->otype)))
+    return UMEM_ERR_INVALID_ARG;
+  const size_t t = T, d = ed->d;
+  const Span in[] = {{table, static_cast<size_t>(ed->vocab) * d * esize(ed->wtype)}, {ids, t * 4}};
+  if (!out_fits({out, t * d * esize(ed->otype)}, in, 2)) return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_embed(*ed, T, table, ids, out, stream));
+}
+
+UMEM_API umem_status umem_embed_backward_workspace_size(const umem_embed_desc* ed, int32_t T, size_t* bytes) {
+  if (bytes == nullptr) return UMEM_ERR_INVALID_ARG;
+  *bytes = 0;
+  umem_status st = check_embed_desc(ed);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK) return st;
+  *bytes = embed_backward_workspace_bytes(*ed, T);
+  return UMEM_OK;
+}
+
+UMEM_API umem_status umem_embed_backward(const umem_embed_desc* ed, int32_t T, const int32_t* ids, const void* dout,
+                                         float* dtable, void* ws, size_t ws_bytes, hipStream_t stream) {
+  umem_status st = check_embed_desc(ed);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK || T == 0) return st;
+  if (!dtable || !aligned(dtable, 4)) return UMEM_ERR_INVALID_ARG;
+  const Span out[] = {{dtable, static_cast<size_t>(ed->vocab) * ed->d * 4}};
+  st = check_embed_backward(ed, T, ids, dout, out, 1, ws, ws_bytes);
+  if (st != UMEM_OK) return st;
+  return hip_status(launch_embed_backward(*ed, T, ids, dout, dtable, nullptr, nullptr, ws, stream));
+}
+
+UMEM_API umem_status umem_embed_backward_rows(const umem_embed_desc* ed, int32_t T, const int32_t* ids,
+                                              const void* dout, int32_t* rows, float* d_rows, int32_t* n_rows, void* ws,
+                                              size_t ws_bytes, hipStream_t stream) {
+  umem_status st = check_embed_desc(ed);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK || T == 0) return st;
+  if (!rows || !d_rows || !n_rows || !aligned(rows, 4) || !aligned(d_rows, 4) || !aligned(n_rows, 4))
+    return UMEM_ERR_INVALID_ARG;
+  const size_t t = T;
+  const Span out[] = {{rows, t * 4}, {d_rows, t * ed->d * 4}, {n_rows, 4}};
+  st = check_embed_backward(ed, T, ids, dout, out, 3, ws, ws_bytes);
+  if (st != UMEM_OK) return st;
+  return hip_status(launch_embed_backward(*ed, T, ids, dout, d_rows, rows, n_rows, ws, stream));
+}
+
+UMEM_API umem_status umem_head_loss_workspace_size(const umem_head_desc* hd, int32_t T, size_t* bytes) {
+  if (bytes == nullptr) return UMEM_ERR_INVALID_ARG;
+  *bytes = 0;
+  umem_status st = check_head_desc(hd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK) return st;
+  *bytes = head_loss_workspace_bytes(*hd, T);
+  return UMEM_OK;
+}
+
+UMEM_API umem_status umem_head_loss(const umem_head_desc* hd, int32_t T, const void* x, const uint16_t* w,
+                                    const int32_t* targets, float* loss, float* lse, void* ws, size_t ws_bytes,
+                                    hipStream_t stream) {
+  umem_status st = check_head_desc(hd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK || T == 0) return st;
+  if (!x || !w || !targets || !loss || !lse) return UMEM_ERR_INVALID_ARG;
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(targets, 4) || !aligned(loss, 4) || !aligned(lse, 4))
+    return UMEM_ERR_INVALID_ARG;
+  const size_t need = head_loss_workspace_bytes(*hd, T), t = T, d = hd->d;
+  if (ws == nullptr || !aligned(ws, kAlign) || ws_bytes < need) return UMEM_ERR_WORKSPACE;
+  const Span in[] = {{x, t * d * esize(hd->xtype)}, {w, static_cast<size_t>(hd->vocab) * d * 2}, {targets, t * 4}};
+  const Span out[] = {{loss, t * 4}, {lse, t * 4}, {ws, need}};
+  for (int i = 0; i < 3; ++i)
+    if (!out_fits(out[i], in, 3) || !out_fits(out[i], out, i)) return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_head_loss(*hd, T, x, w, targets, loss, lse, ws, stream));
+}
+
+UMEM_API umem_status umem_head_backward_workspace_size(const umem_head_desc* hd, int32_t T, size_t* bytes) {
+  if (bytes == nullptr) return UMEM_ERR_INVALID_ARG;
+  *bytes = 0;
+  umem_status st = check_head_desc(hd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK) return st;
+  *bytes = head_backward_workspace_bytes(*hd, T);
+  return UMEM_OK;
+}
+
+UMEM_API umem_status umem_head_backward(const umem_head_desc* hd, int32_t T, const void* x, const uint16_t* w,
+                                        const int32_t* targets, const float* lse, const float* dloss, void* dx,
+                                        void* dw, int32_t accumulate, void* ws, size_t ws_bytes, hipStream_t stream) {
+  umem_status st = check_head_desc(hd);
+  if (st == UMEM_OK) st = check_tokens(T);
+  if (st != UMEM_OK) return st;
+  if (accumulate != 0 && (accumulate != 1 || hd->gtype != UMEM_F32)) return UMEM_ERR_INVALID_ARG;
+  if (T == 0) return UMEM_OK;
+  if (!x || !w || !targets || !lse || !dx || !dw) return UMEM_ERR_INVALID_ARG;
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(dx, 16) || !aligned(dw, 16) || !aligned(targets, 4) ||
+      !aligned(lse, 4) || !aligned(dloss, 4))
+    return UMEM_ERR_INVALID_ARG;
+  const size_t need = head_backward_workspace_bytes(*hd, T), t = T, d = hd->d, v = hd->vocab;
+  if (ws == nullptr || !aligned(ws, kAlign) || ws_bytes < need) return UMEM_ERR_WORKSPACE;
+  const Span in[] = {{x, t * d * esize(hd->xtype)}, {w, v * d * 2}, {targets, t * 4}, {lse, t * 4}, {dloss, t * 4}};
+  const Span out[] = {{dx, t * d * esize(hd->xtype)}, {dw, v * d * esize(hd->gtype)}, {ws, need}};
+  for (int i = 0; i < 3; ++i)
+    if (!out_fits(out[i], in, 5) || !out_fits(out[i], out, i)) return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_head_backward(*hd, T, x, w, targets, lse, dloss, dx, dw, accumulate != 0, ws, stream));
+}
+
+UMEM_API umem_status umem_orthogonalize_workspace_size(const umem_orth_desc* od, size_t* bytes) {
+  if (bytes == nullptr) return UMEM_ERR_INVALID_ARG;
+  *bytes = 0;
+  const umem_status st = check_orth_desc(od);
+  if (st != UMEM_OK) return st;
+  *bytes = orth_workspace_bytes(*od);
+  return UMEM_OK;
+}
+
+UMEM_API umem_status umem_orthogonalize(const umem_orth_desc* od, const void* g, void* out, void* ws, size_t ws_bytes,
+                                        hipStream_t stream) {
+  const umem_status st = check_orth_desc(od);
+  if (st != UMEM_OK) return st;
+  if (!g || !out || !aligned(g, esize(od->gtype)) || !aligned(out, esize(od->otype))) return UMEM_ERR_INVALID_ARG;
+  const size_t need = orth_workspace_bytes(*od), e = static_cast<size_t>(od->n) * od->rows * od->cols;
+  if (ws == nullptr || !aligned(ws, kAlign) || ws_bytes < need) return UMEM_ERR_WORKSPACE;
+  const Span in[] = {{g, e * esize(od->gtype)}, {ws, need}};
+  if (!apart(in[0], in[1]) || !out_fits({out, e * esize(od->otype)}, in, 2, 0)) return UMEM_ERR_INVALID_ARG;
+  return hip_status(launch_orthogonalize(*od, g, out, ws, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
 umem_status forward_into(const umem_desc* desc, int32_t T, const float* q_row, const float* q_col,
                          const float* k_row, const float* k_col, const float* core,
                          const void* values, const int32_t* perm, const uint16_t* w_proj,

@@ -179,6 +179,31 @@ hipError_t launch_adapter_add(const umem_adapter_desc& ad, int T, const void* x,
                               const uint16_t* a, const uint16_t* b, const float* scale, const void* base,
                               void* out, void* ws, hipStream_t s);
 
+// Token rows and their gradient (embed.hip).  ws: embed_backward_workspace_bytes bytes; rows, n_rows: NULL for the
+// dense gradient.
+constexpr int kMaxModelWidth = 16384;
+hipError_t launch_embed(const umem_embed_desc& ed, int T, const void* table, const int32_t* ids, void* out,
+                        hipStream_t s);
+size_t embed_backward_workspace_bytes(const umem_embed_desc& ed, int T);
+hipError_t launch_embed_backward(const umem_embed_desc& ed, int T, const int32_t* ids, const void* dout, float* out,
+                                 int32_t* rows, int32_t* n_rows, void* ws, hipStream_t s);
+
+// The head's cross entropy (head.hip).
+constexpr int kMaxHeadVocab = 1 << 20;
+size_t head_loss_workspace_bytes(const umem_head_desc& hd, int T);
+hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, const uint16_t* w, const int32_t* targets,
+                            float* loss, float* lse, void* ws, hipStream_t s);
+size_t head_backward_workspace_bytes(const umem_head_desc& hd, int T);
+hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, const uint16_t* w, const int32_t* targets,
+                                const float* lse, const float* dloss, void* dx, void* dw, bool accumulate, void* ws,
+                                hipStream_t s);
+
+// Orthogonalised updates (orth.hip).
+constexpr int kMaxOrthSide = 1 << 16, kMaxOrthSteps = 16, kMaxOrthBatch = 65535;
+constexpr int64_t kMaxOrthElements = INT64_C(1) << 33;
+size_t orth_workspace_bytes(const umem_orth_desc& od);
+hipError_t launch_orthogonalize(const umem_orth_desc& od, const void* g, void* out, void* ws, hipStream_t s);
+
 // a8.  ws: project_workspace_bytes(...) bytes, 256-byte aligned (the intermediate and the
 // split-K partials); w_proj == nullptr is the output linear alone ([T, dv] by [dv, d_out]).
 size_t project_workspace_bytes(int T, int expand, int dv, int dv_virt, int d_out);

@@ -1,0 +1,165 @@
+"""Token rows and their gradient on the GPU against float64.
+
+A looked-up row is one fp32 product, rounded once where it is stored in bf16: equal, bit for bit, to the same
+product elsewhere.  A row of the gradient is an fp32 sum of its n terms in some order (n - 1 roundings of at most the
+sum of the absolute values), times the scale, plus what the row held (one rounding each): (n + 2) u of the sizes,
+u = 2^-24.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle.model_oracle as M
+import paper_2411_12364_amd as U
+
+pytestmark = pytest.mark.gpu
+u = 2.0 ** -24
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def host(x):
+    return x.detach().double().cpu().numpy()
+
+
+def offset(x, lead):
+    """A copy of the tensor, `lead` elements into its storage."""
+    room = torch.empty(lead + x.numel(), dtype=x.dtype, device="cuda")
+    room[lead:].copy_(x.reshape(-1))
+    return room[lead:].view(x.shape)
+
+
+def tokens(kind, T, vocab, g):
+    if kind == "same":
+        ids = torch.full((T,), vocab - 1, device="cuda")
+    elif kind == "distinct":
+        ids = torch.randperm(max(T, vocab), generator=g, device="cuda")[:T] % vocab
+    elif kind == "none":
+        ids = torch.full((T,), -1, device="cuda")
+    else:                                                              # a share near 1 / rank, some padded
+        ids = torch.exp(torch.rand((T,), generator=g, device="cuda") * np.log(vocab)).long().clamp(1, vocab) - 1
+        bad = torch.tensor([-1, vocab, -2 ** 31, 2 ** 31 - 1], device="cuda")
+        out = torch.rand((T,), generator=g, device="cuda") < 0.1
+        ids = torch.where(out, bad[torch.arange(T, device="cuda") % 4], ids)
+    return ids.to(torch.int32)
+
+
+def desc(vocab, d, wt, ot, scale):
+    return U.umem_embed_desc(vocab, d, int(wt == torch.bfloat16), int(ot == torch.bfloat16), scale)
+
+
+def workspace(ds, T):
+    st, need = U.umem_embed_backward_workspace_size(ds, T)
+    U.check(st)
+    return torch.full((need,), 0xA5, dtype=torch.uint8, device="cuda")
+
+
+@pytest.mark.parametrize("wt", TYPES)
+@pytest.mark.parametrize("ot", TYPES)
+@pytest.mark.parametrize("T,vocab,d,lead", [(1, 1, 1, 0), (1, 5, 3, 1), (7, 100, 4, 0), (33, 50, 255, 0), (5, 50, 256, 2),
+                                            (64, 300, 257, 0), (129, 70, 513, 3), (300, 1000, 1023, 1),
+                                            (32, 2000, 2048, 0), (3, 9, 16384, 0)])
+def test_rows(T, vocab, d, lead, wt, ot):
+    print(f"[case] embed {T} {vocab} {d} {lead} {wt} {ot}", flush=True)
+    g = gen(T + d)
+    table = offset(torch.randn((vocab, d), generator=g, device="cuda").to(wt), lead)
+    ids = tokens("text", T, vocab, g)
+    room = torch.full((T + 1, d), 7.0, dtype=ot, device="cuda")
+    out = offset(room, lead)
+    U.check(U.umem_embed(desc(vocab, d, wt, ot, 1.7), T, table, ids, out))
+    on = (ids >= 0) & (ids < vocab)
+    want = torch.where(on[:, None], table.float()[ids.clamp(0, vocab - 1).long()] * 1.7, 0.0).to(ot)
+    assert torch.equal(out[:T], want) and (out[T:] == 7.0).all()
+    assert np.abs(host(out[:T]) - M.embed(host(table), ids.cpu().numpy(), float(np.float32(1.7)))).max() <= \
+        8.0 * float(np.float32(1.7)) * (u + (2.0 ** -8 if ot == torch.bfloat16 else 0))
+
+
+def test_rows_past_4_gib():
+    """A table of 4.9 GB: the last rows, and values that are no numbers."""
+    vocab, d = 150000, 16384
+    table = torch.zeros((vocab, d), dtype=torch.bfloat16, device="cuda")
+    table[-3:] = torch.randn((3, d), device="cuda").to(torch.bfloat16)
+    table[-1, 5], table[-1, 6], table[1] = float("nan"), float("inf"), float("nan")
+    ids = torch.tensor([vocab - 1, 0, vocab - 3, vocab, vocab - 2, -1], dtype=torch.int32, device="cuda")
+    out = torch.empty((6, d), device="cuda")
+    U.check(U.umem_embed(desc(vocab, d, torch.bfloat16, torch.float32, 1.0), 6, table, ids, out))
+    want = table[torch.tensor([vocab - 1, 0, vocab - 3, 0, vocab - 2, 0], device="cuda")].float()
+    assert torch.equal(out.nan_to_num(9.0), want.nan_to_num(9.0)) and bool(out[0, 5].isnan()) and bool(out[0, 6].isinf())
+    # and its gradient, 9.8 GB of fp32
+    grad = torch.zeros((vocab, d), device="cuda")
+    dout = torch.randn((6, d), device="cuda")
+    ds = desc(vocab, d, torch.bfloat16, torch.float32, 2.0)
+    U.check(U.umem_embed_backward(ds, 6, ids, dout, grad, workspace(ds, 6), 1 << 30))
+    assert torch.equal(grad[-1], dout[0] * 2) and torch.equal(grad[-3], dout[2] * 2) and torch.equal(grad[0], dout[1] * 2)
+    assert int(grad.count_nonzero(dim=1).count_nonzero()) == 4
+
+
+def check_backward(T, vocab, d, gt, kind, lead=0, scale=0.75, seed=0):
+    g = gen(seed + T + d)
+    ids = tokens(kind, T, vocab, g)
+    dout = offset(torch.randn((T, d), generator=g, device="cuda").to(gt), lead)
+    on = (ids >= 0) & (ids < vocab)
+    dout[~on] = float("nan")                                            # padded places are not read
+    ds = desc(vocab, d, torch.float32, gt, scale)
+    ws = workspace(ds, T)
+    held = torch.randn((vocab, d), generator=g, device="cuda")
+    grad = offset(held, lead)
+    U.check(U.umem_embed_backward(ds, T, ids, dout, grad, ws, ws.numel()))
+    again = offset(held, lead)
+    U.check(U.umem_embed_backward(ds, T, ids, dout, again, ws, ws.numel()))
+    assert torch.equal(grad, again)
+    want, size, n = M.embed_backward(ids.cpu().numpy(), np.nan_to_num(host(dout)), vocab, scale)
+    base = host(held)
+    got = host(grad)
+    assert np.array_equal(got[n == 0], base[n == 0])
+    tol = ((n[:, None] + 2) * size + np.abs(base)) * u
+    assert (np.abs(got - (base + want)) <= tol + u * np.abs(got)).all()
+    # the compact rows
+    rows = torch.full((T,), -7, dtype=torch.int32, device="cuda")
+    d_rows = offset(torch.full((T, d), 9.0, device="cuda"), lead)
+    n_rows = torch.full((1,), -1, dtype=torch.int32, device="cuda")
+    U.check(U.umem_embed_backward_rows(ds, T, ids, dout, rows, d_rows, n_rows, ws, ws.numel()))
+    used = np.nonzero(n)[0]
+    k = int(n_rows)
+    assert k == len(used) and np.array_equal(rows[:k].cpu().numpy(), used)
+    assert (rows[k:] == -7).all() and (d_rows[k:] == 9.0).all()
+    assert (np.abs(host(d_rows[:k]) - want[used]) <= (n[used, None] + 1) * size[used] * u).all()
+    zero = torch.zeros((vocab, d), device="cuda")
+    U.check(U.umem_embed_backward(ds, T, ids, dout, zero, ws, ws.numel()))
+    assert torch.equal(d_rows[:k], zero[rows[:k].long()])
+
+
+@pytest.mark.parametrize("gt", TYPES)
+@pytest.mark.parametrize("kind", ["text", "same", "distinct", "none"])
+@pytest.mark.parametrize("T,vocab,d,lead", [(1, 1, 1, 0), (2, 3, 5, 1), (15, 40, 64, 0), (16, 16, 256, 0), (17, 9, 255, 0),
+                                            (31, 2, 257, 2), (33, 5000, 130, 0), (255, 300, 1023, 1), (1025, 777, 64, 0),
+                                            (2000, 60, 512, 0), (4097, 2049, 96, 0)])
+def test_gradient(T, vocab, d, lead, kind, gt):
+    print(f"[case] embed backward {T} {vocab} {d} {lead} {kind} {gt}", flush=True)
+    check_backward(T, vocab, d, gt, kind, lead)
+
+
+@pytest.mark.parametrize("T,vocab,d,kind", [(70000, 5000, 8, "text"), (70001, 3, 17, "same"), (65536, 200000, 4, "distinct"),
+                                            (100003, 40, 4, "text"), (1 << 20, 70000, 1, "text")])
+def test_gradient_of_many_tokens(T, vocab, d, kind):
+    print(f"[case] embed backward {T} {vocab} {d} {kind}", flush=True)
+    check_backward(T, vocab, d, torch.float32, kind)
+
+
+def test_workspace_of_more_tokens_and_a_stream():
+    """A workspace for the most tokens does for fewer, and a call runs on the stream that it is given."""
+    ds = desc(1000, 96, torch.float32, torch.float32, 1.0)
+    ws = workspace(ds, 70000)
+    side = torch.cuda.Stream()
+    for T in (3, 4096, 4097, 65521, 65536, 65537, 70000):
+        g = gen(T)
+        ids, dout = tokens("text", T, 1000, g), torch.randn((T, 96), generator=g, device="cuda")
+        a, b = torch.zeros((1000, 96), device="cuda"), torch.zeros((1000, 96), device="cuda")
+        U.check(U.umem_embed_backward(ds, T, ids, dout, a, ws, ws.numel()))
+        torch.cuda.synchronize()
+        U.check(U.umem_embed_backward(ds, T, ids, dout, b, ws, ws.numel(), side))
+        side.synchronize()
+        assert torch.equal(a, b)

@@ -1,0 +1,154 @@
+"""Newton-Schulz updates on the GPU against float64.
+
+An error E in X grows by at most a in a step (the step's map has that slope at a singular value of 0, and less
+where they are larger).  A step itself adds what its products lose: parts of 22 bits (2^-22 of an operand), a pair of parts
+left out (2^-22) and fp32 sums over k (2 u (3 k / 32 + 16) of the absolute terms; here of the Frobenius norms, which
+bound them): eps_k of each product of norms, which are at most 1.3 for X, A and B past the first step, and in all
+(a + 2 |b| + 4 |c|) eps_k |X|_F.  So, with the oracle's norms N_j before step j, the result is off by at most
+sum_j a^(steps - 1 - j) (a + 2 |b| + 4 |c|) eps N_j in the Frobenius norm, plus its own rounding.  The sizes' worst cases
+of the sums are far from what happens; the bound's own is that 22 bits are kept: bf16 operands would be 2^13 off.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle.model_oracle as M
+import paper_2411_12364_amd as U
+
+pytestmark = pytest.mark.gpu
+u = 2.0 ** -24
+COEF = (3.4445, -4.7750, 2.0315)
+BF, F = torch.bfloat16, torch.float32
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def host(x):
+    return x.detach().double().cpu().numpy()
+
+
+def desc(n, rows, cols, gt, ot, steps=5, coef=COEF, eps=1e-7, decay=0.0, scale=1.0):
+    return U.umem_orth_desc(n, rows, cols, int(gt == BF), int(ot == BF), steps, *coef, eps, decay, scale)
+
+
+def run(od, g, out):
+    st, need = U.umem_orthogonalize_workspace_size(od)
+    U.check(st)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")         # NaN in every type
+    U.check(U.umem_orthogonalize(od, g, out, ws, ws.numel()))
+    return out
+
+
+def tolerance(norms, k, steps, coef):
+    a, b, c = (abs(v) for v in coef)
+    eps = 3 * 2.0 ** -22 + 2 * u * (3 * k / 32 + 16)
+    return sum(max(a, 1.0) ** (steps - 1 - j) * (a + 2 * b + 4 * c) * eps * norms[j] for j in range(steps))
+
+
+def check(n, rows, cols, gt=F, ot=F, steps=5, coef=COEF, decay=0.0, scale=1.0, lead=0, kind="broad", seed=0):
+    g = gen(seed + rows + 3 * cols)
+    x = torch.randn((n, rows, cols), generator=g, device="cuda") * 1e-3
+    if kind == "steep":                                                 # singular values over three orders of magnitude
+        x = x * torch.logspace(0, -3, cols, device="cuda")
+    elif kind == "low":                                                 # rank 1
+        x = x[:, :, :1] * x[:, :1, :] * 1e6
+    room = torch.empty(lead + x.numel(), dtype=gt, device="cuda")
+    room[lead:] = x.reshape(-1).to(gt)
+    x = room[lead:].view(n, rows, cols)
+    held = (torch.randn((n, rows, cols), generator=g, device="cuda") * 0.1).to(ot)
+    room = torch.full((lead + x.numel() + 8,), 5.0, dtype=ot, device="cuda")
+    out = room[lead:lead + x.numel()].view(n, rows, cols)
+    out.copy_(held if decay else torch.full_like(held, float("nan")))   # without a decay out is not read
+    run(desc(n, rows, cols, gt, ot, steps, coef, decay=decay, scale=scale), x, out)
+    assert (room[lead + x.numel():] == 5.0).all()
+    f32 = [float(np.float32(v)) for v in coef]
+    for j in range(n):
+        want, norms = M.newton_schulz(host(x[j]), steps, *f32, float(np.float32(1e-7)))
+        ref = np.float32(decay) * host(held[j]) + np.float32(scale) * want if decay else np.float32(scale) * want
+        got = host(out[j])
+        tol = abs(scale) * tolerance(norms, max(rows, cols), steps, coef) + 8 * u * np.linalg.norm(ref)
+        tol += (2.0 ** -8 if ot == BF else 0.0) * np.linalg.norm(ref)
+        assert np.linalg.norm(got - ref) <= tol, (j, np.linalg.norm(got - ref), tol)
+
+
+SHAPES = [(1, 1, 1), (1, 1, 9), (1, 7, 1), (3, 2, 3), (1, 8, 8), (2, 63, 65), (1, 64, 64), (1, 65, 64), (2, 100, 31),
+          (1, 127, 129), (1, 130, 260), (3, 33, 500), (1, 500, 33), (1, 256, 256), (1, 200, 1030), (5, 72, 40)]
+
+
+@pytest.mark.parametrize("gt,ot", [(F, F), (BF, F), (F, BF), (BF, BF)])
+@pytest.mark.parametrize("n,rows,cols", SHAPES)
+def test_update(n, rows, cols, gt, ot):
+    print(f"[case] orth {n} {rows} {cols} {gt} {ot}", flush=True)
+    check(n, rows, cols, gt, ot)
+
+
+@pytest.mark.parametrize("rows,cols", [(96, 160), (160, 96), (128, 128)])
+@pytest.mark.parametrize("kw", [dict(steps=1), dict(steps=2), dict(steps=8), dict(coef=(1.5, -0.5, 0.0), steps=12),
+                                dict(coef=(2.0, -1.5, 0.5)), dict(decay=0.9, scale=-0.02), dict(decay=-1.0, scale=3.0),
+                                dict(decay=0.9, scale=-0.02, ot=BF), dict(lead=1), dict(lead=3, gt=BF, ot=BF),
+                                dict(kind="steep"), dict(kind="low"), dict(scale=0.0)])
+def test_steps_and_factors(rows, cols, kw):
+    print(f"[case] orth {rows} {cols} {kw}", flush=True)
+    check(2, rows, cols, **kw)
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 1024, 1300), (1, 1500, 700), (40, 64, 128), (1, 40, 20000), (20000, 2, 3)])
+def test_many_and_large(n, rows, cols):
+    print(f"[case] orth {n} {rows} {cols}", flush=True)
+    if n < 100:
+        check(n, rows, cols)
+        return
+    x = torch.randn((n, rows, cols), generator=gen(1), device="cuda")
+    out = run(desc(n, rows, cols, F, F), x, torch.empty_like(x))
+    for j in (0, 1, n // 2, n - 1):
+        alone = run(desc(1, rows, cols, F, F), x[j:j + 1].clone(), torch.empty((1, rows, cols), device="cuda"))
+        assert torch.equal(out[j], alone[0])
+
+
+def test_matrices_are_apart():
+    """Zeros give zeros, a NaN or an infinity stays with its matrix, and each matrix is what it is alone."""
+    x = torch.randn((4, 48, 80), generator=gen(2), device="cuda")
+    x[1] = 0.0
+    x[2, 5, 7] = float("nan")
+    out = run(desc(4, 48, 80, F, F), x, torch.empty_like(x))
+    assert (out[1] == 0).all() and bool(out[2].isnan().all())
+    for j in (0, 3):
+        assert torch.equal(out[j], run(desc(1, 48, 80, F, F), x[j].clone(), torch.empty_like(x[j])))
+    x[2, 5, 7] = float("inf")
+    out = run(desc(4, 48, 80, F, F), x, torch.empty_like(x))
+    assert bool(out[2].isnan().any()) and bool(out[0].isfinite().all()) and bool(out[3].isfinite().all())
+
+
+def test_any_scale_of_the_gradient():
+    """The norm is fp64: gradients whose squares would overflow or vanish in 32 bits give the same update."""
+    x = torch.randn((1, 64, 96), generator=gen(3), device="cuda")
+    want = run(desc(1, 64, 96, F, F, eps=0.0), x, torch.empty_like(x))
+    for f in (2.0 ** 100, 2.0 ** -100):
+        got = run(desc(1, 64, 96, F, F, eps=0.0), x * f, torch.empty_like(x))
+        assert float((got - want).abs().max()) <= 64 * u * 140 * float(want.abs().max())
+
+
+def test_in_place_and_on_a_stream():
+    x = torch.randn((2, 130, 70), generator=gen(4), device="cuda")
+    want = run(desc(2, 130, 70, F, F), x, torch.empty_like(x))
+    y = x.clone()
+    assert torch.equal(run(desc(2, 130, 70, F, F), y, y), want)
+    od = desc(2, 130, 70, F, F, decay=0.5)
+    y, z = x.clone(), x.clone()
+    assert torch.equal(run(od, y, y), run(od, x, z))                    # g is what out held
+    side = torch.cuda.Stream()
+    ws = torch.empty(U.umem_orthogonalize_workspace_size(od)[1], dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(x)
+    torch.cuda.synchronize()
+    U.check(U.umem_orthogonalize(desc(2, 130, 70, F, F), x, out, ws, ws.numel(), side))
+    side.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_rows_become_orthonormal():
+    """Five steps take the singular values of a random matrix to between 0.6 and 1.3."""
+    x = torch.randn((1, 200, 700), generator=gen(5), device="cuda")
+    s = np.linalg.svd(host(run(desc(1, 200, 700, F, F), x, torch.empty_like(x))[0]), compute_uv=False)
+    assert 0.6 < s.min() and s.max() < 1.3
