@@ -12,7 +12,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libumem.so")
 PROBE_LIB = os.path.join(PKG, "libumem_probe.so")
 SOURCES = ["umem_api.hip", "score.hip", "select.hip", "gather.hip", "project.hip", "query.hip", "sort.hip", "backward.hip",
-           "block.hip", "block_backward.hip", "grad.hip", "adapter.hip", "embed.hip", "head.hip", "orth.hip"]
+           "block.hip", "block_backward.hip", "grad.hip", "adapter.hip", "embed.hip", "head.hip",
+           "orth.hip", "orth_small.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

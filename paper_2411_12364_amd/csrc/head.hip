@@ -101,7 +101,7 @@ template <int BM, int BN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC) void head_stats_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
                                                                  const int32_t* __restrict__ targets,
                                                                  float2* __restrict__ stats, float* __restrict__ goal) {
-  typedef Tile<false, BM, BN, WR, WC> Tl;
+  typedef Tile<false, BM, BN, WR, WC, 2> Tl;
   __shared__ __align__(16) uint16_t buf0[Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[Tl::kElems];
   __shared__ float2 waves[WR][BN];
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(64 * WR * WC) void head_stats_kernel(TilePairs p, i
   Tl tile;
   tile.init(p, at.m * BM, at.n * BN);
   f32x4 acc[Tl::MT][Tl::NT];
-  tile.run(p, 0, p.n * ((p.k + kTileBK - 1) / kTileBK), buf0, buf1, acc);
+  tile.run(p, 0, Tl::slices(p), buf0, buf1, nullptr, nullptr, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
   const int V = p.a_rows, T = p.b_rows;
   const int v0 = at.m * BM + wr * Tl::MT * 16 + 4 * (lane >> 4);
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
                                                                  const float* __restrict__ most, int v_first, int vocab,
                                                                  int piece, int t_pad, uint16_t* __restrict__ rows,
                                                                  uint16_t* __restrict__ cols) {
-  typedef Tile<false, BM, BN, WR, WC> Tl;
+  typedef Tile<false, BM, BN, WR, WC, 2> Tl;
   static_assert(BM * BN <= 2 * Tl::kElems && BM % 64 == 0 && BN % 64 == 0, "a tile of bf16 fits the operands' LDS");
   __shared__ __align__(16) uint16_t buf0[Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[Tl::kElems];
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
   Tl tile;
   tile.init(p, at.m * BM, at.n * BN);
   f32x4 acc[Tl::MT][Tl::NT];
-  tile.run(p, 0, p.n * ((p.k + kTileBK - 1) / kTileBK), buf0, buf1, acc);
+  tile.run(p, 0, Tl::slices(p), buf0, buf1, nullptr, nullptr, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
   const int V = p.a_rows, T = p.b_rows;
   const int m0 = wr * Tl::MT * 16 + 4 * (lane >> 4);
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(64 * WR * WC) void head_product_kernel(TilePairs p,
                                                                    const float* before, OT* out, int64_t ld, float scale,
                                                                    const float* __restrict__ most,
                                                                    const int32_t* __restrict__ targets, int vocab) {
-  typedef Tile<false, BM, BN, WR, WC> Tl;
+  typedef Tile<false, BM, BN, WR, WC, 2> Tl;
   __shared__ __align__(16) uint16_t buf0[Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[Tl::kElems];
   const int item = tile_item(tiles_m * tiles_n);
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(64 * WR * WC) void head_product_kernel(TilePairs p,
   Tl tile;
   tile.init(p, at.m * BM, at.n * BN);
   f32x4 acc[Tl::MT][Tl::NT];
-  tile.run(p, 0, p.n * ((p.k + kTileBK - 1) / kTileBK), buf0, buf1, acc);
+  tile.run(p, 0, Tl::slices(p), buf0, buf1, nullptr, nullptr, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
   const float largest = most_of(most);
 #pragma unroll

@@ -39,10 +39,10 @@ __device__ __forceinline__ float to_f32(T x) {
   return static_cast<float>(x);
 }
 
-// A matrix of [rows][ld] in two parts, one after the other, and how far the next matrix of the batch is.
+// A matrix whose rows hold ld elements: both parts of ld / 2 values (part_at); how far the next matrix of the batch is.
 struct Parts {
   uint16_t* p;
-  int64_t part, ld, matrix;
+  int64_t ld, matrix;
 };
 
 // ---------------------------------------------------------------- norm and first X
@@ -98,99 +98,169 @@ __global__ __launch_bounds__(kThreads) void orth_first_kernel(const T* __restric
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int a = i * 8 + threadIdx.x / 32, b = (threadIdx.x % 32) * 2;
-    if (r0 + a < rows && c0 + b < by_rows.ld) {
+    if (r0 + a < rows) {
       const uint32_t x = tile[a][b], y = tile[a][b + 1];
-      uint16_t* to = by_rows.p + mat * by_rows.matrix + (r0 + a) * by_rows.ld + c0 + b;
+      uint16_t* to = by_rows.p + mat * by_rows.matrix + (r0 + a) * by_rows.ld + part_at(c0 + b);
       *reinterpret_cast<uint32_t*>(to) = (x & 0xffffu) | y << 16;
-      *reinterpret_cast<uint32_t*>(to + by_rows.part) = x >> 16 | (y & 0xffff0000u);
+      *reinterpret_cast<uint32_t*>(to + kPartStep) = x >> 16 | (y & 0xffff0000u);
     }
-    if (c0 + a < cols && r0 + b < by_cols.ld) {
+    if (c0 + a < cols) {
       const uint32_t x = tile[b][a], y = tile[b + 1][a];
-      uint16_t* to = by_cols.p + mat * by_cols.matrix + (c0 + a) * by_cols.ld + r0 + b;
+      uint16_t* to = by_cols.p + mat * by_cols.matrix + (c0 + a) * by_cols.ld + part_at(r0 + b);
       *reinterpret_cast<uint32_t*>(to) = (x & 0xffffu) | y << 16;
-      *reinterpret_cast<uint32_t*>(to + by_cols.part) = x >> 16 | (y & 0xffff0000u);
+      *reinterpret_cast<uint32_t*>(to + kPartStep) = x >> 16 | (y & 0xffff0000u);
     }
   }
 }
 
 // ---------------------------------------------------------------- products
 
-// Four values (times 2^12) at row n, columns m .. m + 3 of a matrix of `cols` columns, and at rows m .. m + 3, column n of
-// its transpose; columns up to the pads become zeros.
-__device__ __forceinline__ void put_row(const Parts& out, int64_t mat, int n, int m, int cols, f32x4 v) {
-  if (m >= out.ld) return;
-  uint32_t hi[4], lo[4];
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    f16_parts(v[r], hi[r], lo[r]);
-    if (m + r >= cols) hi[r] = lo[r] = 0u;
-  }
-  uint16_t* to = out.p + mat * out.matrix + n * out.ld + m;
-  *reinterpret_cast<u32x2*>(to) = u32x2{hi[0] | hi[1] << 16, hi[2] | hi[3] << 16};
-  *reinterpret_cast<u32x2*>(to + out.part) = u32x2{lo[0] | lo[1] << 16, lo[2] | lo[3] << 16};
-}
-__device__ __forceinline__ void put_column(const Parts& out, int64_t mat, int n, int m, int rows, f32x4 v) {
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    if (m + r >= rows) break;
-    uint32_t hi, lo;
-    f16_parts(v[r], hi, lo);
-    uint16_t* to = out.p + mat * out.matrix + (m + r) * out.ld + n;
-    to[0] = static_cast<uint16_t>(hi);
-    to[out.part] = static_cast<uint16_t>(lo);
-  }
-}
-// The four values (times 2^12) at row n, columns m .. m + 3.
-__device__ __forceinline__ f32x4 get_row(const Parts& in, int64_t mat, int n, int m) {
-  const uint16_t* from = in.p + mat * in.matrix + n * in.ld + m;
-  const u32x2 hi = *reinterpret_cast<const u32x2*>(from), lo = *reinterpret_cast<const u32x2*>(from + in.part);
-  return f32x4{bits_f32(hi.x & 0xffffu) + bits_f32(lo.x & 0xffffu), bits_f32(hi.x >> 16) + bits_f32(lo.x >> 16),
-               bits_f32(hi.y & 0xffffu) + bits_f32(lo.y & 0xffffu), bits_f32(hi.y >> 16) + bits_f32(lo.y >> 16)};
-}
-
 enum Mode { kGram, kPoly, kUpdate, kLast };
+constexpr bool symmetric(Mode m) { return m == kGram || m == kPoly; }
 
 struct OrthArgs {
   Parts a, b;             // the product's operands: rows along m and along n, k innermost
   Parts own;              // kPoly: A; kUpdate, kLast: X by rows n, m along its rows
   Parts out, out_t;       // kGram, kPoly: the product (symmetric); kUpdate: X by rows n, and transposed
-  int rows_m, rows_n, k;
-  int tiles_m, tiles_n, items;
-  float alpha, beta;      // kPoly: alpha A + beta A^2; kUpdate: alpha X + B X
-  float decay, scale;     // kLast: final = decay final + scale (alpha X + B X), [n][m] of ld
+  int rows_m, rows_n;
+  int k;                  // elements of a row that the product walks
+  int tiles_m, tiles_n, per, items;        // of a matrix: tiles; of all matrices: items
+  int splits;             // parts of k, each an item of its own with its sums to partial [split][item][BN][BM]
+  float* partial;
+  float alpha, beta;      // kPoly: alpha A + beta A^2; kUpdate, kLast: alpha X + B X
+  float decay, scale;     // kLast: final = decay final + scale (alpha X + B X), [n][m] of final_ld
   void* final;
   int64_t final_ld, final_matrix;
 };
 
-template <Mode MODE, typename OT, int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(64 * WR * WC) void orth_product_kernel(OrthArgs g) {
-  typedef Tile<true, BM, BN, WR, WC> Tl;
+// The matrix and the tile of an item; of a symmetric product the tiles with n <= m alone.
+struct OrthTile {
+  int64_t mat;
+  int m, n;
+};
+template <Mode MODE>
+__device__ __forceinline__ OrthTile orth_tile(const OrthArgs& g, int item) {
+  const int mat = item / g.per, in = item - mat * g.per;
+  if constexpr (!symmetric(MODE)) {
+    const TilePlace at = tile_place(in, g.tiles_m, g.tiles_n);
+    return {mat, at.m, at.n};
+  }
+  int m = static_cast<int>((sqrtf(8.f * in + 1.f) - 1.f) * 0.5f);
+  while ((m + 1) * (m + 2) / 2 <= in) ++m;
+  while (m * (m + 1) / 2 > in) --m;
+  return {mat, m, in - m * (m + 1) / 2};
+}
+
+// The four values (times 2^12) at row n, columns m .. m + 3.
+__device__ __forceinline__ f32x4 get_four(const Parts& in, int64_t mat, int n, int m) {
+  const uint16_t* from = in.p + mat * in.matrix + n * in.ld + part_at(m);
+  const u32x2 hi = *reinterpret_cast<const u32x2*>(from), lo = *reinterpret_cast<const u32x2*>(from + kPartStep);
+  return f32x4{bits_f32(hi.x & 0xffffu) + bits_f32(lo.x & 0xffffu), bits_f32(hi.x >> 16) + bits_f32(lo.x >> 16),
+               bits_f32(hi.y & 0xffffu) + bits_f32(lo.y & 0xffffu), bits_f32(hi.y >> 16) + bits_f32(lo.y >> 16)};
+}
+
+// A product's four sums at (n, m .. m + 3), times 2^24, become four values of the result (times 2^12) with their two parts
+// in a word each, zeros past the matrix; or go to the final output.
+template <Mode MODE, typename OT>
+__device__ __forceinline__ u32x4 finish_four(const OrthArgs& g, int64_t mat, int n, int m, f32x4 v) {
+  const bool in = n < g.rows_n && m < g.rows_m;
+  v *= kDown;
+  if constexpr (MODE != kGram) {
+    if (in) v = g.alpha * get_four(g.own, mat, n, m) + g.beta * v;
+  }
+  if constexpr (MODE == kLast) {
+    if (!in) return u32x4{0u, 0u, 0u, 0u};
+    OT* to = static_cast<OT*>(g.final) + mat * g.final_matrix + n * g.final_ld + m;
+    const float s = g.scale * kDown;
+    typedef OT four __attribute__((ext_vector_type(4), aligned(sizeof(OT))));
+    if (m + 4 <= g.rows_m) {
+      four o;
+      if (g.decay != 0.f) {
+        const four h = *reinterpret_cast<const four*>(to);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] = static_cast<OT>(fmaf(g.decay, to_f32(h[r]), s * v[r]));
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] = static_cast<OT>(s * v[r]);
+      }
+      *reinterpret_cast<four*>(to) = o;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 3; ++r) {
+        if (m + r >= g.rows_m) break;
+        to[r] = static_cast<OT>(g.decay != 0.f ? fmaf(g.decay, to_f32(to[r]), s * v[r]) : s * v[r]);
+      }
+    }
+    return u32x4{0u, 0u, 0u, 0u};
+  }
+  u32x4 w;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    uint32_t hi, lo;
+    f16_parts(v[r], hi, lo);
+    w[r] = in && m + r < g.rows_m ? hi | lo << 16 : 0u;
+  }
+  return w;
+}
+
+// A block of 64 x BM words in LDS, [n][m]; a row's 16-byte pieces are permuted by its number, so that rows and
+// columns are both read without meeting in a bank.
+template <int BM>
+__device__ __forceinline__ int word_at(int n, int m) {
+  return n * BM + ((((m >> 2) ^ n) & (BM / 4 - 1)) << 2) + (m & 3);
+}
+
+// Eight words to a row of both parts.
+__device__ __forceinline__ void put_eight(const Parts& out, int64_t mat, int row, int at, const uint32_t (&w)[8]) {
+  uint16_t* to = out.p + mat * out.matrix + row * out.ld + part_at(at);
+  *reinterpret_cast<u32x4*>(to) = u32x4{(w[0] & 0xffffu) | w[1] << 16, (w[2] & 0xffffu) | w[3] << 16,
+                                        (w[4] & 0xffffu) | w[5] << 16, (w[6] & 0xffffu) | w[7] << 16};
+  *reinterpret_cast<u32x4*>(to + kPartStep) = u32x4{w[0] >> 16 | (w[1] & 0xffff0000u), w[2] >> 16 | (w[3] & 0xffff0000u),
+                                                    w[4] >> 16 | (w[5] & 0xffff0000u), w[6] >> 16 | (w[7] & 0xffff0000u)};
+}
+
+// The block of the result at (m0, n0) from LDS to memory, by rows and (or of a symmetric result the mirrored tile) by
+// columns.
+template <Mode MODE, int BM, int BN, int THREADS, typename At>
+__device__ __forceinline__ void put_block(const OrthArgs& g, int64_t mat, int m0, int n0, bool mirrored, const At& word) {
+  for (int i = threadIdx.x; i < BN * (BM / 8); i += THREADS) {
+    const int n = i / (BM / 8), m = (i % (BM / 8)) * 8;
+    if (n0 + n >= g.rows_n || 2 * (m0 + m) >= g.out.ld) continue;
+    uint32_t w[8];
+    *reinterpret_cast<u32x4*>(w) = *reinterpret_cast<const u32x4*>(word(n, m));
+    *reinterpret_cast<u32x4*>(w + 4) = *reinterpret_cast<const u32x4*>(word(n, m + 4));
+    put_eight(g.out, mat, n0 + n, m0 + m, w);
+  }
+  if (MODE != kUpdate && !mirrored) return;
+  const Parts& out = MODE == kUpdate ? g.out_t : g.out;
+  // eight lanes to 64 consecutive n of a column, eight columns to a wave
+  for (int i = threadIdx.x; i < BM * (BN / 8); i += THREADS) {
+    const int group = i / 64, m = (group % (BM / 8)) * 8 + (i & 7), n = (group / (BM / 8)) * 64 + ((i >> 3) & 7) * 8;
+    if (m0 + m >= g.rows_m || 2 * (n0 + n) >= out.ld) continue;
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = *word(n + j, m);
+    put_eight(out, mat, m0 + m, n0 + n, w);
+  }
+}
+
+template <Mode MODE, TileParts PARTS, typename OT, int BM, int BN, int WR, int WC, int BUFS>
+__global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(BM == 64 ? 3 : 2))) void orth_product_kernel(OrthArgs g) {
+  typedef Tile<true, BM, BN, WR, WC, BUFS, PARTS> Tl;
+  static_assert(BN == 64 ? 2 * BM * BN <= Tl::kElems : BN % 128 == 0 && BM * BN <= Tl::kElems,
+                "a tile of words fits the operands' LDS");
   __shared__ __align__(16) uint16_t buf0[Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[Tl::kElems];
-  const int item = tile_item(g.items);
-  if (item >= g.items) return;
-  constexpr bool kSym = MODE == kGram || MODE == kPoly;
-  const int per = kSym ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n;
-  const int64_t mat = item / per;
-  const int in = item - static_cast<int>(mat) * per;
-  TilePlace at;
-  if constexpr (kSym) {      // the lower triangle: n <= m
-    int m = static_cast<int>((sqrtf(8.f * in + 1.f) - 1.f) * 0.5f);
-    while ((m + 1) * (m + 2) / 2 <= in) ++m;
-    while (m * (m + 1) / 2 > in) --m;
-    at = {m, in - m * (m + 1) / 2};
-  } else {
-    at = tile_place(in, g.tiles_m, g.tiles_n);
-  }
+  __shared__ __align__(16) uint16_t buf2[BUFS > 2 ? Tl::kElems : 8];
+  __shared__ __align__(16) uint16_t buf3[BUFS > 3 ? Tl::kElems : 8];
+  const int all = g.items * g.splits, id = tile_item(all);
+  if (id >= all) return;                                    // the whole workgroup: no barrier is skipped
+  const int split = id / g.items, item = id - split * g.items;
+  const OrthTile at = orth_tile<MODE>(g, item);
   TilePairs p;
-  p.n = 3;
-  const uint16_t *a = g.a.p + mat * g.a.matrix, *b = g.b.p + mat * g.b.matrix;
-  p.a[0] = a;
-  p.b[0] = b + g.b.part;
-  p.a[1] = a + g.a.part;
-  p.b[1] = b;
-  p.a[2] = a;
-  p.b[2] = b;
+  p.n = 1;
+  p.a[0] = g.a.p + at.mat * g.a.matrix;
+  p.b[0] = g.b.p + at.mat * g.b.matrix;
   p.a_rows = g.rows_m;
   p.b_rows = g.rows_n;
   p.k = g.k;
@@ -199,40 +269,64 @@ __global__ __launch_bounds__(64 * WR * WC) void orth_product_kernel(OrthArgs g) 
   Tl tile;
   tile.init(p, at.m * BM, at.n * BN);
   f32x4 acc[Tl::MT][Tl::NT];
-  tile.run(p, 0, 3 * ((g.k + kTileBK - 1) / kTileBK), buf0, buf1, acc);
+  const int64_t slices = Tl::slices(p);
+  const int from = static_cast<int>(slices * split / g.splits), to = static_cast<int>(slices * (split + 1) / g.splits);
+  tile.run(p, from, to, buf0, buf1, buf2, buf3, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
+  const int m_in = wr * Tl::MT * 16 + 4 * (lane >> 4), n_in = wc * Tl::NT * 16 + (lane & 15);
+  if (g.splits > 1) {
+    float* to = g.partial + static_cast<int64_t>(id) * (BM * BN);
 #pragma unroll
-  for (int j = 0; j < Tl::NT; ++j) {
-    const int n = at.n * BN + (wc * Tl::NT + j) * 16 + (lane & 15);
+    for (int j = 0; j < Tl::NT; ++j)
+#pragma unroll
+      for (int i = 0; i < Tl::MT; ++i)
+        *reinterpret_cast<f32x4*>(to + (n_in + j * 16) * BM + m_in + i * 16) = acc[i][j];
+    return;
+  }
+  const auto word = [&](int n, int m) {
+    uint16_t* half = BN == 64 || n < BN / 2 ? buf0 : buf1;
+    return reinterpret_cast<uint32_t*>(half) + word_at<BM>(BN == 64 ? n : n % (BN / 2), m);
+  };
+  if (MODE != kLast) __syncthreads();                       // the last slice has been read
+#pragma unroll
+  for (int j = 0; j < Tl::NT; ++j)
 #pragma unroll
     for (int i = 0; i < Tl::MT; ++i) {
-      const int m = at.m * BM + (wr * Tl::MT + i) * 16 + 4 * (lane >> 4);
-      if (n >= g.rows_n) {                                  // the transpose's pads
-        if (MODE == kUpdate && n < g.out_t.ld) put_column(g.out_t, mat, n, m, g.rows_m, f32x4{0.f, 0.f, 0.f, 0.f});
-        continue;
-      }
-      f32x4 v = acc[i][j] * kDown;                          // times 2^12 of the product
-      if constexpr (MODE != kGram) {
-        if (m < g.own.ld) v = g.alpha * get_row(g.own, mat, n, m) + g.beta * v;
-      }
-      if constexpr (kSym) {
-        put_row(g.out, mat, n, m, g.rows_m, v);
-        if (at.m != at.n) put_column(g.out, mat, n, m, g.rows_m, v);
-      } else if constexpr (MODE == kUpdate) {
-        put_row(g.out, mat, n, m, g.rows_m, v);
-        put_column(g.out_t, mat, n, m, g.rows_m, v);
-      } else {
-        OT* to = static_cast<OT*>(g.final) + mat * g.final_matrix + n * g.final_ld + m;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (m + r >= g.rows_m) break;
-          float o = g.scale * kDown * v[r];
-          if (g.decay != 0.f) o = fmaf(g.decay, to_f32(to[r]), o);
-          to[r] = static_cast<OT>(o);
-        }
-      }
+      const int n = n_in + j * 16, m = m_in + i * 16;
+      const u32x4 w = finish_four<MODE, OT>(g, at.mat, at.n * BN + n, at.m * BM + m, acc[i][j]);
+      if (MODE != kLast) *reinterpret_cast<u32x4*>(word(n, m)) = w;
     }
+  if (MODE == kLast) return;
+  __syncthreads();
+  put_block<MODE, BM, BN, Tl::kThreads>(g, at.mat, at.m * BM, at.n * BN, at.m != at.n, word);
+}
+
+// The sums of the splits, in their order, and what a product does with them; a 64 x 64 block of a tile a workgroup.
+template <Mode MODE, typename OT, int BM>
+__global__ __launch_bounds__(kThreads) void orth_join_kernel(OrthArgs g) {
+  __shared__ __align__(16) uint32_t words[64 * 64];
+  constexpr int kSub = BM / 64;
+  const int item = blockIdx.x / (kSub * kSub), sub = blockIdx.x % (kSub * kSub);
+  const OrthTile at = orth_tile<MODE>(g, item);
+  const int m_in = (sub % kSub) * 64, n_in = (sub / kSub) * 64;
+  const int m0 = at.m * BM + m_in, n0 = at.n * BM + n_in;
+  if (m0 >= g.rows_m || n0 >= g.rows_n) return;
+  const float* from = g.partial + static_cast<int64_t>(item) * (BM * BM);
+  const int64_t next = static_cast<int64_t>(g.items) * (BM * BM);
+  const auto word = [&](int n, int m) { return words + word_at<64>(n, m); };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = (threadIdx.x >> 4) + i * 16, m = (threadIdx.x & 15) * 4;
+    const float* q = from + (n_in + n) * BM + m_in + m;
+    f32x4 v = *reinterpret_cast<const f32x4*>(q);
+#pragma unroll 4
+    for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(q + s * next);
+    const u32x4 w = finish_four<MODE, OT>(g, at.mat, n0 + n, m0 + m, v);
+    if (MODE != kLast) *reinterpret_cast<u32x4*>(word(n, m)) = w;
   }
+  if (MODE == kLast) return;
+  __syncthreads();
+  put_block<MODE, 64, 64, kThreads>(g, at.mat, m0, n0, at.m != at.n, word);
 }
 
 // ---------------------------------------------------------------- host
@@ -240,16 +334,62 @@ __global__ __launch_bounds__(64 * WR * WC) void orth_product_kernel(OrthArgs g) 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 
+// A product's tiles and how often k is split, by what both sizes of tile measured (us; slices of 32 values):
+// a 64 x 64 tile (3 buffers, 3 workgroups a CU) takes 0.25 a slice alone on its CU, 0.4 and 0.6 beside one and two
+// others; a 128 x 128 tile (eight waves, 4 buffers, a CU to itself) 0.47.  So 64 x 64 wins where tiles are few and
+// k is short: 896 x 896 x 896 of A^2 11 and 23, of 2,048 x 2,048 x 2,048 42 and 44; 128 x 128 where there are many: 1,024 x
+// 16,384 of X 141 and 126, 2,048 x 8,192 240 and 210.  A split's partial sums and the launch that adds them take 4 or more: 896
+// x 896 over 2,048 20.7 in one piece, 17.0 in two, 18.6 in four; 1,024 x 1,024 over 16,384 242 in one, 60 in six.
+struct Plan {
+  int bm, splits;
+};
+constexpr int kMostSplits = 16, kCus = 256;
+constexpr size_t kPartialBytes = size_t{64} << 20;
+int64_t tile_count(int bm, int n, int rows_m, int rows_n, bool sym) {
+  const int64_t tm = (rows_m + bm - 1) / bm, tn = (rows_n + bm - 1) / bm;
+  return n * (sym ? tm * (tm + 1) / 2 : tm * tn);
+}
+Plan plan(int n, int rows_m, int rows_n, int slices, bool sym) {
+  Plan best{64, 1};
+  double least = 1e300;
+  for (int bm : {64, 128}) {
+    const int64_t it = tile_count(bm, n, rows_m, rows_n, sym);
+    for (int s = 1; s <= kMostSplits && s <= slices; ++s) {
+      const double bytes = static_cast<double>(it) * s * bm * bm * sizeof(float);
+      if (s > 1 && bytes > kPartialBytes) break;
+      const int64_t wgs = it * s, cus = (wgs + kCus - 1) / kCus;          // workgroups of the fullest CU
+      const double each = (slices + s - 1) / s;
+      double cost = s > 1 ? 4.5 + 0.7 * s + bytes / 2.5e6 : 0.0;
+      if (bm == 128) {
+        cost += static_cast<double>(cus) * (3.0 + 0.47 * each);
+      } else {
+        const int rest = static_cast<int>(cus % 3);
+        cost += static_cast<double>(cus / 3) * (3.0 + 0.6 * each);
+        if (rest) cost += 3.0 + (rest == 1 ? 0.25 : 0.4) * each;
+      }
+      if (cost < least) {
+        least = cost;
+        best = {bm, s};
+      }
+    }
+  }
+  return best;
+}
+
+size_t partial_bytes(const Plan& p, int n, int rows_m, int rows_n, bool sym) {
+  return p.splits == 1 ? 0 : up256(tile_count(p.bm, n, rows_m, rows_n, sym) * p.splits * p.bm * p.bm * sizeof(float));
+}
+
 struct Layout {
-  size_t pieces, x0, t0, x1, t1, a, b, total;
+  size_t pieces, x0, t0, x1, t1, a, b, partial, total;
   int m, k;                                 // the smaller and the larger side
-  int64_t mp, kp;
+  int64_t mp, kp;                           // values of a row
   explicit Layout(const umem_orth_desc& od) {
     m = std::min(od.rows, od.cols);
     k = std::max(od.rows, od.cols);
     mp = up64(m);
     kp = up64(k);
-    const size_t n = od.n, x = up256(n * 2 * m * kp * 2), t = up256(n * 2 * k * mp * 2), q = up256(n * 2 * m * mp * 2);
+    const size_t n = od.n, x = up256(n * 4 * m * kp), t = up256(n * 4 * k * mp), q = up256(n * 4 * m * mp);
     pieces = 0;
     x0 = up256(n * kNormBlocks * sizeof(double));
     t0 = x0 + x;
@@ -257,28 +397,38 @@ struct Layout {
     t1 = x1 + x;
     a = t1 + t;
     b = a + q;
-    total = b + q;
+    partial = b + q;
+    const int on = od.n, xs = static_cast<int>(kp / 32), as = static_cast<int>(mp / 32);
+    total = partial + std::max(std::max(partial_bytes(plan(on, m, m, xs, true), on, m, m, true),
+                                        partial_bytes(plan(on, m, m, as, true), on, m, m, true)),
+                               std::max(partial_bytes(plan(on, k, m, as, false), on, k, m, false),
+                                        partial_bytes(plan(on, m, k, as, false), on, m, k, false)));
   }
 };
 
-Parts parts_at(char* base, size_t at, int rows, int64_t ld) {
-  return {reinterpret_cast<uint16_t*>(base + at), rows * ld, ld, 2 * rows * ld};
+Parts parts_at(char* base, size_t at, int rows, int64_t values) {
+  return {reinterpret_cast<uint16_t*>(base + at), 2 * values, 2 * rows * values};
 }
 
-template <Mode MODE, typename OT>
+template <Mode MODE, TileParts PARTS, typename OT>
 void product(OrthArgs g, int n, hipStream_t s) {
-  constexpr bool kSym = MODE == kGram || MODE == kPoly;
-#define UMEM_ORTH(BM, WR, WC)                                                                                     \
-  {                                                                                                               \
-    g.tiles_m = (g.rows_m + BM - 1) / BM;                                                                         \
-    g.tiles_n = (g.rows_n + BM - 1) / BM;                                                                         \
-    g.items = n * (kSym ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n);                               \
-    hipLaunchKernelGGL((orth_product_kernel<MODE, OT, BM, BM, WR, WC>), dim3(tile_grid(g.items)), dim3(64 * WR * WC), \
-                       0, s, g);                                                                                  \
+  const int slices = g.k / (PARTS == kFirst ? 2 * kTileBK : kTileBK);
+  const Plan pl = plan(n, g.rows_m, g.rows_n, slices, symmetric(MODE));
+  g.splits = pl.splits;
+#define UMEM_ORTH(BM, WR, WC, BUFS)                                                                                 \
+  {                                                                                                                  \
+    g.tiles_m = (g.rows_m + BM - 1) / BM;                                                                            \
+    g.tiles_n = (g.rows_n + BM - 1) / BM;                                                                            \
+    g.per = symmetric(MODE) ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n;                               \
+    g.items = n * g.per;                                                                                             \
+    hipLaunchKernelGGL((orth_product_kernel<MODE, PARTS, OT, BM, BM, WR, WC, BUFS>),                                 \
+                       dim3(tile_grid(g.items * g.splits)), dim3(64 * WR * WC), 0, s, g);                            \
+    if (g.splits > 1)                                                                                                \
+      hipLaunchKernelGGL((orth_join_kernel<MODE, OT, BM>), dim3(g.items * (BM / 64) * (BM / 64)), dim3(kThreads), 0, \
+                         s, g);                                                                                      \
   }
-  const int64_t large = static_cast<int64_t>(n) * ((g.rows_m + 127) / 128) * ((g.rows_n + 127) / 128);
-  if (large >= 512) UMEM_ORTH(128, 2, 2)
-  else UMEM_ORTH(64, 2, 2)
+  if (pl.bm == 128) UMEM_ORTH(128, 4, 2, 4)
+  else UMEM_ORTH(64, 2, 2, 3)
 #undef UMEM_ORTH
 }
 
@@ -293,9 +443,12 @@ void first(const umem_orth_desc& od, const GT* g, double* pieces, const Parts& b
 
 }  // namespace
 
-size_t orth_workspace_bytes(const umem_orth_desc& od) { return Layout(od).total; }
+size_t orth_workspace_bytes(const umem_orth_desc& od) {
+  return std::min(od.rows, od.cols) <= kMaxOrthSmall ? orth_small_workspace_bytes(od) : Layout(od).total;
+}
 
 hipError_t launch_orthogonalize(const umem_orth_desc& od, const void* g, void* out, void* ws, hipStream_t s) {
+  if (std::min(od.rows, od.cols) <= kMaxOrthSmall) return launch_orth_small(od, g, out, ws, s);
   clear_stale_error();
   const Layout L(od);
   char* base = static_cast<char*>(ws);
@@ -309,37 +462,31 @@ hipError_t launch_orthogonalize(const umem_orth_desc& od, const void* g, void* o
   else first(od, static_cast<const __bf16*>(g), pieces, tall ? t : x, tall ? x : t, s);
   for (int step = 0; step < od.steps; ++step) {
     OrthArgs q{};
+    q.partial = reinterpret_cast<float*>(base + L.partial);
     q.a = q.b = x;                                          // A = X X^T
     q.out = a;
     q.rows_m = q.rows_n = L.m;
-    q.k = static_cast<int>(L.kp);
-    product<kGram, float>(q, od.n, s);
+    q.k = static_cast<int>(x.ld);
+    product<kGram, kBoth, float>(q, od.n, s);
     q.a = q.b = q.own = a;                                  // B = b A + c A^2
     q.out = b;
-    q.k = static_cast<int>(L.mp);
+    q.k = static_cast<int>(a.ld);
     q.alpha = od.b;
     q.beta = od.c;
-    product<kPoly, float>(q, od.n, s);
+    product<kPoly, kBoth, float>(q, od.n, s);
     q.alpha = od.a;                                         // X = a X + B X
     q.beta = 1.f;
     const bool last = step + 1 == od.steps;
-    if (!last || !tall) {                                   // m along the larger side
-      q.a = t;
-      q.b = b;
-      q.own = x;
-      q.rows_m = L.k;
-      q.rows_n = L.m;
+    const bool turned = last && tall;                       // the last X goes out as G lies
+    q.a = turned ? b : t;
+    q.b = turned ? t : b;
+    q.own = turned ? t : x;
+    q.rows_m = turned ? L.m : L.k;
+    q.rows_n = turned ? L.k : L.m;
+    if (!last) {
       q.out = x1;
       q.out_t = t1;
-    } else {
-      q.a = b;
-      q.b = t;
-      q.own = t;
-      q.rows_m = L.m;
-      q.rows_n = L.k;
-    }
-    if (!last) {
-      product<kUpdate, float>(q, od.n, s);
+      product<kUpdate, kBoth, float>(q, od.n, s);
       std::swap(x, x1);
       std::swap(t, t1);
       continue;
@@ -349,8 +496,8 @@ hipError_t launch_orthogonalize(const umem_orth_desc& od, const void* g, void* o
     q.final = out;
     q.final_ld = od.cols;
     q.final_matrix = static_cast<int64_t>(od.rows) * od.cols;
-    if (od.otype == UMEM_F32) product<kLast, float>(q, od.n, s);
-    else product<kLast, __bf16>(q, od.n, s);
+    if (od.otype == UMEM_F32) product<kLast, kBoth, float>(q, od.n, s);
+    else product<kLast, kBoth, __bf16>(q, od.n, s);
   }
   return hipGetLastError();
 }

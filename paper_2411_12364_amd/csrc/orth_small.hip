@@ -1,0 +1,268 @@
+// Newton-Schulz updates of matrices whose smaller side is at most 64.  The steps are polynomials of A_0 = X_0 X_0^T,
+// which commute, so they run on m x m matrices alone:
+//
+//   P = a I + b A + c A^2,  Q <- Q P,  A <- P A P;   out = decay out + scale Q X_0
+//
+// and X is read twice and written once, instead of 15 launches that wait for each other.  Taken so, what A_0 loses grows by a^2
+// = 12 a step where X's singular values are small: all of it is fp64 (v_mfma_f64_16x16x4), whose 2^-53 leaves nothing of
+// that to be seen.  Three launches: pieces of G G^T and with them |G|^2 (its trace), the steps, a workgroup a matrix in
+// LDS, and Q G.  Bounded by the chain of 4 small products a step: 64 x 448 in 5 steps 130 us by the large
+// matrices' products.
+#include <algorithm>
+
+#include "umem_internal.h"
+
+namespace umem {
+namespace {
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kStepThreads = 1024;
+constexpr int kSide = kMaxOrthSmall, kPitch = kSide + 2, kTilePitch = kSide + 4;
+constexpr int kMostChunks = 32;
+static_assert(kSide == 64, "16 waves of a 16 x 16 tile each");
+
+// The f64 operands' layout: lane l holds row (or column) l % 16, k = l / 16; of D row l / 16 + 4 r, column l % 16.
+__device__ __forceinline__ f64x4 mfma64(double a, double b, f64x4 c) {
+  return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0);
+}
+
+// A 64-wide slice of G's longer side into registers, and from there into LDS as [smaller side][longer side] with zeros
+// past both.
+template <typename T, bool TALL>
+struct Slice {
+  float v[16];
+  __device__ __forceinline__ void load(const T* g, int m, int64_t k, int64_t k0) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int in = threadIdx.x % 64, out = threadIdx.x / 64 + 4 * i;      // in: along G's rows
+      const int s = TALL ? in : out;
+      const int64_t l = k0 + (TALL ? out : in);
+      v[i] = s < m && l < k ? static_cast<float>(g[TALL ? l * m + s : s * k + l]) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void store(float (*t)[kTilePitch]) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int in = threadIdx.x % 64, out = threadIdx.x / 64 + 4 * i;
+      t[TALL ? in : out][TALL ? out : in] = v[i];
+    }
+  }
+};
+
+// A piece of G G^T (of G^T G where G is tall) over a chunk of the longer side, to pieces[matrix][chunk][64][64].
+template <typename T, bool TALL>
+__global__ __launch_bounds__(kThreads) void orth_small_gram_kernel(const T* __restrict__ g, int m, int k, int chunks,
+                                                                   double* __restrict__ pieces) {
+  __shared__ float t[kSide][kTilePitch];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i0 = (wave >> 1) * 32, j0 = (wave & 1) * 32;
+  const int64_t mat = blockIdx.y;
+  const T* x = g + mat * m * static_cast<int64_t>(k);
+  const int slices = (k + 63) / 64;
+  const int from = static_cast<int>(static_cast<int64_t>(slices) * blockIdx.x / chunks);
+  const int to = static_cast<int>(static_cast<int64_t>(slices) * (blockIdx.x + 1) / chunks);
+  const bool on = i0 < m && j0 < m;
+  f64x4 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = f64x4{0.0, 0.0, 0.0, 0.0};
+  Slice<T, TALL> s;
+  s.load(x, m, k, static_cast<int64_t>(from) * 64);
+  for (int c = from; c < to; ++c) {
+    __syncthreads();
+    s.store(t);
+    __syncthreads();
+    if (c + 1 < to) s.load(x, m, k, static_cast<int64_t>(c + 1) * 64);
+    if (!on) continue;
+#pragma unroll 4
+    for (int q0 = 0; q0 < 64; q0 += 4) {
+      const int q = q0 + (lane >> 4);
+      double a[2], b[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        a[i] = t[i0 + i * 16 + (lane & 15)][q];
+        b[i] = t[j0 + i * 16 + (lane & 15)][q];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mfma64(a[i], b[j], acc[i][j]);
+    }
+  }
+  double* out = pieces + (mat * chunks + blockIdx.x) * kSide * kSide;
+  if (!on) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        out[(i0 + i * 16 + (lane >> 4) + 4 * r) * kSide + j0 + j * 16 + (lane & 15)] = acc[i][j][r];
+}
+
+// The steps of one matrix: q[matrix][64][64] = Q / (|G| + eps).
+__global__ __launch_bounds__(kStepThreads) void orth_small_steps_kernel(const double* __restrict__ pieces, int m, int chunks,
+                                                                        int steps, double a, double b, double c,
+                                                                        float eps, double* __restrict__ q) {
+  __shared__ double A[kSide][kPitch], P[kSide][kPitch], Q[kSide][kPitch], T[kSide][kPitch];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i0 = (wave >> 2) * 16, j0 = (wave & 3) * 16, col = j0 + (lane & 15);
+  const int top = (m + 15) / 16 * 16;                       // rows that hold anything
+  const bool on = i0 < top && j0 < top;                     // (all waves meet the barriers)
+  const int64_t mat = blockIdx.x;
+  const double* from = pieces + mat * chunks * kSide * kSide;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = i0 + (lane >> 4) + 4 * r;
+    double v = 0.0;
+    if (on)
+      for (int p = 0; p < chunks; ++p) v += from[(static_cast<int64_t>(p) * kSide + row) * kSide + col];
+    A[row][col] = v;
+  }
+  __syncthreads();
+  double trace = lane < m ? A[lane][lane] : 0.0;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) trace += __shfl_xor(trace, off, 64);
+  const double norm = sqrt(trace) + static_cast<double>(eps);
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = i0 + (lane >> 4) + 4 * r;
+    A[row][col] = row < m && col < m ? A[row][col] / (norm * norm) : 0.0;
+  }
+  __syncthreads();
+  // a wave's tile of X Y, Y symmetric
+  const auto times = [&](double (*x)[kPitch], double (*y)[kPitch]) {
+    f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+    if (on) {
+#pragma unroll 4
+      for (int k0 = 0; k0 < top; k0 += 4) {
+        const int k = k0 + (lane >> 4);
+        acc = mfma64(x[i0 + (lane & 15)][k], y[j0 + (lane & 15)][k], acc);
+      }
+    }
+    return acc;
+  };
+  const auto put = [&](double (*x)[kPitch], const f64x4& v) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[i0 + (lane >> 4) + 4 * r][col] = v[r];
+  };
+  for (int step = 0; step < steps; ++step) {
+    f64x4 p = times(A, A);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = i0 + (lane >> 4) + 4 * r;
+      p[r] = c * p[r] + b * A[row][col] + (row == col ? a : 0.0);
+    }
+    put(P, p);
+    __syncthreads();
+    const bool last = step + 1 == steps;
+    const f64x4 t = last ? p : times(P, A);
+    const f64x4 n = step == 0 ? p : times(Q, P);
+    put(T, t);
+    __syncthreads();
+    put(Q, n);
+    if (last) break;
+    put(A, times(P, T));
+    __syncthreads();
+  }
+  // (each element by the thread that wrote it)
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = i0 + (lane >> 4) + 4 * r;
+    q[(mat * kSide + row) * kSide + col] = Q[row][col] / norm;
+  }
+}
+
+// out = decay out + scale Q G (G Q where G is tall) over 64 of the longer side, a wave 16 of them.
+template <typename GT, typename OT, bool TALL>
+__global__ __launch_bounds__(kThreads) void orth_small_apply_kernel(const GT* g, int m, int k, const double* __restrict__ q,
+                                                                    OT* out, float decay, float scale) {
+  __shared__ double Q[kSide][kPitch];
+  __shared__ float t[kSide][kTilePitch];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t mat = blockIdx.y, k0 = static_cast<int64_t>(blockIdx.x) * 64, base = mat * m * static_cast<int64_t>(k);
+  Slice<GT, TALL> s;
+  s.load(g + base, m, k, k0);
+#pragma unroll
+  for (int i = 0; i < kSide * kSide / kThreads; ++i) {
+    const int at = i * kThreads + threadIdx.x;
+    Q[at / kSide][at % kSide] = q[mat * kSide * kSide + at];
+  }
+  s.store(t);
+  __syncthreads();
+  const int tiles = (m + 15) / 16;
+  f64x4 acc[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc[i] = f64x4{0.0, 0.0, 0.0, 0.0};
+#pragma unroll 4
+  for (int j0 = 0; j0 < tiles * 16; j0 += 4) {
+    const int j = j0 + (lane >> 4);
+    const double x = t[j][wave * 16 + (lane & 15)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const double w = Q[i * 16 + (lane & 15)][j];
+      acc[i] = TALL ? mfma64(x, w, acc[i]) : mfma64(w, x, acc[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int a = (lane >> 4) + 4 * r, b = lane & 15;
+      const int small = i * 16 + (TALL ? b : a);
+      const int64_t at = k0 + wave * 16 + (TALL ? a : b);
+      if (small >= m || at >= k) continue;
+      OT* to = out + base + (TALL ? at * m + small : small * static_cast<int64_t>(k) + at);
+      double v = static_cast<double>(scale) * acc[i][r];
+      if (decay != 0.f) v = fma(static_cast<double>(decay), static_cast<double>(static_cast<float>(*to)), v);
+      *to = static_cast<OT>(static_cast<float>(v));
+    }
+}
+
+size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
+// Chunks of the longer side: few enough that adding their pieces costs little, and 1,024 workgroups at most.
+int chunk_count(const umem_orth_desc& od) {
+  const int slices = (std::max(od.rows, od.cols) + 63) / 64;
+  return std::min(slices, std::min(kMostChunks, std::max(1, 1024 / od.n)));
+}
+
+template <bool TALL, typename GT, typename OT>
+void run(const umem_orth_desc& od, const GT* g, OT* out, double* pieces, double* q, hipStream_t s) {
+  const int m = std::min(od.rows, od.cols), k = std::max(od.rows, od.cols), chunks = chunk_count(od);
+  hipLaunchKernelGGL((orth_small_gram_kernel<GT, TALL>), dim3(chunks, od.n), dim3(kThreads), 0, s, g, m, k, chunks, pieces);
+  hipLaunchKernelGGL(orth_small_steps_kernel, dim3(od.n), dim3(kStepThreads), 0, s, pieces, m, chunks, od.steps,
+                     static_cast<double>(od.a), static_cast<double>(od.b), static_cast<double>(od.c), od.eps, q);
+  hipLaunchKernelGGL((orth_small_apply_kernel<GT, OT, TALL>), dim3((k + 63) / 64, od.n), dim3(kThreads), 0, s, g, m, k, q,
+                     out, od.decay, od.scale);
+}
+
+}  // namespace
+
+size_t orth_small_workspace_bytes(const umem_orth_desc& od) {
+  return up256(static_cast<size_t>(od.n) * chunk_count(od) * kSide * kSide * sizeof(double)) +
+         static_cast<size_t>(od.n) * kSide * kSide * sizeof(double);
+}
+
+hipError_t launch_orth_small(const umem_orth_desc& od, const void* g, void* out, void* ws, hipStream_t s) {
+  clear_stale_error();
+  double* pieces = static_cast<double*>(ws);
+  double* q = reinterpret_cast<double*>(
+      static_cast<char*>(ws) + up256(static_cast<size_t>(od.n) * chunk_count(od) * kSide * kSide * sizeof(double)));
+  const auto go = [&](auto* x, auto* y) {
+    if (od.rows > od.cols) run<true>(od, x, y, pieces, q, s);
+    else run<false>(od, x, y, pieces, q, s);
+  };
+  const auto from = [&](auto* x) {
+    if (od.otype == UMEM_F32) go(x, static_cast<float*>(out));
+    else go(x, static_cast<__bf16*>(out));
+  };
+  if (od.gtype == UMEM_F32) from(static_cast<const float*>(g));
+  else from(static_cast<const __bf16*>(g));
+  return hipGetLastError();
+}
+
+}  // namespace umem

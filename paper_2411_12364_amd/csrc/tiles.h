@@ -8,13 +8,18 @@
 // that count: the loop walks the pairs one after another over the same accumulators, best from the smallest
 // products to the largest, so that these meet no more roundings than alone.
 //
+// fp16 matrices of two parts are laid out with both in a row, 32 values' first parts, then their second ones
+// (part_at): a slice then holds both parts of 32 values, and a wave takes the three products of them that count from one
+// reading of LDS, the two small ones into accumulators of their own (kBoth); or a slice holds the first parts of 64
+// values alone (kFirst).
+//
 // A workgroup takes a tile of BM x BN, its waves in WR x WC blocks of it, K in slices of 64.  What bounds such a
 // tile is the matrix cores as long as LDS feeds them: a slice of 256 x 256 x 64 takes the matrix cores 2,048
 // clocks and the LDS 1,536 (eight waves of 128 x 64 read 24 KiB each).  Slices go from memory to LDS directly
-// (16 bytes a lane), into one of two buffers while the other is read; a row's eight 16-byte pieces lie permuted by its
-// number (piece c at place c ^ (row & 7)), so that the lanes that read one piece of eight rows meet all banks.
-// The two buffers are arrays of their own: with one array the compiler cannot tell a read of one half from a
-// load into the other and waits for the load before each read.
+// (16 bytes a lane), into the buffers after the one that is read, two to four of them; a row's eight 16-byte pieces lie
+// permuted by its number (piece c at place c ^ (row & 7)), so that the lanes that read one piece of eight rows meet all
+// banks.  The buffers are arrays of their own: within one array the compiler cannot tell a read of one buffer from a
+// load into another and waits for the load before each read.
 #pragma once
 
 #include "umem_internal.h"
@@ -41,8 +46,11 @@ struct TilePairs {
   int64_t a_ld, b_ld;
 };
 
-// What a lane loads in the place of a piece past k.
-static __device__ __align__(16) const uint32_t tile_zeros[4] = {0u, 0u, 0u, 0u};
+// How k lies in a row, and what of it counts: 16-bit values one after another; both parts; the first parts only.
+enum TileParts { kPlain, kBoth, kFirst };
+// Where a row's value k has its first part (the second is 32 elements on), and the row's elements for k values.
+__host__ __device__ __forceinline__ constexpr int64_t part_at(int64_t k) { return (k >> 5) * 64 + (k & 31); }
+constexpr int kPartStep = 32;
 
 template <bool F16>
 __device__ __forceinline__ f32x4 tile_mfma(u32x4 a, u32x4 b, f32x4 c) {
@@ -53,19 +61,20 @@ __device__ __forceinline__ f32x4 tile_mfma(u32x4 a, u32x4 b, f32x4 c) {
 }
 
 typedef __attribute__((address_space(3))) uint32_t lds_u32;
-typedef const __attribute__((address_space(1))) uint32_t global_u32;
 
 // BM x BN tile of WR x WC waves; acc[a][b]: the 16 x 16 block at m = wave's row + 16 a, n = wave's column + 16 b,
 // of which lane l holds m = 4 (l / 16) + 0 .. 3, n = l % 16.
-template <bool F16, int BM, int BN, int WR, int WC>
+template <bool F16, int BM, int BN, int WR, int WC, int BUFS, TileParts PARTS = kPlain>
 struct Tile {
   static constexpr int kThreads = 64 * WR * WC;
   static constexpr int MT = BM / WR / 16, NT = BN / WC / 16;
   static constexpr int kA = BM * 8 / kThreads, kB = BN * 8 / kThreads;       // 16-byte pieces a thread loads
   static constexpr int kElems = (BM + BN) * kTileBK;                         // one buffer
+  static constexpr int kStep = PARTS == kFirst ? 2 * kTileBK : kTileBK;      // a slice's elements of a row in memory
+  static constexpr int kAccs = PARTS == kBoth ? 2 : 1;                       // sets of accumulators
   static_assert(BM * 8 % kThreads == 0 && BN * 8 % kThreads == 0, "whole pieces");
 
-  uint32_t a_off[kA], b_off[kB];          // a lane's pieces, in bytes from the slice's first
+  uint32_t a_off[kA], b_off[kB];          // a lane's pieces, in bytes from the tile's first row
   int col_k;                              // first k of the lane's pieces in a slice, the same for all of them
   int m0, n0;
 
@@ -75,112 +84,182 @@ struct Tile {
     m0 = min(m0_, p.a_rows - 1);            // (a tile past the rows that there are reads the last one)
     n0 = min(n0_, p.b_rows - 1);
     const int tid = threadIdx.x, row = tid >> 3, col = (tid & 7) ^ (row & 7);
-    col_k = col * 8;
+    col_k = PARTS == kFirst ? (col >> 2) * 64 + (col & 3) * 8 : col * 8;
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
       const int r = min(row + i * (kThreads / 8), p.a_rows - 1 - m0);
-      a_off[i] = static_cast<uint32_t>(r * static_cast<int>(p.a_ld) + col * 8) * 2u;
+      a_off[i] = static_cast<uint32_t>(r * static_cast<int>(p.a_ld) + col_k) * 2u;
     }
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
       const int r = min(row + i * (kThreads / 8), p.b_rows - 1 - n0);
-      b_off[i] = static_cast<uint32_t>(r * static_cast<int>(p.b_ld) + col * 8) * 2u;
+      b_off[i] = static_cast<uint32_t>(r * static_cast<int>(p.b_ld) + col_k) * 2u;
     }
   }
 
-  // A slice into a buffer: the tile's first row of both operands at the slice's first k, k0 of k.
-  __device__ __forceinline__ void load(const char* a, const char* b, int k0, int k, uint16_t* lds) const {
+  // The rows from `row` on, as a buffer.
+  __device__ __forceinline__ static __amdgpu_buffer_rsrc_t rows_from(const uint16_t* p, int row, int64_t ld, int rows) {
+    const int64_t bytes = (rows - row) * ld * 2;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p + row * ld), static_cast<short>(0),
+                                             static_cast<int>(bytes < 0xffffffffll ? bytes : 0xffffffffll), 0x00020000);
+  }
+
+  // The slice from k0 on into a buffer; a piece past k is another one here (past_k).
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t a, __amdgpu_buffer_rsrc_t b, int k0, int k,
+                                       uint16_t* lds) const {
     const int wave = threadIdx.x >> 6;
-    const bool tail = k0 + kTileBK > k;
-    if (!tail) {
+    uint32_t back = 0;
+    if (PARTS == kPlain && k0 + kTileBK > k && k0 + col_k >= k) back = static_cast<uint32_t>(col_k) * 2u;
 #pragma unroll
-      for (int i = 0; i < kA; ++i)
-        __builtin_amdgcn_global_load_lds((global_u32*)(a + a_off[i]),
-                                         (lds_u32*)(lds + (i * kThreads + wave * 64) * 8), 16, 0, 0);
+    for (int i = 0; i < kA; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(a, (lds_u32*)(lds + (i * kThreads + wave * 64) * 8), 16, a_off[i] - back,
+                                               k0 * 2, 0, 0);
 #pragma unroll
-      for (int i = 0; i < kB; ++i)
-        __builtin_amdgcn_global_load_lds((global_u32*)(b + b_off[i]),
-                                         (lds_u32*)(lds + BM * kTileBK + (i * kThreads + wave * 64) * 8), 16, 0, 0);
-    } else {
-      const bool in = k0 + col_k < k;
-      const char* z = reinterpret_cast<const char*>(tile_zeros);
-#pragma unroll
-      for (int i = 0; i < kA; ++i)
-        __builtin_amdgcn_global_load_lds((global_u32*)(in ? a + a_off[i] : z),
-                                         (lds_u32*)(lds + (i * kThreads + wave * 64) * 8), 16, 0, 0);
-#pragma unroll
-      for (int i = 0; i < kB; ++i)
-        __builtin_amdgcn_global_load_lds((global_u32*)(in ? b + b_off[i] : z),
-                                         (lds_u32*)(lds + BM * kTileBK + (i * kThreads + wave * 64) * 8), 16, 0, 0);
-    }
+    for (int i = 0; i < kB; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_u32*)(lds + BM * kTileBK + (i * kThreads + wave * 64) * 8), 16,
+                                               b_off[i] - back, k0 * 2, 0, 0);
   }
 
-  __device__ __forceinline__ static void compute(const uint16_t* lds, f32x4 (&acc)[MT][NT]) {
+  // The lane's pieces past k, once they have landed, to zeros.  (Rows of parts are whole slices.)
+  __device__ __forceinline__ void past_k(int k0, int k, uint16_t* lds) const {
+    if (PARTS != kPlain || k0 + kTileBK <= k) return;
+    if (k0 + col_k >= k) {
+#pragma unroll
+      for (int i = 0; i < kA + kB; ++i) {
+        uint16_t* piece = lds + (i < kA ? 0 : BM * kTileBK) + ((i < kA ? i : i - kA) * kThreads + threadIdx.x) * 8;
+        *reinterpret_cast<u32x4*>(piece) = u32x4{0u, 0u, 0u, 0u};
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);                     // lgkmcnt alone
+  }
+
+  __device__ __forceinline__ static void compute(const uint16_t* lds, f32x4 (&acc)[kAccs][MT][NT]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wr = wave / WC, wc = wave % WC;
     const int r = lane & 15, q = lane >> 4;
     const uint16_t* a = lds + (wr * MT * 16 + r) * kTileBK;
     const uint16_t* b = lds + BM * kTileBK + (wc * NT * 16 + r) * kTileBK;
+    const int at0 = (q ^ (r & 7)) * 8, at1 = ((4 + q) ^ (r & 7)) * 8;
+    if constexpr (PARTS == kBoth) {
+      u32x4 a0[MT], a1[MT], b0[NT], b1[NT];
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      const int at = ((kk * 4 + q) ^ (r & 7)) * 8;
-      u32x4 af[MT], bf[NT];
+      for (int i = 0; i < NT; ++i) b0[i] = *reinterpret_cast<const u32x4*>(b + i * 16 * kTileBK + at0);
 #pragma unroll
-      for (int i = 0; i < NT; ++i) bf[i] = *reinterpret_cast<const u32x4*>(b + i * 16 * kTileBK + at);
+      for (int i = 0; i < MT; ++i) a0[i] = *reinterpret_cast<const u32x4*>(a + i * 16 * kTileBK + at0);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) af[i] = *reinterpret_cast<const u32x4*>(a + i * 16 * kTileBK + at);
+      for (int i = 0; i < NT; ++i) b1[i] = *reinterpret_cast<const u32x4*>(b + i * 16 * kTileBK + at1);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a1[i] = *reinterpret_cast<const u32x4*>(a + i * 16 * kTileBK + at1);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = tile_mfma<F16>(af[i], bf[j], acc[i][j]);
+        for (int j = 0; j < NT; ++j) acc[0][i][j] = tile_mfma<F16>(a0[i], b0[j], acc[0][i][j]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[1][i][j] = tile_mfma<F16>(a0[i], b1[j], acc[1][i][j]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[1][i][j] = tile_mfma<F16>(a1[i], b0[j], acc[1][i][j]);
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const int at = kk ? at1 : at0;
+        u32x4 af[MT], bf[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) bf[i] = *reinterpret_cast<const u32x4*>(b + i * 16 * kTileBK + at);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) af[i] = *reinterpret_cast<const u32x4*>(a + i * 16 * kTileBK + at);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[0][i][j] = tile_mfma<F16>(af[i], bf[j], acc[0][i][j]);
+      }
     }
   }
 
-  // Waits until the loads into LDS of all waves have landed and all have read the other buffer.
-  __device__ __forceinline__ static void landed() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+  // Waits until a wave's loads but for those of the last LATER slices have landed, and until all waves have come here:
+  // the slice, at k0 of k in `lds`, is whole, and the buffer before it has been read by everyone.  (A fence would wait
+  // for all loads.)
+  template <int LATER>
+  __device__ __forceinline__ void landed(int k0, int k, uint16_t* lds) const {
+    constexpr int kLoads = LATER * (kA + kB);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((kLoads & 15) | (kLoads >> 4) << 14 | 0x0f70);          // vmcnt alone
+    past_k(k0, k, lds);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   }
 
-  // The product over the slices [from, to) of the pairs' slices laid one after another (ceil(k / 64) each).
+  // The slices of p's pairs laid one after another.
+  __device__ __forceinline__ static int slices(const TilePairs& p) { return p.n * ((p.k + kStep - 1) / kStep); }
+
+  // The product over the slices [from, to) of them, to > from, through BUFS buffers.  Past the last slice that one is
+  // loaded again, and the loop has one end: with loads that may or may not be there, and with an exit in its midst, the
+  // compiler waits for all loads before a read.  All loads have landed when this returns; all waves have read the last
+  // slice only after a barrier.
   __device__ __forceinline__ void run(const TilePairs& p, int from, int to, uint16_t* buf0, uint16_t* buf1,
-                                      f32x4 (&acc)[MT][NT]) const {
+                                      uint16_t* buf2, uint16_t* buf3, f32x4 (&out)[MT][NT]) const {
+    uint16_t* const bufs[4] = {buf0, buf1, buf2, buf3};
+    static_assert(BUFS >= 2 && BUFS <= 4 && (BUFS - 2) * (kA + kB) < 64, "what vmcnt counts");
+    f32x4 acc[kAccs][MT][NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int s = 0; s < kAccs; ++s)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int per = (p.k + kTileBK - 1) / kTileBK;
-    const int k = p.k;
-    int s = from / per, k0 = (from - s * per) * kTileBK;
-    const char *a = nullptr, *b = nullptr;
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[s][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int k = p.k, per = (k + kStep - 1) / kStep;
+    int s = from / per, k0 = (from - s * per) * kStep;      // the next slice to load
+    int at = k0;                                            // where in k the next slice to compute lies
+    int left = to - from, ahead = left;                     // slices to compute, to load
+    const uint16_t *pa = nullptr, *pb = nullptr;
     const auto point = [&] {
-      a = reinterpret_cast<const char*>(p.a[s] + m0 * p.a_ld + k0);
-      b = reinterpret_cast<const char*>(p.b[s] + n0 * p.b_ld + k0);
+      pa = p.a[0];
+      pb = p.b[0];
+#pragma unroll
+      for (int i = 1; i < kMaxPairs; ++i) {
+        pa = p.n > 1 && s == i ? p.a[i] : pa;
+        pb = p.n > 1 && s == i ? p.b[i] : pb;
+      }
     };
-    const auto next = [&] {
-      k0 += kTileBK;
-      a += kTileBK * 2;
-      b += kTileBK * 2;
+    const auto fetch = [&](uint16_t* buf) {
+      load(rows_from(pa, m0, p.a_ld, p.a_rows), rows_from(pb, n0, p.b_ld, p.b_rows), k0, k, buf);
+      if (--ahead <= 0) return;
+      k0 += kStep;
       if (k0 >= k) {
         k0 = 0;
-        if (++s < p.n) point();
+        ++s;
+        point();
       }
     };
     point();
-    load(a, b, k0, k, buf0);
-    int left = to - from;
-    while (true) {
-      landed();
-      next();
-      if (left > 1) load(a, b, k0, k, buf1);
-      compute(buf0, acc);
-      if (--left == 0) break;
-      landed();
-      next();
-      if (left > 1) load(a, b, k0, k, buf0);
-      compute(buf1, acc);
-      if (--left == 0) break;
+#pragma unroll
+    for (int i = 0; i < BUFS - 1; ++i) fetch(bufs[i]);
+    for (; left >= BUFS; left -= BUFS) {
+#pragma unroll
+      for (int i = 0; i < BUFS; ++i) {
+        landed<BUFS - 2>(at, k, bufs[i]);                   // in flight: the BUFS - 2 slices after this one
+        at = at + kStep >= k ? 0 : at + kStep;
+        fetch(bufs[(i + BUFS - 1) % BUFS]);
+        compute(bufs[i], acc);
+      }
     }
+    // the last slices, fewer than the buffers, are all there or on their way
+#pragma unroll
+    for (int i = 0; i < BUFS - 1; ++i) {
+      if (i < left) {
+        landed<0>(at, k, bufs[i]);
+        at = at + kStep >= k ? 0 : at + kStep;
+        compute(bufs[i], acc);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) out[i][j] = kAccs == 2 ? acc[0][i][j] + acc[kAccs - 1][i][j] : acc[0][i][j];
   }
 };
 

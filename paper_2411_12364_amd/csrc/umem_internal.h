@@ -201,6 +201,10 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
 // Orthogonalised updates (orth.hip).
 constexpr int kMaxOrthSide = 1 << 16, kMaxOrthSteps = 16, kMaxOrthBatch = 65535;
 constexpr int64_t kMaxOrthElements = INT64_C(1) << 33;
+// A smaller side of at most kMaxOrthSmall goes by orth_small.hip, others by orth.hip.
+constexpr int kMaxOrthSmall = 64;
+size_t orth_small_workspace_bytes(const umem_orth_desc& od);
+hipError_t launch_orth_small(const umem_orth_desc& od, const void* g, void* out, void* ws, hipStream_t s);
 size_t orth_workspace_bytes(const umem_orth_desc& od);
 hipError_t launch_orthogonalize(const umem_orth_desc& od, const void* g, void* out, void* ws, hipStream_t s);
 
