@@ -11,11 +11,14 @@
 // W are laid out transposed beforehand).  Bounded by the matrix cores: 2 T V d operations forward, 6 T V d backward, but
 // for few tokens, where W is read once at the rate of the memory.
 //
-// Rounding: logits and sums are fp32 of bf16 operands; fp32 x is three bf16 parts, which hold it whole.  r enters its
-// products as one bf16 part where the result is bf16 (both roundings are of the result's own size), and as
-// three, which hold it whole, where the result is fp32.  r is made for losses' gradients of at most 1, and the largest of
-// them and s are multiplied in last, in fp32: the gradient of a mean has one value for all tokens, and a target's
-// r of nearly that value times -s would be rounded the same way for all of them.
+// Rounding: logits and sums are fp32 of bf16 operands; fp32 x is three bf16 parts, which hold it whole.  r is made for
+// losses' gradients of at most 1, and the largest of them and s are multiplied in last, in fp32: the gradient of a
+// mean has one value for all tokens, and a target's r of nearly that value times -s would be rounded the same way
+// for all of them.  For dx r is bf16 beside W: one part where dx is bf16 (both roundings are of the result's own
+// size), three, which hold it whole, where it is fp32.  For dW r and x are fp16, r times 2^15 and x times the power
+// of two that takes its largest value to that: a bf16 x down to 2^-32 of the largest is held whole, and r as
+// one part (2^-12 of it, and 2^-40 of the largest dloss) where dW is bf16, as two (22 bits) where it is fp32, as fp32 x is then.
+// (Three bf16 parts of r hold it as well, at half more time: 8,192 tokens by 7,168 rows of 2,048 560 us, so 370.)
 #include <algorithm>
 
 #include "tiles.h"
@@ -59,23 +62,93 @@ __global__ __launch_bounds__(kThreads) void head_split_kernel(const float* __res
     *reinterpret_cast<u32x2*>(parts + k * n + i) = u32x2{p[0][k] | p[1][k] << 16, p[2][k] | p[3][k] << 16};
 }
 
-// in [rows, cols] (cols a multiple of 8) to out [parts][cols][ld], zeros from `rows` on and in the place of rows whose
-// target is none (0 times what is no number would reach the others' sums).
+// The maxima of kMostBlocks fixed ranges, for a wave of each consumer to take the largest of.
+constexpr int kMostBlocks = 64;
+static_assert(kMostBlocks == kWave, "a lane each");
+
+__device__ __forceinline__ float wave_most(float m) {
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+  return m;
+}
+__device__ __forceinline__ void put_most(float m, float* most) {
+  __shared__ float waves[16];
+  m = wave_most(m);
+  if ((threadIdx.x & (kWave - 1)) == 0) waves[threadIdx.x / kWave] = m;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < static_cast<int>(blockDim.x) / kWave; ++w) m = fmaxf(m, waves[w]);
+  most[blockIdx.x] = m;
+}
+
+__device__ __forceinline__ bool counts(const int32_t* targets, int t, int vocab) {
+  return static_cast<uint32_t>(targets[t]) < static_cast<uint32_t>(vocab);
+}
+
+// The largest finite |x| of the tokens that count; a workgroup walks rows.
+template <typename T>
+__global__ __launch_bounds__(1024) void head_most_x_kernel(const T* __restrict__ x, const int32_t* __restrict__ targets,
+                                                           int tokens, int d, int vocab, float* __restrict__ most) {
+  typedef T eight __attribute__((ext_vector_type(8)));
+  const int64_t pieces = static_cast<int64_t>(tokens) * (d / 8);
+  float m = 0.f;
+#pragma unroll 4
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 1024 + threadIdx.x; i < pieces; i += kMostBlocks * 1024) {
+    const eight v = *reinterpret_cast<const eight*>(x + i * 8);
+    float most8 = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float a = fabsf(static_cast<float>(v[j]));
+      most8 = a < INFINITY ? fmaxf(most8, a) : most8;
+    }
+    if (most8 > m && counts(targets, static_cast<int>(i / (d / 8)), vocab)) m = most8;
+  }
+  put_most(m, most);
+}
+
+// The power of two that x is multiplied by: it takes the largest to between 2^14 and 2^15.
+__device__ __forceinline__ int x_shift(const float* most) {
+  const float m = wave_most(most[threadIdx.x & (kWave - 1)]);
+  int e = 0;
+  frexpf(m, &e);
+  return m > 0.f ? min(max(15 - e, -110), 110) : 0;
+}
+
+// Part i of a value as fp16 parts; what is past the first part of a value that is infinite or none is zero.
+__device__ __forceinline__ uint32_t f16_part(float x, int i) {
+  const _Float16 hi = static_cast<_Float16>(x);
+  if (i == 0) return __builtin_bit_cast(uint16_t, hi);
+  const float v = static_cast<float>(hi);
+  return fabsf(v) < INFINITY ? __builtin_bit_cast(uint16_t, static_cast<_Float16>(x - v)) : 0u;
+}
+
+// in [rows, cols] (cols a multiple of 8) to out [parts][cols][ld], zeros from `rows` on.  With `most` as fp16 parts of the
+// shifted values, and zeros in the place of rows whose target is none (0 times what is no number would reach the
+// others' sums); without as the bits they are.
 template <typename T, int PARTS>
 __global__ __launch_bounds__(kThreads) void head_transpose_kernel(const T* __restrict__ in, int rows, int cols,
                                                                   uint16_t* __restrict__ out, int64_t ld,
+                                                                  const float* __restrict__ most,
                                                                   const int32_t* __restrict__ targets, int vocab) {
   __shared__ uint16_t tile[PARTS][64][66];
   const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+  const int shift = most ? x_shift(most) : 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int r = r0 + i * 4 + threadIdx.x / 64, c = c0 + threadIdx.x % 64;
-    bool on = r < rows && c < cols;
-    if (on && targets) on = static_cast<uint32_t>(targets[r]) < static_cast<uint32_t>(vocab);
+    const bool on = r < rows && c < cols && (targets == nullptr || counts(targets, r, vocab));
     uint32_t p[PARTS] = {};
     if (on) {
-      if constexpr (sizeof(T) == 4) bf16_parts(static_cast<float>(in[static_cast<int64_t>(r) * cols + c]), p);
-      else p[0] = in[static_cast<int64_t>(r) * cols + c];
+      const T v = in[static_cast<int64_t>(r) * cols + c];
+      if (most) {
+        float x;
+        if constexpr (sizeof(T) == 4) x = ldexpf(v, shift);
+        else x = ldexpf(bits_f32(v), shift);
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) p[k] = f16_part(x, k);
+      } else if constexpr (sizeof(T) == 2) {
+        p[0] = v;
+      }
     }
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) tile[k][threadIdx.x % 64][i * 4 + threadIdx.x / 64] = static_cast<uint16_t>(p[k]);
@@ -185,44 +258,80 @@ __global__ __launch_bounds__(kThreads) void head_join_kernel(const float2* __res
   for (int i = 0; i < 16; ++i) sum += sums[i][n];
   const double all = top + log(sum);
   lse[t] = static_cast<float>(all);
-  loss[t] = static_cast<uint32_t>(targets[t]) < static_cast<uint32_t>(vocab) ? static_cast<float>(all - goal[t]) : 0.f;
+  loss[t] = counts(targets, t, vocab) ? static_cast<float>(all - goal[t]) : 0.f;
+}
+
+// The same with a workgroup a token, for few tokens.
+__global__ __launch_bounds__(kThreads) void head_join_few_kernel(const float2* __restrict__ stats,
+                                                                 const float* __restrict__ goal,
+                                                                 const int32_t* __restrict__ targets, int T, int vocab,
+                                                                 int tiles, float* __restrict__ loss,
+                                                                 float* __restrict__ lse) {
+  __shared__ float tops[kThreads / kWave];
+  __shared__ double sums[kThreads / kWave];
+  const int t = blockIdx.x, wave = threadIdx.x / kWave;
+  constexpr int kHeld = 8;                                  // pairs a thread holds while the maximum is found
+  float2 held[kHeld];
+  float top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = threadIdx.x + j * kThreads;
+    held[j] = i < tiles ? stats[static_cast<int64_t>(i) * T + t] : float2{-INFINITY, 0.f};
+    top = fmaxf(top, held[j].x);
+  }
+  for (int i = threadIdx.x + kHeld * kThreads; i < tiles; i += kThreads)
+    top = fmaxf(top, stats[static_cast<int64_t>(i) * T + t].x);
+  top = wave_most(top);
+  if ((threadIdx.x & (kWave - 1)) == 0) tops[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / kWave; ++w) top = fmaxf(top, tops[w]);
+  double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (static_cast<int>(threadIdx.x) + j * kThreads < tiles) sum += held[j].y * exp(static_cast<double>(held[j].x) - top);
+  for (int i = threadIdx.x + kHeld * kThreads; i < tiles; i += kThreads) {
+    const float2 s = stats[static_cast<int64_t>(i) * T + t];
+    sum += s.y * exp(static_cast<double>(s.x) - top);
+  }
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+  if ((threadIdx.x & (kWave - 1)) == 0) sums[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (int w = 1; w < kThreads / kWave; ++w) sum += sums[w];
+  const double all = top + log(sum);
+  lse[t] = static_cast<float>(all);
+  loss[t] = counts(targets, t, vocab) ? static_cast<float>(all - goal[t]) : 0.f;
 }
 
 // ---------------------------------------------------------------- backward
 
-// The largest |dloss| of the tokens that count, as kMostBlocks maxima over fixed ranges.
-constexpr int kMostBlocks = 64;
-
+// The largest |dloss| of the tokens that count.
 __global__ __launch_bounds__(kThreads) void head_most_kernel(const float* __restrict__ dloss,
                                                              const int32_t* __restrict__ targets, int T, int vocab,
                                                              float* __restrict__ most) {
-  __shared__ float waves[kThreads / kWave];
   float m = 0.f;
   for (int t = blockIdx.x * kThreads + threadIdx.x; t < T; t += kMostBlocks * kThreads)
-    if (static_cast<uint32_t>(targets[t]) < static_cast<uint32_t>(vocab)) m = fmaxf(m, fabsf(dloss[t]));
-#pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
-  if ((threadIdx.x & (kWave - 1)) == 0) waves[threadIdx.x / kWave] = m;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-#pragma unroll
-  for (int w = 1; w < kThreads / kWave; ++w) m = fmaxf(m, waves[w]);
-  most[blockIdx.x] = m;
+    if (counts(targets, t, vocab)) m = fmaxf(m, fabsf(dloss[t]));
+  put_most(m, most);
 }
 
 // The largest of them; 1 without any, or where it is no finite number above 0.
 __device__ __forceinline__ float most_of(const float* most) {
   if (most == nullptr) return 1.f;
-  float m = most[threadIdx.x & (kWave - 1)];
-#pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, kWave));
+  const float m = wave_most(most[threadIdx.x & (kWave - 1)]);
   return m > 0.f && m < INFINITY ? m : 1.f;
 }
-static_assert(kMostBlocks == kWave, "a lane each");
 
-// r of a piece of the vocabulary, over s and the largest dloss, in bf16 parts: rows[part][T][piece] and cols[part][piece][t_pad], zeros past the piece's rows
-// of W, past T and for tokens without a target.  The tile goes through LDS, [token][v], its 16-byte
-// pieces permuted by the token's number so that both orders of reading meet all banks.
+// r of a piece of the vocabulary, over s and the largest dloss: rows[part][T][piece] in PR bf16 parts, and times 2^15
+// cols[part][piece][t_pad] in PC fp16 parts; zeros past the piece's rows of W, past T and for tokens without a target.
+// A part at a time goes through LDS, [token][v], its 16-byte pieces permuted by the token's number so that
+// both orders of reading meet all banks.  (Parts kept from one to the next spill 360 registers: 430 us of 620 were the
+// end of a tile.)
+constexpr float kSlopeUp = 32768.f;
+
 template <int BM, int BN, int WR, int WC, int PR, int PC>
 __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
                                                                  const int32_t* __restrict__ targets,
@@ -264,9 +373,10 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
   // token n's first element; a 16-byte piece of it is at place (piece ^ turn(n)) of the 8 in its group
   const auto row_at = [&](int n) { return (n < BN / 2 ? buf0 : buf1) + (n % (BN / 2)) * BM; };
   const auto turn = [](int n) { return (n ^ (n >> 3)) & 7; };
-  constexpr int kParts = PR > PC ? PR : PC;
-#pragma unroll
-  for (int part = 0; part < kParts; ++part) {
+#pragma unroll 1
+  for (int pass = 0; pass < PR + PC; ++pass) {
+    const bool by_rows = pass < PR;
+    const int part = by_rows ? pass : pass - PR;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < Tl::NT; ++j)
@@ -276,26 +386,34 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
         uint32_t b[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          b[r] = bf16_bits(acc[i][j][r]);
-          const float v = bits_f32(b[r]);
-          acc[i][j][r] = fabsf(v) <= 3.4e38f ? acc[i][j][r] - v : 0.f;
+          if (by_rows) {
+            uint32_t parts[PR];
+            bf16_parts(acc[i][j][r], parts);
+            b[r] = parts[0];
+#pragma unroll
+            for (int k = 1; k < PR; ++k) b[r] = part == k ? parts[k] : b[r];
+          } else {
+            b[r] = f16_part(acc[i][j][r] * kSlopeUp, 0);
+            if (PC > 1 && part > 0) b[r] = f16_part(acc[i][j][r] * kSlopeUp, 1);
+          }
         }
         *reinterpret_cast<u32x2*>(row_at(n) + (((m >> 3) ^ turn(n)) << 3) + (m & 7)) =
             u32x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
       }
     __syncthreads();
-    if (part < PR) {
+    if (by_rows) {
       uint16_t* to = rows + static_cast<int64_t>(part) * T * piece;
+#pragma unroll 4
       for (int i = threadIdx.x; i < BN * (BM / 8); i += Tl::kThreads) {
         const int n = i / (BM / 8), c = i % (BM / 8), t = at.n * BN + n, v = at.m * BM + c * 8;
         if (t < T && v < piece)
           *reinterpret_cast<u32x4*>(to + static_cast<int64_t>(t) * piece + v) =
               *reinterpret_cast<const u32x4*>(row_at(n) + ((c ^ turn(n)) << 3));
       }
-    }
-    if (part < PC) {
+    } else {
       uint16_t* to = cols + static_cast<int64_t>(part) * piece * t_pad;
       // eight lanes to a row of eight 16-byte pieces (64 tokens), eight rows of W to a wave
+#pragma unroll 2
       for (int i = threadIdx.x; i < BM * (BN / 8); i += Tl::kThreads) {
         const int group = i / 64, m = (group % (BM / 8)) * 8 + (i & 7), n8 = (group / (BM / 8)) * 64 + ((i >> 3) & 7) * 8;
         const int t = at.n * BN + n8, v = at.m * BM + m;
@@ -310,45 +428,94 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
   }
 }
 
-// A product whose m lies along the rows of the output, [n][m] of ld: out = D scale (the largest dloss) + before (each
-// where it is given).  Rows n whose entry of targets is not in [0, vocab) become zeros.
-template <typename OT, int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(64 * WR * WC) void head_product_kernel(TilePairs p, int tiles_m, int tiles_n,
-                                                                   const float* before, OT* out, int64_t ld, float scale,
-                                                                   const float* __restrict__ most,
-                                                                   const int32_t* __restrict__ targets, int vocab) {
-  typedef Tile<false, BM, BN, WR, WC, 2> Tl;
+// A product whose m lies along the rows of the output, [n][m] of ld.  Of one split of k: out = (D + before) f (dx) or
+// D f + before (dW: whole = false), each without `before` where it is not given, f = scale times the largest dloss, and of
+// shifted operands (x_most) what takes their shifts back; rows n whose entry of targets is none become zeros.  Of
+// several, split i's D is added to sums[i], or written there where first is set.
+struct ProductArgs {
+  int tiles_m, tiles_n, splits;
+  float *sums, *before;
+  bool first, whole;
+  void* out;
+  int64_t ld;
+  float scale;
+  const float *most, *x_most;
+  const int32_t* targets;
+  int vocab;
+};
+
+// f of the output.
+__device__ __forceinline__ float product_factor(const ProductArgs& g) {
+  const float f = g.scale * most_of(g.most);
+  return g.x_most ? f * (1.f / kSlopeUp) : f;
+}
+
+template <bool F16, typename OT, int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void head_product_kernel(TilePairs p, ProductArgs g) {
+  typedef Tile<F16, BM, BN, WR, WC, 2> Tl;
   __shared__ __align__(16) uint16_t buf0[Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[Tl::kElems];
-  const int item = tile_item(tiles_m * tiles_n);
-  if (item >= tiles_m * tiles_n) return;
-  const TilePlace at = tile_place(item, tiles_m, tiles_n);
+  const int tiles = g.tiles_m * g.tiles_n, id = tile_item(tiles * g.splits);
+  if (id >= tiles * g.splits) return;
+  const int split = id / tiles;
+  const TilePlace at = tile_place(id - split * tiles, g.tiles_m, g.tiles_n);
   Tl tile;
   tile.init(p, at.m * BM, at.n * BN);
   f32x4 acc[Tl::MT][Tl::NT];
-  tile.run(p, 0, Tl::slices(p), buf0, buf1, nullptr, nullptr, acc);
+  const int64_t slices = Tl::slices(p);
+  tile.run(p, static_cast<int>(slices * split / g.splits), static_cast<int>(slices * (split + 1) / g.splits), buf0, buf1,
+           nullptr, nullptr, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
-  const float largest = most_of(most);
+  const float f = product_factor(g);
+  const int back = g.x_most ? -x_shift(g.x_most) : 0;
 #pragma unroll
   for (int j = 0; j < Tl::NT; ++j) {
     const int n = at.n * BN + (wc * Tl::NT + j) * 16 + (lane & 15);
     if (n >= p.b_rows) continue;
-    const bool off = targets && static_cast<uint32_t>(targets[n]) >= static_cast<uint32_t>(vocab);
+    const bool off = g.targets && !counts(g.targets, n, g.vocab);
 #pragma unroll
     for (int i = 0; i < Tl::MT; ++i) {
       const int m = at.m * BM + (wr * Tl::MT + i) * 16 + 4 * (lane >> 4);
       if (m >= p.a_rows) continue;
-      const int64_t o = n * ld + m;
-      f32x4 v = acc[i][j] * scale * largest;
-      if (before) v += *reinterpret_cast<const f32x4*>(before + o);
+      const int64_t o = n * g.ld + m;
+      f32x4 v = acc[i][j];
+      if (g.splits > 1) {
+        float* sum = g.sums + split * (p.b_rows * g.ld) + o;
+        if (!g.first) v += *reinterpret_cast<const f32x4*>(sum);
+        *reinterpret_cast<f32x4*>(sum) = v;
+        continue;
+      }
+      if (g.whole && g.before) v += *reinterpret_cast<const f32x4*>(g.before + o);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], back) * f;
+      if (!g.whole && g.before) v += *reinterpret_cast<const f32x4*>(g.before + o);
       if (off) v = f32x4{0.f, 0.f, 0.f, 0.f};
+      OT* out = static_cast<OT*>(g.out) + o;
       if constexpr (sizeof(OT) == 4)
-        *reinterpret_cast<f32x4*>(out + o) = v;
+        *reinterpret_cast<f32x4*>(out) = v;
       else
-        *reinterpret_cast<u32x2*>(out + o) =
+        *reinterpret_cast<u32x2*>(out) =
             u32x2{bf16_bits(v.x) | bf16_bits(v.y) << 16, bf16_bits(v.z) | bf16_bits(v.w) << 16};
     }
   }
+}
+
+// dx from the splits' sums, in their order.
+template <typename OT>
+__global__ __launch_bounds__(kThreads) void head_sum_kernel(ProductArgs g, int T, int d) {
+  const float f = product_factor(g);
+  const int64_t size = static_cast<int64_t>(T) * d;
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
+  if (i >= size) return;
+  f32x4 v = *reinterpret_cast<const f32x4*>(g.sums + i);
+  for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(g.sums + s * size + i);
+  v *= f;
+  if (!counts(g.targets, static_cast<int>(i / d), g.vocab)) v = f32x4{0.f, 0.f, 0.f, 0.f};
+  OT* out = static_cast<OT*>(g.out) + i;
+  if constexpr (sizeof(OT) == 4)
+    *reinterpret_cast<f32x4*>(out) = v;
+  else
+    *reinterpret_cast<u32x2*>(out) = u32x2{bf16_bits(v.x) | bf16_bits(v.y) << 16, bf16_bits(v.z) | bf16_bits(v.w) << 16};
 }
 
 // ---------------------------------------------------------------- host
@@ -362,7 +529,8 @@ bool large_tiles(int m, int n) { return m > 128 && n > kSmallTokens; }
 
 int x_parts(const umem_head_desc& hd) { return hd.xtype == UMEM_F32 ? 3 : 1; }
 int row_parts(const umem_head_desc& hd) { return hd.xtype == UMEM_F32 ? 3 : 1; }       // of r, for dx
-int col_parts(const umem_head_desc& hd) { return hd.gtype == UMEM_F32 ? 3 : 1; }       // of r, for dW
+int col_parts(const umem_head_desc& hd) { return hd.gtype == UMEM_F32 ? 2 : 1; }       // of r, for dW
+int x_col_parts(const umem_head_desc& hd) { return hd.xtype == UMEM_F32 && hd.gtype == UMEM_F32 ? 2 : 1; }
 
 // Rows of the vocabulary in a piece of the backward.  r's scratch holds 2^26 values of a part in each order at most (from
 // 2^18 tokens on 256 rows of every token), W's transposed piece 2^14 rows.
@@ -378,9 +546,24 @@ int piece_rows(const umem_head_desc& hd, int T) {
   return static_cast<int>(up((hd.vocab + pieces - 1) / pieces, 256));
 }
 
+// How often k of dx's product is split: to fill the chip where its tiles are few.  (Their sums' values: tiles of 256 x 256
+// that are split are 128 at most, of all splits 256; those of 64 x 64 are smaller.)
+constexpr int kMostSplits = 8, kLargeWorkgroups = 256, kSmallWorkgroups = 768;
+int dx_splits(const umem_head_desc& hd, int T) {
+  const bool large = large_tiles(hd.d, T);
+  const int side = large ? 256 : 64;
+  const int64_t tiles = (up(hd.d, side) / side) * (up(T, side) / side);
+  const int64_t most = std::min<int64_t>(kMostSplits, piece_rows(hd, T) * row_parts(hd) / 512);
+  return static_cast<int>(std::max<int64_t>(1, std::min(most, (large ? kLargeWorkgroups : kSmallWorkgroups) / tiles)));
+}
+size_t sum_values(const umem_head_desc& hd, int T) {
+  const size_t x = static_cast<size_t>(T) * hd.d;
+  return std::max(x, std::min(kMostSplits * x, static_cast<size_t>(kLargeWorkgroups) * 256 * 256));
+}
+
 // The forward goes by bands of tokens, so that its scratch and its grids are bounded; a workspace for T tokens holds what
 // the small tiles of fewer need.
-constexpr int kBandTokens = 1 << 15;
+constexpr int kBandTokens = 1 << 15, kFewTokens = 512;
 struct ForwardLayout {
   size_t parts, stats, goal, total;
   ForwardLayout(const umem_head_desc& hd, int T) {
@@ -392,17 +575,18 @@ struct ForwardLayout {
   }
 };
 struct BackwardLayout {
-  size_t parts, xt, wt, rows, cols, sum, most, total;
+  size_t parts, xt, wt, rows, cols, sum, most, x_most, total;
   BackwardLayout(const umem_head_desc& hd, int T) {
     const size_t t = T, tp = up(T, 64), d = hd.d, values = piece_values(hd, T);
     parts = 0;
     xt = up256(hd.xtype == UMEM_F32 ? 3 * t * d * 2 : 0);
-    wt = xt + up256(x_parts(hd) * d * tp * 2);
+    wt = xt + up256(x_col_parts(hd) * d * tp * 2);
     rows = wt + up256(d * most_piece(hd) * 2);
     cols = rows + up256(row_parts(hd) * values * 2);
     sum = cols + up256(col_parts(hd) * values * 2);
-    most = sum + up256(t * d * sizeof(float));
-    total = most + up256(kMostBlocks * sizeof(float));
+    most = sum + up256(sum_values(hd, T) * sizeof(float));
+    x_most = most + up256(kMostBlocks * sizeof(float));
+    total = x_most + up256(kMostBlocks * sizeof(float));
   }
 };
 
@@ -427,14 +611,14 @@ void split_x(const umem_head_desc& hd, int T, const void* x, uint16_t* parts, hi
                      static_cast<const float*>(x), parts, n);
 }
 
-template <typename OT>
-void product(const TilePairs& p, const float* before, OT* out, int64_t ld, float scale, const float* most,
-             const int32_t* targets, int vocab, hipStream_t s) {
-#define UMEM_PRODUCT(BM, BN, WR, WC)                                                                              \
-  {                                                                                                               \
-    const int tm = (p.a_rows + BM - 1) / BM, tn = (p.b_rows + BN - 1) / BN;                                       \
-    hipLaunchKernelGGL((head_product_kernel<OT, BM, BN, WR, WC>), dim3(tile_grid(tm * tn)), dim3(64 * WR * WC), 0, \
-                       s, p, tm, tn, before, out, ld, scale, most, targets, vocab);                                            \
+template <bool F16, typename OT>
+void product(const TilePairs& p, ProductArgs g, hipStream_t s) {
+#define UMEM_PRODUCT(BM, BN, WR, WC)                                                                            \
+  {                                                                                                             \
+    g.tiles_m = (p.a_rows + BM - 1) / BM;                                                                       \
+    g.tiles_n = (p.b_rows + BN - 1) / BN;                                                                       \
+    hipLaunchKernelGGL((head_product_kernel<F16, OT, BM, BN, WR, WC>),                                          \
+                       dim3(tile_grid(g.tiles_m * g.tiles_n * g.splits)), dim3(64 * WR * WC), 0, s, p, g);      \
   }
   if (large_tiles(p.a_rows, p.b_rows)) UMEM_PRODUCT(256, 256, 4, 2)
   else UMEM_PRODUCT(64, 64, 2, 2)
@@ -485,8 +669,12 @@ hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, cons
     if (large_tiles(hd.vocab, T)) UMEM_STATS(256, 256, 4, 2)
     else UMEM_STATS(64, 64, 2, 2)
 #undef UMEM_STATS
-    hipLaunchKernelGGL(head_join_kernel, dim3((t + 15) / 16), dim3(kThreads), 0, s, stats, goal, targets + t0, t, hd.vocab,
-                       tiles, loss + t0, lse + t0);
+    if (t <= kFewTokens)
+      hipLaunchKernelGGL(head_join_few_kernel, dim3(t), dim3(kThreads), 0, s, stats, goal, targets + t0, t, hd.vocab, tiles,
+                         loss + t0, lse + t0);
+    else
+      hipLaunchKernelGGL(head_join_kernel, dim3((t + 15) / 16), dim3(kThreads), 0, s, stats, goal, targets + t0, t,
+                         hd.vocab, tiles, loss + t0, lse + t0);
   }
   return hipGetLastError();
 }
@@ -503,29 +691,45 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
   uint16_t *parts = at(L.parts), *xt = at(L.xt), *wt = at(L.wt), *rows = at(L.rows), *cols = at(L.cols);
   float* sum = reinterpret_cast<float*>(base + L.sum);
   const int d = hd.d, V = hd.vocab, t_pad = static_cast<int>(up(T, 64)), piece = piece_rows(hd, T);
-  const int pr = row_parts(hd), pc = col_parts(hd);
+  const int pr = row_parts(hd), pc = col_parts(hd), px = x_col_parts(hd);
   const bool wide = hd.xtype == UMEM_F32;
   float* most = dloss ? reinterpret_cast<float*>(base + L.most) : nullptr;
+  float* x_most = reinterpret_cast<float*>(base + L.x_most);
   if (dloss)
     hipLaunchKernelGGL(head_most_kernel, dim3(kMostBlocks), dim3(kThreads), 0, s, dloss, targets, T, V, most);
+  // x's channels along rows, tokens along k
   const dim3 x_grid(t_pad / 64, (d + 63) / 64);
   if (wide) {
+    const float* xf = static_cast<const float*>(x);
     split_x(hd, T, x, parts, s);
-    hipLaunchKernelGGL((head_transpose_kernel<float, 3>), x_grid, dim3(kThreads), 0, s, static_cast<const float*>(x), T, d,
-                       xt, static_cast<int64_t>(t_pad), targets, V);
+    hipLaunchKernelGGL(head_most_x_kernel<float>, dim3(kMostBlocks), dim3(1024), 0, s, xf, targets, T, d, V, x_most);
+    const auto turn = px == 2 ? head_transpose_kernel<float, 2> : head_transpose_kernel<float, 1>;
+    hipLaunchKernelGGL(turn, x_grid, dim3(kThreads), 0, s, xf, T, d, xt, static_cast<int64_t>(t_pad), x_most, targets, V);
   } else {
+    hipLaunchKernelGGL(head_most_x_kernel<__bf16>, dim3(kMostBlocks), dim3(1024), 0, s, static_cast<const __bf16*>(x),
+                       targets, T, d, V, x_most);
     hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), x_grid, dim3(kThreads), 0, s,
-                       static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_pad), targets, V);
+                       static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_pad), x_most, targets, V);
   }
+  ProductArgs gx{}, gw{};
+  gx.splits = dx_splits(hd, T);
+  gx.sums = sum;
+  gx.whole = true;
+  gw.splits = 1;
+  gx.ld = gw.ld = d;
+  gx.most = gw.most = most;
+  gw.x_most = x_most;
+  gw.scale = hd.scale;
   for (int v0 = 0; v0 < V; v0 += piece) {
     const int v = std::min(piece, V - v0);
+    const bool last = v0 + piece >= V;
     const uint16_t* wp = w + static_cast<int64_t>(v0) * d;
     const TilePairs z = logit_pairs(hd, T, x, parts, wp, v);
-    const auto make = pr == 3 ? (pc == 3 ? slope<3, 3> : slope<3, 1>) : (pc == 3 ? slope<1, 3> : slope<1, 1>);
+    const auto make = pr == 3 ? (pc == 2 ? slope<3, 2> : slope<3, 1>) : (pc == 2 ? slope<1, 2> : slope<1, 1>);
     make(z, hd.scale, targets, lse, dloss, most, v0, V, piece, t_pad, rows, cols, s);
     // dx: channels along m, tokens along n, the piece along k
     hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), dim3(piece / 64, (d + 63) / 64), dim3(kThreads), 0, s, wp, v,
-                       d, wt, static_cast<int64_t>(piece), nullptr, 0);
+                       d, wt, static_cast<int64_t>(piece), nullptr, nullptr, 0);
     TilePairs p{};
     p.n = pr;
     for (int i = 0; i < pr; ++i) {
@@ -536,20 +740,24 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     p.b_rows = T;
     p.k = piece;
     p.a_ld = p.b_ld = piece;
-    const float* before = v0 > 0 ? sum : nullptr;
-    if (v0 + piece < V) product(p, before, sum, d, hd.scale, most, nullptr, 0, s);
-    else if (wide) product(p, before, static_cast<float*>(dx), d, hd.scale, most, targets, V, s);
-    else product(p, before, static_cast<__bf16*>(dx), d, hd.scale, most, targets, V, s);
-    // dW: channels along m, the piece's rows along n, tokens along k.  Of fp32 x and r the pairs of parts that add to
-    // 24 bits of the product; of fp32 x and one part of r what adds to more than r has.
-    static constexpr int kPairs[6][2] = {{0, 2}, {1, 1}, {2, 0}, {0, 1}, {1, 0}, {0, 0}};
+    // (without splits the sum of all pieces but the last is kept in `sum` as it is, and scaled with the last)
+    gx.first = v0 == 0;
+    gx.before = v0 > 0 ? sum : nullptr;
+    gx.out = last ? dx : sum;
+    gx.scale = last ? hd.scale : 1.f;
+    gx.most = last ? most : nullptr;
+    gx.targets = last ? targets : nullptr;
+    gx.vocab = V;
+    if (!last || wide) product<false, float>(p, gx, s);
+    else product<false, __bf16>(p, gx, s);
+    // dW: channels along m, the piece's rows along n, tokens along k; of fp32 x and two parts of r the pairs that count
     p = TilePairs{};
     const int64_t x_part = static_cast<int64_t>(d) * t_pad, c_part = static_cast<int64_t>(piece) * t_pad;
-    for (const auto& xr : kPairs) {
-      const bool in = wide ? (pc == 3 || (xr[1] == 0 && xr[0] < 2)) : (xr[0] == 0 && xr[1] < pc);
-      if (!in) continue;
-      p.a[p.n] = xt + xr[0] * x_part;
-      p.b[p.n++] = cols + xr[1] * c_part;
+    for (int i = 2; i >= 0; --i) {
+      const int xi = i == 2 ? 1 : 0, ri = i == 1 ? 1 : 0;   // from the smallest products to the largest
+      if (xi >= px || ri >= pc) continue;
+      p.a[p.n] = xt + xi * x_part;
+      p.b[p.n++] = cols + ri * c_part;
     }
     p.a_rows = d;
     p.b_rows = v;
@@ -558,10 +766,18 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     const int64_t w_at = static_cast<int64_t>(v0) * d;
     if (hd.gtype == UMEM_F32) {
       float* g = static_cast<float*>(dw) + w_at;
-      product(p, accumulate ? g : nullptr, g, d, hd.scale, most, nullptr, 0, s);
+      gw.out = g;
+      gw.before = accumulate ? g : nullptr;
+      product<true, float>(p, gw, s);
     } else {
-      product(p, nullptr, static_cast<__bf16*>(dw) + w_at, d, hd.scale, most, nullptr, 0, s);
+      gw.out = static_cast<__bf16*>(dw) + w_at;
+      product<true, __bf16>(p, gw, s);
     }
+  }
+  if (gx.splits > 1) {
+    const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(T) * d / 4 + kThreads - 1) / kThreads));
+    if (wide) hipLaunchKernelGGL(head_sum_kernel<float>, grid, dim3(kThreads), 0, s, gx, T, d);
+    else hipLaunchKernelGGL(head_sum_kernel<__bf16>, grid, dim3(kThreads), 0, s, gx, T, d);
   }
   return hipGetLastError();
 }

@@ -47,27 +47,43 @@ struct Parts {
 
 // ---------------------------------------------------------------- norm and first X
 
-constexpr int kNormBlocks = 64;
+// Workgroups that a matrix's norm is spread over: 4,096 elements or more each.
+int norm_blocks(const umem_orth_desc& od) {
+  return static_cast<int>(std::min<int64_t>(512, (static_cast<int64_t>(od.rows) * od.cols + 4095) / 4096));
+}
 
-// |G|^2 of each matrix, in kNormBlocks fp64 pieces of fixed ranges.
+// |G|^2 of each matrix, in fp64 pieces of fixed ranges.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void orth_norm_kernel(const T* __restrict__ g, int64_t size,
                                                              double* __restrict__ pieces) {
+  typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
   __shared__ double waves[kThreads / kWave];
   const T* m = g + blockIdx.y * size;
-  double sum = 0.0;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < size; i += kNormBlocks * kThreads) {
-    const double v = to_f32(m[i]);
-    sum += v * v;
-  }
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads * 4;
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+  int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
+#pragma unroll 4
+  for (; i + 4 <= size; i += step) {
+    const four v = *reinterpret_cast<const four*>(m + i);
 #pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
-  if ((threadIdx.x & (kWave - 1)) == 0) waves[threadIdx.x / kWave] = sum;
+    for (int j = 0; j < 4; ++j) {
+      const double x = to_f32(v[j]);
+      sum[j] = fma(x, x, sum[j]);
+    }
+  }
+  for (; i < size && (i & 3) != 3; ++i) {                   // the last, partial four
+    const double x = to_f32(m[i]);
+    sum[0] = fma(x, x, sum[0]);
+  }
+  double all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) all += __shfl_xor(all, off, kWave);
+  if ((threadIdx.x & (kWave - 1)) == 0) waves[threadIdx.x / kWave] = all;
   __syncthreads();
   if (threadIdx.x == 0) {
 #pragma unroll
-    for (int w = 1; w < kThreads / kWave; ++w) sum += waves[w];
-    pieces[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
+    for (int w = 1; w < kThreads / kWave; ++w) all += waves[w];
+    pieces[blockIdx.y * gridDim.x + blockIdx.x] = all;
   }
 }
 
@@ -75,14 +91,16 @@ __global__ __launch_bounds__(kThreads) void orth_norm_kernel(const T* __restrict
 // by_cols [cols][ld of rows].
 template <typename T>
 __global__ __launch_bounds__(kThreads) void orth_first_kernel(const T* __restrict__ g, int rows, int cols, float eps,
-                                                              const double* __restrict__ pieces, Parts by_rows,
-                                                              Parts by_cols) {
+                                                              const double* __restrict__ pieces, int blocks,
+                                                              Parts by_rows, Parts by_cols) {
   __shared__ uint32_t tile[64][65];
   const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
   const int64_t mat = blockIdx.z;
-  double sum = 0.0;
+  double sum = 0.0;                                         // every wave adds the pieces for itself
 #pragma unroll 8
-  for (int i = 0; i < kNormBlocks; ++i) sum += pieces[mat * kNormBlocks + i];
+  for (int i = threadIdx.x & (kWave - 1); i < blocks; i += kWave) sum += pieces[mat * blocks + i];
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
   const float norm = static_cast<float>(sqrt(sum)) + eps;
   const T* m = g + mat * rows * static_cast<int64_t>(cols);
 #pragma unroll
@@ -391,7 +409,7 @@ struct Layout {
     kp = up64(k);
     const size_t n = od.n, x = up256(n * 4 * m * kp), t = up256(n * 4 * k * mp), q = up256(n * 4 * m * mp);
     pieces = 0;
-    x0 = up256(n * kNormBlocks * sizeof(double));
+    x0 = up256(n * norm_blocks(od) * sizeof(double));
     t0 = x0 + x;
     x1 = t0 + t;
     t1 = x1 + x;
@@ -435,10 +453,10 @@ void product(OrthArgs g, int n, hipStream_t s) {
 template <typename GT>
 void first(const umem_orth_desc& od, const GT* g, double* pieces, const Parts& by_rows, const Parts& by_cols,
            hipStream_t s) {
-  hipLaunchKernelGGL(orth_norm_kernel<GT>, dim3(kNormBlocks, od.n), dim3(kThreads), 0, s, g,
+  hipLaunchKernelGGL(orth_norm_kernel<GT>, dim3(norm_blocks(od), od.n), dim3(kThreads), 0, s, g,
                      static_cast<int64_t>(od.rows) * od.cols, pieces);
   hipLaunchKernelGGL(orth_first_kernel<GT>, dim3((od.cols + 63) / 64, (od.rows + 63) / 64, od.n), dim3(kThreads), 0, s, g,
-                     od.rows, od.cols, od.eps, pieces, by_rows, by_cols);
+                     od.rows, od.cols, od.eps, pieces, norm_blocks(od), by_rows, by_cols);
 }
 
 }  // namespace

@@ -102,25 +102,26 @@ __global__ __launch_bounds__(kThreads) void orth_small_gram_kernel(const T* __re
         out[(i0 + i * 16 + (lane >> 4) + 4 * r) * kSide + j0 + j * 16 + (lane & 15)] = acc[i][j][r];
 }
 
-// The steps of one matrix: q[matrix][64][64] = Q / (|G| + eps).
+// The steps of one matrix of at most TOP rows: q[matrix][64][64] = Q / (|G| + eps).
+template <int TOP>
 __global__ __launch_bounds__(kStepThreads) void orth_small_steps_kernel(const double* __restrict__ pieces, int m, int chunks,
                                                                         int steps, double a, double b, double c,
                                                                         float eps, double* __restrict__ q) {
   __shared__ double A[kSide][kPitch], P[kSide][kPitch], Q[kSide][kPitch], T[kSide][kPitch];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int i0 = (wave >> 2) * 16, j0 = (wave & 3) * 16, col = j0 + (lane & 15);
-  const int top = (m + 15) / 16 * 16;                       // rows that hold anything
-  const bool on = i0 < top && j0 < top;                     // (all waves meet the barriers)
+  const bool on = i0 < TOP && j0 < TOP;                     // (all waves meet the barriers)
   const int64_t mat = blockIdx.x;
   const double* from = pieces + mat * chunks * kSide * kSide;
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+  if (on) {
+#pragma unroll 8
+    for (int p = 0; p < chunks; ++p)
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int row = i0 + (lane >> 4) + 4 * r;
-    double v = 0.0;
-    if (on)
-      for (int p = 0; p < chunks; ++p) v += from[(static_cast<int64_t>(p) * kSide + row) * kSide + col];
-    A[row][col] = v;
+      for (int r = 0; r < 4; ++r) sum[r] += from[(static_cast<int64_t>(p) * kSide + i0 + (lane >> 4) + 4 * r) * kSide + col];
   }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) A[i0 + (lane >> 4) + 4 * r][col] = sum[r];
   __syncthreads();
   double trace = lane < m ? A[lane][lane] : 0.0;
 #pragma unroll
@@ -137,8 +138,8 @@ __global__ __launch_bounds__(kStepThreads) void orth_small_steps_kernel(const do
   const auto times = [&](double (*x)[kPitch], double (*y)[kPitch]) {
     f64x4 acc = {0.0, 0.0, 0.0, 0.0};
     if (on) {
-#pragma unroll 4
-      for (int k0 = 0; k0 < top; k0 += 4) {
+#pragma unroll
+      for (int k0 = 0; k0 < TOP; k0 += 4) {
         const int k = k0 + (lane >> 4);
         acc = mfma64(x[i0 + (lane & 15)][k], y[j0 + (lane & 15)][k], acc);
       }
@@ -193,12 +194,11 @@ __global__ __launch_bounds__(kThreads) void orth_small_apply_kernel(const GT* g,
   }
   s.store(t);
   __syncthreads();
-  const int tiles = (m + 15) / 16;
   f64x4 acc[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) acc[i] = f64x4{0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
-  for (int j0 = 0; j0 < tiles * 16; j0 += 4) {
+  for (int j0 = 0; j0 < kSide; j0 += 4) {
     const int j = j0 + (lane >> 4);
     const double x = t[j][wave * 16 + (lane & 15)];
 #pragma unroll
@@ -234,8 +234,9 @@ template <bool TALL, typename GT, typename OT>
 void run(const umem_orth_desc& od, const GT* g, OT* out, double* pieces, double* q, hipStream_t s) {
   const int m = std::min(od.rows, od.cols), k = std::max(od.rows, od.cols), chunks = chunk_count(od);
   hipLaunchKernelGGL((orth_small_gram_kernel<GT, TALL>), dim3(chunks, od.n), dim3(kThreads), 0, s, g, m, k, chunks, pieces);
-  hipLaunchKernelGGL(orth_small_steps_kernel, dim3(od.n), dim3(kStepThreads), 0, s, pieces, m, chunks, od.steps,
-                     static_cast<double>(od.a), static_cast<double>(od.b), static_cast<double>(od.c), od.eps, q);
+  const auto step = m <= 16 ? orth_small_steps_kernel<16> : m <= 32 ? orth_small_steps_kernel<32> : orth_small_steps_kernel<64>;
+  hipLaunchKernelGGL(step, dim3(od.n), dim3(kStepThreads), 0, s, pieces, m, chunks, od.steps, static_cast<double>(od.a),
+                     static_cast<double>(od.b), static_cast<double>(od.c), od.eps, q);
   hipLaunchKernelGGL((orth_small_apply_kernel<GT, OT, TALL>), dim3((k + 63) / 64, od.n), dim3(kThreads), 0, s, g, m, k, q,
                      out, od.decay, od.scale);
 }

@@ -6,9 +6,11 @@ rounding: 2 u), and there are d / 32 additions of 32 products each after at most
 z_err = 2 u (3 d / 32 + 8) S + 2 u |z|.
 lse and loss move by at most the largest z_err and twice it, and lose a few u of the exponentials' sum (relative, so
 absolute in the logarithm) and their own rounding.
-r = exp(z - lse) - [target] moves by exp(..) (2 z_err + (|z - lse| + 8) u); as one bf16 part it is half a step, 2^-8, off,
-as three parts u.  The sums over the vocabulary or the tokens add 2 u (terms / 32 + 16) per part of their absolute
-terms, and a bf16 result half a step.
+r = exp(z - lse) - [target] moves by exp(..) (2 z_err + (|z - lse| + 8) u).  For dx it is half a step, 2^-8, off as one bf16
+part, u as three.  For dw it is 2^-11 and, below 2^-29 of the largest dloss, 2^-40 of that off as one fp16 part; as two
+2^-22 and 2^-40, as fp32 x is then, relative to the largest x, and the product of the second parts, 2^-22, is left out.
+The sums over the vocabulary or the tokens add 2 u (terms / 32 + 16) per part of their absolute terms, and a
+bf16 result half a step.
 """
 import numpy as np
 import pytest
@@ -106,9 +108,10 @@ def bounds(X, W, Y, G, scale, err, wide_x, wide_g):
     T, V = r.shape
     X = np.where(on[:, None], X, 0.0)
     ex, ew = np.abs(W), np.abs(X)
-    # one part of r loses half a step of it; three lose u, and every part is summed
     tx = off @ ex + (np.abs(r) @ ex) * ((u if wide_x else HALF) + (3 if wide_x else 1) * 2 * u * (V / 32 + 16) + 8 * u)
-    tw = off.T @ ew + (np.abs(r).T @ ew) * ((2 * u if wide_g else HALF + 2.0 ** -16) + 6 * 2 * u * (T / 32 + 16) + 8 * u)
+    tw = off.T @ ew + (np.abs(r).T @ ew) * ((3 * 2.0 ** -22 if wide_g else 2.0 ** -11 + 2.0 ** -11) + 3 * 2 * u * (T / 32 + 16) + 8 * u)
+    most = np.abs(G[on]).max() * abs(scale) if on.any() else 0.0
+    tw += 2.0 ** -40 * (most * ew.sum(axis=0)[None, :] + ew.max() * np.abs(r).sum(axis=0)[:, None])
     return r @ W, r.T @ X, tx, tw
 
 
