@@ -326,7 +326,7 @@ __device__ __forceinline__ float most_of(const float* most) {
 }
 
 // r of a piece of the vocabulary, over s and the largest dloss: rows[part][T][piece] in PR bf16 parts, and times 2^15
-// cols[part][piece][t_pad] in PC fp16 parts; zeros past the piece's rows of W, past T and for tokens without a target.
+// cols[part][piece][t_ld] in PC fp16 parts; zeros past the piece's rows of W, past T and for tokens without a target.
 // A part at a time goes through LDS, [token][v], its 16-byte pieces permuted by the token's number so that
 // both orders of reading meet all banks.  (Parts kept from one to the next spill 360 registers: 430 us of 620 were the
 // end of a tile.)
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
                                                                  const float* __restrict__ lse,
                                                                  const float* __restrict__ dloss,
                                                                  const float* __restrict__ most, int v_first, int vocab,
-                                                                 int piece, int t_pad, uint16_t* __restrict__ rows,
+                                                                 int piece, int t_ld, uint16_t* __restrict__ rows,
                                                                  uint16_t* __restrict__ cols) {
   typedef Tile<false, BM, BN, WR, WC, 2> Tl;
   static_assert(BM * BN <= 2 * Tl::kElems && BM % 64 == 0 && BN % 64 == 0, "a tile of bf16 fits the operands' LDS");
@@ -358,9 +358,9 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
 #pragma unroll
   for (int j = 0; j < Tl::NT; ++j) {
     const int t = at.n * BN + (wc * Tl::NT + j) * 16 + (lane & 15);
-    const int y = t < T ? targets[t] : -1;
-    const bool on = static_cast<uint32_t>(y) < static_cast<uint32_t>(vocab);
-    const float l = on ? lse[t] : 0.f, g = on ? (dloss ? dloss[t] / largest : 1.f) : 0.f;
+    const int tc = min(t, T - 1), y = targets[tc];
+    const bool on = t < T && static_cast<uint32_t>(y) < static_cast<uint32_t>(vocab);
+    const float l = lse[tc], g = dloss ? dloss[tc] / largest : 1.f;
 #pragma unroll
     for (int i = 0; i < Tl::MT; ++i)
 #pragma unroll
@@ -370,13 +370,18 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
         acc[i][j][r] = on && v < V ? g * e : 0.f;
       }
   }
-  // token n's first element; a 16-byte piece of it is at place (piece ^ turn(n)) of the 8 in its group
+  // token n's first element; its 16-byte piece c is at place c ^ turn(n)
   const auto row_at = [&](int n) { return (n < BN / 2 ? buf0 : buf1) + (n % (BN / 2)) * BM; };
-  const auto turn = [](int n) { return (n ^ (n >> 3)) & 7; };
+  const auto turn = [](int n) { return (n ^ (n >> 3)) & (BM / 8 - 1); };
 #pragma unroll 1
   for (int pass = 0; pass < PR + PC; ++pass) {
     const bool by_rows = pass < PR;
     const int part = by_rows ? pass : pass - PR;
+    // (each pass makes its part again: made before the loop, all parts would be kept)
+#pragma unroll
+    for (int j = 0; j < Tl::NT; ++j)
+#pragma unroll
+      for (int i = 0; i < Tl::MT; ++i) asm volatile("" : "+v"(acc[i][j]));
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < Tl::NT; ++j)
@@ -411,17 +416,17 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
               *reinterpret_cast<const u32x4*>(row_at(n) + ((c ^ turn(n)) << 3));
       }
     } else {
-      uint16_t* to = cols + static_cast<int64_t>(part) * piece * t_pad;
-      // eight lanes to a row of eight 16-byte pieces (64 tokens), eight rows of W to a wave
+      uint16_t* to = cols + static_cast<int64_t>(part) * piece * t_ld;
+      // a row of W's tokens to BN / 8 lanes: whole lines
 #pragma unroll 2
       for (int i = threadIdx.x; i < BM * (BN / 8); i += Tl::kThreads) {
-        const int group = i / 64, m = (group % (BM / 8)) * 8 + (i & 7), n8 = (group / (BM / 8)) * 64 + ((i >> 3) & 7) * 8;
+        const int m = i / (BN / 8), n8 = (i % (BN / 8)) * 8;
         const int t = at.n * BN + n8, v = at.m * BM + m;
         uint32_t b[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) b[k] = row_at(n8 + k)[(((m >> 3) ^ turn(n8 + k)) << 3) + (m & 7)];
-        if (t < t_pad && v < piece)
-          *reinterpret_cast<u32x4*>(to + static_cast<int64_t>(v) * t_pad + t) =
+        if (t < t_ld && v < piece)
+          *reinterpret_cast<u32x4*>(to + static_cast<int64_t>(v) * t_ld + t) =
               u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16};
       }
     }
@@ -536,12 +541,15 @@ int x_col_parts(const umem_head_desc& hd) { return hd.xtype == UMEM_F32 && hd.gt
 // 2^18 tokens on 256 rows of every token), W's transposed piece 2^14 rows.
 constexpr int64_t kPieceRows = 1 << 14, kPieceValues = 1 << 26;
 int64_t most_piece(const umem_head_desc& hd) { return std::min(kPieceRows, up(hd.vocab, 256)); }
+// Elements of a row that holds all tokens: T in whole slices, and a line more, as rows a large power of two apart
+// are written and read slower.
+int64_t token_row(int T) { return up(T, 64) + 64; }
 int64_t piece_values(const umem_head_desc& hd, int T) {
-  const int64_t t = up(T, 64);
+  const int64_t t = token_row(T);
   return std::min(t * most_piece(hd), std::max(kPieceValues, t * 256));
 }
 int piece_rows(const umem_head_desc& hd, int T) {
-  const int64_t t = up(T, 64), most = std::min(most_piece(hd), std::max<int64_t>(256, piece_values(hd, T) / t / 256 * 256));
+  const int64_t t = token_row(T), most = std::min(most_piece(hd), std::max<int64_t>(256, piece_values(hd, T) / t / 256 * 256));
   const int64_t pieces = (hd.vocab + most - 1) / most;
   return static_cast<int>(up((hd.vocab + pieces - 1) / pieces, 256));
 }
@@ -577,7 +585,7 @@ struct ForwardLayout {
 struct BackwardLayout {
   size_t parts, xt, wt, rows, cols, sum, most, x_most, total;
   BackwardLayout(const umem_head_desc& hd, int T) {
-    const size_t t = T, tp = up(T, 64), d = hd.d, values = piece_values(hd, T);
+    const size_t t = T, tp = token_row(T), d = hd.d, values = piece_values(hd, T);
     parts = 0;
     xt = up256(hd.xtype == UMEM_F32 ? 3 * t * d * 2 : 0);
     wt = xt + up256(x_col_parts(hd) * d * tp * 2);
@@ -620,23 +628,23 @@ void product(const TilePairs& p, ProductArgs g, hipStream_t s) {
     hipLaunchKernelGGL((head_product_kernel<F16, OT, BM, BN, WR, WC>),                                          \
                        dim3(tile_grid(g.tiles_m * g.tiles_n * g.splits)), dim3(64 * WR * WC), 0, s, p, g);      \
   }
-  if (large_tiles(p.a_rows, p.b_rows)) UMEM_PRODUCT(256, 256, 4, 2)
+  if (large_tiles(p.a_rows, p.b_rows)) UMEM_PRODUCT(256, 256, 2, 4)
   else UMEM_PRODUCT(64, 64, 2, 2)
 #undef UMEM_PRODUCT
 }
 
 template <int PR, int PC>
 void slope(const TilePairs& p, float scale, const int32_t* targets, const float* lse, const float* dloss,
-           const float* most, int v_first, int vocab, int piece, int t_pad, uint16_t* rows, uint16_t* cols,
+           const float* most, int v_first, int vocab, int piece, int t_ld, uint16_t* rows, uint16_t* cols,
            hipStream_t s) {
 #define UMEM_SLOPE(BM, BN, WR, WC)                                                                              \
   {                                                                                                             \
     const int tm = (piece + BM - 1) / BM, tn = (p.b_rows + BN - 1) / BN;                                        \
     hipLaunchKernelGGL((head_slope_kernel<BM, BN, WR, WC, PR, PC>), dim3(tile_grid(tm * tn)),                   \
                        dim3(64 * WR * WC), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first, vocab,    \
-                       piece, t_pad, rows, cols);                                                               \
+                       piece, t_ld, rows, cols);                                                                \
   }
-  if (large_tiles(piece, p.b_rows)) UMEM_SLOPE(256, 256, 4, 2)
+  if (large_tiles(piece, p.b_rows)) UMEM_SLOPE(128, 128, 2, 2)
   else UMEM_SLOPE(64, 64, 2, 2)
 #undef UMEM_SLOPE
 }
@@ -666,7 +674,7 @@ hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, cons
     hipLaunchKernelGGL((head_stats_kernel<BM, BN, WR, WC>), dim3(tile_grid(tiles * tn)), dim3(64 * WR * WC), 0, \
                        s, p, tiles, tn, hd.scale, targets + t0, stats, goal);                                   \
   }
-    if (large_tiles(hd.vocab, T)) UMEM_STATS(256, 256, 4, 2)
+    if (large_tiles(hd.vocab, T)) UMEM_STATS(256, 256, 2, 4)
     else UMEM_STATS(64, 64, 2, 2)
 #undef UMEM_STATS
     if (t <= kFewTokens)
@@ -690,7 +698,7 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
   const auto at = [&](size_t o) { return reinterpret_cast<uint16_t*>(base + o); };
   uint16_t *parts = at(L.parts), *xt = at(L.xt), *wt = at(L.wt), *rows = at(L.rows), *cols = at(L.cols);
   float* sum = reinterpret_cast<float*>(base + L.sum);
-  const int d = hd.d, V = hd.vocab, t_pad = static_cast<int>(up(T, 64)), piece = piece_rows(hd, T);
+  const int d = hd.d, V = hd.vocab, t_pad = static_cast<int>(up(T, 64)), t_ld = static_cast<int>(token_row(T)), piece = piece_rows(hd, T);
   const int pr = row_parts(hd), pc = col_parts(hd), px = x_col_parts(hd);
   const bool wide = hd.xtype == UMEM_F32;
   float* most = dloss ? reinterpret_cast<float*>(base + L.most) : nullptr;
@@ -704,12 +712,12 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     split_x(hd, T, x, parts, s);
     hipLaunchKernelGGL(head_most_x_kernel<float>, dim3(kMostBlocks), dim3(1024), 0, s, xf, targets, T, d, V, x_most);
     const auto turn = px == 2 ? head_transpose_kernel<float, 2> : head_transpose_kernel<float, 1>;
-    hipLaunchKernelGGL(turn, x_grid, dim3(kThreads), 0, s, xf, T, d, xt, static_cast<int64_t>(t_pad), x_most, targets, V);
+    hipLaunchKernelGGL(turn, x_grid, dim3(kThreads), 0, s, xf, T, d, xt, static_cast<int64_t>(t_ld), x_most, targets, V);
   } else {
     hipLaunchKernelGGL(head_most_x_kernel<__bf16>, dim3(kMostBlocks), dim3(1024), 0, s, static_cast<const __bf16*>(x),
                        targets, T, d, V, x_most);
     hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), x_grid, dim3(kThreads), 0, s,
-                       static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_pad), x_most, targets, V);
+                       static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_ld), x_most, targets, V);
   }
   ProductArgs gx{}, gw{};
   gx.splits = dx_splits(hd, T);
@@ -726,7 +734,7 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     const uint16_t* wp = w + static_cast<int64_t>(v0) * d;
     const TilePairs z = logit_pairs(hd, T, x, parts, wp, v);
     const auto make = pr == 3 ? (pc == 2 ? slope<3, 2> : slope<3, 1>) : (pc == 2 ? slope<1, 2> : slope<1, 1>);
-    make(z, hd.scale, targets, lse, dloss, most, v0, V, piece, t_pad, rows, cols, s);
+    make(z, hd.scale, targets, lse, dloss, most, v0, V, piece, t_ld, rows, cols, s);
     // dx: channels along m, tokens along n, the piece along k
     hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), dim3(piece / 64, (d + 63) / 64), dim3(kThreads), 0, s, wp, v,
                        d, wt, static_cast<int64_t>(piece), nullptr, nullptr, 0);
@@ -752,7 +760,7 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     else product<false, __bf16>(p, gx, s);
     // dW: channels along m, the piece's rows along n, tokens along k; of fp32 x and two parts of r the pairs that count
     p = TilePairs{};
-    const int64_t x_part = static_cast<int64_t>(d) * t_pad, c_part = static_cast<int64_t>(piece) * t_pad;
+    const int64_t x_part = static_cast<int64_t>(d) * t_ld, c_part = static_cast<int64_t>(piece) * t_ld;
     for (int i = 2; i >= 0; --i) {
       const int xi = i == 2 ? 1 : 0, ri = i == 1 ? 1 : 0;   // from the smallest products to the largest
       if (xi >= px || ri >= pc) continue;
@@ -762,7 +770,7 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     p.a_rows = d;
     p.b_rows = v;
     p.k = t_pad;
-    p.a_ld = p.b_ld = t_pad;
+    p.a_ld = p.b_ld = t_ld;
     const int64_t w_at = static_cast<int64_t>(v0) * d;
     if (hd.gtype == UMEM_F32) {
       float* g = static_cast<float*>(dw) + w_at;

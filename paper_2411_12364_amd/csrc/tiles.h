@@ -107,17 +107,19 @@ struct Tile {
   // The slice from k0 on into a buffer; a piece past k is another one here (past_k).
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t a, __amdgpu_buffer_rsrc_t b, int k0, int k,
                                        uint16_t* lds) const {
-    const int wave = threadIdx.x >> 6;
-    uint32_t back = 0;
-    if (PARTS == kPlain && k0 + kTileBK > k && k0 + col_k >= k) back = static_cast<uint32_t>(col_k) * 2u;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const auto get = [&](uint32_t back) {
 #pragma unroll
-    for (int i = 0; i < kA; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(a, (lds_u32*)(lds + (i * kThreads + wave * 64) * 8), 16, a_off[i] - back,
-                                               k0 * 2, 0, 0);
+      for (int i = 0; i < kA; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(a, (lds_u32*)(lds + (i * kThreads + wave * 64) * 8), 16,
+                                                 a_off[i] - back, k0 * 2, 0, 0);
 #pragma unroll
-    for (int i = 0; i < kB; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_u32*)(lds + BM * kTileBK + (i * kThreads + wave * 64) * 8), 16,
-                                               b_off[i] - back, k0 * 2, 0, 0);
+      for (int i = 0; i < kB; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_u32*)(lds + BM * kTileBK + (i * kThreads + wave * 64) * 8), 16,
+                                                 b_off[i] - back, k0 * 2, 0, 0);
+    };
+    if (PARTS == kPlain && k0 + kTileBK > k) get(k0 + col_k >= k ? static_cast<uint32_t>(col_k) * 2u : 0u);
+    else get(0u);
   }
 
   // The lane's pieces past k, once they have landed, to zeros.  (Rows of parts are whole slices.)
@@ -150,6 +152,7 @@ struct Tile {
       for (int i = 0; i < NT; ++i) b1[i] = *reinterpret_cast<const u32x4*>(b + i * 16 * kTileBK + at1);
 #pragma unroll
       for (int i = 0; i < MT; ++i) a1[i] = *reinterpret_cast<const u32x4*>(a + i * 16 * kTileBK + at1);
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -162,6 +165,7 @@ struct Tile {
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[1][i][j] = tile_mfma<F16>(a1[i], b0[j], acc[1][i][j]);
+      __builtin_amdgcn_s_setprio(0);
     } else {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
@@ -171,10 +175,12 @@ struct Tile {
         for (int i = 0; i < NT; ++i) bf[i] = *reinterpret_cast<const u32x4*>(b + i * 16 * kTileBK + at);
 #pragma unroll
         for (int i = 0; i < MT; ++i) af[i] = *reinterpret_cast<const u32x4*>(a + i * 16 * kTileBK + at);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int j = 0; j < NT; ++j) acc[0][i][j] = tile_mfma<F16>(af[i], bf[j], acc[0][i][j]);
+        __builtin_amdgcn_s_setprio(0);
       }
     }
   }
