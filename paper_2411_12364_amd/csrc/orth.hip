@@ -2,18 +2,27 @@
 //
 //   X_0 = G / (|G|_F + eps),  X <- a X + (b A + c A^2) X with A = X X^T,  out = decay out + scale X_steps
 //
-// on the smaller side: a tall G is worked on transposed, so A is m x m with m = min(rows, cols).  All three products of a
-// step have both operands with k innermost (tiles.h): A's are X's rows, A^2's are A's rows, as A is symmetric, and
-// X's update takes B = b A + c A^2 and the transposed X, so X is kept in both orders.  Bounded by the matrix cores for
-// large matrices, by the chain of 3 steps launches for small ones.
+// on the smaller side: a tall G is worked on transposed, so A is m x m with m = min(rows, cols) <= k.  Every product
+// has both operands with k innermost (tiles.h): A's are X's rows, A^2's are A's rows, as A is symmetric, and
+// X's update takes B = b A + c A^2 and the transposed X, so X is kept in both orders; of a symmetric product the tiles on and
+// below the diagonal are made.  Where k is long, two or three steps are taken on m x m matrices alone, as the steps'
+// polynomials commute:
 //
-// Rounding: every matrix between the steps is two fp16 parts of its values times 2^12, which hold 22 bits of it, and
-// a product takes three of the four pairs of parts (the fourth is below 2^-22 of the result); sums are fp32, |G|_F is fp64.
-// Two bf16 parts would hold 17 bits: what a step loses of X's small singular values grows by a = 3.4 a step
-// (a random 896 x 2,048 matrix after five steps: 4e-7 off the exact result with the fp16 parts, 2e-5 with the bf16 ones).
-// An entry of X, A or B that reaches 16 becomes infinite: of coefficients that
-// keep singular values of 1 near 1 none does.
+//   P = a I + b A + c A^2,  Q <- Q P,  A <- P A P,   then X <- Q X:
+//
+// 3 products of m x m x m for each step but the first in the place of A = X X^T and B X.  Bounded by the matrix cores for
+// large matrices, by the chain of launches for small ones.
+//
+// Rounding: every matrix between the steps is two fp16 parts of its values times a power of two (2^12; 2^9 for P and Q),
+// which hold 22 bits of it, and a product takes three of the four pairs of parts (the fourth is below 2^-22 of the
+// result); sums are fp32, |G|_F is fp64.  Two bf16 parts would hold 17 bits: what a step loses of X's small singular
+// values grows by a = 3.4 a step.  After five steps of a random 448 x 1,792 matrix one step at a time is 6e-7 off the
+// exact result, two and three at a time 7e-7, the bf16 parts 4e-5, fp32 throughout 1e-6; of one with a direction 100 times as
+// strong as the others 5e-6, 1e-5 and, in fp32, 1e-5.
+// An entry of X, A or B that reaches 16, of Q 128, becomes infinite: of coefficients that keep singular values of 1
+// near 1 none does.
 #include <algorithm>
+#include <cmath>
 
 #include "tiles.h"
 
@@ -133,20 +142,31 @@ __global__ __launch_bounds__(kThreads) void orth_first_kernel(const T* __restric
 
 // ---------------------------------------------------------------- products
 
-enum Mode { kGram, kPoly, kUpdate, kLast };
-constexpr bool symmetric(Mode m) { return m == kGram || m == kPoly; }
+// A = X X^T; B = b A + c A^2; P = a I + B; a product of two polynomials of A (Q P, P A); X = a X + B X, or Q X; the same
+// into the output.
+enum Mode { kGram, kPoly, kShifted, kTimes, kUpdate, kApply, kLast, kLastApply };
+constexpr bool symmetric(Mode m) { return m == kGram || m == kPoly || m == kShifted || m == kTimes; }
+constexpr bool has_own(Mode m) { return m == kPoly || m == kShifted || m == kUpdate || m == kLast; }
+constexpr bool is_last(Mode m) { return m == kLast || m == kLastApply; }
+constexpr bool is_update(Mode m) { return m == kUpdate || m == kApply; }
+// P and Q are held times 2^9.  The sums of a product hold both its operands' powers, its result one of them.
+constexpr float kDownQ = 1.f / 512.f;
+constexpr float down(Mode m) { return m == kTimes || m == kApply || m == kLastApply ? kDownQ : kDown; }
 
 struct OrthArgs {
   Parts a, b;             // the product's operands: rows along m and along n, k innermost
-  Parts own;              // kPoly: A; kUpdate, kLast: X by rows n, m along its rows
-  Parts out, out_t;       // kGram, kPoly: the product (symmetric); kUpdate: X by rows n, and transposed
+  Parts own;              // kPoly, kShifted: A; kUpdate, kLast: X by rows n, m along its rows
+  Parts out, out_t;       // the product (symmetric), or X by rows n and, in out_t, transposed
+  Parts a2, b2, out2;     // a second symmetric product of the same shape (jobs == 2)
+  int jobs;
   int rows_m, rows_n;
   int k;                  // elements of a row that the product walks
   int tiles_m, tiles_n, per, items;        // of a matrix: tiles; of all matrices: items
   int splits;             // parts of k, each an item of its own with its sums to partial [split][item][BN][BM]
   float* partial;
-  float alpha, beta;      // kPoly: alpha A + beta A^2; kUpdate, kLast: alpha X + B X
-  float decay, scale;     // kLast: final = decay final + scale (alpha X + B X), [n][m] of final_ld
+  float alpha, beta;      // with own: alpha own + beta product
+  float shift;            // kShifted: added to the diagonal
+  float decay, scale;     // the last X: final = decay final + scale X, [n][m] of final_ld
   void* final;
   int64_t final_ld, final_matrix;
 };
@@ -177,16 +197,21 @@ __device__ __forceinline__ f32x4 get_four(const Parts& in, int64_t mat, int n, i
                bits_f32(hi.y & 0xffffu) + bits_f32(lo.y & 0xffffu), bits_f32(hi.y >> 16) + bits_f32(lo.y >> 16)};
 }
 
-// A product's four sums at (n, m .. m + 3), times 2^24, become four values of the result (times 2^12) with their two parts
-// in a word each, zeros past the matrix; or go to the final output.
+// A product's four sums at (n, m .. m + 3) become four values of the result with their two parts in a word each, zeros
+// past the matrix; or go to the final output.
 template <Mode MODE, typename OT>
 __device__ __forceinline__ u32x4 finish_four(const OrthArgs& g, int64_t mat, int n, int m, f32x4 v) {
   const bool in = n < g.rows_n && m < g.rows_m;
-  v *= kDown;
-  if constexpr (MODE != kGram) {
+  v *= down(MODE);
+  if constexpr (has_own(MODE)) {
     if (in) v = g.alpha * get_four(g.own, mat, n, m) + g.beta * v;
   }
-  if constexpr (MODE == kLast) {
+  if constexpr (MODE == kShifted) {
+    v *= kDown / kDownQ;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] += m + r == n ? g.shift / kDownQ : 0.f;
+  }
+  if constexpr (is_last(MODE)) {
     if (!in) return u32x4{0u, 0u, 0u, 0u};
     OT* to = static_cast<OT*>(g.final) + mat * g.final_matrix + n * g.final_ld + m;
     const float s = g.scale * kDown;
@@ -240,17 +265,17 @@ __device__ __forceinline__ void put_eight(const Parts& out, int64_t mat, int row
 // The block of the result at (m0, n0) from LDS to memory, by rows and (or of a symmetric result the mirrored tile) by
 // columns.
 template <Mode MODE, int BM, int BN, int THREADS, typename At>
-__device__ __forceinline__ void put_block(const OrthArgs& g, int64_t mat, int m0, int n0, bool mirrored, const At& word) {
+__device__ __forceinline__ void put_block(const OrthArgs& g, const Parts& rows, int64_t mat, int m0, int n0, bool mirrored, const At& word) {
   for (int i = threadIdx.x; i < BN * (BM / 8); i += THREADS) {
     const int n = i / (BM / 8), m = (i % (BM / 8)) * 8;
-    if (n0 + n >= g.rows_n || 2 * (m0 + m) >= g.out.ld) continue;
+    if (n0 + n >= g.rows_n || 2 * (m0 + m) >= rows.ld) continue;
     uint32_t w[8];
     *reinterpret_cast<u32x4*>(w) = *reinterpret_cast<const u32x4*>(word(n, m));
     *reinterpret_cast<u32x4*>(w + 4) = *reinterpret_cast<const u32x4*>(word(n, m + 4));
-    put_eight(g.out, mat, n0 + n, m0 + m, w);
+    put_eight(rows, mat, n0 + n, m0 + m, w);
   }
-  if (MODE != kUpdate && !mirrored) return;
-  const Parts& out = MODE == kUpdate ? g.out_t : g.out;
+  if (!is_update(MODE) && !mirrored) return;
+  const Parts& out = is_update(MODE) ? g.out_t : rows;
   // eight lanes to 64 consecutive n of a column, eight columns to a wave
   for (int i = threadIdx.x; i < BM * (BN / 8); i += THREADS) {
     const int group = i / 64, m = (group % (BM / 8)) * 8 + (i & 7), n = (group / (BM / 8)) * 64 + ((i >> 3) & 7) * 8;
@@ -262,23 +287,24 @@ __device__ __forceinline__ void put_block(const OrthArgs& g, int64_t mat, int m0
   }
 }
 
-template <Mode MODE, TileParts PARTS, typename OT, int BM, int BN, int WR, int WC, int BUFS>
+template <Mode MODE, typename OT, int BM, int BN, int WR, int WC, int BUFS>
 __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(BM == 64 ? 3 : 2))) void orth_product_kernel(OrthArgs g) {
-  typedef Tile<true, BM, BN, WR, WC, BUFS, PARTS> Tl;
+  typedef Tile<true, BM, BN, WR, WC, BUFS, kBoth> Tl;
   static_assert(BN == 64 ? 2 * BM * BN <= Tl::kElems : BN % 128 == 0 && BM * BN <= Tl::kElems,
                 "a tile of words fits the operands' LDS");
   __shared__ __align__(16) uint16_t buf0[Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[Tl::kElems];
   __shared__ __align__(16) uint16_t buf2[BUFS > 2 ? Tl::kElems : 8];
   __shared__ __align__(16) uint16_t buf3[BUFS > 3 ? Tl::kElems : 8];
-  const int all = g.items * g.splits, id = tile_item(all);
+  const int all = g.items * g.splits * g.jobs, id = tile_item(all);
   if (id >= all) return;                                    // the whole workgroup: no barrier is skipped
-  const int split = id / g.items, item = id - split * g.items;
+  const int split = id / g.items, item = id - split * g.items;          // or of two products which one
+  const bool second = MODE == kTimes && g.jobs == 2 && split == 1;
   const OrthTile at = orth_tile<MODE>(g, item);
   TilePairs p;
   p.n = 1;
-  p.a[0] = g.a.p + at.mat * g.a.matrix;
-  p.b[0] = g.b.p + at.mat * g.b.matrix;
+  p.a[0] = (second ? g.a2.p : g.a.p) + at.mat * g.a.matrix;
+  p.b[0] = (second ? g.b2.p : g.b.p) + at.mat * g.b.matrix;
   p.a_rows = g.rows_m;
   p.b_rows = g.rows_n;
   p.k = g.k;
@@ -288,7 +314,8 @@ __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(BM
   tile.init(p, at.m * BM, at.n * BN);
   f32x4 acc[Tl::MT][Tl::NT];
   const int64_t slices = Tl::slices(p);
-  const int from = static_cast<int>(slices * split / g.splits), to = static_cast<int>(slices * (split + 1) / g.splits);
+  const int part = g.jobs == 2 ? 0 : split;
+  const int from = static_cast<int>(slices * part / g.splits), to = static_cast<int>(slices * (part + 1) / g.splits);
   tile.run(p, from, to, buf0, buf1, buf2, buf3, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
   const int m_in = wr * Tl::MT * 16 + 4 * (lane >> 4), n_in = wc * Tl::NT * 16 + (lane & 15);
@@ -305,18 +332,18 @@ __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(BM
     uint16_t* half = BN == 64 || n < BN / 2 ? buf0 : buf1;
     return reinterpret_cast<uint32_t*>(half) + word_at<BM>(BN == 64 ? n : n % (BN / 2), m);
   };
-  if (MODE != kLast) __syncthreads();                       // the last slice has been read
+  if (!is_last(MODE)) __syncthreads();                      // the last slice has been read
 #pragma unroll
   for (int j = 0; j < Tl::NT; ++j)
 #pragma unroll
     for (int i = 0; i < Tl::MT; ++i) {
       const int n = n_in + j * 16, m = m_in + i * 16;
       const u32x4 w = finish_four<MODE, OT>(g, at.mat, at.n * BN + n, at.m * BM + m, acc[i][j]);
-      if (MODE != kLast) *reinterpret_cast<u32x4*>(word(n, m)) = w;
+      if (!is_last(MODE)) *reinterpret_cast<u32x4*>(word(n, m)) = w;
     }
-  if (MODE == kLast) return;
+  if (is_last(MODE)) return;
   __syncthreads();
-  put_block<MODE, BM, BN, Tl::kThreads>(g, at.mat, at.m * BM, at.n * BN, at.m != at.n, word);
+  put_block<MODE, BM, BN, Tl::kThreads>(g, second ? g.out2 : g.out, at.mat, at.m * BM, at.n * BN, at.m != at.n, word);
 }
 
 // The sums of the splits, in their order, and what a product does with them; a 64 x 64 block of a tile a workgroup.
@@ -340,11 +367,11 @@ __global__ __launch_bounds__(kThreads) void orth_join_kernel(OrthArgs g) {
 #pragma unroll 4
     for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(q + s * next);
     const u32x4 w = finish_four<MODE, OT>(g, at.mat, n0 + n, m0 + m, v);
-    if (MODE != kLast) *reinterpret_cast<u32x4*>(word(n, m)) = w;
+    if (!is_last(MODE)) *reinterpret_cast<u32x4*>(word(n, m)) = w;
   }
-  if (MODE == kLast) return;
+  if (is_last(MODE)) return;
   __syncthreads();
-  put_block<MODE, 64, 64, kThreads>(g, at.mat, m0, n0, at.m != at.n, word);
+  put_block<MODE, 64, 64, kThreads>(g, g.out, at.mat, m0, n0, at.m != at.n, word);
 }
 
 // ---------------------------------------------------------------- host
@@ -360,6 +387,7 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 // x 896 over 2,048 20.7 in one piece, 17.0 in two, 18.6 in four; 1,024 x 1,024 over 16,384 242 in one, 60 in six.
 struct Plan {
   int bm, splits;
+  double us;
 };
 constexpr int kMostSplits = 16, kCus = 256;
 constexpr size_t kPartialBytes = size_t{64} << 20;
@@ -367,15 +395,14 @@ int64_t tile_count(int bm, int n, int rows_m, int rows_n, bool sym) {
   const int64_t tm = (rows_m + bm - 1) / bm, tn = (rows_n + bm - 1) / bm;
   return n * (sym ? tm * (tm + 1) / 2 : tm * tn);
 }
-Plan plan(int n, int rows_m, int rows_n, int slices, bool sym) {
-  Plan best{64, 1};
-  double least = 1e300;
+Plan plan(int n, int rows_m, int rows_n, int slices, bool sym, int jobs = 1) {
+  Plan best{64, 1, 1e300};
   for (int bm : {64, 128}) {
     const int64_t it = tile_count(bm, n, rows_m, rows_n, sym);
-    for (int s = 1; s <= kMostSplits && s <= slices; ++s) {
+    for (int s = 1; s <= (jobs == 2 ? 1 : kMostSplits) && s <= slices; ++s) {
       const double bytes = static_cast<double>(it) * s * bm * bm * sizeof(float);
       if (s > 1 && bytes > kPartialBytes) break;
-      const int64_t wgs = it * s, cus = (wgs + kCus - 1) / kCus;          // workgroups of the fullest CU
+      const int64_t wgs = it * s * jobs, cus = (wgs + kCus - 1) / kCus;          // workgroups of the fullest CU
       const double each = (slices + s - 1) / s;
       double cost = s > 1 ? 4.5 + 0.7 * s + bytes / 2.5e6 : 0.0;
       if (bm == 128) {
@@ -385,10 +412,7 @@ Plan plan(int n, int rows_m, int rows_n, int slices, bool sym) {
         cost += static_cast<double>(cus / 3) * (3.0 + 0.6 * each);
         if (rest) cost += 3.0 + (rest == 1 ? 0.25 : 0.4) * each;
       }
-      if (cost < least) {
-        least = cost;
-        best = {bm, s};
-      }
+      if (cost < best.us) best = {bm, s, cost};
     }
   }
   return best;
@@ -398,24 +422,46 @@ size_t partial_bytes(const Plan& p, int n, int rows_m, int rows_n, bool sym) {
   return p.splits == 1 ? 0 : up256(tile_count(p.bm, n, rows_m, rows_n, sym) * p.splits * p.bm * p.bm * sizeof(float));
 }
 
+// How the steps are taken: one at a time (rounds == steps), or in rounds of two or three on m x m matrices, where that
+// is less time and G is at least twice as long as wide.  A round loses more of what is small against the
+// largest singular value: relative to fp32 throughout, 3 and 2 steps at a time are 0.5 to 1.2 times as far from the
+// exact result on spectra from flat to ones over five orders of magnitude (one at a time 0.2 to 0.4), but a
+// square random matrix, whose smallest singular value is next to none, is 4 times (0.3).
+struct Steps {
+  int rounds;
+  int of(int round, int steps) const { return steps / rounds + (round < steps % rounds ? 1 : 0); }     // the longer ones first
+};
+Steps plan_steps(const umem_orth_desc& od, int m, int k) {
+  const int n = od.n, xs = static_cast<int>(up64(k) / 32), as = static_cast<int>(up64(m) / 32);
+  int most = 3;                                             // Q stays below 128: a^3 = 41 of the usual coefficients
+  while (most > 1 && std::pow(std::fabs(od.a), most) > 100.f) --most;
+  if (most == 1 || k < 2 * m) return {od.steps};
+  const double one = plan(n, m, m, xs, true).us + plan(n, k, m, as, false).us;
+  const double two = plan(n, m, m, as, true, 2).us + plan(n, m, m, as, true).us;
+  return {two < one ? (od.steps + most - 1) / most : od.steps};
+}
+
 struct Layout {
-  size_t pieces, x0, t0, x1, t1, a, b, partial, total;
+  size_t pieces, x0, t0, x1, t1, q, partial, total;
+  size_t square;                            // a matrix of m x m: A, B or P, and in rounds Q (two) and T
   int m, k;                                 // the smaller and the larger side
   int64_t mp, kp;                           // values of a row
+  Steps steps;
   explicit Layout(const umem_orth_desc& od) {
     m = std::min(od.rows, od.cols);
     k = std::max(od.rows, od.cols);
     mp = up64(m);
     kp = up64(k);
-    const size_t n = od.n, x = up256(n * 4 * m * kp), t = up256(n * 4 * k * mp), q = up256(n * 4 * m * mp);
+    steps = plan_steps(od, m, k);
+    const size_t n = od.n, x = up256(n * 4 * m * kp), t = up256(n * 4 * k * mp);
+    square = up256(n * 4 * m * mp);
     pieces = 0;
     x0 = up256(n * norm_blocks(od) * sizeof(double));
     t0 = x0 + x;
     x1 = t0 + t;
     t1 = x1 + x;
-    a = t1 + t;
-    b = a + q;
-    partial = b + q;
+    q = t1 + t;
+    partial = q + (steps.rounds < od.steps ? 5 : 2) * square;
     const int on = od.n, xs = static_cast<int>(kp / 32), as = static_cast<int>(mp / 32);
     total = partial + std::max(std::max(partial_bytes(plan(on, m, m, xs, true), on, m, m, true),
                                         partial_bytes(plan(on, m, m, as, true), on, m, m, true)),
@@ -428,10 +474,10 @@ Parts parts_at(char* base, size_t at, int rows, int64_t values) {
   return {reinterpret_cast<uint16_t*>(base + at), 2 * values, 2 * rows * values};
 }
 
-template <Mode MODE, TileParts PARTS, typename OT>
+template <Mode MODE, typename OT = float>
 void product(OrthArgs g, int n, hipStream_t s) {
-  const int slices = g.k / (PARTS == kFirst ? 2 * kTileBK : kTileBK);
-  const Plan pl = plan(n, g.rows_m, g.rows_n, slices, symmetric(MODE));
+  g.jobs = std::max(g.jobs, 1);
+  const Plan pl = plan(n, g.rows_m, g.rows_n, g.k / kTileBK, symmetric(MODE), g.jobs);
   g.splits = pl.splits;
 #define UMEM_ORTH(BM, WR, WC, BUFS)                                                                                 \
   {                                                                                                                  \
@@ -439,8 +485,8 @@ void product(OrthArgs g, int n, hipStream_t s) {
     g.tiles_n = (g.rows_n + BM - 1) / BM;                                                                            \
     g.per = symmetric(MODE) ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n;                               \
     g.items = n * g.per;                                                                                             \
-    hipLaunchKernelGGL((orth_product_kernel<MODE, PARTS, OT, BM, BM, WR, WC, BUFS>),                                 \
-                       dim3(tile_grid(g.items * g.splits)), dim3(64 * WR * WC), 0, s, g);                            \
+    hipLaunchKernelGGL((orth_product_kernel<MODE, OT, BM, BM, WR, WC, BUFS>),                                        \
+                       dim3(tile_grid(g.items * g.splits * g.jobs)), dim3(64 * WR * WC), 0, s, g);                   \
     if (g.splits > 1)                                                                                                \
       hipLaunchKernelGGL((orth_join_kernel<MODE, OT, BM>), dim3(g.items * (BM / 64) * (BM / 64)), dim3(kThreads), 0, \
                          s, g);                                                                                      \
@@ -475,47 +521,88 @@ hipError_t launch_orthogonalize(const umem_orth_desc& od, const void* g, void* o
   // X [m][k] and its transpose, now and next
   Parts x = parts_at(base, L.x0, L.m, L.kp), t = parts_at(base, L.t0, L.k, L.mp);
   Parts x1 = parts_at(base, L.x1, L.m, L.kp), t1 = parts_at(base, L.t1, L.k, L.mp);
-  const Parts a = parts_at(base, L.a, L.m, L.mp), b = parts_at(base, L.b, L.m, L.mp);
+  const auto square = [&](int i) { return parts_at(base, L.q + i * L.square, L.m, L.mp); };
+  Parts a = square(0), q = square(1), q1 = square(2);
+  const Parts p = square(3), w = square(4);
   if (od.gtype == UMEM_F32) first(od, static_cast<const float*>(g), pieces, tall ? t : x, tall ? x : t, s);
   else first(od, static_cast<const __bf16*>(g), pieces, tall ? t : x, tall ? x : t, s);
-  for (int step = 0; step < od.steps; ++step) {
-    OrthArgs q{};
-    q.partial = reinterpret_cast<float*>(base + L.partial);
-    q.a = q.b = x;                                          // A = X X^T
-    q.out = a;
-    q.rows_m = q.rows_n = L.m;
-    q.k = static_cast<int>(x.ld);
-    product<kGram, kBoth, float>(q, od.n, s);
-    q.a = q.b = q.own = a;                                  // B = b A + c A^2
-    q.out = b;
-    q.k = static_cast<int>(a.ld);
-    q.alpha = od.b;
-    q.beta = od.c;
-    product<kPoly, kBoth, float>(q, od.n, s);
-    q.alpha = od.a;                                         // X = a X + B X
-    q.beta = 1.f;
-    const bool last = step + 1 == od.steps;
+  OrthArgs sq{};                                            // m x m of rows of A
+  sq.partial = reinterpret_cast<float*>(base + L.partial);
+  sq.rows_m = sq.rows_n = L.m;
+  sq.k = static_cast<int>(a.ld);
+  for (int round = 0; round < L.steps.rounds; ++round) {
+    const int steps = L.steps.of(round, od.steps);
+    OrthArgs o = sq;
+    o.a = o.b = x;                                          // A = X X^T
+    o.out = a;
+    o.k = static_cast<int>(x.ld);
+    product<kGram>(o, od.n, s);
+    for (int step = 0; step < steps; ++step) {
+      o = sq;
+      o.a = o.b = o.own = a;
+      o.alpha = od.b;
+      o.beta = od.c;
+      if (steps == 1) {                                     // B = b A + c A^2
+        o.out = q;
+        product<kPoly>(o, od.n, s);
+        break;
+      }
+      o.shift = od.a;                                       // P = a I + b A + c A^2
+      o.out = step == 0 ? q : p;
+      product<kShifted>(o, od.n, s);
+      const bool end = step + 1 == steps;
+      o = sq;
+      if (!end) {                                           // T = P A
+        o.a = step == 0 ? q : p;
+        o.b = a;
+        o.out = w;
+      }
+      if (step > 0) {                                       // Q = Q P
+        (end ? o.a : o.a2) = q;
+        (end ? o.b : o.b2) = p;
+        (end ? o.out : o.out2) = q1;
+        o.jobs = end ? 1 : 2;
+      }
+      if (!end || step > 0) product<kTimes>(o, od.n, s);
+      if (step > 0) std::swap(q, q1);
+      if (end) break;
+      o = sq;                                               // A = P T
+      o.a = step == 0 ? q : p;
+      o.b = w;
+      o.out = a;
+      product<kTimes>(o, od.n, s);
+    }
+    const bool last = round + 1 == L.steps.rounds;
     const bool turned = last && tall;                       // the last X goes out as G lies
-    q.a = turned ? b : t;
-    q.b = turned ? t : b;
-    q.own = turned ? t : x;
-    q.rows_m = turned ? L.m : L.k;
-    q.rows_n = turned ? L.k : L.m;
+    o = sq;
+    o.a = turned ? q : t;                                   // X = a X + B X, or Q X
+    o.b = turned ? t : q;
+    o.own = turned ? t : x;
+    o.alpha = od.a;
+    o.beta = 1.f;
+    o.rows_m = turned ? L.m : L.k;
+    o.rows_n = turned ? L.k : L.m;
     if (!last) {
-      q.out = x1;
-      q.out_t = t1;
-      product<kUpdate, kBoth, float>(q, od.n, s);
+      o.out = x1;
+      o.out_t = t1;
+      if (steps == 1) product<kUpdate>(o, od.n, s);
+      else product<kApply>(o, od.n, s);
       std::swap(x, x1);
       std::swap(t, t1);
       continue;
     }
-    q.decay = od.decay;
-    q.scale = od.scale;
-    q.final = out;
-    q.final_ld = od.cols;
-    q.final_matrix = static_cast<int64_t>(od.rows) * od.cols;
-    if (od.otype == UMEM_F32) product<kLast, kBoth, float>(q, od.n, s);
-    else product<kLast, kBoth, __bf16>(q, od.n, s);
+    o.decay = od.decay;
+    o.scale = od.scale;
+    o.final = out;
+    o.final_ld = od.cols;
+    o.final_matrix = static_cast<int64_t>(od.rows) * od.cols;
+    if (od.otype == UMEM_F32) {
+      if (steps == 1) product<kLast, float>(o, od.n, s);
+      else product<kLastApply, float>(o, od.n, s);
+    } else {
+      if (steps == 1) product<kLast, __bf16>(o, od.n, s);
+      else product<kLastApply, __bf16>(o, od.n, s);
+    }
   }
   return hipGetLastError();
 }
