@@ -189,7 +189,7 @@ __device__ __forceinline__ OrthTile orth_tile(const OrthArgs& g, int item) {
   return {mat, m, in - m * (m + 1) / 2};
 }
 
-// The four values (times 2^12) at row n, columns m .. m + 3.
+// The four values at row n, columns m .. m + 3.
 __device__ __forceinline__ f32x4 get_four(const Parts& in, int64_t mat, int n, int m) {
   const uint16_t* from = in.p + mat * in.matrix + n * in.ld + part_at(m);
   const u32x2 hi = *reinterpret_cast<const u32x2*>(from), lo = *reinterpret_cast<const u32x2*>(from + kPartStep);
@@ -287,15 +287,16 @@ __device__ __forceinline__ void put_block(const OrthArgs& g, const Parts& rows, 
   }
 }
 
-template <Mode MODE, typename OT, int BM, int BN, int WR, int WC, int BUFS>
-__global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(BM == 64 ? 3 : 2))) void orth_product_kernel(OrthArgs g) {
-  typedef Tile<true, BM, BN, WR, WC, BUFS, kBoth> Tl;
+template <Mode MODE, typename OT, int BM, int BN, int WR, int WC, int BUFS, int GROUPS>
+__global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_per_eu(BM == 64 ? 3 : 2))) void orth_product_kernel(OrthArgs g) {
+  typedef Tile<true, BM, BN, WR, WC, BUFS, kBoth, GROUPS> Tl;
   static_assert(BN == 64 ? 2 * BM * BN <= Tl::kElems : BN % 128 == 0 && BM * BN <= Tl::kElems,
                 "a tile of words fits the operands' LDS");
-  __shared__ __align__(16) uint16_t buf0[Tl::kElems];
-  __shared__ __align__(16) uint16_t buf1[Tl::kElems];
-  __shared__ __align__(16) uint16_t buf2[BUFS > 2 ? Tl::kElems : 8];
-  __shared__ __align__(16) uint16_t buf3[BUFS > 3 ? Tl::kElems : 8];
+  constexpr int kLds = GROUPS * Tl::kElems;
+  __shared__ __align__(16) uint16_t buf0[kLds];
+  __shared__ __align__(16) uint16_t buf1[kLds];
+  __shared__ __align__(16) uint16_t buf2[BUFS > 2 ? kLds : 8];
+  __shared__ __align__(16) uint16_t buf3[BUFS > 3 ? kLds : 8];
   const int all = g.items * g.splits * g.jobs, id = tile_item(all);
   if (id >= all) return;                                    // the whole workgroup: no barrier is skipped
   const int split = id / g.items, item = id - split * g.items;          // or of two products which one
@@ -316,10 +317,28 @@ __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(BM
   const int64_t slices = Tl::slices(p);
   const int part = g.jobs == 2 ? 0 : split;
   const int from = static_cast<int>(slices * part / g.splits), to = static_cast<int>(slices * (part + 1) / g.splits);
-  tile.run(p, from, to, buf0, buf1, buf2, buf3, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
+  const int group = Tl::group(), mine = group * Tl::kElems;
+  tile.run(p, from, to, buf0 + mine, buf1 + mine, buf2 + (BUFS > 2 ? mine : 0), buf3 + (BUFS > 3 ? mine : 0), acc);
+  const int lane = threadIdx.x & 63, wave = Tl::thread() >> 6, wr = wave / WC, wc = wave % WC;
   const int m_in = wr * Tl::MT * 16 + 4 * (lane >> 4), n_in = wc * Tl::NT * 16 + (lane & 15);
+  if constexpr (GROUPS == 2) {                              // the first group adds what the second has, and goes on alone
+    static_assert(BM * BN * 4 <= kLds * 2, "a group's sums fit a buffer");
+    f32x4* sums = reinterpret_cast<f32x4*>(buf1) + Tl::thread();
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < Tl::NT; ++j)
+#pragma unroll
+      for (int i = 0; i < Tl::MT; ++i)
+        if (group == 1) sums[(j * Tl::MT + i) * Tl::kThreads] = acc[i][j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < Tl::NT; ++j)
+#pragma unroll
+      for (int i = 0; i < Tl::MT; ++i)
+        if (group == 0) acc[i][j] += sums[(j * Tl::MT + i) * Tl::kThreads];
+  }
   if (g.splits > 1) {
+    if (group != 0) return;
     float* to = g.partial + static_cast<int64_t>(id) * (BM * BN);
 #pragma unroll
     for (int j = 0; j < Tl::NT; ++j)
@@ -337,13 +356,14 @@ __global__ __launch_bounds__(64 * WR * WC) __attribute__((amdgpu_waves_per_eu(BM
   for (int j = 0; j < Tl::NT; ++j)
 #pragma unroll
     for (int i = 0; i < Tl::MT; ++i) {
+      if (group != 0) break;
       const int n = n_in + j * 16, m = m_in + i * 16;
       const u32x4 w = finish_four<MODE, OT>(g, at.mat, at.n * BN + n, at.m * BM + m, acc[i][j]);
       if (!is_last(MODE)) *reinterpret_cast<u32x4*>(word(n, m)) = w;
     }
   if (is_last(MODE)) return;
   __syncthreads();
-  put_block<MODE, BM, BN, Tl::kThreads>(g, second ? g.out2 : g.out, at.mat, at.m * BM, at.n * BN, at.m != at.n, word);
+  put_block<MODE, BM, BN, Tl::kThreads * GROUPS>(g, second ? g.out2 : g.out, at.mat, at.m * BM, at.n * BN, at.m != at.n, word);
 }
 
 // The sums of the splits, in their order, and what a product does with them; a 64 x 64 block of a tile a workgroup.
@@ -388,6 +408,7 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 struct Plan {
   int bm, splits;
   double us;
+  bool alone;             // every workgroup has a CU to itself: two groups of waves share its slices
 };
 constexpr int kMostSplits = 16, kCus = 256;
 constexpr size_t kPartialBytes = size_t{64} << 20;
@@ -396,7 +417,7 @@ int64_t tile_count(int bm, int n, int rows_m, int rows_n, bool sym) {
   return n * (sym ? tm * (tm + 1) / 2 : tm * tn);
 }
 Plan plan(int n, int rows_m, int rows_n, int slices, bool sym, int jobs = 1) {
-  Plan best{64, 1, 1e300};
+  Plan best{64, 1, 1e300, false};
   for (int bm : {64, 128}) {
     const int64_t it = tile_count(bm, n, rows_m, rows_n, sym);
     for (int s = 1; s <= (jobs == 2 ? 1 : kMostSplits) && s <= slices; ++s) {
@@ -410,9 +431,9 @@ Plan plan(int n, int rows_m, int rows_n, int slices, bool sym, int jobs = 1) {
       } else {
         const int rest = static_cast<int>(cus % 3);
         cost += static_cast<double>(cus / 3) * (3.0 + 0.6 * each);
-        if (rest) cost += 3.0 + (rest == 1 ? 0.25 : 0.4) * each;
+        if (rest) cost += 3.0 + (cus == 1 ? 0.15 : rest == 1 ? 0.25 : 0.4) * each;
       }
-      if (cost < best.us) best = {bm, s, cost};
+      if (cost < best.us) best = {bm, s, cost, bm == 64 && cus == 1 && each >= 4};
     }
   }
   return best;
@@ -479,20 +500,21 @@ void product(OrthArgs g, int n, hipStream_t s) {
   g.jobs = std::max(g.jobs, 1);
   const Plan pl = plan(n, g.rows_m, g.rows_n, g.k / kTileBK, symmetric(MODE), g.jobs);
   g.splits = pl.splits;
-#define UMEM_ORTH(BM, WR, WC, BUFS)                                                                                 \
+#define UMEM_ORTH(BM, WR, WC, BUFS, GROUPS)                                                                               \
   {                                                                                                                  \
     g.tiles_m = (g.rows_m + BM - 1) / BM;                                                                            \
     g.tiles_n = (g.rows_n + BM - 1) / BM;                                                                            \
     g.per = symmetric(MODE) ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n;                               \
     g.items = n * g.per;                                                                                             \
-    hipLaunchKernelGGL((orth_product_kernel<MODE, OT, BM, BM, WR, WC, BUFS>),                                        \
-                       dim3(tile_grid(g.items * g.splits * g.jobs)), dim3(64 * WR * WC), 0, s, g);                   \
+    hipLaunchKernelGGL((orth_product_kernel<MODE, OT, BM, BM, WR, WC, BUFS, GROUPS>),                                        \
+                       dim3(tile_grid(g.items * g.splits * g.jobs)), dim3(64 * WR * WC * GROUPS), 0, s, g);                   \
     if (g.splits > 1)                                                                                                \
       hipLaunchKernelGGL((orth_join_kernel<MODE, OT, BM>), dim3(g.items * (BM / 64) * (BM / 64)), dim3(kThreads), 0, \
                          s, g);                                                                                      \
   }
-  if (pl.bm == 128) UMEM_ORTH(128, 4, 2, 4)
-  else UMEM_ORTH(64, 2, 2, 3)
+  if (pl.bm == 128) UMEM_ORTH(128, 4, 2, 4, 1)
+  else if (pl.alone) UMEM_ORTH(64, 2, 2, 3, 2)
+  else UMEM_ORTH(64, 2, 2, 3, 1)
 #undef UMEM_ORTH
 }
 

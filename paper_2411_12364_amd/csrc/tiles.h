@@ -63,9 +63,11 @@ typedef __attribute__((address_space(3))) uint32_t lds_u32;
 
 // BM x BN tile of WR x WC waves; acc[a][b]: the 16 x 16 block at m = wave's row + 16 a, n = wave's column + 16 b,
 // of which lane l holds m = 4 (l / 16) + 0 .. 3, n = l % 16.
-template <bool F16, int BM, int BN, int WR, int WC, int BUFS, TileParts PARTS = kPlain>
+// GROUPS > 1: as many sets of waves, each with buffers of its own, take a share of the slices; the caller adds their
+// accumulators.
+template <bool F16, int BM, int BN, int WR, int WC, int BUFS, TileParts PARTS = kPlain, int GROUPS = 1>
 struct Tile {
-  static constexpr int kThreads = 64 * WR * WC;
+  static constexpr int kThreads = 64 * WR * WC;                              // of a group
   static constexpr int MT = BM / WR / 16, NT = BN / WC / 16;
   static constexpr int kA = BM * 8 / kThreads, kB = BN * 8 / kThreads;       // 16-byte pieces a thread loads
   static constexpr int kElems = (BM + BN) * kTileBK;                         // one buffer
@@ -77,12 +79,18 @@ struct Tile {
   int col_k;                              // first k of the lane's pieces in a slice, the same for all of them
   int m0, n0;
 
+  // The thread within its group, and the group.
+  __device__ __forceinline__ static int thread() { return GROUPS == 1 ? threadIdx.x : threadIdx.x % kThreads; }
+  __device__ __forceinline__ static int group() {
+    return GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  }
+
   // The lane's offsets for the tile at (m0, n0).  A row's number mod 8 is the same for all pieces of a lane
   // (the pieces lie kThreads / 8 rows apart), so their column is too.
   __device__ __forceinline__ void init(const TilePairs& p, int m0_, int n0_) {
     m0 = min(m0_, p.a_rows - 1);            // (a tile past the rows that there are reads the last one)
     n0 = min(n0_, p.b_rows - 1);
-    const int tid = threadIdx.x, row = tid >> 3, col = (tid & 7) ^ (row & 7);
+    const int tid = thread(), row = tid >> 3, col = (tid & 7) ^ (row & 7);
     col_k = col * 8;
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
@@ -106,7 +114,7 @@ struct Tile {
   // The slice from k0 on into a buffer; a piece past k is another one here (past_k).
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t a, __amdgpu_buffer_rsrc_t b, int k0, int k,
                                        uint16_t* lds) const {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(thread() >> 6);
     const auto get = [&](uint32_t back) {
 #pragma unroll
       for (int i = 0; i < kA; ++i)
@@ -127,7 +135,7 @@ struct Tile {
     if (k0 + col_k >= k) {
 #pragma unroll
       for (int i = 0; i < kA + kB; ++i) {
-        uint16_t* piece = lds + (i < kA ? 0 : BM * kTileBK) + ((i < kA ? i : i - kA) * kThreads + threadIdx.x) * 8;
+        uint16_t* piece = lds + (i < kA ? 0 : BM * kTileBK) + ((i < kA ? i : i - kA) * kThreads + thread()) * 8;
         *reinterpret_cast<u32x4*>(piece) = u32x4{0u, 0u, 0u, 0u};
       }
     }
@@ -140,7 +148,7 @@ struct Tile {
     u32x4 a[2][MT], b[2][NT];
   };
   __device__ __forceinline__ static void read(const uint16_t* lds, int half, Fragments& f) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = thread() >> 6;
     const int wr = wave / WC, wc = wave % WC;
     const int r = lane & 15, q = lane >> 4;
     const uint16_t* a = lds + (wr * MT * 16 + r) * kTileBK;
@@ -192,7 +200,7 @@ struct Tile {
   // The slices of p's pairs laid one after another.
   __device__ __forceinline__ static int slices(const TilePairs& p) { return p.n * ((p.k + kStep - 1) / kStep); }
 
-  // The product over the slices [from, to) of them, to > from, through BUFS buffers.  Past the last slice that one is
+  // The product over the slices [from, to) of them, to > from (of a group: its share), through BUFS buffers.  Past the last slice that one is
   // loaded again, and the loop has one end: with loads that may or may not be there, and with an exit in its midst, the
   // compiler waits for all loads before a read.  All loads have landed when this returns; all waves have read the last
   // slice only after a barrier.
@@ -207,10 +215,13 @@ struct Tile {
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[s][i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int k = p.k, per = (k + kStep - 1) / kStep;
-    int s = from / per, k0 = (from - s * per) * kStep;      // the next slice to load
+    // Groups meet at the same barriers: each walks as many slices as the largest share has, and leaves out what is not its own.
+    const int share = (to - from + GROUPS - 1) / GROUPS, first = from + group() * share;
+    int mine = GROUPS == 1 ? share : min(share, to - first);
+    const int k = p.k, per = (k + kStep - 1) / kStep, start = GROUPS == 1 ? first : min(first, to - 1);
+    int s = start / per, k0 = (start - s * per) * kStep;    // the next slice to load
     int at = k0;                                            // where in k the next slice to compute lies
-    int left = to - from, ahead = left;                     // slices to compute, to load
+    int left = share, ahead = mine;                         // slices to compute, to load
     const uint16_t *pa = nullptr, *pb = nullptr;
     const auto point = [&] {
       pa = p.a[0];
@@ -240,7 +251,7 @@ struct Tile {
         landed<BUFS - 2>(at, k, bufs[i]);                   // in flight: the BUFS - 2 slices after this one
         at = at + kStep >= k ? 0 : at + kStep;
         fetch(bufs[(i + BUFS - 1) % BUFS]);
-        compute(bufs[i], acc);
+        if (GROUPS == 1 || mine-- > 0) compute(bufs[i], acc);
       }
     }
     // the last slices, fewer than the buffers, are all there or on their way
@@ -249,7 +260,7 @@ struct Tile {
       if (i < left) {
         landed<0>(at, k, bufs[i]);
         at = at + kStep >= k ? 0 : at + kStep;
-        compute(bufs[i], acc);
+        if (GROUPS == 1 || mine-- > 0) compute(bufs[i], acc);
       }
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);
