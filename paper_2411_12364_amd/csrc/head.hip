@@ -327,6 +327,8 @@ __device__ __forceinline__ float most_of(const float* most) {
 
 // r of a piece of the vocabulary, over s and the largest dloss: rows[part][T][piece] in PR bf16 parts, and times 2^15
 // cols[part][piece][t_ld] in PC fp16 parts; zeros past the piece's rows of W, past T and for tokens without a target.
+// lost: what of a target's r one bf16 part of it does not hold, [T] (of it alone r is near the largest dloss in most
+// tokens; dx adds it times W's row: half the error of dx is without that from there).
 // A part at a time goes through LDS, [token][v], its 16-byte pieces permuted by the token's number so that
 // both orders of reading meet all banks.  (Parts kept from one to the next spill 360 registers: 430 us of 620 were the
 // end of a tile.)
@@ -339,7 +341,8 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
                                                                  const float* __restrict__ dloss,
                                                                  const float* __restrict__ most, int v_first, int vocab,
                                                                  int piece, int t_ld, uint16_t* __restrict__ rows,
-                                                                 uint16_t* __restrict__ cols) {
+                                                                 uint16_t* __restrict__ cols,
+                                                                 float* __restrict__ lost) {
   typedef Tile<false, BM, BN, WR, WC, 2> Tl;
   static_assert(BM * BN <= 2 * Tl::kElems && BM % 64 == 0 && BN % 64 == 0, "a tile of bf16 fits the operands' LDS");
   __shared__ __align__(16) uint16_t buf0[Tl::kElems];
@@ -368,6 +371,10 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
         const int v = at.m * BM + m0 + i * 16 + r;
         const float e = __expf(fmaf(acc[i][j][r], scale, -l)) - (v_first + v == y ? 1.f : 0.f);
         acc[i][j][r] = on && v < V ? g * e : 0.f;
+        if (PR == 1 && on && v_first + v == y && v < V) {
+          const float part = bits_f32(bf16_bits(acc[i][j][r]));
+          lost[t] = fabsf(part) <= 3.4e38f ? acc[i][j][r] - part : 0.f;
+        }
       }
   }
   // token n's first element; its 16-byte piece c is at place c ^ turn(n)
@@ -447,7 +454,15 @@ struct ProductArgs {
   const float *most, *x_most;
   const int32_t* targets;
   int vocab;
+  const float* lost;      // with targets: [T], times W's row of the target is added to D
+  const uint16_t* w;
 };
+
+// What is added to row t of dx, columns m .. m + 3, before it is scaled.
+__device__ __forceinline__ f32x4 lost_row(const ProductArgs& g, int t, int m) {
+  const u32x2 b = *reinterpret_cast<const u32x2*>(g.w + g.targets[t] * g.ld + m);
+  return g.lost[t] * f32x4{bits_f32(b.x & 0xffffu), bits_f32(b.x >> 16), bits_f32(b.y & 0xffffu), bits_f32(b.y >> 16)};
+}
 
 // f of the output.
 __device__ __forceinline__ float product_factor(const ProductArgs& g) {
@@ -491,6 +506,7 @@ __global__ __launch_bounds__(64 * WR * WC) void head_product_kernel(TilePairs p,
         continue;
       }
       if (g.whole && g.before) v += *reinterpret_cast<const f32x4*>(g.before + o);
+      if (g.lost && !off) v += lost_row(g, n, m);
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], back) * f;
       if (!g.whole && g.before) v += *reinterpret_cast<const f32x4*>(g.before + o);
@@ -514,8 +530,10 @@ __global__ __launch_bounds__(kThreads) void head_sum_kernel(ProductArgs g, int T
   if (i >= size) return;
   f32x4 v = *reinterpret_cast<const f32x4*>(g.sums + i);
   for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(g.sums + s * size + i);
-  v *= f;
-  if (!counts(g.targets, static_cast<int>(i / d), g.vocab)) v = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int t = static_cast<int>(i / d);
+  const bool on = counts(g.targets, t, g.vocab);
+  if (g.lost && on) v += lost_row(g, t, static_cast<int>(i % d));
+  v = on ? v * f : f32x4{0.f, 0.f, 0.f, 0.f};
   OT* out = static_cast<OT*>(g.out) + i;
   if constexpr (sizeof(OT) == 4)
     *reinterpret_cast<f32x4*>(out) = v;
@@ -528,9 +546,37 @@ __global__ __launch_bounds__(kThreads) void head_sum_kernel(ProductArgs g, int T
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Tiles of 256 x 256 where there are enough rows of both operands, else of 64 x 64.
-constexpr int kSmallTokens = 128;
-bool large_tiles(int m, int n) { return m > 128 && n > kSmallTokens; }
+// A product's tiles, and how often its slices are split, by what the sizes of tile measured (us a slice): 256 x 256,
+// eight waves and a CU to itself, 1.7; 128 x 128, two to a CU, 0.95 both, 0.55 alone; 64 x 64, up to four to a CU, 0.25 alone
+// and 0.2 more with each beside it.  So large tiles where there is one for each CU (7,168 x 8,192 over 2,048: 1.7 a slice
+// for 16 tiles of 64 x 64, which take 3.4), small ones where there are few: 600 x 2,314 over 1,696 46 in 27 large ones, 20 in
+// 95 of 128 x 128.  Small ones are taken up to 4,096 of them.
+constexpr int kCus = 256, kManyTiles = 4096;
+struct TilePlan {
+  int side, splits;
+};
+TilePlan tile_plan(int64_t m, int64_t n, int slices, int most_splits, bool largest) {
+  TilePlan best{64, 1};
+  double least = 1e300;
+  for (int side : {64, 128, 256}) {
+    const int64_t tiles = ((m + side - 1) / side) * ((n + side - 1) / side);
+    if (side == 256 ? !largest : tiles > (side == 128 && !largest ? INT64_MAX : kManyTiles)) continue;
+    for (int s = 1; s <= most_splits && (s == 1 || 8 * s <= slices); ++s) {
+      const int64_t full = (tiles * s + kCus - 1) / kCus;   // of the fullest CU
+      const double each = (slices + s - 1) / s, whole = static_cast<double>(full);
+      double us = s > 1 ? 4.0 + 8e-6 * m * n * s / 3.0 : 0.0;
+      if (side == 256) us += whole * (4.0 + 1.7 * each);
+      else if (side == 128) us += static_cast<double>(full / 2) * (4.0 + 0.95 * each) + (full % 2 ? 4.0 + 0.55 * each : 0.0);
+      else us += static_cast<double>(full / 4) * (4.0 + 0.85 * each) + (full % 4 ? 3.0 + (0.05 + 0.2 * (full % 4)) * each : 0.0);
+      if (us < least) {
+        least = us;
+        best = {side, s};
+      }
+    }
+  }
+  return best;
+}
+int slice_count(int64_t k, int pairs) { return static_cast<int>((k + kTileBK - 1) / kTileBK) * pairs; }
 
 int x_parts(const umem_head_desc& hd) { return hd.xtype == UMEM_F32 ? 3 : 1; }
 int row_parts(const umem_head_desc& hd) { return hd.xtype == UMEM_F32 ? 3 : 1; }       // of r, for dx
@@ -554,36 +600,37 @@ int piece_rows(const umem_head_desc& hd, int T) {
   return static_cast<int>(up((hd.vocab + pieces - 1) / pieces, 256));
 }
 
-// How often k of dx's product is split: to fill the chip where its tiles are few.  (Their sums' values: tiles of 256 x 256
-// that are split are 128 at most, of all splits 256; those of 64 x 64 are smaller.)
-constexpr int kMostSplits = 8, kLargeWorkgroups = 256, kSmallWorkgroups = 768;
-int dx_splits(const umem_head_desc& hd, int T) {
-  const bool large = large_tiles(hd.d, T);
-  const int side = large ? 256 : 64;
-  const int64_t tiles = (up(hd.d, side) / side) * (up(T, side) / side);
-  const int64_t most = std::min<int64_t>(kMostSplits, piece_rows(hd, T) * row_parts(hd) / 512);
-  return static_cast<int>(std::max<int64_t>(1, std::min(most, (large ? kLargeWorkgroups : kSmallWorkgroups) / tiles)));
+// dx's product: k is split where its tiles are few.  (Tiles that are split are as many, with their splits, as the chip
+// holds at most: four of 64 x 64 a CU, two of 128 x 128, one of 256 x 256.)
+constexpr int kMostSplits = 32;
+TilePlan dx_plan(const umem_head_desc& hd, int T) {
+  TilePlan p = tile_plan(hd.d, T, slice_count(piece_rows(hd, T), row_parts(hd)), kMostSplits, true);
+  const int64_t tiles = (up(hd.d, p.side) / p.side) * (up(T, p.side) / p.side);
+  const int64_t most = p.side == 256 ? kCus : p.side == 128 ? 2 * kCus : 4 * kCus;
+  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(p.splits, most / tiles)));
+  return p;
 }
 size_t sum_values(const umem_head_desc& hd, int T) {
   const size_t x = static_cast<size_t>(T) * hd.d;
-  return std::max(x, std::min(kMostSplits * x, static_cast<size_t>(kLargeWorkgroups) * 256 * 256));
+  return std::max(x, std::min(kMostSplits * x, static_cast<size_t>(kCus) * 256 * 256));
 }
 
 // The forward goes by bands of tokens, so that its scratch and its grids are bounded; a workspace for T tokens holds what
-// the small tiles of fewer need.
+// fewer need.
 constexpr int kBandTokens = 1 << 15, kFewTokens = 512;
 struct ForwardLayout {
   size_t parts, stats, goal, total;
   ForwardLayout(const umem_head_desc& hd, int T) {
     const size_t t = std::min(T, kBandTokens), d = hd.d, small = (hd.vocab + 63) / 64, large = (hd.vocab + 255) / 256;
+    // (4,096 tiles of 64 or 128 tokens' width at most hold 2^19 pairs)
     parts = 0;
     stats = up256(hd.xtype == UMEM_F32 ? 3 * t * d * 2 : 0);
-    goal = stats + up256(sizeof(float2) * (large_tiles(hd.vocab, T) ? std::max(small * kSmallTokens, large * t) : small * t));
+    goal = stats + up256(sizeof(float2) * std::max(large * t, std::min(small * t, size_t{1} << 19)));
     total = goal + up256(t * sizeof(float));
   }
 };
 struct BackwardLayout {
-  size_t parts, xt, wt, rows, cols, sum, most, x_most, total;
+  size_t parts, xt, wt, rows, cols, sum, most, x_most, lost, total;
   BackwardLayout(const umem_head_desc& hd, int T) {
     const size_t t = T, tp = token_row(T), d = hd.d, values = piece_values(hd, T);
     parts = 0;
@@ -594,7 +641,8 @@ struct BackwardLayout {
     sum = cols + up256(col_parts(hd) * values * 2);
     most = sum + up256(sum_values(hd, T) * sizeof(float));
     x_most = most + up256(kMostBlocks * sizeof(float));
-    total = x_most + up256(kMostBlocks * sizeof(float));
+    lost = x_most + up256(kMostBlocks * sizeof(float));
+    total = lost + up256(t * sizeof(float));
   }
 };
 
@@ -620,7 +668,7 @@ void split_x(const umem_head_desc& hd, int T, const void* x, uint16_t* parts, hi
 }
 
 template <bool F16, typename OT>
-void product(const TilePairs& p, ProductArgs g, hipStream_t s) {
+void product(const TilePairs& p, ProductArgs g, int side, hipStream_t s) {
 #define UMEM_PRODUCT(BM, BN, WR, WC)                                                                            \
   {                                                                                                             \
     g.tiles_m = (p.a_rows + BM - 1) / BM;                                                                       \
@@ -628,7 +676,8 @@ void product(const TilePairs& p, ProductArgs g, hipStream_t s) {
     hipLaunchKernelGGL((head_product_kernel<F16, OT, BM, BN, WR, WC>),                                          \
                        dim3(tile_grid(g.tiles_m * g.tiles_n * g.splits)), dim3(64 * WR * WC), 0, s, p, g);      \
   }
-  if (large_tiles(p.a_rows, p.b_rows)) UMEM_PRODUCT(256, 256, 2, 4)
+  if (side == 256) UMEM_PRODUCT(256, 256, 2, 4)
+  else if (side == 128) UMEM_PRODUCT(128, 128, 2, 2)
   else UMEM_PRODUCT(64, 64, 2, 2)
 #undef UMEM_PRODUCT
 }
@@ -636,15 +685,16 @@ void product(const TilePairs& p, ProductArgs g, hipStream_t s) {
 template <int PR, int PC>
 void slope(const TilePairs& p, float scale, const int32_t* targets, const float* lse, const float* dloss,
            const float* most, int v_first, int vocab, int piece, int t_ld, uint16_t* rows, uint16_t* cols,
-           hipStream_t s) {
+           float* lost, hipStream_t s) {
 #define UMEM_SLOPE(BM, BN, WR, WC)                                                                              \
   {                                                                                                             \
     const int tm = (piece + BM - 1) / BM, tn = (p.b_rows + BN - 1) / BN;                                        \
     hipLaunchKernelGGL((head_slope_kernel<BM, BN, WR, WC, PR, PC>), dim3(tile_grid(tm * tn)),                   \
                        dim3(64 * WR * WC), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first, vocab,    \
-                       piece, t_ld, rows, cols);                                                                \
+                       piece, t_ld, rows, cols, lost);                                                          \
   }
-  if (large_tiles(piece, p.b_rows)) UMEM_SLOPE(128, 128, 2, 2)
+  // (of 256 x 256 tiles one at a time is on a CU, and nothing beside its end: 340 us, so 316)
+  if (tile_plan(piece, p.b_rows, slice_count(p.k, p.n), 1, false).side == 128) UMEM_SLOPE(128, 128, 2, 2)
   else UMEM_SLOPE(64, 64, 2, 2)
 #undef UMEM_SLOPE
 }
@@ -674,7 +724,9 @@ hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, cons
     hipLaunchKernelGGL((head_stats_kernel<BM, BN, WR, WC>), dim3(tile_grid(tiles * tn)), dim3(64 * WR * WC), 0, \
                        s, p, tiles, tn, hd.scale, targets + t0, stats, goal);                                   \
   }
-    if (large_tiles(hd.vocab, T)) UMEM_STATS(256, 256, 2, 4)
+    const int side = tile_plan(hd.vocab, t, slice_count(p.k, p.n), 1, true).side;
+    if (side == 256) UMEM_STATS(256, 256, 2, 4)
+    else if (side == 128) UMEM_STATS(128, 128, 2, 2)
     else UMEM_STATS(64, 64, 2, 2)
 #undef UMEM_STATS
     if (t <= kFewTokens)
@@ -703,6 +755,7 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
   const bool wide = hd.xtype == UMEM_F32;
   float* most = dloss ? reinterpret_cast<float*>(base + L.most) : nullptr;
   float* x_most = reinterpret_cast<float*>(base + L.x_most);
+  float* lost = reinterpret_cast<float*>(base + L.lost);
   if (dloss)
     hipLaunchKernelGGL(head_most_kernel, dim3(kMostBlocks), dim3(kThreads), 0, s, dloss, targets, T, V, most);
   // x's channels along rows, tokens along k
@@ -720,7 +773,8 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
                        static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_ld), x_most, targets, V);
   }
   ProductArgs gx{}, gw{};
-  gx.splits = dx_splits(hd, T);
+  const TilePlan plan_x = dx_plan(hd, T);
+  gx.splits = plan_x.splits;
   gx.sums = sum;
   gx.whole = true;
   gw.splits = 1;
@@ -734,7 +788,7 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     const uint16_t* wp = w + static_cast<int64_t>(v0) * d;
     const TilePairs z = logit_pairs(hd, T, x, parts, wp, v);
     const auto make = pr == 3 ? (pc == 2 ? slope<3, 2> : slope<3, 1>) : (pc == 2 ? slope<1, 2> : slope<1, 1>);
-    make(z, hd.scale, targets, lse, dloss, most, v0, V, piece, t_ld, rows, cols, s);
+    make(z, hd.scale, targets, lse, dloss, most, v0, V, piece, t_ld, rows, cols, lost, s);
     // dx: channels along m, tokens along n, the piece along k
     hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), dim3(piece / 64, (d + 63) / 64), dim3(kThreads), 0, s, wp, v,
                        d, wt, static_cast<int64_t>(piece), nullptr, nullptr, 0);
@@ -755,9 +809,11 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     gx.scale = last ? hd.scale : 1.f;
     gx.most = last ? most : nullptr;
     gx.targets = last ? targets : nullptr;
+    gx.lost = last && pr == 1 ? lost : nullptr;
+    gx.w = w;
     gx.vocab = V;
-    if (!last || wide) product<false, float>(p, gx, s);
-    else product<false, __bf16>(p, gx, s);
+    if (!last || wide) product<false, float>(p, gx, plan_x.side, s);
+    else product<false, __bf16>(p, gx, plan_x.side, s);
     // dW: channels along m, the piece's rows along n, tokens along k; of fp32 x and two parts of r the pairs that count
     p = TilePairs{};
     const int64_t x_part = static_cast<int64_t>(d) * t_ld, c_part = static_cast<int64_t>(piece) * t_ld;
@@ -771,15 +827,16 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     p.b_rows = v;
     p.k = t_pad;
     p.a_ld = p.b_ld = t_ld;
+    const int side = tile_plan(d, v, slice_count(p.k, p.n), 1, true).side;
     const int64_t w_at = static_cast<int64_t>(v0) * d;
     if (hd.gtype == UMEM_F32) {
       float* g = static_cast<float*>(dw) + w_at;
       gw.out = g;
       gw.before = accumulate ? g : nullptr;
-      product<true, float>(p, gw, s);
+      product<true, float>(p, gw, side, s);
     } else {
       gw.out = static_cast<__bf16*>(dw) + w_at;
-      product<true, __bf16>(p, gw, s);
+      product<true, __bf16>(p, gw, side, s);
     }
   }
   if (gx.splits > 1) {
