@@ -3,7 +3,9 @@
 //   out[t] = s E[ids[t]],    dE[v] += s sum over t with ids[t] = v of dout[t]
 //
 // Both move memory and compute next to nothing.  The gradient sorts the (token, place) pairs, so that every row of the
-// table is summed by its places in order: no atomics, the same bits each time.  A wave takes a run of sorted places
+// table is summed by its places in order: no atomics, the same bits each time.  Up to 4,096 places are sorted by one
+// workgroup in LDS, up to 12,288 by a launch a pass, as a chain of short launches costs more than what they do (8,192
+// places: 15 us in two, 23 by sort.hip's six).  A wave takes a run of sorted places
 // and 256 columns; a row that begins and ends within its run is written at once, what is left at
 // the run's two ends goes to scratch, and a second kernel adds the pieces of rows that pass from run to run.
 #include <algorithm>
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_keys_kernel(const int32_t*
 }
 
 // Rows by their order: a sorted place begins a row where its key is another than the one before.
-constexpr int kRankTile = 4096;
+constexpr int kRankTile = 1024;
 
 __device__ __forceinline__ bool begins(const uint2* pairs, int e) { return e == 0 || pairs[e - 1].x != pairs[e].x; }
 
@@ -152,6 +154,196 @@ __global__ __launch_bounds__(kThreads) void embed_rank_kernel(const uint2* __res
     __syncthreads();
   }
   if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *n_rows = static_cast<int32_t>(run);
+}
+
+// The lanes that have this lane's 8-bit digit.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit) {
+  uint64_t peers = ~0ull;
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    const bool one = digit >> b & 1u;
+    const uint64_t ones = __ballot(one);
+    peers &= one ? ones : ~ones;
+  }
+  return peers;
+}
+
+// Up to kSmallWaves * 64 * STEPS places by one workgroup: a stable radix sort by 8 bits of the key a pass, of words that
+// hold key and place.  A wave ranks its own places, 64 a step, by its running counts of the digit and the lanes
+// below with the same one; the words then change places in LDS.  Places without a row have the key `vocab`, past all
+// rows.  With place the rows' order as well: place, rows and n_rows as embed_rank_kernel writes them.
+constexpr int kSmallWaves = 16, kSmallThreads = kSmallWaves * kWave, kSmallSteps = 4;
+constexpr int kSmallPlaces = kSmallThreads * kSmallSteps;
+
+template <int STEPS>
+__global__ __launch_bounds__(kSmallThreads) void embed_sort_kernel(const int32_t* __restrict__ ids, int T, int vocab,
+                                                                   int place_bits, int passes, uint2* __restrict__ pairs,
+                                                                   uint32_t* __restrict__ n_pairs,
+                                                                   uint32_t* __restrict__ place, int32_t* __restrict__ rows,
+                                                                   int32_t* __restrict__ n_rows) {
+  constexpr int kPlaces = kSmallThreads * STEPS;
+  __shared__ uint32_t words[kPlaces];
+  __shared__ uint16_t count[kSmallWaves][256];
+  __shared__ uint32_t wave_sum[kSmallWaves], total;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int first = wave * STEPS * kWave + lane;
+  uint32_t w[STEPS];
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) {
+    const int t = first + q * kWave;
+    const uint32_t id = t < T ? static_cast<uint32_t>(ids[t]) : 0u;
+    const uint32_t key = min(id, static_cast<uint32_t>(vocab));
+    w[q] = t < T ? key << place_bits | static_cast<uint32_t>(t) : 0xffffffffu;
+  }
+  if (tid == 0) total = static_cast<uint32_t>(T);
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = place_bits + 8 * pass;
+#pragma unroll
+    for (int i = 0; i < 256 / kWave; ++i) count[wave][i * kWave + lane] = 0;
+    wave_lds_order();
+    uint16_t rank[STEPS];
+#pragma unroll
+    for (int q = 0; q < STEPS; ++q) {
+      const uint32_t digit = w[q] >> shift & 255u;
+      const uint64_t peers = same_digit(digit);
+      const uint32_t below = static_cast<uint32_t>(__popcll(peers & lanemask_lt()));
+      const uint32_t have = count[wave][digit];
+      rank[q] = static_cast<uint16_t>(have + below);
+      wave_lds_order();
+      if (below == 0) count[wave][digit] = static_cast<uint16_t>(have + __popcll(peers));
+      wave_lds_order();
+    }
+    __syncthreads();
+    // where each wave's first place of each digit goes: the digits before, then the waves before
+    uint32_t all = 0;
+    if (tid < 256) {
+#pragma unroll
+      for (int v = 0; v < kSmallWaves; ++v) all += count[v][tid];
+    }
+    const uint32_t incl = static_cast<uint32_t>(wave_inclusive_scan(static_cast<int>(all)));
+    if (lane == kWave - 1) wave_sum[wave] = incl;
+    __syncthreads();
+    if (tid < 256) {
+      uint32_t at = incl - all;
+#pragma unroll
+      for (int v = 0; v < 256 / kWave; ++v) at += v < wave ? wave_sum[v] : 0u;
+#pragma unroll
+      for (int v = 0; v < kSmallWaves; ++v) {
+        const uint32_t c = count[v][tid];
+        count[v][tid] = static_cast<uint16_t>(at);          // below 2^16: the places are at most 2^15
+        at += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < STEPS; ++q) words[count[wave][w[q] >> shift & 255u] + rank[q]] = w[q];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < STEPS; ++q) w[q] = words[first + q * kWave];
+  }
+  // (a wave's words are its own from here on but for the one before them)
+  const uint32_t mask = (1u << place_bits) - 1u;
+  uint32_t starts = 0;
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) {
+    const int e = first + q * kWave;
+    const uint32_t key = w[q] >> place_bits;
+    const uint32_t left = e > 0 ? words[e - 1] >> place_bits : 0xffffffffu;
+    const bool row = key < static_cast<uint32_t>(vocab);
+    if (row) pairs[e] = make_uint2(key, w[q] & mask);
+    if (!row && e < T && (e == 0 || left < static_cast<uint32_t>(vocab))) total = static_cast<uint32_t>(e);
+    starts += static_cast<uint32_t>(__popcll(__ballot(row && left != key)));
+  }
+  if (lane == 0) wave_sum[wave] = starts;
+  __syncthreads();
+  if (tid == 0) *n_pairs = total;
+  if (place == nullptr) return;
+  uint32_t run = 0, rows_all = 0;
+#pragma unroll
+  for (int v = 0; v < kSmallWaves; ++v) {
+    run += v < wave ? wave_sum[v] : 0u;
+    rows_all += wave_sum[v];
+  }
+  if (tid == 0) *n_rows = static_cast<int32_t>(rows_all);
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) {
+    const int e = first + q * kWave;
+    const uint32_t key = w[q] >> place_bits;
+    const bool row = key < static_cast<uint32_t>(vocab), begin = row && (e == 0 || words[e - 1] >> place_bits != key);
+    const uint64_t ballot = __ballot(begin);
+    const uint32_t at = run + static_cast<uint32_t>(__popcll(ballot & (lanemask_lt() << 1 | 1ull))) - 1u;   // rows begun up to e
+    if (row) place[e] = at;
+    if (begin) rows[at] = static_cast<int32_t>(key);
+    run += static_cast<uint32_t>(__popcll(ballot));
+  }
+}
+
+// One pass over up to kPassPlaces places, a tile of 512 a workgroup: it counts all digits itself, those of the tiles before
+// its own apart, so that no other kernel stands between (8,192 places 7.7 us a pass, 20,000 17, where sort.hip's three
+// kernels a pass take 13), ranks its
+// tile's places, one a lane, and writes their words to their new places.  The first pass makes the words from ids, the
+// last writes pairs.
+constexpr int kPassThreads = 512, kPassWaves = kPassThreads / kWave, kPassPlaces = 3 << 12;
+
+__global__ __launch_bounds__(kPassThreads) void embed_pass_kernel(const int32_t* __restrict__ ids,
+                                                                  const uint32_t* __restrict__ in, int T, int vocab,
+                                                                  int place_bits, int shift, bool last,
+                                                                  uint32_t* __restrict__ out, uint2* __restrict__ pairs,
+                                                                  uint32_t* __restrict__ n_pairs) {
+  __shared__ uint32_t before[256], after[256], base[256];
+  __shared__ uint16_t count[kPassWaves][256];
+  __shared__ uint32_t wave_sum[4], rowless;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int tile0 = blockIdx.x * kPassThreads;
+  if (tid < 256) before[tid] = after[tid] = 0;
+  if (tid == 0) rowless = 0;
+#pragma unroll
+  for (int i = 0; i < 256 / kWave; ++i) count[wave][i * kWave + lane] = 0;
+  __syncthreads();
+  const auto word = [&](int t) {
+    if (in != nullptr) return in[t];
+    return min(static_cast<uint32_t>(ids[t]), static_cast<uint32_t>(vocab)) << place_bits | static_cast<uint32_t>(t);
+  };
+  uint32_t none = 0;
+#pragma unroll 8
+  for (int t = tid; t < T; t += kPassThreads) {
+    const uint32_t w = word(t);
+    atomicAdd((t < tile0 ? before : after) + (w >> shift & 255u), 1u);
+    none += (w >> place_bits) >= static_cast<uint32_t>(vocab);
+  }
+  const int t = tile0 + tid;
+  const uint32_t w = t < T ? word(t) : 0xffffffffu, digit = w >> shift & 255u;
+  const uint64_t peers = same_digit(digit) & __ballot(t < T);
+  const uint32_t rank = static_cast<uint32_t>(__popcll(peers & lanemask_lt()));
+  if (t < T && rank == 0) count[wave][digit] = static_cast<uint16_t>(__popcll(peers));
+  if (last && none) atomicAdd(&rowless, none);
+  __syncthreads();
+  uint32_t all = 0, incl = 0;
+  if (tid < 256) {
+    all = before[tid] + after[tid];
+    incl = static_cast<uint32_t>(wave_inclusive_scan(static_cast<int>(all)));
+    if (lane == kWave - 1) wave_sum[wave] = incl;
+  }
+  __syncthreads();
+  if (tid < 256) {
+    uint32_t at = incl - all + before[tid];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) at += v < wave ? wave_sum[v] : 0u;
+    base[tid] = at;
+    uint32_t run = 0;
+#pragma unroll
+    for (int v = 0; v < kPassWaves; ++v) {
+      const uint32_t c = count[v][tid];
+      count[v][tid] = static_cast<uint16_t>(run);
+      run += c;
+    }
+  }
+  __syncthreads();
+  if (last && blockIdx.x == 0 && tid == 0) *n_pairs = static_cast<uint32_t>(T) - rowless;
+  if (t >= T) return;
+  const uint32_t to = base[digit] + count[wave][digit] + rank, key = w >> place_bits;
+  if (!last) out[to] = w;
+  else if (key < static_cast<uint32_t>(vocab)) pairs[to] = make_uint2(key, w & ((1u << place_bits) - 1u));
 }
 
 // Where a finished row goes: added to the dense table, or written to its compact row.
@@ -228,22 +420,23 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(const uint2* __rest
   else if (c < d) put_row<ROWS>(out, ROWS ? static_cast<int64_t>(place[last - 1]) : key, d, c, sum, scale);
 }
 
-// Rows that pass from run to run: the wave of the run that a row begins in adds what the following runs hold of it.
+// Rows that pass from run to run: the workgroup of the run that a row begins in adds what the following runs hold of
+// it, each wave a quarter of them.
 template <bool ROWS>
 __global__ __launch_bounds__(kThreads) void embed_join_kernel(const uint2* __restrict__ pairs,
                                                               const uint32_t* __restrict__ n_pairs,
                                                               const uint32_t* __restrict__ place,
                                                               float* __restrict__ out, const float* __restrict__ edge,
-                                                              int run, int slabs, int d, float scale) {
-  const int lane = threadIdx.x & (kWave - 1);
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + threadIdx.x / kWave;
-  const int r = __builtin_amdgcn_readfirstlane(static_cast<int>(item / slabs));
-  const int c = __builtin_amdgcn_readfirstlane(static_cast<int>(item % slabs)) * kSlab + lane * 4;
+                                                              int run, int d, float scale) {
+  constexpr int kWaves = kThreads / kWave;
+  __shared__ f32x4 part[kWaves][kWave];
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = blockIdx.x, c = blockIdx.y * kSlab + lane * 4;
   const int n = static_cast<int>(*n_pairs);
   const int first = r * run, last = first + run;
   if (last >= n) return;                                    // nothing follows
-  const uint32_t key = pairs[last - 1].x;
-  if (pairs[last].x != key || (first > 0 && pairs[first - 1].x == key)) return;
+  const uint32_t key = pairs[last - 1].x, before = first > 0 ? pairs[first - 1].x : ~key;
+  if (pairs[last].x != key || before == key) return;        // (the whole workgroup)
   // the runs after this one that hold more of the row: all but the last of them end within it
   const int runs = (n + run - 1) / run;
   int more = 0;
@@ -257,22 +450,31 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(const uint2* __res
     }
     more += kWave;
   }
-  if (c >= d) return;
   const bool whole = c + 4 <= d;
   const float* p = edge + 2 * static_cast<int64_t>(r) * d + c;
   const auto get = [&](const float* q) { return whole ? load4(q) : load_part(q, d - c); };
-  f32x4 sum = get(p + d);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  const int share = (more + kWaves - 1) / kWaves, end = min(more, (wave + 1) * share);
+  if (c < d) {
+    if (wave == 0) sum = get(p + d);
 #pragma unroll 8
-  for (int i = 1; i <= more; ++i) sum += get(p + 2 * static_cast<int64_t>(i) * d);
+    for (int i = wave * share + 1; i <= end; ++i) sum += get(p + 2 * static_cast<int64_t>(i) * d);
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave != 0 || c >= d) return;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) sum += part[w][lane];
   put_row<ROWS>(out, ROWS ? static_cast<int64_t>(place[last - 1]) : key, d, c, sum, scale);
 }
 
 // Sorted places of a run: 16, so that there are many runs, and from 2^16 places on as many as give 4,096 runs.
 int run_length(int T) { return std::max(16, (T + 4095) / 4096); }
 int most_runs(int T) { return (T + run_length(T) - 1) / run_length(T); }
-int key_bits(int vocab) {
+// The bits of the numbers below `vocab`.
+int key_bits(int64_t vocab) {
   int bits = 1;
-  while (bits < 31 && (INT64_C(1) << bits) < vocab) ++bits;
+  while (bits < 32 && (INT64_C(1) << bits) < vocab) ++bits;
   return bits;
 }
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
@@ -285,13 +487,34 @@ hipError_t backward(const umem_embed_desc& ed, int T, const int32_t* ids, const 
   uint32_t* starts = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(edge) +
                                                  up256(static_cast<size_t>(most_runs(T)) * 2 * ed.d * sizeof(float)));
   const SortPlan p = sort_plan(T, key_bits(ed.vocab), base);
-  hipLaunchKernelGGL(embed_keys_kernel, dim3(p.tiles), dim3(kSortThreads), 0, s, ids, T, ed.vocab, p.keys, p.dbits, p.tile,
-                     p.tiles, p.hist);
-  uint2 *sorted, *dead;
-  const hipError_t e = sort_run(p, kNone, true, s, &sorted, &dead);
-  if (e != hipSuccess) return e;
-  uint32_t* place = reinterpret_cast<uint32_t*>(dead);
-  if (ROWS) {
+  const int place_bits = key_bits(T), word_bits = key_bits(ed.vocab + INT64_C(1));
+  uint2* sorted = p.a;
+  uint32_t* place = reinterpret_cast<uint32_t*>(p.b);
+  const int passes = (word_bits + 7) / 8;
+  const bool packed = place_bits + word_bits <= 32;
+  bool ranked = false;
+  if (T <= kSmallPlaces && packed) {
+    hipLaunchKernelGGL(embed_sort_kernel<kSmallSteps>, dim3(1), dim3(kSmallThreads), 0, s, ids, T, ed.vocab, place_bits,
+                       passes, sorted, p.n, ROWS ? place : nullptr, rows, n_rows);
+    ranked = true;
+  } else if (T <= kPassPlaces && packed) {
+    // the words change between the halves of the other array of pairs
+    uint32_t *in = nullptr, *out = reinterpret_cast<uint32_t*>(p.b), *next = out + T;
+    for (int pass = 0; pass < passes; ++pass) {
+      hipLaunchKernelGGL(embed_pass_kernel, dim3((T + kPassThreads - 1) / kPassThreads), dim3(kPassThreads), 0, s, ids, in, T,
+                         ed.vocab, place_bits, place_bits + 8 * pass, pass + 1 == passes, out, sorted, p.n);
+      in = out;
+      std::swap(out, next);
+    }
+  } else {
+    hipLaunchKernelGGL(embed_keys_kernel, dim3(p.tiles), dim3(kSortThreads), 0, s, ids, T, ed.vocab, p.keys, p.dbits, p.tile,
+                       p.tiles, p.hist);
+    uint2* dead;
+    const hipError_t e = sort_run(p, kNone, true, s, &sorted, &dead);
+    if (e != hipSuccess) return e;
+    place = reinterpret_cast<uint32_t*>(dead);
+  }
+  if (ROWS && !ranked) {
     const int tiles = (T + kRankTile - 1) / kRankTile;
     hipLaunchKernelGGL(embed_count_kernel, dim3(tiles), dim3(kThreads), 0, s, sorted, p.n, starts);
     hipLaunchKernelGGL(embed_rank_kernel, dim3(tiles), dim3(kThreads), 0, s, sorted, p.n, starts, place, rows, n_rows);
@@ -301,8 +524,8 @@ hipError_t backward(const umem_embed_desc& ed, int T, const int32_t* ids, const 
   const dim3 grid(static_cast<unsigned>((items + 3) / 4));
   hipLaunchKernelGGL((embed_sum_kernel<GT, ROWS>), grid, dim3(kThreads), 0, s, sorted, p.n, place, dout, out, edge, run,
                      slabs, ed.d, ed.scale);
-  hipLaunchKernelGGL((embed_join_kernel<ROWS>), grid, dim3(kThreads), 0, s, sorted, p.n, place, out, edge, run, slabs,
-                     ed.d, ed.scale);
+  hipLaunchKernelGGL((embed_join_kernel<ROWS>), dim3(most_runs(T), slabs), dim3(kThreads), 0, s, sorted, p.n, place, out,
+                     edge, run, ed.d, ed.scale);
   return hipGetLastError();
 }
 

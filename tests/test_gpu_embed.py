@@ -143,7 +143,11 @@ def test_gradient(T, vocab, d, lead, kind, gt):
 
 
 @pytest.mark.parametrize("T,vocab,d,kind", [(70000, 5000, 8, "text"), (70001, 3, 17, "same"), (65536, 200000, 4, "distinct"),
-                                            (100003, 40, 4, "text"), (1 << 20, 70000, 1, "text")])
+                                            (100003, 40, 4, "text"), (1 << 20, 70000, 1, "text"),
+                                            (4096, 65535, 8, "text"), (8193, 255, 4, "text"), (16384, 256, 4, "same"),
+                                            (16385, 131071, 4, "text"), (20000, 60000, 12, "text"), (32768, 131071, 3, "text"),
+                                            (32768, 131072, 3, "text"), (32768, 1, 5, "text"), (32769, 9000, 4, "text"),
+                                            (5, 2 ** 27, 1, "distinct"), (9000, 300000, 3, "none")])
 def test_gradient_of_many_tokens(T, vocab, d, kind):
     print(f"[case] embed backward {T} {vocab} {d} {kind}", flush=True)
     check_backward(T, vocab, d, torch.float32, kind)
