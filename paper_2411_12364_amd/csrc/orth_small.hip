@@ -102,77 +102,89 @@ __global__ __launch_bounds__(kThreads) void orth_small_gram_kernel(const T* __re
         out[(i0 + i * 16 + (lane >> 4) + 4 * r) * kSide + j0 + j * 16 + (lane & 15)] = acc[i][j][r];
 }
 
-// The steps of one matrix of at most TOP rows: q[matrix][64][64] = Q / (|G| + eps).
+// The steps of one matrix of at most TOP rows: q[matrix][64][64] = Q / (|G| + eps).  The matrices are symmetric: the 16 x
+// 16 tiles on and below the diagonal are made, a wave's at a time, and written to both places.  T and the next Q, which
+// read the same, are made together: 20 tiles on 16 waves.  What bounds it is the fp64 rate of one CU: 64^3 products
+// of a full square are 4,096 clocks, and 5 steps have 17 squares (with full squares 42 us, so 38).
 template <int TOP>
 __global__ __launch_bounds__(kStepThreads) void orth_small_steps_kernel(const double* __restrict__ pieces, int m, int chunks,
                                                                         int steps, double a, double b, double c,
                                                                         float eps, double* __restrict__ q) {
+  constexpr int kSquare = TOP / 16, kTiles = kSquare * (kSquare + 1) / 2, kWaves = kStepThreads / 64;
+  static_assert(kTiles <= kWaves && 2 * kTiles <= kTiles + kWaves, "a wave has one tile of Q at most");
   __shared__ double A[kSide][kPitch], P[kSide][kPitch], Q[kSide][kPitch], T[kSide][kPitch];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i0 = (wave >> 2) * 16, j0 = (wave & 3) * 16, col = j0 + (lane & 15);
-  const bool on = i0 < TOP && j0 < TOP;                     // (all waves meet the barriers)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t mat = blockIdx.x;
   const double* from = pieces + mat * chunks * kSide * kSide;
-  double sum[4] = {0.0, 0.0, 0.0, 0.0};
-  if (on) {
+  for (int i = threadIdx.x; i < TOP * TOP; i += kStepThreads) {
+    const int row = i / TOP, col = i % TOP;
+    double v = 0.0;
 #pragma unroll 8
-    for (int p = 0; p < chunks; ++p)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sum[r] += from[(static_cast<int64_t>(p) * kSide + i0 + (lane >> 4) + 4 * r) * kSide + col];
+    for (int p = 0; p < chunks; ++p) v += from[(static_cast<int64_t>(p) * kSide + row) * kSide + col];
+    A[row][col] = v;
   }
-#pragma unroll
-  for (int r = 0; r < 4; ++r) A[i0 + (lane >> 4) + 4 * r][col] = sum[r];
   __syncthreads();
   double trace = lane < m ? A[lane][lane] : 0.0;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) trace += __shfl_xor(trace, off, 64);
   const double norm = sqrt(trace) + static_cast<double>(eps);
   __syncthreads();
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int row = i0 + (lane >> 4) + 4 * r;
+  for (int i = threadIdx.x; i < TOP * TOP; i += kStepThreads) {
+    const int row = i / TOP, col = i % TOP;
     A[row][col] = row < m && col < m ? A[row][col] / (norm * norm) : 0.0;
   }
   __syncthreads();
-  // a wave's tile of X Y, Y symmetric
-  const auto times = [&](double (*x)[kPitch], double (*y)[kPitch]) {
+  const auto row_of = [](int tile) { return (tile >= 1) + (tile >= 3) + (tile >= 6); };
+  const auto col_of = [&](int tile) { return tile - row_of(tile) * (row_of(tile) + 1) / 2; };
+  const auto times = [&](double (*x)[kPitch], double (*y)[kPitch], int tile) {
+    const int i0 = row_of(tile) * 16 + (lane & 15), j0 = col_of(tile) * 16 + (lane & 15);
     f64x4 acc = {0.0, 0.0, 0.0, 0.0};
-    if (on) {
 #pragma unroll
-      for (int k0 = 0; k0 < TOP; k0 += 4) {
-        const int k = k0 + (lane >> 4);
-        acc = mfma64(x[i0 + (lane & 15)][k], y[j0 + (lane & 15)][k], acc);
-      }
+    for (int k0 = 0; k0 < TOP; k0 += 4) {
+      const int k = k0 + (lane >> 4);
+      acc = mfma64(x[i0][k], y[j0][k], acc);
     }
     return acc;
   };
-  const auto put = [&](double (*x)[kPitch], const f64x4& v) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) x[i0 + (lane >> 4) + 4 * r][col] = v[r];
-  };
-  for (int step = 0; step < steps; ++step) {
-    f64x4 p = times(A, A);
+  const auto put = [&](double (*x)[kPitch], const f64x4& v, int tile) {
+    const int i0 = row_of(tile) * 16 + (lane >> 4), j = col_of(tile) * 16 + (lane & 15);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int row = i0 + (lane >> 4) + 4 * r;
-      p[r] = c * p[r] + b * A[row][col] + (row == col ? a : 0.0);
+      x[i0 + 4 * r][j] = v[r];
+      x[j][i0 + 4 * r] = v[r];            // (a tile on the diagonal: the other half of it, equal but for a rounding)
     }
-    put(P, p);
+  };
+  for (int step = 0; step < steps; ++step) {
+    if (wave < kTiles) {
+      f64x4 p = times(A, A, wave);
+      const int i0 = row_of(wave) * 16 + (lane >> 4), j = col_of(wave) * 16 + (lane & 15);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[r] = c * p[r] + b * A[i0 + 4 * r][j] + (i0 + 4 * r == j ? a : 0.0);
+      put(P, p, wave);
+      if (step == 0) put(Q, p, wave);
+    }
     __syncthreads();
     const bool last = step + 1 == steps;
-    const f64x4 t = last ? p : times(P, A);
-    const f64x4 n = step == 0 ? p : times(Q, P);
-    put(T, t);
+    const int of_t = last ? 0 : kTiles, of_q = step == 0 ? 0 : kTiles;
+    f64x4 next = {0.0, 0.0, 0.0, 0.0};
+    int mine = -1;                        // the wave's tile of the next Q, which takes the place of the one that is read
+    for (int task = wave; task < of_t + of_q; task += kWaves) {
+      if (task < of_t) {
+        put(T, times(P, A, task), task);
+      } else {
+        mine = task - of_t;
+        next = times(Q, P, mine);
+      }
+    }
     __syncthreads();
-    put(Q, n);
+    if (mine >= 0) put(Q, next, mine);
     if (last) break;
-    put(A, times(P, T));
+    if (wave < kTiles) put(A, times(P, T, wave), wave);
     __syncthreads();
   }
-  // (each element by the thread that wrote it)
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int row = i0 + (lane >> 4) + 4 * r;
+  __syncthreads();
+  for (int i = threadIdx.x; i < TOP * TOP; i += kStepThreads) {
+    const int row = i / TOP, col = i % TOP;
     q[(mat * kSide + row) * kSide + col] = Q[row][col] / norm;
   }
 }
@@ -189,8 +201,8 @@ __global__ __launch_bounds__(kThreads) void orth_small_apply_kernel(const GT* g,
   s.load(g + base, m, k, k0);
 #pragma unroll
   for (int i = 0; i < kSide * kSide / kThreads; ++i) {
-    const int at = i * kThreads + threadIdx.x;
-    Q[at / kSide][at % kSide] = q[mat * kSide * kSide + at];
+    const int at = i * kThreads + threadIdx.x, row = at / kSide, col = at % kSide;
+    Q[row][col] = row < m && col < m ? q[mat * kSide * kSide + at] : 0.0;
   }
   s.store(t);
   __syncthreads();
