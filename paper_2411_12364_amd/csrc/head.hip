@@ -329,10 +329,26 @@ __device__ __forceinline__ float most_of(const float* most) {
 // cols[part][piece][t_ld] in PC fp16 parts; zeros past the piece's rows of W, past T and for tokens without a target.
 // lost: what of a target's r one bf16 part of it does not hold, [T] (of it alone r is near the largest dloss in most
 // tokens; dx adds it times W's row: half the error of dx is without that from there).
-// A part at a time goes through LDS, [token][v], its 16-byte pieces permuted by the token's number so that
-// both orders of reading meet all banks.  (Parts kept from one to the next spill 360 registers: 430 us of 620 were the
-// end of a tile.)
+// The tile's rows are in an order in which a lane holds 8 values of W's rows one after another, and NT tokens one after another, so
+// that both orders are written from the registers, in whole 64- and 128-byte pieces.  (Through LDS, a part at a time,
+// the end of a tile took as long as its products: 7,168 x 8,192 of 2,048 316 us.)
 constexpr float kSlopeUp = 32768.f;
+
+// Within a wave's rows of A, accumulator block i, row 4 q + r (q = lane / 16): 32 (i / 2) + 8 q + 4 (i % 2) + r; within its
+// rows of B, block j, row l: NT l + j.
+struct SlopeRowA {
+  __device__ __forceinline__ int operator()(int row) const {
+    const int i = (row >> 4) & 1, q = (row >> 2) & 3;
+    return (row & ~31) | q << 3 | i << 2 | (row & 3);
+  }
+};
+template <int NT>
+struct SlopeRowB {
+  __device__ __forceinline__ int operator()(int row) const {
+    const int in = row % (16 * NT);
+    return row - in + (in & 15) * NT + (in >> 4);
+  }
+};
 
 template <int BM, int BN, int WR, int WC, int PR, int PC>
 __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
@@ -344,100 +360,95 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
                                                                  uint16_t* __restrict__ cols,
                                                                  float* __restrict__ lost) {
   typedef Tile<false, BM, BN, WR, WC, 2> Tl;
-  static_assert(BM * BN <= 2 * Tl::kElems && BM % 64 == 0 && BN % 64 == 0, "a tile of bf16 fits the operands' LDS");
+  constexpr int MT = Tl::MT, NT = Tl::NT;
+  static_assert(MT % 2 == 0 && (NT == 2 || NT == 4), "pieces of 16 bytes along W's rows, of 4 or 8 along the tokens");
   __shared__ __align__(16) uint16_t buf0[Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[Tl::kElems];
   const int item = tile_item(tiles_m * tiles_n);
   if (item >= tiles_m * tiles_n) return;
   const TilePlace at = tile_place(item, tiles_m, tiles_n);
   Tl tile;
-  tile.init(p, at.m * BM, at.n * BN);
-  f32x4 acc[Tl::MT][Tl::NT];
+  tile.init(p, at.m * BM, at.n * BN, SlopeRowA(), SlopeRowB<NT>());
+  f32x4 acc[MT][NT];
   tile.run(p, 0, Tl::slices(p), buf0, buf1, nullptr, nullptr, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
   const int V = p.a_rows, T = p.b_rows;
-  const int m0 = wr * Tl::MT * 16 + 4 * (lane >> 4);
+  const int v0 = at.m * BM + wr * MT * 16 + 8 * (lane >> 4);       // acc[i][j][r]: row v0 + 32 (i / 2) + 4 (i % 2) + r
+  const int t0 = at.n * BN + wc * NT * 16 + NT * (lane & 15);      // token t0 + j
   const float largest = most_of(most);
 #pragma unroll
-  for (int j = 0; j < Tl::NT; ++j) {
-    const int t = at.n * BN + (wc * Tl::NT + j) * 16 + (lane & 15);
-    const int tc = min(t, T - 1), y = targets[tc];
+  for (int j = 0; j < NT; ++j) {
+    const int t = t0 + j, tc = min(t, T - 1), y = targets[tc];
     const bool on = t < T && static_cast<uint32_t>(y) < static_cast<uint32_t>(vocab);
     const float l = lse[tc], g = dloss ? dloss[tc] / largest : 1.f;
 #pragma unroll
-    for (int i = 0; i < Tl::MT; ++i)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int v = at.m * BM + m0 + i * 16 + r;
-        const float e = __expf(fmaf(acc[i][j][r], scale, -l)) - (v_first + v == y ? 1.f : 0.f);
-        acc[i][j][r] = on && v < V ? g * e : 0.f;
-        if (PR == 1 && on && v_first + v == y && v < V) {
-          const float part = bits_f32(bf16_bits(acc[i][j][r]));
-          lost[t] = fabsf(part) <= 3.4e38f ? acc[i][j][r] - part : 0.f;
-        }
-      }
-  }
-  // token n's first element; its 16-byte piece c is at place c ^ turn(n)
-  const auto row_at = [&](int n) { return (n < BN / 2 ? buf0 : buf1) + (n % (BN / 2)) * BM; };
-  const auto turn = [](int n) { return (n ^ (n >> 3)) & (BM / 8 - 1); };
-#pragma unroll 1
-  for (int pass = 0; pass < PR + PC; ++pass) {
-    const bool by_rows = pass < PR;
-    const int part = by_rows ? pass : pass - PR;
-    // (each pass makes its part again: made before the loop, all parts would be kept)
+      for (int r = 0; r < 4; ++r) acc[i][j][r] = __expf(fmaf(acc[i][j][r], scale, -l));
+    // the target's entry, which few waves hold one of
+    const int in = y - v_first - v0;
+    const bool holds = on && in >= 0 && in < MT * 16 && (in & 31) < 8;
+    const int which = (in >> 5) * 8 + (in & 7);
+    if (__any(holds)) {
 #pragma unroll
-    for (int j = 0; j < Tl::NT; ++j)
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int i = 0; i < Tl::MT; ++i) asm volatile("" : "+v"(acc[i][j]));
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < Tl::NT; ++j)
-#pragma unroll
-      for (int i = 0; i < Tl::MT; ++i) {
-        const int n = (wc * Tl::NT + j) * 16 + (lane & 15), m = m0 + i * 16;
-        uint32_t b[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (by_rows) {
-            uint32_t parts[PR];
-            bf16_parts(acc[i][j][r], parts);
-            b[r] = parts[0];
-#pragma unroll
-            for (int k = 1; k < PR; ++k) b[r] = part == k ? parts[k] : b[r];
-          } else {
-            b[r] = f16_part(acc[i][j][r] * kSlopeUp, 0);
-            if (PC > 1 && part > 0) b[r] = f16_part(acc[i][j][r] * kSlopeUp, 1);
+        for (int r = 0; r < 4; ++r)
+          if (holds && which == 4 * i + r) {
+            acc[i][j][r] -= 1.f;
+            if (PR == 1) {
+              const float whole = g * acc[i][j][r], part = bits_f32(bf16_bits(whole));
+              lost[t] = fabsf(part) <= 3.4e38f ? whole - part : 0.f;
+            }
           }
-        }
-        *reinterpret_cast<u32x2*>(row_at(n) + (((m >> 3) ^ turn(n)) << 3) + (m & 7)) =
-            u32x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
-      }
-    __syncthreads();
-    if (by_rows) {
-      uint16_t* to = rows + static_cast<int64_t>(part) * T * piece;
-#pragma unroll 4
-      for (int i = threadIdx.x; i < BN * (BM / 8); i += Tl::kThreads) {
-        const int n = i / (BM / 8), c = i % (BM / 8), t = at.n * BN + n, v = at.m * BM + c * 8;
-        if (t < T && v < piece)
-          *reinterpret_cast<u32x4*>(to + static_cast<int64_t>(t) * piece + v) =
-              *reinterpret_cast<const u32x4*>(row_at(n) + ((c ^ turn(n)) << 3));
-      }
-    } else {
-      uint16_t* to = cols + static_cast<int64_t>(part) * piece * t_ld;
-      // a row of W's tokens to BN / 8 lanes: whole lines
-#pragma unroll 2
-      for (int i = threadIdx.x; i < BM * (BN / 8); i += Tl::kThreads) {
-        const int m = i / (BN / 8), n8 = (i % (BN / 8)) * 8;
-        const int t = at.n * BN + n8, v = at.m * BM + m;
-        uint32_t b[8];
+    }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) b[k] = row_at(n8 + k)[(((m >> 3) ^ turn(n8 + k)) << 3) + (m & 7)];
-        if (t < t_ld && v < piece)
-          *reinterpret_cast<u32x4*>(to + static_cast<int64_t>(v) * t_ld + t) =
-              u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16};
-      }
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[i][j][r] = on ? g * acc[i][j][r] : 0.f;
+  }
+  if (at.m * BM + BM > V) {               // (uniform: the last rows of W)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (v0 + 32 * (i / 2) + 4 * (i % 2) + r >= V) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j][r] = 0.f;
+        }
+  }
+  // (piece is a multiple of BM)
+  const int64_t by_row = static_cast<int64_t>(T) * piece, by_col = static_cast<int64_t>(piece) * t_ld;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    if (t0 + j >= T) continue;
+    uint16_t* to = rows + static_cast<int64_t>(t0 + j) * piece + v0;
+#pragma unroll
+    for (int i = 0; i < MT; i += 2) {
+      uint32_t b[8][PR];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bf16_parts(acc[i + e / 4][j][e % 4], b[e]);
+#pragma unroll
+      for (int k = 0; k < PR; ++k)
+        *reinterpret_cast<u32x4*>(to + k * by_row + 16 * i) =
+            u32x4{b[0][k] | b[1][k] << 16, b[2][k] | b[3][k] << 16, b[4][k] | b[5][k] << 16, b[6][k] | b[7][k] << 16};
     }
   }
+  if (t0 >= t_ld) return;
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      uint16_t* to = cols + static_cast<int64_t>(v0 + 32 * (i / 2) + 4 * (i % 2) + r) * t_ld + t0;
+#pragma unroll
+      for (int k = 0; k < PC; ++k) {
+        uint32_t b[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) b[j] = f16_part(acc[i][j][r] * kSlopeUp, k);
+        if constexpr (NT == 4) *reinterpret_cast<u32x2*>(to + k * by_col) = u32x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
+        else *reinterpret_cast<uint32_t*>(to + k * by_col) = b[0] | b[1] << 16;
+      }
+    }
 }
 
 // A product whose m lies along the rows of the output, [n][m] of ld.  Of one split of k: out = (D + before) f (dx) or
@@ -547,7 +558,7 @@ size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // A product's tiles, and how often its slices are split, by what the sizes of tile measured (us a slice): 256 x 256,
-// eight waves and a CU to itself, 1.7; 128 x 128, two to a CU, 0.95 both, 0.55 alone; 64 x 64, up to four to a CU, 0.25 alone
+// eight waves and a CU to itself, 1.7; 128 x 128, two to a CU, 0.95 both, 0.7 alone; 64 x 64, up to four to a CU, 0.25 alone
 // and 0.2 more with each beside it.  So large tiles where there is one for each CU (7,168 x 8,192 over 2,048: 1.7 a slice
 // for 16 tiles of 64 x 64, which take 3.4), small ones where there are few: 600 x 2,314 over 1,696 46 in 27 large ones, 20 in
 // 95 of 128 x 128.  Small ones are taken up to 4,096 of them.
@@ -566,7 +577,7 @@ TilePlan tile_plan(int64_t m, int64_t n, int slices, int most_splits, bool large
       const double each = (slices + s - 1) / s, whole = static_cast<double>(full);
       double us = s > 1 ? 4.0 + 8e-6 * m * n * s / 3.0 : 0.0;
       if (side == 256) us += whole * (4.0 + 1.7 * each);
-      else if (side == 128) us += static_cast<double>(full / 2) * (4.0 + 0.95 * each) + (full % 2 ? 4.0 + 0.55 * each : 0.0);
+      else if (side == 128) us += static_cast<double>(full / 2) * (4.0 + 0.95 * each) + (full % 2 ? 4.0 + 0.7 * each : 0.0);
       else us += static_cast<double>(full / 4) * (4.0 + 0.85 * each) + (full % 4 ? 3.0 + (0.05 + 0.2 * (full % 4)) * each : 0.0);
       if (us < least) {
         least = us;
@@ -693,7 +704,7 @@ void slope(const TilePairs& p, float scale, const int32_t* targets, const float*
                        dim3(64 * WR * WC), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first, vocab,    \
                        piece, t_ld, rows, cols, lost);                                                          \
   }
-  // (of 256 x 256 tiles one at a time is on a CU, and nothing beside its end: 340 us, so 316)
+  // (of 256 x 256 tiles one at a time is on a CU, and nothing beside its end)
   if (tile_plan(piece, p.b_rows, slice_count(p.k, p.n), 1, false).side == 128) UMEM_SLOPE(128, 128, 2, 2)
   else UMEM_SLOPE(64, 64, 2, 2)
 #undef UMEM_SLOPE

@@ -86,20 +86,25 @@ struct Tile {
   }
 
   // The lane's offsets for the tile at (m0, n0).  A row's number mod 8 is the same for all pieces of a lane
-  // (the pieces lie kThreads / 8 rows apart), so their column is too.
-  __device__ __forceinline__ void init(const TilePairs& p, int m0_, int n0_) {
+  // (the pieces lie kThreads / 8 rows apart), so their column is too.  The tile's row i of A is a_row(i) of the matrix's
+  // from m0 on, and so B's: an order of the rows that suits how the caller writes the accumulators.
+  struct InOrder {
+    __device__ __forceinline__ int operator()(int row) const { return row; }
+  };
+  template <typename RowA = InOrder, typename RowB = InOrder>
+  __device__ __forceinline__ void init(const TilePairs& p, int m0_, int n0_, RowA a_row = {}, RowB b_row = {}) {
     m0 = min(m0_, p.a_rows - 1);            // (a tile past the rows that there are reads the last one)
     n0 = min(n0_, p.b_rows - 1);
     const int tid = thread(), row = tid >> 3, col = (tid & 7) ^ (row & 7);
     col_k = col * 8;
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
-      const int r = min(row + i * (kThreads / 8), p.a_rows - 1 - m0);
+      const int r = min(a_row(row + i * (kThreads / 8)), p.a_rows - 1 - m0);
       a_off[i] = static_cast<uint32_t>(r * static_cast<int>(p.a_ld) + col_k) * 2u;
     }
 #pragma unroll
     for (int i = 0; i < kB; ++i) {
-      const int r = min(row + i * (kThreads / 8), p.b_rows - 1 - n0);
+      const int r = min(b_row(row + i * (kThreads / 8)), p.b_rows - 1 - n0);
       b_off[i] = static_cast<uint32_t>(r * static_cast<int>(p.b_ld) + col_k) * 2u;
     }
   }
