@@ -20,6 +20,8 @@
 // one part (2^-12 of it, and 2^-40 of the largest dloss) where dW is bf16, as two (22 bits) where it is fp32, as fp32 x is then.
 // (Three bf16 parts of r hold it as well, at half more time: 8,192 tokens by 7,168 rows of 2,048 560 us, so 370.)
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "tiles.h"
 
@@ -63,8 +65,8 @@ __global__ __launch_bounds__(kThreads) void head_split_kernel(const float* __res
 }
 
 // The maxima of kMostBlocks fixed ranges, for a wave of each consumer to take the largest of.
-constexpr int kMostBlocks = 64;
-static_assert(kMostBlocks == kWave, "a lane each");
+constexpr int kMostBlocks = 256;
+static_assert(kMostBlocks == 4 * kWave, "four a lane");
 
 __device__ __forceinline__ float wave_most(float m) {
 #pragma unroll
@@ -85,10 +87,11 @@ __device__ __forceinline__ bool counts(const int32_t* targets, int t, int vocab)
   return static_cast<uint32_t>(targets[t]) < static_cast<uint32_t>(vocab);
 }
 
-// The largest finite |x| of the tokens that count; a workgroup walks rows.
+// The largest finite |x| of the tokens that count, and (most: with a dloss) the largest |dloss| of theirs.
 template <typename T>
-__global__ __launch_bounds__(1024) void head_most_x_kernel(const T* __restrict__ x, const int32_t* __restrict__ targets,
-                                                           int tokens, int d, int vocab, float* __restrict__ most) {
+__global__ __launch_bounds__(1024) void head_most_kernel(const T* __restrict__ x, const float* __restrict__ dloss,
+                                                         const int32_t* __restrict__ targets, int tokens, int d, int vocab,
+                                                         float* __restrict__ most, float* __restrict__ most_x) {
   typedef T eight __attribute__((ext_vector_type(8)));
   const int64_t pieces = static_cast<int64_t>(tokens) * (d / 8);
   float m = 0.f;
@@ -103,12 +106,24 @@ __global__ __launch_bounds__(1024) void head_most_x_kernel(const T* __restrict__
     }
     if (most8 > m && counts(targets, static_cast<int>(i / (d / 8)), vocab)) m = most8;
   }
+  put_most(m, most_x);
+  if (!dloss) return;
+  m = 0.f;
+  for (int t = blockIdx.x * 1024 + threadIdx.x; t < tokens; t += kMostBlocks * 1024)
+    if (counts(targets, t, vocab)) m = fmaxf(m, fabsf(dloss[t]));
+  __syncthreads();
   put_most(m, most);
+}
+
+// The largest of the blocks' maxima, to every lane.
+__device__ __forceinline__ float all_most(const float* most) {
+  const f32x4 m = reinterpret_cast<const f32x4*>(most)[threadIdx.x & (kWave - 1)];
+  return wave_most(fmaxf(fmaxf(m.x, m.y), fmaxf(m.z, m.w)));
 }
 
 // The power of two that x is multiplied by: it takes the largest to between 2^14 and 2^15.
 __device__ __forceinline__ int x_shift(const float* most) {
-  const float m = wave_most(most[threadIdx.x & (kWave - 1)]);
+  const float m = all_most(most);
   int e = 0;
   frexpf(m, &e);
   return m > 0.f ? min(max(15 - e, -110), 110) : 0;
@@ -168,54 +183,76 @@ __global__ __launch_bounds__(kThreads) void head_transpose_kernel(const T* __res
 
 // ---------------------------------------------------------------- forward
 
-// Each token's (reference, sum of exp(z - reference)) over the tile's rows of W, to stats[tile][T]; the reference is
-// the maximum, or 0 where that is not finite.  goal[t]: the target's logit, by the tile that holds it.
-template <int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(64 * WR * WC) void head_stats_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
-                                                                 const int32_t* __restrict__ targets,
-                                                                 float2* __restrict__ stats, float* __restrict__ goal) {
-  typedef Tile<false, BM, BN, WR, WC, 2> Tl;
-  __shared__ __align__(16) uint16_t buf0[Tl::kElems];
-  __shared__ __align__(16) uint16_t buf1[Tl::kElems];
+// Each token's (reference, sum of exp(z - reference |scale|)) over the tile's rows of W, to stats[tile][T]; z = |scale| u, u the
+// product (with its sign turned where scale is below 0), the reference is the largest u, or 0 where that is infinite or none;
+// with a sum of 0 -infinity, so that it raises no other's.
+// goal[t]: the target's u, by the tile that holds it.  The end of a tile takes 8 clocks of a lane's for each logit, 4 of
+// them exp2's: with the target and W's last row looked for at each the kernel took 1.05 times as long.
+constexpr float kLog2e = 1.44269504f, kLargest = 3.4e38f;
+
+template <int BM, int BN, int WR, int WC, int GROUPS>
+__global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_stats_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
+                                                                          const int32_t* __restrict__ targets,
+                                                                          float2* __restrict__ stats,
+                                                                          float* __restrict__ goal) {
+  typedef Tile<false, BM, BN, WR, WC, 2, kPlain, GROUPS> Tl;
+  constexpr int MT = Tl::MT, NT = Tl::NE;
+  __shared__ __align__(16) uint16_t buf0[GROUPS * Tl::kElems];
+  __shared__ __align__(16) uint16_t buf1[GROUPS * Tl::kElems];
   __shared__ float2 waves[WR][BN];
   const int item = tile_item(tiles_m * tiles_n);
   if (item >= tiles_m * tiles_n) return;                    // the whole workgroup: no barrier is skipped
   const TilePlace at = tile_place(item, tiles_m, tiles_n);
   Tl tile;
   tile.init(p, at.m * BM, at.n * BN);
-  f32x4 acc[Tl::MT][Tl::NT];
-  tile.run(p, 0, Tl::slices(p), buf0, buf1, nullptr, nullptr, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
+  const int group = Tl::group(), own = group * Tl::kElems;
+  f32x4 all[MT][Tl::NT], acc[MT][NT];
+  tile.run(p, 0, Tl::slices(p), buf0 + own, buf1 + own, nullptr, nullptr, all);
+  Tl::share(all, buf0, acc);
+  const int lane = threadIdx.x & 63, wave = Tl::thread() >> 6, wr = wave / WC, wc = wave % WC;
   const int V = p.a_rows, T = p.b_rows;
-  const int v0 = at.m * BM + wr * Tl::MT * 16 + 4 * (lane >> 4);
+  const int v0 = at.m * BM + wr * MT * 16 + 4 * (lane >> 4);
+  const float c = fminf(fabsf(scale) * kLog2e, kLargest);
+  const bool edge = at.m * BM + BM > V;                     // (uniform: W's last rows)
 #pragma unroll
-  for (int j = 0; j < Tl::NT; ++j) {
-    const int n = (wc * Tl::NT + j) * 16 + (lane & 15), t = at.n * BN + n;
-    const int y = t < T ? targets[t] : -1;
-    float top = -INFINITY;
+  for (int j = 0; j < NT; ++j) {
+    const int n = (wc * Tl::NT + group * NT + j) * 16 + (lane & 15), t = at.n * BN + n;
+    if (scale < 0.f) {
 #pragma unroll
-    for (int i = 0; i < Tl::MT; ++i)
+      for (int i = 0; i < MT; ++i) acc[i][j] = -acc[i][j];
+    }
+    const int in = (t < T ? targets[t] : -1) - v0;          // the target's entry, which few waves hold one of
+    const bool holds = in >= 0 && in < MT * 16 && (in & 15) < 4 && v0 + in < V;
+    if (__any(holds)) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int v = v0 + i * 16 + r;
-        acc[i][j][r] = v < V ? acc[i][j][r] * scale : -INFINITY;
-        if (v == y && v < V) goal[t] = acc[i][j][r];
-        top = fmaxf(top, acc[i][j][r]);
-      }
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    top = fabsf(top) < INFINITY ? top : 0.f;
-    float sum = 0.f;
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int i = 0; i < Tl::MT; ++i)
+        for (int r = 0; r < 4; ++r)
+          if (holds && in == 16 * i + r) goal[t] = acc[i][j][r];
+    }
+    float top = -INFINITY, sum = 0.f;
+    const auto over = [&](auto last) {
+      const auto there = [&](int i, int r) { return !last || v0 + i * 16 + r < V; };
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sum += __expf(acc[i][j][r] - top);
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = there(i, r) ? fmaxf(top, acc[i][j][r]) : top;
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      top = fabsf(top) < INFINITY ? top : 0.f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += there(i, r) ? __builtin_amdgcn_exp2f((acc[i][j][r] - top) * c) : 0.f;
+    };
+    if (edge) over(std::true_type());
+    else over(std::false_type());
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
-    if (lane < 16) waves[wr][n] = float2{top, sum};
+    if (lane < 16) waves[wr][n] = float2{sum == 0.f ? -INFINITY : top, sum};
   }
   __syncthreads();
-  for (int n = threadIdx.x; n < BN; n += Tl::kThreads) {
+  for (int n = threadIdx.x; n < BN; n += Tl::kThreads * GROUPS) {
     const int t = at.n * BN + n;
     if (t >= T) continue;
     float top = waves[0][n].x;
@@ -223,16 +260,17 @@ __global__ __launch_bounds__(64 * WR * WC) void head_stats_kernel(TilePairs p, i
     for (int w = 1; w < WR; ++w) top = fmaxf(top, waves[w][n].x);
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < WR; ++w) sum += waves[w][n].y * __expf(waves[w][n].x - top);
+    for (int w = 0; w < WR; ++w)
+      if (waves[w][n].y != 0.f) sum += waves[w][n].y * __builtin_amdgcn_exp2f((waves[w][n].x - top) * c);
     stats[static_cast<int64_t>(at.m) * T + t] = float2{top, sum};
   }
 }
 
-// The tiles' pairs of each token, 16 lanes a token, added in fp64 in the order of the tiles.
+// The tiles' pairs of each token, 16 lanes a token, added in fp64 in the order of the tiles; scale here is |scale|.
 __global__ __launch_bounds__(kThreads) void head_join_kernel(const float2* __restrict__ stats,
                                                              const float* __restrict__ goal,
                                                              const int32_t* __restrict__ targets, int T, int vocab,
-                                                             int tiles, float* __restrict__ loss,
+                                                             int tiles, double scale, float* __restrict__ loss,
                                                              float* __restrict__ lse) {
   __shared__ float tops[16][17];
   __shared__ double sums[16][17];
@@ -248,7 +286,7 @@ __global__ __launch_bounds__(kThreads) void head_join_kernel(const float2* __res
   if (t < T)
     for (int i = q; i < tiles; i += 16) {
       const float2 s = stats[static_cast<int64_t>(i) * T + t];
-      sum += s.y * exp(static_cast<double>(s.x) - top);
+      if (s.y != 0.f) sum += s.y * exp((static_cast<double>(s.x) - top) * scale);
     }
   sums[q][n] = sum;
   __syncthreads();
@@ -256,16 +294,16 @@ __global__ __launch_bounds__(kThreads) void head_join_kernel(const float2* __res
   sum = 0.0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) sum += sums[i][n];
-  const double all = top + log(sum);
+  const double all = top * scale + log(sum);
   lse[t] = static_cast<float>(all);
-  loss[t] = counts(targets, t, vocab) ? static_cast<float>(all - goal[t]) : 0.f;
+  loss[t] = counts(targets, t, vocab) ? static_cast<float>(all - goal[t] * scale) : 0.f;
 }
 
 // The same with a workgroup a token, for few tokens.
 __global__ __launch_bounds__(kThreads) void head_join_few_kernel(const float2* __restrict__ stats,
                                                                  const float* __restrict__ goal,
                                                                  const int32_t* __restrict__ targets, int T, int vocab,
-                                                                 int tiles, float* __restrict__ loss,
+                                                                 int tiles, double scale, float* __restrict__ loss,
                                                                  float* __restrict__ lse) {
   __shared__ float tops[kThreads / kWave];
   __shared__ double sums[kThreads / kWave];
@@ -289,10 +327,10 @@ __global__ __launch_bounds__(kThreads) void head_join_few_kernel(const float2* _
   double sum = 0.0;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
-    if (static_cast<int>(threadIdx.x) + j * kThreads < tiles) sum += held[j].y * exp(static_cast<double>(held[j].x) - top);
+    if (held[j].y != 0.f) sum += held[j].y * exp((static_cast<double>(held[j].x) - top) * scale);
   for (int i = threadIdx.x + kHeld * kThreads; i < tiles; i += kThreads) {
     const float2 s = stats[static_cast<int64_t>(i) * T + t];
-    sum += s.y * exp(static_cast<double>(s.x) - top);
+    if (s.y != 0.f) sum += s.y * exp((static_cast<double>(s.x) - top) * scale);
   }
 #pragma unroll
   for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
@@ -301,27 +339,17 @@ __global__ __launch_bounds__(kThreads) void head_join_few_kernel(const float2* _
   if (threadIdx.x != 0) return;
 #pragma unroll
   for (int w = 1; w < kThreads / kWave; ++w) sum += sums[w];
-  const double all = top + log(sum);
+  const double all = top * scale + log(sum);
   lse[t] = static_cast<float>(all);
-  loss[t] = counts(targets, t, vocab) ? static_cast<float>(all - goal[t]) : 0.f;
+  loss[t] = counts(targets, t, vocab) ? static_cast<float>(all - goal[t] * scale) : 0.f;
 }
 
 // ---------------------------------------------------------------- backward
 
-// The largest |dloss| of the tokens that count.
-__global__ __launch_bounds__(kThreads) void head_most_kernel(const float* __restrict__ dloss,
-                                                             const int32_t* __restrict__ targets, int T, int vocab,
-                                                             float* __restrict__ most) {
-  float m = 0.f;
-  for (int t = blockIdx.x * kThreads + threadIdx.x; t < T; t += kMostBlocks * kThreads)
-    if (counts(targets, t, vocab)) m = fmaxf(m, fabsf(dloss[t]));
-  put_most(m, most);
-}
-
-// The largest of them; 1 without any, or where it is no finite number above 0.
+// The largest |dloss|; 1 without any, or where it is no finite number above 0.
 __device__ __forceinline__ float most_of(const float* most) {
   if (most == nullptr) return 1.f;
-  const float m = wave_most(most[threadIdx.x & (kWave - 1)]);
+  const float m = all_most(most);
   return m > 0.f && m < INFINITY ? m : 1.f;
 }
 
@@ -350,8 +378,8 @@ struct SlopeRowB {
   }
 };
 
-template <int BM, int BN, int WR, int WC, int PR, int PC>
-__global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
+template <int BM, int BN, int WR, int WC, int GROUPS, int PR, int PC>
+__global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
                                                                  const int32_t* __restrict__ targets,
                                                                  const float* __restrict__ lse,
                                                                  const float* __restrict__ dloss,
@@ -359,22 +387,24 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
                                                                  int piece, int t_ld, uint16_t* __restrict__ rows,
                                                                  uint16_t* __restrict__ cols,
                                                                  float* __restrict__ lost) {
-  typedef Tile<false, BM, BN, WR, WC, 2> Tl;
-  constexpr int MT = Tl::MT, NT = Tl::NT;
-  static_assert(MT % 2 == 0 && (NT == 2 || NT == 4), "pieces of 16 bytes along W's rows, of 4 or 8 along the tokens");
-  __shared__ __align__(16) uint16_t buf0[Tl::kElems];
-  __shared__ __align__(16) uint16_t buf1[Tl::kElems];
+  typedef Tile<false, BM, BN, WR, WC, 2, kPlain, GROUPS> Tl;
+  constexpr int MT = Tl::MT, NT = Tl::NE;
+  static_assert(MT % 2 == 0 && (NT == 1 || NT == 2 || NT == 4), "pieces of 16 bytes along W's rows, of NT along the tokens");
+  __shared__ __align__(16) uint16_t buf0[GROUPS * Tl::kElems];
+  __shared__ __align__(16) uint16_t buf1[GROUPS * Tl::kElems];
   const int item = tile_item(tiles_m * tiles_n);
   if (item >= tiles_m * tiles_n) return;
   const TilePlace at = tile_place(item, tiles_m, tiles_n);
   Tl tile;
-  tile.init(p, at.m * BM, at.n * BN, SlopeRowA(), SlopeRowB<NT>());
-  f32x4 acc[MT][NT];
-  tile.run(p, 0, Tl::slices(p), buf0, buf1, nullptr, nullptr, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
+  tile.init(p, at.m * BM, at.n * BN, SlopeRowA(), SlopeRowB<Tl::NT>());
+  const int group = Tl::group(), own = group * Tl::kElems;
+  f32x4 all[MT][Tl::NT], acc[MT][NT];
+  tile.run(p, 0, Tl::slices(p), buf0 + own, buf1 + own, nullptr, nullptr, all);
+  Tl::share(all, buf0, acc);
+  const int lane = threadIdx.x & 63, wave = Tl::thread() >> 6, wr = wave / WC, wc = wave % WC;
   const int V = p.a_rows, T = p.b_rows;
   const int v0 = at.m * BM + wr * MT * 16 + 8 * (lane >> 4);       // acc[i][j][r]: row v0 + 32 (i / 2) + 4 (i % 2) + r
-  const int t0 = at.n * BN + wc * NT * 16 + NT * (lane & 15);      // token t0 + j
+  const int t0 = at.n * BN + wc * Tl::NT * 16 + Tl::NT * (lane & 15) + group * NT;     // token t0 + j
   const float largest = most_of(most);
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
@@ -446,7 +476,8 @@ __global__ __launch_bounds__(64 * WR * WC) void head_slope_kernel(TilePairs p, i
 #pragma unroll
         for (int j = 0; j < NT; ++j) b[j] = f16_part(acc[i][j][r] * kSlopeUp, k);
         if constexpr (NT == 4) *reinterpret_cast<u32x2*>(to + k * by_col) = u32x2{b[0] | b[1] << 16, b[2] | b[3] << 16};
-        else *reinterpret_cast<uint32_t*>(to + k * by_col) = b[0] | b[1] << 16;
+        else if constexpr (NT == 2) *reinterpret_cast<uint32_t*>(to + k * by_col) = b[0] | b[1] << 16;
+        else to[k * by_col] = static_cast<uint16_t>(b[0]);
       }
     }
 }
@@ -481,11 +512,15 @@ __device__ __forceinline__ float product_factor(const ProductArgs& g) {
   return g.x_most ? f * (1.f / kSlopeUp) : f;
 }
 
-template <bool F16, typename OT, int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(64 * WR * WC) void head_product_kernel(TilePairs p, ProductArgs g) {
-  typedef Tile<F16, BM, BN, WR, WC, 2> Tl;
-  __shared__ __align__(16) uint16_t buf0[Tl::kElems];
-  __shared__ __align__(16) uint16_t buf1[Tl::kElems];
+// GROUPS sets of waves share a tile's slices where there are too few tiles for more than one on a CU: with one wave on each
+// of its parts a CU waits for every slice.
+template <bool F16, typename OT, int BM, int BN, int WR, int WC, int BUFS, int GROUPS>
+__global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(TilePairs p, ProductArgs g) {
+  typedef Tile<F16, BM, BN, WR, WC, BUFS, kPlain, GROUPS> Tl;
+  __shared__ __align__(16) uint16_t buf0[GROUPS * Tl::kElems];
+  __shared__ __align__(16) uint16_t buf1[GROUPS * Tl::kElems];
+  __shared__ __align__(16) uint16_t buf2[BUFS > 2 ? GROUPS * Tl::kElems : 8];
+  __shared__ __align__(16) uint16_t buf3[BUFS > 3 ? GROUPS * Tl::kElems : 8];
   const int tiles = g.tiles_m * g.tiles_n, id = tile_item(tiles * g.splits);
   if (id >= tiles * g.splits) return;
   const int split = id / tiles;
@@ -494,9 +529,28 @@ __global__ __launch_bounds__(64 * WR * WC) void head_product_kernel(TilePairs p,
   tile.init(p, at.m * BM, at.n * BN);
   f32x4 acc[Tl::MT][Tl::NT];
   const int64_t slices = Tl::slices(p);
-  tile.run(p, static_cast<int>(slices * split / g.splits), static_cast<int>(slices * (split + 1) / g.splits), buf0, buf1,
-           nullptr, nullptr, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / WC, wc = wave % WC;
+  const int group = Tl::group(), own = group * Tl::kElems;
+  tile.run(p, static_cast<int>(slices * split / g.splits), static_cast<int>(slices * (split + 1) / g.splits), buf0 + own,
+           buf1 + own, buf2 + (BUFS > 2 ? own : 0), buf3 + (BUFS > 3 ? own : 0), acc);
+  if constexpr (GROUPS > 1) {             // the first group adds what the others have, in their order, and goes on alone
+    static_assert((GROUPS - 1) * BM * BN * 4 <= GROUPS * Tl::kElems * 2, "the groups' sums fit a buffer");
+    f32x4* sums = reinterpret_cast<f32x4*>(buf0) + Tl::thread();
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < Tl::NT; ++j)
+#pragma unroll
+      for (int i = 0; i < Tl::MT; ++i)
+        if (group > 0) sums[((group - 1) * Tl::MT * Tl::NT + j * Tl::MT + i) * Tl::kThreads] = acc[i][j];
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 0; k < GROUPS - 1; ++k)
+#pragma unroll
+      for (int j = 0; j < Tl::NT; ++j)
+#pragma unroll
+        for (int i = 0; i < Tl::MT; ++i) acc[i][j] += sums[(k * Tl::MT * Tl::NT + j * Tl::MT + i) * Tl::kThreads];
+  }
+  const int lane = threadIdx.x & 63, wave = Tl::thread() >> 6, wr = wave / WC, wc = wave % WC;
   const float f = product_factor(g);
   const int back = g.x_most ? -x_shift(g.x_most) : 0;
 #pragma unroll
@@ -680,16 +734,18 @@ void split_x(const umem_head_desc& hd, int T, const void* x, uint16_t* parts, hi
 
 template <bool F16, typename OT>
 void product(const TilePairs& p, ProductArgs g, int side, hipStream_t s) {
-#define UMEM_PRODUCT(BM, BN, WR, WC)                                                                            \
-  {                                                                                                             \
-    g.tiles_m = (p.a_rows + BM - 1) / BM;                                                                       \
-    g.tiles_n = (p.b_rows + BN - 1) / BN;                                                                       \
-    hipLaunchKernelGGL((head_product_kernel<F16, OT, BM, BN, WR, WC>),                                          \
-                       dim3(tile_grid(g.tiles_m * g.tiles_n * g.splits)), dim3(64 * WR * WC), 0, s, p, g);      \
-  }
-  if (side == 256) UMEM_PRODUCT(256, 256, 2, 4)
-  else if (side == 128) UMEM_PRODUCT(128, 128, 2, 2)
-  else UMEM_PRODUCT(64, 64, 2, 2)
+#define UMEM_PRODUCT(BM, WR, WC, BUFS, GROUPS)                                                                  \
+  hipLaunchKernelGGL((head_product_kernel<F16, OT, BM, BM, WR, WC, BUFS, GROUPS>), dim3(tile_grid(items)),      \
+                     dim3(64 * WR * WC * GROUPS), 0, s, p, g)
+  g.tiles_m = (p.a_rows + side - 1) / side;
+  g.tiles_n = (p.b_rows + side - 1) / side;
+  const int items = g.tiles_m * g.tiles_n * g.splits;
+  if (side == 256) UMEM_PRODUCT(256, 2, 4, 2, 1);
+  else if (side == 128 && items > kCus) UMEM_PRODUCT(128, 2, 2, 2, 1);
+  else if (side == 128) UMEM_PRODUCT(128, 2, 2, 2, 2);
+  else if (items > 2 * kCus) UMEM_PRODUCT(64, 2, 2, 2, 1);
+  else if (items > kCus) UMEM_PRODUCT(64, 2, 2, 2, 2);
+  else UMEM_PRODUCT(64, 2, 2, 2, 4);
 #undef UMEM_PRODUCT
 }
 
@@ -697,16 +753,17 @@ template <int PR, int PC>
 void slope(const TilePairs& p, float scale, const int32_t* targets, const float* lse, const float* dloss,
            const float* most, int v_first, int vocab, int piece, int t_ld, uint16_t* rows, uint16_t* cols,
            float* lost, hipStream_t s) {
-#define UMEM_SLOPE(BM, BN, WR, WC)                                                                              \
-  {                                                                                                             \
-    const int tm = (piece + BM - 1) / BM, tn = (p.b_rows + BN - 1) / BN;                                        \
-    hipLaunchKernelGGL((head_slope_kernel<BM, BN, WR, WC, PR, PC>), dim3(tile_grid(tm * tn)),                   \
-                       dim3(64 * WR * WC), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first, vocab,    \
-                       piece, t_ld, rows, cols, lost);                                                          \
-  }
   // (of 256 x 256 tiles one at a time is on a CU, and nothing beside its end)
-  if (tile_plan(piece, p.b_rows, slice_count(p.k, p.n), 1, false).side == 128) UMEM_SLOPE(128, 128, 2, 2)
-  else UMEM_SLOPE(64, 64, 2, 2)
+  const int side = tile_plan(piece, p.b_rows, slice_count(p.k, p.n), 1, false).side;
+  const int tm = (piece + side - 1) / side, tn = (p.b_rows + side - 1) / side;
+#define UMEM_SLOPE(BM, WR, WC, GROUPS)                                                                          \
+  hipLaunchKernelGGL((head_slope_kernel<BM, BM, WR, WC, GROUPS, PR, PC>), dim3(tile_grid(tm * tn)),             \
+                     dim3(64 * WR * WC * GROUPS), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first,   \
+                     vocab, piece, t_ld, rows, cols, lost)
+  if (side == 128 && tm * tn > kCus) UMEM_SLOPE(128, 2, 2, 1);
+  else if (side == 128) UMEM_SLOPE(128, 2, 2, 2);
+  else if (tm * tn > 2 * kCus) UMEM_SLOPE(64, 2, 2, 1);
+  else UMEM_SLOPE(64, 2, 2, 2);
 #undef UMEM_SLOPE
 }
 
@@ -727,25 +784,24 @@ hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, cons
     const char* xb = static_cast<const char*>(x) + static_cast<size_t>(t0) * hd.d * (hd.xtype == UMEM_F32 ? 4 : 2);
     if (hd.xtype == UMEM_F32) split_x(hd, t, xb, parts, s);
     const TilePairs p = logit_pairs(hd, t, xb, parts, w, hd.vocab);
-    int tiles = 0;
-#define UMEM_STATS(BM, BN, WR, WC)                                                                              \
-  {                                                                                                             \
-    const int tn = (t + BN - 1) / BN;                                                                           \
-    tiles = (hd.vocab + BM - 1) / BM;                                                                           \
-    hipLaunchKernelGGL((head_stats_kernel<BM, BN, WR, WC>), dim3(tile_grid(tiles * tn)), dim3(64 * WR * WC), 0, \
-                       s, p, tiles, tn, hd.scale, targets + t0, stats, goal);                                   \
-  }
     const int side = tile_plan(hd.vocab, t, slice_count(p.k, p.n), 1, true).side;
-    if (side == 256) UMEM_STATS(256, 256, 2, 4)
-    else if (side == 128) UMEM_STATS(128, 128, 2, 2)
-    else UMEM_STATS(64, 64, 2, 2)
+    const int tiles = (hd.vocab + side - 1) / side, tn = (t + side - 1) / side;
+    const double scale = std::fabs(hd.scale);
+#define UMEM_STATS(BM, WR, WC, GROUPS)                                                                           \
+  hipLaunchKernelGGL((head_stats_kernel<BM, BM, WR, WC, GROUPS>), dim3(tile_grid(tiles * tn)),                   \
+                     dim3(64 * WR * WC * GROUPS), 0, s, p, tiles, tn, hd.scale, targets + t0, stats, goal)
+    if (side == 256) UMEM_STATS(256, 2, 4, 1);
+    else if (side == 128 && tiles * tn > kCus) UMEM_STATS(128, 2, 2, 1);
+    else if (side == 128) UMEM_STATS(128, 2, 2, 2);
+    else if (tiles * tn > 2 * kCus) UMEM_STATS(64, 2, 2, 1);
+    else UMEM_STATS(64, 2, 2, 2);
 #undef UMEM_STATS
     if (t <= kFewTokens)
       hipLaunchKernelGGL(head_join_few_kernel, dim3(t), dim3(kThreads), 0, s, stats, goal, targets + t0, t, hd.vocab, tiles,
-                         loss + t0, lse + t0);
+                         scale, loss + t0, lse + t0);
     else
       hipLaunchKernelGGL(head_join_kernel, dim3((t + 15) / 16), dim3(kThreads), 0, s, stats, goal, targets + t0, t,
-                         hd.vocab, tiles, loss + t0, lse + t0);
+                         hd.vocab, tiles, scale, loss + t0, lse + t0);
   }
   return hipGetLastError();
 }
@@ -767,19 +823,17 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
   float* most = dloss ? reinterpret_cast<float*>(base + L.most) : nullptr;
   float* x_most = reinterpret_cast<float*>(base + L.x_most);
   float* lost = reinterpret_cast<float*>(base + L.lost);
-  if (dloss)
-    hipLaunchKernelGGL(head_most_kernel, dim3(kMostBlocks), dim3(kThreads), 0, s, dloss, targets, T, V, most);
   // x's channels along rows, tokens along k
   const dim3 x_grid(t_pad / 64, (d + 63) / 64);
   if (wide) {
     const float* xf = static_cast<const float*>(x);
     split_x(hd, T, x, parts, s);
-    hipLaunchKernelGGL(head_most_x_kernel<float>, dim3(kMostBlocks), dim3(1024), 0, s, xf, targets, T, d, V, x_most);
+    hipLaunchKernelGGL(head_most_kernel<float>, dim3(kMostBlocks), dim3(1024), 0, s, xf, dloss, targets, T, d, V, most, x_most);
     const auto turn = px == 2 ? head_transpose_kernel<float, 2> : head_transpose_kernel<float, 1>;
     hipLaunchKernelGGL(turn, x_grid, dim3(kThreads), 0, s, xf, T, d, xt, static_cast<int64_t>(t_ld), x_most, targets, V);
   } else {
-    hipLaunchKernelGGL(head_most_x_kernel<__bf16>, dim3(kMostBlocks), dim3(1024), 0, s, static_cast<const __bf16*>(x),
-                       targets, T, d, V, x_most);
+    hipLaunchKernelGGL(head_most_kernel<__bf16>, dim3(kMostBlocks), dim3(1024), 0, s, static_cast<const __bf16*>(x), dloss,
+                       targets, T, d, V, most, x_most);
     hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), x_grid, dim3(kThreads), 0, s,
                        static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_ld), x_most, targets, V);
   }

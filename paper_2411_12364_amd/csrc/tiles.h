@@ -274,6 +274,36 @@ struct Tile {
 #pragma unroll
       for (int j = 0; j < NT; ++j) out[i][j] = kAccs == 2 ? acc[0][i][j] + acc[kAccs - 1][i][j] : acc[0][i][j];
   }
+
+  // What each of two groups keeps of the tile for its end, the sums of both: the half of the columns' blocks with its
+  // number, through all of a buffer of GROUPS kElems.  (Of one group: everything.)
+  static constexpr int NE = NT / (GROUPS > 1 ? 2 : 1);
+  __device__ __forceinline__ static void share(const f32x4 (&acc)[MT][NT], uint16_t* lds, f32x4 (&out)[MT][NE]) {
+    if constexpr (GROUPS == 1) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) out[i][j] = acc[i][j];
+    } else {
+      static_assert(GROUPS == 2 && NT % 2 == 0 && BM * BN * 4 <= GROUPS * kElems * 2, "halves of a tile fit a buffer");
+      const int g = group();
+      f32x4* const to = reinterpret_cast<f32x4*>(lds) + g * MT * NE * kThreads + thread();
+      const f32x4* const from = reinterpret_cast<const f32x4*>(lds) + (1 - g) * MT * NE * kThreads + thread();
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NE; ++j) to[(i * NE + j) * kThreads] = g == 0 ? acc[i][j + NE] : acc[i][j];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+          const f32x4 other = from[(i * NE + j) * kThreads], own = g == 0 ? acc[i][j] : acc[i][j + NE];
+          out[i][j] = g == 0 ? own + other : other + own;
+        }
+    }
+  }
 };
 
 // The tile that a workgroup takes: the items of one XCD (workgroups go to the XCDs in turn) are consecutive, and run down

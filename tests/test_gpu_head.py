@@ -260,6 +260,32 @@ def test_large_logits():
     assert abs(float(dx[0, 0]) - 98 * np.exp(-64.0)) <= (2 * HALF + 80 * u) * 98 * np.exp(-64.0)
 
 
+@pytest.mark.parametrize("scale", (1.0, -1.0))
+@pytest.mark.parametrize("T, vocab", ((5, 70), (5, 130), (300, 300), (3000, 5000), (520, 200)))
+def test_logits_far_below_zero(T, vocab, scale):
+    """All logits about -300, so that a reference of 0 anywhere (of a wave without rows of W) would lose them; some rows'
+    are -infinity, a whole tile's among them."""
+    d = 8
+    rng = np.random.default_rng(vocab)
+    x = torch.zeros((T, d), dtype=BF, device="cuda")
+    w = torch.zeros((vocab, d), dtype=BF, device="cuda")
+    x[:, 0] = 16.0 * scale
+    x[:, 1] = torch.tensor(rng.integers(0, 2, size=T), device="cuda").to(BF)
+    w[:, 0] = torch.tensor(-19.0 + rng.integers(0, 8, size=vocab) / 8, device="cuda").to(BF)
+    w[:, 1] = scale
+    w[vocab // 2:vocab - 1, 0] = -float("inf")
+    y = torch.tensor(rng.integers(0, vocab // 2, size=T), device="cuda", dtype=torch.int32)
+    loss, lse = forward(desc(vocab, d, BF, F, scale), x, w, y)
+    z = np.outer(host(x)[:, 0], host(w)[:, 0]) * scale + host(x)[:, 1:2]
+    top = z.max(axis=1)
+    exact = top + np.log(np.exp(z - top[:, None]).sum(axis=1))
+    goal = z[np.arange(T), y.cpu().numpy()]
+    # products and z are exact; exp2's argument and value, sums of 256 and a rounding of either output
+    slack = 300 * u + u * np.abs(exact)
+    assert (np.abs(host(lse) - exact) <= slack).all()
+    assert (np.abs(host(loss) - (exact - goal)) <= 300 * u + u * np.abs(exact - goal)).all()
+
+
 def test_gradients_against_differences():
     """The gradients along random directions against central differences of the float64 loss."""
     T, vocab, d = 90, 150, 64
