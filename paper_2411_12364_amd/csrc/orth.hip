@@ -321,46 +321,44 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_
   tile.run(p, from, to, buf0 + mine, buf1 + mine, buf2 + (BUFS > 2 ? mine : 0), buf3 + (BUFS > 3 ? mine : 0), acc);
   const int lane = threadIdx.x & 63, wave = Tl::thread() >> 6, wr = wave / WC, wc = wave % WC;
   const int m_in = wr * Tl::MT * 16 + 4 * (lane >> 4), n_in = wc * Tl::NT * 16 + (lane & 15);
-  if constexpr (GROUPS == 2) {                              // the first group adds what the second has, and goes on alone
-    static_assert(BM * BN * 4 <= kLds * 2, "a group's sums fit a buffer");
+  // Of several groups each ends a share of the tile's blocks, the sums of all of them in their order.
+  constexpr int kBlocks = Tl::MT * Tl::NT, kOwn = kBlocks / GROUPS;
+  f32x4 sum[kOwn];
+  if constexpr (GROUPS > 1) {
+    static_assert(kBlocks % GROUPS == 0 && BM * BN * 4 <= Tl::kElems * 2, "a group's blocks fit its part of a buffer");
     f32x4* sums = reinterpret_cast<f32x4*>(buf1) + Tl::thread();
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < Tl::NT; ++j)
-#pragma unroll
-      for (int i = 0; i < Tl::MT; ++i)
-        if (group == 1) sums[(j * Tl::MT + i) * Tl::kThreads] = acc[i][j];
+    for (int o = 0; o < kBlocks; ++o) sums[(group * kBlocks + o) * Tl::kThreads] = acc[o % Tl::MT][o / Tl::MT];
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < Tl::NT; ++j)
+    for (int o = 0; o < kOwn; ++o) {
+      sum[o] = sums[(group * kOwn + o) * Tl::kThreads];
 #pragma unroll
-      for (int i = 0; i < Tl::MT; ++i)
-        if (group == 0) acc[i][j] += sums[(j * Tl::MT + i) * Tl::kThreads];
+      for (int i = 1; i < GROUPS; ++i) sum[o] += sums[(i * kBlocks + group * kOwn + o) * Tl::kThreads];
+    }
+  } else {
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o) sum[o] = acc[o % Tl::MT][o / Tl::MT];
   }
+  const auto m_of = [&](int o) { return m_in + (GROUPS == 1 ? o : group * kOwn + o) % Tl::MT * 16; };
+  const auto n_of = [&](int o) { return n_in + (GROUPS == 1 ? o : group * kOwn + o) / Tl::MT * 16; };
   if (g.splits > 1) {
-    if (group != 0) return;
     float* to = g.partial + static_cast<int64_t>(id) * (BM * BN);
 #pragma unroll
-    for (int j = 0; j < Tl::NT; ++j)
-#pragma unroll
-      for (int i = 0; i < Tl::MT; ++i)
-        *reinterpret_cast<f32x4*>(to + (n_in + j * 16) * BM + m_in + i * 16) = acc[i][j];
+    for (int o = 0; o < kOwn; ++o) *reinterpret_cast<f32x4*>(to + n_of(o) * BM + m_of(o)) = sum[o];
     return;
   }
   const auto word = [&](int n, int m) {
     uint16_t* half = BN == 64 || n < BN / 2 ? buf0 : buf1;
     return reinterpret_cast<uint32_t*>(half) + word_at<BM>(BN == 64 ? n : n % (BN / 2), m);
   };
-  if (!is_last(MODE)) __syncthreads();                      // the last slice has been read
+  if (!is_last(MODE) && GROUPS == 1) __syncthreads();       // the last slice has been read
 #pragma unroll
-  for (int j = 0; j < Tl::NT; ++j)
-#pragma unroll
-    for (int i = 0; i < Tl::MT; ++i) {
-      if (group != 0) break;
-      const int n = n_in + j * 16, m = m_in + i * 16;
-      const u32x4 w = finish_four<MODE, OT>(g, at.mat, at.n * BN + n, at.m * BM + m, acc[i][j]);
-      if (!is_last(MODE)) *reinterpret_cast<u32x4*>(word(n, m)) = w;
-    }
+  for (int o = 0; o < kOwn; ++o) {
+    const u32x4 w = finish_four<MODE, OT>(g, at.mat, at.n * BN + n_of(o), at.m * BM + m_of(o), sum[o]);
+    if (!is_last(MODE)) *reinterpret_cast<u32x4*>(word(n_of(o), m_of(o))) = w;
+  }
   if (is_last(MODE)) return;
   __syncthreads();
   put_block<MODE, BM, BN, Tl::kThreads * GROUPS>(g, second ? g.out2 : g.out, at.mat, at.m * BM, at.n * BN, at.m != at.n, word);
@@ -408,7 +406,8 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 struct Plan {
   int bm, splits;
   double us;
-  bool alone;             // every workgroup has a CU to itself: two groups of waves share its slices
+  bool alone;             // every workgroup has a CU to itself: two groups of waves share its slices (four with two buffers
+                          // each 1.15 times as long; two where two workgroups share a CU, or four buffers, the same)
 };
 constexpr int kMostSplits = 16, kCus = 256;
 constexpr size_t kPartialBytes = size_t{64} << 20;
