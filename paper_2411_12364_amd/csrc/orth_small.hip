@@ -29,13 +29,14 @@ __device__ __forceinline__ f64x4 mfma64(double a, double b, f64x4 c) {
 
 // A 64-wide slice of G's longer side into registers, and from there into LDS as [smaller side][longer side] with zeros
 // past both.
-template <typename T, bool TALL>
+template <typename T, bool TALL, int THREADS = kThreads>
 struct Slice {
-  float v[16];
+  static constexpr int kEach = kSide * 64 / THREADS;
+  float v[kEach];
   __device__ __forceinline__ void load(const T* g, int m, int64_t k, int64_t k0) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int in = threadIdx.x % 64, out = threadIdx.x / 64 + 4 * i;      // in: along G's rows
+    for (int i = 0; i < kEach; ++i) {
+      const int in = threadIdx.x % 64, out = threadIdx.x / 64 + THREADS / 64 * i;       // in: along G's rows
       const int s = TALL ? in : out;
       const int64_t l = k0 + (TALL ? out : in);
       v[i] = s < m && l < k ? static_cast<float>(g[TALL ? l * m + s : s * k + l]) : 0.f;
@@ -43,8 +44,8 @@ struct Slice {
   }
   __device__ __forceinline__ void store(float (*t)[kTilePitch]) const {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int in = threadIdx.x % 64, out = threadIdx.x / 64 + 4 * i;
+    for (int i = 0; i < kEach; ++i) {
+      const int in = threadIdx.x % 64, out = threadIdx.x / 64 + THREADS / 64 * i;
       t[TALL ? in : out][TALL ? out : in] = v[i];
     }
   }
@@ -189,49 +190,43 @@ __global__ __launch_bounds__(kStepThreads) void orth_small_steps_kernel(const do
   }
 }
 
-// out = decay out + scale Q G (G Q where G is tall) over 64 of the longer side, a wave 16 of them.
+// out = decay out + scale Q G (G Q where G is tall) over 64 of the longer side, a 16 x 16 block a wave (with four blocks a
+// wave, one wave to each of a CU's parts, 64 x 448 took 10 us, so 5.6).
 template <typename GT, typename OT, bool TALL>
-__global__ __launch_bounds__(kThreads) void orth_small_apply_kernel(const GT* g, int m, int k, const double* __restrict__ q,
-                                                                    OT* out, float decay, float scale) {
+__global__ __launch_bounds__(kStepThreads) void orth_small_apply_kernel(const GT* g, int m, int k, const double* __restrict__ q,
+                                                                        OT* out, float decay, float scale) {
   __shared__ double Q[kSide][kPitch];
   __shared__ float t[kSide][kTilePitch];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i0 = (wave >> 2) * 16, l0 = (wave & 3) * 16;
   const int64_t mat = blockIdx.y, k0 = static_cast<int64_t>(blockIdx.x) * 64, base = mat * m * static_cast<int64_t>(k);
-  Slice<GT, TALL> s;
+  Slice<GT, TALL, kStepThreads> s;
   s.load(g + base, m, k, k0);
 #pragma unroll
-  for (int i = 0; i < kSide * kSide / kThreads; ++i) {
-    const int at = i * kThreads + threadIdx.x, row = at / kSide, col = at % kSide;
+  for (int i = 0; i < kSide * kSide / kStepThreads; ++i) {
+    const int at = i * kStepThreads + threadIdx.x, row = at / kSide, col = at % kSide;
     Q[row][col] = row < m && col < m ? q[mat * kSide * kSide + at] : 0.0;
   }
   s.store(t);
   __syncthreads();
-  f64x4 acc[4];
+  if (i0 >= m) return;
+  f64x4 acc = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) acc[i] = f64x4{0.0, 0.0, 0.0, 0.0};
-#pragma unroll 4
   for (int j0 = 0; j0 < kSide; j0 += 4) {
     const int j = j0 + (lane >> 4);
-    const double x = t[j][wave * 16 + (lane & 15)];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const double w = Q[i * 16 + (lane & 15)][j];
-      acc[i] = TALL ? mfma64(x, w, acc[i]) : mfma64(w, x, acc[i]);
-    }
+    const double x = t[j][l0 + (lane & 15)], w = Q[i0 + (lane & 15)][j];
+    acc = TALL ? mfma64(x, w, acc) : mfma64(w, x, acc);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int a = (lane >> 4) + 4 * r, b = lane & 15;
-      const int small = i * 16 + (TALL ? b : a);
-      const int64_t at = k0 + wave * 16 + (TALL ? a : b);
-      if (small >= m || at >= k) continue;
-      OT* to = out + base + (TALL ? at * m + small : small * static_cast<int64_t>(k) + at);
-      double v = static_cast<double>(scale) * acc[i][r];
-      if (decay != 0.f) v = fma(static_cast<double>(decay), static_cast<double>(static_cast<float>(*to)), v);
-      *to = static_cast<OT>(static_cast<float>(v));
-    }
+  for (int r = 0; r < 4; ++r) {
+    const int a = (lane >> 4) + 4 * r, b = lane & 15;
+    const int small = i0 + (TALL ? b : a);
+    const int64_t at = k0 + l0 + (TALL ? a : b);
+    if (small >= m || at >= k) continue;
+    OT* to = out + base + (TALL ? at * m + small : small * static_cast<int64_t>(k) + at);
+    double v = static_cast<double>(scale) * acc[r];
+    if (decay != 0.f) v = fma(static_cast<double>(decay), static_cast<double>(static_cast<float>(*to)), v);
+    *to = static_cast<OT>(static_cast<float>(v));
+  }
 }
 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
@@ -246,10 +241,10 @@ template <bool TALL, typename GT, typename OT>
 void run(const umem_orth_desc& od, const GT* g, OT* out, double* pieces, double* q, hipStream_t s) {
   const int m = std::min(od.rows, od.cols), k = std::max(od.rows, od.cols), chunks = chunk_count(od);
   hipLaunchKernelGGL((orth_small_gram_kernel<GT, TALL>), dim3(chunks, od.n), dim3(kThreads), 0, s, g, m, k, chunks, pieces);
-  const auto step = m <= 16 ? orth_small_steps_kernel<16> : m <= 32 ? orth_small_steps_kernel<32> : orth_small_steps_kernel<64>;
+  const auto step = m <= 16 ? orth_small_steps_kernel<16> : m <= 32 ? orth_small_steps_kernel<32> : m <= 48 ? orth_small_steps_kernel<48> : orth_small_steps_kernel<64>;
   hipLaunchKernelGGL(step, dim3(od.n), dim3(kStepThreads), 0, s, pieces, m, chunks, od.steps, static_cast<double>(od.a),
                      static_cast<double>(od.b), static_cast<double>(od.c), od.eps, q);
-  hipLaunchKernelGGL((orth_small_apply_kernel<GT, OT, TALL>), dim3((k + 63) / 64, od.n), dim3(kThreads), 0, s, g, m, k, q,
+  hipLaunchKernelGGL((orth_small_apply_kernel<GT, OT, TALL>), dim3((k + 63) / 64, od.n), dim3(kStepThreads), 0, s, g, m, k, q,
                      out, od.decay, od.scale);
 }
 

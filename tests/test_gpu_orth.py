@@ -119,7 +119,8 @@ def test_update(n, rows, cols, gt, ot):
     check(n, rows, cols, gt, ot)
 
 
-@pytest.mark.parametrize("rows,cols", [(96, 160), (160, 96), (128, 128), (80, 4000), (6000, 72)])
+@pytest.mark.parametrize("rows,cols", [(96, 160), (160, 96), (128, 128), (80, 4000), (6000, 72), (64, 200), (90, 49), (48, 500), (17, 30),
+                                       (333, 16)])
 @pytest.mark.parametrize("kw", [dict(steps=3), dict(steps=4), dict(steps=6), dict(steps=7), dict(steps=16, coef=(1.5, -0.5, 0.0)),
                                 dict(coef=(6.0, -13.0, 8.0), steps=2), dict(coef=(11.0, -20.0, 10.0), steps=2), dict(steps=1), dict(steps=2), dict(steps=8), dict(coef=(1.5, -0.5, 0.0), steps=12),
                                 dict(coef=(2.0, -1.5, 0.5)), dict(decay=0.9, scale=-0.02), dict(decay=-1.0, scale=3.0),
