@@ -468,8 +468,10 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(const uint2* __res
   put_row<ROWS>(out, ROWS ? static_cast<int64_t>(place[last - 1]) : key, d, c, sum, scale);
 }
 
-// Sorted places of a run: 16, so that there are many runs, and from 2^16 places on as many as give 4,096 runs.
-int run_length(int T) { return std::max(16, (T + 4095) / 4096); }
+// Sorted places of a run: 16, so that there are many runs, and from 2^16 places on as many as give 4,096 runs; of up
+// to 2,048 places 8, which a wave has in flight at once.
+constexpr int kShortPlaces = 2048;
+int run_length(int T) { return T <= kShortPlaces ? kAhead : std::max(16, (T + 4095) / 4096); }
 int most_runs(int T) { return (T + run_length(T) - 1) / run_length(T); }
 // The bits of the numbers below `vocab`.
 int key_bits(int64_t vocab) {
@@ -494,8 +496,9 @@ hipError_t backward(const umem_embed_desc& ed, int T, const int32_t* ids, const 
   const bool packed = place_bits + word_bits <= 32;
   bool ranked = false;
   if (T <= kSmallPlaces && packed) {
-    hipLaunchKernelGGL(embed_sort_kernel<kSmallSteps>, dim3(1), dim3(kSmallThreads), 0, s, ids, T, ed.vocab, place_bits,
-                       passes, sorted, p.n, ROWS ? place : nullptr, rows, n_rows);
+    const auto sort = T <= kSmallThreads ? embed_sort_kernel<1> : embed_sort_kernel<kSmallSteps>;
+    hipLaunchKernelGGL(sort, dim3(1), dim3(kSmallThreads), 0, s, ids, T, ed.vocab, place_bits, passes, sorted, p.n,
+                       ROWS ? place : nullptr, rows, n_rows);
     ranked = true;
   } else if (T <= kPassPlaces && packed) {
     // the words change between the halves of the other array of pairs
@@ -524,8 +527,9 @@ hipError_t backward(const umem_embed_desc& ed, int T, const int32_t* ids, const 
   const dim3 grid(static_cast<unsigned>((items + 3) / 4));
   hipLaunchKernelGGL((embed_sum_kernel<GT, ROWS>), grid, dim3(kThreads), 0, s, sorted, p.n, place, dout, out, edge, run,
                      slabs, ed.d, ed.scale);
-  hipLaunchKernelGGL((embed_join_kernel<ROWS>), dim3(most_runs(T), slabs), dim3(kThreads), 0, s, sorted, p.n, place, out,
-                     edge, run, ed.d, ed.scale);
+  if (most_runs(T) > 1)
+    hipLaunchKernelGGL((embed_join_kernel<ROWS>), dim3(most_runs(T), slabs), dim3(kThreads), 0, s, sorted, p.n, place, out,
+                       edge, run, ed.d, ed.scale);
   return hipGetLastError();
 }
 
@@ -555,7 +559,7 @@ hipError_t launch_embed(const umem_embed_desc& ed, int T, const void* table, con
 size_t embed_backward_workspace_bytes(const umem_embed_desc& ed, int T) {
   if (T == 0) return 0;
   // (as many runs as any number of tokens up to T has: 4,096 from 2^16 - 15 of them on)
-  const int runs = T > (1 << 16) - 16 ? 4096 : most_runs(T);
+  const int runs = T > (1 << 16) - 16 ? 4096 : std::max(most_runs(T), most_runs(std::min(T, kShortPlaces)));
   return up256(sort_workspace_bytes(T)) + up256(static_cast<size_t>(runs) * 2 * ed.d * sizeof(float)) +
          up256(static_cast<size_t>((T + kRankTile - 1) / kRankTile) * sizeof(uint32_t));
 }

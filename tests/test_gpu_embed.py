@@ -136,7 +136,8 @@ def check_backward(T, vocab, d, gt, kind, lead=0, scale=0.75, seed=0):
 @pytest.mark.parametrize("kind", ["text", "same", "distinct", "none"])
 @pytest.mark.parametrize("T,vocab,d,lead", [(1, 1, 1, 0), (2, 3, 5, 1), (15, 40, 64, 0), (16, 16, 256, 0), (17, 9, 255, 0),
                                             (31, 2, 257, 2), (33, 5000, 130, 0), (255, 300, 1023, 1), (1025, 777, 64, 0),
-                                            (2000, 60, 512, 0), (4097, 2049, 96, 0)])
+                                            (2000, 60, 512, 0), (4097, 2049, 96, 0), (8, 3, 5, 0), (9, 2, 260, 0),
+                                            (1023, 900, 8, 0), (1024, 3, 260, 0), (2048, 5, 72, 0), (2049, 5, 72, 0)])
 def test_gradient(T, vocab, d, lead, kind, gt):
     print(f"[case] embed backward {T} {vocab} {d} {lead} {kind} {gt}", flush=True)
     check_backward(T, vocab, d, gt, kind, lead)
@@ -158,7 +159,7 @@ def test_workspace_of_more_tokens_and_a_stream():
     ds = desc(1000, 96, torch.float32, torch.float32, 1.0)
     ws = workspace(ds, 70000)
     side = torch.cuda.Stream()
-    for T in (3, 4096, 4097, 65521, 65536, 65537, 70000):
+    for T in (3, 1024, 2048, 2049, 4096, 4097, 65521, 65536, 65537, 70000):
         g = gen(T)
         ids, dout = tokens("text", T, 1000, g), torch.randn((T, 96), generator=g, device="cuda")
         a, b = torch.zeros((1000, 96), device="cuda"), torch.zeros((1000, 96), device="cuda")
