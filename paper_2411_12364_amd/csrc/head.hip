@@ -197,12 +197,14 @@ __global__ __launch_bounds__(kThreads) void head_transpose_kernel(const T* __res
 
 // ---------------------------------------------------------------- forward
 
-// Each token's (reference, sum of exp(z - reference |scale|)) over the tile's rows of W, to stats[tile][T]; z = |scale| u, u the
-// product (with its sign turned where scale is below 0), the reference is the largest u, or 0 where that is infinite or none;
-// with a sum of 0 -infinity, so that it raises no other's.
-// goal[t]: the target's u, by the tile that holds it.  The end of a tile takes 8 clocks of a lane's for each logit, 4 of
-// them exp2's: with the target and W's last row looked for at each the kernel took 1.05 times as long.
-constexpr float kLog2e = 1.44269504f, kLargest = 3.4e38f;
+// Each token's (reference, sum of exp(z - reference)) over the tile's rows of W, to stats[tile][T], in units of u, the
+// product with its sign turned where scale is below 0: z = |scale| u (and spread_of).  The reference is the largest u, or 0
+// where that is infinite or none; with a sum of 0 it is -infinity, so that it raises no other's.  goal[t]: the target's u,
+// by the tile that holds it.  The end of a tile takes 8 clocks of a lane's for each logit, 4 of them exp2's: with the target
+// and W's last row looked for at each the kernel took 1.05 times as long.
+constexpr float kLog2e = 1.44269504f;
+// What the products are multiplied by, so that |scale| log2(e) does not overflow; scale / it takes scale's place.
+__host__ __device__ __forceinline__ float spread_of(float scale) { return fabsf(scale) > 1e38f ? 4.f : 1.f; }
 
 template <int BM, int BN, int WR, int WC, int GROUPS>
 __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_stats_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
@@ -226,14 +228,14 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_stats_kernel(TileP
   const int lane = threadIdx.x & 63, wave = Tl::thread() >> 6, wr = wave / WC, wc = wave % WC;
   const int V = p.a_rows, T = p.b_rows;
   const int v0 = at.m * BM + wr * MT * 16 + 4 * (lane >> 4);
-  const float c = fminf(fabsf(scale) * kLog2e, kLargest);
+  const float spread = spread_of(scale), turn = scale < 0.f ? -spread : spread, c = fabsf(scale) / spread * kLog2e;
   const bool edge = at.m * BM + BM > V;                     // (uniform: W's last rows)
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const int n = (wc * Tl::NT + group * NT + j) * 16 + (lane & 15), t = at.n * BN + n;
-    if (scale < 0.f) {
+    if (turn != 1.f) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) acc[i][j] = -acc[i][j];
+      for (int i = 0; i < MT; ++i) acc[i][j] *= turn;
     }
     const int in = (t < T ? targets[t] : -1) - v0;          // the target's entry, which few waves hold one of
     const bool holds = in >= 0 && in < MT * 16 && (in & 15) < 4 && v0 + in < V;
@@ -280,7 +282,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_stats_kernel(TileP
   }
 }
 
-// The tiles' pairs of each token, 16 lanes a token, added in fp64 in the order of the tiles; scale here is |scale|.
+// The tiles' pairs of each token, 16 lanes a token, added in fp64 in the order of the tiles; scale here is u's factor.
 __global__ __launch_bounds__(kThreads) void head_join_kernel(const float2* __restrict__ stats,
                                                              const float* __restrict__ goal,
                                                              const int32_t* __restrict__ targets, int T, int vocab,
@@ -800,7 +802,7 @@ hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, cons
     const TilePairs p = logit_pairs(hd, t, xb, parts, w, hd.vocab);
     const int side = tile_plan(hd.vocab, t, slice_count(p.k, p.n), 1, true).side;
     const int tiles = (hd.vocab + side - 1) / side, tn = (t + side - 1) / side;
-    const double scale = std::fabs(hd.scale);
+    const double scale = std::fabs(hd.scale / spread_of(hd.scale));
 #define UMEM_STATS(BM, WR, WC, GROUPS)                                                                           \
   hipLaunchKernelGGL((head_stats_kernel<BM, BM, WR, WC, GROUPS>), dim3(tile_grid(tiles * tn)),                   \
                      dim3(64 * WR * WC * GROUPS), 0, s, p, tiles, tn, hd.scale, targets + t0, stats, goal)

@@ -148,7 +148,7 @@ def test_loss_and_gradients(T, vocab, d, xt, gt):
 
 @pytest.mark.parametrize("xt,gt", [(F, F), (BF, F), (BF, BF)])
 @pytest.mark.parametrize("kw", [dict(scale=0.25), dict(scale=-3.0), dict(none=0.0), dict(none=1.0), dict(uniform=True),
-                                dict(none=0.9, scale=8.0), dict(scale=0.0001)])
+                                dict(none=0.9, scale=8.0), dict(scale=0.0001), dict(scale=-0.0001)])
 def test_scales_and_masks(kw, xt, gt):
     print(f"[case] head {kw} {xt} {gt}", flush=True)
     check(150, 400, 128, xt, gt, **kw)
@@ -158,6 +158,21 @@ def test_scales_and_masks(kw, xt, gt):
                                              (140, 140, 2048, F, F), (300, 20000, 64, BF, BF)])
 def test_pieces_and_long_sums(T, vocab, d, xt, gt):
     """A vocabulary of several pieces, many tokens, wide states."""
+    print(f"[case] head {T} {vocab} {d} {xt} {gt}", flush=True)
+    check(T, vocab, d, xt, gt)
+
+
+# Sizes that between them reach every tile, group and split of the four products, in each type.
+TILES = [(148, 11497, 72), (3, 10974, 144), (452, 8507, 72), (3, 13437, 200), (6331, 327, 72), (3, 6922, 584), (5634, 656, 72)]
+TILES_OF_X = [(4186, 6, 200), (6636, 5, 272), (7168, 4, 392), (6148, 4, 656), (4617, 4, 1688), (4604, 279, 72)]
+
+
+@pytest.mark.parametrize("T,vocab,d,xt,gt", [(*t, BF, BF) for t in TILES] + [(*t, BF, F) for t in TILES] +
+                         [(*t, F, BF) for t in TILES_OF_X] + [(*t, BF, BF) for t in TILES_OF_X] +
+                         [(3, 8297, 80, BF, F), (4, 16296, 896, BF, F), (4, 12778, 1736, BF, BF), (3, 5054, 1560, F, BF),
+                          (4604, 279, 72, BF, F), (4604, 279, 72, F, F), (6331, 327, 72, F, F), (5634, 656, 72, F, F),
+                          (2908, 1052, 88, F, BF), (2052, 5024, 72, F, BF), (6209, 1290, 152, F, BF)])
+def test_tiles(T, vocab, d, xt, gt):
     print(f"[case] head {T} {vocab} {d} {xt} {gt}", flush=True)
     check(T, vocab, d, xt, gt)
 
@@ -240,6 +255,37 @@ def test_infinite_logits():
     w[150:, 0] = float("inf")
     loss, lse = forward(ds, x, w, y)
     assert bool((lse == float("inf")).all()) and bool((loss == float("inf")).all())
+
+
+@pytest.mark.parametrize("xt,gt", [(F, F), (BF, BF)])
+def test_no_scale(xt, gt):
+    """A factor of 0: every logit is 0, and every gradient."""
+    T, vocab, d = 70, 300, 64
+    x, w, y, dloss = make(T, vocab, d, xt)
+    ds = desc(vocab, d, xt, gt, 0.0)
+    loss, lse = forward(ds, x, w, y)
+    assert float((lse - np.log(300.0)).abs().max()) <= 16 * u
+    assert torch.equal(loss, torch.where((y >= 0) & (y < vocab), lse, 0.0))
+    dx, dw = backward(ds, x, w, y, lse, dloss, gt)
+    assert not dx.any() and not dw.any()
+
+
+@pytest.mark.parametrize("scale", [3.0e38, -3.0e38])
+def test_largest_scale(scale):
+    """A factor near the largest fp32: logits of tiny states are finite."""
+    T, vocab, d = 9, 150, 8
+    g = gen(5)
+    x = torch.randn((T, d), generator=g, device="cuda") * 2.0 ** -120
+    w = (torch.randn((vocab, d), generator=g, device="cuda") * 2.0 ** -8).to(BF)
+    y = torch.arange(T, device="cuda").to(torch.int32)
+    loss, lse = forward(desc(vocab, d, F, F, scale), x, w, y)
+    X, W = host(x), host(w)
+    scale = float(np.float32(scale))
+    want, want_lse = M.head_loss(X, W, y.cpu().numpy(), scale)
+    # x's bf16 parts below 2^-133 are lost: |x| is off by 2^-134 in each
+    err = abs(scale) * 2.0 ** -134 * np.abs(W).sum(axis=1).max() + z_error(X, W, scale).max()
+    assert (np.abs(host(lse) - want_lse) <= err + 16 * u + 2 * u * np.abs(want_lse)).all()
+    assert (np.abs(host(loss) - want) <= 2 * err + 16 * u + 2 * u * np.abs(want)).all()
 
 
 def test_large_logits():
