@@ -54,6 +54,15 @@ struct Parts {
   int64_t ld, matrix;
 };
 
+// Eight words to a row of both parts.
+__device__ __forceinline__ void put_eight(const Parts& out, int64_t mat, int row, int at, const uint32_t (&w)[8]) {
+  uint16_t* to = out.p + mat * out.matrix + row * out.ld + part_at(at);
+  *reinterpret_cast<u32x4*>(to) = u32x4{(w[0] & 0xffffu) | w[1] << 16, (w[2] & 0xffffu) | w[3] << 16,
+                                        (w[4] & 0xffffu) | w[5] << 16, (w[6] & 0xffffu) | w[7] << 16};
+  *reinterpret_cast<u32x4*>(to + kPartStep) = u32x4{w[0] >> 16 | (w[1] & 0xffff0000u), w[2] >> 16 | (w[3] & 0xffff0000u),
+                                                    w[4] >> 16 | (w[5] & 0xffff0000u), w[6] >> 16 | (w[7] & 0xffff0000u)};
+}
+
 // ---------------------------------------------------------------- norm and first X
 
 // Workgroups that a matrix's norm is spread over: 4,096 elements or more each.
@@ -103,39 +112,40 @@ __global__ __launch_bounds__(kThreads) void orth_first_kernel(const T* __restric
                                                               const double* __restrict__ pieces, int blocks,
                                                               Parts by_rows, Parts by_cols) {
   __shared__ uint32_t tile[64][65];
-  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, c = threadIdx.x % 64;
   const int64_t mat = blockIdx.z;
+  const T* m = g + mat * rows * static_cast<int64_t>(cols) + min(c0 + c, cols - 1);
+  float v[16];                                              // all under way before the first is waited for
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    v[i] = to_f32(m[min(r0 + i * 4 + static_cast<int>(threadIdx.x / 64), rows - 1) * static_cast<int64_t>(cols)]);
   double sum = 0.0;                                         // every wave adds the pieces for itself
 #pragma unroll 8
   for (int i = threadIdx.x & (kWave - 1); i < blocks; i += kWave) sum += pieces[mat * blocks + i];
 #pragma unroll
   for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
   const float norm = static_cast<float>(sqrt(sum)) + eps;
-  const T* m = g + mat * rows * static_cast<int64_t>(cols);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int r = i * 4 + threadIdx.x / 64, c = threadIdx.x % 64;
-    const bool in = r0 + r < rows && c0 + c < cols;
-    const float v = in ? to_f32(m[(r0 + r) * static_cast<int64_t>(cols) + c0 + c]) / norm : 0.f;
+    const int r = i * 4 + threadIdx.x / 64;
     uint32_t hi, lo;
-    f16_parts(v * kUp, hi, lo);
-    tile[r][c] = in ? hi | lo << 16 : 0u;
+    f16_parts(v[i] / norm * kUp, hi, lo);
+    tile[r][c] = r0 + r < rows && c0 + c < cols ? hi | lo << 16 : 0u;
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int a = i * 8 + threadIdx.x / 32, b = (threadIdx.x % 32) * 2;
+  for (int i = 0; i < 2; ++i) {
+    const int a = i * 32 + threadIdx.x / 8, b = (threadIdx.x % 8) * 8;
+    uint32_t w[8];
     if (r0 + a < rows) {
-      const uint32_t x = tile[a][b], y = tile[a][b + 1];
-      uint16_t* to = by_rows.p + mat * by_rows.matrix + (r0 + a) * by_rows.ld + part_at(c0 + b);
-      *reinterpret_cast<uint32_t*>(to) = (x & 0xffffu) | y << 16;
-      *reinterpret_cast<uint32_t*>(to + kPartStep) = x >> 16 | (y & 0xffff0000u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = tile[a][b + j];
+      put_eight(by_rows, mat, r0 + a, c0 + b, w);
     }
     if (c0 + a < cols) {
-      const uint32_t x = tile[b][a], y = tile[b + 1][a];
-      uint16_t* to = by_cols.p + mat * by_cols.matrix + (c0 + a) * by_cols.ld + part_at(r0 + b);
-      *reinterpret_cast<uint32_t*>(to) = (x & 0xffffu) | y << 16;
-      *reinterpret_cast<uint32_t*>(to + kPartStep) = x >> 16 | (y & 0xffff0000u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = tile[b + j][a];
+      put_eight(by_cols, mat, c0 + a, r0 + b, w);
     }
   }
 }
@@ -253,14 +263,6 @@ __device__ __forceinline__ int word_at(int n, int m) {
   return n * BM + ((((m >> 2) ^ n) & (BM / 4 - 1)) << 2) + (m & 3);
 }
 
-// Eight words to a row of both parts.
-__device__ __forceinline__ void put_eight(const Parts& out, int64_t mat, int row, int at, const uint32_t (&w)[8]) {
-  uint16_t* to = out.p + mat * out.matrix + row * out.ld + part_at(at);
-  *reinterpret_cast<u32x4*>(to) = u32x4{(w[0] & 0xffffu) | w[1] << 16, (w[2] & 0xffffu) | w[3] << 16,
-                                        (w[4] & 0xffffu) | w[5] << 16, (w[6] & 0xffffu) | w[7] << 16};
-  *reinterpret_cast<u32x4*>(to + kPartStep) = u32x4{w[0] >> 16 | (w[1] & 0xffff0000u), w[2] >> 16 | (w[3] & 0xffff0000u),
-                                                    w[4] >> 16 | (w[5] & 0xffff0000u), w[6] >> 16 | (w[7] & 0xffff0000u)};
-}
 
 // The block of the result at (m0, n0) from LDS to memory, by rows and (or of a symmetric result the mirrored tile) by
 // columns.
@@ -288,7 +290,7 @@ __device__ __forceinline__ void put_block(const OrthArgs& g, const Parts& rows, 
 }
 
 template <Mode MODE, typename OT, int BM, int BN, int WR, int WC, int BUFS, int GROUPS>
-__global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_per_eu(BM == 64 ? 3 : 2))) void orth_product_kernel(OrthArgs g) {
+__global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_per_eu(BM == 64 && GROUPS == 1 ? 3 : 2))) void orth_product_kernel(OrthArgs g) {
   typedef Tile<true, BM, BN, WR, WC, BUFS, kBoth, GROUPS> Tl;
   static_assert(BN == 64 ? 2 * BM * BN <= Tl::kElems : BN % 128 == 0 && BM * BN <= Tl::kElems,
                 "a tile of words fits the operands' LDS");
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_
   }
   const auto m_of = [&](int o) { return m_in + (GROUPS == 1 ? o : group * kOwn + o) % Tl::MT * 16; };
   const auto n_of = [&](int o) { return n_in + (GROUPS == 1 ? o : group * kOwn + o) / Tl::MT * 16; };
-  if (g.splits > 1) {
+  if (MODE == kGram && g.splits > 1) {
     float* to = g.partial + static_cast<int64_t>(id) * (BM * BN);
 #pragma unroll
     for (int o = 0; o < kOwn; ++o) *reinterpret_cast<f32x4*>(to + n_of(o) * BM + m_of(o)) = sum[o];
@@ -364,13 +366,13 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_
   put_block<MODE, BM, BN, Tl::kThreads * GROUPS>(g, second ? g.out2 : g.out, at.mat, at.m * BM, at.n * BN, at.m != at.n, word);
 }
 
-// The sums of the splits, in their order, and what a product does with them; a 64 x 64 block of a tile a workgroup.
-template <Mode MODE, typename OT, int BM>
+// The sums of the splits of X X^T, in their order; a 64 x 64 block of a tile a workgroup.
+template <int BM>
 __global__ __launch_bounds__(kThreads) void orth_join_kernel(OrthArgs g) {
   __shared__ __align__(16) uint32_t words[64 * 64];
   constexpr int kSub = BM / 64;
   const int item = blockIdx.x / (kSub * kSub), sub = blockIdx.x % (kSub * kSub);
-  const OrthTile at = orth_tile<MODE>(g, item);
+  const OrthTile at = orth_tile<kGram>(g, item);
   const int m_in = (sub % kSub) * 64, n_in = (sub / kSub) * 64;
   const int m0 = at.m * BM + m_in, n0 = at.n * BM + n_in;
   if (m0 >= g.rows_m || n0 >= g.rows_n) return;
@@ -384,12 +386,10 @@ __global__ __launch_bounds__(kThreads) void orth_join_kernel(OrthArgs g) {
     f32x4 v = *reinterpret_cast<const f32x4*>(q);
 #pragma unroll 4
     for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(q + s * next);
-    const u32x4 w = finish_four<MODE, OT>(g, at.mat, n0 + n, m0 + m, v);
-    if (!is_last(MODE)) *reinterpret_cast<u32x4*>(word(n, m)) = w;
+    *reinterpret_cast<u32x4*>(word(n, m)) = finish_four<kGram, float>(g, at.mat, n0 + n, m0 + m, v);
   }
-  if (is_last(MODE)) return;
   __syncthreads();
-  put_block<MODE, 64, 64, kThreads>(g, g.out, at.mat, m0, n0, at.m != at.n, word);
+  put_block<kGram, 64, 64, kThreads>(g, g.out, at.mat, m0, n0, at.m != at.n, word);
 }
 
 // ---------------------------------------------------------------- host
@@ -415,11 +415,11 @@ int64_t tile_count(int bm, int n, int rows_m, int rows_n, bool sym) {
   const int64_t tm = (rows_m + bm - 1) / bm, tn = (rows_n + bm - 1) / bm;
   return n * (sym ? tm * (tm + 1) / 2 : tm * tn);
 }
-Plan plan(int n, int rows_m, int rows_n, int slices, bool sym, int jobs = 1) {
+Plan plan(int n, int rows_m, int rows_n, int slices, bool sym, int jobs = 1, int most_splits = 1) {
   Plan best{64, 1, 1e300, false};
   for (int bm : {64, 128}) {
     const int64_t it = tile_count(bm, n, rows_m, rows_n, sym);
-    for (int s = 1; s <= (jobs == 2 ? 1 : kMostSplits) && s <= slices; ++s) {
+    for (int s = 1; s <= most_splits && s <= slices; ++s) {
       const double bytes = static_cast<double>(it) * s * bm * bm * sizeof(float);
       if (s > 1 && bytes > kPartialBytes) break;
       const int64_t wgs = it * s * jobs, cus = (wgs + kCus - 1) / kCus;          // workgroups of the fullest CU
@@ -438,8 +438,11 @@ Plan plan(int n, int rows_m, int rows_n, int slices, bool sym, int jobs = 1) {
   return best;
 }
 
-size_t partial_bytes(const Plan& p, int n, int rows_m, int rows_n, bool sym) {
-  return p.splits == 1 ? 0 : up256(tile_count(p.bm, n, rows_m, rows_n, sym) * p.splits * p.bm * p.bm * sizeof(float));
+// Of X X^T, whose k is the longer side; the other products' k is the shorter one, and a split of it never pays.
+Plan plan_gram(int n, int m, int slices) { return plan(n, m, m, slices, true, 1, kMostSplits); }
+size_t partial_bytes(int n, int m, int slices) {
+  const Plan p = plan_gram(n, m, slices);
+  return p.splits == 1 ? 0 : up256(tile_count(p.bm, n, m, m, true) * p.splits * p.bm * p.bm * sizeof(float));
 }
 
 // How the steps are taken: one at a time (rounds == steps), or in rounds of two or three on m x m matrices, where that
@@ -456,7 +459,7 @@ Steps plan_steps(const umem_orth_desc& od, int m, int k) {
   int most = 3;                                             // Q stays below 128: a^3 = 41 of the usual coefficients
   while (most > 1 && std::pow(std::fabs(od.a), most) > 100.f) --most;
   if (most == 1 || k < 2 * m) return {od.steps};
-  const double one = plan(n, m, m, xs, true).us + plan(n, k, m, as, false).us;
+  const double one = plan_gram(n, m, xs).us + plan(n, k, m, as, false).us;
   const double two = plan(n, m, m, as, true, 2).us + plan(n, m, m, as, true).us;
   return {two < one ? (od.steps + most - 1) / most : od.steps};
 }
@@ -482,11 +485,7 @@ struct Layout {
     t1 = x1 + x;
     q = t1 + t;
     partial = q + (steps.rounds < od.steps ? 5 : 2) * square;
-    const int on = od.n, xs = static_cast<int>(kp / 32), as = static_cast<int>(mp / 32);
-    total = partial + std::max(std::max(partial_bytes(plan(on, m, m, xs, true), on, m, m, true),
-                                        partial_bytes(plan(on, m, m, as, true), on, m, m, true)),
-                               std::max(partial_bytes(plan(on, k, m, as, false), on, k, m, false),
-                                        partial_bytes(plan(on, m, k, as, false), on, m, k, false)));
+    total = partial + partial_bytes(od.n, m, static_cast<int>(kp / 32));
   }
 };
 
@@ -497,7 +496,8 @@ Parts parts_at(char* base, size_t at, int rows, int64_t values) {
 template <Mode MODE, typename OT = float>
 void product(OrthArgs g, int n, hipStream_t s) {
   g.jobs = std::max(g.jobs, 1);
-  const Plan pl = plan(n, g.rows_m, g.rows_n, g.k / kTileBK, symmetric(MODE), g.jobs);
+  const Plan pl = MODE == kGram ? plan_gram(n, g.rows_m, g.k / kTileBK)
+                                : plan(n, g.rows_m, g.rows_n, g.k / kTileBK, symmetric(MODE), g.jobs);
   g.splits = pl.splits;
 #define UMEM_ORTH(BM, WR, WC, BUFS, GROUPS)                                                                               \
   {                                                                                                                  \
@@ -507,9 +507,8 @@ void product(OrthArgs g, int n, hipStream_t s) {
     g.items = n * g.per;                                                                                             \
     hipLaunchKernelGGL((orth_product_kernel<MODE, OT, BM, BM, WR, WC, BUFS, GROUPS>),                                        \
                        dim3(tile_grid(g.items * g.splits * g.jobs)), dim3(64 * WR * WC * GROUPS), 0, s, g);                   \
-    if (g.splits > 1)                                                                                                \
-      hipLaunchKernelGGL((orth_join_kernel<MODE, OT, BM>), dim3(g.items * (BM / 64) * (BM / 64)), dim3(kThreads), 0, \
-                         s, g);                                                                                      \
+    if (MODE == kGram && g.splits > 1)                                                                               \
+      hipLaunchKernelGGL(orth_join_kernel<BM>, dim3(g.items * (BM / 64) * (BM / 64)), dim3(kThreads), 0, s, g);      \
   }
   if (pl.bm == 128) UMEM_ORTH(128, 4, 2, 4, 1)
   else if (pl.alone) UMEM_ORTH(64, 2, 2, 3, 2)

@@ -144,6 +144,18 @@ def test_many_and_large(n, rows, cols):
         assert torch.equal(out[j], alone[0])
 
 
+# Sizes that between them reach every tile, group and split of each of the products.
+@pytest.mark.parametrize("n,rows,cols,steps,ot", [(1, 70, 70, 2, F), (1, 71, 2146, 2, F), (100, 163, 70, 3, F), (100, 69, 81, 2, F),
+                                                  (100, 71, 136, 2, F), (30, 326, 326, 1, BF), (1, 70, 71, 1, BF),
+                                                  (1, 71, 143, 2, BF), (2, 4426, 70, 1, BF), (2, 69, 4252, 2, F),
+                                                  (2, 69, 4252, 2, BF), (30, 547, 70, 2, BF), (100, 69, 2156, 1, F),
+                                                  (30, 321, 790, 2, F), (40, 132, 6457, 1, F), (30, 70, 547, 5, F),
+                                                  (100, 163, 70, 6, BF)])
+def test_tiles(n, rows, cols, steps, ot):
+    print(f"[case] orth {n} {rows} {cols} {steps} {ot}", flush=True)
+    check(n, rows, cols, ot=ot, steps=steps)
+
+
 def test_matrices_are_apart():
     """Zeros give zeros, a NaN or an infinity stays with its matrix, and each matrix is what it is alone."""
     x = torch.randn((4, 48, 80), generator=gen(2), device="cuda")
