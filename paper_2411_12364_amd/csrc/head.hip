@@ -206,12 +206,12 @@ constexpr float kLog2e = 1.44269504f;
 // What the products are multiplied by, so that |scale| log2(e) does not overflow; scale / it takes scale's place.
 __host__ __device__ __forceinline__ float spread_of(float scale) { return fabsf(scale) > 1e38f ? 4.f : 1.f; }
 
-template <int BM, int BN, int WR, int WC, int GROUPS>
+template <int BM, int BN, int WR, int WC, int GROUPS, TileParts PARTS>
 __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_stats_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
                                                                           const int32_t* __restrict__ targets,
                                                                           float2* __restrict__ stats,
                                                                           float* __restrict__ goal) {
-  typedef Tile<false, BM, BN, WR, WC, 2, kPlain, GROUPS> Tl;
+  typedef Tile<false, BM, BN, WR, WC, 2, PARTS, GROUPS> Tl;
   constexpr int MT = Tl::MT, NT = Tl::NE;
   __shared__ __align__(16) uint16_t buf0[GROUPS * Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[GROUPS * Tl::kElems];
@@ -394,7 +394,7 @@ struct SlopeRowB {
   }
 };
 
-template <int BM, int BN, int WR, int WC, int GROUPS, int PR, int PC>
+template <int BM, int BN, int WR, int WC, int GROUPS, TileParts PARTS, int PR, int PC>
 __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
                                                                  const int32_t* __restrict__ targets,
                                                                  const float* __restrict__ lse,
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TileP
                                                                  int piece, int t_ld, uint16_t* __restrict__ rows,
                                                                  uint16_t* __restrict__ cols,
                                                                  float* __restrict__ lost) {
-  typedef Tile<false, BM, BN, WR, WC, 2, kPlain, GROUPS> Tl;
+  typedef Tile<false, BM, BN, WR, WC, 2, PARTS, GROUPS> Tl;
   constexpr int MT = Tl::MT, NT = Tl::NE;
   static_assert(MT % 2 == 0 && (NT == 1 || NT == 2 || NT == 4), "pieces of 16 bytes along W's rows, of NT along the tokens");
   __shared__ __align__(16) uint16_t buf0[GROUPS * Tl::kElems];
@@ -530,13 +530,11 @@ __device__ __forceinline__ float product_factor(const ProductArgs& g) {
 
 // GROUPS sets of waves share a tile's slices where there are too few tiles for more than one on a CU: with one wave on each
 // of its parts a CU waits for every slice.
-template <bool F16, typename OT, int BM, int BN, int WR, int WC, int BUFS, int GROUPS>
+template <bool F16, typename OT, int BM, int BN, int WR, int WC, int GROUPS, TileParts PARTS>
 __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(TilePairs p, ProductArgs g) {
-  typedef Tile<F16, BM, BN, WR, WC, BUFS, kPlain, GROUPS> Tl;
+  typedef Tile<F16, BM, BN, WR, WC, 2, PARTS, GROUPS> Tl;
   __shared__ __align__(16) uint16_t buf0[GROUPS * Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[GROUPS * Tl::kElems];
-  __shared__ __align__(16) uint16_t buf2[BUFS > 2 ? GROUPS * Tl::kElems : 8];
-  __shared__ __align__(16) uint16_t buf3[BUFS > 3 ? GROUPS * Tl::kElems : 8];
   const int tiles = g.tiles_m * g.tiles_n, id = tile_item(tiles * g.splits);
   if (id >= tiles * g.splits) return;
   const int split = id / tiles;
@@ -547,7 +545,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
   const int64_t slices = Tl::slices(p);
   const int group = Tl::group(), own = group * Tl::kElems;
   tile.run(p, static_cast<int>(slices * split / g.splits), static_cast<int>(slices * (split + 1) / g.splits), buf0 + own,
-           buf1 + own, buf2 + (BUFS > 2 ? own : 0), buf3 + (BUFS > 3 ? own : 0), acc);
+           buf1 + own, nullptr, nullptr, acc);
   if constexpr (GROUPS > 1) {             // the first group adds what the others have, in their order, and goes on alone
     static_assert((GROUPS - 1) * BM * BN * 4 <= GROUPS * Tl::kElems * 2, "the groups' sums fit a buffer");
     f32x4* sums = reinterpret_cast<f32x4*>(buf0) + Tl::thread();
@@ -750,18 +748,21 @@ void split_x(const umem_head_desc& hd, int T, const void* x, uint16_t* parts, hi
 
 template <bool F16, typename OT>
 void product(const TilePairs& p, ProductArgs g, int side, hipStream_t s) {
-#define UMEM_PRODUCT(BM, WR, WC, BUFS, GROUPS)                                                                  \
-  hipLaunchKernelGGL((head_product_kernel<F16, OT, BM, BM, WR, WC, BUFS, GROUPS>), dim3(tile_grid(items)),      \
-                     dim3(64 * WR * WC * GROUPS), 0, s, p, g)
+#define UMEM_PRODUCT(BM, WC, GROUPS, PARTS)                                                                     \
+  hipLaunchKernelGGL((head_product_kernel<F16, OT, BM, BM, 2, WC, GROUPS, PARTS>), dim3(tile_grid(items)),      \
+                     dim3(128 * WC * GROUPS), 0, s, p, g)
   g.tiles_m = (p.a_rows + side - 1) / side;
   g.tiles_n = (p.b_rows + side - 1) / side;
   const int items = g.tiles_m * g.tiles_n * g.splits;
-  if (side == 256) UMEM_PRODUCT(256, 2, 4, 2, 1);
-  else if (side == 128 && items > kCus) UMEM_PRODUCT(128, 2, 2, 2, 1);
-  else if (side == 128) UMEM_PRODUCT(128, 2, 2, 2, 2);
-  else if (items > 2 * kCus) UMEM_PRODUCT(64, 2, 2, 2, 1);
-  else if (items > kCus) UMEM_PRODUCT(64, 2, 2, 2, 2);
-  else UMEM_PRODUCT(64, 2, 2, 2, 4);
+  constexpr TileParts kParts = !F16 && sizeof(OT) == 4 ? kThree : kPlain;       // (dx of fp32 alone has three of r)
+  if (side == 256) UMEM_PRODUCT(256, 4, 1, kPlain);
+  else if (side == 128 && items > kCus) UMEM_PRODUCT(128, 2, 1, kPlain);
+  else if (side == 128) UMEM_PRODUCT(128, 2, 2, kPlain);
+  else if (!F16 && p.n == 3 && items > kCus) UMEM_PRODUCT(64, 2, 1, kParts);
+  else if (!F16 && p.n == 3) UMEM_PRODUCT(64, 2, 2, kParts);
+  else if (items > 2 * kCus) UMEM_PRODUCT(64, 2, 1, kPlain);
+  else if (items > kCus) UMEM_PRODUCT(64, 2, 2, kPlain);
+  else UMEM_PRODUCT(64, 2, 4, kPlain);
 #undef UMEM_PRODUCT
 }
 
@@ -772,14 +773,17 @@ void slope(const TilePairs& p, float scale, const int32_t* targets, const float*
   // (of 256 x 256 tiles one at a time is on a CU, and nothing beside its end)
   const int side = tile_plan(piece, p.b_rows, slice_count(p.k, p.n), 1, false).side;
   const int tm = (piece + side - 1) / side, tn = (p.b_rows + side - 1) / side;
-#define UMEM_SLOPE(BM, WR, WC, GROUPS)                                                                          \
-  hipLaunchKernelGGL((head_slope_kernel<BM, BM, WR, WC, GROUPS, PR, PC>), dim3(tile_grid(tm * tn)),             \
-                     dim3(64 * WR * WC * GROUPS), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first,   \
-                     vocab, piece, t_ld, rows, cols, lost)
-  if (side == 128 && tm * tn > kCus) UMEM_SLOPE(128, 2, 2, 1);
-  else if (side == 128) UMEM_SLOPE(128, 2, 2, 2);
-  else if (tm * tn > 2 * kCus) UMEM_SLOPE(64, 2, 2, 1);
-  else UMEM_SLOPE(64, 2, 2, 2);
+  constexpr TileParts kParts = PR == 3 ? kThree : kPlain;
+#define UMEM_SLOPE(BM, GROUPS, PARTS)                                                                            \
+  hipLaunchKernelGGL((head_slope_kernel<BM, BM, 2, 2, GROUPS, PARTS, PR, PC>), dim3(tile_grid(tm * tn)),        \
+                     dim3(256 * GROUPS), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first, vocab,     \
+                     piece, t_ld, rows, cols, lost)
+  if (side == 128 && tm * tn > kCus) UMEM_SLOPE(128, 1, kPlain);
+  else if (side == 128) UMEM_SLOPE(128, 2, kPlain);
+  else if (PR == 3 && tm * tn > kCus) UMEM_SLOPE(64, 1, kParts);
+  else if (PR == 3) UMEM_SLOPE(64, 2, kParts);
+  else if (tm * tn > 2 * kCus) UMEM_SLOPE(64, 1, kPlain);
+  else UMEM_SLOPE(64, 2, kPlain);
 #undef UMEM_SLOPE
 }
 
@@ -803,14 +807,16 @@ hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, cons
     const int side = tile_plan(hd.vocab, t, slice_count(p.k, p.n), 1, true).side;
     const int tiles = (hd.vocab + side - 1) / side, tn = (t + side - 1) / side;
     const double scale = std::fabs(hd.scale / spread_of(hd.scale));
-#define UMEM_STATS(BM, WR, WC, GROUPS)                                                                           \
-  hipLaunchKernelGGL((head_stats_kernel<BM, BM, WR, WC, GROUPS>), dim3(tile_grid(tiles * tn)),                   \
-                     dim3(64 * WR * WC * GROUPS), 0, s, p, tiles, tn, hd.scale, targets + t0, stats, goal)
-    if (side == 256) UMEM_STATS(256, 2, 4, 1);
-    else if (side == 128 && tiles * tn > kCus) UMEM_STATS(128, 2, 2, 1);
-    else if (side == 128) UMEM_STATS(128, 2, 2, 2);
-    else if (tiles * tn > 2 * kCus) UMEM_STATS(64, 2, 2, 1);
-    else UMEM_STATS(64, 2, 2, 2);
+#define UMEM_STATS(BM, WC, GROUPS, PARTS)                                                                        \
+  hipLaunchKernelGGL((head_stats_kernel<BM, BM, 2, WC, GROUPS, PARTS>), dim3(tile_grid(tiles * tn)),             \
+                     dim3(128 * WC * GROUPS), 0, s, p, tiles, tn, hd.scale, targets + t0, stats, goal)
+    if (side == 256) UMEM_STATS(256, 4, 1, kPlain);
+    else if (side == 128 && tiles * tn > kCus) UMEM_STATS(128, 2, 1, kPlain);
+    else if (side == 128) UMEM_STATS(128, 2, 2, kPlain);
+    else if (p.n == 3 && tiles * tn > kCus) UMEM_STATS(64, 2, 1, kThree);
+    else if (p.n == 3) UMEM_STATS(64, 2, 2, kThree);
+    else if (tiles * tn > 2 * kCus) UMEM_STATS(64, 2, 1, kPlain);
+    else UMEM_STATS(64, 2, 2, kPlain);
 #undef UMEM_STATS
     if (t <= kFewTokens)
       hipLaunchKernelGGL(head_join_few_kernel, dim3(t), dim3(kThreads), 0, s, stats, goal, targets + t0, t, hd.vocab, tiles,

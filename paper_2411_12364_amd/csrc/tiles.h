@@ -45,8 +45,10 @@ struct TilePairs {
   int64_t a_ld, b_ld;
 };
 
-// How k lies in a row: 16-bit values one after another, or both parts of values.
-enum TileParts { kPlain, kBoth };
+// How k lies in a row: 16-bit values one after another, or both parts of values.  kThree: B is three matrices b[0] to b[2]
+// whose products with the one A are added (a value's parts, the smallest first), a slice of all of them at a time, so that
+// A passes once: 1,845 x 1,032 tokens over 1,032 34 us a pair after another, so 26.
+enum TileParts { kPlain, kBoth, kThree };
 // Where a row's value k has its first part (the second is 32 elements on), and the row's elements for k values.
 __host__ __device__ __forceinline__ constexpr int64_t part_at(int64_t k) { return (k >> 5) * 64 + (k & 31); }
 constexpr int kPartStep = 32;
@@ -70,7 +72,8 @@ struct Tile {
   static constexpr int kThreads = 64 * WR * WC;                              // of a group
   static constexpr int MT = BM / WR / 16, NT = BN / WC / 16;
   static constexpr int kA = BM * 8 / kThreads, kB = BN * 8 / kThreads;       // 16-byte pieces a thread loads
-  static constexpr int kElems = (BM + BN) * kTileBK;                         // one buffer
+  static constexpr int kBs = PARTS == kThree ? 3 : 1, kLoadsOf = kA + kBs * kB;
+  static constexpr int kElems = (BM + kBs * BN) * kTileBK;                   // one buffer
   static constexpr int kStep = kTileBK;                                      // a slice's elements of a row
   static constexpr int kAccs = PARTS == kBoth ? 2 : 1;                       // sets of accumulators
   static_assert(BM * 8 % kThreads == 0 && BN * 8 % kThreads == 0, "whole pieces");
@@ -117,7 +120,7 @@ struct Tile {
   }
 
   // The slice from k0 on into a buffer; a piece past k is another one here (past_k).
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t a, __amdgpu_buffer_rsrc_t b, int k0, int k,
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t a, const __amdgpu_buffer_rsrc_t (&b)[kBs], int k0, int k,
                                        uint16_t* lds) const {
     const int wave = __builtin_amdgcn_readfirstlane(thread() >> 6);
     const auto get = [&](uint32_t back) {
@@ -126,20 +129,23 @@ struct Tile {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(a, (lds_u32*)(lds + (i * kThreads + wave * 64) * 8), 16,
                                                  a_off[i] - back, k0 * 2, 0, 0);
 #pragma unroll
-      for (int i = 0; i < kB; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_u32*)(lds + BM * kTileBK + (i * kThreads + wave * 64) * 8), 16,
-                                                 b_off[i] - back, k0 * 2, 0, 0);
+      for (int s = 0; s < kBs; ++s)
+#pragma unroll
+        for (int i = 0; i < kB; ++i)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(
+              b[s], (lds_u32*)(lds + (BM + s * BN) * kTileBK + (i * kThreads + wave * 64) * 8), 16, b_off[i] - back,
+              k0 * 2, 0, 0);
     };
-    if (PARTS == kPlain && k0 + kTileBK > k) get(k0 + col_k >= k ? static_cast<uint32_t>(col_k) * 2u : 0u);
+    if (PARTS != kBoth && k0 + kTileBK > k) get(k0 + col_k >= k ? static_cast<uint32_t>(col_k) * 2u : 0u);
     else get(0u);
   }
 
   // The lane's pieces past k, once they have landed, to zeros.  (Rows of parts are whole slices.)
   __device__ __forceinline__ void past_k(int k0, int k, uint16_t* lds) const {
-    if (PARTS != kPlain || k0 + kTileBK <= k) return;
+    if (PARTS == kBoth || k0 + kTileBK <= k) return;
     if (k0 + col_k >= k) {
 #pragma unroll
-      for (int i = 0; i < kA + kB; ++i) {
+      for (int i = 0; i < kLoadsOf; ++i) {
         uint16_t* piece = lds + (i < kA ? 0 : BM * kTileBK) + ((i < kA ? i : i - kA) * kThreads + thread()) * 8;
         *reinterpret_cast<u32x4*>(piece) = u32x4{0u, 0u, 0u, 0u};
       }
@@ -153,16 +159,22 @@ struct Tile {
     u32x4 a[2][MT], b[2][NT];
   };
   __device__ __forceinline__ static void read(const uint16_t* lds, int half, Fragments& f) {
+    read_b(lds, half, 0, f);
+    read_a(lds, half, f);
+  }
+  __device__ __forceinline__ static void read_a(const uint16_t* lds, int half, Fragments& f) {
     const int lane = threadIdx.x & 63, wave = thread() >> 6;
-    const int wr = wave / WC, wc = wave % WC;
-    const int r = lane & 15, q = lane >> 4;
-    const uint16_t* a = lds + (wr * MT * 16 + r) * kTileBK;
-    const uint16_t* b = lds + BM * kTileBK + (wc * NT * 16 + r) * kTileBK;
-    const int at = ((half * 4 + q) ^ (r & 7)) * 8;
-#pragma unroll
-    for (int i = 0; i < NT; ++i) f.b[half][i] = *reinterpret_cast<const u32x4*>(b + i * 16 * kTileBK + at);
+    const int r = lane & 15, q = lane >> 4, at = ((half * 4 + q) ^ (r & 7)) * 8;
+    const uint16_t* a = lds + (wave / WC * MT * 16 + r) * kTileBK;
 #pragma unroll
     for (int i = 0; i < MT; ++i) f.a[half][i] = *reinterpret_cast<const u32x4*>(a + i * 16 * kTileBK + at);
+  }
+  __device__ __forceinline__ static void read_b(const uint16_t* lds, int half, int which, Fragments& f) {
+    const int lane = threadIdx.x & 63, wave = thread() >> 6;
+    const int r = lane & 15, q = lane >> 4, at = ((half * 4 + q) ^ (r & 7)) * 8;
+    const uint16_t* b = lds + (BM + which * BN + wave % WC * NT * 16 + r) * kTileBK;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) f.b[half][i] = *reinterpret_cast<const u32x4*>(b + i * 16 * kTileBK + at);
   }
   // (With its priority raised meanwhile, a wave's products are not held up by another's reads: 3 to 5 percent.)
   __device__ __forceinline__ static void multiply(const Fragments& f, int x, int y, f32x4 (&acc)[MT][NT]) {
@@ -176,12 +188,23 @@ struct Tile {
   // (Reading a slice's fragments while the slice before is multiplied measured the same.)
   __device__ __forceinline__ static void compute(const uint16_t* lds, f32x4 (&acc)[kAccs][MT][NT]) {
     Fragments f;
-    read(lds, 0, f);
+    if constexpr (PARTS != kThree) read(lds, 0, f);
     if constexpr (PARTS == kBoth) {
       read(lds, 1, f);
       multiply(f, 0, 0, acc[0]);
       multiply(f, 0, 1, acc[kAccs - 1]);
       multiply(f, 1, 0, acc[kAccs - 1]);
+    } else if constexpr (PARTS == kThree) {
+      // (a part's fragments are read while the ones before are multiplied)
+      read(lds, 0, f);
+      read_a(lds, 1, f);
+#pragma unroll
+      for (int s = 0; s < kBs; ++s) {
+        read_b(lds, 1, s, f);
+        multiply(f, 0, 0, acc[0]);
+        if (s + 1 < kBs) read_b(lds, 0, s + 1, f);
+        multiply(f, 1, 1, acc[0]);
+      }
     } else {
       multiply(f, 0, 0, acc[0]);
       read(lds, 1, f);
@@ -194,7 +217,7 @@ struct Tile {
   // for all loads.)
   template <int LATER>
   __device__ __forceinline__ void landed(int k0, int k, uint16_t* lds) const {
-    constexpr int kLoads = LATER * (kA + kB);
+    constexpr int kLoads = LATER * kLoadsOf;
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt((kLoads & 15) | (kLoads >> 4) << 14 | 0x0f70);          // vmcnt alone
     past_k(k0, k, lds);
@@ -203,7 +226,7 @@ struct Tile {
   }
 
   // The slices of p's pairs laid one after another.
-  __device__ __forceinline__ static int slices(const TilePairs& p) { return p.n * ((p.k + kStep - 1) / kStep); }
+  __device__ __forceinline__ static int slices(const TilePairs& p) { return (PARTS == kThree ? 1 : p.n) * ((p.k + kStep - 1) / kStep); }
 
   // The product over the slices [from, to) of them, to > from (of a group: its share), through BUFS buffers.  Past the last slice that one is
   // loaded again, and the loop has one end: with loads that may or may not be there, and with an exit in its midst, the
@@ -212,7 +235,7 @@ struct Tile {
   __device__ __forceinline__ void run(const TilePairs& p, int from, int to, uint16_t* buf0, uint16_t* buf1,
                                       uint16_t* buf2, uint16_t* buf3, f32x4 (&out)[MT][NT]) const {
     uint16_t* const bufs[4] = {buf0, buf1, buf2, buf3};
-    static_assert(BUFS >= 2 && BUFS <= 4 && (BUFS - 2) * (kA + kB) < 64, "what vmcnt counts");
+    static_assert(BUFS >= 2 && BUFS <= 4 && (BUFS - 2) * kLoadsOf < 64, "what vmcnt counts");
     f32x4 acc[kAccs][MT][NT];
 #pragma unroll
     for (int s = 0; s < kAccs; ++s)
@@ -233,12 +256,15 @@ struct Tile {
       pb = p.b[0];
 #pragma unroll
       for (int i = 1; i < kMaxPairs; ++i) {
-        pa = p.n > 1 && s == i ? p.a[i] : pa;
-        pb = p.n > 1 && s == i ? p.b[i] : pb;
+        pa = PARTS != kThree && p.n > 1 && s == i ? p.a[i] : pa;
+        pb = PARTS != kThree && p.n > 1 && s == i ? p.b[i] : pb;
       }
     };
     const auto fetch = [&](uint16_t* buf) {
-      load(rows_from(pa, m0, p.a_ld, p.a_rows), rows_from(pb, n0, p.b_ld, p.b_rows), k0, k, buf);
+      __amdgpu_buffer_rsrc_t b[kBs];
+#pragma unroll
+      for (int i = 0; i < kBs; ++i) b[i] = rows_from(PARTS == kThree ? p.b[i] : pb, n0, p.b_ld, p.b_rows);
+      load(rows_from(pa, m0, p.a_ld, p.a_rows), b, k0, k, buf);
       if (--ahead <= 0) return;
       k0 += kStep;
       if (k0 >= k) {
