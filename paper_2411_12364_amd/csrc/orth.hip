@@ -278,9 +278,11 @@ __device__ __forceinline__ void put_block(const OrthArgs& g, const Parts& rows, 
   }
   if (!is_update(MODE) && !mirrored) return;
   const Parts& out = is_update(MODE) ? g.out_t : rows;
-  // eight lanes to 64 consecutive n of a column, eight columns to a wave
+  // eight lanes (of 32 columns four) to 64 consecutive n of a column, eight columns together
+  constexpr int kPieces = BN < 64 ? BN / 8 : 8;
   for (int i = threadIdx.x; i < BM * (BN / 8); i += THREADS) {
-    const int group = i / 64, m = (group % (BM / 8)) * 8 + (i & 7), n = (group / (BM / 8)) * 64 + ((i >> 3) & 7) * 8;
+    const int group = i / (8 * kPieces), m = (group % (BM / 8)) * 8 + (i & 7);
+    const int n = (group / (BM / 8)) * 64 + ((i >> 3) % kPieces) * 8;
     if (m0 + m >= g.rows_m || 2 * (n0 + n) >= out.ld) continue;
     uint32_t w[8];
 #pragma unroll
@@ -290,11 +292,11 @@ __device__ __forceinline__ void put_block(const OrthArgs& g, const Parts& rows, 
 }
 
 template <Mode MODE, typename OT, int BM, int BN, int WR, int WC, int BUFS, int GROUPS>
-__global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_per_eu(BM == 64 && GROUPS == 1 ? 3 : 2))) void orth_product_kernel(OrthArgs g) {
+__global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_per_eu(BN == 64 && GROUPS == 1 ? 3 : 2))) void orth_product_kernel(OrthArgs g) {
   typedef Tile<true, BM, BN, WR, WC, BUFS, kBoth, GROUPS> Tl;
-  static_assert(BN == 64 ? 2 * BM * BN <= Tl::kElems : BN % 128 == 0 && BM * BN <= Tl::kElems,
+  constexpr int kLds = GROUPS * Tl::kElems, kHalves = BM / BN;
+  static_assert(BN <= 64 ? 2 * BM * BN <= kLds : BN % 128 == 0 && BM * BN <= Tl::kElems,
                 "a tile of words fits the operands' LDS");
-  constexpr int kLds = GROUPS * Tl::kElems;
   __shared__ __align__(16) uint16_t buf0[kLds];
   __shared__ __align__(16) uint16_t buf1[kLds];
   __shared__ __align__(16) uint16_t buf2[BUFS > 2 ? kLds : 8];
@@ -303,7 +305,8 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_
   if (id >= all) return;                                    // the whole workgroup: no barrier is skipped
   const int split = id / g.items, item = id - split * g.items;          // or of two products which one
   const bool second = MODE == kTimes && g.jobs == 2 && split == 1;
-  const OrthTile at = orth_tile<MODE>(g, item);
+  const OrthTile at = orth_tile<MODE>(g, item / kHalves);
+  const int m0 = at.m * BM, n0 = at.n * BM + item % kHalves * BN;
   TilePairs p;
   p.n = 1;
   p.a[0] = (second ? g.a2.p : g.a.p) + at.mat * g.a.matrix;
@@ -314,7 +317,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_
   p.a_ld = g.a.ld;
   p.b_ld = g.b.ld;
   Tl tile;
-  tile.init(p, at.m * BM, at.n * BN);
+  tile.init(p, m0, n0);
   f32x4 acc[Tl::MT][Tl::NT];
   const int64_t slices = Tl::slices(p);
   const int part = g.jobs == 2 ? 0 : split;
@@ -352,18 +355,18 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) __attribute__((amdgpu_waves_
     return;
   }
   const auto word = [&](int n, int m) {
-    uint16_t* half = BN == 64 || n < BN / 2 ? buf0 : buf1;
-    return reinterpret_cast<uint32_t*>(half) + word_at<BM>(BN == 64 ? n : n % (BN / 2), m);
+    uint16_t* half = BN <= 64 || n < BN / 2 ? buf0 : buf1;
+    return reinterpret_cast<uint32_t*>(half) + word_at<BM>(BN <= 64 ? n : n % (BN / 2), m);
   };
   if (!is_last(MODE) && GROUPS == 1) __syncthreads();       // the last slice has been read
 #pragma unroll
   for (int o = 0; o < kOwn; ++o) {
-    const u32x4 w = finish_four<MODE, OT>(g, at.mat, at.n * BN + n_of(o), at.m * BM + m_of(o), sum[o]);
+    const u32x4 w = finish_four<MODE, OT>(g, at.mat, n0 + n_of(o), m0 + m_of(o), sum[o]);
     if (!is_last(MODE)) *reinterpret_cast<u32x4*>(word(n_of(o), m_of(o))) = w;
   }
   if (is_last(MODE)) return;
   __syncthreads();
-  put_block<MODE, BM, BN, Tl::kThreads * GROUPS>(g, second ? g.out2 : g.out, at.mat, at.m * BM, at.n * BN, at.m != at.n, word);
+  put_block<MODE, BM, BN, Tl::kThreads * GROUPS>(g, second ? g.out2 : g.out, at.mat, m0, n0, at.m != at.n, word);
 }
 
 // The sums of the splits of X X^T, in their order; a 64 x 64 block of a tile a workgroup.
@@ -406,6 +409,7 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 struct Plan {
   int bm, splits;
   double us;
+  bool halves;            // a workgroup takes half a tile, with four groups of waves: 896 x 896 x 896 11.0 -> 10.2 us
   bool alone;             // every workgroup has a CU to itself: two groups of waves share its slices (four with two buffers
                           // each 1.15 times as long; two where two workgroups share a CU, or four buffers, the same)
 };
@@ -416,7 +420,7 @@ int64_t tile_count(int bm, int n, int rows_m, int rows_n, bool sym) {
   return n * (sym ? tm * (tm + 1) / 2 : tm * tn);
 }
 Plan plan(int n, int rows_m, int rows_n, int slices, bool sym, int jobs = 1, int most_splits = 1) {
-  Plan best{64, 1, 1e300, false};
+  Plan best{64, 1, 1e300, false, false};
   for (int bm : {64, 128}) {
     const int64_t it = tile_count(bm, n, rows_m, rows_n, sym);
     for (int s = 1; s <= most_splits && s <= slices; ++s) {
@@ -425,14 +429,15 @@ Plan plan(int n, int rows_m, int rows_n, int slices, bool sym, int jobs = 1, int
       const int64_t wgs = it * s * jobs, cus = (wgs + kCus - 1) / kCus;          // workgroups of the fullest CU
       const double each = (slices + s - 1) / s;
       double cost = s > 1 ? 4.5 + 0.7 * s + bytes / 2.5e6 : 0.0;
+      const bool halves = sym && bm == 64 && s == 1 && 2 * wgs <= kCus && each >= 8;
       if (bm == 128) {
         cost += static_cast<double>(cus) * (3.0 + 0.47 * each);
       } else {
         const int rest = static_cast<int>(cus % 3);
         cost += static_cast<double>(cus / 3) * (3.0 + 0.6 * each);
-        if (rest) cost += 3.0 + (cus == 1 ? 0.15 : rest == 1 ? 0.25 : 0.4) * each;
+        if (rest) cost += 3.0 + (halves ? 0.1 : cus == 1 ? 0.15 : rest == 1 ? 0.25 : 0.4) * each;
       }
-      if (cost < best.us) best = {bm, s, cost, bm == 64 && cus == 1 && each >= 4};
+      if (cost < best.us) best = {bm, s, cost, halves, bm == 64 && cus == 1 && each >= 4};
     }
   }
   return best;
@@ -499,20 +504,22 @@ void product(OrthArgs g, int n, hipStream_t s) {
   const Plan pl = MODE == kGram ? plan_gram(n, g.rows_m, g.k / kTileBK)
                                 : plan(n, g.rows_m, g.rows_n, g.k / kTileBK, symmetric(MODE), g.jobs);
   g.splits = pl.splits;
-#define UMEM_ORTH(BM, WR, WC, BUFS, GROUPS)                                                                               \
+  constexpr int kHalf = symmetric(MODE) ? 32 : 64;          // (the others have no halves, and no instance of their own)
+#define UMEM_ORTH(BM, BN, WR, WC, BUFS, GROUPS)                                                                      \
   {                                                                                                                  \
     g.tiles_m = (g.rows_m + BM - 1) / BM;                                                                            \
     g.tiles_n = (g.rows_n + BM - 1) / BM;                                                                            \
     g.per = symmetric(MODE) ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n;                               \
-    g.items = n * g.per;                                                                                             \
-    hipLaunchKernelGGL((orth_product_kernel<MODE, OT, BM, BM, WR, WC, BUFS, GROUPS>),                                        \
-                       dim3(tile_grid(g.items * g.splits * g.jobs)), dim3(64 * WR * WC * GROUPS), 0, s, g);                   \
+    g.items = n * g.per * (BM / BN);                                                                                 \
+    hipLaunchKernelGGL((orth_product_kernel<MODE, OT, BM, BN, WR, WC, BUFS, GROUPS>),                                \
+                       dim3(tile_grid(g.items * g.splits * g.jobs)), dim3(64 * WR * WC * GROUPS), 0, s, g);          \
     if (MODE == kGram && g.splits > 1)                                                                               \
       hipLaunchKernelGGL(orth_join_kernel<BM>, dim3(g.items * (BM / 64) * (BM / 64)), dim3(kThreads), 0, s, g);      \
   }
-  if (pl.bm == 128) UMEM_ORTH(128, 4, 2, 4, 1)
-  else if (pl.alone) UMEM_ORTH(64, 2, 2, 3, 2)
-  else UMEM_ORTH(64, 2, 2, 3, 1)
+  if (pl.bm == 128) UMEM_ORTH(128, 128, 4, 2, 4, 1)
+  else if (symmetric(MODE) && pl.halves) UMEM_ORTH(64, kHalf, 2, kHalf / 32, 3, 128 / kHalf)
+  else if (pl.alone) UMEM_ORTH(64, 64, 2, 2, 3, 2)
+  else UMEM_ORTH(64, 64, 2, 2, 3, 1)
 #undef UMEM_ORTH
 }
 

@@ -150,7 +150,8 @@ def test_many_and_large(n, rows, cols):
                                                   (1, 71, 143, 2, BF), (2, 4426, 70, 1, BF), (2, 69, 4252, 2, F),
                                                   (2, 69, 4252, 2, BF), (30, 547, 70, 2, BF), (100, 69, 2156, 1, F),
                                                   (30, 321, 790, 2, F), (40, 132, 6457, 1, F), (30, 70, 547, 5, F),
-                                                  (100, 163, 70, 6, BF)])
+                                                  (100, 163, 70, 6, BF), (50, 70, 90, 2, F), (60, 66, 300, 5, F),
+                                                  (2, 300, 2000, 5, F), (1, 700, 800, 2, BF), (4, 450, 230, 3, F)])
 def test_tiles(n, rows, cols, steps, ot):
     print(f"[case] orth {n} {rows} {cols} {steps} {ot}", flush=True)
     check(n, rows, cols, ot=ot, steps=steps)
