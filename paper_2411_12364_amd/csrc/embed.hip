@@ -4,8 +4,8 @@
 //
 // Both move memory and compute next to nothing.  The gradient sorts the (token, place) pairs, so that every row of the
 // table is summed by its places in order: no atomics, the same bits each time.  Up to 4,096 places are sorted by one
-// workgroup in LDS, up to 12,288 by a launch a pass, as a chain of short launches costs more than what they do (8,192
-// places: 15 us in two, 23 by sort.hip's six).  A wave takes a run of sorted places
+// workgroup in LDS, up to 32,768 by a launch a pass, as a chain of short launches costs more than what they do (8,192
+// places: 11 us in two, 23 by sort.hip's six).  A wave takes a run of sorted places
 // and 256 columns; a row that begins and ends within its run is written at once, what is left at
 // the run's two ends goes to scratch, and a second kernel adds the pieces of rows that pass from run to run.
 #include <algorithm>
@@ -279,54 +279,80 @@ __global__ __launch_bounds__(kSmallThreads) void embed_sort_kernel(const int32_t
 }
 
 // One pass over up to kPassPlaces places, a tile of 512 a workgroup: it counts all digits itself, those of the tiles before
-// its own apart, so that no other kernel stands between (8,192 places 7.7 us a pass, 20,000 17, where sort.hip's three
-// kernels a pass take 13), ranks its
-// tile's places, one a lane, and writes their words to their new places.  The first pass makes the words from ids, the
-// last writes pairs.
-constexpr int kPassThreads = 512, kPassWaves = kPassThreads / kWave, kPassPlaces = 3 << 12;
+// its own apart, so that no other kernel stands between (8,192 places 5.3 us a pass, 20,000 8.4, where sort.hip's three
+// kernels a pass take 13), ranks its tile's places, one a lane, and writes their words to their new places.  The first
+// pass makes the words from ids, the last writes pairs.
+constexpr int kPassThreads = 512, kPassWaves = kPassThreads / kWave, kPassPlaces = 32 << 10;
 
 __global__ __launch_bounds__(kPassThreads) void embed_pass_kernel(const int32_t* __restrict__ ids,
                                                                   const uint32_t* __restrict__ in, int T, int vocab,
                                                                   int place_bits, int shift, bool last,
                                                                   uint32_t* __restrict__ out, uint2* __restrict__ pairs,
                                                                   uint32_t* __restrict__ n_pairs) {
-  __shared__ uint32_t before[256], after[256], base[256];
+  // (16 copies of each count: tokens' high digits are few, and lanes that add to one word wait for each other)
+  constexpr int kCopies = 16;
+  __shared__ uint32_t before[256][kCopies], after[256][kCopies], base[256];
   __shared__ uint16_t count[kPassWaves][256];
   __shared__ uint32_t wave_sum[4], rowless;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int tile0 = blockIdx.x * kPassThreads;
-  if (tid < 256) before[tid] = after[tid] = 0;
+#pragma unroll
+  for (int i = 0; i < 256 * kCopies / kPassThreads; ++i)
+    (&before[0][0])[i * kPassThreads + tid] = (&after[0][0])[i * kPassThreads + tid] = 0;
   if (tid == 0) rowless = 0;
 #pragma unroll
   for (int i = 0; i < 256 / kWave; ++i) count[wave][i * kWave + lane] = 0;
   __syncthreads();
-  const auto word = [&](int t) {
-    if (in != nullptr) return in[t];
-    return min(static_cast<uint32_t>(ids[t]), static_cast<uint32_t>(vocab)) << place_bits | static_cast<uint32_t>(t);
+  typedef uint32_t four __attribute__((ext_vector_type(4), aligned(4)));
+  const uint32_t* from = in != nullptr ? in : reinterpret_cast<const uint32_t*>(ids);
+  const auto word = [&](uint32_t v, int t) {
+    return in != nullptr ? v : min(v, static_cast<uint32_t>(vocab)) << place_bits | static_cast<uint32_t>(t);
   };
   uint32_t none = 0;
-#pragma unroll 8
-  for (int t = tid; t < T; t += kPassThreads) {
-    const uint32_t w = word(t);
-    atomicAdd((t < tile0 ? before : after) + (w >> shift & 255u), 1u);
+  const auto add = [&](uint32_t v, int t) {
+    const uint32_t w = word(v, t);
+    atomicAdd((t < tile0 ? before : after)[w >> shift & 255u] + lane % kCopies, 1u);
     none += (w >> place_bits) >= static_cast<uint32_t>(vocab);
+  };
+  constexpr int kFours = 4;               // loads under way
+  for (int t0 = tid * 4; t0 < T; t0 += kFours * 4 * kPassThreads) {
+    four v[kFours];
+#pragma unroll
+    for (int i = 0; i < kFours; ++i)
+      v[i] = *reinterpret_cast<const four*>(from + max(min(t0 + i * 4 * kPassThreads, T - 4), 0));
+#pragma unroll
+    for (int i = 0; i < kFours; ++i) {
+      const int t = t0 + i * 4 * kPassThreads;
+      if (t + 4 <= T) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) add(v[i][j], t + j);
+      } else {
+        for (int e = t; e < T; ++e) add(from[e], e);
+      }
+    }
   }
   const int t = tile0 + tid;
-  const uint32_t w = t < T ? word(t) : 0xffffffffu, digit = w >> shift & 255u;
+  const uint32_t w = t < T ? word(from[t], t) : 0xffffffffu, digit = w >> shift & 255u;
   const uint64_t peers = same_digit(digit) & __ballot(t < T);
   const uint32_t rank = static_cast<uint32_t>(__popcll(peers & lanemask_lt()));
   if (t < T && rank == 0) count[wave][digit] = static_cast<uint16_t>(__popcll(peers));
   if (last && none) atomicAdd(&rowless, none);
   __syncthreads();
-  uint32_t all = 0, incl = 0;
+  uint32_t all = 0, incl = 0, ahead = 0;
   if (tid < 256) {
-    all = before[tid] + after[tid];
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int c = (i + tid) % kCopies;
+      ahead += before[tid][c];
+      all += after[tid][c];
+    }
+    all += ahead;
     incl = static_cast<uint32_t>(wave_inclusive_scan(static_cast<int>(all)));
     if (lane == kWave - 1) wave_sum[wave] = incl;
   }
   __syncthreads();
   if (tid < 256) {
-    uint32_t at = incl - all + before[tid];
+    uint32_t at = incl - all + ahead;
 #pragma unroll
     for (int v = 0; v < 4; ++v) at += v < wave ? wave_sum[v] : 0u;
     base[tid] = at;
