@@ -591,8 +591,10 @@ UMEM_API umem_status umem_head_backward_workspace_size(const umem_head_desc* hd,
  *   dx          [T, d] of xtype;  dw [vocab, d] of gtype; both 16-byte aligned
  *   accumulate  0: dw is written; 1: added to (fp32 only, UMEM_ERR_INVALID_ARG otherwise)
  *   ws          256-byte aligned scratch of umem_head_backward_workspace_size bytes
- * r enters the products as bf16 where the result is bf16 (which is then rounded once more), and whole, as a sum of
- * bf16 parts, where it is fp32.  The sums over tokens run in a fixed order.  dx, dw and ws overlap neither an
+ * For dx r is bf16 where x is (a target's entry counts whole all the same), and whole where x is fp32.  For dw, in
+ * units of the largest |dloss| and of the largest |x| of the tokens that count, r has 11 bits where dw is bf16 and 22
+ * where it is fp32, and x as many as it has, 22 of fp32; what lies below 2^-40 of these units is lost.  Results are
+ * rounded once more to their type.  The sums run in a fixed order.  dx, dw and ws overlap neither an
  * input nor each other (UMEM_ERR_INVALID_ARG).  T == 0 writes nothing. */
 UMEM_API umem_status umem_head_backward(const umem_head_desc* hd, int32_t T, const void* x, const uint16_t* w,
                                const int32_t* targets, const float* lse, const float* dloss, void* dx, void* dw,
@@ -617,7 +619,9 @@ typedef struct umem_orth_desc {
  * Limits (UMEM_ERR_UNSUPPORTED beyond them): rows and cols <= 2^16; n < 2^16; n * rows * cols <= 2^33; steps <= 16.
  * Between the steps a matrix has 22 bits of each value of 2^-14 or more and an absolute error of 2^-37 below; its
  * values stay below 16 where the coefficients keep singular values of [0, 1] there (an entry of X, A or b A + c A^2
- * that reaches 16 becomes infinite).  Sums are fp32, the norm fp64. */
+ * that reaches 16 becomes infinite).  Sums are fp32, the norm fp64.  Where G is at least twice as long as wide, two or
+ * three steps may be taken at a time on products of A (as long as |a| to that power is at most 100), and where the
+ * smaller side is at most 64 all of them, in fp64. */
 UMEM_API umem_status umem_orthogonalize_workspace_size(const umem_orth_desc* od, size_t* bytes);
 
 /*   g    [n, rows, cols] of gtype;  out [n, rows, cols] of otype (may equal g); both aligned to their elements

@@ -11,7 +11,9 @@
 //   P = a I + b A + c A^2,  Q <- Q P,  A <- P A P,   then X <- Q X:
 //
 // 3 products of m x m x m for each step but the first in the place of A = X X^T and B X.  Bounded by the matrix cores for
-// large matrices, by the chain of launches for small ones.
+// large matrices, by the chain of launches for small ones.  Measured, five steps: 896 x 2,048 in 18 launches 196 us, of which
+// the 13 products of 896 x 896 x 896 take 8 to 10 each; 1,024 x 16,384 580 us, X X^T 52 + 9 (36 of 64 tiles, three pairs of
+// parts: 1.1 PFLOP/s), X's update 123, 0.84 PFLOP/s.
 //
 // Rounding: every matrix between the steps is two fp16 parts of its values times a power of two (2^12; 2^9 for P and Q),
 // which hold 22 bits of it, and a product takes three of the four pairs of parts (the fourth is below 2^-22 of the

@@ -337,8 +337,9 @@ struct Tile {
 struct TilePlace {
   int m, n;
 };
+template <int BAND = 4>
 __device__ __forceinline__ TilePlace tile_place(int item, int tiles_m, int tiles_n) {
-  constexpr int kBand = 4;
+  constexpr int kBand = BAND;
   const int band = item / (kBand * tiles_n), first = band * kBand;
   const int high = min(kBand, tiles_m - first);
   const int in = item - first * tiles_n;
