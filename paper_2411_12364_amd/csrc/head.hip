@@ -12,6 +12,9 @@
 // for few tokens, where W is read once at the rate of the memory.  Measured: 16 tokens by 50,000 rows of 2,048 40 + 5 us (W
 // at 5.2 TB/s); 8,192 tokens by 50,000 of 2,048, forward and backward with dW in fp32, 7.8 ms for 8.4 TFLOP: the logits 1.36 ms
 // (1.23 PFLOP/s), then for each 7,168 rows r 258 us, W's transpose 12, dx 206 (1.17 PFLOP/s), dW 408 (two products, 1.18).
+// Tokens that do not count are left out of the backward: a list of those that do is made first, and every product's grid and
+// length follow its count on the device (2,000 tokens, a third of them without a target, by 32,003 of 1,024 642 us with
+// them, so 528).
 //
 // Rounding: logits and sums are fp32 of bf16 operands; fp32 x is three bf16 parts, which hold it whole.  r is made for
 // losses' gradients of at most 1, and the largest of them and s are multiplied in last, in fp32: the gradient of a
@@ -52,12 +55,25 @@ __device__ __forceinline__ void bf16_parts(float x, uint32_t (&p)[N]) {
 
 // ---------------------------------------------------------------- layouts
 
-// fp32 x to its parts, [3][T][d].
+// A token that counts, for the backward: those that do not are left out of all its products.
+struct __align__(16) Token {
+  float lse, dloss;
+  int32_t target, row;
+};
+
+// fp32 x [T][d], n = T d, to its parts [3][T][d]; with a list its tokens' rows alone, one after another.
 __global__ __launch_bounds__(kThreads) void head_split_kernel(const float* __restrict__ x, uint16_t* __restrict__ parts,
-                                                              size_t n) {
+                                                              size_t n, int d, const Token* __restrict__ list,
+                                                              const int* __restrict__ count) {
   const size_t i = (static_cast<size_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
   if (i >= n) return;
-  const f32x4 v = *reinterpret_cast<const f32x4*>(x + i);
+  size_t from = i;
+  if (list != nullptr) {
+    const uint32_t four = static_cast<uint32_t>(i / 4), t = four / (d / 4);
+    if (t >= static_cast<uint32_t>(*count)) return;
+    from = static_cast<size_t>(list[t].row) * d + (four - t * (d / 4)) * 4;
+  }
+  const f32x4 v = *reinterpret_cast<const f32x4*>(x + from);
   uint32_t p[4][3];
 #pragma unroll
   for (int j = 0; j < 4; ++j) bf16_parts(v[j], p[j]);
@@ -89,29 +105,62 @@ __device__ __forceinline__ bool counts(const int32_t* targets, int t, int vocab)
   return static_cast<uint32_t>(targets[t]) < static_cast<uint32_t>(vocab);
 }
 
-// The largest finite |x| of the tokens that count, and (most: with a dloss) the largest |dloss| of theirs.
+// The list of the tokens that count, in their order, and their number; the largest finite |x| of theirs and (with a dloss)
+// the largest |dloss|; zeros to the others' rows of dx.
 template <typename T>
-__global__ __launch_bounds__(1024) void head_most_kernel(const T* __restrict__ x, const float* __restrict__ dloss,
+__global__ __launch_bounds__(1024) void head_list_kernel(const T* __restrict__ x, const float* __restrict__ lse,
+                                                         const float* __restrict__ dloss,
                                                          const int32_t* __restrict__ targets, int tokens, int d, int vocab,
-                                                         float* __restrict__ most, float* __restrict__ most_x) {
+                                                         Token* __restrict__ list, int* __restrict__ count,
+                                                         float* __restrict__ most, float* __restrict__ most_x,
+                                                         T* __restrict__ dx) {
+  constexpr int kWaves = 1024 / kWave;
+  __shared__ int earlier[kWaves], here[kWaves];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  for (int64_t first = blockIdx.x * 1024; first < tokens; first += kMostBlocks * 1024) {
+    int before = 0;                       // of the tokens ahead of these 1,024, counted by every workgroup for itself
+#pragma unroll 8
+    for (int t = tid; t < first; t += 1024) before += counts(targets, t, vocab) ? 1 : 0;
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) before += __shfl_xor(before, off, kWave);
+    const int t = static_cast<int>(first) + tid;
+    const bool on = t < tokens && counts(targets, t, vocab);
+    const uint64_t ballot = __ballot(on);
+    if (lane == 0) {
+      earlier[wave] = before;
+      here[wave] = __popcll(ballot);
+    }
+    __syncthreads();
+    int at = __popcll(ballot & lanemask_lt()), all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      at += earlier[w] + (w < wave ? here[w] : 0);
+      all += earlier[w] + here[w];
+    }
+    if (on) list[at] = Token{lse[t], dloss ? dloss[t] : 1.f, targets[t], t};
+    if (tid == 0 && first + 1024 >= tokens) *count = all;
+    __syncthreads();
+  }
   typedef T eight __attribute__((ext_vector_type(8)));
-  const int64_t pieces = static_cast<int64_t>(tokens) * (d / 8);
+  const uint32_t row = d / 8, pieces = static_cast<uint32_t>(tokens) * row;       // at most 2^31
   float m = 0.f;
 #pragma unroll 4
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 1024 + threadIdx.x; i < pieces; i += kMostBlocks * 1024) {
-    const eight v = *reinterpret_cast<const eight*>(x + i * 8);
-    float most8 = 0.f;
+  for (uint32_t i = blockIdx.x * 1024 + tid; i < pieces; i += kMostBlocks * 1024) {
+    const eight v = *reinterpret_cast<const eight*>(x + static_cast<int64_t>(i) * 8);
+    if (counts(targets, static_cast<int>(i / row), vocab)) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float a = fabsf(static_cast<float>(v[j]));
-      most8 = a < INFINITY ? fmaxf(most8, a) : most8;
+      for (int j = 0; j < 8; ++j) {
+        const float a = fabsf(static_cast<float>(v[j]));
+        m = a < INFINITY ? fmaxf(m, a) : m;
+      }
+    } else {
+      *reinterpret_cast<eight*>(dx + static_cast<int64_t>(i) * 8) = eight{};
     }
-    if (most8 > m && counts(targets, static_cast<int>(i / (d / 8)), vocab)) m = most8;
   }
   put_most(m, most_x);
   if (!dloss) return;
   m = 0.f;
-  for (int t = blockIdx.x * 1024 + threadIdx.x; t < tokens; t += kMostBlocks * 1024)
+  for (int t = blockIdx.x * 1024 + tid; t < tokens; t += kMostBlocks * 1024)
     if (counts(targets, t, vocab)) m = fmaxf(m, fabsf(dloss[t]));
   __syncthreads();
   put_most(m, most);
@@ -139,34 +188,40 @@ __device__ __forceinline__ uint32_t f16_part(float x, int i) {
   return fabsf(v) < INFINITY ? __builtin_bit_cast(uint16_t, static_cast<_Float16>(x - v)) : 0u;
 }
 
-// in [rows, cols] (cols a multiple of 8) to out [parts][cols][ld] (ld a multiple of 64), zeros from `rows` on.  With `most`
-// as fp16 parts of the shifted values, and zeros in the place of rows whose target is none (0 times what is no number would
-// reach the others' sums); without as the bits they are.  Every load is under way before the first is waited for: of
-// 1,032 x 1,032 fp32 to two parts 13.8 us with a load at a time, so 5.3.
+// in [rows, cols] (cols a multiple of 8) to out [parts][cols][ld] (ld a multiple of 64), zeros from `rows` on, to a multiple of 64.  With
+// a list its tokens' rows alone, one after another, and bf16 ones to `copy` as they are.  With `most` as fp16 parts of the
+// shifted values; without as the bits they are.  Every load is under way before the first is waited for: of 1,032 x 1,032
+// fp32 to two parts 13.8 us with a load at a time, so 5.3.
 template <typename T, int PARTS>
 __global__ __launch_bounds__(kThreads) void head_transpose_kernel(const T* __restrict__ in, int rows, int cols,
                                                                   uint16_t* __restrict__ out, int64_t ld,
                                                                   const float* __restrict__ most,
-                                                                  const int32_t* __restrict__ targets, int vocab) {
+                                                                  const Token* __restrict__ list,
+                                                                  const int* __restrict__ count,
+                                                                  T* __restrict__ copy) {
   constexpr int kN = 16 / sizeof(T), kAcross = 64 / kN, kPieces = 64 * kAcross / kThreads;
   typedef T piece __attribute__((ext_vector_type(kN)));
   __shared__ uint16_t tile[PARTS][64][66];
   const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
   const int in_c = (threadIdx.x % kAcross) * kN, in_r = threadIdx.x / kAcross;
   const int c = min(c0 + in_c, cols - kN);
+  if (list != nullptr) {
+    rows = *count;
+    if (r0 >= rows) return;
+  }
   piece v[kPieces];
-  int y[kPieces];
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) {
     const int r = min(r0 + in_r + i * (kThreads / kAcross), rows - 1);
-    v[i] = *reinterpret_cast<const piece*>(in + static_cast<int64_t>(r) * cols + c);
-    y[i] = targets ? targets[r] : 0;
+    v[i] = *reinterpret_cast<const piece*>(in + static_cast<int64_t>(list ? list[r].row : r) * cols + c);
   }
   const int shift = most ? x_shift(most) : 0;
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) {
     const int at = in_r + i * (kThreads / kAcross);
-    const bool on = r0 + at < rows && (targets == nullptr || static_cast<uint32_t>(y[i]) < static_cast<uint32_t>(vocab));
+    const bool on = r0 + at < rows;
+    if (copy != nullptr && on && c0 + in_c < cols)
+      *reinterpret_cast<piece*>(copy + static_cast<int64_t>(r0 + at) * cols + c) = v[i];
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
       uint32_t p[PARTS] = {};
@@ -372,7 +427,7 @@ __device__ __forceinline__ float most_of(const float* most) {
 }
 
 // r of a piece of the vocabulary, over s and the largest dloss: rows[part][T][piece] in PR bf16 parts, and times 2^15
-// cols[part][piece][t_ld] in PC fp16 parts; zeros past the piece's rows of W, past T and for tokens without a target.
+// cols[part][piece][t_ld] in PC fp16 parts; zeros past the piece's rows of W and past the tokens.
 // lost: what of a target's r one bf16 part of it does not hold, [T] (of it alone r is near the largest dloss in most
 // tokens; dx adds it times W's row: half the error of dx is without that from there).
 // The tile's rows are in an order in which a lane holds 8 values of W's rows one after another, and NT tokens one after another, so
@@ -397,11 +452,10 @@ struct SlopeRowB {
 };
 
 template <int BM, int BN, int WR, int WC, int GROUPS, TileParts PARTS, int PR, int PC>
-__global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TilePairs p, int tiles_m, int tiles_n, float scale,
-                                                                 const int32_t* __restrict__ targets,
-                                                                 const float* __restrict__ lse,
-                                                                 const float* __restrict__ dloss,
-                                                                 const float* __restrict__ most, int v_first, int vocab,
+__global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TilePairs p, int tiles_m, int of, float scale,
+                                                                 const Token* __restrict__ list,
+                                                                 const int* __restrict__ count,
+                                                                 const float* __restrict__ most, int v_first,
                                                                  int piece, int t_ld, uint16_t* __restrict__ rows,
                                                                  uint16_t* __restrict__ cols,
                                                                  float* __restrict__ lost) {
@@ -410,6 +464,8 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TileP
   static_assert(MT % 2 == 0 && (NT == 1 || NT == 2 || NT == 4), "pieces of 16 bytes along W's rows, of NT along the tokens");
   __shared__ __align__(16) uint16_t buf0[GROUPS * Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[GROUPS * Tl::kElems];
+  const int T = *count, tiles_n = (T + BN - 1) / BN;
+  p.b_rows = T;
   const int item = tile_item(tiles_m * tiles_n);
   if (item >= tiles_m * tiles_n) return;
   const TilePlace at = tile_place<8>(item, tiles_m, tiles_n);        // (bands of 8: 258 us, of 4 272)
@@ -420,15 +476,17 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TileP
   tile.run(p, 0, Tl::slices(p), buf0 + own, buf1 + own, nullptr, nullptr, all);
   Tl::share(all, buf0, acc);
   const int lane = threadIdx.x & 63, wave = Tl::thread() >> 6, wr = wave / WC, wc = wave % WC;
-  const int V = p.a_rows, T = p.b_rows;
+  const int V = p.a_rows;
   const int v0 = at.m * BM + wr * MT * 16 + 8 * (lane >> 4);       // acc[i][j][r]: row v0 + 32 (i / 2) + 4 (i % 2) + r
   const int t0 = at.n * BN + wc * Tl::NT * 16 + Tl::NT * (lane & 15) + group * NT;     // token t0 + j
   const float largest = most_of(most);
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
-    const int t = t0 + j, tc = min(t, T - 1), y = targets[tc];
-    const bool on = t < T && static_cast<uint32_t>(y) < static_cast<uint32_t>(vocab);
-    const float l = lse[tc], g = dloss ? dloss[tc] / largest : 1.f;
+    const int t = t0 + j;
+    const bool on = t < T;
+    const Token token = list[min(t, T - 1)];
+    const int y = token.target;
+    const float l = token.lse, g = token.dloss / largest;
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -466,7 +524,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TileP
         }
   }
   // (piece is a multiple of BM)
-  const int64_t by_row = static_cast<int64_t>(T) * piece, by_col = static_cast<int64_t>(piece) * t_ld;
+  const int64_t by_row = static_cast<int64_t>(of) * piece, by_col = static_cast<int64_t>(piece) * t_ld;
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     if (t0 + j >= T) continue;
@@ -502,7 +560,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_slope_kernel(TileP
 
 // A product whose m lies along the rows of the output, [n][m] of ld.  Of one split of k: out = (D + before) f (dx) or
 // D f + before (dW: whole = false), each without `before` where it is not given, f = scale times the largest dloss, and of
-// shifted operands (x_most) what takes their shifts back; rows n whose entry of targets is none become zeros.  Of
+// shifted operands (x_most) what takes their shifts back.  Of
 // several, split i's D is added to sums[i], or written there where first is set.
 struct ProductArgs {
   int tiles_m, tiles_n, splits;
@@ -512,15 +570,17 @@ struct ProductArgs {
   int64_t ld;
   float scale;
   const float *most, *x_most;
-  const int32_t* targets;
-  int vocab;
-  const float* lost;      // with targets: [T], times W's row of the target is added to D
+  const int* count;       // tokens that count: rows n, or (along_k) k of the product
+  bool along_k;
+  const Token* list;      // given where row n goes to its token's place in out
+  const float* lost;      // [n], times W's row of the target is added to D
   const uint16_t* w;
+  int64_t sum_size;       // from one split's sums to the next's
 };
 
 // What is added to row t of dx, columns m .. m + 3, before it is scaled.
 __device__ __forceinline__ f32x4 lost_row(const ProductArgs& g, int t, int m) {
-  const u32x2 b = *reinterpret_cast<const u32x2*>(g.w + g.targets[t] * g.ld + m);
+  const u32x2 b = *reinterpret_cast<const u32x2*>(g.w + g.list[t].target * g.ld + m);
   return g.lost[t] * f32x4{bits_f32(b.x & 0xffffu), bits_f32(b.x >> 16), bits_f32(b.y & 0xffffu), bits_f32(b.y >> 16)};
 }
 
@@ -537,6 +597,13 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
   typedef Tile<F16, BM, BN, WR, WC, 2, PARTS, GROUPS> Tl;
   __shared__ __align__(16) uint16_t buf0[GROUPS * Tl::kElems];
   __shared__ __align__(16) uint16_t buf1[GROUPS * Tl::kElems];
+  const int counted = *g.count;
+  if (g.along_k) {
+    p.k = (counted + 63) / 64 * 64;
+  } else {
+    p.b_rows = counted;
+    g.tiles_n = (counted + BN - 1) / BN;
+  }
   const int tiles = g.tiles_m * g.tiles_n, id = tile_item(tiles * g.splits);
   if (id >= tiles * g.splits) return;
   const int split = id / tiles;
@@ -546,8 +613,15 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
   f32x4 acc[Tl::MT][Tl::NT];
   const int64_t slices = Tl::slices(p);
   const int group = Tl::group(), own = group * Tl::kElems;
-  tile.run(p, static_cast<int>(slices * split / g.splits), static_cast<int>(slices * (split + 1) / g.splits), buf0 + own,
-           buf1 + own, nullptr, nullptr, acc);
+  const int from = static_cast<int>(slices * split / g.splits), to = static_cast<int>(slices * (split + 1) / g.splits);
+  if (to > from) {
+    tile.run(p, from, to, buf0 + own, buf1 + own, nullptr, nullptr, acc);
+  } else {                                // (no token counts)
+#pragma unroll
+    for (int i = 0; i < Tl::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < Tl::NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   if constexpr (GROUPS > 1) {             // the first group adds what the others have, in their order, and goes on alone
     static_assert((GROUPS - 1) * BM * BN * 4 <= GROUPS * Tl::kElems * 2, "the groups' sums fit a buffer");
     f32x4* sums = reinterpret_cast<f32x4*>(buf0) + Tl::thread();
@@ -573,7 +647,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
   for (int j = 0; j < Tl::NT; ++j) {
     const int n = at.n * BN + (wc * Tl::NT + j) * 16 + (lane & 15);
     if (n >= p.b_rows) continue;
-    const bool off = g.targets && !counts(g.targets, n, g.vocab);
+    const int64_t out_row = g.list ? g.list[n].row : n;
 #pragma unroll
     for (int i = 0; i < Tl::MT; ++i) {
       const int m = at.m * BM + (wr * Tl::MT + i) * 16 + 4 * (lane >> 4);
@@ -581,18 +655,17 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
       const int64_t o = n * g.ld + m;
       f32x4 v = acc[i][j];
       if (g.splits > 1) {
-        float* sum = g.sums + split * (p.b_rows * g.ld) + o;
+        float* sum = g.sums + split * g.sum_size + o;
         if (!g.first) v += *reinterpret_cast<const f32x4*>(sum);
         *reinterpret_cast<f32x4*>(sum) = v;
         continue;
       }
       if (g.whole && g.before) v += *reinterpret_cast<const f32x4*>(g.before + o);
-      if (g.lost && !off) v += lost_row(g, n, m);
+      if (g.lost) v += lost_row(g, n, m);
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], back) * f;
       if (!g.whole && g.before) v += *reinterpret_cast<const f32x4*>(g.before + o);
-      if (off) v = f32x4{0.f, 0.f, 0.f, 0.f};
-      OT* out = static_cast<OT*>(g.out) + o;
+      OT* out = static_cast<OT*>(g.out) + out_row * g.ld + m;
       if constexpr (sizeof(OT) == 4)
         *reinterpret_cast<f32x4*>(out) = v;
       else
@@ -604,18 +677,16 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
 
 // dx from the splits' sums, in their order.
 template <typename OT>
-__global__ __launch_bounds__(kThreads) void head_sum_kernel(ProductArgs g, int T, int d) {
+__global__ __launch_bounds__(kThreads) void head_sum_kernel(ProductArgs g) {
   const float f = product_factor(g);
-  const int64_t size = static_cast<int64_t>(T) * d;
   const int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
-  if (i >= size) return;
+  if (i >= *g.count * g.ld) return;
   f32x4 v = *reinterpret_cast<const f32x4*>(g.sums + i);
-  for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(g.sums + s * size + i);
-  const int t = static_cast<int>(i / d);
-  const bool on = counts(g.targets, t, g.vocab);
-  if (g.lost && on) v += lost_row(g, t, static_cast<int>(i % d));
-  v = on ? v * f : f32x4{0.f, 0.f, 0.f, 0.f};
-  OT* out = static_cast<OT*>(g.out) + i;
+  for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(g.sums + s * g.sum_size + i);
+  const int t = static_cast<int>(i / g.ld), m = static_cast<int>(i - t * g.ld);
+  if (g.lost) v += lost_row(g, t, m);
+  v *= f;
+  OT* out = static_cast<OT*>(g.out) + g.list[t].row * g.ld + m;
   if constexpr (sizeof(OT) == 4)
     *reinterpret_cast<f32x4*>(out) = v;
   else
@@ -711,11 +782,11 @@ struct ForwardLayout {
   }
 };
 struct BackwardLayout {
-  size_t parts, xt, wt, rows, cols, sum, most, x_most, lost, total;
+  size_t parts, xt, wt, rows, cols, sum, most, x_most, lost, list, count, total;
   BackwardLayout(const umem_head_desc& hd, int T) {
     const size_t t = T, tp = token_row(T), d = hd.d, values = piece_values(hd, T);
     parts = 0;
-    xt = up256(hd.xtype == UMEM_F32 ? 3 * t * d * 2 : 0);
+    xt = up256((hd.xtype == UMEM_F32 ? 3 : 1) * t * d * 2);
     wt = xt + up256(x_col_parts(hd) * d * tp * 2);
     rows = wt + up256(d * most_piece(hd) * 2);
     cols = rows + up256(row_parts(hd) * values * 2);
@@ -723,7 +794,9 @@ struct BackwardLayout {
     most = sum + up256(sum_values(hd, T) * sizeof(float));
     x_most = most + up256(kMostBlocks * sizeof(float));
     lost = x_most + up256(kMostBlocks * sizeof(float));
-    total = lost + up256(t * sizeof(float));
+    list = lost + up256(t * sizeof(float));
+    count = list + up256(t * sizeof(Token));
+    total = count + 256;
   }
 };
 
@@ -742,10 +815,11 @@ TilePairs logit_pairs(const umem_head_desc& hd, int T, const void* x, const uint
   return p;
 }
 
-void split_x(const umem_head_desc& hd, int T, const void* x, uint16_t* parts, hipStream_t s) {
+void split_x(const umem_head_desc& hd, int T, const void* x, uint16_t* parts, const Token* list, const int* count,
+             hipStream_t s) {
   const size_t n = static_cast<size_t>(T) * hd.d;
   hipLaunchKernelGGL(head_split_kernel, dim3(static_cast<unsigned>((n / 4 + kThreads - 1) / kThreads)), dim3(kThreads), 0, s,
-                     static_cast<const float*>(x), parts, n);
+                     static_cast<const float*>(x), parts, n, hd.d, list, count);
 }
 
 template <bool F16, typename OT>
@@ -769,17 +843,16 @@ void product(const TilePairs& p, ProductArgs g, int side, hipStream_t s) {
 }
 
 template <int PR, int PC>
-void slope(const TilePairs& p, float scale, const int32_t* targets, const float* lse, const float* dloss,
-           const float* most, int v_first, int vocab, int piece, int t_ld, uint16_t* rows, uint16_t* cols,
-           float* lost, hipStream_t s) {
+void slope(const TilePairs& p, float scale, const Token* list, const int* count, const float* most, int v_first, int piece,
+           int t_ld, uint16_t* rows, uint16_t* cols, float* lost, hipStream_t s) {
   // (of 256 x 256 tiles one at a time is on a CU, and nothing beside its end)
   const int side = tile_plan(piece, p.b_rows, slice_count(p.k, p.n), 1, false).side;
   const int tm = (piece + side - 1) / side, tn = (p.b_rows + side - 1) / side;
   constexpr TileParts kParts = PR == 3 ? kThree : kPlain;
 #define UMEM_SLOPE(BM, GROUPS, PARTS)                                                                            \
   hipLaunchKernelGGL((head_slope_kernel<BM, BM, 2, 2, GROUPS, PARTS, PR, PC>), dim3(tile_grid(tm * tn)),        \
-                     dim3(256 * GROUPS), 0, s, p, tm, tn, scale, targets, lse, dloss, most, v_first, vocab,     \
-                     piece, t_ld, rows, cols, lost)
+                     dim3(256 * GROUPS), 0, s, p, tm, p.b_rows, scale, list, count, most, v_first, piece, t_ld, \
+                     rows, cols, lost)
   if (side == 128 && tm * tn > kCus) UMEM_SLOPE(128, 1, kPlain);
   else if (side == 128) UMEM_SLOPE(128, 2, kPlain);
   else if (PR == 3 && tm * tn > kCus) UMEM_SLOPE(64, 1, kParts);
@@ -804,7 +877,7 @@ hipError_t launch_head_loss(const umem_head_desc& hd, int T, const void* x, cons
   for (int t0 = 0; t0 < T; t0 += kBandTokens) {
     const int t = std::min(kBandTokens, T - t0);
     const char* xb = static_cast<const char*>(x) + static_cast<size_t>(t0) * hd.d * (hd.xtype == UMEM_F32 ? 4 : 2);
-    if (hd.xtype == UMEM_F32) split_x(hd, t, xb, parts, s);
+    if (hd.xtype == UMEM_F32) split_x(hd, t, xb, parts, nullptr, nullptr, s);
     const TilePairs p = logit_pairs(hd, t, xb, parts, w, hd.vocab);
     const int side = tile_plan(hd.vocab, t, slice_count(p.k, p.n), 1, true).side;
     const int tiles = (hd.vocab + side - 1) / side, tn = (t + side - 1) / side;
@@ -847,25 +920,32 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
   float* most = dloss ? reinterpret_cast<float*>(base + L.most) : nullptr;
   float* x_most = reinterpret_cast<float*>(base + L.x_most);
   float* lost = reinterpret_cast<float*>(base + L.lost);
-  // x's channels along rows, tokens along k
+  Token* list = reinterpret_cast<Token*>(base + L.list);
+  int* count = reinterpret_cast<int*>(base + L.count);
+  // x's channels along rows, the tokens that count along k
   const dim3 x_grid(t_pad / 64, (d + 63) / 64);
   if (wide) {
     const float* xf = static_cast<const float*>(x);
-    split_x(hd, T, x, parts, s);
-    hipLaunchKernelGGL(head_most_kernel<float>, dim3(kMostBlocks), dim3(1024), 0, s, xf, dloss, targets, T, d, V, most, x_most);
+    hipLaunchKernelGGL(head_list_kernel<float>, dim3(kMostBlocks), dim3(1024), 0, s, xf, lse, dloss, targets, T, d, V, list,
+                       count, most, x_most, static_cast<float*>(dx));
+    split_x(hd, T, x, parts, list, count, s);
     const auto turn = px == 2 ? head_transpose_kernel<float, 2> : head_transpose_kernel<float, 1>;
-    hipLaunchKernelGGL(turn, x_grid, dim3(kThreads), 0, s, xf, T, d, xt, static_cast<int64_t>(t_ld), x_most, targets, V);
+    hipLaunchKernelGGL(turn, x_grid, dim3(kThreads), 0, s, xf, T, d, xt, static_cast<int64_t>(t_ld), x_most, list, count,
+                       nullptr);
   } else {
-    hipLaunchKernelGGL(head_most_kernel<__bf16>, dim3(kMostBlocks), dim3(1024), 0, s, static_cast<const __bf16*>(x), dloss,
-                       targets, T, d, V, most, x_most);
+    hipLaunchKernelGGL(head_list_kernel<__bf16>, dim3(kMostBlocks), dim3(1024), 0, s, static_cast<const __bf16*>(x), lse,
+                       dloss, targets, T, d, V, list, count, most, x_most, static_cast<__bf16*>(dx));
     hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), x_grid, dim3(kThreads), 0, s,
-                       static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_ld), x_most, targets, V);
+                       static_cast<const uint16_t*>(x), T, d, xt, static_cast<int64_t>(t_ld), x_most, list, count, parts);
   }
   ProductArgs gx{}, gw{};
   const TilePlan plan_x = dx_plan(hd, T);
   gx.splits = plan_x.splits;
   gx.sums = sum;
   gx.whole = true;
+  gx.sum_size = static_cast<int64_t>(T) * d;
+  gx.count = gw.count = count;
+  gw.along_k = true;
   gw.splits = 1;
   gx.ld = gw.ld = d;
   gx.most = gw.most = most;
@@ -875,12 +955,12 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     const int v = std::min(piece, V - v0);
     const bool last = v0 + piece >= V;
     const uint16_t* wp = w + static_cast<int64_t>(v0) * d;
-    const TilePairs z = logit_pairs(hd, T, x, parts, wp, v);
+    const TilePairs z = logit_pairs(hd, T, parts, parts, wp, v);     // (bf16: the copy of the tokens that count)
     const auto make = pr == 3 ? (pc == 2 ? slope<3, 2> : slope<3, 1>) : (pc == 2 ? slope<1, 2> : slope<1, 1>);
-    make(z, hd.scale, targets, lse, dloss, most, v0, V, piece, t_ld, rows, cols, lost, s);
+    make(z, hd.scale, list, count, most, v0, piece, t_ld, rows, cols, lost, s);
     // dx: channels along m, tokens along n, the piece along k
     hipLaunchKernelGGL((head_transpose_kernel<uint16_t, 1>), dim3(piece / 64, (d + 63) / 64), dim3(kThreads), 0, s, wp, v,
-                       d, wt, static_cast<int64_t>(piece), nullptr, nullptr, 0);
+                       d, wt, static_cast<int64_t>(piece), nullptr, nullptr, nullptr, nullptr);
     TilePairs p{};
     p.n = pr;
     for (int i = 0; i < pr; ++i) {
@@ -897,10 +977,9 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
     gx.out = last ? dx : sum;
     gx.scale = last ? hd.scale : 1.f;
     gx.most = last ? most : nullptr;
-    gx.targets = last ? targets : nullptr;
+    gx.list = last ? list : nullptr;
     gx.lost = last && pr == 1 ? lost : nullptr;
     gx.w = w;
-    gx.vocab = V;
     if (!last || wide) product<false, float>(p, gx, plan_x.side, s);
     else product<false, __bf16>(p, gx, plan_x.side, s);
     // dW: channels along m, the piece's rows along n, tokens along k; of fp32 x and two parts of r the pairs that count
@@ -930,8 +1009,8 @@ hipError_t launch_head_backward(const umem_head_desc& hd, int T, const void* x, 
   }
   if (gx.splits > 1) {
     const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(T) * d / 4 + kThreads - 1) / kThreads));
-    if (wide) hipLaunchKernelGGL(head_sum_kernel<float>, grid, dim3(kThreads), 0, s, gx, T, d);
-    else hipLaunchKernelGGL(head_sum_kernel<__bf16>, grid, dim3(kThreads), 0, s, gx, T, d);
+    if (wide) hipLaunchKernelGGL(head_sum_kernel<float>, grid, dim3(kThreads), 0, s, gx);
+    else hipLaunchKernelGGL(head_sum_kernel<__bf16>, grid, dim3(kThreads), 0, s, gx);
   }
   return hipGetLastError();
 }

@@ -345,9 +345,10 @@ __device__ __forceinline__ TilePlace tile_place(int item, int tiles_m, int tiles
   const int in = item - first * tiles_n;
   return {first + in % high, in / high};
 }
+// (`items`, and past it, of a workgroup without one: a grid may be of more)
 __device__ __forceinline__ int tile_item(int items) {
-  const int per = (items + kTileXcds - 1) / kTileXcds;
-  return (blockIdx.x % kTileXcds) * per + blockIdx.x / kTileXcds;
+  const int per = (items + kTileXcds - 1) / kTileXcds, in = blockIdx.x / kTileXcds;
+  return in < per ? (blockIdx.x % kTileXcds) * per + in : items;
 }
 inline int tile_grid(int items) { return (items + kTileXcds - 1) / kTileXcds * kTileXcds; }
 

@@ -201,6 +201,27 @@ def test_pieces_of_many_tokens():
     assert bool(((dw.double() - r.t().contiguous() @ x.double()).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("T", [1023, 1024, 1025, 300001])
+@pytest.mark.parametrize("xt", [F, BF])
+def test_few_of_many_tokens_count(T, xt):
+    """A few tokens among many that do not count: their gradients are the formula's, the others' rows of dx zero."""
+    vocab, d = 40, 16
+    x, w, y, dloss = make(T, vocab, d, xt, none=0.0)
+    on = torch.zeros(T, dtype=torch.bool, device="cuda")
+    on[torch.randperm(T, generator=gen(T), device="cuda")[:60]] = True
+    on[T - 1] = True
+    y[~on] = -1
+    ds = desc(vocab, d, xt, F, 1.0)
+    _, lse = forward(ds, x, w, y)
+    dx, dw = backward(ds, x, w, y, lse, dloss, F)
+    assert not dx[~on].any()
+    few = [t[on].contiguous() for t in (x, y, lse, dloss)]
+    X, W, Y, G = host(few[0]), host(w), few[1].cpu().numpy(), host(few[3])
+    want_x, want_w, tx, tw = bounds(X, W, Y, G, 1.0, z_error(X, W, 1.0), xt == F, True)
+    tx += (0 if xt == F else HALF) * (np.abs(want_x) + tx) + 2.0 ** -130
+    assert (np.abs(host(dx[on]) - want_x) <= tx).all() and (np.abs(host(dw) - want_w) <= tw + 2.0 ** -130).all()
+
+
 def test_no_dloss_is_ones():
     x, w, y, _ = make(70, 200, 64, BF)
     ds = desc(200, 64, BF, F, 1.0)
