@@ -10,8 +10,8 @@
 // scratch in bf16 in both orders, and two more products take it, all three with k innermost (x and the piece's rows of
 // W are laid out transposed beforehand).  Bounded by the matrix cores: 2 T V d operations forward, 6 T V d backward, but
 // for few tokens, where W is read once at the rate of the memory.  Measured: 16 tokens by 50,000 rows of 2,048 40 + 5 us (W
-// at 5.2 TB/s); 8,192 tokens by 50,000 of 2,048, forward and backward with dW in fp32, 7.8 ms for 8.4 TFLOP: the logits 1.36 ms
-// (1.23 PFLOP/s), then for each 7,168 rows r 258 us, W's transpose 12, dx 206 (1.17 PFLOP/s), dW 408 (two products, 1.18).
+// at 5.2 TB/s); 8,192 tokens by 50,000 of 2,048, forward and backward with dW in fp32, 7.5 ms for 8.3 TFLOP: the logits 1.33 ms
+// (1.25 PFLOP/s), then for each 7,168 rows r 252 us, W's transpose 11, dx 207 (1.14 PFLOP/s), dW 399 (two products, 1.18).
 // Tokens that do not count are left out of the backward: a list of those that do is made first, and every product's grid and
 // length follow its count on the device (2,000 tokens, a third of them without a target, by 32,003 of 1,024 642 us with
 // them, so 528).
