@@ -177,7 +177,7 @@ __device__ __forceinline__ int x_shift(const float* most) {
   const float m = all_most(most);
   int e = 0;
   frexpf(m, &e);
-  return m > 0.f ? min(max(15 - e, -110), 110) : 0;
+  return m > 0.f ? 15 - e : 0;
 }
 
 // Part i of a value as fp16 parts; what is past the first part of a value that is infinite or none is zero.
@@ -433,7 +433,8 @@ __device__ __forceinline__ float most_of(const float* most) {
 // The tile's rows are in an order in which a lane holds 8 values of W's rows one after another, and NT tokens one after another, so
 // that both orders are written from the registers, in whole 64- and 128-byte pieces.  (Through LDS, a part at a time,
 // the end of a tile took as long as its products: 7,168 x 8,192 of 2,048 316 us, so 258, 0.93 PFLOP/s.)
-constexpr float kSlopeUp = 32768.f;
+constexpr int kSlopeBits = 15;
+constexpr float kSlopeUp = 1 << kSlopeBits;
 
 // Within a wave's rows of A, accumulator block i, row 4 q + r (q = lane / 16): 32 (i / 2) + 8 q + 4 (i % 2) + r; within its
 // rows of B, block j, row l: NT l + j.
@@ -584,10 +585,17 @@ __device__ __forceinline__ f32x4 lost_row(const ProductArgs& g, int t, int m) {
   return g.lost[t] * f32x4{bits_f32(b.x & 0xffffu), bits_f32(b.x >> 16), bits_f32(b.y & 0xffffu), bits_f32(b.y >> 16)};
 }
 
-// f of the output.
-__device__ __forceinline__ float product_factor(const ProductArgs& g) {
-  const float f = g.scale * most_of(g.most);
-  return g.x_most ? f * (1.f / kSlopeUp) : f;
+// What the sums are multiplied by, 2^e m with m below 1, as neither its own parts nor a sum times one of them need be within
+// fp32 where the result is.
+struct Factor {
+  float m;
+  int e;
+  __device__ __forceinline__ float operator()(float v) const { return ldexpf(v * m, e); }
+};
+__device__ __forceinline__ Factor product_factor(const ProductArgs& g) {
+  int e = 0;
+  const double m = frexp(static_cast<double>(g.scale) * most_of(g.most), &e);
+  return {static_cast<float>(m), g.x_most ? e - kSlopeBits - x_shift(g.x_most) : e};
 }
 
 // GROUPS sets of waves share a tile's slices where there are too few tiles for more than one on a CU: with one wave on each
@@ -641,8 +649,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
         for (int i = 0; i < Tl::MT; ++i) acc[i][j] += sums[(k * Tl::MT * Tl::NT + j * Tl::MT + i) * Tl::kThreads];
   }
   const int lane = threadIdx.x & 63, wave = Tl::thread() >> 6, wr = wave / WC, wc = wave % WC;
-  const float f = product_factor(g);
-  const int back = g.x_most ? -x_shift(g.x_most) : 0;
+  const Factor f = product_factor(g);
 #pragma unroll
   for (int j = 0; j < Tl::NT; ++j) {
     const int n = at.n * BN + (wc * Tl::NT + j) * 16 + (lane & 15);
@@ -663,7 +670,7 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
       if (g.whole && g.before) v += *reinterpret_cast<const f32x4*>(g.before + o);
       if (g.lost) v += lost_row(g, n, m);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], back) * f;
+      for (int r = 0; r < 4; ++r) v[r] = f(v[r]);
       if (!g.whole && g.before) v += *reinterpret_cast<const f32x4*>(g.before + o);
       OT* out = static_cast<OT*>(g.out) + out_row * g.ld + m;
       if constexpr (sizeof(OT) == 4)
@@ -678,14 +685,15 @@ __global__ __launch_bounds__(64 * WR * WC * GROUPS) void head_product_kernel(Til
 // dx from the splits' sums, in their order.
 template <typename OT>
 __global__ __launch_bounds__(kThreads) void head_sum_kernel(ProductArgs g) {
-  const float f = product_factor(g);
+  const Factor f = product_factor(g);
   const int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
   if (i >= *g.count * g.ld) return;
   f32x4 v = *reinterpret_cast<const f32x4*>(g.sums + i);
   for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const f32x4*>(g.sums + s * g.sum_size + i);
   const int t = static_cast<int>(i / g.ld), m = static_cast<int>(i - t * g.ld);
   if (g.lost) v += lost_row(g, t, m);
-  v *= f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = f(v[r]);
   OT* out = static_cast<OT*>(g.out) + g.list[t].row * g.ld + m;
   if constexpr (sizeof(OT) == 4)
     *reinterpret_cast<f32x4*>(out) = v;

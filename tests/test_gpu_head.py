@@ -222,6 +222,30 @@ def test_few_of_many_tokens_count(T, xt):
     assert (np.abs(host(dx[on]) - want_x) <= tx).all() and (np.abs(host(dw) - want_w) <= tw + 2.0 ** -130).all()
 
 
+@pytest.mark.parametrize("xt,gt", [(F, F), (BF, BF), (F, BF)])
+@pytest.mark.parametrize("T,vocab,d", [(40, 90, 64), (700, 300, 96)])
+def test_powers_of_two(T, vocab, d, xt, gt):
+    """Hidden states times 2^100, the weight times 2^-100: the same losses, and gradients that differ by those powers alone;
+    states up to the largest, with gradients of the losses so small that the weight's gradient is within fp32."""
+    x, w, y, dloss = make(T, vocab, d, xt, none=0.1)
+    ds = desc(vocab, d, xt, gt, 0.5)
+    loss, lse = forward(ds, x, w, y)
+    dx, dw = backward(ds, x, w, y, lse, dloss, gt)
+    big, small = x * 2.0 ** 100, w * 2.0 ** -100
+    loss2, lse2 = forward(ds, big, small, y)
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2)
+    dx2, dw2 = backward(ds, big, small, y, lse, dloss * 2.0 ** 20, gt)
+    assert torch.equal(dx2.double(), dx.double() * 2.0 ** -80) and torch.equal(dw2 * 2.0 ** -60, dw * 2.0 ** 60)
+    big, small = x.clamp(-7.9, 7.9) * 2.0 ** 125, w * 2.0 ** -115
+    w = small * 2.0 ** 115                # (entries of w below 2^-11 lose bits in `small`, which is below 2^-126 there)
+    ds, near = desc(vocab, d, xt, gt, 2.0 ** -10), desc(vocab, d, xt, gt, 1.0)
+    _, lse = forward(near, x.clamp(-7.9, 7.9), w, y)
+    assert torch.equal(forward(ds, big, small, y)[1], lse)
+    _, dw = backward(near, x.clamp(-7.9, 7.9), w, y, lse, dloss, gt)
+    _, dw2 = backward(ds, big, small, y, lse, dloss * 2.0 ** -100, gt)
+    assert torch.equal(dw2 * 2.0 ** -15, dw)
+
+
 def test_no_dloss_is_ones():
     x, w, y, _ = make(70, 200, 64, BF)
     ds = desc(200, 64, BF, F, 1.0)
