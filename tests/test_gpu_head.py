@@ -246,6 +246,54 @@ def test_powers_of_two(T, vocab, d, xt, gt):
     assert torch.equal(dw2 * 2.0 ** -15, dw)
 
 
+@pytest.mark.parametrize("T,vocab", [(20, 1 << 20), (1 << 20, 70)])
+def test_past_4_gib(T, vocab):
+    """A weight, and hidden states, of 4.8 GB: the largest vocabulary and the most tokens that the calls take."""
+    d = 2304
+    print(f"[case] head {T} {vocab} {d}", flush=True)
+    g = gen(3)
+    fill = lambda n, std: torch.empty((n, d), dtype=BF, device="cuda").normal_(std=std, generator=g)   # noqa: E731
+    x, w = fill(T, 1.0), fill(vocab, 2.0 / d ** 0.5)
+    y = torch.randint(0, vocab, (T,), generator=g, device="cuda").to(torch.int32)
+    y[T - 1], y[0] = vocab - 1, -1
+    dloss = torch.rand((T,), generator=g, device="cuda") + 0.5
+    ds = desc(vocab, d, BF, F, 1.0)
+    loss, lse = forward(ds, x, w, y)
+    step = 1 << 14
+    z = torch.empty((T, vocab), dtype=torch.float32, device="cuda")      # logits rounded to 32 bits: 2^-24 of their 16
+    for t in range(0, T, step):
+        for v in range(0, vocab, step):
+            z[t:t + step, v:v + step] = x[t:t + step].double() @ w[v:v + step].double().t().contiguous()
+    # sums over d of products of about 4 2^-5.6 with fp32 roundings, their rest in the sizes
+    err = 2 * u * (d / 32 + 16) * 60 + 64 * u
+    want = torch.cat([torch.logsumexp(c.double(), 1) for c in z.split(step)]) if T > step else torch.logsumexp(z.double(), 1)
+    goal = z.gather(1, y.clamp(min=0).long()[:, None])[:, 0].double()
+    assert float((lse - want).abs().max()) <= err
+    assert float((loss - torch.where(y >= 0, want - goal, 0.0)).abs().max()) <= 2 * err
+    dx, dw = backward(ds, x, w, y, lse, dloss, F)
+    on = (y >= 0).double() * dloss.double()
+    rows = torch.tensor([0, 1, 9, T // 2, T - 2, T - 1], device="cuda")
+    cols = torch.tensor([0, 1, vocab // 2, vocab - 2, vocab - 1], device="cuda")
+
+    def slope(t, v):
+        r = torch.exp(z[t][:, v].double() - want[t][:, None]) - (y[t][:, None] == v[None]).double()
+        return r * on[t][:, None]
+    every_v, every_t = torch.arange(vocab, device="cuda"), torch.arange(T, device="cuda")
+    got, size = torch.zeros((len(rows), d), dtype=torch.float64, device="cuda"), 0.0
+    for v in every_v.split(step):
+        r = slope(rows, v)
+        got += r @ w[v].double()
+        size = size + r.abs() @ w[v].double().abs()
+    assert bool(((dx[rows].double() - got).abs() <= HALF * got.abs() + (HALF + 4 * err) * size + 1e-12).all())
+    got, size = torch.zeros((len(cols), d), dtype=torch.float64, device="cuda"), 0.0
+    for t in every_t.split(step):
+        r = slope(t, cols).t().contiguous()
+        got += r @ x[t].double()
+        size = size + r.abs() @ x[t].double().abs()
+    lost = 2.0 ** -40 * 1.5 * 8.0 * T                                   # what lies below 2^-40 of the largest r, of each token
+    assert bool(((dw[cols].double() - got).abs() <= (4 * err + 6 * 2 * u * (min(T, 1 << 16) / 32 + 16)) * size + lost).all())
+
+
 def test_no_dloss_is_ones():
     x, w, y, _ = make(70, 200, 64, BF)
     ds = desc(200, 64, BF, F, 1.0)

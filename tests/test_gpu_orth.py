@@ -157,6 +157,20 @@ def test_tiles(n, rows, cols, steps, ot):
     check(n, rows, cols, ot=ot, steps=steps)
 
 
+@pytest.mark.parametrize("n,rows,cols", [(300, 65, 65536), (300, 65536, 66), (300, 64, 65536)])
+def test_past_4_gib(n, rows, cols):
+    """Batches of 5 GB: the first and the last matrices."""
+    print(f"[case] orth {n} {rows} {cols}", flush=True)
+    x = torch.empty((n, rows, cols), device="cuda").normal_(generator=gen(n))
+    out = run(desc(n, rows, cols, F, F, 2), x, torch.empty_like(x))
+    f32 = [float(np.float32(v)) for v in COEF]
+    for j in (0, n - 1):
+        want, norms = M.newton_schulz(host(x[j]), 2, *f32, float(np.float32(1e-7)))
+        tol = tolerance(norms, max(rows, cols), 2, COEF) + 8 * u * np.linalg.norm(want)
+        assert np.linalg.norm(host(out[j]) - want) <= tol
+    assert bool(out.isfinite().all())
+
+
 def test_matrices_are_apart():
     """Zeros give zeros, a NaN or an infinity stays with its matrix, and each matrix is what it is alone."""
     x = torch.randn((4, 48, 80), generator=gen(2), device="cuda")
