@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void orth_small_gram_kernel(const T* __re
 // The steps of one matrix of at most TOP rows: q[matrix][64][64] = Q / (|G| + eps).  The matrices are symmetric: the 16 x
 // 16 tiles on and below the diagonal are made, a wave's at a time, and written to both places.  T and the next Q, which
 // read the same, are made together: 20 tiles on 16 waves.  What bounds it is the fp64 rate of one CU: 64^3 products
-// of a full square are 4,096 clocks, and 5 steps have 17 squares (with full squares 42 us, so 38).
+// of a full square are 4,096 clocks, and 5 steps have 17 squares (with full squares 42 us, so 34).
 template <int TOP>
 __global__ __launch_bounds__(kStepThreads) void orth_small_steps_kernel(const double* __restrict__ pieces, int m, int chunks,
                                                                         int steps, double a, double b, double c,
@@ -117,22 +117,30 @@ __global__ __launch_bounds__(kStepThreads) void orth_small_steps_kernel(const do
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t mat = blockIdx.x;
   const double* from = pieces + mat * chunks * kSide * kSide;
-  for (int i = threadIdx.x; i < TOP * TOP; i += kStepThreads) {
-    const int row = i / TOP, col = i % TOP;
-    double v = 0.0;
-#pragma unroll 8
-    for (int p = 0; p < chunks; ++p) v += from[(static_cast<int64_t>(p) * kSide + row) * kSide + col];
-    A[row][col] = v;
+  constexpr int kEach = (TOP * TOP + kStepThreads - 1) / kStepThreads;
+  double v[kEach] = {};
+#pragma unroll 4
+  for (int p = 0; p < chunks; ++p)
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = min(i * kStepThreads + static_cast<int>(threadIdx.x), TOP * TOP - 1);
+      v[i] += from[(static_cast<int64_t>(p) * kSide + at / TOP) * kSide + at % TOP];
+    }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = i * kStepThreads + threadIdx.x;
+    if (at < TOP * TOP) A[at / TOP][at % TOP] = v[i];
   }
   __syncthreads();
   double trace = lane < m ? A[lane][lane] : 0.0;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) trace += __shfl_xor(trace, off, 64);
-  const double norm = sqrt(trace) + static_cast<double>(eps);
+  const double norm = sqrt(trace) + static_cast<double>(eps), inverse = 1.0 / norm;
   __syncthreads();
-  for (int i = threadIdx.x; i < TOP * TOP; i += kStepThreads) {
-    const int row = i / TOP, col = i % TOP;
-    A[row][col] = row < m && col < m ? A[row][col] / (norm * norm) : 0.0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = i * kStepThreads + threadIdx.x, row = at / TOP, col = at % TOP;
+    if (at < TOP * TOP) A[row][col] = row < m && col < m ? v[i] * inverse * inverse : 0.0;
   }
   __syncthreads();
   const auto row_of = [](int tile) { return (tile >= 1) + (tile >= 3) + (tile >= 6); };
@@ -184,9 +192,10 @@ __global__ __launch_bounds__(kStepThreads) void orth_small_steps_kernel(const do
     __syncthreads();
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < TOP * TOP; i += kStepThreads) {
-    const int row = i / TOP, col = i % TOP;
-    q[(mat * kSide + row) * kSide + col] = Q[row][col] / norm;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = i * kStepThreads + threadIdx.x, row = at / TOP, col = at % TOP;
+    if (at < TOP * TOP) q[(mat * kSide + row) * kSide + col] = Q[row][col] * inverse;
   }
 }
 
