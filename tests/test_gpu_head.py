@@ -171,7 +171,9 @@ TILES_OF_X = [(4186, 6, 200), (6636, 5, 272), (7168, 4, 392), (6148, 4, 656), (4
                          [(*t, F, BF) for t in TILES_OF_X] + [(*t, BF, BF) for t in TILES_OF_X] +
                          [(3, 8297, 80, BF, F), (4, 16296, 896, BF, F), (4, 12778, 1736, BF, BF), (3, 5054, 1560, F, BF),
                           (4604, 279, 72, BF, F), (4604, 279, 72, F, F), (6331, 327, 72, F, F), (5634, 656, 72, F, F),
-                          (263, 17135, 816, BF, F), (2908, 1052, 88, F, BF), (2052, 5024, 72, F, BF), (6209, 1290, 152, F, BF)])
+                          (2198, 5574, 16, BF, BF), (6268, 5, 1864, F, F), (3139, 5, 1768, F, F),
+                          (4266, 1693, 264, F, F), (929, 8196, 72, F, F), (3000, 700, 264, BF, BF), (263, 17135, 816, BF, F),
+                          (2908, 1052, 88, F, BF), (2052, 5024, 72, F, BF), (6209, 1290, 152, F, BF)])
 def test_tiles(T, vocab, d, xt, gt):
     print(f"[case] head {T} {vocab} {d} {xt} {gt}", flush=True)
     check(T, vocab, d, xt, gt)
