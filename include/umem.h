@@ -621,7 +621,7 @@ typedef struct umem_orth_desc {
  * values stay below 16 where the coefficients keep singular values of [0, 1] there (an entry of X, A or b A + c A^2
  * that reaches 16 becomes infinite).  Sums are fp32, the norm fp64.  Where G is at least twice as long as wide, two or
  * three steps may be taken at a time on products of A (as long as |a| to that power is at most 100), and where the
- * smaller side is at most 64 all of them, in fp64. */
+ * smaller side is at most 64 all of them, or as many at a time as keep |a|^(3 steps) within 2^33, in fp64. */
 UMEM_API umem_status umem_orthogonalize_workspace_size(const umem_orth_desc* od, size_t* bytes);
 
 /*   g    [n, rows, cols] of gtype;  out [n, rows, cols] of otype (may equal g); both aligned to their elements
