@@ -32,7 +32,8 @@ namespace umem {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kUp = 4096.f, kDown = 1.f / 4096.f;
+constexpr int kUpBits = 12;
+constexpr float kDown = 1.f / (1 << kUpBits);
 
 __device__ __forceinline__ uint32_t f16_bits(float x) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(x)); }
 __device__ __forceinline__ float bits_f32(uint32_t b) {
@@ -126,12 +127,13 @@ __global__ __launch_bounds__(kThreads) void orth_first_kernel(const T* __restric
   for (int i = threadIdx.x & (kWave - 1); i < blocks; i += kWave) sum += pieces[mat * blocks + i];
 #pragma unroll
   for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
-  const float norm = static_cast<float>(sqrt(sum)) + eps;
+  int e = 0;                                                // (the norm of values within fp32 may be past it)
+  const float norm = static_cast<float>(frexp(sqrt(sum) + static_cast<double>(eps), &e));
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int r = i * 4 + threadIdx.x / 64;
     uint32_t hi, lo;
-    f16_parts(v[i] / norm * kUp, hi, lo);
+    f16_parts(ldexpf(v[i], kUpBits - e) / norm, hi, lo);
     tile[r][c] = r0 + r < rows && c0 + c < cols ? hi | lo << 16 : 0u;
   }
   __syncthreads();

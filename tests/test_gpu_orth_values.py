@@ -68,3 +68,31 @@ def test_many_steps_in_place():
         want = run(od, x, torch.empty_like(x))
         assert torch.equal(x, kept)
         assert torch.equal(run(od, x, x), want)
+
+
+# Both ways of taking the steps beside the small sides' one: single steps, and rounds of them on long matrices.
+LARGE = [(96, 160), (160, 96), (70, 3000), (3000, 70)]
+
+
+@pytest.mark.parametrize("gt", [F, BF])
+@pytest.mark.parametrize("rows,cols", LARGE + [(64, 96)])
+def test_any_scale_of_the_gradient(rows, cols, gt):
+    """A power of two times G gives the same bits, where the norm is past the largest fp32 and where values have few bits left."""
+    print(f"[case] orth {rows} {cols} {gt}", flush=True)
+    x = torch.randn((1, rows, cols), generator=gen(rows), device="cuda").clamp(-3.9, 3.9).to(gt)
+    od = desc(1, rows, cols, gt, F, eps=0.0)
+    want = run(od, x, torch.empty((1, rows, cols), device="cuda"))
+    assert bool(want.isfinite().all()) and float(want.norm()) > 1
+    for e in (100, 126, -100, -120 if gt == BF else -126):
+        big = torch.ldexp(x.double().cpu(), torch.tensor(e)).to(gt)
+        back = torch.ldexp(big.double(), torch.tensor(-e)).to(gt)       # what is left of x
+        if e > 0:
+            assert torch.equal(back, x.cpu()) and bool(big.isfinite().all())
+            assert e < 126 or float(big.double().norm()) > 3.5e38
+        ref = run(od, back.cuda(), torch.empty((1, rows, cols), device="cuda"))
+        assert torch.equal(run(od, big.cuda(), torch.empty((1, rows, cols), device="cuda")), ref), e
+    od = desc(1, rows, cols, gt, F, eps=1e38)                            # an eps of the norm's size
+    big = torch.ldexp(x.double().cpu(), torch.tensor(126)).to(gt)
+    got = run(od, big.cuda(), torch.empty((1, rows, cols), device="cuda"))
+    want, _ = M.newton_schulz(host(big[0]), 5, *F32, float(np.float32(1e38)))
+    assert np.linalg.norm(host(got[0]) - want) <= 1e-4 * np.linalg.norm(want)
