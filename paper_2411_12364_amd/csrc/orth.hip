@@ -228,24 +228,24 @@ __device__ __forceinline__ u32x4 finish_four(const OrthArgs& g, int64_t mat, int
   if constexpr (is_last(MODE)) {
     if (!in) return u32x4{0u, 0u, 0u, 0u};
     OT* to = static_cast<OT*>(g.final) + mat * g.final_matrix + n * g.final_ld + m;
-    const float s = g.scale * kDown;
+    v *= kDown;                           // (not as a part of the scale, which may be as small as fp32 holds)
     typedef OT four __attribute__((ext_vector_type(4), aligned(sizeof(OT))));
     if (m + 4 <= g.rows_m) {
       four o;
       if (g.decay != 0.f) {
         const four h = *reinterpret_cast<const four*>(to);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[r] = static_cast<OT>(fmaf(g.decay, to_f32(h[r]), s * v[r]));
+        for (int r = 0; r < 4; ++r) o[r] = static_cast<OT>(fmaf(g.decay, to_f32(h[r]), g.scale * v[r]));
       } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[r] = static_cast<OT>(s * v[r]);
+        for (int r = 0; r < 4; ++r) o[r] = static_cast<OT>(g.scale * v[r]);
       }
       *reinterpret_cast<four*>(to) = o;
     } else {
 #pragma unroll
       for (int r = 0; r < 3; ++r) {
         if (m + r >= g.rows_m) break;
-        to[r] = static_cast<OT>(g.decay != 0.f ? fmaf(g.decay, to_f32(to[r]), s * v[r]) : s * v[r]);
+        to[r] = static_cast<OT>(g.decay != 0.f ? fmaf(g.decay, to_f32(to[r]), g.scale * v[r]) : g.scale * v[r]);
       }
     }
     return u32x4{0u, 0u, 0u, 0u};

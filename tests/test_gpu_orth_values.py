@@ -96,3 +96,22 @@ def test_any_scale_of_the_gradient(rows, cols, gt):
     got = run(od, big.cuda(), torch.empty((1, rows, cols), device="cuda"))
     want, _ = M.newton_schulz(host(big[0]), 5, *F32, float(np.float32(1e38)))
     assert np.linalg.norm(host(got[0]) - want) <= 1e-4 * np.linalg.norm(want)
+
+
+# Of X in fp32 the product with scale is one rounding (u, or half the smallest subnormal); the small sides' X is rounded
+# after the product instead, so X itself differs by a rounding: 2 u and 2^-149 in all.  With decay one sum more.
+@pytest.mark.parametrize("rows,cols", LARGE + [(64, 96)])
+def test_any_scale_of_the_update(rows, cols):
+    """Factors near the smallest and the largest fp32 multiply X as others do."""
+    print(f"[case] orth {rows} {cols}", flush=True)
+    x = torch.randn((1, rows, cols), generator=gen(rows + 1), device="cuda")
+    held = torch.randn((1, rows, cols), generator=gen(rows + 2), device="cuda")
+    want = host(run(desc(1, rows, cols, F, F), x, torch.empty_like(x)))
+    for f in (1.3 * 2.0 ** -116, -1.7 * 2.0 ** -122, 1.1 * 2.0 ** -40, 1.9 * 2.0 ** 126):
+        f = float(np.float32(f))
+        got = host(run(desc(1, rows, cols, F, F, scale=f), x, torch.empty_like(x)))
+        assert (np.abs(got - f * want) <= 2 * u * np.abs(f * want) + 2.0 ** -149).all(), f
+        small = held * min(abs(f), 1.0)
+        got = host(run(desc(1, rows, cols, F, F, decay=0.5, scale=f), x, small.clone()))
+        ref, size = 0.5 * host(small) + f * want, 0.5 * np.abs(host(small)) + np.abs(f * want)
+        assert (np.abs(got - ref) <= 3 * u * size + 2.0 ** -148).all(), f
