@@ -141,7 +141,8 @@ __global__ __launch_bounds__(1024) void head_list_kernel(const T* __restrict__ x
     if (tid == 0 && first + 1024 >= tokens) *count = all;
     __syncthreads();
   }
-  typedef T eight __attribute__((ext_vector_type(8)));
+  typedef T eight __attribute__((ext_vector_type(8), aligned(16)));
+  static_assert(alignof(eight) == 16, "what x and dx are aligned to (eight fp32 by themselves claim 32 bytes)");
   const uint32_t row = d / 8, pieces = static_cast<uint32_t>(tokens) * row;       // at most 2^31
   float m = 0.f;
 #pragma unroll 4
