@@ -565,7 +565,7 @@ typedef struct umem_head_desc {
 /* Requirements (UMEM_ERR_INVALID_ARG otherwise): vocab, d >= 1, the types as listed, a finite scale.
  * Limits (UMEM_ERR_UNSUPPORTED beyond them): d a multiple of 8; d <= 16384; vocab <= 2^20; T <= 2^20.
  * Sums, statistics and losses are fp32 or more.  fp32 x is not rounded: it enters the matrix cores as a
- * sum of bf16 parts.  A logit of NaN makes its token's loss NaN; what one token holds stays with it in loss, lse and dx. */
+ * sum of bf16 parts (a value past 3.39e38, which bf16 does not hold, as an infinity).  A logit of NaN makes its token's loss NaN; what one token holds stays with it in loss, lse and dx. */
 
 /* Scratch bytes that umem_head_loss needs for T tokens or fewer. */
 UMEM_API umem_status umem_head_loss_workspace_size(const umem_head_desc* hd, int32_t T, size_t* bytes);
@@ -580,7 +580,9 @@ UMEM_API umem_status umem_head_loss(const umem_head_desc* hd, int32_t T, const v
                            hipStream_t stream);
 
 /* Scratch bytes that umem_head_backward needs for T tokens or fewer: r below for a piece of the vocabulary at a
- * time, x and the piece of w transposed, a sum of dx in fp32. */
+ * time in both orders, x and the piece of w transposed, the rows of x that count (of fp32 x as parts), a sum of dx in
+ * fp32 and, up to 64 MiB for each gradient, the sums of products that are split.  2,000 bf16 tokens by 32,003 of 1,024
+ * with a bf16 dw take 315 MB, 8,192 fp32 ones by 50,000 of 2,048 with an fp32 dw 1.04 GB. */
 UMEM_API umem_status umem_head_backward_workspace_size(const umem_head_desc* hd, int32_t T, size_t* bytes);
 
 /* Backward of umem_head_loss; the logits are made again from x and w:
@@ -591,11 +593,12 @@ UMEM_API umem_status umem_head_backward_workspace_size(const umem_head_desc* hd,
  *   dx          [T, d] of xtype;  dw [vocab, d] of gtype; both 16-byte aligned
  *   accumulate  0: dw is written; 1: added to (fp32 only, UMEM_ERR_INVALID_ARG otherwise)
  *   ws          256-byte aligned scratch of umem_head_backward_workspace_size bytes
- * For dx r is bf16 where x is (a target's entry counts whole all the same), and whole where x is fp32.  For dw, in
- * units of the largest |dloss| and of the largest |x| of the tokens that count, r has 11 bits where dw is bf16 and 22
- * where it is fp32, and x as many as it has, 22 of fp32; what lies below 2^-40 of these units is lost.  Results are
- * rounded once more to their type.  The sums run in a fixed order.  dx, dw and ws overlap neither an
- * input nor each other (UMEM_ERR_INVALID_ARG).  T == 0 writes nothing. */
+ * For dx r is bf16 where x is (a target's entry counts whole all the same), and whole where x is fp32; what lies below
+ * 2^-126 of the largest |dloss| is lost.  For dw, in units of the largest |dloss| and of the largest |x| of the tokens
+ * that count, r has 11 bits where dw is bf16 and 22 where it is fp32, and so has fp32 x, while bf16 x has all of its own;
+ * what lies below 2^-40 of these units is lost (so a token whose dloss is 2^-20 of the largest has at most 20 bits of
+ * r, and one of 2^-40 does not reach dw).  Results are rounded once more to their type.  The sums run in a fixed order.
+ * dx, dw and ws overlap neither an input nor each other (UMEM_ERR_INVALID_ARG).  T == 0 writes nothing. */
 UMEM_API umem_status umem_head_backward(const umem_head_desc* hd, int32_t T, const void* x, const uint16_t* w,
                                const int32_t* targets, const float* lse, const float* dloss, void* dx, void* dw,
                                int32_t accumulate, void* ws, size_t ws_bytes, hipStream_t stream);
@@ -619,7 +622,8 @@ typedef struct umem_orth_desc {
  * Limits (UMEM_ERR_UNSUPPORTED beyond them): rows and cols <= 2^16; n < 2^16; n * rows * cols <= 2^33; steps <= 16.
  * Between the steps a matrix has 22 bits of each value of 2^-14 or more and an absolute error of 2^-37 below; its
  * values stay below 16 where the coefficients keep singular values of [0, 1] there (an entry of X, A or b A + c A^2
- * that reaches 16 becomes infinite).  Sums are fp32, the norm fp64.  Where G is at least twice as long as wide, two or
+ * that reaches 16 becomes infinite).  Sums are fp32, the norm fp64.  So in directions whose singular value is next to
+ * none X holds noise of 2^-22 of the largest, which grows by |a| a step as they do, as it would in fp32.  Where G is at least twice as long as wide, two or
  * three steps may be taken at a time on products of A (as long as |a| to that power is at most 100), and where the
  * smaller side is at most 64 all of them, or as many at a time as keep |a|^(3 steps) within 2^33, in fp64. */
 UMEM_API umem_status umem_orthogonalize_workspace_size(const umem_orth_desc* od, size_t* bytes);
