@@ -5,7 +5,7 @@
 // Both move memory and compute next to nothing.  The gradient sorts the (token, place) pairs, so that every row of the
 // table is summed by its places in order: no atomics, the same bits each time.  Up to 4,096 places are sorted by one
 // workgroup in LDS, up to 32,768 by a launch a pass, as a chain of short launches costs more than what they do (8,192
-// places: 11 us in two, 23 by sort.hip's six).  A wave takes a run of sorted places
+// places: 11 us in two, 23 by sort.hip's six, 17 by one workgroup with eight places a thread).  A wave takes a run of sorted places
 // and 256 columns; a row that begins and ends within its run is written at once, what is left at
 // the run's two ends goes to scratch, and a second kernel adds the pieces of rows that pass from run to run.
 #include <algorithm>

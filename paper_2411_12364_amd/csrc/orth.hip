@@ -11,8 +11,8 @@
 //   P = a I + b A + c A^2,  Q <- Q P,  A <- P A P,   then X <- Q X:
 //
 // 3 products of m x m x m for each step but the first in the place of A = X X^T and B X.  Bounded by the matrix cores for
-// large matrices, by the chain of launches for small ones.  Measured, five steps: 896 x 2,048 in 18 launches 196 us, of which
-// the 13 products of 896 x 896 x 896 take 8 to 10 each; 1,024 x 16,384 580 us, X X^T 52 + 9 (36 of 64 tiles, three pairs of
+// large matrices, by the chain of launches for small ones.  Measured, five steps: 896 x 2,048 in 19 launches 191 us, of which
+// the 13 products of 896 x 896 x 896 take 9.5 each (one, of two at a time, 12); 1,024 x 16,384 580 us, X X^T 52 + 9 (36 of 64 tiles, three pairs of
 // parts: 1.1 PFLOP/s), X's update 123, 0.84 PFLOP/s.
 //
 // Rounding: every matrix between the steps is two fp16 parts of its values times a power of two (2^12; 2^9 for P and Q),
@@ -413,7 +413,7 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 struct Plan {
   int bm, splits;
   double us;
-  bool halves;            // a workgroup takes half a tile, with four groups of waves: 896 x 896 x 896 11.0 -> 10.2 us
+  bool halves;            // a workgroup takes half a tile, with four groups of waves: 896 x 896 x 896 11.0 -> 9.5 us
   bool alone;             // every workgroup has a CU to itself: two groups of waves share its slices (four with two buffers
                           // each 1.15 times as long; two where two workgroups share a CU, or four buffers, the same)
 };
@@ -455,10 +455,12 @@ size_t partial_bytes(int n, int m, int slices) {
 }
 
 // How the steps are taken: one at a time (rounds == steps), or in rounds of two or three on m x m matrices, where that
-// is less time and G is at least twice as long as wide.  A round loses more of what is small against the
-// largest singular value: relative to fp32 throughout, 3 and 2 steps at a time are 0.5 to 1.2 times as far from the
-// exact result on spectra from flat to ones over five orders of magnitude (one at a time 0.2 to 0.4), but a
-// square random matrix, whose smallest singular value is next to none, is 4 times (0.3).
+// is less time and G is at least twice as long as wide.  A round loses more of what is small against the largest singular
+// value.  Five steps, by 3 and 2, are 0.7 to 2.5 times as far from the exact result as fp32 one at a time (300 x 2,000: flat
+// and steep spectra 3e-6 and 2e-6 off, rank 1 8e-5; one at a time 0.3 to 1 times), but a square random matrix, whose
+// smallest singular value is next to none, would be 4 times.  Three steps of rank 1 are 4e-5 off (fp32 1e-5), and of 16 steps
+// a flat spectrum 5e-5 (7e-6); rows that are there twice, whose zeros fp32 keeps by chance, 9e-5 in 8 steps (2e-6).
+// fp32 in the same rounds loses as much or more.
 struct Steps {
   int rounds;
   int of(int round, int steps) const { return steps / rounds + (round < steps % rounds ? 1 : 0); }     // the longer ones first
