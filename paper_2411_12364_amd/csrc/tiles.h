@@ -33,7 +33,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTileXcds = 8;
 constexpr int kTileBK = 64;             // K's slice: a row's 128 bytes
-constexpr int kMaxPairs = 6;
+constexpr int kMaxPairs = 3;            // three parts of an fp32 value, or three of the four of two values in two parts
 
 // The parts' pairs of a product.  Rows of ld elements (a multiple of 8), the first k of which count (a multiple of 8);
 // every row is 16-byte aligned.  a_rows, b_rows: the rows there are (reads stay below them).
